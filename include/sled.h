@@ -297,6 +297,90 @@ int sled_accept_rows_static(const float* logits, const int32_t* cu_rows, const i
 int sled_attention_ragged(sled_engine* e, int32_t layer, const uint64_t* ctx_ids, const int32_t* q_len,
                           int32_t n_reqs, const void* q, void* out, float* device_ms);
 
+/* ---- operators over a paged cache (device-resident operands) ------------------------- */
+
+/* A cache that the caller owns, in the layout of the engine's pool: K and V are [n_layers][n_pages][n_kv_heads][page_size]
+ * [head_dim], contiguous, 16-byte aligned; key x of request i lies in page page_table[i][x / page_size] at slot
+ * x % page_size, for every layer and KV head.  The paper leaves the cache to future work (Section 5); these operators are
+ * what a server needs of it beyond the chain drafts of sled_verify_batch.
+ *
+ * All arrays, the request descriptions included, are DEVICE memory of one GPU; the calls enqueue their kernels on `stream`
+ * (cudaStream_t or NULL for the default stream) and return without waiting, so they can be captured into a CUDA graph.
+ * The GPU that holds k is used, whichever device is current.  What the host can see is checked before anything is
+ * launched (SLED_ERR_ARG; SLED_ERR_NO_DEVICE without a GPU).  What only the GPU can see is checked by the kernels: a
+ * request whose numbers do not hold together - n_kv beyond its table row, fewer keys than rows, rows outside the call, a
+ * tree of more than SLED_MAX_TREE_NODES nodes - is left out; a page outside the pool is read as page 0 and never written
+ * (eviction leaves its request out), and a parent that is not an earlier node makes its node unused.  Each of these, and a device-side wait that runs out, sets *status (DEVICE,
+ * one int32, may be NULL) to the sled_status if it was 0; no call clears it.  Entries of a table row behind the request's
+ * last page, slots behind its last key and pages of nobody are never looked at, or do not change results whatever they
+ * hold.  A page belongs to at most one request of a call that writes to the cache or to key_weights.
+ * workspace: at least the bytes that the call's _workspace function names, 256-byte aligned, used from the call until its
+ * kernels have run: calls (or captured graphs) that may run at the same time need a workspace each.  It need not be
+ * cleared and nothing in it outlives the call. */
+#define SLED_MAX_TREE_NODES 128
+typedef struct sled_paged_kv {
+  void* k;
+  void* v;                    /* may be NULL for sled_block_bounds */
+  int32_t dtype;              /* sled_dtype of k and v, and of q, out and bounds */
+  int32_t n_layers;           /* 1, but for sled_evict_keys */
+  int32_t n_pages, n_kv_heads;
+  int32_t page_size;          /* a multiple of 16, at most 256 */
+  int32_t head_dim;           /* 32, 64 or 128 */
+  const int32_t* page_table;  /* [n_reqs] rows of table_cols entries, table_stride entries apart */
+  int32_t table_stride, table_cols;
+  const int32_t* n_kv;        /* [n_reqs] cached keys */
+  int32_t n_reqs;
+} sled_paged_kv;
+
+/* Attention of drafted trees.  Request i's newest cu_q[i+1] - cu_q[i] keys are the nodes of a tree of drafted tokens,
+ * parents before children; row cu_q[i] + j is node j.  It sees the request's older keys, itself and its ancestors.
+ * parents[cu_q[i] + j]: node j's parent as an index among the request's nodes, -1: it follows the older keys directly,
+ * -2: the node is unused - its row is 0 (lse -infinity) and nobody sees it, nor those that hang on it.  parents NULL: every request is a
+ * chain (row j sees the keys up to its own), of any length.  Softmax in fp32 over scale * q.k; scale 0: 1/sqrt(head_dim).
+ *   q, out  [n_rows][n_q_heads][head_dim], rows q_stride / out_stride elements apart (even numbers of bf16 elements,
+ *           4-byte aligned); rows that belong to no request are left alone
+ *   lse     [n_rows][n_q_heads] fp32: natural logarithm of the sum of exponentials; may be NULL
+ *   key_weights  may be NULL; [n_pages][n_kv_heads][page_size] fp32: every key's attention weight, summed over the
+ *           request's rows and the heads that share the KV head, is added to its entry */
+int64_t sled_attention_tree_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t weigh);
+int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride, const int32_t* cu_q, const int32_t* parents,
+                        int32_t n_rows, int32_t n_q_heads, float scale, void* out, int64_t out_stride, float* lse,
+                        float* key_weights, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Eviction by accumulated attention weight, in all layers at once.  Where request i has more than `budget` keys, every
+ * (layer, KV head) keeps for itself its first n_sink slots, its last n_recent and, of those between, the
+ * budget - n_sink - n_recent with the largest key_weights (the lower slot among equals; a NaN counts as the largest).
+ * They end up in the slots 0 .. budget-1: kept keys below budget - n_recent stay where they are, the places that became
+ * free there take the other kept ones, both in ascending order, and the last n_recent follow in their order.  The order of the
+ * older keys is of no consequence (a key carries its position).  Requests within the budget are left as they are.  The
+ * caller goes on with min(n_kv, budget) keys.
+ *   key_weights      [n_layers][n_pages][n_kv_heads][page_size] fp32
+ *   key_weights_out  the weights of the kept keys, at their new slots: key_weights itself, or an array that does not
+ *                    overlap it (then requests within the budget are copied, and slots behind the kept keys left alone) */
+int64_t sled_evict_keys_workspace(const sled_paged_kv* kv);
+int sled_evict_keys(const sled_paged_kv* kv, float* key_weights, float* key_weights_out, int32_t budget, int32_t n_sink,
+                    int32_t n_recent, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Smallest and largest key of every block (page), per KV head and dimension: bounds [n_pages][n_kv_heads][2][head_dim] of
+ * the cache's type, 16-byte aligned.  Written for the blocks that hold any of request i's keys first[i] .. n_kv[i]-1 (first
+ * NULL: all); a NaN among the keys gives NaN. */
+int sled_block_bounds(const sled_paged_kv* kv, const int32_t* first, void* bounds, int32_t* status, void* stream);
+
+/* Attention over the blocks that a cheap score selects for each query.  Chains as in sled_attention_tree without parents:
+ * row j of request i is the key x = n_kv[i] - q_len + j and sees no key behind it.  It reads the n_local blocks that end
+ * with its own and, of the earlier ones, the n_blocks - n_local of largest score - the largest, over the heads that share
+ * the KV head, of sum_d max(q_d low_d, q_d high_d), which no q.k of the block exceeds - the lower block among equals, a
+ * NaN being the largest.  Where there are no more than n_blocks blocks the result is that of full attention.
+ *   bounds  as sled_block_bounds leaves them, for every block before a query's last n_local
+ *   1 <= n_local <= n_blocks
+ *   blocks  may be NULL; [n_rows][n_kv_heads][n_blocks]: the blocks that were read, ascending; entries behind a row's own
+ *           block count are left alone */
+int64_t sled_attention_blocks_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks);
+int sled_attention_blocks(const sled_paged_kv* kv, const void* bounds, const void* q, int64_t q_stride, const int32_t* cu_q,
+                          int32_t n_rows, int32_t n_q_heads, float scale, int32_t n_blocks, int32_t n_local, void* out,
+                          int64_t out_stride, int32_t* blocks, int32_t* status, void* workspace, int64_t workspace_bytes,
+                          void* stream);
+
 /* ---- test and benchmark hooks ------------------------------------------------------- */
 
 /* Opens a context with given cache content instead of a prefill.  K, V: HOST or DEVICE,

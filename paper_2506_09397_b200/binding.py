@@ -34,6 +34,8 @@ EXPORTS = (
     "sled_server_config", "sled_submit", "sled_step", "sled_poll", "sled_queued",
     "sled_planner_create", "sled_planner_destroy", "sled_planner_push", "sled_planner_next_batch", "sled_planner_queued",
     "sled_debug_plan_attention",
+    "sled_attention_tree", "sled_attention_tree_workspace", "sled_evict_keys", "sled_evict_keys_workspace",
+    "sled_block_bounds", "sled_attention_blocks", "sled_attention_blocks_workspace",
 )
 
 
@@ -62,6 +64,13 @@ class SledRequest(C.Structure):
 
 class SledResult(C.Structure):
     _fields_ = [("n_accepted", C.c_int32), ("next_token", C.c_int32), ("status", C.c_int32)]
+
+
+class SledPagedKv(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int32) for n in (
+        "dtype", "n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim")] + [
+        ("page_table", C.c_void_p), ("table_stride", C.c_int32), ("table_cols", C.c_int32), ("n_kv", C.c_void_p),
+        ("n_reqs", C.c_int32)]
 
 
 class SledStats(C.Structure):
@@ -137,6 +146,14 @@ def lib():
             "sled_planner_next_batch": (I32, [P, I32, P, I32]),
             "sled_planner_queued": (I32, [P]),
             "sled_debug_plan_attention": (C.c_int, [P, P, I32, I32, I32, I32, C.c_int64, P]),
+            "sled_attention_tree_workspace": (I64, [C.POINTER(SledPagedKv), I32, I32, I32]),
+            "sled_attention_tree": (C.c_int, [C.POINTER(SledPagedKv), P, I64, P, P, I32, I32, F, P, I64, P, P, P, P, I64, P]),
+            "sled_evict_keys_workspace": (I64, [C.POINTER(SledPagedKv)]),
+            "sled_evict_keys": (C.c_int, [C.POINTER(SledPagedKv), P, P, I32, I32, I32, P, P, I64, P]),
+            "sled_block_bounds": (C.c_int, [C.POINTER(SledPagedKv), P, P, P, P]),
+            "sled_attention_blocks_workspace": (I64, [C.POINTER(SledPagedKv), I32, I32, I32]),
+            "sled_attention_blocks": (C.c_int, [C.POINTER(SledPagedKv), P, P, I64, P, I32, I32, F, I32, I32, P, I64, P, P, P,
+                                                I64, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -502,3 +519,166 @@ def plan_attention(n_keys, q_tokens, n_kv_heads: int, group: int, resident_block
     _check(lib().sled_debug_plan_attention(nk.ctypes.data, qt.ctypes.data, len(nk), n_kv_heads, group, resident_blocks,
                                            part_rows_cap, out.ctypes.data), "sled_debug_plan_attention")
     return [int(c) for c in out]
+
+
+# ---- operators over a paged cache: torch CUDA tensors in, enqueued on torch's current stream of the cache's device -----
+_TORCH_DT = {torch.float32: SLED_F32, torch.bfloat16: SLED_BF16}
+
+
+def _refuse(what: str, why: str):
+    raise SledError(SLED_ERR_ARG, f"{what} ({why})")
+
+
+def _ints(t, what: str, name: str, dev, shape=None):
+    """A CUDA int32 tensor that is contiguous along its last dimension; returns its address (0 for None)."""
+    if t is None:
+        return 0
+    if t.dtype != torch.int32 or t.device != dev or (t.numel() > 1 and t.stride(-1) != 1):
+        _refuse(what, f"{name} must be an int32 tensor on {dev}, contiguous along its last dimension")
+    if shape is not None and tuple(t.shape) != shape:
+        _refuse(what, f"{name} must have shape {shape}")
+    return t.data_ptr()
+
+
+def _floats(t, what: str, name: str, dev, shape):
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.device != dev or tuple(t.shape) != shape or not t.is_contiguous():
+        _refuse(what, f"{name} must be a contiguous fp32 tensor of shape {shape} on {dev}")
+    return t.data_ptr()
+
+
+def _paged(what: str, k, v, page_table, n_kv, layers: bool = False) -> SledPagedKv:
+    """The cache description of a call, from K, V [n_pages, n_kv_heads, page_size, head_dim] (with a leading n_layers
+    where the operator works on all layers), page_table [n_reqs, cols] and n_kv [n_reqs]."""
+    dev = k.device
+    if dev.type != "cuda":
+        raise SledError(SLED_ERR_NO_DEVICE, f"{what} (tensors must be on a CUDA device)")
+    if k.dtype not in _TORCH_DT or not (k.dim() == 4 or (layers and k.dim() == 5)):
+        _refuse(what, "the cache must be fp32 or bf16, [n_pages, n_kv_heads, page_size, head_dim]"
+                + (", with n_layers in front for all layers" if layers else ""))
+    for name, t in (("k", k), ("v", v)):
+        if t is not None and (t.dtype != k.dtype or t.device != dev or t.shape != k.shape or not t.is_contiguous()):
+            _refuse(what, f"{name} must be contiguous, and v like k")
+    if page_table.dim() != 2 or n_kv.dim() != 1 or n_kv.shape[0] != page_table.shape[0]:
+        _refuse(what, "page_table [n_reqs, cols] and n_kv [n_reqs]")
+    n_reqs, cols = page_table.shape
+    stride = page_table.stride(0) if n_reqs > 1 else cols
+    if stride < cols:
+        _refuse(what, "rows of page_table must not overlap")
+    n_pages, n_heads, page_size, head_dim = k.shape[-4:]
+    return SledPagedKv(k.data_ptr(), 0 if v is None else v.data_ptr(), _TORCH_DT[k.dtype], k.shape[0] if k.dim() == 5 else 1,
+                       n_pages, n_heads, page_size, head_dim, _ints(page_table, what, "page_table", dev), stride, cols,
+                       _ints(n_kv, what, "n_kv", dev), n_reqs)
+
+
+def _query_rows(what: str, q, out, k, n_reqs: int, cu_q):
+    """(out, row strides) of q [rows, n_q_heads, head_dim], whose rows may be apart (a slice of a wider projection)."""
+    if q.dim() != 3 or q.dtype != k.dtype or q.device != k.device or q.shape[2] != k.shape[-1]:
+        _refuse(what, "q must be [rows, n_q_heads, head_dim] of the cache's type and device")
+    if cu_q.shape != (n_reqs + 1,):
+        _refuse(what, "cu_q must be [n_reqs + 1]")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
+        _refuse(what, "out must be like q")
+    strides = []
+    for t in (q, out):
+        _, heads, h = t.shape
+        if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != h)):
+            _refuse(what, "a row of q and of out must be contiguous")
+        strides.append(t.stride(0) if t.shape[0] > 1 else heads * h)
+    return out, strides
+
+
+def _workspace(n_bytes: int, dev, what: str):
+    if n_bytes < 0:
+        raise SledError(int(n_bytes), what)
+    return torch.empty(n_bytes, dtype=torch.uint8, device=dev) if n_bytes else None
+
+
+def _stream_of(dev) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: float = 0.0, out=None, lse=None,
+                   key_weights=None, status=None):
+    """sled_attention_tree: attention of every request's newest keys, the nodes of a tree of drafted tokens, over its paged
+    cache.  q [rows, n_q_heads, head_dim]; k, v [n_pages, n_kv_heads, page_size, head_dim]; page_table [n_reqs, cols],
+    n_kv [n_reqs], cu_q [n_reqs + 1], parents [rows] int32 (None: chains).  Optional outputs: lse [rows, n_q_heads] fp32;
+    key_weights [n_pages, n_kv_heads, page_size] fp32, added to.  status: one int32 that receives what the kernels found
+    wrong (see check_status).  Enqueued on torch's current stream; returns out."""
+    what = "sled_attention_tree"
+    kv = _paged(what, k, v, page_table, n_kv)
+    dev = k.device
+    out, (qs, os_) = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
+    rows, heads = q.shape[:2]
+    ws = _workspace(lib().sled_attention_tree_workspace(C.byref(kv), rows, heads, int(key_weights is not None)), dev, what)
+    _check(lib().sled_attention_tree(
+        C.byref(kv), q.data_ptr(), qs, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
+        scale, out.data_ptr(), os_, _floats(lse, what, "lse", dev, (rows, heads)),
+        _floats(key_weights, what, "key_weights", dev, tuple(k.shape[:3])), _ints(status, what, "status", dev),
+        ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0, _stream_of(dev)), what)
+    return out
+
+
+def evict_keys(k, v, key_weights, page_table, n_kv, budget: int, *, n_sink: int = 0, n_recent: int = 0, key_weights_out=None,
+               status=None) -> None:
+    """sled_evict_keys: every (layer, KV head) of a request with more than `budget` keys keeps its n_sink first, its n_recent
+    last and those of largest key_weights.  k, v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (or one layer without
+    the first dimension), changed in place; key_weights [n_layers, n_pages, n_kv_heads, page_size] fp32, changed in place
+    unless key_weights_out is given.  The caller goes on with min(n_kv, budget) keys."""
+    what = "sled_evict_keys"
+    kv = _paged(what, k, v, page_table, n_kv, layers=True)
+    dev = k.device
+    ws = _workspace(lib().sled_evict_keys_workspace(C.byref(kv)), dev, what)
+    w = _floats(key_weights, what, "key_weights", dev, tuple(k.shape[:-1]))
+    w_out = _floats(key_weights_out, what, "key_weights_out", dev, tuple(k.shape[:-1])) or w
+    _check(lib().sled_evict_keys(C.byref(kv), w, w_out, budget, n_sink, n_recent, _ints(status, what, "status", dev),
+                                 ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0, _stream_of(dev)), what)
+
+
+def block_bounds(k, page_table, n_kv, bounds, *, first=None, status=None) -> None:
+    """sled_block_bounds: smallest and largest key of every page, into bounds [n_pages, n_kv_heads, 2, head_dim] of the
+    cache's type, for the pages that hold request i's keys first[i] .. n_kv[i]-1 (first None: all)."""
+    what = "sled_block_bounds"
+    kv = _paged(what, k, None, page_table, n_kv)
+    dev = k.device
+    _check_bounds(what, bounds, k)
+    _check(lib().sled_block_bounds(C.byref(kv), _ints(first, what, "first", dev, (kv.n_reqs,)), bounds.data_ptr(),
+                                   _ints(status, what, "status", dev), _stream_of(dev)), what)
+
+
+def _check_bounds(what: str, bounds, k) -> None:
+    if bounds.dtype != k.dtype or bounds.device != k.device or not bounds.is_contiguous() or \
+            tuple(bounds.shape) != (k.shape[0], k.shape[1], 2, k.shape[3]):
+        _refuse(what, "bounds must be contiguous [n_pages, n_kv_heads, 2, head_dim] of the cache's type and device")
+
+
+def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, n_local: int = 1, scale: float = 0.0, out=None,
+                     blocks=None, status=None):
+    """sled_attention_blocks: causal attention of every request's newest keys over the n_local last blocks (pages) and the
+    n_blocks - n_local earlier ones of largest score for the query.  bounds as block_bounds leaves them; blocks (optional)
+    [rows, n_kv_heads, n_blocks] int32 receives what was read.  Enqueued on torch's current stream; returns out."""
+    what = "sled_attention_blocks"
+    kv = _paged(what, k, v, page_table, n_kv)
+    dev = k.device
+    _check_bounds(what, bounds, k)
+    out, (qs, os_) = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
+    rows, heads = q.shape[:2]
+    ws = _workspace(lib().sled_attention_blocks_workspace(C.byref(kv), rows, heads, n_blocks), dev, what)
+    if blocks is not None and not blocks.is_contiguous():
+        _refuse(what, "blocks must be contiguous")
+    _check(lib().sled_attention_blocks(
+        C.byref(kv), bounds.data_ptr(), q.data_ptr(), qs, _ints(cu_q, what, "cu_q", dev), rows, heads, scale, n_blocks, n_local,
+        out.data_ptr(), os_, _ints(blocks, what, "blocks", dev, (rows, kv.n_kv_heads, n_blocks)),
+        _ints(status, what, "status", dev), ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0,
+        _stream_of(dev)), what)
+    return out
+
+
+def check_status(status) -> None:
+    """Waits for the operators that were given `status` and raises what they found wrong."""
+    code = int(status.reshape(-1)[0].item())
+    if code != SLED_OK:
+        raise SledError(code, "operator over a paged cache")

@@ -1,0 +1,57 @@
+// Operators over a caller's paged key-value cache (device-resident operands): launchers shared by the C entry points
+// (paged_api.cu).  Every launcher only enqueues work on the given stream and returns the number of kernels it launched
+// (negative: the launch failed).
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace sled {
+
+// One layer of a cache and what every request owns of it.  All pointers are device pointers.  The kernels check every
+// entry that they follow: a request whose description does not hold together (lengths that do not fit its table row,
+// rows outside the call, a page outside the pool, a parent that is not an earlier node) is left out and reported in
+// `status`; it never leads outside the arrays.
+struct PagedCache {
+  const char* k;
+  const char* v;
+  int dtype;                  // DType of K and V
+  int n_layers, n_pages, Hkv, ps, h;
+  int64_t layer_bytes;        // distance between layers (eviction)
+  const int32_t* table;       // [n_reqs][table_stride], table_cols entries of a row belong to the request
+  int table_stride, table_cols;
+  const int32_t* n_kv;        // [n_reqs]
+  int n_reqs;
+  int32_t* status;            // one word or null; receives a negative sled_status
+};
+
+// The queries of a call: request i owns rows cu_q[i] .. cu_q[i+1]-1, its newest keys' tokens.
+struct PagedRows {
+  const int32_t* cu_q;
+  const int32_t* parents;     // null: a chain
+  const char* q;              // [T][Hq][h], rows q_stride elements apart
+  char* out;
+  float* lse;                 // [T][Hq] natural logarithm, or null
+  int64_t q_stride, out_stride;
+  int T, Hq;
+  float scale;
+};
+
+// Attention of the rows over everything they see (list null) or over the blocks list[t][kv head][list_len], ascending,
+// min(list_len, own block + 1) of them.  key_weights (optional, needs r.lse): [n_pages][Hkv][ps], added to.
+int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, int n_local,
+                           float* key_weights, cudaStream_t s);
+// bounds[page][Hkv][2][h] of the pages that hold the keys first[i] .. n_kv[i]-1 (first null: all keys)
+int launch_block_bounds(const PagedCache& c, const int32_t* first, void* bounds, cudaStream_t s);
+// the blocks of every (row, KV head), ascending, into list [T][Hkv][n_blocks]; scores: room for [T][Hkv][table_cols]
+int launch_block_choice(const PagedCache& c, const PagedRows& r, const void* bounds, int n_blocks, int n_local, float* scores,
+                        int32_t* list, cudaStream_t s);
+// weights, weights_out: [n_layers][n_pages][Hkv][ps], the same array or disjoint ones; pairs: room for
+// [n_layers][n_reqs][Hkv][table_cols * ps]
+int launch_evict(const PagedCache& c, float* weights, float* weights_out, int64_t weight_layer, int budget, int n_sink, int n_recent,
+                 int32_t* pairs, cudaStream_t s);
+
+constexpr int kMaxTreeNodes = 128;   // nodes of one request's tree (chains have no limit)
+
+}  // namespace sled

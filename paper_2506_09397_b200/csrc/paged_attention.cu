@@ -1,0 +1,157 @@
+// Attention of a batch's newest tokens over a paged cache: a tree (or chain) of tokens per request, optionally with the
+// attention weight of every cached key added up, or over the blocks of the cache that were chosen per query.
+//
+// For a query row r (token, head) and the keys x it sees: s_x = scale q.k_x, p_x = exp(s_x - lse), lse = ln sum exp s_x,
+// o = sum p_x v_x.  One pass over the keys with the running maximum and sum; a row that sees nothing gets o = 0 and
+// lse = -inf.
+#include "paged_device.cuh"
+
+namespace sled {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// One block of four warps per (token, head); warp w takes every fourth key, the lanes share the head dimension.
+template <typename T, int H>
+__global__ void __launch_bounds__(128) attn_row_kernel(PagedCache c, PagedRows r, const int32_t* list, int list_len, int n_local) {
+  constexpr int D = H / 32;
+  const int t = blockIdx.x, head = blockIdx.y;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (t == 0 && head == 0)   // one block reports the requests that are left out
+    for (int b = threadIdx.x; b < c.n_reqs; b += blockDim.x) {
+      const ReqView w = req_view(c, r, b);
+      if (!w.ok) set_status(c.status, req_fault(r, w));
+    }
+  const int i = req_of_row(r.cu_q, c.n_reqs, t);
+  const ReqView v = req_view(c, r, i);
+  if (!v.ok) return;
+  const int j = t - v.row0;
+  if (j < 0 || j >= v.m) return;   // rows behind the last request
+  const int g = head / (r.Hq / c.Hkv), prefix = v.n - v.m;
+  uint32_t bits[kMaxTreeNodes / 32] = {};
+  if (r.parents) ancestors_of(r.parents + v.row0, j, bits, warp == 0 && lane == 0 ? c.status : nullptr);
+  bool none = r.parents != nullptr;
+  for (int w = 0; w < kMaxTreeNodes / 32; ++w) none = none && bits[w] == 0;
+  const T* q = reinterpret_cast<const T*>(r.q) + t * r.q_stride + static_cast<int64_t>(head) * H + lane * D;
+  float qf[D], o[D];
+#pragma unroll
+  for (int d = 0; d < D; ++d) { qf[d] = to_f32(q[d]); o[d] = 0.f; }
+  float m = -INFINITY, l = 0.f;
+  const int32_t* table = c.table + static_cast<int64_t>(i) * c.table_stride;
+  const int last = r.parents ? v.n - 1 : prefix + j;   // no key behind this one is seen
+  const int own = last / c.ps;
+  const int n_here = list ? min(list_len, own + 1) * c.ps : last + 1;
+  const int32_t* mine = list ? list + (static_cast<int64_t>(t) * c.Hkv + g) * list_len : nullptr;
+  for (int e = warp; e < n_here && !none; e += 4) {
+    const int x = list ? mine[e / c.ps] * c.ps + e % c.ps : e;
+    if (x > last) continue;
+    if (r.parents && x >= prefix) {
+      const int a = x - prefix;
+      if (!((bits[a >> 5] >> (a & 31)) & 1u)) continue;
+    }
+    const int page = checked_page(c, table[x / c.ps]);
+    const int64_t at = ((static_cast<int64_t>(page) * c.Hkv + g) * c.ps + x % c.ps) * H + lane * D;
+    const T* k = reinterpret_cast<const T*>(c.k) + at;
+    const T* vv = reinterpret_cast<const T*>(c.v) + at;
+    float s = 0.f;
+#pragma unroll
+    for (int d = 0; d < D; ++d) s = fmaf(qf[d], to_f32(k[d]), s);
+    s = warp_sum(s) * r.scale * kLog2e;
+    const float mn = fmaxf(m, s);
+    if (s == -INFINITY && mn == -INFINITY) continue;   // nothing but infinitely small scores so far
+    const float al = exp2f(m - mn), p = exp2f(s - mn);
+    l = l * al + p;
+#pragma unroll
+    for (int d = 0; d < D; ++d) o[d] = fmaf(p, to_f32(vv[d]), o[d] * al);
+    m = mn;
+  }
+  __shared__ float so[4][H], sm[4], sl[4];
+#pragma unroll
+  for (int d = 0; d < D; ++d) so[warp][lane * D + d] = o[d];
+  if (lane == 0) { sm[warp] = m; sl[warp] = l; }
+  __syncthreads();
+  float M = -INFINITY;
+  bool nan = false;
+  for (int w = 0; w < 4; ++w) { M = fmaxf(M, sm[w]); nan |= sl[w] != sl[w]; }
+  float den = 0.f;
+  for (int w = 0; w < 4; ++w) den += sm[w] == -INFINITY ? 0.f : exp2f(sm[w] - M) * sl[w];
+  for (int d = threadIdx.x; d < H; d += 128) {
+    float num = 0.f;
+    for (int w = 0; w < 4; ++w) num += sm[w] == -INFINITY ? 0.f : exp2f(sm[w] - M) * so[w][d];
+    reinterpret_cast<T*>(r.out)[t * r.out_stride + static_cast<int64_t>(head) * H + d] =
+        from_f32<T>(M == -INFINITY && !nan ? 0.f : num / den);
+  }
+  if (threadIdx.x == 0 && r.lse)
+    r.lse[static_cast<int64_t>(t) * r.Hq + head] = M == -INFINITY && !nan ? -INFINITY : (M + log2f(den)) * kLn2;
+}
+
+// Adds every key's attention weight: one block per (page of a request, KV head), a warp takes every fourth key of the
+// page and goes through the rows in order.
+template <typename T, int H>
+__global__ void __launch_bounds__(128) key_weight_kernel(PagedCache c, PagedRows r, float* key_weights) {
+  constexpr int D = H / 32;
+  const int i = blockIdx.z, g = blockIdx.y, group = r.Hq / c.Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const ReqView v = req_view(c, r, i);
+  const int x0 = blockIdx.x * c.ps;
+  if (!v.ok || v.m == 0 || x0 >= v.n) return;
+  const int prefix = v.n - v.m;
+  const int page = c.table[static_cast<int64_t>(i) * c.table_stride + blockIdx.x];
+  if (!page_exists(c, page)) return;   // reported by the attention kernel
+  for (int e = warp; e < c.ps && x0 + e < v.n; e += 4) {
+    const int x = x0 + e;
+    const int64_t at = (static_cast<int64_t>(page) * c.Hkv + g) * c.ps + e;
+    const T* k = reinterpret_cast<const T*>(c.k) + at * H + lane * D;
+    float sum = 0.f;
+    for (int j = 0; j < v.m; ++j) {
+      if (!r.parents && x > prefix + j) continue;
+      if (r.parents && x >= prefix) {
+        uint32_t bits[kMaxTreeNodes / 32];
+        ancestors_of(r.parents + v.row0, j, bits, nullptr);
+        if (!((bits[(x - prefix) >> 5] >> ((x - prefix) & 31)) & 1u)) continue;
+      }
+      for (int hh = 0; hh < group; ++hh) {
+        const int head = g * group + hh, t = v.row0 + j;
+        const float lse = r.lse[static_cast<int64_t>(t) * r.Hq + head];
+        const T* q = reinterpret_cast<const T*>(r.q) + t * r.q_stride + static_cast<int64_t>(head) * H + lane * D;
+        float s = 0.f;
+#pragma unroll
+        for (int d = 0; d < D; ++d) s = fmaf(to_f32(q[d]), to_f32(k[d]), s);
+        s = warp_sum(s) * r.scale;
+        if (lse != -INFINITY) sum += exp2f((s - lse) * kLog2e);
+      }
+    }
+    if (lane == 0) key_weights[at] += sum;
+  }
+}
+
+template <typename T, int H>
+int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, int n_local, float* key_weights, cudaStream_t s) {
+  attn_row_kernel<T, H><<<dim3(r.T, r.Hq), 128, 0, s>>>(c, r, list, list_len, n_local);
+  int n = 1;
+  if (key_weights) {
+    key_weight_kernel<T, H><<<dim3(c.table_cols, c.Hkv, c.n_reqs), 128, 0, s>>>(c, r, key_weights);
+    ++n;
+  }
+  return cudaGetLastError() == cudaSuccess ? n : -1;
+}
+
+}  // namespace
+
+int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, int n_local,
+                           float* key_weights, cudaStream_t s) {
+  if (c.dtype == 1) {
+    if (c.h == 32) return launch_rows<__nv_bfloat16, 32>(c, r, list, list_len, n_local, key_weights, s);
+    if (c.h == 64) return launch_rows<__nv_bfloat16, 64>(c, r, list, list_len, n_local, key_weights, s);
+    if (c.h == 128) return launch_rows<__nv_bfloat16, 128>(c, r, list, list_len, n_local, key_weights, s);
+  } else {
+    if (c.h == 32) return launch_rows<float, 32>(c, r, list, list_len, n_local, key_weights, s);
+    if (c.h == 64) return launch_rows<float, 64>(c, r, list, list_len, n_local, key_weights, s);
+    if (c.h == 128) return launch_rows<float, 128>(c, r, list, list_len, n_local, key_weights, s);
+  }
+  return -1;
+}
+
+}  // namespace sled
