@@ -342,7 +342,7 @@ typedef struct sled_paged_kv {
  *   lse     [n_rows][n_q_heads] fp32: natural logarithm of the sum of exponentials; may be NULL
  *   key_weights  may be NULL; [n_pages][n_kv_heads][page_size] fp32: every key's attention weight, summed over the
  *           request's rows and the heads that share the KV head, is added to its entry */
-int64_t sled_attention_tree_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t weigh);
+int sled_attention_tree_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t weigh, int64_t* bytes);
 int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride, const int32_t* cu_q, const int32_t* parents,
                         int32_t n_rows, int32_t n_q_heads, float scale, void* out, int64_t out_stride, float* lse,
                         float* key_weights, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
@@ -357,7 +357,7 @@ int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride
  *   key_weights      [n_layers][n_pages][n_kv_heads][page_size] fp32
  *   key_weights_out  the weights of the kept keys, at their new slots: key_weights itself, or an array that does not
  *                    overlap it (then requests within the budget are copied, and slots behind the kept keys left alone) */
-int64_t sled_evict_keys_workspace(const sled_paged_kv* kv);
+int sled_evict_keys_workspace(const sled_paged_kv* kv, int64_t* bytes);
 int sled_evict_keys(const sled_paged_kv* kv, float* key_weights, float* key_weights_out, int32_t budget, int32_t n_sink,
                     int32_t n_recent, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
 
@@ -375,7 +375,7 @@ int sled_block_bounds(const sled_paged_kv* kv, const int32_t* first, void* bound
  *   1 <= n_local <= n_blocks
  *   blocks  may be NULL; [n_rows][n_kv_heads][n_blocks]: the blocks that were read, ascending; entries behind a row's own
  *           block count are left alone */
-int64_t sled_attention_blocks_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks);
+int sled_attention_blocks_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks, int64_t* bytes);
 int sled_attention_blocks(const sled_paged_kv* kv, const void* bounds, const void* q, int64_t q_stride, const int32_t* cu_q,
                           int32_t n_rows, int32_t n_q_heads, float scale, int32_t n_blocks, int32_t n_local, void* out,
                           int64_t out_stride, int32_t* blocks, int32_t* status, void* workspace, int64_t workspace_bytes,

@@ -146,12 +146,12 @@ def lib():
             "sled_planner_next_batch": (I32, [P, I32, P, I32]),
             "sled_planner_queued": (I32, [P]),
             "sled_debug_plan_attention": (C.c_int, [P, P, I32, I32, I32, I32, C.c_int64, P]),
-            "sled_attention_tree_workspace": (I64, [C.POINTER(SledPagedKv), I32, I32, I32]),
+            "sled_attention_tree_workspace": (C.c_int, [C.POINTER(SledPagedKv), I32, I32, I32, C.POINTER(I64)]),
             "sled_attention_tree": (C.c_int, [C.POINTER(SledPagedKv), P, I64, P, P, I32, I32, F, P, I64, P, P, P, P, I64, P]),
-            "sled_evict_keys_workspace": (I64, [C.POINTER(SledPagedKv)]),
+            "sled_evict_keys_workspace": (C.c_int, [C.POINTER(SledPagedKv), C.POINTER(I64)]),
             "sled_evict_keys": (C.c_int, [C.POINTER(SledPagedKv), P, P, I32, I32, I32, P, P, I64, P]),
             "sled_block_bounds": (C.c_int, [C.POINTER(SledPagedKv), P, P, P, P]),
-            "sled_attention_blocks_workspace": (I64, [C.POINTER(SledPagedKv), I32, I32, I32]),
+            "sled_attention_blocks_workspace": (C.c_int, [C.POINTER(SledPagedKv), I32, I32, I32, C.POINTER(I64)]),
             "sled_attention_blocks": (C.c_int, [C.POINTER(SledPagedKv), P, P, I64, P, I32, I32, F, I32, I32, P, I64, P, P, P,
                                                 I64, P]),
         }
@@ -591,10 +591,14 @@ def _query_rows(what: str, q, out, k, n_reqs: int, cu_q):
     return out, strides
 
 
-def _workspace(n_bytes: int, dev, what: str):
-    if n_bytes < 0:
-        raise SledError(int(n_bytes), what)
-    return torch.empty(n_bytes, dtype=torch.uint8, device=dev) if n_bytes else None
+def _workspace(what: str, dev, kv, *sizes):
+    """(tensor to be kept until the call has been made, address, bytes) of the workspace that the call asks for."""
+    n = C.c_int64()
+    _check(getattr(lib(), what + "_workspace")(C.byref(kv), *sizes, C.byref(n)), what)
+    if not n.value:
+        return None, 0, 0
+    t = torch.empty(n.value, dtype=torch.uint8, device=dev)
+    return t, t.data_ptr(), n.value
 
 
 def _stream_of(dev) -> int:
@@ -613,12 +617,12 @@ def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: floa
     dev = k.device
     out, (qs, os_) = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
     rows, heads = q.shape[:2]
-    ws = _workspace(lib().sled_attention_tree_workspace(C.byref(kv), rows, heads, int(key_weights is not None)), dev, what)
+    _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, int(key_weights is not None))
     _check(lib().sled_attention_tree(
         C.byref(kv), q.data_ptr(), qs, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
         scale, out.data_ptr(), os_, _floats(lse, what, "lse", dev, (rows, heads)),
         _floats(key_weights, what, "key_weights", dev, tuple(k.shape[:3])), _ints(status, what, "status", dev),
-        ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0, _stream_of(dev)), what)
+        ws, ws_bytes, _stream_of(dev)), what)
     return out
 
 
@@ -631,11 +635,11 @@ def evict_keys(k, v, key_weights, page_table, n_kv, budget: int, *, n_sink: int 
     what = "sled_evict_keys"
     kv = _paged(what, k, v, page_table, n_kv, layers=True)
     dev = k.device
-    ws = _workspace(lib().sled_evict_keys_workspace(C.byref(kv)), dev, what)
+    _held, ws, ws_bytes = _workspace(what, dev, kv)
     w = _floats(key_weights, what, "key_weights", dev, tuple(k.shape[:-1]))
     w_out = _floats(key_weights_out, what, "key_weights_out", dev, tuple(k.shape[:-1])) or w
     _check(lib().sled_evict_keys(C.byref(kv), w, w_out, budget, n_sink, n_recent, _ints(status, what, "status", dev),
-                                 ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0, _stream_of(dev)), what)
+                                 ws, ws_bytes, _stream_of(dev)), what)
 
 
 def block_bounds(k, page_table, n_kv, bounds, *, first=None, status=None) -> None:
@@ -666,13 +670,13 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
     _check_bounds(what, bounds, k)
     out, (qs, os_) = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
     rows, heads = q.shape[:2]
-    ws = _workspace(lib().sled_attention_blocks_workspace(C.byref(kv), rows, heads, n_blocks), dev, what)
+    _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, n_blocks)
     if blocks is not None and not blocks.is_contiguous():
         _refuse(what, "blocks must be contiguous")
     _check(lib().sled_attention_blocks(
         C.byref(kv), bounds.data_ptr(), q.data_ptr(), qs, _ints(cu_q, what, "cu_q", dev), rows, heads, scale, n_blocks, n_local,
         out.data_ptr(), os_, _ints(blocks, what, "blocks", dev, (rows, kv.n_kv_heads, n_blocks)),
-        _ints(status, what, "status", dev), ws.data_ptr() if ws is not None else 0, ws.numel() if ws is not None else 0,
+        _ints(status, what, "status", dev), ws, ws_bytes,
         _stream_of(dev)), what)
     return out
 

@@ -128,13 +128,24 @@ int64_t list_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_blocks) {
   return align256(static_cast<int64_t>(n_rows) * kv->n_kv_heads * n_blocks * 4);
 }
 
+int64_t tree_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, bool weigh) {
+  return weigh ? lse_bytes(n_rows, n_q_heads) : 0;
+}
+int64_t blocks_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_blocks) {
+  return list_bytes(kv, n_rows, n_blocks) + list_bytes(kv, n_rows, kv->table_cols);
+}
+int64_t evict_bytes(const sled_paged_kv* kv) {
+  return align256(static_cast<int64_t>(kv->n_layers) * kv->n_reqs * kv->n_kv_heads * kv->table_cols * kv->page_size * 4);
+}
+
 }  // namespace
 
 extern "C" {
 
-int64_t sled_attention_tree_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t weigh) {
-  if (check_cache(kv, true, false) || n_rows < 0 || n_q_heads < 1) return SLED_ERR_ARG;
-  return weigh ? lse_bytes(n_rows, n_q_heads) : 0;
+int sled_attention_tree_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t weigh, int64_t* bytes) {
+  if (check_cache(kv, true, false) || n_rows < 0 || n_q_heads < 1 || !bytes) return SLED_ERR_ARG;
+  *bytes = tree_bytes(kv, n_rows, n_q_heads, weigh != 0);
+  return SLED_OK;
 }
 
 int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride, const int32_t* cu_q, const int32_t* parents,
@@ -143,7 +154,7 @@ int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride
   int rc = check_cache(kv, true, false);
   if (!rc) rc = check_rows(kv, q, q_stride, cu_q, n_rows, n_q_heads, scale, out, out_stride);
   if (!rc && (!aligned(parents, 4) || !aligned(lse, 4) || !aligned(key_weights, 4) || !aligned(status, 4))) rc = SLED_ERR_ARG;
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, sled_attention_tree_workspace(kv, n_rows, n_q_heads, key_weights != nullptr));
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, tree_bytes(kv, n_rows, n_q_heads, key_weights != nullptr));
   if (rc) return rc;
   if (n_rows == 0 || kv->n_reqs == 0) return SLED_OK;
   OnDeviceOf device(kv->k);
@@ -155,9 +166,10 @@ int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride
   return done(launch_paged_attention(c, r, nullptr, 0, 0, key_weights, static_cast<cudaStream_t>(stream)), "sled_attention_tree");
 }
 
-int64_t sled_evict_keys_workspace(const sled_paged_kv* kv) {
-  if (check_cache(kv, true, true)) return SLED_ERR_ARG;
-  return align256(static_cast<int64_t>(kv->n_layers) * kv->n_reqs * kv->n_kv_heads * kv->table_cols * kv->page_size * 4);
+int sled_evict_keys_workspace(const sled_paged_kv* kv, int64_t* bytes) {
+  if (check_cache(kv, true, true) || !bytes) return SLED_ERR_ARG;
+  *bytes = evict_bytes(kv);
+  return SLED_OK;
 }
 
 int sled_evict_keys(const sled_paged_kv* kv, float* key_weights, float* key_weights_out, int32_t budget, int32_t n_sink,
@@ -169,7 +181,7 @@ int sled_evict_keys(const sled_paged_kv* kv, float* key_weights, float* key_weig
     return SLED_ERR_ARG;
   if (!aligned(key_weights, 4) || !aligned(key_weights_out, 4) || !aligned(status, 4)) return SLED_ERR_ARG;
   if (!same_or_apart(key_weights, key_weights_out, per_layer * kv->n_layers * 4)) return SLED_ERR_ARG;
-  rc = check_workspace(workspace, workspace_bytes, sled_evict_keys_workspace(kv));
+  rc = check_workspace(workspace, workspace_bytes, evict_bytes(kv));
   if (rc) return rc;
   if (kv->n_reqs == 0 || kv->table_cols == 0) return SLED_OK;
   OnDeviceOf device(kv->k);
@@ -188,9 +200,10 @@ int sled_block_bounds(const sled_paged_kv* kv, const int32_t* first, void* bound
   return done(launch_block_bounds(cache_of(kv, status), first, bounds, static_cast<cudaStream_t>(stream)), "sled_block_bounds");
 }
 
-int64_t sled_attention_blocks_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks) {
-  if (check_cache(kv, true, false) || n_rows < 0 || n_q_heads < 1 || n_blocks < 1) return SLED_ERR_ARG;
-  return list_bytes(kv, n_rows, n_blocks) + list_bytes(kv, n_rows, kv->table_cols);
+int sled_attention_blocks_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks, int64_t* bytes) {
+  if (check_cache(kv, true, false) || n_rows < 0 || n_q_heads < 1 || n_blocks < 1 || !bytes) return SLED_ERR_ARG;
+  *bytes = blocks_bytes(kv, n_rows, n_blocks);
+  return SLED_OK;
 }
 
 int sled_attention_blocks(const sled_paged_kv* kv, const void* bounds, const void* q, int64_t q_stride, const int32_t* cu_q,
@@ -199,7 +212,7 @@ int sled_attention_blocks(const sled_paged_kv* kv, const void* bounds, const voi
   int rc = check_cache(kv, true, false);
   if (!rc) rc = check_rows(kv, q, q_stride, cu_q, n_rows, n_q_heads, scale, out, out_stride);
   if (!rc && (!bounds || !aligned(bounds, 16) || !aligned(blocks, 4) || !aligned(status, 4) || n_local < 1 || n_blocks < n_local)) rc = SLED_ERR_ARG;
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, sled_attention_blocks_workspace(kv, n_rows, n_q_heads, n_blocks));
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, blocks_bytes(kv, n_rows, n_blocks));
   if (rc) return rc;
   if (n_rows == 0 || kv->n_reqs == 0) return SLED_OK;
   OnDeviceOf device(kv->k);

@@ -20,6 +20,12 @@ def _tree(kv, *, q=4096, q_stride=256, cu=256, parents=0, rows=4, heads=4, scale
                                        lse, weights, status, ws, ws_bytes, 0)
 
 
+def _bytes(what, *args):
+    n = C.c_int64(-1)
+    assert getattr(B.lib(), what + "_workspace")(*args, C.byref(n)) == B.SLED_OK
+    return n.value
+
+
 BAD_CACHES = [dict(k=0), dict(k=4100), dict(v=8200), dict(dtype=2), dict(head_dim=96), dict(head_dim=0), dict(page_size=8),
               dict(page_size=24), dict(page_size=512), dict(page_size=0), dict(n_layers=0), dict(n_pages=0), dict(n_kv_heads=0),
               dict(n_reqs=-1), dict(table_cols=-1), dict(table_stride=4), dict(page_table=0), dict(n_kv=0), dict(n_kv=513),
@@ -30,11 +36,11 @@ BAD_CACHES = [dict(k=0), dict(k=4100), dict(v=8200), dict(dtype=2), dict(head_di
 def test_bad_caches_are_refused_by_every_operator(change):
     kv = _kv(**change)
     assert _tree(kv, ws=256, ws_bytes=1 << 60) == B.SLED_ERR_ARG
-    assert B.lib().sled_attention_tree_workspace(C.byref(kv), 4, 4, 0) == B.SLED_ERR_ARG
+    assert B.lib().sled_attention_tree_workspace(C.byref(kv), 4, 4, 0, C.byref(C.c_int64())) == B.SLED_ERR_ARG
     assert B.lib().sled_evict_keys(C.byref(kv), 256, 256, 32, 1, 1, 0, 256, 1 << 60, 0) == B.SLED_ERR_ARG
-    assert B.lib().sled_evict_keys_workspace(C.byref(kv)) == B.SLED_ERR_ARG
+    assert B.lib().sled_evict_keys_workspace(C.byref(kv), C.byref(C.c_int64())) == B.SLED_ERR_ARG
     assert B.lib().sled_attention_blocks(C.byref(kv), 256, 4096, 256, 256, 4, 4, 0.0, 4, 1, 4096, 256, 0, 0, 256, 1 << 60, 0) == B.SLED_ERR_ARG
-    assert B.lib().sled_attention_blocks_workspace(C.byref(kv), 4, 4, 4) == B.SLED_ERR_ARG
+    assert B.lib().sled_attention_blocks_workspace(C.byref(kv), 4, 4, 4, C.byref(C.c_int64())) == B.SLED_ERR_ARG
     if "v" not in change:
         assert B.lib().sled_block_bounds(C.byref(kv), 0, 256, 0, 0) == B.SLED_ERR_ARG
 
@@ -59,7 +65,7 @@ def test_a_layer_dimension_is_refused_where_it_means_nothing():
     assert _tree(kv, ws=256, ws_bytes=1 << 60) == B.SLED_ERR_ARG
     assert B.lib().sled_block_bounds(C.byref(kv), 0, 256, 0, 0) == B.SLED_ERR_ARG
     assert B.lib().sled_attention_blocks(C.byref(kv), 256, 4096, 256, 256, 4, 4, 0.0, 4, 1, 4096, 256, 0, 0, 256, 1 << 60, 0) == B.SLED_ERR_ARG
-    assert B.lib().sled_evict_keys_workspace(C.byref(kv)) > 0
+    assert _bytes("sled_evict_keys", C.byref(kv)) > 0
 
 
 @pytest.mark.parametrize("budget,sink,recent,w,w_out", [(0, 0, 0, 256, 256), (-5, 0, 0, 256, 256), (8, -1, 0, 256, 256), (8, 0, -1, 256, 256),
@@ -79,14 +85,14 @@ def test_bad_block_choices_are_refused(n_blocks, n_local, bounds, blocks):
 
 def test_workspaces_that_are_too_small_or_crooked_are_refused():
     kv = _kv()
-    need = B.lib().sled_attention_tree_workspace(C.byref(kv), 4, 4, 1)
+    need = _bytes("sled_attention_tree", C.byref(kv), 4, 4, 1)
     assert need > 0
     for ws, have in ((0, need), (256, need - 1), (264, need)):
         assert _tree(kv, weights=256, ws=ws, ws_bytes=have) == B.SLED_ERR_ARG
-    need = B.lib().sled_evict_keys_workspace(C.byref(kv))
+    need = _bytes("sled_evict_keys", C.byref(kv))
     for ws, have in ((0, need), (256, need - 1), (264, need)):
         assert B.lib().sled_evict_keys(C.byref(kv), 256, 256, 32, 1, 1, 0, ws, have, 0) == B.SLED_ERR_ARG
-    need = B.lib().sled_attention_blocks_workspace(C.byref(kv), 4, 4, 4)
+    need = _bytes("sled_attention_blocks", C.byref(kv), 4, 4, 4)
     for ws, have in ((0, need), (256, need - 1), (264, need)):
         assert B.lib().sled_attention_blocks(C.byref(kv), 256, 4096, 256, 256, 4, 4, 0.0, 4, 1, 4096, 256, 0, 0, ws, have, 0) == B.SLED_ERR_ARG
 
