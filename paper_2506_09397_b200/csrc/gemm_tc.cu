@@ -931,6 +931,23 @@ int tma_map_bf16_rows(CUtensorMap* map, const void* dev_ptr, long long rows, int
   return make_map(map, dev_ptr, rows, cols, box_rows);
 }
 
+int tma_map_bf16_row_groups(CUtensorMap* map, const void* dev_ptr, long long rows, int cols, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn || cols % 64 || (reinterpret_cast<uintptr_t>(dev_ptr) & 15)) return -1;
+  cuuint64_t dims[3] = {64, static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(cols / 64)};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(cols) * 2, 128};
+  cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(cols / 64)};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(dev_ptr), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    std::fprintf(stderr, "sled: cuTensorMapEncodeTiled failed (%d) rows=%lld cols=%d box=%d\n", static_cast<int>(r), rows, cols, box_rows);
+    return -1;
+  }
+  return 0;
+}
+
 size_t tc_weight_tiled_bytes(int N, int K) {
   return static_cast<size_t>((N + kBlockM - 1) / kBlockM) * ((K + kBlockK - 1) / kBlockK) * kWStageBytes;
 }

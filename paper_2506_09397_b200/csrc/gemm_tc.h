@@ -51,6 +51,9 @@ struct TcEpilogue {       // what happens to the finished sums (see emit16 in ge
 
 // 2D bf16 tensor map over a row-major [rows][cols] array: boxes of 64 columns x box_rows rows, 128-byte swizzle
 int tma_map_bf16_rows(CUtensorMap* map, const void* dev_ptr, long long rows, int cols, int box_rows);
+// the same array with all its columns in one box: coordinates {column within 64, row, column / 64}, the box lands as
+// [cols / 64][box_rows][64 columns], 128-byte swizzle
+int tma_map_bf16_row_groups(CUtensorMap* map, const void* dev_ptr, long long rows, int cols, int box_rows);
 // Bytes of the tiled copy of an [N][K] matrix, and its construction from the row-major matrix (both in
 // device memory; `tiled` 16-byte aligned, tc_weight_tiled_bytes(N, K) long).  The row-major copy is not
 // needed afterwards.  Synchronises the device.

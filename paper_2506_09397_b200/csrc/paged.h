@@ -40,8 +40,14 @@ struct PagedRows {
 
 // Attention of the rows over everything they see (list null) or over the blocks list[t][kv head][list_len], ascending,
 // min(list_len, own block + 1) of them.  key_weights (optional, needs r.lse): [n_pages][Hkv][ps], added to.
-int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, int n_local,
-                           float* key_weights, cudaStream_t s);
+// ws: paged_attention_workspace bytes.
+int64_t paged_attention_workspace(int dtype, int h);
+int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,
+                           cudaStream_t s);
+// the attention itself on tensor cores (bf16, head_dim 64 or 128)
+constexpr int kMaxPagedBlocks = 320;   // two on each of up to 160 SMs
+int64_t paged_mma_workspace(int h);
+int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, char* ws, cudaStream_t s);
 // bounds[page][Hkv][2][h] of the pages that hold the keys first[i] .. n_kv[i]-1 (first null: all keys)
 int launch_block_bounds(const PagedCache& c, const int32_t* first, void* bounds, cudaStream_t s);
 // the blocks of every (row, KV head), ascending, into list [T][Hkv][n_blocks]; scores: room for [T][Hkv][table_cols]

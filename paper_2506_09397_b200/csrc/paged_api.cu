@@ -128,11 +128,12 @@ int64_t list_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_blocks) {
   return align256(static_cast<int64_t>(n_rows) * kv->n_kv_heads * n_blocks * 4);
 }
 
+int64_t attention_bytes(const sled_paged_kv* kv) { return align256(paged_attention_workspace(kv->dtype == SLED_BF16 ? BF16 : F32, kv->head_dim)); }
 int64_t tree_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, bool weigh) {
-  return weigh ? lse_bytes(n_rows, n_q_heads) : 0;
+  return attention_bytes(kv) + (weigh ? lse_bytes(n_rows, n_q_heads) : 0);
 }
 int64_t blocks_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_blocks) {
-  return list_bytes(kv, n_rows, n_blocks) + list_bytes(kv, n_rows, kv->table_cols);
+  return attention_bytes(kv) + list_bytes(kv, n_rows, n_blocks) + list_bytes(kv, n_rows, kv->table_cols);
 }
 int64_t evict_bytes(const sled_paged_kv* kv) {
   return align256(static_cast<int64_t>(kv->n_layers) * kv->n_reqs * kv->n_kv_heads * kv->table_cols * kv->page_size * 4);
@@ -160,10 +161,10 @@ int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride
   OnDeviceOf device(kv->k);
   if (device.rc()) return device.rc();
   char* ws = static_cast<char*>(workspace);
-  if (key_weights && !lse) lse = reinterpret_cast<float*>(ws);
+  if (key_weights && !lse) lse = reinterpret_cast<float*>(ws + attention_bytes(kv));
   const PagedCache c = cache_of(kv, status);
   const PagedRows r = rows_of(kv, q, q_stride, cu_q, parents, n_rows, n_q_heads, scale, out, out_stride, lse);
-  return done(launch_paged_attention(c, r, nullptr, 0, 0, key_weights, static_cast<cudaStream_t>(stream)), "sled_attention_tree");
+  return done(launch_paged_attention(c, r, nullptr, 0, key_weights, ws, static_cast<cudaStream_t>(stream)), "sled_attention_tree");
 }
 
 int sled_evict_keys_workspace(const sled_paged_kv* kv, int64_t* bytes) {
@@ -219,12 +220,12 @@ int sled_attention_blocks(const sled_paged_kv* kv, const void* bounds, const voi
   if (device.rc()) return device.rc();
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  float* scores = reinterpret_cast<float*>(ws);
-  int32_t* list = blocks ? blocks : reinterpret_cast<int32_t*>(ws + list_bytes(kv, n_rows, kv->table_cols));
+  float* scores = reinterpret_cast<float*>(ws + attention_bytes(kv));
+  int32_t* list = blocks ? blocks : reinterpret_cast<int32_t*>(ws + attention_bytes(kv) + list_bytes(kv, n_rows, kv->table_cols));
   const PagedCache c = cache_of(kv, status);
   const PagedRows r = rows_of(kv, q, q_stride, cu_q, nullptr, n_rows, n_q_heads, scale, out, out_stride, nullptr);
   int n = launch_block_choice(c, r, bounds, n_blocks, n_local, scores, list, s);
-  if (n >= 0) n = launch_paged_attention(c, r, list, n_blocks, n_local, nullptr, s);
+  if (n >= 0) n = launch_paged_attention(c, r, list, n_blocks, nullptr, ws, s);
   return done(n, "sled_attention_blocks");
 }
 

@@ -15,7 +15,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // One block of four warps per (token, head); warp w takes every fourth key, the lanes share the head dimension.
 template <typename T, int H>
-__global__ void __launch_bounds__(128) attn_row_kernel(PagedCache c, PagedRows r, const int32_t* list, int list_len, int n_local) {
+__global__ void __launch_bounds__(128) attn_row_kernel(PagedCache c, PagedRows r, const int32_t* list, int list_len) {
   constexpr int D = H / 32;
   const int t = blockIdx.x, head = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -128,9 +128,14 @@ __global__ void __launch_bounds__(128) key_weight_kernel(PagedCache c, PagedRows
 }
 
 template <typename T, int H>
-int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, int n_local, float* key_weights, cudaStream_t s) {
-  attn_row_kernel<T, H><<<dim3(r.T, r.Hq), 128, 0, s>>>(c, r, list, list_len, n_local);
+int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws, cudaStream_t s) {
   int n = 1;
+  if (sizeof(T) == 2 && H >= 64) {
+    n = launch_paged_mma(c, r, list, list_len, ws, s);
+    if (n < 0) return n;
+  } else {
+    attn_row_kernel<T, H><<<dim3(r.T, r.Hq), 128, 0, s>>>(c, r, list, list_len);
+  }
   if (key_weights) {
     key_weight_kernel<T, H><<<dim3(c.table_cols, c.Hkv, c.n_reqs), 128, 0, s>>>(c, r, key_weights);
     ++n;
@@ -140,16 +145,18 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
 
 }  // namespace
 
-int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, int n_local,
-                           float* key_weights, cudaStream_t s) {
+int64_t paged_attention_workspace(int dtype, int h) { return dtype == 1 && h >= 64 ? paged_mma_workspace(h) : 0; }
+
+int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,
+                           cudaStream_t s) {
   if (c.dtype == 1) {
-    if (c.h == 32) return launch_rows<__nv_bfloat16, 32>(c, r, list, list_len, n_local, key_weights, s);
-    if (c.h == 64) return launch_rows<__nv_bfloat16, 64>(c, r, list, list_len, n_local, key_weights, s);
-    if (c.h == 128) return launch_rows<__nv_bfloat16, 128>(c, r, list, list_len, n_local, key_weights, s);
+    if (c.h == 32) return launch_rows<__nv_bfloat16, 32>(c, r, list, list_len, key_weights, ws, s);
+    if (c.h == 64) return launch_rows<__nv_bfloat16, 64>(c, r, list, list_len, key_weights, ws, s);
+    if (c.h == 128) return launch_rows<__nv_bfloat16, 128>(c, r, list, list_len, key_weights, ws, s);
   } else {
-    if (c.h == 32) return launch_rows<float, 32>(c, r, list, list_len, n_local, key_weights, s);
-    if (c.h == 64) return launch_rows<float, 64>(c, r, list, list_len, n_local, key_weights, s);
-    if (c.h == 128) return launch_rows<float, 128>(c, r, list, list_len, n_local, key_weights, s);
+    if (c.h == 32) return launch_rows<float, 32>(c, r, list, list_len, key_weights, ws, s);
+    if (c.h == 64) return launch_rows<float, 64>(c, r, list, list_len, key_weights, ws, s);
+    if (c.h == 128) return launch_rows<float, 128>(c, r, list, list_len, key_weights, ws, s);
   }
   return -1;
 }

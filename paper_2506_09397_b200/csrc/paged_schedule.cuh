@@ -1,0 +1,149 @@
+// How the attention kernels over a paged cache share their work out: on the device, from the lengths alone.
+//
+// The work of a call is a line of key tiles.  Request by request, a request's units - (KV head, block of up to kUnitRows
+// query rows), or with chosen blocks (token, KV head, block of rows) - follow each other, and a unit is `tiles` tiles of
+// kTile keys.  A tile weighs what it costs (a number that depends on how many rows meet it); block c of G takes the tiles
+// that begin in [c C / G, (c + 1) C / G) of the total weight C; G is no larger than leaves every block a tile.  All blocks are resident and end together, whatever the
+// lengths are, a long context spreads over as many of them as it takes, and nothing has to be known on the host.  A unit
+// that is cut leaves one partial result per block; only a block's first and last unit can be cut, so two places per
+// block hold them.
+#pragma once
+#include "paged_device.cuh"
+
+namespace sled {
+
+constexpr int kTile = 64;        // keys per tile
+constexpr int kUnitRows = 64;    // query rows of a unit at most
+
+// one request's share of the line
+struct ReqWork {
+  ReqView v;
+  int tiles;        // of a unit
+  int n_rb;         // row blocks
+  int units;
+  int weight;       // of a tile
+  __device__ __forceinline__ long long count() const { return static_cast<long long>(units) * tiles; }
+  __device__ __forceinline__ long long cost() const { return count() * weight; }
+};
+
+// Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM).
+constexpr int kMinShare = 32;
+__device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
+
+// list_len > 0: units attend to chosen blocks, at most list_len per token
+__device__ __forceinline__ ReqWork req_work(const PagedCache& c, const PagedRows& r, int list_len, int i) {
+  ReqWork w;
+  w.v = req_view(c, r, i);
+  const int group = r.Hq / c.Hkv;
+  w.tiles = w.units = w.n_rb = 0;
+  w.weight = 1;
+  if (!w.v.ok || w.v.m == 0) return w;
+  const int rows = list_len > 0 ? group : w.v.m * group;
+  int keys = w.v.n;
+  if (list_len > 0) keys = min(static_cast<long long>(list_len), static_cast<long long>((w.v.n - 1) / c.ps + 1)) * c.ps;
+  w.tiles = (keys + kTile - 1) / kTile;
+  w.n_rb = (rows + kUnitRows - 1) / kUnitRows;
+  w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
+  w.weight = tile_weight(min(rows, kUnitRows));
+  return w;
+}
+
+struct Share {
+  int req;               // first request
+  long long at;          // where it begins on the line
+  long long from, to;    // this block's part of the line
+  long long total;
+  int n_blocks;          // blocks that share the line: every one of them gets a tile
+};
+
+// All threads of the block call it (blockDim.x a multiple of 32, at most 1024).  Block 0 reports requests left out.
+__device__ __forceinline__ Share block_share(const PagedCache& c, const PagedRows& r, int list_len, int block, int max_blocks) {
+  __shared__ long long sums[33];
+  __shared__ Share mine;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  const int per = (c.n_reqs + blockDim.x - 1) / blockDim.x;
+  const int first = min(static_cast<int>(threadIdx.x) * per, c.n_reqs), last = min(first + per, c.n_reqs);
+  long long own = 0;
+  for (int i = first; i < last; ++i) {
+    const ReqWork w = req_work(c, r, list_len, i);
+    own += w.cost();
+    if (block == 0 && !w.v.ok) set_status(c.status, req_fault(r, w.v));
+  }
+  long long x = own;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) sums[warp] = x;
+  if (threadIdx.x == 0) mine = Share{0, 0, 0, 0, 0, 1};
+  __syncthreads();
+  long long before = 0, total = 0;
+  for (int k = 0; k < nw; ++k) {
+    if (k < warp) before += sums[k];
+    total += sums[k];
+  }
+  long long at = before + x - own;
+  // a part of the line that is longer than any tile holds the beginning of one
+  const int n_blocks = static_cast<int>(max(1LL, min(static_cast<long long>(max_blocks), total / kMinShare)));
+  const long long from = block < n_blocks ? total * block / n_blocks : 0, to = block < n_blocks ? total * (block + 1) / n_blocks : 0;
+  if (from < to && at <= from && from < at + own) {
+    int i = first;
+    for (;; ++i) {
+      const long long cost = req_work(c, r, list_len, i).cost();
+      if (from < at + cost) break;
+      at += cost;
+    }
+    mine = Share{i, at, from, to, total, n_blocks};
+  }
+  __syncthreads();
+  return mine;
+}
+
+// the block that owns the tile which begins at `at`
+__device__ __forceinline__ int owner_of(long long at, long long total, int n_blocks) {
+  return static_cast<int>(((at + 1) * n_blocks - 1) / total);
+}
+
+// A stretch of one unit that a block works on.
+struct Segment {
+  int req, j, g, rb;     // j: the token (chosen blocks), otherwise unused
+  int t0, t1;            // tiles
+  bool whole;            // the unit is not cut
+  int slot;              // place of the partial result: 2 * block for the block's first tile, 2 * block + 1 otherwise
+  int last_block;        // cut units, where t0 == 0: the block that ends the unit; -1 otherwise
+};
+
+// Calls f(work of the request, segment) for every segment of the share, in order.
+template <typename F>
+__device__ __forceinline__ void for_segments(const PagedCache& c, const PagedRows& r, int list_len, const Share& s, int block, F f) {
+  long long at = s.at;
+  bool first = true;
+  for (int i = s.req; at < s.to; ++i) {
+    const ReqWork w = req_work(c, r, list_len, i);
+    const long long cost = w.cost();
+    if (cost == 0) continue;
+    const long long lt_end = min(w.count(), (s.to - at + w.weight - 1) / w.weight);
+    for (long long lt = s.from > at ? (s.from - at + w.weight - 1) / w.weight : 0; lt < lt_end;) {
+      const int u = static_cast<int>(lt / w.tiles);
+      Segment g;
+      g.req = i;
+      g.t0 = static_cast<int>(lt - static_cast<long long>(u) * w.tiles);
+      g.t1 = static_cast<int>(min(static_cast<long long>(w.tiles), g.t0 + (lt_end - lt)));
+      g.rb = u % w.n_rb;
+      g.g = u / w.n_rb % c.Hkv;
+      g.j = u / w.n_rb / c.Hkv;
+      g.whole = g.t0 == 0 && g.t1 == w.tiles;
+      g.slot = 2 * block + (first ? 0 : 1);
+      g.last_block = -1;
+      if (g.t0 == 0 && !g.whole)
+        g.last_block = owner_of(at + ((static_cast<long long>(u) + 1) * w.tiles - 1) * w.weight, s.total, s.n_blocks);
+      f(w, g);
+      first = false;
+      lt += g.t1 - g.t0;
+    }
+    at += cost;
+  }
+}
+
+}  // namespace sled
