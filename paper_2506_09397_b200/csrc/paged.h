@@ -41,13 +41,16 @@ struct PagedRows {
 // Attention of the rows over everything they see (list null) or over the blocks list[t][kv head][list_len], ascending,
 // min(list_len, own block + 1) of them.  key_weights (optional, needs r.lse): [n_pages][Hkv][ps], added to.
 // ws: paged_attention_workspace bytes.
-int64_t paged_attention_workspace(int dtype, int h);
+int64_t paged_attention_workspace(int dtype, int h, int64_t rows_heads, int64_t keys, bool weigh);
 int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,
                            cudaStream_t s);
-// the attention itself on tensor cores (bf16, head_dim 64 or 128)
+// the attention itself on tensor cores (bf16, head_dim 64 or 128); scores (optional): [T][Hq][table_cols * ps] receives
+// scale q.k in units of log2, -infinity where a row does not see a key, up to the request's last key
 constexpr int kMaxPagedBlocks = 320;   // two on each of up to 160 SMs
 int64_t paged_mma_workspace(int h);
-int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, char* ws, cudaStream_t s);
+int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s);
+// the number of SMs of the current device, or a negative value
+int paged_device(int* sms);
 // bounds[page][Hkv][2][h] of the pages that hold the keys first[i] .. n_kv[i]-1 (first null: all keys)
 int launch_block_bounds(const PagedCache& c, const int32_t* first, void* bounds, cudaStream_t s);
 // the blocks of every (row, KV head), ascending, into list [T][Hkv][n_blocks]; scores: room for [T][Hkv][table_cols]

@@ -128,12 +128,15 @@ int64_t list_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_blocks) {
   return align256(static_cast<int64_t>(n_rows) * kv->n_kv_heads * n_blocks * 4);
 }
 
-int64_t attention_bytes(const sled_paged_kv* kv) { return align256(paged_attention_workspace(kv->dtype == SLED_BF16 ? BF16 : F32, kv->head_dim)); }
-int64_t tree_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, bool weigh) {
-  return attention_bytes(kv) + (weigh ? lse_bytes(n_rows, n_q_heads) : 0);
+int64_t attention_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, bool weigh) {
+  return align256(paged_attention_workspace(kv->dtype == SLED_BF16 ? BF16 : F32, kv->head_dim, static_cast<int64_t>(n_rows) * n_q_heads,
+                                            static_cast<int64_t>(kv->table_cols) * kv->page_size, weigh));
 }
-int64_t blocks_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_blocks) {
-  return attention_bytes(kv) + list_bytes(kv, n_rows, n_blocks) + list_bytes(kv, n_rows, kv->table_cols);
+int64_t tree_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, bool weigh) {
+  return attention_bytes(kv, n_rows, n_q_heads, weigh) + (weigh ? lse_bytes(n_rows, n_q_heads) : 0);
+}
+int64_t blocks_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks) {
+  return attention_bytes(kv, n_rows, n_q_heads, false) + list_bytes(kv, n_rows, n_blocks) + list_bytes(kv, n_rows, kv->table_cols);
 }
 int64_t evict_bytes(const sled_paged_kv* kv) {
   return align256(static_cast<int64_t>(kv->n_layers) * kv->n_reqs * kv->n_kv_heads * kv->table_cols * kv->page_size * 4);
@@ -161,7 +164,7 @@ int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride
   OnDeviceOf device(kv->k);
   if (device.rc()) return device.rc();
   char* ws = static_cast<char*>(workspace);
-  if (key_weights && !lse) lse = reinterpret_cast<float*>(ws + attention_bytes(kv));
+  if (key_weights && !lse) lse = reinterpret_cast<float*>(ws + attention_bytes(kv, n_rows, n_q_heads, true));
   const PagedCache c = cache_of(kv, status);
   const PagedRows r = rows_of(kv, q, q_stride, cu_q, parents, n_rows, n_q_heads, scale, out, out_stride, lse);
   return done(launch_paged_attention(c, r, nullptr, 0, key_weights, ws, static_cast<cudaStream_t>(stream)), "sled_attention_tree");
@@ -203,7 +206,7 @@ int sled_block_bounds(const sled_paged_kv* kv, const int32_t* first, void* bound
 
 int sled_attention_blocks_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks, int64_t* bytes) {
   if (check_cache(kv, true, false) || n_rows < 0 || n_q_heads < 1 || n_blocks < 1 || !bytes) return SLED_ERR_ARG;
-  *bytes = blocks_bytes(kv, n_rows, n_blocks);
+  *bytes = blocks_bytes(kv, n_rows, n_q_heads, n_blocks);
   return SLED_OK;
 }
 
@@ -213,15 +216,15 @@ int sled_attention_blocks(const sled_paged_kv* kv, const void* bounds, const voi
   int rc = check_cache(kv, true, false);
   if (!rc) rc = check_rows(kv, q, q_stride, cu_q, n_rows, n_q_heads, scale, out, out_stride);
   if (!rc && (!bounds || !aligned(bounds, 16) || !aligned(blocks, 4) || !aligned(status, 4) || n_local < 1 || n_blocks < n_local)) rc = SLED_ERR_ARG;
-  if (!rc) rc = check_workspace(workspace, workspace_bytes, blocks_bytes(kv, n_rows, n_blocks));
+  if (!rc) rc = check_workspace(workspace, workspace_bytes, blocks_bytes(kv, n_rows, n_q_heads, n_blocks));
   if (rc) return rc;
   if (n_rows == 0 || kv->n_reqs == 0) return SLED_OK;
   OnDeviceOf device(kv->k);
   if (device.rc()) return device.rc();
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  float* scores = reinterpret_cast<float*>(ws + attention_bytes(kv));
-  int32_t* list = blocks ? blocks : reinterpret_cast<int32_t*>(ws + attention_bytes(kv) + list_bytes(kv, n_rows, kv->table_cols));
+  float* scores = reinterpret_cast<float*>(ws + attention_bytes(kv, n_rows, n_q_heads, false));
+  int32_t* list = blocks ? blocks : reinterpret_cast<int32_t*>(ws + attention_bytes(kv, n_rows, n_q_heads, false) + list_bytes(kv, n_rows, kv->table_cols));
   const PagedCache c = cache_of(kv, status);
   const PagedRows r = rows_of(kv, q, q_stride, cu_q, nullptr, n_rows, n_q_heads, scale, out, out_stride, nullptr);
   int n = launch_block_choice(c, r, bounds, n_blocks, n_local, scores, list, s);

@@ -4,7 +4,7 @@
 // For a query row r (token, head) and the keys x it sees: s_x = scale q.k_x, p_x = exp(s_x - lse), lse = ln sum exp s_x,
 // o = sum p_x v_x.  One pass over the keys with the running maximum and sum; a row that sees nothing gets o = 0 and
 // lse = -inf.
-#include "paged_device.cuh"
+#include "paged_schedule.cuh"
 
 namespace sled {
 
@@ -127,12 +127,79 @@ __global__ void __launch_bounds__(128) key_weight_kernel(PagedCache c, PagedRows
   }
 }
 
+// The same from the scores that the attention kernel left: every key's sum over the rows of exp2(score - lse).  A thread
+// has four keys and every fourth row, the rows' sums meet in shared memory; one addition per key, no atomics.
+__global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, PagedRows r, const float* scores, int64_t keys, float* key_weights) {
+  constexpr int kRowsAtOnce = 512;
+  __shared__ float lse[kRowsAtOnce];
+  __shared__ float4 sums[4][64];
+  pdl_wait();
+  const AttentionLine line{c, r, kWholeRows};
+  const Share share = block_share(line, blockIdx.x, gridDim.x);
+  if (share.from >= share.to) return;
+  const int quad = threadIdx.x & 63, part = threadIdx.x >> 6, group = r.Hq / c.Hkv;
+  for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
+    const int rows = w.v.m * group, end = min(sg.t1 * kTile, w.v.n);
+    for (int x0 = sg.t0 * kTile; x0 < end; x0 += 256) {
+      const int x = x0 + quad * 4;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int first = 0; first < rows; first += kRowsAtOnce) {
+        const int here = min(kRowsAtOnce, rows - first);
+        __syncthreads();
+        for (int i = threadIdx.x; i < here; i += 256) {
+          const int j = (first + i) / group, hh = (first + i) % group;
+          const float l = r.lse[static_cast<int64_t>(w.v.row0 + j) * r.Hq + sg.g * group + hh];
+          lse[i] = l == -INFINITY ? INFINITY : l * kLog2e;   // a row that saw nothing adds nothing
+        }
+        __syncthreads();
+        if (x < end) {
+#pragma unroll 4
+          for (int i = part; i < here; i += 4) {
+            const int j = (first + i) / group, hh = (first + i) % group;
+            const float4 s = *reinterpret_cast<const float4*>(scores + (static_cast<int64_t>(w.v.row0 + j) * r.Hq + sg.g * group + hh) * keys + x);
+            sum.x += exp2f(s.x - lse[i]);
+            sum.y += exp2f(s.y - lse[i]);
+            sum.z += exp2f(s.z - lse[i]);
+            sum.w += exp2f(s.w - lse[i]);
+          }
+        }
+      }
+      sums[part][quad] = sum;
+      __syncthreads();
+      const int mine = x0 + threadIdx.x;   // and now a key per thread
+      if (mine < end) {
+        const int page = c.table[static_cast<int64_t>(sg.req) * c.table_stride + mine / c.ps];
+        if (page_exists(c, page)) {
+          const float* s = reinterpret_cast<const float*>(sums) + threadIdx.x;
+          key_weights[(static_cast<int64_t>(page) * c.Hkv + sg.g) * c.ps + mine % c.ps] += (s[0] + s[256]) + (s[512] + s[768]);
+        }
+      }
+      __syncthreads();
+    }
+  });
+}
+
+// Scores are kept where they take no more than this; otherwise the weights are computed from the keys again.
+constexpr int64_t kMostScoreBytes = 512LL << 20;
+bool keeps_scores(int dtype, int h, int64_t rows_heads, int64_t keys) {
+  return dtype == 1 && h >= 64 && rows_heads * keys * 4 <= kMostScoreBytes;
+}
+
 template <typename T, int H>
 int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws, cudaStream_t s) {
   int n = 1;
   if (sizeof(T) == 2 && H >= 64) {
-    n = launch_paged_mma(c, r, list, list_len, ws, s);
+    const int64_t keys = static_cast<int64_t>(c.table_cols) * c.ps;
+    const bool keep = key_weights && keeps_scores(c.dtype, H, static_cast<int64_t>(r.T) * r.Hq, keys);
+    float* scores = keep ? reinterpret_cast<float*>(ws + (paged_mma_workspace(H) + 255) / 256 * 256) : nullptr;
+    n = launch_paged_mma(c, r, list, list_len, scores, ws, s);
     if (n < 0) return n;
+    if (keep) {
+      int sms = 0;
+      if (paged_device(&sms) < 0) return -1;
+      SLED_LAUNCH_PDL(key_weight_sum_kernel, dim3(4 * sms), dim3(256), 0, s, c, r, scores, keys, key_weights);
+      return cudaGetLastError() == cudaSuccess ? n + 1 : -1;
+    }
   } else {
     attn_row_kernel<T, H><<<dim3(r.T, r.Hq), 128, 0, s>>>(c, r, list, list_len);
   }
@@ -145,7 +212,10 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
 
 }  // namespace
 
-int64_t paged_attention_workspace(int dtype, int h) { return dtype == 1 && h >= 64 ? paged_mma_workspace(h) : 0; }
+int64_t paged_attention_workspace(int dtype, int h, int64_t rows_heads, int64_t keys, bool weigh) {
+  if (dtype != 1 || h < 64) return 0;
+  return (paged_mma_workspace(h) + 255) / 256 * 256 + (weigh && keeps_scores(dtype, h, rows_heads, keys) ? rows_heads * keys * 4 : 0);
+}
 
 int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,
                            cudaStream_t s) {

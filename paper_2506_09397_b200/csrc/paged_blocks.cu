@@ -6,7 +6,8 @@
 // of the earlier ones, those of largest score, the lower block first among equals.
 #include <algorithm>
 
-#include "paged_device.cuh"
+#include "paged_schedule.cuh"
+#include "warp_mma.cuh"
 
 namespace sled {
 
@@ -57,14 +58,158 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(PagedCache c, const i
   }
 }
 
-// One block per (token, KV head): scores of the earlier blocks into `scores`, then the choice, ascending, into `list`.
+// the larger of two scores; a NaN is the largest
+__device__ __forceinline__ float larger(float a, float b) { return a != a || b != b ? NAN : fmaxf(a, b); }
+
+// Earlier blocks of a request's tokens, in tiles of 64, for units of (KV head, up to 64 rows); nothing where all blocks of
+// the request's last token are read anyway.
+struct ScoreLine {
+  const PagedCache& c;
+  const PagedRows& r;
+  int n_blocks, n_local;
+  __device__ __forceinline__ int tokens() const { return max(1, kUnitRows / (r.Hq / c.Hkv)); }   // of a unit
+  __device__ __forceinline__ ReqWork operator()(int i) const {
+    ReqWork w;
+    w.v = req_view(c, r, i);
+    w.tiles = w.units = w.n_rb = 0;
+    w.weight = 1;
+    if (!w.v.ok || w.v.m == 0) return w;
+    const int blocks = (w.v.n - 1) / c.ps + 1;
+    if (blocks <= n_blocks || n_blocks == n_local) return w;
+    w.tiles = (blocks - n_local + 63) / 64;
+    w.n_rb = (w.v.m + tokens() - 1) / tokens();
+    w.units = w.n_rb * c.Hkv;
+    w.weight = tile_weight(min(w.v.m * (r.Hq / c.Hkv), kUnitRows));
+    return w;
+  }
+};
+
+// Scores on the tensor cores: rows [min(q, 0), max(q, 0)] against the bounds as they lie in memory, [low, high], a
+// contraction over 2 H.  The order of the terms is free, so a thread takes 16 consecutive bytes of a row as two
+// instructions' operands (both sides alike) and the bounds go from memory straight into registers.  A warp has 16 of the
+// tile's 64 blocks and all the unit's rows; the maximum over a group's heads is taken in shared memory.
+// Bound by the bytes of the bounds: 4 H per block and KV head.
+template <int H>
+__global__ void __launch_bounds__(128) block_score_kernel(PagedCache c, PagedRows r, const __nv_bfloat16* bounds, int n_blocks,
+                                                          int n_local, float* scores) {
+  constexpr int kRow = H + 8;                      // padded: eight rows' 16-byte pieces meet no bank twice
+  __shared__ __align__(16) __nv_bfloat16 qs[kUnitRows * kRow];
+  __shared__ float tile[kUnitRows][65];
+  pdl_launch_dependents();
+  pdl_wait();
+  const ScoreLine line{c, r, n_blocks, n_local};
+  const Share share = block_share(line, blockIdx.x, gridDim.x);
+  if (share.from >= share.to) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3, group = r.Hq / c.Hkv;
+  for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
+    const int j0 = sg.rb * line.tokens(), nj = min(line.tokens(), w.v.m - j0), rows = nj * group;
+    __syncthreads();
+    for (int e = threadIdx.x; e < kUnitRows * (H / 2); e += 128) {
+      const int row = e / (H / 2), d = e % (H / 2);
+      uint32_t x = 0;
+      if (row < rows)
+        x = reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(r.q) + (w.v.row0 + j0 + row / group) * r.q_stride +
+                                              static_cast<int64_t>(sg.g * group + row % group) * H)[d];
+      *reinterpret_cast<uint32_t*>(qs + row * kRow + 2 * d) = x;
+    }
+    __syncthreads();
+    const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
+    const int early = (w.v.n - 1) / c.ps + 1 - n_local;
+    for (int t = sg.t0; t < sg.t1; ++t) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        const int b = t * 64 + warp * 16 + nt * 8 + gq;
+        uint4 bb[H / 16];                          // this thread's quarter of block b's bounds
+        if (b < early) {
+          const int page = checked_page(c, table[b]);
+          const uint4* src = reinterpret_cast<const uint4*>(bounds + (static_cast<int64_t>(page) * c.Hkv + sg.g) * 2 * H) + tq;
+#pragma unroll
+          for (int k = 0; k < H / 16; ++k) bb[k] = src[4 * k];
+        } else {
+#pragma unroll
+          for (int k = 0; k < H / 16; ++k) bb[k] = make_uint4(0, 0, 0, 0);
+        }
+        for (int mt = 0; mt * 16 < rows; ++mt) {
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = 0; k < H / 16; ++k) {       // 32 terms at a time; the first half of them against the lower bounds
+            const bool low = k < H / 32;
+            const uint4 lo = *reinterpret_cast<const uint4*>(qs + (mt * 16 + gq) * kRow + (k % (H / 32)) * 32 + tq * 8);
+            const uint4 hi = *reinterpret_cast<const uint4*>(qs + (mt * 16 + gq + 8) * kRow + (k % (H / 32)) * 32 + tq * 8);
+            auto half = [&](uint32_t x) {
+              const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&x), z = __floats2bfloat162_rn(0.f, 0.f);
+              const __nv_bfloat162 y = low ? __hmin2_nan(v, z) : __hmax2_nan(v, z);
+              return *reinterpret_cast<const uint32_t*>(&y);
+            };
+            const uint32_t a0[4] = {half(lo.x), half(hi.x), half(lo.y), half(hi.y)};
+            mma_bf16(s, a0, bb[k].x, bb[k].y);
+            const uint32_t a1[4] = {half(lo.z), half(hi.z), half(lo.w), half(hi.w)};
+            mma_bf16(s, a1, bb[k].z, bb[k].w);
+          }
+          const int col = warp * 16 + nt * 8 + 2 * tq;
+          tile[mt * 16 + gq][col] = s[0];
+          tile[mt * 16 + gq][col + 1] = s[1];
+          tile[mt * 16 + gq + 8][col] = s[2];
+          tile[mt * 16 + gq + 8][col + 1] = s[3];
+        }
+      }
+      __syncthreads();
+      for (int e = threadIdx.x; e < nj * 64; e += 128) {
+        const int j = e >> 6, col = e & 63, b = t * 64 + col;
+        float best = tile[j * group][col];
+        for (int hh = 1; hh < group; ++hh) best = larger(best, tile[j * group + hh][col]);
+        if (b < early) scores[(static_cast<int64_t>(w.v.row0 + j0 + j) * c.Hkv + sg.g) * c.table_cols + b] = best;
+      }
+      __syncthreads();
+    }
+  });
+}
+
+// The same without tensor cores (fp32 caches and small or odd shapes): a warp per block and row, the lanes share the head.
 template <typename T, int H>
-__global__ void __launch_bounds__(256) block_choice_kernel(PagedCache c, PagedRows r, const T* bounds, int n_blocks, int n_local,
-                                                           float* scores, int32_t* list) {
+__global__ void __launch_bounds__(256) block_score_row_kernel(PagedCache c, PagedRows r, const T* bounds, int n_blocks, int n_local, float* scores) {
   constexpr int D = H / 32;
-  __shared__ int hist[256], scratch[33], pick[2];
+  pdl_launch_dependents();
+  pdl_wait();
   const int t = blockIdx.x, g = blockIdx.y, group = r.Hq / c.Hkv;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int i = req_of_row(r.cu_q, c.n_reqs, t);
+  const ReqView v = req_view(c, r, i);
+  const int j = t - v.row0;
+  if (!v.ok || j < 0 || j >= v.m) return;
+  const int own = (v.n - v.m + j) / c.ps, early = own + 1 - n_local;
+  if (own + 1 <= n_blocks) return;
+  float* sc = scores + (static_cast<int64_t>(t) * c.Hkv + g) * c.table_cols;
+  for (int b = blockIdx.z * 8 + warp; b < early; b += gridDim.z * 8) {
+    const int page = checked_page(c, c.table[static_cast<int64_t>(i) * c.table_stride + b]);
+    const T* lo = bounds + (static_cast<int64_t>(page) * c.Hkv + g) * 2 * H + lane * D;
+    float low[D], high[D], best = -INFINITY;
+#pragma unroll
+    for (int d = 0; d < D; ++d) { low[d] = to_f32(lo[d]); high[d] = to_f32(lo[H + d]); }
+    for (int hh = 0; hh < group; ++hh) {
+      const T* q = reinterpret_cast<const T*>(r.q) + t * r.q_stride + static_cast<int64_t>(g * group + hh) * H + lane * D;
+      float s = 0.f;
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        const float x = to_f32(q[d]);
+        s = fmaf(fmaxf(x, 0.f), high[d], s);
+        s = fmaf(fminf(x, 0.f), low[d], s);
+      }
+      best = larger(best, warp_sum(s));
+    }
+    if (lane == 0) sc[b] = best;
+  }
+}
+
+// The choice: one block per (token, KV head); the scores of up to kMostCached blocks stay in shared memory.
+constexpr int kMostCached = 8192;
+__global__ void __launch_bounds__(256) block_choice_kernel(PagedCache c, PagedRows r, int n_blocks, int n_local, const float* scores,
+                                                           int32_t* list) {
+  __shared__ int hist[256], scratch[33], pick[2];
+  __shared__ uint32_t cached[kMostCached];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int t = blockIdx.x, g = blockIdx.y;
   const int i = req_of_row(r.cu_q, c.n_reqs, t);
   const ReqView v = req_view(c, r, i);
   const int j = t - v.row0;
@@ -76,34 +221,18 @@ __global__ void __launch_bounds__(256) block_choice_kernel(PagedCache c, PagedRo
     return;
   }
   const int early = own + 1 - n_local, want = n_blocks - n_local;   // early > want
-  float* sc = scores + (static_cast<int64_t>(t) * c.Hkv + g) * c.table_cols;
-  for (int b = warp; b < early; b += 8) {
-    const int page = checked_page(c, c.table[static_cast<int64_t>(i) * c.table_stride + b]);
-    const T* lo = bounds + (static_cast<int64_t>(page) * c.Hkv + g) * 2 * H + lane * D;
-    float best = -INFINITY;
-    for (int hh = 0; hh < group; ++hh) {
-      const T* q = reinterpret_cast<const T*>(r.q) + t * r.q_stride + static_cast<int64_t>(g * group + hh) * H + lane * D;
-      float s = 0.f;
-#pragma unroll
-      for (int d = 0; d < D; ++d) {
-        const float x = to_f32(q[d]);
-        s = fmaf(fmaxf(x, 0.f), to_f32(lo[H + d]), s);
-        s = fmaf(fminf(x, 0.f), to_f32(lo[d]), s);
-      }
-      s = warp_sum(s);
-      best = s != s || best != best ? NAN : fmaxf(best, s);
-    }
-    if (lane == 0) sc[b] = best;
-  }
+  const float* sc = scores + (static_cast<int64_t>(t) * c.Hkv + g) * c.table_cols;
+  for (int b = threadIdx.x; b < min(early, kMostCached) && want > 0; b += blockDim.x) cached[b] = rank_bits(sc[b]);
   __syncthreads();
+  auto rank = [&](int b) { return b < kMostCached ? cached[b] : rank_bits(sc[b]); };
   int greater = 0;
   uint32_t edge = 0xffffffffu;
-  if (want > 0) edge = select_largest([&](int b) { return rank_bits(sc[b]); }, early, want, hist, pick, &greater);
+  if (want > 0) edge = select_largest(rank, early, want, hist, pick, &greater);
   int taken = 0, ties = 0;
   const int tie_want = want - greater;
   for (int b0 = 0; b0 < early && want > 0; b0 += blockDim.x) {
     const int b = b0 + threadIdx.x;
-    const uint32_t x = b < early ? rank_bits(sc[b]) : 0;
+    const uint32_t x = b < early ? rank(b) : 0;
     const bool tie = b < early && x == edge;
     int n_tie, n_take;
     const int tie_rank = ties + block_scan(tie, scratch, &n_tie);
@@ -123,8 +252,20 @@ int bounds_typed(const PagedCache& c, const int32_t* first, void* bounds, cudaSt
 }
 template <typename T, int H>
 int choice_typed(const PagedCache& c, const PagedRows& r, const void* bounds, int n_blocks, int n_local, float* scores, int32_t* list, cudaStream_t s) {
-  block_choice_kernel<T, H><<<dim3(r.T, c.Hkv), 256, 0, s>>>(c, r, static_cast<const T*>(bounds), n_blocks, n_local, scores, list);
-  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+  int sms = 0;
+  if (paged_device(&sms) < 0) return -1;
+  if constexpr (sizeof(T) == 2 && H >= 64) {
+    if (r.Hq / c.Hkv <= kUnitRows) {
+      SLED_LAUNCH_PDL(block_score_kernel<H>, dim3(4 * sms), dim3(128), 0, s, c, r, static_cast<const T*>(bounds), n_blocks, n_local, scores);
+      SLED_LAUNCH_PDL(block_choice_kernel, dim3(r.T, c.Hkv), dim3(256), 0, s, c, r, n_blocks, n_local, static_cast<const float*>(scores), list);
+      return cudaGetLastError() == cudaSuccess ? 2 : -1;
+    }
+  }
+  // enough blocks per row to fill the machine with few rows
+  const int z = std::max(1, std::min((c.table_cols + 7) / 8, static_cast<int>(8LL * sms / (static_cast<long long>(r.T) * c.Hkv))));
+  SLED_LAUNCH_PDL((block_score_row_kernel<T, H>), dim3(r.T, c.Hkv, z), dim3(256), 0, s, c, r, static_cast<const T*>(bounds), n_blocks, n_local, scores);
+  SLED_LAUNCH_PDL(block_choice_kernel, dim3(r.T, c.Hkv), dim3(256), 0, s, c, r, n_blocks, n_local, static_cast<const float*>(scores), list);
+  return cudaGetLastError() == cudaSuccess ? 2 : -1;
 }
 
 }  // namespace

@@ -59,6 +59,8 @@ struct Parts {
   float* acc;      // [2 * blocks][kUnitRows][H], not normalised
   float* ml;       // [2 * blocks][kUnitRows][2]
   int4* desc;      // [blocks] {last block or -1, first slot, request, unit of the request}
+  float* scores;   // null, or [rows][Hq][keys]
+  int64_t keys;
 };
 
 // One stretch of a unit: MT warps cover the rows, 4 / MT the keys of a tile.
@@ -128,6 +130,16 @@ __device__ __forceinline__ void consume(const PagedCache& c, const PagedRows& r,
               else if (u.j < 0) seen = a <= j;
             }
             if (!seen) sc[nt][e] = -INFINITY;
+          }
+      }
+      if (parts.scores) {
+        float* s_lo = parts.scores + (static_cast<int64_t>(u.row0 + j_lo) * r.Hq + h_lo) * parts.keys + k0 + 2 * tq;
+        float* s_hi = parts.scores + (static_cast<int64_t>(u.row0 + j_hi) * r.Hq + h_hi) * parts.keys + k0 + 2 * tq;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          if (k0 + nt * 8 + 2 * tq < u.end) {
+            if (v_lo) *reinterpret_cast<float2*>(s_lo + nt * 8) = make_float2(sc[nt][0] * scale, sc[nt][1] * scale);
+            if (v_hi) *reinterpret_cast<float2*>(s_hi + nt * 8) = make_float2(sc[nt][2] * scale, sc[nt][3] * scale);
           }
       }
       float mx_lo = -INFINITY, mx_hi = -INFINITY;
@@ -393,14 +405,15 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
   }
   __syncthreads();
   pdl_wait();
-  const Share share = block_share(c, r, list_len, blockIdx.x, gridDim.x);
+  const AttentionLine line{c, r, list_len};
+  const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (threadIdx.x == 0) parts.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
   if (share.from >= share.to) return;
 
   if (warp == 4) {
     const uint64_t policy = policy_evict_first();
     const int cpp = c.ps / 16;                  // 16-key groups of a page
-    for_segments(c, r, list_len, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
+    for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
       const UnitRows u = unit_rows(c, r, list_len, w, sg);
       const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
       const int32_t* mine = list_len > 0 ? list + (static_cast<int64_t>(w.v.row0 + sg.j) * c.Hkv + sg.g) * list_len : nullptr;
@@ -448,7 +461,7 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
     float* merge = reinterpret_cast<float*>(ptr + S::kOffMerge);
     uint32_t* tree = reinterpret_cast<uint32_t*>(ptr + S::kOffTree);
     int tree_of = -1;
-    for_segments(c, r, list_len, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
+    for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
       const UnitRows u = unit_rows(c, r, list_len, w, sg);
       if (r.parents && tree_of != sg.req) {     // what every node sees among the nodes
         tree_of = sg.req;
@@ -486,7 +499,7 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
   if (d.x < 0) return;
   constexpr int D = H / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const ReqWork w = req_work(c, r, list_len, d.z);
+  const ReqWork w = AttentionLine{c, r, list_len}(d.z);
   Segment sg{};
   sg.req = d.z;
   sg.rb = d.w % w.n_rb;
@@ -538,7 +551,9 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
 
 constexpr int kMaxDevices = 64;
 
-int device_sms(int* sms) {   // SMs of the current device, asked for once per device
+}  // namespace
+
+int paged_device(int* sms) {   // asked for once per device
   static int known[kMaxDevices] = {};
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return -1;
@@ -551,11 +566,13 @@ int device_sms(int* sms) {   // SMs of the current device, asked for once per de
   return dev;
 }
 
+namespace {
+
 template <int H>
-int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, char* ws, cudaStream_t s) {
+int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s) {
   static bool configured[kMaxDevices] = {};
   int sms = 0;
-  const int dev = device_sms(&sms);
+  const int dev = paged_device(&sms);
   if (dev < 0) return -1;
   if (!configured[dev]) {
     if (cudaFuncSetAttribute(paged_mma_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<H>::kTotal) != cudaSuccess) return -1;
@@ -569,6 +586,8 @@ int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int l
   parts.acc = reinterpret_cast<float*>(ws);
   parts.ml = parts.acc + 2LL * kMaxPagedBlocks * kUnitRows * H;
   parts.desc = reinterpret_cast<int4*>(parts.ml + 2LL * kMaxPagedBlocks * kUnitRows * 2);
+  parts.scores = scores;
+  parts.keys = static_cast<int64_t>(c.table_cols) * c.ps;
   SLED_LAUNCH_PDL(paged_mma_kernel<H>, dim3(blocks), dim3(160), Smem<H>::kTotal, s, c, r, list, list_len, parts, map_k, map_v);
   SLED_LAUNCH_PDL(paged_merge_kernel<H>, dim3(blocks, 2), dim3(512), 0, s, c, r, list_len, parts);
   return cudaGetLastError() == cudaSuccess ? 2 : -1;
@@ -580,8 +599,8 @@ int64_t paged_mma_workspace(int h) {
   return 2LL * kMaxPagedBlocks * kUnitRows * (h + 2) * 4 + kMaxPagedBlocks * 16LL;
 }
 
-int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, char* ws, cudaStream_t s) {
-  return c.h == 128 ? launch_h<128>(c, r, list, list_len, ws, s) : launch_h<64>(c, r, list, list_len, ws, s);
+int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s) {
+  return c.h == 128 ? launch_h<128>(c, r, list, list_len, scores, ws, s) : launch_h<64>(c, r, list, list_len, scores, ws, s);
 }
 
 }  // namespace sled

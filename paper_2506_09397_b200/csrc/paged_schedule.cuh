@@ -30,23 +30,30 @@ struct ReqWork {
 constexpr int kMinShare = 32;
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
 
-// list_len > 0: units attend to chosen blocks, at most list_len per token
-__device__ __forceinline__ ReqWork req_work(const PagedCache& c, const PagedRows& r, int list_len, int i) {
-  ReqWork w;
-  w.v = req_view(c, r, i);
-  const int group = r.Hq / c.Hkv;
-  w.tiles = w.units = w.n_rb = 0;
-  w.weight = 1;
-  if (!w.v.ok || w.v.m == 0) return w;
-  const int rows = list_len > 0 ? group : w.v.m * group;
-  int keys = w.v.n;
-  if (list_len > 0) keys = min(static_cast<long long>(list_len), static_cast<long long>((w.v.n - 1) / c.ps + 1)) * c.ps;
-  w.tiles = (keys + kTile - 1) / kTile;
-  w.n_rb = (rows + kUnitRows - 1) / kUnitRows;
-  w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
-  w.weight = tile_weight(min(rows, kUnitRows));
-  return w;
-}
+// The work of attention.  list_len > 0: units attend to chosen blocks, at most list_len per token.  kWholeRows: a unit has
+// all rows of its request (kernels that work key by key); a tile then weighs what its rows do, up to the largest weight.
+constexpr int kWholeRows = -1;
+struct AttentionLine {
+  const PagedCache& c;
+  const PagedRows& r;
+  int list_len;
+  __device__ __forceinline__ ReqWork operator()(int i) const {
+    ReqWork w;
+    w.v = req_view(c, r, i);
+    const int group = r.Hq / c.Hkv;
+    w.tiles = w.units = w.n_rb = 0;
+    w.weight = 1;
+    if (!w.v.ok || w.v.m == 0) return w;
+    const int rows = list_len > 0 ? group : w.v.m * group;
+    int keys = w.v.n;
+    if (list_len > 0) keys = min(list_len, (w.v.n - 1) / c.ps + 1) * c.ps;
+    w.tiles = (keys + kTile - 1) / kTile;
+    w.n_rb = list_len == kWholeRows ? 1 : (rows + kUnitRows - 1) / kUnitRows;
+    w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
+    w.weight = list_len == kWholeRows ? min(rows, kMinShare - 1) : tile_weight(min(rows, kUnitRows));
+    return w;
+  }
+};
 
 struct Share {
   int req;               // first request
@@ -57,17 +64,18 @@ struct Share {
 };
 
 // All threads of the block call it (blockDim.x a multiple of 32, at most 1024).  Block 0 reports requests left out.
-__device__ __forceinline__ Share block_share(const PagedCache& c, const PagedRows& r, int list_len, int block, int max_blocks) {
+template <typename Line>
+__device__ __forceinline__ Share block_share(const Line& line, int block, int max_blocks) {
   __shared__ long long sums[33];
   __shared__ Share mine;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
-  const int per = (c.n_reqs + blockDim.x - 1) / blockDim.x;
-  const int first = min(static_cast<int>(threadIdx.x) * per, c.n_reqs), last = min(first + per, c.n_reqs);
+  const int n_reqs = line.c.n_reqs, per = (n_reqs + blockDim.x - 1) / blockDim.x;
+  const int first = min(static_cast<int>(threadIdx.x) * per, n_reqs), last = min(first + per, n_reqs);
   long long own = 0;
   for (int i = first; i < last; ++i) {
-    const ReqWork w = req_work(c, r, list_len, i);
+    const ReqWork w = line(i);
     own += w.cost();
-    if (block == 0 && !w.v.ok) set_status(c.status, req_fault(r, w.v));
+    if (block == 0 && !w.v.ok) set_status(line.c.status, req_fault(line.r, w.v));
   }
   long long x = own;
 #pragma unroll
@@ -90,7 +98,7 @@ __device__ __forceinline__ Share block_share(const PagedCache& c, const PagedRow
   if (from < to && at <= from && from < at + own) {
     int i = first;
     for (;; ++i) {
-      const long long cost = req_work(c, r, list_len, i).cost();
+      const long long cost = line(i).cost();
       if (from < at + cost) break;
       at += cost;
     }
@@ -115,12 +123,12 @@ struct Segment {
 };
 
 // Calls f(work of the request, segment) for every segment of the share, in order.
-template <typename F>
-__device__ __forceinline__ void for_segments(const PagedCache& c, const PagedRows& r, int list_len, const Share& s, int block, F f) {
+template <typename Line, typename F>
+__device__ __forceinline__ void for_segments(const Line& line, const Share& s, int block, F f) {
   long long at = s.at;
   bool first = true;
   for (int i = s.req; at < s.to; ++i) {
-    const ReqWork w = req_work(c, r, list_len, i);
+    const ReqWork w = line(i);
     const long long cost = w.cost();
     if (cost == 0) continue;
     const long long lt_end = min(w.count(), (s.to - at + w.weight - 1) / w.weight);
@@ -131,8 +139,8 @@ __device__ __forceinline__ void for_segments(const PagedCache& c, const PagedRow
       g.t0 = static_cast<int>(lt - static_cast<long long>(u) * w.tiles);
       g.t1 = static_cast<int>(min(static_cast<long long>(w.tiles), g.t0 + (lt_end - lt)));
       g.rb = u % w.n_rb;
-      g.g = u / w.n_rb % c.Hkv;
-      g.j = u / w.n_rb / c.Hkv;
+      g.g = u / w.n_rb % line.c.Hkv;
+      g.j = u / w.n_rb / line.c.Hkv;
       g.whole = g.t0 == 0 && g.t1 == w.tiles;
       g.slot = 2 * block + (first ? 0 : 1);
       g.last_block = -1;
