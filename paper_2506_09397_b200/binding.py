@@ -533,9 +533,9 @@ def _ints(t, what: str, name: str, dev, shape=None):
     """A CUDA int32 tensor that is contiguous along its last dimension; returns its address (0 for None)."""
     if t is None:
         return 0
-    if t.dtype != torch.int32 or t.device != dev or (t.numel() > 1 and t.stride(-1) != 1):
+    if t.dtype is not torch.int32 or t.device != dev or (t.stride(-1) != 1 and t.numel() > 1):
         _refuse(what, f"{name} must be an int32 tensor on {dev}, contiguous along its last dimension")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         _refuse(what, f"{name} must have shape {shape}")
     return t.data_ptr()
 
@@ -543,66 +543,71 @@ def _ints(t, what: str, name: str, dev, shape=None):
 def _floats(t, what: str, name: str, dev, shape):
     if t is None:
         return 0
-    if t.dtype != torch.float32 or t.device != dev or tuple(t.shape) != shape or not t.is_contiguous():
-        _refuse(what, f"{name} must be a contiguous fp32 tensor of shape {shape} on {dev}")
+    if t.dtype is not torch.float32 or t.device != dev or t.shape != shape or not t.is_contiguous():
+        _refuse(what, f"{name} must be a contiguous fp32 tensor of shape {tuple(shape)} on {dev}")
     return t.data_ptr()
 
 
 def _paged(what: str, k, v, page_table, n_kv, layers: bool = False) -> SledPagedKv:
     """The cache description of a call, from K, V [n_pages, n_kv_heads, page_size, head_dim] (with a leading n_layers
     where the operator works on all layers), page_table [n_reqs, cols] and n_kv [n_reqs]."""
-    dev = k.device
+    dev, shape = k.device, k.shape
     if dev.type != "cuda":
         raise SledError(SLED_ERR_NO_DEVICE, f"{what} (tensors must be on a CUDA device)")
-    if k.dtype not in _TORCH_DT or not (k.dim() == 4 or (layers and k.dim() == 5)):
+    dtype = _TORCH_DT.get(k.dtype)
+    if dtype is None or not (len(shape) == 4 or (layers and len(shape) == 5)):
         _refuse(what, "the cache must be fp32 or bf16, [n_pages, n_kv_heads, page_size, head_dim]"
                 + (", with n_layers in front for all layers" if layers else ""))
-    for name, t in (("k", k), ("v", v)):
-        if t is not None and (t.dtype != k.dtype or t.device != dev or t.shape != k.shape or not t.is_contiguous()):
-            _refuse(what, f"{name} must be contiguous, and v like k")
+    if not k.is_contiguous() or (v is not None and (v.dtype != k.dtype or v.device != dev or v.shape != shape or not v.is_contiguous())):
+        _refuse(what, "k must be contiguous, and v like k")
     if page_table.dim() != 2 or n_kv.dim() != 1 or n_kv.shape[0] != page_table.shape[0]:
         _refuse(what, "page_table [n_reqs, cols] and n_kv [n_reqs]")
     n_reqs, cols = page_table.shape
     stride = page_table.stride(0) if n_reqs > 1 else cols
     if stride < cols:
         _refuse(what, "rows of page_table must not overlap")
-    n_pages, n_heads, page_size, head_dim = k.shape[-4:]
-    return SledPagedKv(k.data_ptr(), 0 if v is None else v.data_ptr(), _TORCH_DT[k.dtype], k.shape[0] if k.dim() == 5 else 1,
+    n_pages, n_heads, page_size, head_dim = shape[-4:]
+    return SledPagedKv(k.data_ptr(), 0 if v is None else v.data_ptr(), dtype, shape[0] if len(shape) == 5 else 1,
                        n_pages, n_heads, page_size, head_dim, _ints(page_table, what, "page_table", dev), stride, cols,
                        _ints(n_kv, what, "n_kv", dev), n_reqs)
 
 
+def _row_stride(t, what: str, name: str):
+    """Elements between the rows of q or out [rows, n_q_heads, head_dim]; a row itself is contiguous."""
+    rows, heads, h = t.shape
+    if t.is_contiguous():
+        return heads * h
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != h):
+        _refuse(what, f"a row of {name} must be contiguous")
+    return t.stride(0) if rows > 1 else heads * h
+
+
 def _query_rows(what: str, q, out, k, n_reqs: int, cu_q):
-    """(out, row strides) of q [rows, n_q_heads, head_dim], whose rows may be apart (a slice of a wider projection)."""
-    if q.dim() != 3 or q.dtype != k.dtype or q.device != k.device or q.shape[2] != k.shape[-1]:
+    """(out, q's and out's row strides); rows may be apart (q a slice of a wider projection)."""
+    if q.dim() != 3 or q.dtype != k.dtype or q.device != k.device or q.shape[2] != k.shape[3]:
         _refuse(what, "q must be [rows, n_q_heads, head_dim] of the cache's type and device")
     if cu_q.shape != (n_reqs + 1,):
         _refuse(what, "cu_q must be [n_reqs + 1]")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
         _refuse(what, "out must be like q")
-    strides = []
-    for t in (q, out):
-        _, heads, h = t.shape
-        if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != h)):
-            _refuse(what, "a row of q and of out must be contiguous")
-        strides.append(t.stride(0) if t.shape[0] > 1 else heads * h)
-    return out, strides
+    return out, _row_stride(q, what, "q"), _row_stride(out, what, "out")
 
 
 def _workspace(what: str, dev, kv, *sizes):
     """(tensor to be kept until the call has been made, address, bytes) of the workspace that the call asks for."""
     n = C.c_int64()
-    _check(getattr(lib(), what + "_workspace")(C.byref(kv), *sizes, C.byref(n)), what)
-    if not n.value:
+    _check(getattr(lib(), what + "_workspace")(kv, *sizes, n), what)
+    n = n.value
+    if not n:
         return None, 0, 0
-    t = torch.empty(n.value, dtype=torch.uint8, device=dev)
-    return t, t.data_ptr(), n.value
+    t = torch.empty(n, dtype=torch.uint8, device=dev)
+    return t, t.data_ptr(), n
 
 
 def _stream_of(dev) -> int:
-    return torch.cuda.current_stream(dev).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: float = 0.0, out=None, lse=None,
@@ -615,13 +620,13 @@ def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: floa
     what = "sled_attention_tree"
     kv = _paged(what, k, v, page_table, n_kv)
     dev = k.device
-    out, (qs, os_) = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
-    rows, heads = q.shape[:2]
+    out, q_stride, out_stride = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
+    rows, heads, _ = q.shape
     _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, int(key_weights is not None))
     _check(lib().sled_attention_tree(
-        C.byref(kv), q.data_ptr(), qs, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
-        scale, out.data_ptr(), os_, _floats(lse, what, "lse", dev, (rows, heads)),
-        _floats(key_weights, what, "key_weights", dev, tuple(k.shape[:3])), _ints(status, what, "status", dev),
+        kv, q.data_ptr(), q_stride, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
+        scale, out.data_ptr(), out_stride, _floats(lse, what, "lse", dev, (rows, heads)),
+        _floats(key_weights, what, "key_weights", dev, k.shape[:3]), _ints(status, what, "status", dev),
         ws, ws_bytes, _stream_of(dev)), what)
     return out
 
@@ -636,9 +641,9 @@ def evict_keys(k, v, key_weights, page_table, n_kv, budget: int, *, n_sink: int 
     kv = _paged(what, k, v, page_table, n_kv, layers=True)
     dev = k.device
     _held, ws, ws_bytes = _workspace(what, dev, kv)
-    w = _floats(key_weights, what, "key_weights", dev, tuple(k.shape[:-1]))
-    w_out = _floats(key_weights_out, what, "key_weights_out", dev, tuple(k.shape[:-1])) or w
-    _check(lib().sled_evict_keys(C.byref(kv), w, w_out, budget, n_sink, n_recent, _ints(status, what, "status", dev),
+    w = _floats(key_weights, what, "key_weights", dev, k.shape[:-1])
+    w_out = _floats(key_weights_out, what, "key_weights_out", dev, k.shape[:-1]) or w
+    _check(lib().sled_evict_keys(kv, w, w_out, budget, n_sink, n_recent, _ints(status, what, "status", dev),
                                  ws, ws_bytes, _stream_of(dev)), what)
 
 
@@ -649,7 +654,7 @@ def block_bounds(k, page_table, n_kv, bounds, *, first=None, status=None) -> Non
     kv = _paged(what, k, None, page_table, n_kv)
     dev = k.device
     _check_bounds(what, bounds, k)
-    _check(lib().sled_block_bounds(C.byref(kv), _ints(first, what, "first", dev, (kv.n_reqs,)), bounds.data_ptr(),
+    _check(lib().sled_block_bounds(kv, _ints(first, what, "first", dev, (kv.n_reqs,)), bounds.data_ptr(),
                                    _ints(status, what, "status", dev), _stream_of(dev)), what)
 
 
@@ -668,14 +673,14 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
     kv = _paged(what, k, v, page_table, n_kv)
     dev = k.device
     _check_bounds(what, bounds, k)
-    out, (qs, os_) = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
-    rows, heads = q.shape[:2]
+    out, q_stride, out_stride = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
+    rows, heads, _ = q.shape
     _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, n_blocks)
     if blocks is not None and not blocks.is_contiguous():
         _refuse(what, "blocks must be contiguous")
     _check(lib().sled_attention_blocks(
-        C.byref(kv), bounds.data_ptr(), q.data_ptr(), qs, _ints(cu_q, what, "cu_q", dev), rows, heads, scale, n_blocks, n_local,
-        out.data_ptr(), os_, _ints(blocks, what, "blocks", dev, (rows, kv.n_kv_heads, n_blocks)),
+        kv, bounds.data_ptr(), q.data_ptr(), q_stride, _ints(cu_q, what, "cu_q", dev), rows, heads, scale, n_blocks, n_local,
+        out.data_ptr(), out_stride, _ints(blocks, what, "blocks", dev, (rows, kv.n_kv_heads, n_blocks)),
         _ints(status, what, "status", dev), ws, ws_bytes,
         _stream_of(dev)), what)
     return out

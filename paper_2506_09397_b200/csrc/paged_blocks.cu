@@ -13,49 +13,100 @@ namespace sled {
 
 namespace {
 
-// One warp per (page of a request, KV head): the lanes share the head dimension, every key row is read once.
+// Blocks whose bounds are asked for, for units of a KV head: a tile is a block.
+struct BoundsLine {
+  const PagedCache& c;
+  const int32_t* first;
+  __device__ __forceinline__ int32_t fault(const ReqView&) const { return SLED_ERR_ARG; }
+  __device__ __forceinline__ int from(int i) const { return first ? max(0, first[i]) / c.ps : 0; }
+  __device__ __forceinline__ ReqWork operator()(int i) const {
+    ReqWork w;
+    w.v.n = c.n_kv[i];
+    w.v.m = w.v.row0 = 0;
+    w.v.ok = w.v.n >= 0 && w.v.n <= static_cast<int64_t>(c.table_cols) * c.ps;
+    w.n_rb = 1;
+    w.tiles = w.v.ok ? max(0, (w.v.n + c.ps - 1) / c.ps - from(i)) : 0;
+    w.units = w.tiles ? c.Hkv : 0;
+    w.weight = kMinShare / 8;   // a block gets work for all its warps, at least
+    return w;
+  }
+};
+
+template <typename T> struct Vec;           // 16 bytes of keys
+template <> struct Vec<float> {
+  static constexpr int kElems = 4, kWords = 4;
+  static __device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) {
+    const float x = __uint_as_float(a), y = __uint_as_float(b);
+    return __float_as_uint(x != x || y != y ? NAN : fminf(x, y));
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    const float x = __uint_as_float(a), y = __uint_as_float(b);
+    return __float_as_uint(x != x || y != y ? NAN : fmaxf(x, y));
+  }
+};
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int kElems = 8, kWords = 4;
+  static __device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmin2_nan(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+};
+
+// A warp per (block, KV head): the lanes take 16 bytes each, kRows rows at a time, four such loads under way; every key is
+// read once, which is what bounds it.
 template <typename T, int H>
 __global__ void __launch_bounds__(256) block_bounds_kernel(PagedCache c, const int32_t* first, T* bounds) {
-  constexpr int D = H / 32;
-  const int i = blockIdx.y;
-  const int lane = threadIdx.x & 31;
-  const int n = c.n_kv[i];
-  if (n < 0 || n > static_cast<int64_t>(c.table_cols) * c.ps) {
-    if (threadIdx.x == 0 && blockIdx.x == 0) set_status(c.status, SLED_ERR_ARG);
-    return;
-  }
-  const int from = first ? max(0, first[i]) : 0;
-  const int b0 = from / c.ps, nb = (n + c.ps - 1) / c.ps;
-  const int work = max(0, nb - b0) * c.Hkv;
-  for (int w = blockIdx.x * 8 + (threadIdx.x >> 5); w < work; w += gridDim.x * 8) {
-    const int b = b0 + w / c.Hkv, g = w % c.Hkv;
-    const int page = c.table[static_cast<int64_t>(i) * c.table_stride + b];
-    if (!page_exists(c, page)) {
-      if (lane == 0) set_status(c.status, SLED_ERR_ARG);
-      continue;
-    }
-    const int64_t at = (static_cast<int64_t>(page) * c.Hkv + g) * c.ps * H;
-    const T* k = reinterpret_cast<const T*>(c.k) + at + lane * D;
-    const int count = min(c.ps, n - b * c.ps);
-    float lo[D], hi[D];
-#pragma unroll
-    for (int d = 0; d < D; ++d) { lo[d] = INFINITY; hi[d] = -INFINITY; }
-    bool nan[D] = {};
-    for (int e = 0; e < count; ++e)
-#pragma unroll
-      for (int d = 0; d < D; ++d) {
-        const float x = to_f32(k[static_cast<int64_t>(e) * H + d]);
-        nan[d] |= x != x;
-        lo[d] = fminf(lo[d], x);
-        hi[d] = fmaxf(hi[d], x);
+  using V = Vec<T>;
+  constexpr int kLanes = H / V::kElems, kRows = 32 / kLanes;   // lanes of a key row; rows that a warp reads at once
+  pdl_launch_dependents();
+  pdl_wait();
+  const BoundsLine line{c, first};
+  const Share share = block_share(line, blockIdx.x, gridDim.x);
+  if (share.from >= share.to) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = lane % kLanes, sub = lane / kLanes;
+  for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
+    const int from = line.from(sg.req);
+    for (int t = sg.t0 + warp; t < sg.t1; t += 8) {
+      const int b = from + t, page = c.table[static_cast<int64_t>(sg.req) * c.table_stride + b];
+      if (!page_exists(c, page)) {
+        if (lane == 0) set_status(c.status, SLED_ERR_ARG);
+        continue;
       }
-    T* out = bounds + (static_cast<int64_t>(page) * c.Hkv + g) * 2 * H + lane * D;
+      const int count = min(c.ps, w.v.n - b * c.ps);
+      const uint4* k = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(c.k) + (static_cast<int64_t>(page) * c.Hkv + sg.g) * c.ps * H) + col;
+      uint32_t lo[4], hi[4];
+      {
+        const uint4 x = k[min(sub, count - 1) * kLanes];      // rows behind the last key repeat it
+        lo[0] = hi[0] = x.x; lo[1] = hi[1] = x.y; lo[2] = hi[2] = x.z; lo[3] = hi[3] = x.w;
+      }
+      for (int e = 0; e < count; e += 4 * kRows) {
+        uint4 x[4];
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      out[d] = from_f32<T>(nan[d] ? NAN : lo[d]);
-      out[H + d] = from_f32<T>(nan[d] ? NAN : hi[d]);
+        for (int z = 0; z < 4; ++z) x[z] = k[min(e + z * kRows + sub, count - 1) * kLanes];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          lo[0] = V::smaller(lo[0], x[z].x); lo[1] = V::smaller(lo[1], x[z].y); lo[2] = V::smaller(lo[2], x[z].z); lo[3] = V::smaller(lo[3], x[z].w);
+          hi[0] = V::larger(hi[0], x[z].x); hi[1] = V::larger(hi[1], x[z].y); hi[2] = V::larger(hi[2], x[z].z); hi[3] = V::larger(hi[3], x[z].w);
+        }
+      }
+#pragma unroll
+      for (int o = kLanes; o < 32; o <<= 1)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          lo[z] = V::smaller(lo[z], __shfl_xor_sync(0xffffffffu, lo[z], o));
+          hi[z] = V::larger(hi[z], __shfl_xor_sync(0xffffffffu, hi[z], o));
+        }
+      if (sub == 0) {
+        uint4* out = reinterpret_cast<uint4*>(bounds + (static_cast<int64_t>(page) * c.Hkv + sg.g) * 2 * H) + col;
+        out[0] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        out[kLanes] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      }
     }
-  }
+  });
 }
 
 // the larger of two scores; a NaN is the largest
@@ -67,6 +118,7 @@ struct ScoreLine {
   const PagedCache& c;
   const PagedRows& r;
   int n_blocks, n_local;
+  __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
   __device__ __forceinline__ int tokens() const { return max(1, kUnitRows / (r.Hq / c.Hkv)); }   // of a unit
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
@@ -79,7 +131,7 @@ struct ScoreLine {
     w.tiles = (blocks - n_local + 63) / 64;
     w.n_rb = (w.v.m + tokens() - 1) / tokens();
     w.units = w.n_rb * c.Hkv;
-    w.weight = tile_weight(min(w.v.m * (r.Hq / c.Hkv), kUnitRows));
+    w.weight = kMinShare;
     return w;
   }
 };
@@ -205,7 +257,7 @@ __global__ void __launch_bounds__(256) block_score_row_kernel(PagedCache c, Page
 constexpr int kMostCached = 8192;
 __global__ void __launch_bounds__(256) block_choice_kernel(PagedCache c, PagedRows r, int n_blocks, int n_local, const float* scores,
                                                            int32_t* list) {
-  __shared__ int hist[256], scratch[33], pick[2];
+  __shared__ int hist[2048], scratch[36];
   __shared__ uint32_t cached[kMostCached];
   pdl_launch_dependents();
   pdl_wait();
@@ -222,32 +274,38 @@ __global__ void __launch_bounds__(256) block_choice_kernel(PagedCache c, PagedRo
   }
   const int early = own + 1 - n_local, want = n_blocks - n_local;   // early > want
   const float* sc = scores + (static_cast<int64_t>(t) * c.Hkv + g) * c.table_cols;
-  for (int b = threadIdx.x; b < min(early, kMostCached) && want > 0; b += blockDim.x) cached[b] = rank_bits(sc[b]);
-  __syncthreads();
-  auto rank = [&](int b) { return b < kMostCached ? cached[b] : rank_bits(sc[b]); };
-  int greater = 0;
-  uint32_t edge = 0xffffffffu;
-  if (want > 0) edge = select_largest(rank, early, want, hist, pick, &greater);
-  int taken = 0, ties = 0;
-  const int tie_want = want - greater;
-  for (int b0 = 0; b0 < early && want > 0; b0 += blockDim.x) {
-    const int b = b0 + threadIdx.x;
-    const uint32_t x = b < early ? rank(b) : 0;
-    const bool tie = b < early && x == edge;
-    int n_tie, n_take;
-    const int tie_rank = ties + block_scan(tie, scratch, &n_tie);
-    const bool take = b < early && (x > edge || (tie && tie_rank < tie_want));
-    const int at = taken + block_scan(take, scratch, &n_take);
-    if (take) mine[at] = b;
-    taken += n_take;
-    ties += n_tie;
+  if (want > 0) {
+    for (int b = threadIdx.x; b < min(early, kMostCached); b += blockDim.x) cached[b] = rank_bits(sc[b]);
+    __syncthreads();
+    auto rank = [&](int b) { return b < kMostCached ? cached[b] : rank_bits(sc[b]); };
+    int greater = 0, total;
+    const uint32_t edge = select_largest(rank, early, want, hist, scratch, &greater);
+    const int missing = want - greater;
+    // a thread goes through a stretch of blocks, in order; before its first one come so many greater ones and equals
+    const int per = (early + blockDim.x - 1) / blockDim.x, b0 = min(static_cast<int>(threadIdx.x) * per, early), b1 = min(b0 + per, early);
+    int above = 0, ties = 0;
+    for (int b = b0; b < b1; ++b) {
+      const uint32_t x = rank(b);
+      above += x > edge;
+      ties += x == edge;
+    }
+    above = block_scan(above, scratch, &total);
+    ties = block_scan(ties, scratch, &total);
+    for (int b = b0; b < b1; ++b) {
+      const uint32_t x = rank(b);
+      if (x > edge || (x == edge && ties < missing)) mine[above + min(ties, missing)] = b;
+      above += x > edge;
+      ties += x == edge;
+    }
   }
   for (int b = threadIdx.x; b < n_local; b += blockDim.x) mine[want + b] = early + b;
 }
 
 template <typename T, int H>
 int bounds_typed(const PagedCache& c, const int32_t* first, void* bounds, cudaStream_t s) {
-  block_bounds_kernel<T, H><<<dim3(std::min(64, (c.table_cols * c.Hkv + 7) / 8), c.n_reqs), 256, 0, s>>>(c, first, static_cast<T*>(bounds));
+  int sms = 0;
+  if (paged_device(&sms) < 0) return -1;
+  SLED_LAUNCH_PDL((block_bounds_kernel<T, H>), dim3(8 * sms), dim3(256), 0, s, c, first, static_cast<T*>(bounds));
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 template <typename T, int H>

@@ -109,45 +109,43 @@ __device__ __forceinline__ int block_scan(int v, int* scratch, int* total) {
   return before + x - v;
 }
 
-// The want-th largest of n keys (1 <= want <= n), found digit by digit from the top: key(i) -> uint32_t.  *greater
-// receives how many keys are larger than the result.  hist: 256 words of shared memory, scratch: 2 words.  All threads
-// of the block call it.
+// An edge for the `want` largest of n keys (1 <= want <= n): they are the keys above it and, of those equal to it, as many
+// as are missing (want - *greater).  Found digit by digit from the top (11, 11 and 10 bits); it ends early where a digit
+// divides the keys as wanted.  key(i) -> uint32_t.  hist: 2048 words of shared memory, scratch: 36.  All threads of the
+// block (a power of two of them, 32 .. 1024) call it.
 template <typename KeyFn>
 __device__ __forceinline__ uint32_t select_largest(KeyFn key, int n, int want, int* hist, int* scratch, int* greater) {
   uint32_t prefix = 0, mask = 0;
   int above = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int b = threadIdx.x; b < 256; b += blockDim.x) hist[b] = 0;
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048, per = bins / static_cast<int>(blockDim.x);
+    for (int b = threadIdx.x; b < bins; b += blockDim.x) hist[b] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
       const uint32_t x = key(i);
-      if ((x & mask) == prefix) atomicAdd(&hist[(x >> shift) & 255], 1);
+      if ((x & mask) == prefix) atomicAdd(&hist[(x >> shift) & (bins - 1)], 1);
     }
     __syncthreads();
-    if (threadIdx.x < 32) {   // lane b owns digits 8b .. 8b+7, counted from the top
-      const int lane = threadIdx.x, top = 255 - 8 * lane;
-      int own = 0;
-#pragma unroll
-      for (int d = 0; d < 8; ++d) own += hist[top - d];
-      int incl = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
-      }
-      int run = above + incl - own;
-      if (run < want && run + own >= want) {
-        for (int d = 0; d < 8; ++d) {
-          const int c = hist[top - d];
-          if (run + c >= want) { scratch[0] = top - d; scratch[1] = run; break; }
-          run += c;
-        }
+    const int top = bins - 1 - static_cast<int>(threadIdx.x) * per;   // this thread's digits, counted from the top
+    int own = 0, total;
+    for (int d = 0; d < per; ++d) own += hist[top - d];
+    int run = above + block_scan(own, scratch, &total);
+    if (run < want && run + own >= want) {
+      for (int d = 0; d < per; ++d) {
+        const int c = hist[top - d];
+        if (run + c >= want) { scratch[33] = top - d; scratch[34] = run; scratch[35] = c; break; }
+        run += c;
       }
     }
     __syncthreads();
-    prefix |= static_cast<uint32_t>(scratch[0]) << shift;
-    mask |= 255u << shift;
-    above = scratch[1];
+    prefix |= static_cast<uint32_t>(scratch[33]) << shift;
+    mask |= static_cast<uint32_t>(bins - 1) << shift;
+    above = scratch[34];
+    if (above + scratch[35] == want && prefix != 0) {   // everything that begins like this is wanted
+      *greater = want;
+      return prefix - 1;
+    }
     __syncthreads();
   }
   *greater = above;

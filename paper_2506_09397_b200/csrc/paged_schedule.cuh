@@ -13,7 +13,7 @@
 namespace sled {
 
 constexpr int kTile = 64;        // keys per tile
-constexpr int kUnitRows = 64;    // query rows of a unit at most
+constexpr int kUnitRows = 64;    // query rows of a unit at most (tensor cores)
 
 // one request's share of the line
 struct ReqWork {
@@ -37,6 +37,8 @@ struct AttentionLine {
   const PagedCache& c;
   const PagedRows& r;
   int list_len;
+  int unit_rows = kUnitRows, tile = kTile;
+  __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
     w.v = req_view(c, r, i);
@@ -47,10 +49,10 @@ struct AttentionLine {
     const int rows = list_len > 0 ? group : w.v.m * group;
     int keys = w.v.n;
     if (list_len > 0) keys = min(list_len, (w.v.n - 1) / c.ps + 1) * c.ps;
-    w.tiles = (keys + kTile - 1) / kTile;
-    w.n_rb = list_len == kWholeRows ? 1 : (rows + kUnitRows - 1) / kUnitRows;
+    w.tiles = (keys + tile - 1) / tile;
+    w.n_rb = list_len == kWholeRows ? 1 : (rows + unit_rows - 1) / unit_rows;
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
-    w.weight = list_len == kWholeRows ? min(rows, kMinShare - 1) : tile_weight(min(rows, kUnitRows));
+    w.weight = list_len == kWholeRows ? min(rows, kMinShare - 1) : unit_rows == kUnitRows ? tile_weight(min(rows, kUnitRows)) : 8 + min(rows, unit_rows);
     return w;
   }
 };
@@ -58,24 +60,29 @@ struct AttentionLine {
 struct Share {
   int req;               // first request
   long long at;          // where it begins on the line
-  long long from, to;    // this block's part of the line
+  long long from, to;    // this share's part of the line
   long long total;
-  int n_blocks;          // blocks that share the line: every one of them gets a tile
+  int count;             // shares that the line is cut into: every one of them gets a tile
 };
 
-// All threads of the block call it (blockDim.x a multiple of 32, at most 1024).  Block 0 reports requests left out.
-template <typename Line>
-__device__ __forceinline__ Share block_share(const Line& line, int block, int max_blocks) {
+// quotient of numbers that mostly fit 32 bits
+__device__ __forceinline__ long long divide(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
+
+// Shares `first`, .. `first` + kShares - 1 of at most `most`, into out[] (shared memory).  All threads of the block call it
+// (blockDim.x a multiple of 32, at most 1024).  The block with share 0 reports the requests that are left out.
+template <int kShares, typename Line>
+__device__ __forceinline__ void block_shares(const Line& line, int first, int most, Share* out) {
   __shared__ long long sums[33];
-  __shared__ Share mine;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
   const int n_reqs = line.c.n_reqs, per = (n_reqs + blockDim.x - 1) / blockDim.x;
-  const int first = min(static_cast<int>(threadIdx.x) * per, n_reqs), last = min(first + per, n_reqs);
+  const int i0 = min(static_cast<int>(threadIdx.x) * per, n_reqs), i1 = min(i0 + per, n_reqs);
   long long own = 0;
-  for (int i = first; i < last; ++i) {
+  for (int i = i0; i < i1; ++i) {
     const ReqWork w = line(i);
     own += w.cost();
-    if (block == 0 && !w.v.ok) set_status(line.c.status, req_fault(line.r, w.v));
+    if (first == 0 && !w.v.ok) set_status(line.c.status, line.fault(w.v));
   }
   long long x = own;
 #pragma unroll
@@ -84,33 +91,46 @@ __device__ __forceinline__ Share block_share(const Line& line, int block, int ma
     if (lane >= o) x += y;
   }
   if (lane == 31) sums[warp] = x;
-  if (threadIdx.x == 0) mine = Share{0, 0, 0, 0, 0, 1};
+  if (threadIdx.x < kShares) out[threadIdx.x] = Share{0, 0, 0, 0, 0, 1};
   __syncthreads();
   long long before = 0, total = 0;
   for (int k = 0; k < nw; ++k) {
     if (k < warp) before += sums[k];
     total += sums[k];
   }
-  long long at = before + x - own;
   // a part of the line that is longer than any tile holds the beginning of one
-  const int n_blocks = static_cast<int>(max(1LL, min(static_cast<long long>(max_blocks), total / kMinShare)));
-  const long long from = block < n_blocks ? total * block / n_blocks : 0, to = block < n_blocks ? total * (block + 1) / n_blocks : 0;
-  if (from < to && at <= from && from < at + own) {
-    int i = first;
-    for (;; ++i) {
-      const long long cost = line(i).cost();
-      if (from < at + cost) break;
-      at += cost;
+  const int count = static_cast<int>(max(1LL, min(static_cast<long long>(most), total / kMinShare)));
+  const long long each = divide(total, count), rest = total - each * count;   // the first `rest` shares are one longer
+  long long at = before + x - own;
+  const long long end = at + own;
+#pragma unroll
+  for (int k = 0; k < kShares; ++k) {
+    const int mine = first + k;
+    const long long from = each * mine + min(static_cast<long long>(mine), rest), to = from + each + (mine < rest);
+    if (mine < count && from < to && at <= from && from < end) {
+      long long begin = at;
+      int i = i0;
+      for (;; ++i) {
+        const long long cost = line(i).cost();
+        if (from < begin + cost) break;
+        begin += cost;
+      }
+      out[k] = Share{i, begin, from, to, total, count};
     }
-    mine = Share{i, at, from, to, total, n_blocks};
   }
   __syncthreads();
+}
+template <typename Line>
+__device__ __forceinline__ Share block_share(const Line& line, int block, int most) {
+  __shared__ Share mine;
+  block_shares<1>(line, block, most, &mine);
   return mine;
 }
 
-// the block that owns the tile which begins at `at`
-__device__ __forceinline__ int owner_of(long long at, long long total, int n_blocks) {
-  return static_cast<int>(((at + 1) * n_blocks - 1) / total);
+// the share that owns the tile which begins at `at`
+__device__ __forceinline__ int owner_of(long long at, const Share& s) {
+  const long long each = divide(s.total, s.count), rest = s.total - each * s.count, longer = (each + 1) * rest;
+  return static_cast<int>(at < longer ? divide(at, each + 1) : rest + divide(at - longer, each));
 }
 
 // A stretch of one unit that a block works on.
@@ -131,9 +151,9 @@ __device__ __forceinline__ void for_segments(const Line& line, const Share& s, i
     const ReqWork w = line(i);
     const long long cost = w.cost();
     if (cost == 0) continue;
-    const long long lt_end = min(w.count(), (s.to - at + w.weight - 1) / w.weight);
-    for (long long lt = s.from > at ? (s.from - at + w.weight - 1) / w.weight : 0; lt < lt_end;) {
-      const int u = static_cast<int>(lt / w.tiles);
+    const long long lt_end = min(w.count(), divide(s.to - at + w.weight - 1, w.weight));
+    for (long long lt = s.from > at ? divide(s.from - at + w.weight - 1, w.weight) : 0; lt < lt_end;) {
+      const int u = static_cast<int>(divide(lt, w.tiles));
       Segment g;
       g.req = i;
       g.t0 = static_cast<int>(lt - static_cast<long long>(u) * w.tiles);
@@ -145,7 +165,7 @@ __device__ __forceinline__ void for_segments(const Line& line, const Share& s, i
       g.slot = 2 * block + (first ? 0 : 1);
       g.last_block = -1;
       if (g.t0 == 0 && !g.whole)
-        g.last_block = owner_of(at + ((static_cast<long long>(u) + 1) * w.tiles - 1) * w.weight, s.total, s.n_blocks);
+        g.last_block = owner_of(at + ((static_cast<long long>(u) + 1) * w.tiles - 1) * w.weight, s);
       f(w, g);
       first = false;
       lt += g.t1 - g.t0;
