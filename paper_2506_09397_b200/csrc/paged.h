@@ -49,6 +49,12 @@ int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_
 constexpr int kMaxPagedBlocks = 320;   // two on each of up to 160 SMs
 int64_t paged_mma_workspace(int h);
 int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s);
+// the same on the 5th-generation tensor cores, for requests with many query rows
+int64_t paged_tc_workspace(int h);
+int launch_paged_tc(const PagedCache& c, const PagedRows& r, float* scores, char* ws, cudaStream_t s);
+// joins the partial results of units of unit_rows rows that were cut in tiles of `tile` keys over `blocks` blocks
+int launch_paged_merge(const PagedCache& c, const PagedRows& r, int list_len, int unit_rows, int tile, int blocks, float* acc, float* ml,
+                       int4* desc, cudaStream_t s);
 // the number of SMs of the current device, or a negative value
 int paged_device(int* sms);
 // bounds[page][Hkv][2][h] of the pages that hold the keys first[i] .. n_kv[i]-1 (first null: all keys)

@@ -179,6 +179,13 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
   });
 }
 
+// Rows per request (on average) above which the tcgen05 kernel is used.
+constexpr int kTcRows = 24;
+int64_t parts_bytes(int h) {
+  const int64_t a = paged_mma_workspace(h), b = paged_tc_workspace(h);
+  return ((a > b ? a : b) + 255) / 256 * 256;
+}
+
 // Scores are kept where they take no more than this; otherwise the weights are computed from the keys again.
 constexpr int64_t kMostScoreBytes = 512LL << 20;
 bool keeps_scores(int dtype, int h, int64_t rows_heads, int64_t keys) {
@@ -191,8 +198,10 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
   if (sizeof(T) == 2 && H >= 64) {
     const int64_t keys = static_cast<int64_t>(c.table_cols) * c.ps;
     const bool keep = key_weights && keeps_scores(c.dtype, H, static_cast<int64_t>(r.T) * r.Hq, keys);
-    float* scores = keep ? reinterpret_cast<float*>(ws + (paged_mma_workspace(H) + 255) / 256 * 256) : nullptr;
-    n = launch_paged_mma(c, r, list, list_len, scores, ws, s);
+    float* scores = keep ? reinterpret_cast<float*>(ws + parts_bytes(H)) : nullptr;
+    // many rows per request: the tcgen05 kernel
+    if (!list && static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kTcRows) * c.n_reqs) n = launch_paged_tc(c, r, scores, ws, s);
+    else n = launch_paged_mma(c, r, list, list_len, scores, ws, s);
     if (n < 0) return n;
     if (keep) {
       int sms = 0;
@@ -214,7 +223,7 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
 
 int64_t paged_attention_workspace(int dtype, int h, int64_t rows_heads, int64_t keys, bool weigh) {
   if (dtype != 1 || h < 64) return 0;
-  return (paged_mma_workspace(h) + 255) / 256 * 256 + (weigh && keeps_scores(dtype, h, rows_heads, keys) ? rows_heads * keys * 4 : 0);
+  return parts_bytes(h) + (weigh && keeps_scores(dtype, h, rows_heads, keys) ? rows_heads * keys * 4 : 0);
 }
 
 int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,

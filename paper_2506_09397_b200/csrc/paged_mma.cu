@@ -356,23 +356,24 @@ __device__ __forceinline__ void consume(const PagedCache& c, const PagedRows& r,
   }
 }
 
-__device__ __forceinline__ UnitRows unit_rows(const PagedCache& c, const PagedRows& r, int list_len, const ReqWork& w, const Segment& sg) {
+__device__ __forceinline__ UnitRows unit_rows(const PagedCache& c, const PagedRows& r, int list_len, const ReqWork& w, const Segment& sg,
+                                              int rows = kUnitRows) {
   UnitRows u;
   u.req = sg.req;
   u.row0 = w.v.row0;
   u.m = w.v.m;
   u.group = r.Hq / c.Hkv;
   u.g = sg.g;
-  u.first = sg.rb * kUnitRows;
+  u.first = sg.rb * rows;
   if (list_len > 0) {
     u.j = sg.j;
-    u.count = min(kUnitRows, u.group - u.first);
+    u.count = min(rows, u.group - u.first);
     const int x = w.v.n - w.v.m + sg.j, own = x / c.ps;   // the last chosen block is the token's own
     u.end = (min(list_len, own + 1) - 1) * c.ps + x - own * c.ps + 1;
     u.prefix = u.end;
   } else {
     u.j = -1;
-    u.count = min(kUnitRows, w.v.m * u.group - u.first);
+    u.count = min(rows, w.v.m * u.group - u.first);
     u.end = w.v.n;
     u.prefix = w.v.n - w.v.m;
   }
@@ -493,21 +494,22 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
 
 // The partial results of the units that were cut.  Block b finishes the one that block b began, a warp per row.
 template <int H>
-__global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, const PagedRows r, int list_len, const Parts parts) {
+__global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, const PagedRows r, int list_len, int unit, int tile,
+                                                          const Parts parts) {
   pdl_wait();
   const int4 d = parts.desc[blockIdx.x];
   if (d.x < 0) return;
   constexpr int D = H / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const ReqWork w = AttentionLine{c, r, list_len}(d.z);
+  const ReqWork w = AttentionLine{c, r, list_len, unit, tile}(d.z);
   Segment sg{};
   sg.req = d.z;
   sg.rb = d.w % w.n_rb;
   sg.g = d.w / w.n_rb % c.Hkv;
   sg.j = d.w / w.n_rb / c.Hkv;
-  const UnitRows u = unit_rows(c, r, list_len, w, sg);
+  const UnitRows u = unit_rows(c, r, list_len, w, sg, unit);
   const int n_parts = d.x - static_cast<int>(blockIdx.x) + 1;
-  auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? d.y : 2 * (blockIdx.x + p)) * kUnitRows; };
+  auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? d.y : 2 * (blockIdx.x + p)) * unit; };
   for (int row = blockIdx.y * 16 + warp; row < u.count; row += gridDim.y * 16) {
     float M = -INFINITY;
     bool nan = false;
@@ -589,11 +591,21 @@ int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int l
   parts.scores = scores;
   parts.keys = static_cast<int64_t>(c.table_cols) * c.ps;
   SLED_LAUNCH_PDL(paged_mma_kernel<H>, dim3(blocks), dim3(160), Smem<H>::kTotal, s, c, r, list, list_len, parts, map_k, map_v);
-  SLED_LAUNCH_PDL(paged_merge_kernel<H>, dim3(blocks, 2), dim3(512), 0, s, c, r, list_len, parts);
-  return cudaGetLastError() == cudaSuccess ? 2 : -1;
+  if (cudaGetLastError() != cudaSuccess) return -1;
+  const int n = launch_paged_merge(c, r, list_len, kUnitRows, kTile, blocks, parts.acc, parts.ml, parts.desc, s);
+  return n < 0 ? n : n + 1;
 }
 
 }  // namespace
+
+int launch_paged_merge(const PagedCache& c, const PagedRows& r, int list_len, int unit_rows, int tile, int blocks, float* acc, float* ml,
+                       int4* desc, cudaStream_t s) {
+  const Parts parts{acc, ml, desc, nullptr, 0};
+  const dim3 grid(blocks, unit_rows > kUnitRows ? 4 : 2);
+  if (c.h == 128) SLED_LAUNCH_PDL(paged_merge_kernel<128>, grid, dim3(512), 0, s, c, r, list_len, unit_rows, tile, parts);
+  else SLED_LAUNCH_PDL(paged_merge_kernel<64>, grid, dim3(512), 0, s, c, r, list_len, unit_rows, tile, parts);
+  return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
 
 int64_t paged_mma_workspace(int h) {
   return 2LL * kMaxPagedBlocks * kUnitRows * (h + 2) * 4 + kMaxPagedBlocks * 16LL;

@@ -52,7 +52,10 @@ struct AttentionLine {
     w.tiles = (keys + tile - 1) / tile;
     w.n_rb = list_len == kWholeRows ? 1 : (rows + unit_rows - 1) / unit_rows;
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
-    w.weight = list_len == kWholeRows ? min(rows, kMinShare - 1) : unit_rows == kUnitRows ? tile_weight(min(rows, kUnitRows)) : 8 + min(rows, unit_rows);
+    w.weight = list_len == kWholeRows ? min(rows, kMinShare - 1)
+               : unit_rows == kUnitRows ? tile_weight(min(rows, kUnitRows))
+               : unit_rows > kUnitRows  ? (rows > unit_rows / 2 ? 20 : 16)
+                                        : 8 + min(rows, unit_rows);
     return w;
   }
 };
