@@ -54,6 +54,9 @@ int tma_map_bf16_rows(CUtensorMap* map, const void* dev_ptr, long long rows, int
 // the same array with all its columns in one box: coordinates {column within 64, row, column / 64}, the box lands as
 // [cols / 64][box_rows][64 columns], 128-byte swizzle
 int tma_map_bf16_row_groups(CUtensorMap* map, const void* dev_ptr, long long rows, int cols, int box_rows);
+// the same array as groups of eight rows: coordinates {column within 64, row within 8, column / 64, row / 8}; the box, 16
+// rows with all their columns, lands as [2][cols / 64][8 rows][64 columns], 128-byte swizzle.  rows: a multiple of 16
+int tma_map_bf16_row_octets(CUtensorMap* map, const void* dev_ptr, long long rows, int cols);
 // Bytes of the tiled copy of an [N][K] matrix, and its construction from the row-major matrix (both in
 // device memory; `tiled` 16-byte aligned, tc_weight_tiled_bytes(N, K) long).  The row-major copy is not
 // needed afterwards.  Synchronises the device.

@@ -145,36 +145,55 @@ struct Segment {
   int last_block;        // cut units, where t0 == 0: the block that ends the unit; -1 otherwise
 };
 
-// Calls f(work of the request, segment) for every segment of the share, in order.
+// The segments of a share, in order.
+template <typename Line>
+struct Walk {
+  const Line& line;
+  const Share& s;
+  int block, i;
+  long long at, lt = 0, lt_end = 0;
+  ReqWork w;               // of the current segment's request
+  bool first = true, fresh = true;
+  __device__ __forceinline__ Walk(const Line& l, const Share& share, int b) : line(l), s(share), block(b), i(share.req), at(share.at) {
+    w.tiles = 1;
+    w.units = 0;
+    w.weight = 1;
+  }
+  __device__ __forceinline__ bool next(Segment& g) {
+    while (lt >= lt_end) {
+      if (!fresh) {
+        at += w.cost();
+        ++i;
+      }
+      fresh = false;
+      if (at >= s.to) return false;
+      w = line(i);
+      lt_end = min(w.count(), divide(s.to - at + w.weight - 1, w.weight));
+      lt = s.from > at ? divide(s.from - at + w.weight - 1, w.weight) : 0;
+    }
+    const int u = static_cast<int>(divide(lt, w.tiles));
+    g.req = i;
+    g.t0 = static_cast<int>(lt - static_cast<long long>(u) * w.tiles);
+    g.t1 = static_cast<int>(min(static_cast<long long>(w.tiles), g.t0 + (lt_end - lt)));
+    g.rb = u % w.n_rb;
+    g.g = u / w.n_rb % line.c.Hkv;
+    g.j = u / w.n_rb / line.c.Hkv;
+    g.whole = g.t0 == 0 && g.t1 == w.tiles;
+    g.slot = 2 * block + (first ? 0 : 1);
+    g.last_block = -1;
+    if (g.t0 == 0 && !g.whole) g.last_block = owner_of(at + ((static_cast<long long>(u) + 1) * w.tiles - 1) * w.weight, s);
+    first = false;
+    lt += g.t1 - g.t0;
+    return true;
+  }
+};
+
+// Calls f(work of the request, segment) for every segment of the share.
 template <typename Line, typename F>
 __device__ __forceinline__ void for_segments(const Line& line, const Share& s, int block, F f) {
-  long long at = s.at;
-  bool first = true;
-  for (int i = s.req; at < s.to; ++i) {
-    const ReqWork w = line(i);
-    const long long cost = w.cost();
-    if (cost == 0) continue;
-    const long long lt_end = min(w.count(), divide(s.to - at + w.weight - 1, w.weight));
-    for (long long lt = s.from > at ? divide(s.from - at + w.weight - 1, w.weight) : 0; lt < lt_end;) {
-      const int u = static_cast<int>(divide(lt, w.tiles));
-      Segment g;
-      g.req = i;
-      g.t0 = static_cast<int>(lt - static_cast<long long>(u) * w.tiles);
-      g.t1 = static_cast<int>(min(static_cast<long long>(w.tiles), g.t0 + (lt_end - lt)));
-      g.rb = u % w.n_rb;
-      g.g = u / w.n_rb % line.c.Hkv;
-      g.j = u / w.n_rb / line.c.Hkv;
-      g.whole = g.t0 == 0 && g.t1 == w.tiles;
-      g.slot = 2 * block + (first ? 0 : 1);
-      g.last_block = -1;
-      if (g.t0 == 0 && !g.whole)
-        g.last_block = owner_of(at + ((static_cast<long long>(u) + 1) * w.tiles - 1) * w.weight, s);
-      f(w, g);
-      first = false;
-      lt += g.t1 - g.t0;
-    }
-    at += cost;
-  }
+  Walk<Line> walk(line, s, block);
+  Segment g;
+  while (walk.next(g)) f(walk.w, g);
 }
 
 }  // namespace sled

@@ -13,8 +13,8 @@
 // it by more than 8 (in units of log2: harmless for bf16 probabilities and fp32 sums, and it cancels in the end), which
 // means rescaling the row of O in tensor memory and happens in a unit's first tiles.
 //   warps 0-3, 4-7 : softmax and output of the two groups
-//   warp 8         : TMA, three K and two V tiles under way (one block per SM)
-//   warp 9         : tensor-memory allocation, products (one thread)
+//   warps 8, 10    : TMA of K and of V (one block per SM)
+//   warp 9         : tensor-memory allocation, products (one thread); warp 11 only completes the warpgroup
 // The work is shared out as paged_schedule.cuh says.  What binds: the bytes of K and V up to 128 rows, the exponentials
 // (16 a clock and SM) above.  Every wait is bounded; when one runs out the block says so in *status, lets what is under
 // way land, frees its tensor memory and returns.
@@ -32,43 +32,37 @@ constexpr float kRaiseBy = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 
-template <int H>
+// kGroups: softmax groups that have rows of their own in the largest unit (1: units of up to 128 rows, 2: up to 256).
+// K, V and Q lie in groups of eight rows, [H / 64][8 rows][64 columns], as a copy of 16 cached keys leaves them.
+template <int H, int kGroups>
 struct Tc {
   static constexpr int kHalves = H / 64;
-  static constexpr int kHalf = kKeys * 128;              // [128 rows][64 columns]: 16 KB
-  static constexpr int kTileBytes = kHalves * kHalf;     // K, V or 128 rows of Q
-  static constexpr int kKStages = H == 128 ? 3 : 5, kVStages = H == 128 ? 2 : 4;
-  static constexpr int kOffQ = 0;                        // two groups of rows; the second also carries the merge
+  static constexpr int kOctet = kHalves * 1024;          // eight rows
+  static constexpr int kTileBytes = 16 * kOctet;         // K, V or 128 rows of Q
+  static constexpr int kKStages = H == 64 ? 5 : 3, kVStages = H == 64 ? 4 : 2;
+  // Q of 256 rows, or of two units of 128: the next unit's is brought in under the end of one.  The merge of a unit's
+  // groups takes place in the unit's own Q, which is done with by then.
+  static constexpr int kOffQ = 0;
   static constexpr int kOffK = 2 * kTileBytes;
   static constexpr int kOffV = kOffK + kKStages * kTileBytes;
   static constexpr int kOffBar = kOffV + kVStages * kTileBytes;
-  static constexpr int kTotal = kOffBar + 256 + 1024;    // alignment slack
+  static constexpr int kOffTree = kOffBar + 256;         // parents of the nodes, one byte each, of two units
+  static constexpr int kOffTop = kOffTree + 2 * kMaxTreeNodes;   // row maxima and sums of the merge
+  static constexpr int kTotal = kOffTop + 2 * kGroupRows * 4 + 1024;   // alignment slack
 };
-static_assert(Tc<128>::kTotal + 1024 <= 227 * 1024 && Tc<64>::kTotal + 1024 <= 227 * 1024, "shared memory of one block");
+static_assert(kMaxTreeNodes == 128);
+static_assert(Tc<128, 1>::kTotal + 512 <= 227 * 1024 && Tc<64, 1>::kTotal + 512 <= 227 * 1024, "shared memory of one block");
 
 // barriers, 8 bytes each
 enum { B_KFULL = 0, B_KEMPTY = 5, B_VFULL = 10, B_VEMPTY = 14, B_QFULL = 18, B_SFULL = 19, B_PFULL = 21, B_ODONE = 23, B_COUNT = 25 };
 static_assert(B_COUNT * 8 + 4 <= 256);
 
-// bounded wait of the single-thread roles: they share their schedulers with softmax warps and sleep between polls
-__device__ __forceinline__ bool mbar_wait_idle(uint32_t bar, uint32_t parity, volatile int* stop) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const long long t0 = clock64();
-  for (;;) {
-    __nanosleep(20);
-    if (mbar_try_wait(bar, parity)) return true;
-    if (*stop != 0 || clock64() - t0 > kWaitCycles) return false;
-  }
-}
-
-// Operand descriptors, 128-byte swizzle, rows of 128 bytes, groups of 8 rows 1024 bytes apart.  K-major: the contraction
+// Operand descriptors, 128-byte swizzle, rows of 128 bytes, groups of 8 rows `octet` bytes apart.  K-major: the contraction
 // runs along a row (Q, K).  MN-major: down the rows (V); the leading offset is the distance to the next 64 columns.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t leading) {
-  return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | (static_cast<uint64_t>(leading) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) |
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t leading, uint32_t octet) {
+  return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | (static_cast<uint64_t>(leading) << 16) | (static_cast<uint64_t>(octet >> 4) << 32) |
          (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
 }
-__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr) { return operand_desc(addr, 1); }
-__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr, uint32_t leading_bytes) { return operand_desc(addr, leading_bytes >> 4); }
 
 __device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -92,29 +86,51 @@ __device__ __forceinline__ void umma_commit(uint32_t bar) {
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint64_t policy) {
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int octet, uint32_t bar, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0], [%1, {%3, %4}], [%2], %5;"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "l"(policy)
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%3, %3, %3, %4}], [%2], %5;"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(octet), "l"(policy)
       : "memory");
 }
+__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int octet) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %1, %1, %2}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(octet) : "memory");
+}
 
-// 32 consecutive columns of this warp's 32 lanes (thread = lane)
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float* v) {
-  uint32_t r[32];
+// 32 consecutive columns of this warp's 32 lanes (thread = lane); the values may be used after tmem_ld_wait()
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t addr, float* v) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15,"
-      " %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(addr)
-      : "memory");
+      " %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
+        "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(addr));
+}
+// the registers are named so that no use of them moves ahead of the wait
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait(float* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+  for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float* v) {
+  tmem_ld32_nowait(addr, v);
+  tmem_ld_wait<32>(v);
+}
+// two products at a time
+__device__ __forceinline__ void fma2(float& a, float& b, float scale, float add) {
+  asm("{\n\t.reg .b64 x, y, z;\n\t"
+      "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(a), "+f"(b) : "f"(scale), "f"(add));
+}
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
+  asm("{\n\t.reg .b64 p, q;\n\t"
+      "mov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\t"
+      "add.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}"
+      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* v) {
   asm volatile(
@@ -126,8 +142,8 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* v) {
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 struct TcParts {
-  float* acc;      // [2 * blocks][256][H], not normalised
-  float* ml;       // [2 * blocks][256][2]
+  float* acc;      // [2 * blocks][rows of a unit][H], not normalised
+  float* ml;       // [2 * blocks][rows of a unit][2]
   int4* desc;      // [blocks] {last block or -1, first slot, request, unit of the request}
   float* scores;   // null, or [rows][Hq][keys]
   int64_t keys;
@@ -162,23 +178,35 @@ struct RowView {
   }
 };
 
-template <int H>
-__global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, const PagedRows r, const TcParts parts,
+// a unit, or the stretch of it that the block works on
+struct TcUnit {
+  Segment sg;
+  int row0, m, n, n_rb;
+};
+
+template <int H, int kGroups>
+__global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, const PagedRows r, const TcParts parts,
                                                           const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  using L = Tc<H>;
+  using L = Tc<H, kGroups>;
+  constexpr int kUnit = kGroups * kGroupRows;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ int stop_word, odd_word;                // odd: a key of this unit's last tiles has a value that is not finite
-  __shared__ int32_t parent[kMaxTreeNodes];
+  __shared__ int stop_word;
+  __shared__ int odd_words[2];           // a key of the unit's last tiles has a value that is not finite
+  __shared__ int unused_words[2];        // the unit's tree has unused nodes
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* ptr = smem_raw + (base - raw);
   volatile int* stop = &stop_word;
-  volatile int* odd = &odd_word;
+  volatile int* odd = odd_words;
+  volatile int* unused = unused_words;
+  signed char* parents = reinterpret_cast<signed char*>(ptr + L::kOffTree);
+  float* tops = reinterpret_cast<float*>(ptr + L::kOffTop);
+  float* sums = tops + kGroupRows;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ptr + L::kOffBar + 8 * B_COUNT);
   auto bar = [&](int i) { return base + L::kOffBar + 8u * static_cast<uint32_t>(i); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    *stop = 0;
+    *stop = odd[0] = odd[1] = unused[0] = unused[1] = 0;
     for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 1); mbar_init(bar(B_KEMPTY + s), 1); }
     for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 1); mbar_init(bar(B_VEMPTY + s), 1); }
     mbar_init(bar(B_QFULL), 8);
@@ -201,206 +229,250 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
   fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_wait();
-  const AttentionLine line{c, r, 0, 2 * kGroupRows, kKeys};
+  const AttentionLine line{c, r, 0, kUnit, kKeys};
   const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (threadIdx.x == 0) parts.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
 
-  if (warp == 8) {
-    // ------------------------------------------------------------------------------------------------ TMA
-    const uint64_t policy = policy_evict_first();
-    const int cpp = c.ps / 16;
-    int ik = 0, iv = 0;
-    for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
-      const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
-      const int groups = (w.v.n + 15) / 16, n_tiles = sg.t1 - sg.t0;
-      // lane l looks up the 16-key groups l & 7 of the tiles (l >> 3), four tiles at a time
-      auto rows_of = [&](int t) {
-        const int e = t * 8 + lane;
-        if (e >= groups || e >= sg.t1 * 8) return 0;
-        const int b = e / cpp;
-        return (checked_page(c, table[b]) * c.Hkv + sg.g) * c.ps + (e - b * cpp) * 16;
-      };
-      auto load = [&](int t, int rows, int t_rows, const CUtensorMap* map, uint32_t dst, uint32_t full) {
-        const int n_here = min(8, groups - t * 8);
-        if (lane == 0) mbar_expect(full, n_here * 16 * H * 2);
-#pragma unroll
-        for (int p = 0; p < 8; ++p) {
-          const int y = __shfl_sync(0xffffffffu, rows, (t - t_rows) * 8 + p);
-          if (lane == 0 && p < n_here)
-#pragma unroll
-            for (int hh = 0; hh < L::kHalves; ++hh) tma_load_2d(dst + hh * L::kHalf + p * 2048, map, hh * 64, y, full, policy);
+  // The registers of the block, 384 x 168, go where they are needed: 4 warps x 88, 8 warps x 200 (62,464 of 64,512).
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 8 || warp == 10) {
+      // ------------------------------------------------------------------------------------------------ TMA: K, V
+      const bool is_k = warp == 8;
+      const CUtensorMap* map = is_k ? &map_k : &map_v;
+      const uint32_t ring = base + (is_k ? L::kOffK : L::kOffV);
+      const int stages = is_k ? L::kKStages : L::kVStages, b_full = is_k ? B_KFULL : B_VFULL, b_empty = is_k ? B_KEMPTY : B_VEMPTY;
+      const uint64_t policy = policy_evict_first();
+      const int cpp = c.ps / 16;
+      int st = 0, phase = 1;
+      for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
+        const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
+        const int groups = min((w.v.n + 15) / 16, sg.t1 * 8);     // 16-key groups up to the end of the segment
+        auto octet_of = [&](int e) {                              // where group e begins, in rows / 8
+          if (e >= groups) return 0;
+          const int b = e / cpp;
+          return ((checked_page(c, table[b]) * c.Hkv + sg.g) * c.ps + (e - b * cpp) * 16) >> 3;
+        };
+        // lane l looks after group l of four tiles; what comes after them is asked into L2, since shared memory holds too
+        // little to cover the latency of DRAM while tiles wait for their softmax
+        int octet = octet_of(sg.t0 * 8 + lane), later = 0;
+        for (int t = sg.t0; t < sg.t1; ++t) {
+          const int ahead = (t - sg.t0) & 3;
+          if (ahead == 0) {
+            if (t > sg.t0) octet = later;
+            later = octet_of((t + 4) * 8 + lane);
+            if ((t + 4) * 8 + lane < groups) tma_prefetch_4d(map, later);
+          }
+          bool ok = true;
+          if (lane == 0) ok = !*stop && mbar_wait(bar(b_empty + st), phase, stop);
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) { *stop = 1; return; }
+          const int n_here = min(8, groups - t * 8);
+          if (lane == 0) mbar_expect(bar(b_full + st), n_here * 16 * H * 2);
+          __syncwarp();
+          if ((lane >> 3) == ahead && (lane & 7) < n_here)
+            tma_load_4d(ring + st * L::kTileBytes + (lane & 7) * 2 * L::kOctet, map, octet, bar(b_full + st), policy);
+          if (++st == stages) { st = 0; phase ^= 1; }
         }
-      };
-      auto wait = [&](uint32_t b, uint32_t parity) {
-        bool ok = true;
-        if (lane == 0) ok = !*stop && mbar_wait_idle(b, parity, stop);
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) *stop = 1;
-        return ok;
-      };
-      // K runs one tile ahead of V: the order in which they are needed
-      int k_rows = 0, v_rows = 0, k_at = -4, v_at = -4;
-      for (int t = 0; t <= n_tiles; ++t) {
-        if (t < n_tiles) {
-          if (t - k_at >= 4) { k_at = t; k_rows = rows_of(sg.t0 + t); }
-          const int st = ik % L::kKStages;
-          if (!wait(bar(B_KEMPTY + st), ((ik / L::kKStages) & 1) ^ 1)) return;
-          load(sg.t0 + t, k_rows, sg.t0 + k_at, &map_k, base + L::kOffK + st * L::kTileBytes, bar(B_KFULL + st));
-          ++ik;
-        }
-        if (t > 0) {
-          if (t - 1 - v_at >= 4) { v_at = t - 1; v_rows = rows_of(sg.t0 + t - 1); }
-          const int st = iv % L::kVStages;
-          if (!wait(bar(B_VEMPTY + st), ((iv / L::kVStages) & 1) ^ 1)) return;
-          load(sg.t0 + t - 1, v_rows, sg.t0 + v_at, &map_v, base + L::kOffV + st * L::kTileBytes, bar(B_VFULL + st));
-          ++iv;
-        }
-      }
-    });
-  } else if (warp == 9) {
-    // ------------------------------------------------------------------------------------------------ products
-    if (lane == 0) {
+      });
+    } else if (warp == 9 && lane == 0) {
+      // ------------------------------------------------------------------------------------------------ products
       constexpr uint32_t kFormat = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(128 >> 4) << 24);   // fp32 += bf16 x bf16, M 128
       constexpr uint32_t idesc_s = kFormat | (static_cast<uint32_t>(kKeys >> 3) << 17);
       constexpr uint32_t idesc_o = kFormat | (static_cast<uint32_t>(H >> 3) << 17) | (1u << 16);                    // V is MN-major
-      int ik = 0, iv = 0, units = 0, ip[2] = {0, 0};
+      int kst = 0, kphase = 0, vst = 0, vphase = 0, units = 0, ip[2] = {0, 0};
       for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
         if (*stop) return;
-        const bool both = w.v.m * group - sg.rb * 2 * kGroupRows > kGroupRows;   // both groups have rows of their own
+        const bool both = kGroups == 2 && w.v.m * group - sg.rb * kUnit > kGroupRows;   // both groups have rows of their own
         const int n_tiles = sg.t1 - sg.t0;
-        bool ok = mbar_wait_idle(bar(B_QFULL), units & 1, stop);
+        const uint32_t q0 = base + L::kOffQ + (kGroups == 1 ? units & 1 : 0) * L::kTileBytes;
+        bool ok = mbar_wait(bar(B_QFULL), units & 1, stop);
         ++units;
-        const int ik0 = ik, iv0 = iv;
-        auto scores = [&](int s, int t, bool last_reader) {
-          const int st = (ik0 + t) % L::kKStages;
-          if (!mbar_wait_idle(bar(B_KFULL + st), ((ik0 + t) / L::kKStages) & 1, stop)) return false;
+        // K tiles and V tiles are used in order; a tile that both groups take is given back by the second
+        auto scores = [&](int s, bool last_reader) {
+          if (!mbar_wait(bar(B_KFULL + kst), kphase, stop)) return false;
           fence_after();
-          const uint32_t q = base + L::kOffQ + (both ? s * L::kTileBytes : 0), k = base + L::kOffK + st * L::kTileBytes;
+          const uint64_t q = operand_desc(q0 + (both ? s : 0) * L::kTileBytes, 1, L::kOctet);
+          const uint64_t k = operand_desc(base + L::kOffK + kst * L::kTileBytes, 1, L::kOctet);
 #pragma unroll
-          for (int ks = 0; ks < H / 16; ++ks)
-            umma_ss(tmem + s * 128, desc_k_major(q + (ks >> 2) * L::kHalf + (ks & 3) * 32), desc_k_major(k + (ks >> 2) * L::kHalf + (ks & 3) * 32),
-                    idesc_s, ks != 0);
+          for (int ks = 0; ks < H / 16; ++ks) {
+            const uint32_t step = ((ks >> 2) * 1024 + (ks & 3) * 32) >> 4;
+            umma_ss(tmem + s * 128, q + step, k + step, idesc_s, ks != 0);
+          }
           umma_commit(bar(B_SFULL + s));
-          if (last_reader) umma_commit(bar(B_KEMPTY + st));
+          if (last_reader) {
+            umma_commit(bar(B_KEMPTY + kst));
+            if (++kst == L::kKStages) { kst = 0; kphase ^= 1; }
+          }
           return true;
         };
-        auto output = [&](int s, int t, bool first, bool last_reader) {
-          const int st = (iv0 + t) % L::kVStages;
-          if (!mbar_wait_idle(bar(B_VFULL + st), ((iv0 + t) / L::kVStages) & 1, stop)) return false;
-          if (!mbar_wait_idle(bar(B_PFULL + s), ip[s] & 1, stop)) return false;
+        auto output = [&](int s, bool first, bool last_reader) {
+          if (!mbar_wait(bar(B_VFULL + vst), vphase, stop)) return false;
+          if (!mbar_wait(bar(B_PFULL + s), ip[s] & 1, stop)) return false;
           ++ip[s];
           fence_after();
-          const uint32_t v = base + L::kOffV + st * L::kTileBytes;
+          const uint64_t v = operand_desc(base + L::kOffV + vst * L::kTileBytes, 1024 >> 4, L::kOctet);
 #pragma unroll
           for (int kt = 0; kt < kKeys / 16; ++kt)
-            umma_ts(tmem + 256 + s * 128, tmem + s * 128 + kt * 8, desc_mn_major(v + kt * 2048, L::kHalf), idesc_o, !first || kt != 0);
-          if (last_reader) umma_commit(bar(B_VEMPTY + st));
+            umma_ts(tmem + 256 + s * 128, tmem + s * 128 + kt * 8, v + ((kt * 2 * L::kOctet) >> 4), idesc_o, !first || kt != 0);
+          if (last_reader) {
+            umma_commit(bar(B_VEMPTY + vst));
+            if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
+          }
           return true;
         };
         if (both) {
-          if (ok) ok = scores(0, 0, false) && scores(1, 0, true);
+          ok = ok && scores(0, false) && scores(1, true);
           for (int t = 0; ok && t < n_tiles; ++t)
-            for (int s = 0; ok && s < 2; ++s) {
-              ok = output(s, t, t == 0, s == 1);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              ok = ok && output(s, t == 0, s == 1);
               if (!ok) break;
-              if (t + 1 < n_tiles) ok = scores(s, t + 1, s == 1);
+              if (t + 1 < n_tiles) ok = scores(s, s == 1);
               else umma_commit(bar(B_ODONE + s));
             }
         } else {
-          if (ok) ok = scores(0, 0, true);
-          if (ok && n_tiles > 1) ok = scores(1, 1, true);
+          ok = ok && scores(0, true);
+          if (n_tiles > 1) ok = ok && scores(1, true);
           for (int t = 0; ok && t < n_tiles; ++t) {
             const int s = t & 1;
-            ok = output(s, t, t < 2, true);
+            ok = output(s, t < 2, true);
             if (!ok) break;
-            if (t + 2 < n_tiles) ok = scores(s, t + 2, true);
+            if (t + 2 < n_tiles) ok = scores(s, true);
             else umma_commit(bar(B_ODONE + s));
           }
         }
-        ik += n_tiles;
-        iv += n_tiles;
         if (!ok) *stop = 1;
       });
     }
     __syncwarp();
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     // ------------------------------------------------------------------------------------------------ softmax, output
     const int s = warp >> 2, row_in_group = threadIdx.x & 127;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tmem_s = tmem + lanes + s * 128, tmem_o = tmem + lanes + 256 + s * 128;
     const float scale = r.scale * kLog2e;
-    int is = 0, io = 0, iv = 0;
-    for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
-      const int first = sg.rb * 2 * kGroupRows, rows = min(2 * kGroupRows, w.v.m * group - first);
-      const bool both = rows > kGroupRows;
-      const int n_tiles = sg.t1 - sg.t0, prefix = w.v.n - w.v.m, end = w.v.n;
+    // rows of q and out in 16-byte pieces where they lie so
+    const bool wide_q = (reinterpret_cast<uintptr_t>(r.q) & 15) == 0 && r.q_stride % 8 == 0;
+    const bool wide_out = (reinterpret_cast<uintptr_t>(r.out) & 15) == 0 && r.out_stride % 8 == 0;
+    int is = 0, io = 0, vst = 0, vphase = 0, units = 0;
+    Walk<AttentionLine> walk(line, share, blockIdx.x);
+    TcUnit next;
+    auto advance = [&]() {
+      if (!walk.next(next.sg)) return false;
+      next.row0 = walk.w.v.row0;
+      next.m = walk.w.v.m;
+      next.n = walk.w.v.n;
+      next.n_rb = walk.w.n_rb;
+      return true;
+    };
+    auto has_both = [&](const TcUnit& u) { return kGroups == 2 && u.m * group - u.sg.rb * kUnit > kGroupRows; };
+    // Q of a unit into its place (a thread its row; without rows of their own the second group brings the parents), with
+    // 0 for rows that do not exist
+    auto bring = [&](const TcUnit& u, int which) {
+      const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first), row = has_both(u) ? s * kGroupRows + row_in_group : row_in_group;
+      if (has_both(u) || s == 0) {
+        const bool there = row < rows;
+        const int j = there ? (first + row) / group : 0, head = u.sg.g * group + (there ? (first + row) % group : 0);
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(r.q) + (u.row0 + j) * r.q_stride +
+                                                                static_cast<int64_t>(head) * H);
+        const uint32_t dst = base + L::kOffQ + (kGroups == 1 ? which : s) * L::kTileBytes + (row_in_group >> 3) * L::kOctet + (row & 7) * 128;
+        uint4 x[H / 8];
+#pragma unroll
+        for (int k = 0; k < H / 8; ++k) {
+          x[k] = make_uint4(0, 0, 0, 0);
+          if (there) {
+            if (wide_q) x[k] = reinterpret_cast<const uint4*>(src)[k];
+            else x[k] = make_uint4(src[4 * k], src[4 * k + 1], src[4 * k + 2], src[4 * k + 3]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < H / 8; ++k)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                       ::"r"(dst + (k >> 3) * 1024 + (((k & 7) ^ (row & 7)) << 4)), "r"(x[k].x), "r"(x[k].y), "r"(x[k].z), "r"(x[k].w) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      }
+      if (r.parents && s == 1 && row_in_group < u.m) {
+        int p = r.parents[u.row0 + row_in_group];
+        if (p < -2 || p >= row_in_group) {
+          set_status(c.status, SLED_ERR_ARG);
+          p = -2;
+        }
+        if (p == -2) unused[which] = 1;
+        parents[which * kMaxTreeNodes + row_in_group] = static_cast<signed char>(p);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_QFULL));
+    };
+    bool have = advance();
+    if (have) bring(next, 0);
+    while (have) {
+      const TcUnit u = next;
+      const int which = units & 1;
+      ++units;
+      const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first);
+      const bool both = has_both(u);
+      const int n_tiles = u.sg.t1 - u.sg.t0, prefix = u.n - u.m, end = u.n;
       const int row = (both ? s * kGroupRows : 0) + row_in_group;      // of the unit
       const bool valid = row < rows, active = (row & ~31) < rows;      // whole warps without rows only keep up
-      const int j = valid ? (first + row) / group : 0, head = sg.g * group + (valid ? (first + row) % group : 0);
-      const int64_t t_row = w.v.row0 + j;
-      // the last unit's Q, merge area, parents and flag are done with
+      const int j = valid ? (first + row) / group : 0, head = u.sg.g * group + (valid ? (first + row) % group : 0);
+      const int64_t t_row = u.row0 + j;
+      // the parents are there, and the last unit is done with everything
       asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (threadIdx.x == 0) *odd = 0;
-      if (r.parents && static_cast<int>(threadIdx.x) < w.v.m) parent[threadIdx.x] = r.parents[w.v.row0 + threadIdx.x];
-      {
-        // Q: with two groups a thread brings in its row, else two threads share one
-        const int q_row = both ? row : (threadIdx.x & 255) >> 1;
-        constexpr int kChunks = H / 8;
-        const int c0 = both ? 0 : (threadIdx.x & 1) * (kChunks / 2), c1 = both ? kChunks : c0 + kChunks / 2;
-        const bool there = q_row < rows;
-        const int qj = there ? (first + q_row) / group : 0, qh = sg.g * group + (there ? (first + q_row) % group : 0);
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(r.q) + (w.v.row0 + qj) * r.q_stride +
-                                                                static_cast<int64_t>(qh) * H);
-        const uint32_t dst = base + L::kOffQ + (q_row >> 7) * L::kTileBytes + (q_row & 127) * 128;
-#pragma unroll 4
-        for (int k = c0; k < c1; ++k) {
-          uint4 x = make_uint4(0, 0, 0, 0);
-          if (there) x = make_uint4(src[4 * k], src[4 * k + 1], src[4 * k + 2], src[4 * k + 3]);
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                       ::"r"(dst + (k >> 3) * L::kHalf + (((k & 7) ^ (q_row & 7)) << 4)), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_QFULL));
-      }
+      if (threadIdx.x == 0) odd[which ^ 1] = 0;
       RowView view;
       view.tree = r.parents != nullptr;
       view.last = prefix + j;
 #pragma unroll
       for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
       bool dead = false;
-      if (view.tree) {
-        asm volatile("bar.sync 1, 256;" ::: "memory");   // the parents are there
-        ancestors_of(parent, j, view.bits, c.status);
-        dead = !(view.bits[0] | view.bits[1] | view.bits[2] | view.bits[3]);
+      if (view.tree && (u.sg.t1 * kKeys > prefix || unused[which])) {
+        int a = j;
+        while (a >= 0) {     // a parent is an earlier node: this ends
+#pragma unroll
+          for (int i = 0; i < kMaxTreeNodes / 32; ++i)
+            if (i == (a >> 5)) view.bits[i] |= 1u << (a & 31);
+          a = parents[which * kMaxTreeNodes + a];
+        }
+        dead = a == -2;
+        if (dead) {
+#pragma unroll
+          for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
+        }
       }
       float m = -INFINITY, l = 0.f;
       bool ok = true;
-      const int step = both ? 1 : 2;
-      const int t_first = both ? 0 : s;
-      for (int t = t_first; t < n_tiles; t += step) {
+      const int step = both ? 1 : 2, t_first = both ? 0 : s;
+      for (int t = 0; t < n_tiles; ++t) {
+        const int my_vst = vst, my_vphase = vphase;
+        if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
+        if (!ok || t < t_first || (step == 2 && ((t ^ s) & 1))) continue;
         // (every decision to give up is the whole warp's: the instructions that follow need all lanes)
-        if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_SFULL + s), is & 1, stop))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_SFULL + s), is & 1, stop))) { ok = false; continue; }
         ++is;
         fence_after();
-        const int x0 = (sg.t0 + t) * kKeys;
+        const int x0 = (u.sg.t0 + t) * kKeys;
         const bool masked = x0 + kKeys > prefix;
         if (active) {
-          float mx = -INFINITY;
+          float v[kKeys];
 #pragma unroll
-          for (int q = 0; q < kKeys / 32; ++q) {
-            float v[32];
-            tmem_ld32(tmem_s + q * 32, v);
-            if (masked) {
+          for (int q = 0; q < kKeys / 32; ++q) tmem_ld32_nowait(tmem_s + q * 32, v + q * 32);
+          tmem_ld_wait<kKeys>(v);
+          if (masked) {
+#pragma unroll
+            for (int q = 0; q < kKeys / 32; ++q) {
               const uint32_t see = view.seen(x0 + q * 32, prefix, end);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = (see >> i) & 1u ? v[i] : -INFINITY;
+              for (int i = 0; i < 32; ++i) v[q * 32 + i] = (see >> i) & 1u ? v[q * 32 + i] : -INFINITY;
             }
-            float a = v[0], b = v[1], d = v[2], e = v[3];
-#pragma unroll
-            for (int i = 4; i < 32; i += 4) { a = fmaxf(a, v[i]); b = fmaxf(b, v[i + 1]); d = fmaxf(d, v[i + 2]); e = fmaxf(e, v[i + 3]); }
-            mx = fmaxf(mx, fmaxf(fmaxf(a, b), fmaxf(d, e)));
           }
+          float top[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+          for (int i = 4; i < kKeys; i += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top[e] = fmaxf(top[e], i + 4 < kKeys ? fmaxf(v[i + e], v[i + 4 + e]) : v[i + e]);
+          float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
           mx *= scale;
           const bool raise = mx > m + kRaiseBy || (m == -INFINITY && mx > -INFINITY);
           if (__any_sync(0xffffffffu, raise)) {
@@ -408,46 +480,40 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
             if (raise) m = mx;
             l *= f;
             if (t != t_first) {   // the products so far are complete: they came before these scores
-#pragma unroll
+#pragma unroll 1
               for (int q = 0; q < H / 32; ++q) {
-                float v[32];
-                tmem_ld32(tmem_o + q * 32, v);
-                uint32_t u[32];
+                float o[32];
+                tmem_ld32(tmem_o + q * 32, o);
+                uint32_t x[32];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(v[i] * f);
-                tmem_st16(tmem_o + q * 32, u);
-                tmem_st16(tmem_o + q * 32 + 16, u + 16);
+                for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(o[i] * f);
+                tmem_st16(tmem_o + q * 32, x);
+                tmem_st16(tmem_o + q * 32 + 16, x + 16);
               }
               tmem_st_wait();
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
           float sum0 = 0.f, sum1 = 0.f;
-          float* sc = parts.scores && valid ? parts.scores + (t_row * r.Hq + head) * parts.keys + x0 : nullptr;
+          if (parts.scores && valid) {
+            float* sc = parts.scores + (t_row * r.Hq + head) * parts.keys + x0;
+#pragma unroll
+            for (int i = 0; i < kKeys; i += 4)
+              if (x0 + i < end) *reinterpret_cast<float4*>(sc + i) = make_float4(v[i] * scale, v[i + 1] * scale, v[i + 2] * scale, v[i + 3] * scale);
+          }
 #pragma unroll
           for (int q = 0; q < kKeys / 32; ++q) {
-            float v[32];
-            tmem_ld32(tmem_s + q * 32, v);
-            if (masked) {
-              const uint32_t see = view.seen(x0 + q * 32, prefix, end);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = (see >> i) & 1u ? v[i] : -INFINITY;
-            }
-            if (sc) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 4)
-                if (x0 + q * 32 + i < end)
-                  *reinterpret_cast<float4*>(sc + q * 32 + i) = make_float4(v[i] * scale, v[i + 1] * scale, v[i + 2] * scale, v[i + 3] * scale);
-            }
             uint32_t p[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float a = exp2_approx(fmaf(v[2 * i], scale, -ref)), b = exp2_approx(fmaf(v[2 * i + 1], scale, -ref));
-              sum0 += a;
-              sum1 += b;
+              float a = v[q * 32 + 2 * i], b = v[q * 32 + 2 * i + 1];
+              fma2(a, b, scale, -ref);
+              a = exp2_approx(a);
+              b = exp2_approx(b);
+              add2(sum0, sum1, a, b);
               p[i] = pack_bf16(a, b);
             }
-            tmem_st16(tmem_s + q * 16, p);     // P lies over the scores that have been read
+            tmem_st16(tmem_s + q * 16, p);     // P lies over the scores
           }
           l += sum0 + sum1;
           tmem_st_wait();
@@ -455,15 +521,15 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
         if (masked && (s == 0 || !both)) {
           // A probability of 0 does not silence a value that is not finite: values of positions that hold no key become
           // 0 here, and so do those that are not finite, which the rows that see them get back at the end.
-          const int st = (iv + t) % L::kVStages, x = x0 + row_in_group;
-          if (!__all_sync(0xffffffffu, mbar_wait(bar(B_VFULL + st), ((iv + t) / L::kVStages) & 1, stop))) { ok = false; break; }
-          const uint32_t v = base + L::kOffV + st * L::kTileBytes + row_in_group * 128;
+          const int x = x0 + row_in_group;
+          if (!__all_sync(0xffffffffu, mbar_wait(bar(B_VFULL + my_vst), my_vphase, stop))) { ok = false; continue; }
+          const uint32_t v = base + L::kOffV + my_vst * L::kTileBytes + (row_in_group >> 3) * L::kOctet + (row_in_group & 7) * 128;
           bool found = false;
 #pragma unroll
           for (int hh = 0; hh < L::kHalves; ++hh)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              const uint32_t a = v + hh * L::kHalf + k * 16;
+              const uint32_t a = v + hh * 1024 + k * 16;
               uint32_t y[4];
               asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(a));
               bool change = x >= end;
@@ -476,28 +542,34 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
               }
               if (change) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
             }
-          if (found) *odd = 1;
+          if (found) odd[which] = 1;
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(B_PFULL + s));
       }
-      const bool worked = t_first < n_tiles;
-      if (ok && worked) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(B_ODONE + s), io & 1, stop));
-        ++io;
+      // The next unit's Q goes where nothing reads any more: its group's own rows, whose scores have all been seen, or the
+      // other buffer.  Only a unit of 256 rows' worth whose groups shared the first 128 still needs its Q for the merge.
+      have = advance();
+      const bool early = kGroups == 1 || both;
+      if (early && threadIdx.x == 128) unused[which ^ 1] = 0;
+      if (early && have) {
+        if (s == 1) asm volatile("bar.sync 2, 128;" ::: "memory");     // the flag is down before anyone raises it
+        bring(next, which ^ 1);
       }
-      iv += n_tiles;
+      const bool worked = t_first < n_tiles;
+      if (ok && worked) ok = __all_sync(0xffffffffu, mbar_wait(bar(B_ODONE + s), io & 1, stop));
+      if (worked) ++io;
       if (!ok) *stop = 1;
       fence_after();
       // values that were left out, for the rows that see them
       auto add_odd = [&](float* v, int d0) {
-        for (int x = max(prefix & ~(kKeys - 1), sg.t0 * kKeys); x < min(end, sg.t1 * kKeys); ++x) {
-          if (!both && ((x / kKeys - sg.t0) & 1) != s) continue;
+        for (int x = max(prefix & ~(kKeys - 1), u.sg.t0 * kKeys); x < min(end, u.sg.t1 * kKeys); ++x) {
+          if (!both && ((x / kKeys - u.sg.t0) & 1) != s) continue;
           if (!(view.seen(x & ~31, prefix, end) >> (x & 31) & 1u)) continue;
-          const int page = checked_page(c, c.table[static_cast<int64_t>(sg.req) * c.table_stride + x / c.ps]);
-          const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(c.v) + ((static_cast<int64_t>(page) * c.Hkv + sg.g) * c.ps + x % c.ps) * H + d0;
+          const int page = checked_page(c, c.table[static_cast<int64_t>(u.sg.req) * c.table_stride + x / c.ps]);
+          const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(c.v) + ((static_cast<int64_t>(page) * c.Hkv + u.sg.g) * c.ps + x % c.ps) * H + d0;
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const float y = __bfloat162float(src[i]);
@@ -508,7 +580,7 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
       auto read_o = [&](int q, float* v) {       // 32 columns of the row's output
         if (worked && ok) {
           tmem_ld32(tmem_o + q * 32, v);
-          if (*odd) add_odd(v, q * 32);
+          if (odd[which]) add_odd(v, q * 32);
         } else {
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = 0.f;
@@ -517,22 +589,29 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
       // 32 columns of a row of this unit's result
       auto write_o = [&](int q, const float* v, float inv) {
         if (!valid || !ok || *stop) return;
-        if (sg.whole) {
+        if (u.sg.whole) {
           uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(head) * H) + q * 16;
+          uint32_t p[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) out[i] = dead ? 0u : pack_bf16(v[2 * i] * inv, v[2 * i + 1] * inv);
+          for (int i = 0; i < 16; ++i) p[i] = dead ? 0u : pack_bf16(v[2 * i] * inv, v[2 * i + 1] * inv);
+          if (wide_out) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) out[i] = p[i];
+          }
         } else {
-          float4* acc = reinterpret_cast<float4*>(parts.acc + (static_cast<int64_t>(sg.slot) * 2 * kGroupRows + row) * H + q * 32);
+          float4* acc = reinterpret_cast<float4*>(parts.acc + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * H + q * 32);
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[i] = dead ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
         }
       };
       if (!both && n_tiles > 1) {
         // the second group hands its half of the keys over, [columns][128 rows], as many columns at a time as the area holds
-        float* area = reinterpret_cast<float*>(ptr + L::kOffQ + L::kTileBytes);
-        float2* ml = reinterpret_cast<float2*>(ptr + L::kOffQ);                    // Q is done with: every product of the unit is complete
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (s == 1) ml[row_in_group] = make_float2(m, l);
+        float* area = reinterpret_cast<float*>(ptr + L::kOffQ + (kGroups == 1 ? which : 0) * L::kTileBytes);
+        asm volatile("bar.sync 1, 256;" ::: "memory");      // every product of the unit is complete
+        if (s == 1) { tops[row_in_group] = m; sums[row_in_group] = l; }
         constexpr int kAtOnce = L::kTileBytes / (128 * 4) / 32;                    // chunks of 32 columns
         float f_mine = 1.f, f_other = 0.f, inv = 0.f;
 #pragma unroll 1
@@ -549,7 +628,7 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
           asm volatile("bar.sync 1, 256;" ::: "memory");
           if (s == 0) {
             if (q0 == 0) {
-              const float2 x = ml[row_in_group];
+              const float2 x = make_float2(tops[row_in_group], sums[row_in_group]);
               const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
               f_mine = exp2_approx(m - ref);
               f_other = exp2_approx(x.x - ref);
@@ -580,16 +659,22 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
         }
       }
       if (valid && (both || s == 0) && ok && !*stop) {
-        if (!sg.whole) {
-          *reinterpret_cast<float2*>(parts.ml + (static_cast<int64_t>(sg.slot) * 2 * kGroupRows + row) * 2) = make_float2(m, l);
+        if (!u.sg.whole) {
+          *reinterpret_cast<float2*>(parts.ml + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * 2) = make_float2(m, l);
         } else if (r.lse) {
           r.lse[t_row * r.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
         }
       }
       fence_before();        // O has been read: the next unit's products may overwrite it
-      if (sg.last_block >= 0 && threadIdx.x == 0)
-        parts.desc[blockIdx.x] = make_int4(sg.last_block, sg.slot, sg.req, sg.g * w.n_rb + sg.rb);
-    });
+      if (u.sg.last_block >= 0 && threadIdx.x == 0)
+        parts.desc[blockIdx.x] = make_int4(u.sg.last_block, u.sg.slot, u.sg.req, u.sg.g * u.n_rb + u.sg.rb);
+      if (!early) {
+        asm volatile("bar.sync 1, 256;" ::: "memory");      // the merge is done with Q
+        if (threadIdx.x == 128) unused[which ^ 1] = 0;
+        if (s == 1) asm volatile("bar.sync 2, 128;" ::: "memory");
+        if (have) bring(next, which ^ 1);
+      }
+    }
   }
 
   fence_before();
@@ -604,19 +689,19 @@ __global__ void __launch_bounds__(320, 1) paged_tc_kernel(const PagedCache c, co
 
 constexpr int kMaxDevices = 64;
 
-template <int H>
+template <int H, int kGroups>
 int launch_h(const PagedCache& c, const PagedRows& r, float* scores, char* ws, cudaStream_t s) {
   static bool configured[kMaxDevices] = {};
   int sms = 0;
   const int dev = paged_device(&sms);
   if (dev < 0) return -1;
   if (!configured[dev]) {
-    if (cudaFuncSetAttribute(paged_tc_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<H>::kTotal) != cudaSuccess) return -1;
+    if (cudaFuncSetAttribute(paged_tc_kernel<H, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<H, kGroups>::kTotal) != cudaSuccess) return -1;
     configured[dev] = true;
   }
   CUtensorMap map_k, map_v;
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps;
-  if (tma_map_bf16_rows(&map_k, c.k, rows, H, 16) || tma_map_bf16_rows(&map_v, c.v, rows, H, 16)) return -1;
+  if (tma_map_bf16_row_octets(&map_k, c.k, rows, H) || tma_map_bf16_row_octets(&map_v, c.v, rows, H)) return -1;
   const int blocks = min(sms, kMaxPagedBlocks / 2);
   TcParts parts;
   parts.acc = reinterpret_cast<float*>(ws);
@@ -624,9 +709,9 @@ int launch_h(const PagedCache& c, const PagedRows& r, float* scores, char* ws, c
   parts.desc = reinterpret_cast<int4*>(parts.ml + static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * 2);
   parts.scores = scores;
   parts.keys = static_cast<int64_t>(c.table_cols) * c.ps;
-  SLED_LAUNCH_PDL(paged_tc_kernel<H>, dim3(blocks), dim3(320), Tc<H>::kTotal, s, c, r, parts, map_k, map_v);
+  SLED_LAUNCH_PDL((paged_tc_kernel<H, kGroups>), dim3(blocks), dim3(384), (Tc<H, kGroups>::kTotal), s, c, r, parts, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return -1;
-  const int n = launch_paged_merge(c, r, 0, 2 * kGroupRows, kKeys, blocks, parts.acc, parts.ml, parts.desc, s);
+  const int n = launch_paged_merge(c, r, 0, kGroups * kGroupRows, kKeys, blocks, parts.acc, parts.ml, parts.desc, s);
   return n < 0 ? n : n + 1;
 }
 
@@ -637,7 +722,10 @@ int64_t paged_tc_workspace(int h) {
 }
 
 int launch_paged_tc(const PagedCache& c, const PagedRows& r, float* scores, char* ws, cudaStream_t s) {
-  return c.h == 128 ? launch_h<128>(c, r, scores, ws, s) : launch_h<64>(c, r, scores, ws, s);
+  // units of 256 rows where the requests have more than 128 on average
+  const bool wide = static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kGroupRows) * c.n_reqs;
+  if (c.h == 128) return wide ? launch_h<128, 2>(c, r, scores, ws, s) : launch_h<128, 1>(c, r, scores, ws, s);
+  return wide ? launch_h<64, 2>(c, r, scores, ws, s) : launch_h<64, 1>(c, r, scores, ws, s);
 }
 
 }  // namespace sled
