@@ -965,6 +965,24 @@ int tma_map_bf16_row_octets(CUtensorMap* map, const void* dev_ptr, long long row
   return 0;
 }
 
+int tma_map_bf16_heads(CUtensorMap* map, const void* dev_ptr, long long rows, int heads, int cols, long long row_stride, int box_heads,
+                       int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn || cols % 64 || row_stride % 8 || (reinterpret_cast<uintptr_t>(dev_ptr) & 15)) return -1;
+  cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(cols / 64)};
+  cuuint64_t strides[3] = {static_cast<cuuint64_t>(cols) * 2, static_cast<cuuint64_t>(row_stride) * 2, 128};
+  cuuint32_t box[4] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(cols / 64)};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(dev_ptr), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    std::fprintf(stderr, "sled: cuTensorMapEncodeTiled failed (%d) rows=%lld heads=%d cols=%d\n", static_cast<int>(r), rows, heads, cols);
+    return -1;
+  }
+  return 0;
+}
+
 size_t tc_weight_tiled_bytes(int N, int K) {
   return static_cast<size_t>((N + kBlockM - 1) / kBlockM) * ((K + kBlockK - 1) / kBlockK) * kWStageBytes;
 }

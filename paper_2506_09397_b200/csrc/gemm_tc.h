@@ -57,6 +57,10 @@ int tma_map_bf16_row_groups(CUtensorMap* map, const void* dev_ptr, long long row
 // the same array as groups of eight rows: coordinates {column within 64, row within 8, column / 64, row / 8}; the box, 16
 // rows with all their columns, lands as [2][cols / 64][8 rows][64 columns], 128-byte swizzle.  rows: a multiple of 16
 int tma_map_bf16_row_octets(CUtensorMap* map, const void* dev_ptr, long long rows, int cols);
+// [rows][heads][cols] with rows row_stride elements apart: boxes of box_rows rows x box_heads heads, coordinates {0, head,
+// row, 0}, landing as [cols / 64][box_rows * box_heads][64 columns], 128-byte swizzle; what lies outside is 0
+int tma_map_bf16_heads(CUtensorMap* map, const void* dev_ptr, long long rows, int heads, int cols, long long row_stride, int box_heads,
+                       int box_rows);
 // Bytes of the tiled copy of an [N][K] matrix, and its construction from the row-major matrix (both in
 // device memory; `tiled` 16-byte aligned, tc_weight_tiled_bytes(N, K) long).  The row-major copy is not
 // needed afterwards.  Synchronises the device.

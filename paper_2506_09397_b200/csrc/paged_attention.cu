@@ -200,7 +200,7 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
     const bool keep = key_weights && keeps_scores(c.dtype, H, static_cast<int64_t>(r.T) * r.Hq, keys);
     float* scores = keep ? reinterpret_cast<float*>(ws + parts_bytes(H)) : nullptr;
     // many rows per request: the tcgen05 kernel
-    if (!list && static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kTcRows) * c.n_reqs) n = launch_paged_tc(c, r, scores, ws, s);
+    if (!list && paged_tc_serves(c, r) && static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kTcRows) * c.n_reqs) n = launch_paged_tc(c, r, scores, ws, s);
     else n = launch_paged_mma(c, r, list, list_len, scores, ws, s);
     if (n < 0) return n;
     if (keep) {

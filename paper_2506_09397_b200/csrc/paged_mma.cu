@@ -509,6 +509,19 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
   sg.j = d.w / w.n_rb / c.Hkv;
   const UnitRows u = unit_rows(c, r, list_len, w, sg, unit);
   const int n_parts = d.x - static_cast<int>(blockIdx.x) + 1;
+  // Rows of unused nodes are 0, whatever the partial results say: a stretch of keys without nodes does not know of them.
+  __shared__ signed char parents[kMaxTreeNodes];
+  bool unused = false;
+  if (r.parents && list_len == 0) {
+    bool any = false;
+    if (static_cast<int>(threadIdx.x) < u.m) {
+      const int p = r.parents[u.row0 + threadIdx.x];
+      const bool wrong = p < -1 || p >= static_cast<int>(threadIdx.x);
+      parents[threadIdx.x] = static_cast<signed char>(wrong ? -2 : p);
+      any = wrong;
+    }
+    unused = __syncthreads_or(any);
+  }
   auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? d.y : 2 * (blockIdx.x + p)) * unit; };
   for (int row = blockIdx.y * 16 + warp; row < u.count; row += gridDim.y * 16) {
     float M = -INFINITY;
@@ -541,12 +554,17 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
       }
     }
     den = warp_sum(den);
-    const bool none = M == -INFINITY && !nan;
+    bool none = M == -INFINITY && !nan;
+    if (unused) {
+      int a = u.token(row);
+      while (a >= 0) a = parents[a];
+      none |= a == -2;
+    }
     const float inv = none ? 0.f : 1.f / den;
     const int t = u.row0 + u.token(row), head = u.head(row);
     uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t * r.out_stride + static_cast<int64_t>(head) * H) + lane * (D / 2);
 #pragma unroll
-    for (int e = 0; e < D / 2; ++e) out[e] = pack_bf16(num[2 * e] * inv, num[2 * e + 1] * inv);
+    for (int e = 0; e < D / 2; ++e) out[e] = none ? 0u : pack_bf16(num[2 * e] * inv, num[2 * e + 1] * inv);
     if (r.lse && lane == 0) r.lse[static_cast<int64_t>(t) * r.Hq + head] = none ? -INFINITY : (M + log2f(den)) * kLn2;
   }
 }

@@ -19,6 +19,7 @@
 // (16 a clock and SM) above.  Every wait is bounded; when one runs out the block says so in *status, lets what is under
 // way land, frees its tensor memory and returns.
 #include "gemm_tc.h"
+#include "kernels.h"
 #include "paged_schedule.cuh"
 #include "warp_mma.cuh"
 
@@ -33,7 +34,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // kGroups: softmax groups that have rows of their own in the largest unit (1: units of up to 128 rows, 2: up to 256).
-// K, V and Q lie in groups of eight rows, [H / 64][8 rows][64 columns], as a copy of 16 cached keys leaves them.
+// K and V lie in groups of eight rows, [H / 64][8 rows][64 columns], as a copy of 16 cached keys leaves them; 128 rows of Q
+// as [H / 64][128 rows][64 columns].
 template <int H, int kGroups>
 struct Tc {
   static constexpr int kHalves = H / 64;
@@ -46,7 +48,7 @@ struct Tc {
   static constexpr int kOffK = 2 * kTileBytes;
   static constexpr int kOffV = kOffK + kKStages * kTileBytes;
   static constexpr int kOffBar = kOffV + kVStages * kTileBytes;
-  static constexpr int kOffTree = kOffBar + 256;         // parents of the nodes, one byte each, of two units
+  static constexpr int kOffTree = kOffBar + 256;         // parents of the nodes, one byte each, for either group
   static constexpr int kOffTop = kOffTree + 2 * kMaxTreeNodes;   // row maxima and sums of the merge
   static constexpr int kTotal = kOffTop + 2 * kGroupRows * 4 + 1024;   // alignment slack
 };
@@ -54,7 +56,7 @@ static_assert(kMaxTreeNodes == 128);
 static_assert(Tc<128, 1>::kTotal + 512 <= 227 * 1024 && Tc<64, 1>::kTotal + 512 <= 227 * 1024, "shared memory of one block");
 
 // barriers, 8 bytes each
-enum { B_KFULL = 0, B_KEMPTY = 5, B_VFULL = 10, B_VEMPTY = 14, B_QFULL = 18, B_SFULL = 19, B_PFULL = 21, B_ODONE = 23, B_COUNT = 25 };
+enum { B_KFULL = 0, B_KEMPTY = 5, B_VFULL = 10, B_VEMPTY = 14, B_QFULL = 18, B_QEMPTY = 20, B_SFULL = 22, B_PFULL = 24, B_ODONE = 28, B_COUNT = 30 };
 static_assert(B_COUNT * 8 + 4 <= 256);
 
 // Operand descriptors, 128-byte swizzle, rows of 128 bytes, groups of 8 rows `octet` bytes apart.  K-major: the contraction
@@ -92,6 +94,17 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       " [%0], [%1, {%3, %3, %3, %4}], [%2], %5;"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(octet), "l"(policy)
       : "memory");
+}
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int head, int token, uint32_t bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%3, %4, %5, %3}], [%2], %6;"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(head), "r"(token), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {   // 32 bytes, a whole sector
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 __device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int octet) {
   asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %1, %1, %2}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(octet) : "memory");
@@ -186,19 +199,18 @@ struct TcUnit {
 
 template <int H, int kGroups>
 __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, const PagedRows r, const TcParts parts,
-                                                          const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+                                                          const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                                          const __grid_constant__ CUtensorMap map_v) {
   using L = Tc<H, kGroups>;
   constexpr int kUnit = kGroups * kGroupRows;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int stop_word;
-  __shared__ int odd_words[2];           // a key of the unit's last tiles has a value that is not finite
-  __shared__ int unused_words[2];        // the unit's tree has unused nodes
+  __shared__ int odd_words[2];           // the last units in which a key of the masked tiles had a value that is not finite
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* ptr = smem_raw + (base - raw);
   volatile int* stop = &stop_word;
   volatile int* odd = odd_words;
-  volatile int* unused = unused_words;
-  signed char* parents = reinterpret_cast<signed char*>(ptr + L::kOffTree);
+  signed char* parents = reinterpret_cast<signed char*>(ptr + L::kOffTree) + (threadIdx.x >> 7 & 1) * kMaxTreeNodes;
   float* tops = reinterpret_cast<float*>(ptr + L::kOffTop);
   float* sums = tops + kGroupRows;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ptr + L::kOffBar + 8 * B_COUNT);
@@ -206,16 +218,19 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    *stop = odd[0] = odd[1] = unused[0] = unused[1] = 0;
+    *stop = odd[0] = odd[1] = 0;
     for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 1); mbar_init(bar(B_KEMPTY + s), 1); }
     for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 1); mbar_init(bar(B_VEMPTY + s), 1); }
-    mbar_init(bar(B_QFULL), 8);
     for (int s = 0; s < 2; ++s) {
+      mbar_init(bar(B_QFULL + s), 1);
+      mbar_init(bar(B_QEMPTY + s), 8);
       mbar_init(bar(B_SFULL + s), 1);
-      mbar_init(bar(B_PFULL + s), 4);
+      mbar_init(bar(B_PFULL + 2 * s), 4);
+      mbar_init(bar(B_PFULL + 2 * s + 1), 4);
       mbar_init(bar(B_ODONE + s), 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&map_q);
     prefetch_map(&map_k);
     prefetch_map(&map_v);
   }
@@ -244,7 +259,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       const int stages = is_k ? L::kKStages : L::kVStages, b_full = is_k ? B_KFULL : B_VFULL, b_empty = is_k ? B_KEMPTY : B_VEMPTY;
       const uint64_t policy = policy_evict_first();
       const int cpp = c.ps / 16;
-      int st = 0, phase = 1;
+      int st = 0, phase = 1, units = 0;
       for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
         const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
         const int groups = min((w.v.n + 15) / 16, sg.t1 * 8);     // 16-key groups up to the end of the segment
@@ -253,6 +268,23 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           const int b = e / cpp;
           return ((checked_page(c, table[b]) * c.Hkv + sg.g) * c.ps + (e - b * cpp) * 16) >> 3;
         };
+        if (is_k) {     // the unit's Q first
+          const int which = kGroups == 1 ? units & 1 : 0, left = w.v.m * group - sg.rb * kUnit;
+          const bool both = kGroups == 2 && left > kGroupRows;
+          bool ok = true;
+          if (lane == 0) {
+            ok = !*stop && mbar_wait(bar(B_QEMPTY + which), ((kGroups == 1 ? units >> 1 : units) & 1) ^ 1, stop);
+            if (ok) {
+              mbar_expect(bar(B_QFULL + which), (both ? 2 : 1) * L::kTileBytes);
+              for (int s = 0; s < (both ? 2 : 1); ++s)
+                tma_load_rows(base + L::kOffQ + (which + s) * L::kTileBytes, &map_q, sg.g * group,
+                              w.v.row0 + (sg.rb * kUnit + s * kGroupRows) / group, bar(B_QFULL + which), policy);
+            }
+          }
+          ok = __shfl_sync(0xffffffffu, ok, 0);
+          if (!ok) { *stop = 1; return; }
+          ++units;
+        }
         // lane l looks after group l of four tiles; what comes after them is asked into L2, since shared memory holds too
         // little to cover the latency of DRAM while tiles wait for their softmax
         int octet = octet_of(sg.t0 * 8 + lane), later = 0;
@@ -285,19 +317,20 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
         if (*stop) return;
         const bool both = kGroups == 2 && w.v.m * group - sg.rb * kUnit > kGroupRows;   // both groups have rows of their own
         const int n_tiles = sg.t1 - sg.t0;
-        const uint32_t q0 = base + L::kOffQ + (kGroups == 1 ? units & 1 : 0) * L::kTileBytes;
-        bool ok = mbar_wait(bar(B_QFULL), units & 1, stop);
+        const int which = kGroups == 1 ? units & 1 : 0;
+        const uint32_t q0 = base + L::kOffQ + which * L::kTileBytes;
+        bool ok = mbar_wait(bar(B_QFULL + which), (kGroups == 1 ? units >> 1 : units) & 1, stop);
         ++units;
         // K tiles and V tiles are used in order; a tile that both groups take is given back by the second
         auto scores = [&](int s, bool last_reader) {
           if (!mbar_wait(bar(B_KFULL + kst), kphase, stop)) return false;
           fence_after();
-          const uint64_t q = operand_desc(q0 + (both ? s : 0) * L::kTileBytes, 1, L::kOctet);
+          const uint64_t q = operand_desc(q0 + (both ? s : 0) * L::kTileBytes, 1, 1024);
           const uint64_t k = operand_desc(base + L::kOffK + kst * L::kTileBytes, 1, L::kOctet);
 #pragma unroll
           for (int ks = 0; ks < H / 16; ++ks) {
-            const uint32_t step = ((ks >> 2) * 1024 + (ks & 3) * 32) >> 4;
-            umma_ss(tmem + s * 128, q + step, k + step, idesc_s, ks != 0);
+            const uint32_t within = (ks & 3) * 32;
+            umma_ss(tmem + s * 128, q + (((ks >> 2) * kGroupRows * 128 + within) >> 4), k + (((ks >> 2) * 1024 + within) >> 4), idesc_s, ks != 0);
           }
           umma_commit(bar(B_SFULL + s));
           if (last_reader) {
@@ -308,13 +341,16 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
         };
         auto output = [&](int s, bool first, bool last_reader) {
           if (!mbar_wait(bar(B_VFULL + vst), vphase, stop)) return false;
-          if (!mbar_wait(bar(B_PFULL + s), ip[s] & 1, stop)) return false;
-          ++ip[s];
-          fence_after();
           const uint64_t v = operand_desc(base + L::kOffV + vst * L::kTileBytes, 1024 >> 4, L::kOctet);
 #pragma unroll
-          for (int kt = 0; kt < kKeys / 16; ++kt)
-            umma_ts(tmem + 256 + s * 128, tmem + s * 128 + kt * 8, v + ((kt * 2 * L::kOctet) >> 4), idesc_o, !first || kt != 0);
+          for (int half = 0; half < 2; ++half) {     // the second half of P is still being made under the first half's products
+            if (!mbar_wait(bar(B_PFULL + 2 * s + half), ip[s] & 1, stop)) return false;
+            fence_after();
+#pragma unroll
+            for (int kt = half * (kKeys / 32); kt < (half + 1) * (kKeys / 32); ++kt)
+              umma_ts(tmem + 256 + s * 128, tmem + s * 128 + kt * 8, v + ((kt * 2 * L::kOctet) >> 4), idesc_o, !first || kt != 0);
+          }
+          ++ip[s];
           if (last_reader) {
             umma_commit(bar(B_VEMPTY + vst));
             if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
@@ -353,94 +389,33 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tmem_s = tmem + lanes + s * 128, tmem_o = tmem + lanes + 256 + s * 128;
     const float scale = r.scale * kLog2e;
-    // rows of q and out in 16-byte pieces where they lie so
-    const bool wide_q = (reinterpret_cast<uintptr_t>(r.q) & 15) == 0 && r.q_stride % 8 == 0;
-    const bool wide_out = (reinterpret_cast<uintptr_t>(r.out) & 15) == 0 && r.out_stride % 8 == 0;
     int is = 0, io = 0, vst = 0, vphase = 0, units = 0;
     Walk<AttentionLine> walk(line, share, blockIdx.x);
-    TcUnit next;
-    auto advance = [&]() {
-      if (!walk.next(next.sg)) return false;
-      next.row0 = walk.w.v.row0;
-      next.m = walk.w.v.m;
-      next.n = walk.w.v.n;
-      next.n_rb = walk.w.n_rb;
-      return true;
-    };
-    auto has_both = [&](const TcUnit& u) { return kGroups == 2 && u.m * group - u.sg.rb * kUnit > kGroupRows; };
-    // Q of a unit into its place (a thread its row; without rows of their own the second group brings the parents), with
-    // 0 for rows that do not exist
-    auto bring = [&](const TcUnit& u, int which) {
-      const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first), row = has_both(u) ? s * kGroupRows + row_in_group : row_in_group;
-      if (has_both(u) || s == 0) {
-        const bool there = row < rows;
-        const int j = there ? (first + row) / group : 0, head = u.sg.g * group + (there ? (first + row) % group : 0);
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(r.q) + (u.row0 + j) * r.q_stride +
-                                                                static_cast<int64_t>(head) * H);
-        const uint32_t dst = base + L::kOffQ + (kGroups == 1 ? which : s) * L::kTileBytes + (row_in_group >> 3) * L::kOctet + (row & 7) * 128;
-        uint4 x[H / 8];
-#pragma unroll
-        for (int k = 0; k < H / 8; ++k) {
-          x[k] = make_uint4(0, 0, 0, 0);
-          if (there) {
-            if (wide_q) x[k] = reinterpret_cast<const uint4*>(src)[k];
-            else x[k] = make_uint4(src[4 * k], src[4 * k + 1], src[4 * k + 2], src[4 * k + 3]);
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < H / 8; ++k)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                       ::"r"(dst + (k >> 3) * 1024 + (((k & 7) ^ (row & 7)) << 4)), "r"(x[k].x), "r"(x[k].y), "r"(x[k].z), "r"(x[k].w) : "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      }
-      if (r.parents && s == 1 && row_in_group < u.m) {
-        int p = r.parents[u.row0 + row_in_group];
-        if (p < -2 || p >= row_in_group) {
-          set_status(c.status, SLED_ERR_ARG);
-          p = -2;
-        }
-        if (p == -2) unused[which] = 1;
-        parents[which * kMaxTreeNodes + row_in_group] = static_cast<signed char>(p);
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_QFULL));
-    };
-    bool have = advance();
-    if (have) bring(next, 0);
-    while (have) {
-      const TcUnit u = next;
-      const int which = units & 1;
+    TcUnit u;
+    while (walk.next(u.sg)) {
+      u.row0 = walk.w.v.row0;
+      u.m = walk.w.v.m;
+      u.n = walk.w.v.n;
+      u.n_rb = walk.w.n_rb;
+      const int which = kGroups == 1 ? units & 1 : 0;
       ++units;
       const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first);
-      const bool both = has_both(u);
+      const bool both = kGroups == 2 && rows > kGroupRows;
       const int n_tiles = u.sg.t1 - u.sg.t0, prefix = u.n - u.m, end = u.n;
       const int row = (both ? s * kGroupRows : 0) + row_in_group;      // of the unit
       const bool valid = row < rows, active = (row & ~31) < rows;      // whole warps without rows only keep up
       const int j = valid ? (first + row) / group : 0, head = u.sg.g * group + (valid ? (first + row) % group : 0);
       const int64_t t_row = u.row0 + j;
-      // the parents are there, and the last unit is done with everything
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      if (threadIdx.x == 0) odd[which ^ 1] = 0;
+      // What the row sees of the nodes is found out when the first tile that holds one comes up; the parents are on their
+      // way until then.  (A stretch without such a tile need not know of unused nodes: the merge leaves them out.)
       RowView view;
       view.tree = r.parents != nullptr;
       view.last = prefix + j;
 #pragma unroll
       for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
-      bool dead = false;
-      if (view.tree && (u.sg.t1 * kKeys > prefix || unused[which])) {
-        int a = j;
-        while (a >= 0) {     // a parent is an earlier node: this ends
-#pragma unroll
-          for (int i = 0; i < kMaxTreeNodes / 32; ++i)
-            if (i == (a >> 5)) view.bits[i] |= 1u << (a & 31);
-          a = parents[which * kMaxTreeNodes + a];
-        }
-        dead = a == -2;
-        if (dead) {
-#pragma unroll
-          for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
-        }
-      }
+      bool dead = false, known = !view.tree;
+      int my_parent = -1;
+      if (view.tree && u.sg.t1 * kKeys > prefix && row_in_group < u.m) my_parent = r.parents[u.row0 + row_in_group];
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       const int step = both ? 1 : 2, t_first = both ? 0 : s;
@@ -452,8 +427,61 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
         if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_SFULL + s), is & 1, stop))) { ok = false; continue; }
         ++is;
         fence_after();
+        // with rows of their own the groups are done with Q once the last scores are there
+        if (both && t + 1 == n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY + which));
         const int x0 = (u.sg.t0 + t) * kKeys;
         const bool masked = x0 + kKeys > prefix;
+        if (masked && !known) {
+          known = true;
+          if (row_in_group < u.m) {
+            if (my_parent < -2 || my_parent >= row_in_group) {
+              set_status(c.status, SLED_ERR_ARG);
+              my_parent = -2;
+            }
+            parents[row_in_group] = static_cast<signed char>(my_parent);
+          }
+          if (s == 0) asm volatile("bar.sync 2, 128;" ::: "memory");
+          else asm volatile("bar.sync 3, 128;" ::: "memory");
+          int a = j;
+          while (a >= 0) {     // a parent is an earlier node: this ends
+#pragma unroll
+            for (int i = 0; i < kMaxTreeNodes / 32; ++i)
+              if (i == (a >> 5)) view.bits[i] |= 1u << (a & 31);
+            a = parents[a];
+          }
+          dead = a == -2;
+          if (dead) {
+#pragma unroll
+            for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
+          }
+        }
+        if (masked && (s == 0 || !both)) {
+          // A probability of 0 does not silence a value that is not finite: values of positions that hold no key become
+          // 0 here, and so do those that are not finite, which the rows that see them get back at the end.
+          const int x = x0 + row_in_group;
+          if (!__all_sync(0xffffffffu, mbar_wait(bar(B_VFULL + my_vst), my_vphase, stop))) { ok = false; continue; }
+          const uint32_t v = base + L::kOffV + my_vst * L::kTileBytes + (row_in_group >> 3) * L::kOctet + (row_in_group & 7) * 128;
+          bool found = false;
+#pragma unroll
+          for (int hh = 0; hh < L::kHalves; ++hh)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t a = v + hh * 1024 + k * 16;
+              uint32_t y[4];
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(a));
+              bool change = x >= end;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t off = ((y[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((y[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+                found |= off != 0 && x < end;
+                change |= off != 0;
+                y[e] = x >= end ? 0u : y[e] & ~off;
+              }
+              if (change) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+            }
+          if (found) odd[units & 1] = units;
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
         if (active) {
           float v[kKeys];
 #pragma unroll
@@ -514,49 +542,22 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
               p[i] = pack_bf16(a, b);
             }
             tmem_st16(tmem_s + q * 16, p);     // P lies over the scores
+            if (q == kKeys / 64 - 1) {
+              tmem_st_wait();
+              fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * s));
+            }
           }
           l += sum0 + sum1;
           tmem_st_wait();
         }
-        if (masked && (s == 0 || !both)) {
-          // A probability of 0 does not silence a value that is not finite: values of positions that hold no key become
-          // 0 here, and so do those that are not finite, which the rows that see them get back at the end.
-          const int x = x0 + row_in_group;
-          if (!__all_sync(0xffffffffu, mbar_wait(bar(B_VFULL + my_vst), my_vphase, stop))) { ok = false; continue; }
-          const uint32_t v = base + L::kOffV + my_vst * L::kTileBytes + (row_in_group >> 3) * L::kOctet + (row_in_group & 7) * 128;
-          bool found = false;
-#pragma unroll
-          for (int hh = 0; hh < L::kHalves; ++hh)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint32_t a = v + hh * 1024 + k * 16;
-              uint32_t y[4];
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(a));
-              bool change = x >= end;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t off = ((y[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((y[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-                found |= off != 0 && x < end;
-                change |= off != 0;
-                y[e] = x >= end ? 0u : y[e] & ~off;
-              }
-              if (change) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
-            }
-          if (found) odd[which] = 1;
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        }
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_PFULL + s));
-      }
-      // The next unit's Q goes where nothing reads any more: its group's own rows, whose scores have all been seen, or the
-      // other buffer.  Only a unit of 256 rows' worth whose groups shared the first 128 still needs its Q for the merge.
-      have = advance();
-      const bool early = kGroups == 1 || both;
-      if (early && threadIdx.x == 128) unused[which ^ 1] = 0;
-      if (early && have) {
-        if (s == 1) asm volatile("bar.sync 2, 128;" ::: "memory");     // the flag is down before anyone raises it
-        bring(next, which ^ 1);
+        if (lane == 0) {
+          if (!active) mbar_arrive(bar(B_PFULL + 2 * s));
+          mbar_arrive(bar(B_PFULL + 2 * s + 1));
+        }
       }
       const bool worked = t_first < n_tiles;
       if (ok && worked) ok = __all_sync(0xffffffffu, mbar_wait(bar(B_ODONE + s), io & 1, stop));
@@ -580,7 +581,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       auto read_o = [&](int q, float* v) {       // 32 columns of the row's output
         if (worked && ok) {
           tmem_ld32(tmem_o + q * 32, v);
-          if (odd[which]) add_odd(v, q * 32);
+          if (odd[units & 1] == units) add_odd(v, q * 32);
         } else {
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = 0.f;
@@ -590,26 +591,24 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       auto write_o = [&](int q, const float* v, float inv) {
         if (!valid || !ok || *stop) return;
         if (u.sg.whole) {
-          uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(head) * H) + q * 16;
+          char* out = reinterpret_cast<char*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(head) * H + q * 32);
           uint32_t p[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) p[i] = dead ? 0u : pack_bf16(v[2 * i] * inv, v[2 * i + 1] * inv);
-          if (wide_out) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) out[i] = p[i];
-          }
+          store32(out, p);
+          store32(out + 32, p + 8);
         } else {
-          float4* acc = reinterpret_cast<float4*>(parts.acc + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * H + q * 32);
+          char* acc = reinterpret_cast<char*>(parts.acc + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * H + q * 32);
+          uint32_t x[32];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) acc[i] = dead ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          for (int i = 0; i < 32; ++i) x[i] = dead ? 0u : __float_as_uint(v[i]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) store32(acc + 32 * i, x + 8 * i);
         }
       };
       if (!both && n_tiles > 1) {
         // the second group hands its half of the keys over, [columns][128 rows], as many columns at a time as the area holds
-        float* area = reinterpret_cast<float*>(ptr + L::kOffQ + (kGroups == 1 ? which : 0) * L::kTileBytes);
+        float* area = reinterpret_cast<float*>(ptr + L::kOffQ + which * L::kTileBytes);
         asm volatile("bar.sync 1, 256;" ::: "memory");      // every product of the unit is complete
         if (s == 1) { tops[row_in_group] = m; sums[row_in_group] = l; }
         constexpr int kAtOnce = L::kTileBytes / (128 * 4) / 32;                    // chunks of 32 columns
@@ -668,11 +667,10 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       fence_before();        // O has been read: the next unit's products may overwrite it
       if (u.sg.last_block >= 0 && threadIdx.x == 0)
         parts.desc[blockIdx.x] = make_int4(u.sg.last_block, u.sg.slot, u.sg.req, u.sg.g * u.n_rb + u.sg.rb);
-      if (!early) {
-        asm volatile("bar.sync 1, 256;" ::: "memory");      // the merge is done with Q
-        if (threadIdx.x == 128) unused[which ^ 1] = 0;
-        if (s == 1) asm volatile("bar.sync 2, 128;" ::: "memory");
-        if (have) bring(next, which ^ 1);
+      if (!both) {           // nobody reads or writes the unit's Q any more
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_QEMPTY + which));
       }
     }
   }
@@ -699,7 +697,8 @@ int launch_h(const PagedCache& c, const PagedRows& r, float* scores, char* ws, c
     if (cudaFuncSetAttribute(paged_tc_kernel<H, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<H, kGroups>::kTotal) != cudaSuccess) return -1;
     configured[dev] = true;
   }
-  CUtensorMap map_k, map_v;
+  CUtensorMap map_q, map_k, map_v;
+  if (tma_map_bf16_heads(&map_q, r.q, r.T, r.Hq, H, r.q_stride, r.Hq / c.Hkv, kGroupRows / (r.Hq / c.Hkv))) return -1;
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps;
   if (tma_map_bf16_row_octets(&map_k, c.k, rows, H) || tma_map_bf16_row_octets(&map_v, c.v, rows, H)) return -1;
   const int blocks = min(sms, kMaxPagedBlocks / 2);
@@ -709,7 +708,7 @@ int launch_h(const PagedCache& c, const PagedRows& r, float* scores, char* ws, c
   parts.desc = reinterpret_cast<int4*>(parts.ml + static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * 2);
   parts.scores = scores;
   parts.keys = static_cast<int64_t>(c.table_cols) * c.ps;
-  SLED_LAUNCH_PDL((paged_tc_kernel<H, kGroups>), dim3(blocks), dim3(384), (Tc<H, kGroups>::kTotal), s, c, r, parts, map_k, map_v);
+  SLED_LAUNCH_PDL((paged_tc_kernel<H, kGroups>), dim3(blocks), dim3(384), (Tc<H, kGroups>::kTotal), s, c, r, parts, map_q, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return -1;
   const int n = launch_paged_merge(c, r, 0, kGroups * kGroupRows, kKeys, blocks, parts.acc, parts.ml, parts.desc, s);
   return n < 0 ? n : n + 1;
@@ -719,6 +718,13 @@ int launch_h(const PagedCache& c, const PagedRows& r, float* scores, char* ws, c
 
 int64_t paged_tc_workspace(int h) {
   return static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * (h + 2) * 4 + kMaxPagedBlocks * 16LL;
+}
+
+// Q comes in by TMA, heads of whole tokens, and results go out a sector at a time
+bool paged_tc_serves(const PagedCache& c, const PagedRows& r) {
+  const int group = r.Hq / c.Hkv;
+  return c.dtype == BF16 && (c.h == 64 || c.h == 128) && kGroupRows % group == 0 && r.q_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(r.q) & 15) == 0 &&
+         r.out_stride % 16 == 0 && (reinterpret_cast<uintptr_t>(r.out) & 31) == 0;
 }
 
 int launch_paged_tc(const PagedCache& c, const PagedRows& r, float* scores, char* ws, cudaStream_t s) {
