@@ -26,8 +26,10 @@ struct ReqWork {
   __device__ __forceinline__ long long cost() const { return count() * weight; }
 };
 
-// Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM).
-constexpr int kMinShare = 32;
+// Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM), in
+// sixteenths.  Beginning and ending a unit costs a number of tiles as well; it is spread over the unit's tiles.
+constexpr int kMinShare = 64;
+__device__ __forceinline__ int unit_weight(int tile, int unit, int tiles) { return min(tile + unit / tiles, kMinShare - 1); }
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
 
 // The work of attention.  list_len > 0: units attend to chosen blocks, at most list_len per token.  kWholeRows: a unit has
@@ -52,10 +54,10 @@ struct AttentionLine {
     w.tiles = (keys + tile - 1) / tile;
     w.n_rb = list_len == kWholeRows ? 1 : (rows + unit_rows - 1) / unit_rows;
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
-    w.weight = list_len == kWholeRows ? min(rows, kMinShare - 1)
-               : unit_rows == kUnitRows ? tile_weight(min(rows, kUnitRows))
-               : unit_rows > kUnitRows  ? (rows > unit_rows / 2 ? 20 : 16)
-                                        : 8 + min(rows, unit_rows);
+    if (list_len == kWholeRows) w.weight = min(rows, kMinShare - 1);
+    else if (unit_rows == kUnitRows) w.weight = unit_weight(tile_weight(min(rows, kUnitRows)), 32, w.tiles);
+    else if (unit_rows > kUnitRows) w.weight = unit_weight(rows > kUnitRows * 2 ? 18 : 16, 64, w.tiles);
+    else w.weight = unit_weight(8 + min(rows, unit_rows), 32, w.tiles);
     return w;
   }
 };

@@ -42,15 +42,14 @@ struct Tc {
   static constexpr int kOctet = kHalves * 1024;          // eight rows
   static constexpr int kTileBytes = 16 * kOctet;         // K, V or 128 rows of Q
   static constexpr int kKStages = H == 64 ? 5 : 3, kVStages = H == 64 ? 4 : 2;
-  // Q of 256 rows, or of two units of 128: the next unit's is brought in under the end of one.  The merge of a unit's
-  // groups takes place in the unit's own Q, which is done with by then.
+  // Q of 256 rows, or of two units of 128: the next unit's is brought in under the end of one.
   static constexpr int kOffQ = 0;
   static constexpr int kOffK = 2 * kTileBytes;
   static constexpr int kOffV = kOffK + kKStages * kTileBytes;
   static constexpr int kOffBar = kOffV + kVStages * kTileBytes;
   static constexpr int kOffTree = kOffBar + 256;         // parents of the nodes, one byte each, for either group
-  static constexpr int kOffTop = kOffTree + 2 * kMaxTreeNodes;   // row maxima and sums of the merge
-  static constexpr int kTotal = kOffTop + 2 * kGroupRows * 4 + 1024;   // alignment slack
+  static constexpr int kOffTop = kOffTree + 2 * kMaxTreeNodes;   // what the groups tell each other about a row
+  static constexpr int kTotal = kOffTop + kGroupRows * 8 + 1024;       // alignment slack
 };
 static_assert(kMaxTreeNodes == 128);
 static_assert(Tc<128, 1>::kTotal + 512 <= 227 * 1024 && Tc<64, 1>::kTotal + 512 <= 227 * 1024, "shared memory of one block");
@@ -211,8 +210,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
   volatile int* stop = &stop_word;
   volatile int* odd = odd_words;
   signed char* parents = reinterpret_cast<signed char*>(ptr + L::kOffTree) + (threadIdx.x >> 7 & 1) * kMaxTreeNodes;
-  float* tops = reinterpret_cast<float*>(ptr + L::kOffTop);
-  float* sums = tops + kGroupRows;
+  float2* tops = reinterpret_cast<float2*>(ptr + L::kOffTop);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ptr + L::kOffBar + 8 * B_COUNT);
   auto bar = [&](int i) { return base + L::kOffBar + 8u * static_cast<uint32_t>(i); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
@@ -389,14 +387,20 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tmem_s = tmem + lanes + s * 128, tmem_o = tmem + lanes + 256 + s * 128;
     const float scale = r.scale * kLog2e;
-    int is = 0, io = 0, vst = 0, vphase = 0, units = 0;
+    int is = 0, vst = 0, vphase = 0, units = 0;
     Walk<AttentionLine> walk(line, share, blockIdx.x);
-    TcUnit u;
-    while (walk.next(u.sg)) {
-      u.row0 = walk.w.v.row0;
-      u.m = walk.w.v.m;
-      u.n = walk.w.v.n;
-      u.n_rb = walk.w.n_rb;
+    TcUnit next;
+    auto advance = [&]() {
+      if (!walk.next(next.sg)) return false;
+      next.row0 = walk.w.v.row0;
+      next.m = walk.w.v.m;
+      next.n = walk.w.v.n;
+      next.n_rb = walk.w.n_rb;
+      return true;
+    };
+    int done[2] = {0, 0};       // units that either group has finished
+    for (bool have = advance(); have;) {
+      const TcUnit u = next;
       const int which = kGroups == 1 ? units & 1 : 0;
       ++units;
       const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first);
@@ -406,19 +410,42 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       const bool valid = row < rows, active = (row & ~31) < rows;      // whole warps without rows only keep up
       const int j = valid ? (first + row) / group : 0, head = u.sg.g * group + (valid ? (first + row) % group : 0);
       const int64_t t_row = u.row0 + j;
-      // What the row sees of the nodes is found out when the first tile that holds one comes up; the parents are on their
-      // way until then.  (A stretch without such a tile need not know of unused nodes: the merge leaves them out.)
+      // What the row sees of the nodes.  (A stretch without any of them need not know of unused ones: the merge leaves
+      // those out.)  Either group has its own copy of the parents, so that neither waits for the other.
       RowView view;
       view.tree = r.parents != nullptr;
       view.last = prefix + j;
 #pragma unroll
       for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
-      bool dead = false, known = !view.tree;
-      int my_parent = -1;
-      if (view.tree && u.sg.t1 * kKeys > prefix && row_in_group < u.m) my_parent = r.parents[u.row0 + row_in_group];
+      bool dead = false;
+      if (view.tree && u.sg.t1 * kKeys > prefix) {
+        if (row_in_group < u.m) {
+          int p = r.parents[u.row0 + row_in_group];
+          if (p < -2 || p >= row_in_group) {
+            set_status(c.status, SLED_ERR_ARG);
+            p = -2;
+          }
+          parents[row_in_group] = static_cast<signed char>(p);
+        }
+        if (s == 0) asm volatile("bar.sync 2, 128;" ::: "memory");
+        else asm volatile("bar.sync 3, 128;" ::: "memory");
+        int a = j;
+        while (a >= 0) {     // a parent is an earlier node: this ends
+#pragma unroll
+          for (int i = 0; i < kMaxTreeNodes / 32; ++i)
+            if (i == (a >> 5)) view.bits[i] |= 1u << (a & 31);
+          a = parents[a];
+        }
+        dead = a == -2;
+        if (dead) {
+#pragma unroll
+          for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
+        }
+      }
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       const int step = both ? 1 : 2, t_first = both ? 0 : s;
+      if (t_first >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY + which));
       for (int t = 0; t < n_tiles; ++t) {
         const int my_vst = vst, my_vphase = vphase;
         if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
@@ -427,34 +454,9 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
         if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_SFULL + s), is & 1, stop))) { ok = false; continue; }
         ++is;
         fence_after();
-        // with rows of their own the groups are done with Q once the last scores are there
-        if (both && t + 1 == n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY + which));
+        if (t + step >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY + which));    // the group is done with Q
         const int x0 = (u.sg.t0 + t) * kKeys;
         const bool masked = x0 + kKeys > prefix;
-        if (masked && !known) {
-          known = true;
-          if (row_in_group < u.m) {
-            if (my_parent < -2 || my_parent >= row_in_group) {
-              set_status(c.status, SLED_ERR_ARG);
-              my_parent = -2;
-            }
-            parents[row_in_group] = static_cast<signed char>(my_parent);
-          }
-          if (s == 0) asm volatile("bar.sync 2, 128;" ::: "memory");
-          else asm volatile("bar.sync 3, 128;" ::: "memory");
-          int a = j;
-          while (a >= 0) {     // a parent is an earlier node: this ends
-#pragma unroll
-            for (int i = 0; i < kMaxTreeNodes / 32; ++i)
-              if (i == (a >> 5)) view.bits[i] |= 1u << (a & 31);
-            a = parents[a];
-          }
-          dead = a == -2;
-          if (dead) {
-#pragma unroll
-            for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
-          }
-        }
         if (masked && (s == 0 || !both)) {
           // A probability of 0 does not silence a value that is not finite: values of positions that hold no key become
           // 0 here, and so do those that are not finite, which the rows that see them get back at the end.
@@ -466,7 +468,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           for (int hh = 0; hh < L::kHalves; ++hh)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              const uint32_t a = v + hh * 1024 + k * 16;
+              const uint32_t a = v + hh * 1024 + ((k ^ (row_in_group & 7)) << 4);    // eight rows, eight banks
               uint32_t y[4];
               asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(a));
               bool change = x >= end;
@@ -559,15 +561,52 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           mbar_arrive(bar(B_PFULL + 2 * s + 1));
         }
       }
-      const bool worked = t_first < n_tiles;
-      if (ok && worked) ok = __all_sync(0xffffffffu, mbar_wait(bar(B_ODONE + s), io & 1, stop));
-      if (worked) ++io;
+      have = advance();
+      // The groups' results.  With rows of their own each writes its own; groups that shared rows also share the writing,
+      // half of the columns each: both results of a row are in the same lane of tensor memory, only maximum and sum have
+      // to be exchanged.
+      const bool joint = !both && n_tiles > 1;
+      if (joint) {
+        if (s == 1) tops[row_in_group] = make_float2(m, l);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(B_ODONE), done[0] & 1, stop) && mbar_wait(bar(B_ODONE + 1), done[1] & 1, stop));
+      } else if (t_first < n_tiles && ok) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bar(B_ODONE + s), done[s] & 1, stop));
+      }
+      ++done[0];
+      if (both || joint) ++done[1];
       if (!ok) *stop = 1;
       fence_after();
-      // values that were left out, for the rows that see them
-      auto add_odd = [&](float* v, int d0) {
+      float f_mine = 1.f, f_other = 0.f;      // factors of the group's own result and of the other's
+      if (!joint || s == 0) {
+        if (joint) {
+          const float2 x = tops[row_in_group];
+          const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
+          f_mine = exp2_approx(m - ref);
+          f_other = exp2_approx(x.x - ref);
+          l = l * f_mine + x.y * f_other;
+          m = top;
+        }
+        if (dead) { m = -INFINITY; l = 0.f; }
+        if (u.sg.whole) {
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          f_mine *= inv;
+          f_other *= inv;
+        }
+        if (joint) tops[row_in_group] = make_float2(f_other, f_mine);
+      }
+      if (joint) {
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (s == 1) {
+          const float2 x = tops[row_in_group];
+          f_mine = x.x;
+          f_other = x.y;
+        }
+      }
+      // values that were left out of a group's products, for the rows that see them
+      auto add_odd = [&](float* v, int d0, int whose) {
         for (int x = max(prefix & ~(kKeys - 1), u.sg.t0 * kKeys); x < min(end, u.sg.t1 * kKeys); ++x) {
-          if (!both && ((x / kKeys - u.sg.t0) & 1) != s) continue;
+          if (!both && ((x / kKeys - u.sg.t0) & 1) != whose) continue;
           if (!(view.seen(x & ~31, prefix, end) >> (x & 31) & 1u)) continue;
           const int page = checked_page(c, c.table[static_cast<int64_t>(u.sg.req) * c.table_stride + x / c.ps]);
           const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(c.v) + ((static_cast<int64_t>(page) * c.Hkv + u.sg.g) * c.ps + x % c.ps) * H + d0;
@@ -578,100 +617,52 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           }
         }
       };
-      auto read_o = [&](int q, float* v) {       // 32 columns of the row's output
-        if (worked && ok) {
-          tmem_ld32(tmem_o + q * 32, v);
-          if (odd[units & 1] == units) add_odd(v, q * 32);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = 0.f;
-        }
-      };
-      // 32 columns of a row of this unit's result
-      auto write_o = [&](int q, const float* v, float inv) {
-        if (!valid || !ok || *stop) return;
-        if (u.sg.whole) {
-          char* out = reinterpret_cast<char*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(head) * H + q * 32);
-          uint32_t p[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) p[i] = dead ? 0u : pack_bf16(v[2 * i] * inv, v[2 * i + 1] * inv);
-          store32(out, p);
-          store32(out + 32, p + 8);
-        } else {
-          char* acc = reinterpret_cast<char*>(parts.acc + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * H + q * 32);
-          uint32_t x[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = dead ? 0u : __float_as_uint(v[i]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) store32(acc + 32 * i, x + 8 * i);
-        }
-      };
-      if (!both && n_tiles > 1) {
-        // the second group hands its half of the keys over, [columns][128 rows], as many columns at a time as the area holds
-        float* area = reinterpret_cast<float*>(ptr + L::kOffQ + which * L::kTileBytes);
-        asm volatile("bar.sync 1, 256;" ::: "memory");      // every product of the unit is complete
-        if (s == 1) { tops[row_in_group] = m; sums[row_in_group] = l; }
-        constexpr int kAtOnce = L::kTileBytes / (128 * 4) / 32;                    // chunks of 32 columns
-        float f_mine = 1.f, f_other = 0.f, inv = 0.f;
+      const bool writes = ok && active && (both || joint || s == 0);
+      const int q0 = joint ? s * (H / 64) : 0, q1 = joint ? q0 + H / 64 : H / 32;      // chunks of 32 columns
+      if (writes) {
 #pragma unroll 1
-        for (int q0 = 0; q0 < H / 32; q0 += kAtOnce) {
-          if (s == 1) {
-#pragma unroll 1
-            for (int q = 0; q < kAtOnce; ++q) {
-              float v[32];
-              read_o(q0 + q, v);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) area[(q * 32 + i) * 128 + row_in_group] = v[i];
-            }
-          }
-          asm volatile("bar.sync 1, 256;" ::: "memory");
-          if (s == 0) {
-            if (q0 == 0) {
-              const float2 x = make_float2(tops[row_in_group], sums[row_in_group]);
-              const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
-              f_mine = exp2_approx(m - ref);
-              f_other = exp2_approx(x.x - ref);
-              l = l * f_mine + x.y * f_other;
-              m = top;
-              if (dead) { m = -INFINITY; l = 0.f; }
-              inv = l == 0.f ? 0.f : 1.f / l;
-            }
-#pragma unroll 1
-            for (int q = 0; q < kAtOnce; ++q) {
-              float v[32];
-              read_o(q0 + q, v);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = v[i] * f_mine + area[(q * 32 + i) * 128 + row_in_group] * f_other;
-              write_o(q0 + q, v, inv);
-            }
-          }
-          asm volatile("bar.sync 1, 256;" ::: "memory");
-        }
-      } else if ((both || s == 0) && active) {
-        if (dead) { m = -INFINITY; l = 0.f; }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll 1
-        for (int q = 0; q < H / 32; ++q) {
+        for (int q = q0; q < q1; ++q) {
           float v[32];
-          read_o(q, v);
-          write_o(q, v, inv);
+          tmem_ld32(tmem_o + q * 32, v);
+          if (odd[units & 1] == units) add_odd(v, q * 32, s);
+          if (joint) {
+            float o[32];
+            tmem_ld32(tmem + lanes + 256 + (s ^ 1) * 128 + q * 32, o);
+            if (odd[units & 1] == units) add_odd(o, q * 32, s ^ 1);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = v[i] * f_mine + o[i] * f_other;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= f_mine;
+          }
+          if (valid && u.sg.whole) {
+            char* out = reinterpret_cast<char*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(head) * H + q * 32);
+            uint32_t p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = dead ? 0u : pack_bf16(v[2 * i], v[2 * i + 1]);
+            store32(out, p);
+            store32(out + 32, p + 8);
+          } else if (valid) {
+            char* acc = reinterpret_cast<char*>(parts.acc + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * H + q * 32);
+            uint32_t x[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = dead ? 0u : __float_as_uint(v[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) store32(acc + 32 * i, x + 8 * i);
+          }
         }
-      }
-      if (valid && (both || s == 0) && ok && !*stop) {
-        if (!u.sg.whole) {
-          *reinterpret_cast<float2*>(parts.ml + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * 2) = make_float2(m, l);
-        } else if (r.lse) {
-          r.lse[t_row * r.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        if (valid && (both || s == 0)) {
+          if (!u.sg.whole) {
+            *reinterpret_cast<float2*>(parts.ml + (static_cast<int64_t>(u.sg.slot) * kUnit + row) * 2) = make_float2(m, l);
+          } else if (r.lse) {
+            r.lse[t_row * r.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+          }
         }
       }
       fence_before();        // O has been read: the next unit's products may overwrite it
+      if (joint) asm volatile("bar.sync 1, 256;" ::: "memory");     // by both
       if (u.sg.last_block >= 0 && threadIdx.x == 0)
         parts.desc[blockIdx.x] = make_int4(u.sg.last_block, u.sg.slot, u.sg.req, u.sg.g * u.n_rb + u.sg.rb);
-      if (!both) {           // nobody reads or writes the unit's Q any more
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_QEMPTY + which));
-      }
     }
   }
 
