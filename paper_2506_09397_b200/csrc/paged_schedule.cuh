@@ -28,7 +28,7 @@ struct ReqWork {
 
 // Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM), in
 // sixteenths.  Beginning and ending a unit costs a number of tiles as well; it is spread over the unit's tiles.
-constexpr int kMinShare = 64;
+constexpr int kMinShare = 128;
 __device__ __forceinline__ int unit_weight(int tile, int unit, int tiles) { return min(tile + unit / tiles, kMinShare - 1); }
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
 
@@ -56,7 +56,7 @@ struct AttentionLine {
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
     if (list_len == kWholeRows) w.weight = min(rows, kMinShare - 1);
     else if (unit_rows == kUnitRows) w.weight = unit_weight(tile_weight(min(rows, kUnitRows)), 32, w.tiles);
-    else if (unit_rows > kUnitRows) w.weight = unit_weight(rows > kUnitRows * 2 ? 18 : 16, 64, w.tiles);
+    else if (unit_rows > kUnitRows) w.weight = rows > kUnitRows * 2 ? unit_weight(38, 240, w.tiles) : unit_weight(16, 160, w.tiles);
     else w.weight = unit_weight(8 + min(rows, unit_rows), 32, w.tiles);
     return w;
   }

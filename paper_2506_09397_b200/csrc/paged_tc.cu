@@ -41,10 +41,9 @@ struct Tc {
   static constexpr int kHalves = H / 64;
   static constexpr int kOctet = kHalves * 1024;          // eight rows
   static constexpr int kTileBytes = 16 * kOctet;         // K, V or 128 rows of Q
-  static constexpr int kKStages = H == 64 ? 5 : 3, kVStages = H == 64 ? 4 : 2;
-  // Q of 256 rows, or of two units of 128: the next unit's is brought in under the end of one.
+  static constexpr int kKStages = H == 64 ? 5 : 3, kVStages = H == 64 ? 4 : kGroups == 1 ? 3 : 2;
   static constexpr int kOffQ = 0;
-  static constexpr int kOffK = 2 * kTileBytes;
+  static constexpr int kOffK = kGroups * kTileBytes;
   static constexpr int kOffV = kOffK + kKStages * kTileBytes;
   static constexpr int kOffBar = kOffV + kVStages * kTileBytes;
   static constexpr int kOffTree = kOffBar + 256;         // parents of the nodes, one byte each, for either group
@@ -52,10 +51,10 @@ struct Tc {
   static constexpr int kTotal = kOffTop + kGroupRows * 8 + 1024;       // alignment slack
 };
 static_assert(kMaxTreeNodes == 128);
-static_assert(Tc<128, 1>::kTotal + 512 <= 227 * 1024 && Tc<64, 1>::kTotal + 512 <= 227 * 1024, "shared memory of one block");
+static_assert(Tc<128, 1>::kTotal + 512 <= 227 * 1024 && Tc<128, 2>::kTotal + 512 <= 227 * 1024 && Tc<64, 2>::kTotal + 512 <= 227 * 1024, "shared memory of one block");
 
 // barriers, 8 bytes each
-enum { B_KFULL = 0, B_KEMPTY = 5, B_VFULL = 10, B_VEMPTY = 14, B_QFULL = 18, B_QEMPTY = 20, B_SFULL = 22, B_PFULL = 24, B_ODONE = 28, B_COUNT = 30 };
+enum { B_KFULL = 0, B_KEMPTY = 5, B_VFULL = 10, B_VEMPTY = 14, B_QFULL = 18, B_QEMPTY = 19, B_SFULL = 20, B_PFULL = 22, B_ODONE = 26, B_COUNT = 28 };
 static_assert(B_COUNT * 8 + 4 <= 256);
 
 // Operand descriptors, 128-byte swizzle, rows of 128 bytes, groups of 8 rows `octet` bytes apart.  K-major: the contraction
@@ -219,9 +218,9 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
     *stop = odd[0] = odd[1] = 0;
     for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 1); mbar_init(bar(B_KEMPTY + s), 1); }
     for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 1); mbar_init(bar(B_VEMPTY + s), 1); }
+    mbar_init(bar(B_QFULL), 1);
+    mbar_init(bar(B_QEMPTY), 8);
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bar(B_QFULL + s), 1);
-      mbar_init(bar(B_QEMPTY + s), 8);
       mbar_init(bar(B_SFULL + s), 1);
       mbar_init(bar(B_PFULL + 2 * s), 4);
       mbar_init(bar(B_PFULL + 2 * s + 1), 4);
@@ -267,16 +266,16 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           return ((checked_page(c, table[b]) * c.Hkv + sg.g) * c.ps + (e - b * cpp) * 16) >> 3;
         };
         if (is_k) {     // the unit's Q first
-          const int which = kGroups == 1 ? units & 1 : 0, left = w.v.m * group - sg.rb * kUnit;
+          const int left = w.v.m * group - sg.rb * kUnit;
           const bool both = kGroups == 2 && left > kGroupRows;
           bool ok = true;
           if (lane == 0) {
-            ok = !*stop && mbar_wait(bar(B_QEMPTY + which), ((kGroups == 1 ? units >> 1 : units) & 1) ^ 1, stop);
+            ok = !*stop && mbar_wait(bar(B_QEMPTY), (units & 1) ^ 1, stop);
             if (ok) {
-              mbar_expect(bar(B_QFULL + which), (both ? 2 : 1) * L::kTileBytes);
+              mbar_expect(bar(B_QFULL), (both ? 2 : 1) * L::kTileBytes);
               for (int s = 0; s < (both ? 2 : 1); ++s)
-                tma_load_rows(base + L::kOffQ + (which + s) * L::kTileBytes, &map_q, sg.g * group,
-                              w.v.row0 + (sg.rb * kUnit + s * kGroupRows) / group, bar(B_QFULL + which), policy);
+                tma_load_rows(base + L::kOffQ + s * L::kTileBytes, &map_q, sg.g * group,
+                              w.v.row0 + (sg.rb * kUnit + s * kGroupRows) / group, bar(B_QFULL), policy);
             }
           }
           ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -290,6 +289,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           const int ahead = (t - sg.t0) & 3;
           if (ahead == 0) {
             if (t > sg.t0) octet = later;
+            if (t == sg.t0 && (lane >> 3) >= 2 && sg.t0 * 8 + lane < groups) tma_prefetch_4d(map, octet);
             later = octet_of((t + 4) * 8 + lane);
             if ((t + 4) * 8 + lane < groups) tma_prefetch_4d(map, later);
           }
@@ -315,9 +315,8 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
         if (*stop) return;
         const bool both = kGroups == 2 && w.v.m * group - sg.rb * kUnit > kGroupRows;   // both groups have rows of their own
         const int n_tiles = sg.t1 - sg.t0;
-        const int which = kGroups == 1 ? units & 1 : 0;
-        const uint32_t q0 = base + L::kOffQ + which * L::kTileBytes;
-        bool ok = mbar_wait(bar(B_QFULL + which), (kGroups == 1 ? units >> 1 : units) & 1, stop);
+        const uint32_t q0 = base + L::kOffQ;
+        bool ok = mbar_wait(bar(B_QFULL), units & 1, stop);
         ++units;
         // K tiles and V tiles are used in order; a tile that both groups take is given back by the second
         auto scores = [&](int s, bool last_reader) {
@@ -401,7 +400,6 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
     int done[2] = {0, 0};       // units that either group has finished
     for (bool have = advance(); have;) {
       const TcUnit u = next;
-      const int which = kGroups == 1 ? units & 1 : 0;
       ++units;
       const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first);
       const bool both = kGroups == 2 && rows > kGroupRows;
@@ -445,7 +443,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       const int step = both ? 1 : 2, t_first = both ? 0 : s;
-      if (t_first >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY + which));
+      if (t_first >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY));
       for (int t = 0; t < n_tiles; ++t) {
         const int my_vst = vst, my_vphase = vphase;
         if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
@@ -454,7 +452,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
         if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_SFULL + s), is & 1, stop))) { ok = false; continue; }
         ++is;
         fence_after();
-        if (t + step >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY + which));    // the group is done with Q
+        if (t + step >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY));    // the group is done with Q
         const int x0 = (u.sg.t0 + t) * kKeys;
         const bool masked = x0 + kKeys > prefix;
         if (masked && (s == 0 || !both)) {
@@ -463,25 +461,33 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           const int x = x0 + row_in_group;
           if (!__all_sync(0xffffffffu, mbar_wait(bar(B_VFULL + my_vst), my_vphase, stop))) { ok = false; continue; }
           const uint32_t v = base + L::kOffV + my_vst * L::kTileBytes + (row_in_group >> 3) * L::kOctet + (row_in_group & 7) * 128;
-          bool found = false;
+          // (the eight lanes of a quarter warp take different sixteenths of their rows: eight rows, eight banks)
+          auto piece = [&](int k) { return v + (k >> 3) * 1024 + (((k & 7) ^ (row_in_group & 7)) << 4); };
+          if (x >= end) {
 #pragma unroll
-          for (int hh = 0; hh < L::kHalves; ++hh)
+            for (int k = 0; k < H / 8; ++k) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(piece(k)), "r"(0) : "memory");
+          } else {
+            uint32_t found = 0;      // all ones in an exponent carry into bit 15 or 31
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint32_t a = v + hh * 1024 + ((k ^ (row_in_group & 7)) << 4);    // eight rows, eight banks
+            for (int k = 0; k < H / 8; ++k) {
               uint32_t y[4];
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(a));
-              bool change = x >= end;
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y[0]), "=r"(y[1]), "=r"(y[2]), "=r"(y[3]) : "r"(piece(k)));
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t off = ((y[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((y[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-                found |= off != 0 && x < end;
-                change |= off != 0;
-                y[e] = x >= end ? 0u : y[e] & ~off;
-              }
-              if (change) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+              for (int e = 0; e < 4; ++e) found |= (y[e] & 0x7f807f80u) + 0x00800080u;
             }
-          if (found) odd[units & 1] = units;
+            if (found & 0x80008000u) {
+              odd[units & 1] = units;
+#pragma unroll 1
+              for (int k = 0; k < H / 8; ++k)
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e) {
+                  uint32_t y;
+                  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(y) : "r"(piece(k) + 4 * e));
+                  const uint32_t off = ((y & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((y & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+                  asm volatile("st.shared.b32 [%0], %1;" ::"r"(piece(k) + 4 * e), "r"(y & ~off) : "memory");
+                }
+            }
+          }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         if (active) {
