@@ -52,7 +52,9 @@ int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* lis
 // the same on the 5th-generation tensor cores, for requests with many query rows
 int64_t paged_tc_workspace(int h);
 bool paged_tc_serves(const PagedCache& c, const PagedRows& r);
-int launch_paged_tc(const PagedCache& c, const PagedRows& r, float* scores, char* ws, cudaStream_t s);
+int launch_paged_tc(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s);
+// adds the attention weights of the keys (bf16, head_dim 64 or 128; r.lse is set, paged_tc_serves)
+int launch_paged_weigh(const PagedCache& c, const PagedRows& r, float* key_weights, cudaStream_t s);
 // joins the partial results of units of unit_rows rows that were cut in tiles of `tile` keys over `blocks` blocks
 int launch_paged_merge(const PagedCache& c, const PagedRows& r, int list_len, int unit_rows, int tile, int blocks, float* acc, float* ml,
                        int4* desc, cudaStream_t s);

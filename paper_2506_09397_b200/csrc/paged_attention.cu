@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
   });
 }
 
-// Rows per request (on average) above which the tcgen05 kernel is used.
+// Rows per request (on average) above which the tcgen05 kernels are used.
 constexpr int kTcRows = 24;
 int64_t parts_bytes(int h) {
   const int64_t a = paged_mma_workspace(h), b = paged_tc_workspace(h);
@@ -195,13 +195,18 @@ bool keeps_scores(int dtype, int h, int64_t rows_heads, int64_t keys) {
 template <typename T, int H>
 int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws, cudaStream_t s) {
   int n = 1;
-  if (sizeof(T) == 2 && H >= 64) {
+  if constexpr (sizeof(T) == 2 && H >= 64) {
+    // many rows per request: the tcgen05 kernels
+    if (!list && paged_tc_serves(c, r) && static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kTcRows) * c.n_reqs) {
+      n = launch_paged_tc(c, r, ws, s);
+      if (n < 0 || !key_weights) return n;
+      const int w = launch_paged_weigh(c, r, key_weights, s);
+      return w < 0 ? w : n + w;
+    }
     const int64_t keys = static_cast<int64_t>(c.table_cols) * c.ps;
     const bool keep = key_weights && keeps_scores(c.dtype, H, static_cast<int64_t>(r.T) * r.Hq, keys);
     float* scores = keep ? reinterpret_cast<float*>(ws + parts_bytes(H)) : nullptr;
-    // many rows per request: the tcgen05 kernel
-    if (!list && paged_tc_serves(c, r) && static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kTcRows) * c.n_reqs) n = launch_paged_tc(c, r, scores, ws, s);
-    else n = launch_paged_mma(c, r, list, list_len, scores, ws, s);
+    n = launch_paged_mma(c, r, list, list_len, scores, ws, s);
     if (n < 0) return n;
     if (keep) {
       int sms = 0;

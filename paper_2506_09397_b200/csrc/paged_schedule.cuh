@@ -54,7 +54,7 @@ struct AttentionLine {
     w.tiles = (keys + tile - 1) / tile;
     w.n_rb = list_len == kWholeRows ? 1 : (rows + unit_rows - 1) / unit_rows;
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
-    if (list_len == kWholeRows) w.weight = min(rows, kMinShare - 1);
+    if (list_len == kWholeRows) w.weight = min(16 + rows, kMinShare - 1);
     else if (unit_rows == kUnitRows) w.weight = unit_weight(tile_weight(min(rows, kUnitRows)), 32, w.tiles);
     else if (unit_rows > kUnitRows) w.weight = rows > kUnitRows * 2 ? unit_weight(38, 240, w.tiles) : unit_weight(16, 160, w.tiles);
     else w.weight = unit_weight(8 + min(rows, unit_rows), 32, w.tiles);

@@ -21,7 +21,7 @@
 #include "gemm_tc.h"
 #include "kernels.h"
 #include "paged_schedule.cuh"
-#include "warp_mma.cuh"
+#include "tcgen05_ptx.cuh"
 
 namespace sled {
 
@@ -57,107 +57,10 @@ static_assert(Tc<128, 1>::kTotal + 512 <= 227 * 1024 && Tc<128, 2>::kTotal + 512
 enum { B_KFULL = 0, B_KEMPTY = 5, B_VFULL = 10, B_VEMPTY = 14, B_QFULL = 18, B_QEMPTY = 19, B_SFULL = 20, B_PFULL = 22, B_ODONE = 26, B_COUNT = 28 };
 static_assert(B_COUNT * 8 + 4 <= 256);
 
-// Operand descriptors, 128-byte swizzle, rows of 128 bytes, groups of 8 rows `octet` bytes apart.  K-major: the contraction
-// runs along a row (Q, K).  MN-major: down the rows (V); the leading offset is the distance to the next 64 columns.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t leading, uint32_t octet) {
-  return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | (static_cast<uint64_t>(leading) << 16) | (static_cast<uint64_t>(octet >> 4) << 32) |
-         (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
-}
-
-__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
-      : "memory");
-}
-__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {   // A in tensor memory
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
-      : "memory");
-}
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int octet, uint32_t bar, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0], [%1, {%3, %3, %3, %4}], [%2], %5;"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(octet), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int head, int token, uint32_t bar, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0], [%1, {%3, %4, %5, %3}], [%2], %6;"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(0), "r"(head), "r"(token), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void store32(void* p, const uint32_t* v) {   // 32 bytes, a whole sector
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-}
-__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map, int octet) {
-  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %1, %1, %2}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(octet) : "memory");
-}
-
-// 32 consecutive columns of this warp's 32 lanes (thread = lane); the values may be used after tmem_ld_wait()
-__device__ __forceinline__ void tmem_ld32_nowait(uint32_t addr, float* v) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15,"
-      " %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
-        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
-        "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
-        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
-      : "r"(addr));
-}
-// the registers are named so that no use of them moves ahead of the wait
-template <int N>
-__device__ __forceinline__ void tmem_ld_wait(float* v) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
-}
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float* v) {
-  tmem_ld32_nowait(addr, v);
-  tmem_ld_wait<32>(v);
-}
-// two products at a time
-__device__ __forceinline__ void fma2(float& a, float& b, float scale, float add) {
-  asm("{\n\t.reg .b64 x, y, z;\n\t"
-      "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
-      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
-      : "+f"(a), "+f"(b) : "f"(scale), "f"(add));
-}
-__device__ __forceinline__ void add2(float& a, float& b, float x, float y) {
-  asm("{\n\t.reg .b64 p, q;\n\t"
-      "mov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\t"
-      "add.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}"
-      : "+f"(a), "+f"(b) : "f"(x), "f"(y));
-}
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
 struct TcParts {
   float* acc;      // [2 * blocks][rows of a unit][H], not normalised
   float* ml;       // [2 * blocks][rows of a unit][2]
   int4* desc;      // [blocks] {last block or -1, first slot, request, unit of the request}
-  float* scores;   // null, or [rows][Hq][keys]
-  int64_t keys;
 };
 
 // what a row sees of the request's own nodes
@@ -491,18 +394,27 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         if (active) {
+          // What a row does not see becomes -infinity in tensor memory, in a pass of its own: the code that every tile runs
+          // through stays short (a tile's first run waits for its instructions).
+          if (masked) {
+#pragma unroll 1
+            for (int q = 0; q < kKeys / 32; ++q) {
+              const uint32_t see = view.seen(x0 + q * 32, prefix, end);
+              if (__all_sync(0xffffffffu, see == 0xffffffffu)) continue;
+              float x[32];
+              tmem_ld32(tmem_s + q * 32, x);
+              uint32_t y[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) y[i] = (see >> i) & 1u ? __float_as_uint(x[i]) : 0xff800000u;
+              tmem_st16(tmem_s + q * 32, y);
+              tmem_st16(tmem_s + q * 32 + 16, y + 16);
+            }
+            tmem_st_wait();
+          }
           float v[kKeys];
 #pragma unroll
           for (int q = 0; q < kKeys / 32; ++q) tmem_ld32_nowait(tmem_s + q * 32, v + q * 32);
           tmem_ld_wait<kKeys>(v);
-          if (masked) {
-#pragma unroll
-            for (int q = 0; q < kKeys / 32; ++q) {
-              const uint32_t see = view.seen(x0 + q * 32, prefix, end);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[q * 32 + i] = (see >> i) & 1u ? v[q * 32 + i] : -INFINITY;
-            }
-          }
           float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
           for (int i = 4; i < kKeys; i += 8)
@@ -531,12 +443,6 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           }
           const float ref = m == -INFINITY ? 0.f : m;
           float sum0 = 0.f, sum1 = 0.f;
-          if (parts.scores && valid) {
-            float* sc = parts.scores + (t_row * r.Hq + head) * parts.keys + x0;
-#pragma unroll
-            for (int i = 0; i < kKeys; i += 4)
-              if (x0 + i < end) *reinterpret_cast<float4*>(sc + i) = make_float4(v[i] * scale, v[i + 1] * scale, v[i + 2] * scale, v[i + 3] * scale);
-          }
 #pragma unroll
           for (int q = 0; q < kKeys / 32; ++q) {
             uint32_t p[16];
@@ -685,7 +591,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
 constexpr int kMaxDevices = 64;
 
 template <int H, int kGroups>
-int launch_h(const PagedCache& c, const PagedRows& r, float* scores, char* ws, cudaStream_t s) {
+int launch_h(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) {
   static bool configured[kMaxDevices] = {};
   int sms = 0;
   const int dev = paged_device(&sms);
@@ -703,8 +609,6 @@ int launch_h(const PagedCache& c, const PagedRows& r, float* scores, char* ws, c
   parts.acc = reinterpret_cast<float*>(ws);
   parts.ml = parts.acc + static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * H;
   parts.desc = reinterpret_cast<int4*>(parts.ml + static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * 2);
-  parts.scores = scores;
-  parts.keys = static_cast<int64_t>(c.table_cols) * c.ps;
   SLED_LAUNCH_PDL((paged_tc_kernel<H, kGroups>), dim3(blocks), dim3(384), (Tc<H, kGroups>::kTotal), s, c, r, parts, map_q, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return -1;
   const int n = launch_paged_merge(c, r, 0, kGroups * kGroupRows, kKeys, blocks, parts.acc, parts.ml, parts.desc, s);
@@ -724,11 +628,11 @@ bool paged_tc_serves(const PagedCache& c, const PagedRows& r) {
          r.out_stride % 16 == 0 && (reinterpret_cast<uintptr_t>(r.out) & 31) == 0;
 }
 
-int launch_paged_tc(const PagedCache& c, const PagedRows& r, float* scores, char* ws, cudaStream_t s) {
+int launch_paged_tc(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) {
   // units of 256 rows where the requests have more than 128 on average
   const bool wide = static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kGroupRows) * c.n_reqs;
-  if (c.h == 128) return wide ? launch_h<128, 2>(c, r, scores, ws, s) : launch_h<128, 1>(c, r, scores, ws, s);
-  return wide ? launch_h<64, 2>(c, r, scores, ws, s) : launch_h<64, 1>(c, r, scores, ws, s);
+  if (c.h == 128) return wide ? launch_h<128, 2>(c, r, ws, s) : launch_h<128, 1>(c, r, ws, s);
+  return wide ? launch_h<64, 2>(c, r, ws, s) : launch_h<64, 1>(c, r, ws, s);
 }
 
 }  // namespace sled

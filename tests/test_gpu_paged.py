@@ -194,7 +194,8 @@ def test_a_request_that_does_not_hold_together_is_left_out(fault, dtype):
     q = _queries([rows], 4, 64, dtype, 3).cuda()
     parents = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
     cu = _cu(q_len)
-    good = B.attention_tree(q, k, v, table, n_kv, cu, parents)
+    good = B.attention_tree(q, k, v, table, n_kv, cu, parents, key_weights=torch.zeros(k.shape[:3], device="cuda"))
+    near = lambda a, b: bool(((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 1e-3).all())   # the work is shared out anew
     code = B.SLED_ERR_ARG
     if fault == "keys beyond the table":
         n_kv[1] = 16 * table.shape[1] + 1
@@ -218,9 +219,9 @@ def test_a_request_that_does_not_hold_together_is_left_out(fault, dtype):
     with pytest.raises(B.SledError) as e:
         B.check_status(status)
     assert e.value.code == code
-    assert torch.equal(out[:4], good[:4])
+    assert near(out[:4], good[:4])
     if fault not in ("rows beyond the call", "rows run backwards", "tree too large"):
-        assert bool((out[4:9] == 3).all()) and torch.equal(out[9:12], good[9:12])
+        assert bool((out[4:9] == 3).all()) and near(out[9:12], good[9:12])
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
