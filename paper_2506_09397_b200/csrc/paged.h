@@ -49,6 +49,9 @@ int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_
 constexpr int kMaxPagedBlocks = 320;   // two on each of up to 160 SMs
 int64_t paged_mma_workspace(int h);
 int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s);
+// the same for fp32 caches, on CUDA cores
+int64_t paged_f32_workspace(int h);
+int launch_paged_f32(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s);
 // the same on the 5th-generation tensor cores, for requests with many query rows
 int64_t paged_tc_workspace(int h);
 bool paged_tc_serves(const PagedCache& c, const PagedRows& r);

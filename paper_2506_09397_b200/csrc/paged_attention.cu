@@ -181,15 +181,15 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
 
 // Rows per request (on average) above which the tcgen05 kernels are used.
 constexpr int kTcRows = 24;
-int64_t parts_bytes(int h) {
-  const int64_t a = paged_mma_workspace(h), b = paged_tc_workspace(h);
+int64_t parts_bytes(int dtype, int h) {
+  const int64_t a = dtype == 1 ? paged_mma_workspace(h) : paged_f32_workspace(h), b = dtype == 1 ? paged_tc_workspace(h) : 0;
   return ((a > b ? a : b) + 255) / 256 * 256;
 }
 
 // Scores are kept where they take no more than this; otherwise the weights are computed from the keys again.
 constexpr int64_t kMostScoreBytes = 512LL << 20;
 bool keeps_scores(int dtype, int h, int64_t rows_heads, int64_t keys) {
-  return dtype == 1 && h >= 64 && rows_heads * keys * 4 <= kMostScoreBytes;
+  return (dtype == 0 || h >= 64) && rows_heads * keys * 4 <= kMostScoreBytes;
 }
 
 template <typename T, int H>
@@ -203,10 +203,12 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
       const int w = launch_paged_weigh(c, r, key_weights, s);
       return w < 0 ? w : n + w;
     }
+  }
+  if constexpr (sizeof(T) == 4 || H >= 64) {
     const int64_t keys = static_cast<int64_t>(c.table_cols) * c.ps;
     const bool keep = key_weights && keeps_scores(c.dtype, H, static_cast<int64_t>(r.T) * r.Hq, keys);
-    float* scores = keep ? reinterpret_cast<float*>(ws + parts_bytes(H)) : nullptr;
-    n = launch_paged_mma(c, r, list, list_len, scores, ws, s);
+    float* scores = keep ? reinterpret_cast<float*>(ws + parts_bytes(c.dtype, H)) : nullptr;
+    n = sizeof(T) == 4 ? launch_paged_f32(c, r, list, list_len, scores, ws, s) : launch_paged_mma(c, r, list, list_len, scores, ws, s);
     if (n < 0) return n;
     if (keep) {
       int sms = 0;
@@ -227,8 +229,8 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
 }  // namespace
 
 int64_t paged_attention_workspace(int dtype, int h, int64_t rows_heads, int64_t keys, bool weigh) {
-  if (dtype != 1 || h < 64) return 0;
-  return parts_bytes(h) + (weigh && keeps_scores(dtype, h, rows_heads, keys) ? rows_heads * keys * 4 : 0);
+  if (dtype == 1 && h < 64) return 0;
+  return parts_bytes(dtype, h) + (weigh && keeps_scores(dtype, h, rows_heads, keys) ? rows_heads * keys * 4 : 0);
 }
 
 int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,

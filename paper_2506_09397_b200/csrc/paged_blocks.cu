@@ -18,6 +18,7 @@ struct BoundsLine {
   const PagedCache& c;
   const int32_t* first;
   __device__ __forceinline__ int32_t fault(const ReqView&) const { return SLED_ERR_ARG; }
+  __device__ __forceinline__ int min_share() const { return 8; }   // a block gets work for all its warps, at least
   __device__ __forceinline__ int from(int i) const { return first ? max(0, first[i]) / c.ps : 0; }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
@@ -27,7 +28,7 @@ struct BoundsLine {
     w.n_rb = 1;
     w.tiles = w.v.ok ? max(0, (w.v.n + c.ps - 1) / c.ps - from(i)) : 0;
     w.units = w.tiles ? c.Hkv : 0;
-    w.weight = kMinShare / 8;   // a block gets work for all its warps, at least
+    w.weight = 1;
     return w;
   }
 };
@@ -119,6 +120,7 @@ struct ScoreLine {
   const PagedRows& r;
   int n_blocks, n_local;
   __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
+  __device__ __forceinline__ int min_share() const { return 1; }
   __device__ __forceinline__ int tokens() const { return max(1, kUnitRows / (r.Hq / c.Hkv)); }   // of a unit
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
@@ -131,7 +133,7 @@ struct ScoreLine {
     w.tiles = (blocks - n_local + 63) / 64;
     w.n_rb = (w.v.m + tokens() - 1) / tokens();
     w.units = w.n_rb * c.Hkv;
-    w.weight = kMinShare;
+    w.weight = 1;
     return w;
   }
 };

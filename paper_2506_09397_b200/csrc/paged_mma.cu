@@ -9,6 +9,7 @@
 // partial (maximum, sum, output) for the merge kernel.
 // What binds: the bytes of K and V up to about 32 rows, the tensor path above.
 #include "gemm_tc.h"
+#include "kernels.h"
 #include "paged_schedule.cuh"
 #include "warp_mma.cuh"
 
@@ -493,7 +494,7 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
 }
 
 // The partial results of the units that were cut.  Block b finishes the one that block b began, a warp per row.
-template <int H>
+template <typename T, int H>
 __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, const PagedRows r, int list_len, int unit, int tile,
                                                           const Parts parts) {
   pdl_wait();
@@ -514,16 +515,17 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
   bool unused = false;
   if (r.parents && list_len == 0) {
     bool any = false;
-    if (static_cast<int>(threadIdx.x) < u.m) {
-      const int p = r.parents[u.row0 + threadIdx.x];
-      const bool wrong = p < -1 || p >= static_cast<int>(threadIdx.x);
-      parents[threadIdx.x] = static_cast<signed char>(wrong ? -2 : p);
-      any = wrong;
+    for (int i = threadIdx.x; i < u.m; i += blockDim.x) {
+      const int p = r.parents[u.row0 + i];
+      const bool wrong = p < -1 || p >= i;
+      parents[i] = static_cast<signed char>(wrong ? -2 : p);
+      any |= wrong;
     }
     unused = __syncthreads_or(any);
   }
   auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? d.y : 2 * (blockIdx.x + p)) * unit; };
-  for (int row = blockIdx.y * 16 + warp; row < u.count; row += gridDim.y * 16) {
+  const int n_warps = blockDim.x >> 5;
+  for (int row = blockIdx.y * n_warps + warp; row < u.count; row += gridDim.y * n_warps) {
     float M = -INFINITY;
     bool nan = false;
     for (int p = lane; p < n_parts; p += 32) {
@@ -562,9 +564,14 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
     }
     const float inv = none ? 0.f : 1.f / den;
     const int t = u.row0 + u.token(row), head = u.head(row);
-    uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t * r.out_stride + static_cast<int64_t>(head) * H) + lane * (D / 2);
+    T* out = reinterpret_cast<T*>(r.out) + t * r.out_stride + static_cast<int64_t>(head) * H + lane * D;
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int e = 0; e < D / 2; ++e) out[e] = none ? 0u : pack_bf16(num[2 * e] * inv, num[2 * e + 1] * inv);
+      for (int e = 0; e < D / 2; ++e) reinterpret_cast<uint32_t*>(out)[e] = none ? 0u : pack_bf16(num[2 * e] * inv, num[2 * e + 1] * inv);
+    } else {
+#pragma unroll
+      for (int e = 0; e < D; ++e) out[e] = none ? 0.f : num[e] * inv;
+    }
     if (r.lse && lane == 0) r.lse[static_cast<int64_t>(t) * r.Hq + head] = none ? -INFINITY : (M + log2f(den)) * kLn2;
   }
 }
@@ -619,9 +626,15 @@ int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int l
 int launch_paged_merge(const PagedCache& c, const PagedRows& r, int list_len, int unit_rows, int tile, int blocks, float* acc, float* ml,
                        int4* desc, cudaStream_t s) {
   const Parts parts{acc, ml, desc, nullptr, 0};
-  const dim3 grid(blocks, unit_rows > kUnitRows ? 4 : 2);
-  if (c.h == 128) SLED_LAUNCH_PDL(paged_merge_kernel<128>, grid, dim3(512), 0, s, c, r, list_len, unit_rows, tile, parts);
-  else SLED_LAUNCH_PDL(paged_merge_kernel<64>, grid, dim3(512), 0, s, c, r, list_len, unit_rows, tile, parts);
+  const dim3 grid(blocks, unit_rows > kUnitRows ? 4 : unit_rows < kUnitRows ? 1 : 2);
+  const int threads = min(512, 32 * unit_rows);   // a warp for each of a small unit's rows
+#define SLED_MERGE(T, H) SLED_LAUNCH_PDL((paged_merge_kernel<T, H>), grid, dim3(threads), 0, s, c, r, list_len, unit_rows, tile, parts)
+  if (c.dtype == BF16 && c.h == 128) SLED_MERGE(__nv_bfloat16, 128);
+  else if (c.dtype == BF16) SLED_MERGE(__nv_bfloat16, 64);
+  else if (c.h == 128) SLED_MERGE(float, 128);
+  else if (c.h == 64) SLED_MERGE(float, 64);
+  else SLED_MERGE(float, 32);
+#undef SLED_MERGE
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 

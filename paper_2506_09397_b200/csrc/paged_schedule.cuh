@@ -28,8 +28,9 @@ struct ReqWork {
 
 // Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM), in
 // sixteenths.  Beginning and ending a unit costs a number of tiles as well; it is spread over the unit's tiles.
-constexpr int kMinShare = 128;
-__device__ __forceinline__ int unit_weight(int tile, int unit, int tiles) { return min(tile + unit / tiles, kMinShare - 1); }
+constexpr int kMinShare = 128;      // of a block
+constexpr int kMinWarpShare = 24;   // of a warp that has a share of its own
+__device__ __forceinline__ int unit_weight(int tile, int unit, int tiles, int most = kMinShare - 1) { return min(tile + unit / tiles, most); }
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
 
 // The work of attention.  list_len > 0: units attend to chosen blocks, at most list_len per token.  kWholeRows: a unit has
@@ -41,6 +42,7 @@ struct AttentionLine {
   int list_len;
   int unit_rows = kUnitRows, tile = kTile;
   __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
+  __device__ __forceinline__ int min_share() const { return unit_rows < kUnitRows ? kMinWarpShare : kMinShare; }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
     w.v = req_view(c, r, i);
@@ -57,7 +59,7 @@ struct AttentionLine {
     if (list_len == kWholeRows) w.weight = min(16 + rows, kMinShare - 1);
     else if (unit_rows == kUnitRows) w.weight = unit_weight(tile_weight(min(rows, kUnitRows)), 32, w.tiles);
     else if (unit_rows > kUnitRows) w.weight = rows > kUnitRows * 2 ? unit_weight(38, 240, w.tiles) : unit_weight(16, 160, w.tiles);
-    else w.weight = unit_weight(8 + min(rows, unit_rows), 32, w.tiles);
+    else w.weight = unit_weight(12, 24, w.tiles, kMinWarpShare - 1);
     return w;
   }
 };
@@ -104,7 +106,7 @@ __device__ __forceinline__ void block_shares(const Line& line, int first, int mo
     total += sums[k];
   }
   // a part of the line that is longer than any tile holds the beginning of one
-  const int count = static_cast<int>(max(1LL, min(static_cast<long long>(most), total / kMinShare)));
+  const int count = static_cast<int>(max(1LL, min(static_cast<long long>(most), total / line.min_share())));
   const long long each = divide(total, count), rest = total - each * count;   // the first `rest` shares are one longer
   long long at = before + x - own;
   const long long end = at + own;
