@@ -28,7 +28,7 @@ struct ReqWork {
 
 // Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM), in
 // sixteenths.  Beginning and ending a unit costs a number of tiles as well; it is spread over the unit's tiles.
-constexpr int kMinShare = 128;      // of a block
+constexpr int kMinShare = 64;      // of a block
 constexpr int kMinWarpShare = 24;   // of a warp that has a share of its own
 __device__ __forceinline__ int unit_weight(int tile, int unit, int tiles, int most = kMinShare - 1) { return min(tile + unit / tiles, most); }
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
