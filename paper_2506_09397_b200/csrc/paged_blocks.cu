@@ -113,7 +113,9 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(PagedCache c, const i
 // the larger of two scores; a NaN is the largest
 __device__ __forceinline__ float larger(float a, float b) { return a != a || b != b ? NAN : fmaxf(a, b); }
 
-// Earlier blocks of a request's tokens, in tiles of 64, for units of (KV head, up to 64 rows); nothing where all blocks of
+constexpr int kScoreRows = 48;
+
+// Earlier blocks of a request's tokens, in tiles of 64, for units of (KV head, up to 48 rows); nothing where all blocks of
 // the request's last token are read anyway.
 struct ScoreLine {
   const PagedCache& c;
@@ -121,7 +123,7 @@ struct ScoreLine {
   int n_blocks, n_local;
   __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
   __device__ __forceinline__ int min_share() const { return 1; }
-  __device__ __forceinline__ int tokens() const { return max(1, kUnitRows / (r.Hq / c.Hkv)); }   // of a unit
+  __device__ __forceinline__ int tokens() const { return max(1, kScoreRows / (r.Hq / c.Hkv)); }   // of a unit
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
     w.v = req_view(c, r, i);
@@ -140,73 +142,96 @@ struct ScoreLine {
 
 // Scores on the tensor cores: rows [min(q, 0), max(q, 0)] against the bounds as they lie in memory, [low, high], a
 // contraction over 2 H.  The order of the terms is free, so a thread takes 16 consecutive bytes of a row as two
-// instructions' operands (both sides alike) and the bounds go from memory straight into registers.  A warp has 16 of the
-// tile's 64 blocks and all the unit's rows; the maximum over a group's heads is taken in shared memory.
+// instructions' operands (both sides alike) and the bounds go from memory straight into registers, a tile ahead.  A warp
+// has 16 of the tile's 64 blocks and all the unit's rows; the maximum over a group's heads is taken in shared memory.
 // Bound by the bytes of the bounds: 4 H per block and KV head.
 template <int H>
-__global__ void __launch_bounds__(128) block_score_kernel(PagedCache c, PagedRows r, const __nv_bfloat16* bounds, int n_blocks,
-                                                          int n_local, float* scores) {
-  constexpr int kRow = H + 8;                      // padded: eight rows' 16-byte pieces meet no bank twice
-  __shared__ __align__(16) __nv_bfloat16 qs[kUnitRows * kRow];
-  __shared__ float tile[kUnitRows][65];
+__global__ void __launch_bounds__(128, 3) block_score_kernel(PagedCache c, PagedRows r, const __nv_bfloat16* bounds, int n_blocks,
+                                                             int n_local, float* scores) {
+  constexpr int kRow = 2 * H + 8;                  // padded: eight rows' 16-byte pieces meet no bank twice
+  constexpr int kPieces = H / 16;                  // 32 terms each
+  __shared__ __align__(16) __nv_bfloat16 qs[kScoreRows * kRow];
+  __shared__ float tile[kScoreRows][65];
   pdl_launch_dependents();
   pdl_wait();
   const ScoreLine line{c, r, n_blocks, n_local};
   const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (share.from >= share.to) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3, group = r.Hq / c.Hkv;
+  const bool wide_q = (reinterpret_cast<uintptr_t>(r.q) & 15) == 0 && r.q_stride % 8 == 0;
   for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
     const int j0 = sg.rb * line.tokens(), nj = min(line.tokens(), w.v.m - j0), rows = nj * group;
-    __syncthreads();
-    for (int e = threadIdx.x; e < kUnitRows * (H / 2); e += 128) {
-      const int row = e / (H / 2), d = e % (H / 2);
-      uint32_t x = 0;
-      if (row < rows)
-        x = reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(r.q) + (w.v.row0 + j0 + row / group) * r.q_stride +
-                                              static_cast<int64_t>(sg.g * group + row % group) * H)[d];
-      *reinterpret_cast<uint32_t*>(qs + row * kRow + 2 * d) = x;
-    }
-    __syncthreads();
     const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
     const int early = (w.v.n - 1) / c.ps + 1 - n_local;
-    for (int t = sg.t0; t < sg.t1; ++t) {
+    uint4 bb[2][kPieces];                          // this thread's quarters of the bounds of two blocks
+    auto fetch = [&](int t) {
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) {
         const int b = t * 64 + warp * 16 + nt * 8 + gq;
-        uint4 bb[H / 16];                          // this thread's quarter of block b's bounds
-        if (b < early) {
-          const int page = checked_page(c, table[b]);
-          const uint4* src = reinterpret_cast<const uint4*>(bounds + (static_cast<int64_t>(page) * c.Hkv + sg.g) * 2 * H) + tq;
+        const bool there = b < early;
+        const uint4* src = reinterpret_cast<const uint4*>(bounds) + tq;
+        if (there) src += (static_cast<int64_t>(checked_page(c, table[b])) * c.Hkv + sg.g) * (2 * H / 8);
 #pragma unroll
-          for (int k = 0; k < H / 16; ++k) bb[k] = src[4 * k];
-        } else {
+        for (int k = 0; k < kPieces; ++k) bb[nt][k] = there ? src[4 * k] : make_uint4(0, 0, 0, 0);
+      }
+    };
+    fetch(sg.t0);
+    __syncthreads();
+    {
+      // the rows as the two halves of the contraction, all loads under way at once
+      constexpr int kVecs = kScoreRows * (H / 8) / 128;
+      uint4 x[kVecs];
 #pragma unroll
-          for (int k = 0; k < H / 16; ++k) bb[k] = make_uint4(0, 0, 0, 0);
-        }
-        for (int mt = 0; mt * 16 < rows; ++mt) {
-          float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int k = 0; k < H / 16; ++k) {       // 32 terms at a time; the first half of them against the lower bounds
-            const bool low = k < H / 32;
-            const uint4 lo = *reinterpret_cast<const uint4*>(qs + (mt * 16 + gq) * kRow + (k % (H / 32)) * 32 + tq * 8);
-            const uint4 hi = *reinterpret_cast<const uint4*>(qs + (mt * 16 + gq + 8) * kRow + (k % (H / 32)) * 32 + tq * 8);
-            auto half = [&](uint32_t x) {
-              const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&x), z = __floats2bfloat162_rn(0.f, 0.f);
-              const __nv_bfloat162 y = low ? __hmin2_nan(v, z) : __hmax2_nan(v, z);
-              return *reinterpret_cast<const uint32_t*>(&y);
-            };
-            const uint32_t a0[4] = {half(lo.x), half(hi.x), half(lo.y), half(hi.y)};
-            mma_bf16(s, a0, bb[k].x, bb[k].y);
-            const uint32_t a1[4] = {half(lo.z), half(hi.z), half(lo.w), half(hi.w)};
-            mma_bf16(s, a1, bb[k].z, bb[k].w);
-          }
-          const int col = warp * 16 + nt * 8 + 2 * tq;
-          tile[mt * 16 + gq][col] = s[0];
-          tile[mt * 16 + gq][col + 1] = s[1];
-          tile[mt * 16 + gq + 8][col] = s[2];
-          tile[mt * 16 + gq + 8][col + 1] = s[3];
+      for (int i = 0; i < kVecs; ++i) {
+        const int e = i * 128 + threadIdx.x, row = e / (H / 8), d = e % (H / 8);
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (row < rows) {
+          const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(r.q) + (w.v.row0 + j0 + row / group) * r.q_stride +
+                                                                  static_cast<int64_t>(sg.g * group + row % group) * H) + 4 * d;
+          if (wide_q) x[i] = *reinterpret_cast<const uint4*>(src);
+          else x[i] = make_uint4(src[0], src[1], src[2], src[3]);
         }
       }
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        const int e = i * 128 + threadIdx.x, row = e / (H / 8), d = e % (H / 8);
+        const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        uint32_t low[4], high[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          low[k] = Vec<__nv_bfloat16>::smaller(in[k], 0u);
+          high[k] = Vec<__nv_bfloat16>::larger(in[k], 0u);
+        }
+        *reinterpret_cast<uint4*>(qs + row * kRow + 8 * d) = make_uint4(low[0], low[1], low[2], low[3]);
+        *reinterpret_cast<uint4*>(qs + row * kRow + H + 8 * d) = make_uint4(high[0], high[1], high[2], high[3]);
+      }
+    }
+    __syncthreads();
+    for (int t = sg.t0; t < sg.t1; ++t) {
+#pragma unroll 1
+      for (int mt = 0; mt * 16 < rows; ++mt) {
+        float s[2][4] = {};
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+          const uint4 lo = *reinterpret_cast<const uint4*>(qs + (mt * 16 + gq) * kRow + k * 32 + tq * 8);
+          const uint4 hi = *reinterpret_cast<const uint4*>(qs + (mt * 16 + gq + 8) * kRow + k * 32 + tq * 8);
+          const uint32_t a0[4] = {lo.x, hi.x, lo.y, hi.y}, a1[4] = {lo.z, hi.z, lo.w, hi.w};
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            mma_bf16(s[nt], a0, bb[nt][k].x, bb[nt][k].y);
+            mma_bf16(s[nt], a1, bb[nt][k].z, bb[nt][k].w);
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          const int col = warp * 16 + nt * 8 + 2 * tq;
+          tile[mt * 16 + gq][col] = s[nt][0];
+          tile[mt * 16 + gq][col + 1] = s[nt][1];
+          tile[mt * 16 + gq + 8][col] = s[nt][2];
+          tile[mt * 16 + gq + 8][col + 1] = s[nt][3];
+        }
+      }
+      if (t + 1 < sg.t1) fetch(t + 1);
       __syncthreads();
       for (int e = threadIdx.x; e < nj * 64; e += 128) {
         const int j = e >> 6, col = e & 63, b = t * 64 + col;
@@ -257,7 +282,7 @@ __global__ void __launch_bounds__(256) block_score_row_kernel(PagedCache c, Page
 
 // The choice: one block per (token, KV head); the scores of up to kMostCached blocks stay in shared memory.
 constexpr int kMostCached = 8192;
-__global__ void __launch_bounds__(256) block_choice_kernel(PagedCache c, PagedRows r, int n_blocks, int n_local, const float* scores,
+__global__ void __launch_bounds__(1024) block_choice_kernel(PagedCache c, PagedRows r, int n_blocks, int n_local, const float* scores,
                                                            int32_t* list) {
   __shared__ int hist[2048], scratch[36];
   __shared__ uint32_t cached[kMostCached];
@@ -314,17 +339,19 @@ template <typename T, int H>
 int choice_typed(const PagedCache& c, const PagedRows& r, const void* bounds, int n_blocks, int n_local, float* scores, int32_t* list, cudaStream_t s) {
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
+  // few choices among many blocks: a large block each; many choices share an SM
+  const int threads = c.table_cols > 512 && static_cast<int64_t>(r.T) * c.Hkv <= 2 * sms ? 1024 : 256;
   if constexpr (sizeof(T) == 2 && H >= 64) {
-    if (r.Hq / c.Hkv <= kUnitRows) {
-      SLED_LAUNCH_PDL(block_score_kernel<H>, dim3(4 * sms), dim3(128), 0, s, c, r, static_cast<const T*>(bounds), n_blocks, n_local, scores);
-      SLED_LAUNCH_PDL(block_choice_kernel, dim3(r.T, c.Hkv), dim3(256), 0, s, c, r, n_blocks, n_local, static_cast<const float*>(scores), list);
+    if (r.Hq / c.Hkv <= kScoreRows) {
+      SLED_LAUNCH_PDL(block_score_kernel<H>, dim3(3 * sms), dim3(128), 0, s, c, r, static_cast<const T*>(bounds), n_blocks, n_local, scores);
+      SLED_LAUNCH_PDL(block_choice_kernel, dim3(r.T, c.Hkv), dim3(threads), 0, s, c, r, n_blocks, n_local, static_cast<const float*>(scores), list);
       return cudaGetLastError() == cudaSuccess ? 2 : -1;
     }
   }
   // enough blocks per row to fill the machine with few rows
   const int z = std::max(1, std::min((c.table_cols + 7) / 8, static_cast<int>(8LL * sms / (static_cast<long long>(r.T) * c.Hkv))));
   SLED_LAUNCH_PDL((block_score_row_kernel<T, H>), dim3(r.T, c.Hkv, z), dim3(256), 0, s, c, r, static_cast<const T*>(bounds), n_blocks, n_local, scores);
-  SLED_LAUNCH_PDL(block_choice_kernel, dim3(r.T, c.Hkv), dim3(256), 0, s, c, r, n_blocks, n_local, static_cast<const float*>(scores), list);
+  SLED_LAUNCH_PDL(block_choice_kernel, dim3(r.T, c.Hkv), dim3(threads), 0, s, c, r, n_blocks, n_local, static_cast<const float*>(scores), list);
   return cudaGetLastError() == cudaSuccess ? 2 : -1;
 }
 
