@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(256) block_score_row_kernel(PagedCache c, Page
 }
 
 // The choice: one block per (token, KV head); the scores of up to kMostCached blocks stay in shared memory.
-constexpr int kMostCached = 8192;
+constexpr int kMostCached = 4096;
 __global__ void __launch_bounds__(1024) block_choice_kernel(PagedCache c, PagedRows r, int n_blocks, int n_local, const float* scores,
                                                            int32_t* list) {
   __shared__ int hist[2048], scratch[36];

@@ -41,7 +41,11 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(PagedCache c, const flo
   float* w_out = weights_out + weight_layer * layer;
   const bool in_place = weights == weights_out;
   // row of a slot in the pool: fits 31 bits
-  auto row = [&](int x) { return (table[x / c.ps] * c.Hkv + g) * c.ps + x % c.ps; };
+  const int shift = (c.ps & (c.ps - 1)) == 0 ? __ffs(c.ps) - 1 : -1;   // a division costs more than the rest of it
+  auto row = [&](int x) {
+    const int page = shift >= 0 ? x >> shift : x / c.ps;
+    return (table[page] * c.Hkv + g) * c.ps + (x - page * c.ps);
+  };
   if (n <= budget) {
     if (!in_place)
       for (int x = threadIdx.x; x < n; x += kThreads) { const int at = row(x); w_out[at] = w[at]; }
