@@ -1,11 +1,13 @@
 // Attention over a paged fp32 cache (CUDA cores; sums, products and probabilities all in fp32).
 //
 // Every warp has a share of the line of key tiles to itself and meets no other: a unit is up to 4 query rows of a KV head,
-// a tile 32 keys.  K and V come in through two buffers of the warp's own, 32 keys x 32 dimensions at a time, by
-// 16-byte asynchronous copies, the next one under the current one's arithmetic.  Scores: a lane has a key and all rows
-// (its key's row is padded against bank conflicts, the queries are broadcast).  Output: a lane has one of
-// a piece's dimensions of all rows, the probabilities are broadcast.  With R rows a byte of cache meets R / 4 multiply-adds: the
-// bytes bind for single tokens, shared memory and the multiply-adds from about eight rows on.
+// a tile 32 keys.  K and V come in through a ring of the warp's own, 4 KB at a time, by 16-byte asynchronous copies, the next
+// ones under the current one's arithmetic: K as 32 dimensions of the tile's keys, V as whole rows of some of them, so that
+// neither loop knows which piece it has and the code stays short (a warp runs it a handful of times).  Scores: a lane has a
+// key and all rows (the key's 16-byte parts are permuted against bank conflicts, the queries are broadcast).  Output: a lane
+// has H / 32 neighbouring dimensions of all rows, the probabilities are broadcast.  With R rows a byte of cache meets R / 4
+// multiply-adds: the bytes bind for single tokens, shared memory and the multiply-adds from about eight rows on.
+#include <algorithm>
 #include "kernels.h"
 #include "paged_schedule.cuh"
 #include "warp_mma.cuh"
@@ -17,18 +19,19 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kRows = 4;           // of a unit at most (with more a warp's code is longer than its first run is worth, and there are fewer warps)
 constexpr int kKeys = 32;          // of a tile
+constexpr int kBuffers = 2;        // pieces under way or in use
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int H>
 struct F32 {
-  static constexpr int kDims = 32;                   // of a piece of K or V
-  static constexpr int kPieces = H / kDims;
-  static constexpr int kPitch = kDims + 4;
-  static constexpr int kBuffer = kKeys * kPitch;     // floats
+  static constexpr int kDims = 32;                   // of a piece of K
+  static constexpr int kPieces = H / kDims;          // of a tile's K, and of its V
+  static constexpr int kVKeys = kKeys / kPieces;     // of a piece of V
+  static constexpr int kBuffer = kKeys * kDims;      // floats
   static constexpr int kQ = kRows * H, kP = kRows * kKeys;
   static constexpr int kTree = kRows * (kMaxTreeNodes / 32) + kMaxTreeNodes / 4;
-  static constexpr int kWarp = 2 * kBuffer + kQ + kP + kTree;
+  static constexpr int kWarp = kBuffers * kBuffer + kQ + kP + kTree;
   static constexpr int kBytes = kWarps * kWarp * 4;
 };
 
@@ -44,15 +47,19 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+
 // One stretch of a unit.
 template <int H>
 __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, const ReqWork& w,
                                         const Segment& sg, const F32Parts& parts, float* mem) {
   using L = F32<H>;
-  constexpr int R = kRows, PER = 1;              // dimensions of a lane in a piece
+  constexpr int R = kRows, PER = H / 32;         // dimensions of a lane
   const int lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
   float* buffers = mem;
-  float* q = mem + 2 * L::kBuffer;
+  float* q = mem + kBuffers * L::kBuffer;
   float* p = q + L::kQ;
   uint32_t* tree = reinterpret_cast<uint32_t*>(p + L::kP);
   signed char* parents = reinterpret_cast<signed char*>(tree + kRows * (kMaxTreeNodes / 32));
@@ -68,27 +75,85 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
     end = w.v.n;
     prefix = w.v.n - w.v.m;
   }
-  auto token = [&](int i) { return list_len > 0 ? sg.j : (first + i) / group; };
-  auto head = [&](int i) { return sg.g * group + (first + i) % group; };
-  __syncwarp();
-#pragma unroll 1
-  for (int i = 0; i < R; ++i) {
-    const float* src = reinterpret_cast<const float*>(r.q) + (w.v.row0 + token(min(i, rows - 1))) * r.q_stride + static_cast<int64_t>(head(min(i, rows - 1))) * H;
-#pragma unroll
-    for (int d = 0; d < H / 32; ++d) q[i * H + d * 32 + lane] = i < rows ? src[d * 32 + lane] : 0.f;
-  }
+  // row i's token and head within the group, from row to row
+  const int token0 = list_len > 0 ? sg.j : first / group, head0 = list_len > 0 ? first : first - token0 * group;
+  auto next_row = [&](int& token, int& head) {
+    if (++head == group) {
+      head = 0;
+      ++token;
+    }
+  };
+  const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
+  const int32_t* mine = list_len > 0 ? list + (static_cast<int64_t>(w.v.row0 + sg.j) * c.Hkv + sg.g) * list_len : nullptr;
+  const int cpp = c.ps / 16, groups = (end + 15) / 16, shift = (cpp & (cpp - 1)) == 0 ? __ffs(cpp) - 1 : -1;
+  // where a tile's two groups of 16 keys begin, in keys of the pool, is found by lanes 0 and 1; the page's number is read a
+  // tile before it is looked at
+  auto block_of = [&](int t) {
+    const int e = min(t * 2 + (lane & 1), groups - 1);
+    return shift >= 0 ? e >> shift : e / cpp;
+  };
+  auto page_of = [&](int t) {
+    const int b = block_of(t);
+    return table[mine ? mine[b] : b];
+  };
+  auto locate = [&](int t, int page) {
+    const int e = min(t * 2 + (lane & 1), groups - 1);
+    return (checked_page(c, page) * c.Hkv + sg.g) * c.ps + (e - block_of(t) * cpp) * 16;
+  };
+  // the pieces in order, tile by tile those of K and then those of V, are fetched kBuffers - 1 ahead
+  int ft = sg.t0, fn = 0, fbuf = 0, page = page_of(ft), next_page = page_of(ft + 1), at = 0;
   const bool nodes = r.parents && list_len <= 0;
+  const int parent = nodes && lane < w.v.m ? r.parents[w.v.row0 + lane] : 0;
+  __syncwarp();              // the segment before is done with this warp's memory
+#pragma unroll 1
+  for (int i = 0, token = token0, head = head0; i < R; ++i) {
+    const float* src = reinterpret_cast<const float*>(r.q) + (w.v.row0 + token) * r.q_stride + static_cast<int64_t>(sg.g * group + head) * H;
+#pragma unroll
+    for (int d = 0; d < H; d += 32) copy4(smem_u32(q + i * H + d + lane), src + d + lane, i < rows);
+    if (i + 1 < rows) next_row(token, head);
+  }
+  auto fetch = [&] {
+    if (ft < sg.t1) {
+      if (fn == 0) {
+        at = locate(ft, page);
+        page = next_page;
+        next_page = page_of(ft + 2);
+      }
+      const bool is_v = fn >= L::kPieces;
+      constexpr int kVShift = H == 128 ? 5 : H == 64 ? 4 : 3;
+      const int chunk_shift = is_v ? kVShift : 3, key0 = is_v ? (fn - L::kPieces) * L::kVKeys : 0;   // 16-byte parts of a row
+      const float* pool = reinterpret_cast<const float*>(is_v ? c.v : c.k) + (is_v ? 0 : fn * L::kDims);
+      const uint32_t dst = smem_u32(buffers + fbuf * L::kBuffer);
+      const int ch = lane & ((1 << chunk_shift) - 1), step = 32 >> chunk_shift;
+      const int64_t g0 = __shfl_sync(0xffffffffu, at, 0), g1 = __shfl_sync(0xffffffffu, at, 1) - 16;
+      int key = key0 + (lane >> chunk_shift);
+#pragma unroll 4
+      for (int i = 0; i < L::kBuffer / 128; ++i) {
+        const int part = is_v ? i * 32 + lane : (i * 32 + lane) ^ (key & 7);
+        copy16(dst + part * 16, pool + ((key < 16 ? g0 : g1) + key) * H + ch * 4, ft * kKeys + key < end);
+        key += step;
+      }
+      if (++fn == 2 * L::kPieces) {
+        fn = 0;
+        ++ft;
+      }
+      if (++fbuf == kBuffers) fbuf = 0;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll 1
+  for (int i = 0; i < kBuffers - 1; ++i) fetch();
   bool dead = false;         // of row `lane`
   if (nodes) {
     for (int i = lane; i < w.v.m; i += 32) {
-      const int x = r.parents[w.v.row0 + i];
+      const int x = i == lane ? parent : r.parents[w.v.row0 + i];
       if (x < -2 || x >= i) set_status(c.status, SLED_ERR_ARG);
       parents[i] = static_cast<signed char>(x < -1 || x >= i ? -2 : x);
     }
     __syncwarp();
     if (lane < rows) {
       uint32_t bits[kMaxTreeNodes / 32] = {};
-      int a = token(lane);
+      int a = (first + lane) / group;
       while (a >= 0) {
 #pragma unroll
         for (int k = 0; k < kMaxTreeNodes / 32; ++k)
@@ -103,35 +168,6 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
   __syncwarp();
   const uint32_t dead_rows = __ballot_sync(0xffffffffu, dead);
 
-  const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
-  const int32_t* mine = list_len > 0 ? list + (static_cast<int64_t>(w.v.row0 + sg.j) * c.Hkv + sg.g) * list_len : nullptr;
-  const int cpp = c.ps / 16, groups = (end + 15) / 16;
-  // where the tile's two groups of 16 keys begin, in keys of the pool; found by lanes 0 and 1
-  auto locate = [&](int t) {
-    int at = 0;
-    const int e = t * 2 + (lane & 1);
-    if (e < groups) {
-      const int b = e / cpp;
-      at = (checked_page(c, table[mine ? mine[b] : b]) * c.Hkv + sg.g) * c.ps + (e - b * cpp) * 16;
-    }
-    return at;
-  };
-  int at = locate(sg.t0), at_next = 0;
-  // piece n of tile t: the pieces of K, then those of V
-  auto fetch = [&](int t, int n, int where, int buffer) {
-    const float* pool = reinterpret_cast<const float*>(n < L::kPieces ? c.k : c.v) + n % L::kPieces * L::kDims;
-    const uint32_t dst = smem_u32(buffers + buffer * L::kBuffer);
-    constexpr int kChunks = L::kDims / 4;        // 16-byte pieces of a row
-#pragma unroll 4
-    for (int i = 0; i < kChunks; ++i) {
-      const int e = i * 32 + lane, key = e / kChunks, ch = e % kChunks;
-      const int g0 = __shfl_sync(0xffffffffu, where, 0), g1 = __shfl_sync(0xffffffffu, where, 1);
-      const int64_t row = static_cast<int64_t>(key < 16 ? g0 : g1) + (key & 15);
-      copy16(dst + (key * L::kPitch + ch * 4) * 4, pool + row * H + ch * 4, t * kKeys + key < end);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-
   float m[R], l[R], o[R][H / 32];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -142,33 +178,28 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
   }
   const float scale = r.scale * kLog2e;
   int buffer = 0;
-  fetch(sg.t0, 0, at, 0);
+#pragma unroll 1
   for (int t = sg.t0; t < sg.t1; ++t) {
-    if (t + 1 < sg.t1) at_next = locate(t + 1);
     float s[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) s[i] = 0.f;
     const int x = t * kKeys + lane;
     const bool masked = (t + 1) * kKeys > prefix;
-#pragma unroll
+#pragma unroll 1
     for (int n = 0; n < 2 * L::kPieces; ++n) {
-      // the next piece goes into the other buffer, which everybody has left
+      asm volatile("cp.async.wait_group %0;" ::"n"(kBuffers - 2) : "memory");
       __syncwarp();
-      const bool last = n + 1 == 2 * L::kPieces;
-      if (!last) fetch(t, n + 1, at, buffer ^ 1);
-      else if (t + 1 < sg.t1) fetch(t + 1, 0, at_next, buffer ^ 1);
-      else asm volatile("cp.async.commit_group;" ::: "memory");
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
-      __syncwarp();
+      fetch();             // into the buffer of the piece before, which everybody has left
       const float* piece = buffers + buffer * L::kBuffer;
+      if (++buffer == kBuffers) buffer = 0;
       if (n < L::kPieces) {
         const float* qn = q + n * L::kDims;
 #pragma unroll 2
-        for (int d = 0; d < L::kDims; d += 4) {
-          const float4 k4 = *reinterpret_cast<const float4*>(piece + lane * L::kPitch + d);
+        for (int d = 0; d < L::kDims / 4; ++d) {
+          const float4 k4 = *reinterpret_cast<const float4*>(piece + lane * L::kDims + (d ^ (lane & 7)) * 4);
 #pragma unroll
           for (int i = 0; i < R; ++i) {
-            const float4 q4 = *reinterpret_cast<const float4*>(qn + i * H + d);
+            const float4 q4 = *reinterpret_cast<const float4*>(qn + i * H + d * 4);
             s[i] = fmaf(q4.x, k4.x, s[i]);
             s[i] = fmaf(q4.y, k4.y, s[i]);
             s[i] = fmaf(q4.z, k4.z, s[i]);
@@ -176,6 +207,7 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
           }
         }
         if (n + 1 == L::kPieces) {
+          int token = token0, head = head0;
 #pragma unroll
           for (int i = 0; i < R; ++i) {
             s[i] *= scale;
@@ -184,74 +216,99 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
               if (see && x >= prefix) {
                 const int a = x - prefix;
                 if (nodes) see = (tree[i * (kMaxTreeNodes / 32) + (a >> 5)] >> (a & 31)) & 1u;
-                else if (list_len <= 0) see = a <= token(i);
+                else if (list_len <= 0) see = a <= token;
               }
               if (!see) s[i] = -INFINITY;
             }
             if (parts.scores && i < rows && x < end)
-              parts.scores[(static_cast<int64_t>(w.v.row0 + token(i)) * r.Hq + head(i)) * parts.keys + x] = s[i];
+              parts.scores[(static_cast<int64_t>(w.v.row0 + token) * r.Hq + sg.g * group + head) * parts.keys + x] = s[i];
+            next_row(token, head);
             const float top = fmaxf(m[i], warp_max(s[i])), ref = top == -INFINITY ? 0.f : top;
             const float f = exp2f(m[i] - ref), pi = exp2f(s[i] - ref);
             m[i] = top;
             l[i] = l[i] * f + pi;              // of this lane's keys
 #pragma unroll
-            for (int d = 0; d < H / 32; ++d) o[i][d] *= f;
+            for (int d = 0; d < PER; ++d) o[i][d] *= f;
             p[i * kKeys + lane] = pi;
           }
           __syncwarp();
         }
       } else {
+        const float* pn = p + (n - L::kPieces) * L::kVKeys;
 #pragma unroll 1
-        for (int key = 0; key < kKeys; key += 4) {
+        for (int key = 0; key < L::kVKeys; key += 4) {
           float v[4][PER];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            v[e][0] = piece[(key + e) * L::kPitch + lane];
+            const float* src = piece + (key + e) * H + lane * PER;
+            if constexpr (PER == 4) {
+              const float4 y = *reinterpret_cast<const float4*>(src);
+              v[e][0] = y.x; v[e][1] = y.y; v[e][2] = y.z; v[e][3] = y.w;
+            } else if constexpr (PER == 2) {
+              const float2 y = *reinterpret_cast<const float2*>(src);
+              v[e][0] = y.x; v[e][1] = y.y;
+            } else {
+              v[e][0] = *src;
+            }
           }
-#pragma unroll
-          for (int i = 0; i < R; ++i) {
-            const float4 p4 = *reinterpret_cast<const float4*>(p + i * kKeys + key);
-            const float pe[4] = {p4.x, p4.y, p4.z, p4.w};
+          // a probability of 0 does not silence a value that is not finite: such keys are left out where they are masked
+          bool finite = true;
+          if (masked)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
+              for (int d = 0; d < PER; ++d) finite = finite && fabsf(v[e][d]) < INFINITY;
+          if (finite) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const float4 p4 = *reinterpret_cast<const float4*>(pn + i * kKeys + key);
+#pragma unroll
               for (int d = 0; d < PER; ++d) {
-                // (n is a constant of the unrolled loop: so is the place in o)
-                float& y = o[i][(n - L::kPieces) * PER + d];
-                // a probability of 0 does not silence a value that is not finite
-                if (masked) y = pe[e] != 0.f ? fmaf(pe[e], v[e][d], y) : y;
-                else y = fmaf(pe[e], v[e][d], y);
+                o[i][d] = fmaf(p4.x, v[0][d], o[i][d]);
+                o[i][d] = fmaf(p4.y, v[1][d], o[i][d]);
+                o[i][d] = fmaf(p4.z, v[2][d], o[i][d]);
+                o[i][d] = fmaf(p4.w, v[3][d], o[i][d]);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll 1
+              for (int e = 0; e < 4; ++e) {
+                const float pe = pn[i * kKeys + key + e];
+                if (pe == 0.f) continue;
+#pragma unroll
+                for (int d = 0; d < PER; ++d) o[i][d] = fmaf(pe, piece[(key + e) * H + lane * PER + d], o[i][d]);
               }
           }
         }
       }
-      buffer ^= 1;
     }
-    at = at_next;
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
 
+  int token = token0, head = head0;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     if (i >= rows) break;
     float sum = warp_sum(l[i]), top = m[i];
     const bool none = (dead_rows >> i) & 1u;
     if (none) { sum = 0.f; top = -INFINITY; }
-    const int64_t t_row = w.v.row0 + token(i);
+    const int64_t t_row = w.v.row0 + token;
+    const int h_row = sg.g * group + head;
+    next_row(token, head);
     float* dst;
     float f = 1.f;
     if (sg.whole) {
-      dst = reinterpret_cast<float*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(head(i)) * H;
+      dst = reinterpret_cast<float*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(h_row) * H;
       f = sum == 0.f ? 0.f : 1.f / sum;
-      if (r.lse && lane == 0) r.lse[t_row * r.Hq + head(i)] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      if (r.lse && lane == 0) r.lse[t_row * r.Hq + h_row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     } else {
       dst = parts.acc + (static_cast<int64_t>(sg.slot) * kRows + i) * H;
       if (lane == 0) *reinterpret_cast<float2*>(parts.ml + (static_cast<int64_t>(sg.slot) * kRows + i) * 2) = make_float2(top, sum);
     }
 #pragma unroll
-    for (int n = 0; n < L::kPieces; ++n)
-#pragma unroll
-      for (int d = 0; d < PER; ++d) dst[n * L::kDims + lane * PER + d] = none ? 0.f : o[i][n * PER + d] * f;
+    for (int d = 0; d < PER; ++d) dst[lane * PER + d] = none ? 0.f : o[i][d] * f;
   }
 }
 
@@ -277,7 +334,7 @@ __global__ void __launch_bounds__(32 * kWarps) paged_f32_kernel(const PagedCache
 }
 
 constexpr int kMaxDevices = 64;
-constexpr int kPerSm = 4;                     // blocks (shared memory holds five, or four with head_dim 128)
+constexpr int kPerSm = 4;                     // blocks at most
 constexpr int kMaxShares = kMaxPagedBlocks / 2 * kPerSm * kWarps;
 
 template <int H>
@@ -290,7 +347,8 @@ int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int l
     if (cudaFuncSetAttribute(paged_f32_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, F32<H>::kBytes) != cudaSuccess) return -1;
     configured[dev] = true;
   }
-  const int blocks = min(kPerSm * sms, kMaxShares / kWarps);
+  constexpr int kResident = std::min(kPerSm, 227 * 1024 / (F32<H>::kBytes + 1024));   // as many as shared memory holds
+  const int blocks = min(kResident * sms, kMaxShares / kWarps);
   F32Parts parts;
   parts.acc = reinterpret_cast<float*>(ws);
   parts.ml = parts.acc + 2LL * kMaxShares * kRows * H;

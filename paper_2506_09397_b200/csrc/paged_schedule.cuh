@@ -70,6 +70,7 @@ struct Share {
   long long from, to;    // this share's part of the line
   long long total;
   int count;             // shares that the line is cut into: every one of them gets a tile
+  ReqWork w;             // of the first request
 };
 
 // quotient of numbers that mostly fit 32 bits
@@ -86,8 +87,10 @@ __device__ __forceinline__ void block_shares(const Line& line, int first, int mo
   const int n_reqs = line.c.n_reqs, per = (n_reqs + blockDim.x - 1) / blockDim.x;
   const int i0 = min(static_cast<int>(threadIdx.x) * per, n_reqs), i1 = min(i0 + per, n_reqs);
   long long own = 0;
+  ReqWork w;
+#pragma unroll 1
   for (int i = i0; i < i1; ++i) {
-    const ReqWork w = line(i);
+    w = line(i);
     own += w.cost();
     if (first == 0 && !w.v.ok) set_status(line.c.status, line.fault(w.v));
   }
@@ -98,7 +101,7 @@ __device__ __forceinline__ void block_shares(const Line& line, int first, int mo
     if (lane >= o) x += y;
   }
   if (lane == 31) sums[warp] = x;
-  if (threadIdx.x < kShares) out[threadIdx.x] = Share{0, 0, 0, 0, 0, 1};
+  if (threadIdx.x < kShares) out[threadIdx.x].from = out[threadIdx.x].to = out[threadIdx.x].at = 0;
   __syncthreads();
   long long before = 0, total = 0;
   for (int k = 0; k < nw; ++k) {
@@ -110,19 +113,22 @@ __device__ __forceinline__ void block_shares(const Line& line, int first, int mo
   const long long each = divide(total, count), rest = total - each * count;   // the first `rest` shares are one longer
   long long at = before + x - own;
   const long long end = at + own;
-#pragma unroll
+#pragma unroll 1
   for (int k = 0; k < kShares; ++k) {
     const int mine = first + k;
     const long long from = each * mine + min(static_cast<long long>(mine), rest), to = from + each + (mine < rest);
     if (mine < count && from < to && at <= from && from < end) {
       long long begin = at;
       int i = i0;
-      for (;; ++i) {
-        const long long cost = line(i).cost();
-        if (from < begin + cost) break;
-        begin += cost;
+      if (per > 1) {         // (a thread that has one request knows it already)
+#pragma unroll 1
+        for (;; ++i) {
+          w = line(i);
+          if (from < begin + w.cost()) break;
+          begin += w.cost();
+        }
       }
-      out[k] = Share{i, begin, from, to, total, count};
+      out[k] = Share{i, begin, from, to, total, count, w};
     }
   }
   __syncthreads();
@@ -158,20 +164,16 @@ struct Walk {
   long long at, lt = 0, lt_end = 0;
   ReqWork w;               // of the current segment's request
   bool first = true, fresh = true;
-  __device__ __forceinline__ Walk(const Line& l, const Share& share, int b) : line(l), s(share), block(b), i(share.req), at(share.at) {
-    w.tiles = 1;
-    w.units = 0;
-    w.weight = 1;
-  }
+  __device__ __forceinline__ Walk(const Line& l, const Share& share, int b) : line(l), s(share), block(b), i(share.req), at(share.at), w(share.w) {}
   __device__ __forceinline__ bool next(Segment& g) {
     while (lt >= lt_end) {
       if (!fresh) {
         at += w.cost();
         ++i;
       }
-      fresh = false;
       if (at >= s.to) return false;
-      w = line(i);
+      if (!fresh) w = line(i);
+      fresh = false;
       lt_end = min(w.count(), divide(s.to - at + w.weight - 1, w.weight));
       lt = s.from > at ? divide(s.from - at + w.weight - 1, w.weight) : 0;
     }
