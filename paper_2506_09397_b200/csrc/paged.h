@@ -58,9 +58,8 @@ bool paged_tc_serves(const PagedCache& c, const PagedRows& r);
 int launch_paged_tc(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s);
 // adds the attention weights of the keys (bf16, head_dim 64 or 128; r.lse is set, paged_tc_serves)
 int launch_paged_weigh(const PagedCache& c, const PagedRows& r, float* key_weights, cudaStream_t s);
-// joins the partial results of units of unit_rows rows that were cut in tiles of `tile` keys over `blocks` blocks
-int launch_paged_merge(const PagedCache& c, const PagedRows& r, int list_len, int unit_rows, int tile, int blocks, float* acc, float* ml,
-                       int4* desc, cudaStream_t s);
+// joins the partial results of units of unit_rows rows that were cut over `blocks` shares; desc: two words of 16 bytes a share
+int launch_paged_merge(const PagedCache& c, const PagedRows& r, int unit_rows, int blocks, float* acc, float* ml, int4* desc, cudaStream_t s);
 // the number of SMs of the current device, or a negative value
 int paged_device(int* sms);
 // bounds[page][Hkv][2][h] of the pages that hold the keys first[i] .. n_kv[i]-1 (first null: all keys)

@@ -38,7 +38,7 @@ struct F32 {
 struct F32Parts {
   float* acc;      // [2 * shares][kRows][H]
   float* ml;       // [2 * shares][kRows][2]
-  int4* desc;      // [shares]
+  int4* desc;      // [shares][2]
   float* scores;   // null, or [rows][Hq][keys]
   int64_t keys;
 };
@@ -322,13 +322,13 @@ __global__ void __launch_bounds__(32 * kWarps) paged_f32_kernel(const PagedCache
   const AttentionLine line{c, r, list_len, kRows, kKeys};
   block_shares<kWarps>(line, blockIdx.x * kWarps, gridDim.x * kWarps, shares);
   const int warp = threadIdx.x >> 5, mine = blockIdx.x * kWarps + warp;
-  if ((threadIdx.x & 31) == 0) parts.desc[mine] = make_int4(-1, 0, 0, 0);
+  if ((threadIdx.x & 31) == 0) leave_none(parts.desc, mine);
   float* mem = smem + warp * F32<H>::kWarp;
   for_segments(line, shares[warp], mine, [&](const ReqWork& w, const Segment& sg) {
     work_on<H>(c, r, list, list_len, w, sg, parts, mem);
     if (sg.last_block >= 0 && (threadIdx.x & 31) == 0) {
-      const int unit = (list_len > 0 ? sg.j * c.Hkv + sg.g : sg.g) * w.n_rb + sg.rb;
-      parts.desc[mine] = make_int4(sg.last_block, sg.slot, sg.req, unit);
+      const int first = sg.rb * kRows, group = r.Hq / c.Hkv;
+      leave_cut(parts.desc, mine, sg, w.v.row0, w.v.m, list_len > 0 ? sg.j : -1, first, min(kRows, (list_len > 0 ? group : w.v.m * group) - first));
     }
   });
 }
@@ -357,13 +357,13 @@ int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int l
   parts.keys = static_cast<int64_t>(c.table_cols) * c.ps;
   SLED_LAUNCH_PDL(paged_f32_kernel<H>, dim3(blocks), dim3(32 * kWarps), F32<H>::kBytes, s, c, r, list, list_len, parts);
   if (cudaGetLastError() != cudaSuccess) return -1;
-  const int n = launch_paged_merge(c, r, list_len, kRows, kKeys, blocks * kWarps, parts.acc, parts.ml, parts.desc, s);
+  const int n = launch_paged_merge(c, r, kRows, blocks * kWarps, parts.acc, parts.ml, parts.desc, s);
   return n < 0 ? n : n + 1;
 }
 
 }  // namespace
 
-int64_t paged_f32_workspace(int h) { return 2LL * kMaxShares * kRows * (h + 2) * 4 + kMaxShares * 16LL; }
+int64_t paged_f32_workspace(int h) { return 2LL * kMaxShares * kRows * (h + 2) * 4 + kMaxShares * 32LL; }
 
 int launch_paged_f32(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s) {
   if (c.h == 128) return launch_h<128>(c, r, list, list_len, scores, ws, s);

@@ -8,6 +8,8 @@
 // paged_schedule.cuh says: all blocks resident, two on an SM, equal shares of the line of tiles; units that were cut leave
 // partial (maximum, sum, output) for the merge kernel.
 // What binds: the bytes of K and V up to about 32 rows, the tensor path above.
+#include <type_traits>
+
 #include "gemm_tc.h"
 #include "kernels.h"
 #include "paged_schedule.cuh"
@@ -59,7 +61,7 @@ struct UnitRows {
 struct Parts {
   float* acc;      // [2 * blocks][kUnitRows][H], not normalised
   float* ml;       // [2 * blocks][kUnitRows][2]
-  int4* desc;      // [blocks] {last block or -1, first slot, request, unit of the request}
+  int4* desc;      // [blocks][2]: CutUnit
   float* scores;   // null, or [rows][Hq][keys]
   int64_t keys;
 };
@@ -357,8 +359,8 @@ __device__ __forceinline__ void consume(const PagedCache& c, const PagedRows& r,
   }
 }
 
-__device__ __forceinline__ UnitRows unit_rows(const PagedCache& c, const PagedRows& r, int list_len, const ReqWork& w, const Segment& sg,
-                                              int rows = kUnitRows) {
+__device__ __forceinline__ UnitRows unit_rows(const PagedCache& c, const PagedRows& r, int list_len, const ReqWork& w, const Segment& sg) {
+  constexpr int rows = kUnitRows;
   UnitRows u;
   u.req = sg.req;
   u.row0 = w.v.row0;
@@ -409,7 +411,7 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
   pdl_wait();
   const AttentionLine line{c, r, list_len};
   const Share share = block_share(line, blockIdx.x, gridDim.x);
-  if (threadIdx.x == 0) parts.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  if (threadIdx.x == 0) leave_none(parts.desc, blockIdx.x);
   if (share.from >= share.to) return;
 
   if (warp == 4) {
@@ -479,10 +481,7 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
       if (u.count <= 16) consume<H, 1>(c, r, u, sg, ring, stop, merge, tree, parts);
       else if (u.count <= 32) consume<H, 2>(c, r, u, sg, ring, stop, merge, tree, parts);
       else consume<H, 4>(c, r, u, sg, ring, stop, merge, tree, parts);
-      if (sg.last_block >= 0 && threadIdx.x == 0) {
-        const int unit = (list_len > 0 ? sg.j * c.Hkv + sg.g : sg.g) * w.n_rb + sg.rb;
-        parts.desc[blockIdx.x] = make_int4(sg.last_block, sg.slot, sg.req, unit);
-      }
+      if (sg.last_block >= 0 && threadIdx.x == 0) leave_cut(parts.desc, blockIdx.x, sg, u.row0, u.m, u.j, u.first, u.count);
     });
   }
   __syncthreads();
@@ -493,27 +492,36 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
   }
 }
 
-// The partial results of the units that were cut.  Block b finishes the one that block b began, a warp per row.
+// The partial results of the units that were cut.  Block b finishes the one that block b began, a warp per row: the first
+// kAtOnce parts of a row and all parts' maxima and sums are under way before any of them is looked at.  Bound by the latency
+// of two dependent loads and of its launch.
 template <typename T, int H>
-__global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, const PagedRows r, int list_len, int unit, int tile,
-                                                          const Parts parts) {
+__global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, const PagedRows r, int unit, const Parts parts) {
   pdl_wait();
-  const int4 d = parts.desc[blockIdx.x];
-  if (d.x < 0) return;
-  constexpr int D = H / 32;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const ReqWork w = AttentionLine{c, r, list_len, unit, tile}(d.z);
-  Segment sg{};
-  sg.req = d.z;
-  sg.rb = d.w % w.n_rb;
-  sg.g = d.w / w.n_rb % c.Hkv;
-  sg.j = d.w / w.n_rb / c.Hkv;
-  const UnitRows u = unit_rows(c, r, list_len, w, sg, unit);
-  const int n_parts = d.x - static_cast<int>(blockIdx.x) + 1;
+  const CutUnit u = cut_unit(parts.desc, blockIdx.x);
+  if (u.last_block < 0) return;
+  constexpr int D = H / 32, kAtOnce = 8;
+  using Words = typename std::conditional<D == 4, float4, typename std::conditional<D == 2, float2, float>::type>::type;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
+  const int n_parts = u.last_block - static_cast<int>(blockIdx.x) + 1, n_warps = blockDim.x >> 5;
+  auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? u.slot : 2 * (blockIdx.x + p)) * unit; };
+  int row = blockIdx.y * n_warps + warp;
+  float2 ml;
+  float acc[kAtOnce][D];
+  auto part = [&](int p, float* to) { *reinterpret_cast<Words*>(to) = *reinterpret_cast<const Words*>(parts.acc + (slot(p) + row) * H + lane * D); };
+  auto load = [&] {
+    ml = make_float2(-INFINITY, 0.f);
+    if (row >= u.count) return;
+    if (lane < n_parts) ml = *reinterpret_cast<const float2*>(parts.ml + (slot(lane) + row) * 2);
+#pragma unroll
+    for (int p = 0; p < kAtOnce; ++p)
+      if (p < n_parts) part(p, acc[p]);
+  };
+  load();
   // Rows of unused nodes are 0, whatever the partial results say: a stretch of keys without nodes does not know of them.
   __shared__ signed char parents[kMaxTreeNodes];
   bool unused = false;
-  if (r.parents && list_len == 0) {
+  if (r.parents && u.j < 0) {
     bool any = false;
     for (int i = threadIdx.x; i < u.m; i += blockDim.x) {
       const int p = r.parents[u.row0 + i];
@@ -523,47 +531,56 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
     }
     unused = __syncthreads_or(any);
   }
-  auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? d.y : 2 * (blockIdx.x + p)) * unit; };
-  const int n_warps = blockDim.x >> 5;
-  for (int row = blockIdx.y * n_warps + warp; row < u.count; row += gridDim.y * n_warps) {
-    float M = -INFINITY;
-    bool nan = false;
-    for (int p = lane; p < n_parts; p += 32) {
-      const float2 ml = *reinterpret_cast<const float2*>(parts.ml + (slot(p) + row) * 2);
-      M = fmaxf(M, ml.x);
-      nan |= ml.y != ml.y;
+  for (; row < u.count; row += gridDim.y * n_warps, load()) {
+    float M = ml.x;
+    bool nan = ml.y != ml.y;
+    for (int p = 32 + lane; p < n_parts; p += 32) {
+      const float2 x = *reinterpret_cast<const float2*>(parts.ml + (slot(p) + row) * 2);
+      M = fmaxf(M, x.x);
+      nan |= x.y != x.y;
     }
     M = warp_max(M);
     nan = __any_sync(0xffffffffu, nan);
     const float ref = M == -INFINITY ? 0.f : M;
-    float den = 0.f, num[D];
+    float f = exp2_approx(ml.x - ref), den = f * ml.y, num[D];
 #pragma unroll
     for (int e = 0; e < D; ++e) num[e] = 0.f;
+#pragma unroll
+    for (int p = 0; p < kAtOnce; ++p) {
+      const float fp = __shfl_sync(0xffffffffu, f, p);
+      if (p < n_parts) {
+#pragma unroll
+        for (int e = 0; e < D; ++e) num[e] = fmaf(fp, acc[p][e], num[e]);
+      }
+    }
     for (int p0 = 0; p0 < n_parts; p0 += 32) {
-      float f = 0.f;
-      if (p0 + lane < n_parts) {
-        const float2 ml = *reinterpret_cast<const float2*>(parts.ml + (slot(p0 + lane) + row) * 2);
-        f = exp2_approx(ml.x - ref);
-        den = fmaf(f, ml.y, den);
+      if (p0 > 0) {
+        f = 0.f;
+        if (p0 + lane < n_parts) {
+          const float2 x = *reinterpret_cast<const float2*>(parts.ml + (slot(p0 + lane) + row) * 2);
+          f = exp2_approx(x.x - ref);
+          den = fmaf(f, x.y, den);
+        }
       }
       const int here = min(32, n_parts - p0);
 #pragma unroll 4
-      for (int p = 0; p < here; ++p) {
+      for (int p = p0 > 0 ? 0 : kAtOnce; p < here; ++p) {
         const float fp = __shfl_sync(0xffffffffu, f, p);
-        const float* src = parts.acc + (slot(p0 + p) + row) * H + lane * D;
+        float x[D];
+        part(p0 + p, x);
 #pragma unroll
-        for (int e = 0; e < D; ++e) num[e] = fmaf(fp, src[e], num[e]);
+        for (int e = 0; e < D; ++e) num[e] = fmaf(fp, x[e], num[e]);
       }
     }
     den = warp_sum(den);
     bool none = M == -INFINITY && !nan;
     if (unused) {
-      int a = u.token(row);
+      int a = (u.first + row) / group;
       while (a >= 0) a = parents[a];
       none |= a == -2;
     }
     const float inv = none ? 0.f : 1.f / den;
-    const int t = u.row0 + u.token(row), head = u.head(row);
+    const int of = (u.first + row) / group, t = u.row0 + (u.j >= 0 ? u.j : of), head = u.g * group + (u.first + row) - of * group;
     T* out = reinterpret_cast<T*>(r.out) + t * r.out_stride + static_cast<int64_t>(head) * H + lane * D;
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -617,18 +634,17 @@ int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int l
   parts.keys = static_cast<int64_t>(c.table_cols) * c.ps;
   SLED_LAUNCH_PDL(paged_mma_kernel<H>, dim3(blocks), dim3(160), Smem<H>::kTotal, s, c, r, list, list_len, parts, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return -1;
-  const int n = launch_paged_merge(c, r, list_len, kUnitRows, kTile, blocks, parts.acc, parts.ml, parts.desc, s);
+  const int n = launch_paged_merge(c, r, kUnitRows, blocks, parts.acc, parts.ml, parts.desc, s);
   return n < 0 ? n : n + 1;
 }
 
 }  // namespace
 
-int launch_paged_merge(const PagedCache& c, const PagedRows& r, int list_len, int unit_rows, int tile, int blocks, float* acc, float* ml,
-                       int4* desc, cudaStream_t s) {
+int launch_paged_merge(const PagedCache& c, const PagedRows& r, int unit_rows, int blocks, float* acc, float* ml, int4* desc, cudaStream_t s) {
   const Parts parts{acc, ml, desc, nullptr, 0};
   const dim3 grid(blocks, unit_rows > kUnitRows ? 4 : unit_rows < kUnitRows ? 1 : 2);
   const int threads = min(512, 32 * unit_rows);   // a warp for each of a small unit's rows
-#define SLED_MERGE(T, H) SLED_LAUNCH_PDL((paged_merge_kernel<T, H>), grid, dim3(threads), 0, s, c, r, list_len, unit_rows, tile, parts)
+#define SLED_MERGE(T, H) SLED_LAUNCH_PDL((paged_merge_kernel<T, H>), grid, dim3(threads), 0, s, c, r, unit_rows, parts)
   if (c.dtype == BF16 && c.h == 128) SLED_MERGE(__nv_bfloat16, 128);
   else if (c.dtype == BF16) SLED_MERGE(__nv_bfloat16, 64);
   else if (c.h == 128) SLED_MERGE(float, 128);
@@ -639,7 +655,7 @@ int launch_paged_merge(const PagedCache& c, const PagedRows& r, int list_len, in
 }
 
 int64_t paged_mma_workspace(int h) {
-  return 2LL * kMaxPagedBlocks * kUnitRows * (h + 2) * 4 + kMaxPagedBlocks * 16LL;
+  return 2LL * kMaxPagedBlocks * kUnitRows * (h + 2) * 4 + kMaxPagedBlocks * 32LL;
 }
 
 int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s) {

@@ -155,6 +155,22 @@ struct Segment {
   int last_block;        // cut units, where t0 == 0: the block that ends the unit; -1 otherwise
 };
 
+// What the merge has to know of a cut unit, left by the share that begins it at its own place (two int4 of `desc`).
+struct CutUnit {
+  int last_block, slot;        // the share that ends the unit, or -1 where this share begins none; place of the first partial result
+  int row0, m, g, j;           // the request's rows; KV head; the token, or -1: all of them
+  int first, count;            // rows of the unit
+};
+__device__ __forceinline__ void leave_none(int4* desc, int block) { desc[2 * block].x = -1; }
+__device__ __forceinline__ void leave_cut(int4* desc, int block, const Segment& sg, int row0, int m, int j, int first, int count) {
+  desc[2 * block] = make_int4(sg.last_block, sg.slot, row0, m);
+  desc[2 * block + 1] = make_int4(sg.g, j, first, count);
+}
+__device__ __forceinline__ CutUnit cut_unit(const int4* desc, int block) {
+  const int4 a = desc[2 * block], b = desc[2 * block + 1];
+  return CutUnit{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
 // The segments of a share, in order.
 template <typename Line>
 struct Walk {

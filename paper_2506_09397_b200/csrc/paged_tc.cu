@@ -60,7 +60,7 @@ static_assert(B_COUNT * 8 + 4 <= 256);
 struct TcParts {
   float* acc;      // [2 * blocks][rows of a unit][H], not normalised
   float* ml;       // [2 * blocks][rows of a unit][2]
-  int4* desc;      // [blocks] {last block or -1, first slot, request, unit of the request}
+  int4* desc;      // [blocks][2]: CutUnit
 };
 
 // what a row sees of the request's own nodes
@@ -95,7 +95,7 @@ struct RowView {
 // a unit, or the stretch of it that the block works on
 struct TcUnit {
   Segment sg;
-  int row0, m, n, n_rb;
+  int row0, m, n;
 };
 
 template <int H, int kGroups>
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
   pdl_wait();
   const AttentionLine line{c, r, 0, kUnit, kKeys};
   const Share share = block_share(line, blockIdx.x, gridDim.x);
-  if (threadIdx.x == 0) parts.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  if (threadIdx.x == 0) leave_none(parts.desc, blockIdx.x);
 
   // The registers of the block, 384 x 168, go where they are needed: 4 warps x 88, 8 warps x 200 (62,464 of 64,512).
   if (warp >= 8) {
@@ -297,7 +297,6 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       next.row0 = walk.w.v.row0;
       next.m = walk.w.v.m;
       next.n = walk.w.v.n;
-      next.n_rb = walk.w.n_rb;
       return true;
     };
     int done[2] = {0, 0};       // units that either group has finished
@@ -574,7 +573,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       fence_before();        // O has been read: the next unit's products may overwrite it
       if (joint) asm volatile("bar.sync 1, 256;" ::: "memory");     // by both
       if (u.sg.last_block >= 0 && threadIdx.x == 0)
-        parts.desc[blockIdx.x] = make_int4(u.sg.last_block, u.sg.slot, u.sg.req, u.sg.g * u.n_rb + u.sg.rb);
+        leave_cut(parts.desc, blockIdx.x, u.sg, u.row0, u.m, -1, u.sg.rb * kUnit, min(kUnit, u.m * (r.Hq / c.Hkv) - u.sg.rb * kUnit));
     }
   }
 
@@ -611,14 +610,14 @@ int launch_h(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) 
   parts.desc = reinterpret_cast<int4*>(parts.ml + static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * 2);
   SLED_LAUNCH_PDL((paged_tc_kernel<H, kGroups>), dim3(blocks), dim3(384), (Tc<H, kGroups>::kTotal), s, c, r, parts, map_q, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return -1;
-  const int n = launch_paged_merge(c, r, 0, kGroups * kGroupRows, kKeys, blocks, parts.acc, parts.ml, parts.desc, s);
+  const int n = launch_paged_merge(c, r, kGroups * kGroupRows, blocks, parts.acc, parts.ml, parts.desc, s);
   return n < 0 ? n : n + 1;
 }
 
 }  // namespace
 
 int64_t paged_tc_workspace(int h) {
-  return static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * (h + 2) * 4 + kMaxPagedBlocks * 16LL;
+  return static_cast<int64_t>(kMaxPagedBlocks) * 2 * kGroupRows * (h + 2) * 4 + kMaxPagedBlocks * 32LL;
 }
 
 // Q comes in by TMA, heads of whole tokens, and results go out a sector at a time
