@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
         }
       }
       const int here = min(32, n_parts - p0);
-#pragma unroll 4
+#pragma unroll 8
       for (int p = p0 > 0 ? 0 : kAtOnce; p < here; ++p) {
         const float fp = __shfl_sync(0xffffffffu, f, p);
         float x[D];

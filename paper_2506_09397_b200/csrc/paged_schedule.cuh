@@ -29,6 +29,7 @@ struct ReqWork {
 // Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM), in
 // sixteenths.  Beginning and ending a unit costs a number of tiles as well; it is spread over the unit's tiles.
 constexpr int kMinShare = 64;      // of a block
+constexpr int kMinMmaShare = 32;
 constexpr int kMinWarpShare = 24;   // of a warp that has a share of its own
 __device__ __forceinline__ int unit_weight(int tile, int unit, int tiles, int most = kMinShare - 1) { return min(tile + unit / tiles, most); }
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
@@ -42,7 +43,7 @@ struct AttentionLine {
   int list_len;
   int unit_rows = kUnitRows, tile = kTile;
   __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
-  __device__ __forceinline__ int min_share() const { return unit_rows < kUnitRows ? kMinWarpShare : kMinShare; }
+  __device__ __forceinline__ int min_share() const { return list_len == kWholeRows ? kMinShare : unit_rows == kUnitRows ? kMinMmaShare : unit_rows < kUnitRows ? kMinWarpShare : 1; }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
     w.v = req_view(c, r, i);
@@ -79,19 +80,26 @@ __device__ __forceinline__ long long divide(long long a, long long b) {
 }
 
 // Shares `first`, .. `first` + kShares - 1 of at most `most`, into out[] (shared memory).  All threads of the block call it
-// (blockDim.x a multiple of 32, at most 1024).  The block with share 0 reports the requests that are left out.
+// (blockDim.x a multiple of 32, at most 32 * kMostWarps).  The block with share 0 reports the requests that are left out.
+constexpr int kMostWarps = 12;
 template <int kShares, typename Line>
 __device__ __forceinline__ void block_shares(const Line& line, int first, int most, Share* out) {
-  __shared__ long long sums[33];
+  __shared__ long long sums[kMostWarps];   // (little, so that attention blocks still share an SM)
+  __shared__ int2 weights[kMostWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
   const int n_reqs = line.c.n_reqs, per = (n_reqs + blockDim.x - 1) / blockDim.x;
   const int i0 = min(static_cast<int>(threadIdx.x) * per, n_reqs), i1 = min(i0 + per, n_reqs);
   long long own = 0;
   ReqWork w;
+  int heaviest = 1, lightest = 1 << 30;        // tile
 #pragma unroll 1
   for (int i = i0; i < i1; ++i) {
     w = line(i);
     own += w.cost();
+    if (w.units > 0) {
+      heaviest = max(heaviest, w.weight);
+      lightest = min(lightest, w.weight);
+    }
     if (first == 0 && !w.v.ok) set_status(line.c.status, line.fault(w.v));
   }
   long long x = own;
@@ -100,16 +108,28 @@ __device__ __forceinline__ void block_shares(const Line& line, int first, int mo
     const long long y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  if (lane == 31) sums[warp] = x;
+  heaviest = __reduce_max_sync(0xffffffffu, heaviest);
+  lightest = __reduce_min_sync(0xffffffffu, lightest);
+  if (lane == 31) {
+    sums[warp] = x;
+    weights[warp] = make_int2(heaviest, lightest);
+  }
   if (threadIdx.x < kShares) out[threadIdx.x].from = out[threadIdx.x].to = out[threadIdx.x].at = 0;
   __syncthreads();
   long long before = 0, total = 0;
   for (int k = 0; k < nw; ++k) {
     if (k < warp) before += sums[k];
     total += sums[k];
+    heaviest = max(heaviest, weights[k].x);
+    lightest = min(lightest, weights[k].y);
   }
-  // a part of the line that is longer than any tile holds the beginning of one
-  const int count = static_cast<int>(max(1LL, min(static_cast<long long>(most), total / line.min_share())));
+  // A part of the line that is no shorter than any tile holds the beginning of one.  Whole tiles to a share: the longest
+  // share is no longer for it, there are fewer of them, and units are cut in the same places where they are alike.
+  const long long least = max(divide(total + most - 1, most), static_cast<long long>(max(line.min_share(), heaviest)));
+  const long long whole = divide(least + lightest - 1, lightest) * lightest;
+  long long many = divide(total + whole - 1, whole);
+  if (many * heaviest > total) --many;
+  const int count = static_cast<int>(max(1LL, many));
   const long long each = divide(total, count), rest = total - each * count;   // the first `rest` shares are one longer
   long long at = before + x - own;
   const long long end = at + own;
