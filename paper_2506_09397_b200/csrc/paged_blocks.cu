@@ -332,7 +332,7 @@ template <typename T, int H>
 int bounds_typed(const PagedCache& c, const int32_t* first, void* bounds, cudaStream_t s) {
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
-  SLED_LAUNCH_PDL((block_bounds_kernel<T, H>), dim3(8 * sms), dim3(256), 0, s, c, first, static_cast<T*>(bounds));
+  SLED_LAUNCH_PDL((block_bounds_kernel<T, H>), dim3(4 * sms), dim3(256), 0, s, c, first, static_cast<T*>(bounds));
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 template <typename T, int H>
