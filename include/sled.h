@@ -310,10 +310,12 @@ int sled_attention_ragged(sled_engine* e, int32_t layer, const uint64_t* ctx_ids
  * launched (SLED_ERR_ARG; SLED_ERR_NO_DEVICE without a GPU).  What only the GPU can see is checked by the kernels: a
  * request whose numbers do not hold together - n_kv beyond its table row, fewer keys than rows, rows outside the call, a
  * tree of more than SLED_MAX_TREE_NODES nodes - is left out; a page outside the pool is read as page 0 and never written
- * (eviction leaves its request out), and a parent that is not an earlier node makes its node unused.  Each of these, and a device-side wait that runs out, sets *status (DEVICE,
- * one int32, may be NULL) to the sled_status if it was 0; no call clears it.  Entries of a table row behind the request's
+ * (eviction leaves its request out), and a parent that is not an earlier node makes its node unused.  Each of these, and a
+ * device-side wait that runs out, sets *status (DEVICE, one int32, may be NULL) to the sled_status if it was 0; no call
+ * clears it.  Entries of a table row behind the request's
  * last page, slots behind its last key and pages of nobody are never looked at, or do not change results whatever they
- * hold.  A page belongs to at most one request of a call that writes to the cache or to key_weights.
+ * hold.  A page belongs to at most one request, once, of a call that writes to the cache or to key_weights; out, lse and
+ * key_weights share no memory with what the call reads.
  * workspace: at least the bytes that the call's _workspace function names, 256-byte aligned, used from the call until its
  * kernels have run: calls (or captured graphs) that may run at the same time need a workspace each.  It need not be
  * cleared and nothing in it outlives the call. */
@@ -327,7 +329,7 @@ typedef struct sled_paged_kv {
   int32_t page_size;          /* a multiple of 16, at most 256 */
   int32_t head_dim;           /* 32, 64 or 128 */
   const int32_t* page_table;  /* [n_reqs] rows of table_cols entries, table_stride entries apart */
-  int32_t table_stride, table_cols;
+  int32_t table_stride, table_cols;   /* table_cols * page_size at most 2^31 - 1025 */
   const int32_t* n_kv;        /* [n_reqs] cached keys */
   int32_t n_reqs;
 } sled_paged_kv;
@@ -338,7 +340,7 @@ typedef struct sled_paged_kv {
  * -2: the node is unused - its row is 0 (lse -infinity) and nobody sees it, nor those that hang on it.  parents NULL: every request is a
  * chain (row j sees the keys up to its own), of any length.  Softmax in fp32 over scale * q.k; scale 0: 1/sqrt(head_dim).
  *   q, out  [n_rows][n_q_heads][head_dim], rows q_stride / out_stride elements apart (even numbers of bf16 elements,
- *           4-byte aligned); rows that belong to no request are left alone
+ *           4-byte aligned), n_rows * n_q_heads below 2^31; rows that belong to no request are left alone
  *   lse     [n_rows][n_q_heads] fp32: natural logarithm of the sum of exponentials; may be NULL
  *   key_weights  may be NULL; [n_pages][n_kv_heads][page_size] fp32: every key's attention weight, summed over the
  *           request's rows and the heads that share the KV head, is added to its entry */

@@ -592,6 +592,8 @@ def _query_rows(what: str, q, out, k, n_reqs: int, cu_q):
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
         _refuse(what, "out must be like q")
+    elif out.data_ptr() == q.data_ptr() and q.numel():
+        _refuse(what, "out must not be q: queries are read until the call has run")
     return out, _row_stride(q, what, "q"), _row_stride(out, what, "out")
 
 

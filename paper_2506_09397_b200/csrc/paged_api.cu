@@ -2,6 +2,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
+#include <initializer_list>
 
 #include "../../include/sled.h"
 #include "kernels.h"
@@ -13,7 +14,23 @@ namespace {
 
 using namespace sled;
 
-int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
+// A workspace of more than kMostBytes bytes, or whose size does not fit 64 bits, is refused; -1 stands for it.
+constexpr int64_t kMostBytes = 1LL << 60;
+int64_t align256(int64_t v) { return v < 0 ? v : (v + 255) / 256 * 256; }
+int64_t product(std::initializer_list<int64_t> factors) {
+  int64_t n = 1;
+  for (const int64_t f : factors)
+    if (__builtin_mul_overflow(n, f, &n) || n > kMostBytes) return -1;
+  return n;
+}
+int64_t sum(std::initializer_list<int64_t> parts) {
+  int64_t n = 0;
+  for (const int64_t p : parts) {
+    if (p < 0) return -1;
+    n += p;
+  }
+  return n;
+}
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -28,15 +45,16 @@ int check_cache(const sled_paged_kv* kv, bool need_v, bool layers) {
   if (kv->n_reqs < 0 || kv->n_reqs > 65535 || kv->table_cols < 0 || kv->table_stride < kv->table_cols) return SLED_ERR_ARG;
   if (kv->n_layers > 65535) return SLED_ERR_ARG;
   if (!aligned(kv->k, 16) || (kv->v && !aligned(kv->v, 16)) || !aligned(kv->page_table, 4) || !aligned(kv->n_kv, 4)) return SLED_ERR_ARG;
-  // rows of one layer, and keys of one request, are counted in 32 bits
+  // rows of one layer, and keys of one request (rounded up to tiles), are counted in 32 bits
   if (static_cast<int64_t>(kv->n_pages) * kv->n_kv_heads * kv->page_size > INT32_MAX) return SLED_ERR_ARG;
-  if (static_cast<int64_t>(kv->table_cols) * kv->page_size > INT32_MAX) return SLED_ERR_ARG;
+  if (static_cast<int64_t>(kv->table_cols) * kv->page_size > INT32_MAX - 1024) return SLED_ERR_ARG;
   return SLED_OK;
 }
 
 int check_rows(const sled_paged_kv* kv, const void* q, int64_t q_stride, const int32_t* cu_q, int32_t n_rows, int32_t n_q_heads,
                float scale, const void* out, int64_t out_stride) {
   if (n_rows < 0 || n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % kv->n_kv_heads) return SLED_ERR_ARG;
+  if (static_cast<int64_t>(n_rows) * n_q_heads > INT32_MAX) return SLED_ERR_ARG;   // (row, head) pairs are counted in 32 bits
   if (!(scale >= 0.f) || scale > 3.0e38f || !cu_q || !aligned(cu_q, 4)) return SLED_ERR_ARG;
   if (n_rows > 0 && (!q || !out)) return SLED_ERR_ARG;
   const int64_t row = static_cast<int64_t>(n_q_heads) * kv->head_dim;
@@ -114,7 +132,7 @@ int done(int n, const char* what) {
 }
 
 int check_workspace(const void* workspace, int64_t have, int64_t need) {
-  return need > 0 && (!workspace || have < need || !aligned(workspace, 256)) ? SLED_ERR_ARG : SLED_OK;
+  return need < 0 || (need > 0 && (!workspace || have < need || !aligned(workspace, 256))) ? SLED_ERR_ARG : SLED_OK;
 }
 
 // the same arrays, or arrays that share no byte
@@ -123,9 +141,9 @@ bool same_or_apart(const void* a, const void* b, int64_t bytes) {
   return x == y || x + bytes <= y || y + bytes <= x;
 }
 
-int64_t lse_bytes(int32_t n_rows, int32_t n_q_heads) { return align256(static_cast<int64_t>(n_rows) * n_q_heads * 4); }
+int64_t lse_bytes(int32_t n_rows, int32_t n_q_heads) { return align256(product({n_rows, n_q_heads, 4})); }
 int64_t list_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_blocks) {
-  return align256(static_cast<int64_t>(n_rows) * kv->n_kv_heads * n_blocks * 4);
+  return align256(product({n_rows, kv->n_kv_heads, n_blocks, 4}));
 }
 
 int64_t attention_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, bool weigh) {
@@ -133,13 +151,13 @@ int64_t attention_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_hea
                                             static_cast<int64_t>(kv->table_cols) * kv->page_size, weigh));
 }
 int64_t tree_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, bool weigh) {
-  return attention_bytes(kv, n_rows, n_q_heads, weigh) + (weigh ? lse_bytes(n_rows, n_q_heads) : 0);
+  return sum({attention_bytes(kv, n_rows, n_q_heads, weigh), weigh ? lse_bytes(n_rows, n_q_heads) : 0});
 }
 int64_t blocks_bytes(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks) {
-  return attention_bytes(kv, n_rows, n_q_heads, false) + list_bytes(kv, n_rows, n_blocks) + list_bytes(kv, n_rows, kv->table_cols);
+  return sum({attention_bytes(kv, n_rows, n_q_heads, false), list_bytes(kv, n_rows, n_blocks), list_bytes(kv, n_rows, kv->table_cols)});
 }
 int64_t evict_bytes(const sled_paged_kv* kv) {
-  return align256(static_cast<int64_t>(kv->n_layers) * kv->n_reqs * kv->n_kv_heads * kv->table_cols * kv->page_size * 4);
+  return align256(product({kv->n_layers, kv->n_reqs, kv->n_kv_heads, kv->table_cols, kv->page_size, 4}));
 }
 
 }  // namespace
@@ -148,7 +166,9 @@ extern "C" {
 
 int sled_attention_tree_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t weigh, int64_t* bytes) {
   if (check_cache(kv, true, false) || n_rows < 0 || n_q_heads < 1 || !bytes) return SLED_ERR_ARG;
-  *bytes = tree_bytes(kv, n_rows, n_q_heads, weigh != 0);
+  const int64_t n = tree_bytes(kv, n_rows, n_q_heads, weigh != 0);
+  if (n < 0) return SLED_ERR_ARG;
+  *bytes = n;
   return SLED_OK;
 }
 
@@ -172,7 +192,9 @@ int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride
 
 int sled_evict_keys_workspace(const sled_paged_kv* kv, int64_t* bytes) {
   if (check_cache(kv, true, true) || !bytes) return SLED_ERR_ARG;
-  *bytes = evict_bytes(kv);
+  const int64_t n = evict_bytes(kv);
+  if (n < 0) return SLED_ERR_ARG;
+  *bytes = n;
   return SLED_OK;
 }
 
@@ -206,7 +228,9 @@ int sled_block_bounds(const sled_paged_kv* kv, const int32_t* first, void* bound
 
 int sled_attention_blocks_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int32_t n_blocks, int64_t* bytes) {
   if (check_cache(kv, true, false) || n_rows < 0 || n_q_heads < 1 || n_blocks < 1 || !bytes) return SLED_ERR_ARG;
-  *bytes = blocks_bytes(kv, n_rows, n_q_heads, n_blocks);
+  const int64_t n = blocks_bytes(kv, n_rows, n_q_heads, n_blocks);
+  if (n < 0) return SLED_ERR_ARG;
+  *bytes = n;
   return SLED_OK;
 }
 

@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(128) attn_row_kernel(PagedCache c, PagedRows r
   const int n_here = list ? min(list_len, own + 1) * c.ps : last + 1;
   const int32_t* mine = list ? list + (static_cast<int64_t>(t) * c.Hkv + g) * list_len : nullptr;
   for (int e = warp; e < n_here && !none; e += 4) {
-    const int x = list ? mine[e / c.ps] * c.ps + e % c.ps : e;
+    const int x = list ? checked_block(c, mine[e / c.ps]) * c.ps + e % c.ps : e;
     if (x > last) continue;
     if (r.parents && x >= prefix) {
       const int a = x - prefix;
@@ -189,7 +189,7 @@ int64_t parts_bytes(int dtype, int h) {
 // Scores are kept where they take no more than this; otherwise the weights are computed from the keys again.
 constexpr int64_t kMostScoreBytes = 512LL << 20;
 bool keeps_scores(int dtype, int h, int64_t rows_heads, int64_t keys) {
-  return (dtype == 0 || h >= 64) && rows_heads * keys * 4 <= kMostScoreBytes;
+  return (dtype == 0 || h >= 64) && (keys == 0 || rows_heads <= kMostScoreBytes / 4 / keys);
 }
 
 template <typename T, int H>

@@ -40,6 +40,13 @@ __device__ __forceinline__ int checked_page(const PagedCache& c, int page) {
   set_status(c.status, SLED_ERR_ARG);
   return 0;
 }
+// entry of a list of chosen blocks, a column of the page table; where rows of two requests overlap, one of them may find
+// entries that nobody wrote
+__device__ __forceinline__ int checked_block(const PagedCache& c, int block) {
+  if (static_cast<unsigned>(block) < static_cast<unsigned>(c.table_cols)) return block;
+  set_status(c.status, SLED_ERR_ARG);
+  return 0;
+}
 
 // What node j of a request sees among the request's own nodes, as a bit set of kMaxTreeNodes bits: itself and its
 // ancestors.  Nothing for an unused node (parent -2) or one that hangs on an unused node; a parent that is not an

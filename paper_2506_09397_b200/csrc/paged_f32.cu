@@ -94,7 +94,7 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
   };
   auto page_of = [&](int t) {
     const int b = block_of(t);
-    return table[mine ? mine[b] : b];
+    return table[mine ? checked_block(c, mine[b]) : b];
   };
   auto locate = [&](int t, int page) {
     const int e = min(t * 2 + (lane & 1), groups - 1);

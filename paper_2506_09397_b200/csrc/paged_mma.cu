@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
           row = 0;
           if (e < groups && e < sg.t1 * 4) {
             const int b = e / cpp;
-            const int page = checked_page(c, table[mine ? mine[b] : b]);
+            const int page = checked_page(c, table[mine ? checked_block(c, mine[b]) : b]);
             row = (page * c.Hkv + sg.g) * c.ps + (e - b * cpp) * 16;
           }
         }

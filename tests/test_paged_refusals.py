@@ -117,3 +117,19 @@ def test_the_binding_refuses_tensors_of_the_host():
     with pytest.raises(B.SledError) as e:
         B.block_bounds(k, i.view(1, 1), i, torch.zeros(4, 2, 2, 64))
     assert e.value.code == B.SLED_ERR_NO_DEVICE
+
+
+def test_sizes_beyond_any_memory_are_refused_and_do_not_wrap_around():
+    n = C.c_int64(-7)
+    many = _kv(n_pages=1, n_kv_heads=65535, n_reqs=65535, table_cols=(1 << 27) - 128, table_stride=1 << 27)
+    assert B.lib().sled_attention_blocks_workspace(C.byref(many), 2 ** 31 - 1, 65535, 2 ** 31 - 1, C.byref(n)) == B.SLED_ERR_ARG
+    assert B.lib().sled_evict_keys_workspace(C.byref(_kv(n_layers=65535, n_pages=1, n_kv_heads=65535, n_reqs=65535, table_cols=(1 << 27) - 128,
+                                                         table_stride=1 << 27)), C.byref(n)) == B.SLED_ERR_ARG
+    assert n.value == -7
+    assert B.lib().sled_evict_keys(C.byref(_kv(n_layers=65535, n_pages=1, n_kv_heads=65535, n_reqs=65535, table_cols=(1 << 27) - 128,
+                                               table_stride=1 << 27)), 256, 256, 32, 1, 1, 0, 256, 2 ** 63 - 1, 0) == B.SLED_ERR_ARG
+    # scores of this many (row, key) pairs are not kept: the workspace stays small
+    assert _bytes("sled_attention_tree", C.byref(many), 2 ** 31 - 1, 1, 1) < 1 << 36
+    # (row, head) pairs and the keys of a request are counted in 32 bits
+    assert _tree(_kv(n_kv_heads=1), rows=2 ** 30, heads=4, ws=256, ws_bytes=1 << 60) == B.SLED_ERR_ARG
+    assert _tree(_kv(table_cols=(1 << 27) - 1, table_stride=1 << 27), ws=256, ws_bytes=1 << 60) == B.SLED_ERR_ARG
