@@ -34,7 +34,7 @@ struct PagedRows {
   char* out;
   float* lse;                 // [T][Hq] natural logarithm, or null
   int64_t q_stride, out_stride;
-  int T, Hq;
+  int T, Hq, group;           // group: query heads per KV head
   float scale;
 };
 

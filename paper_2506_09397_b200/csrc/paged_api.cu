@@ -120,6 +120,7 @@ PagedRows rows_of(const sled_paged_kv* kv, const void* q, int64_t q_stride, cons
   r.out_stride = out_stride;
   r.T = n_rows;
   r.Hq = n_q_heads;
+  r.group = n_q_heads / kv->n_kv_heads;
   r.scale = scale > 0.f ? scale : 1.f / sqrtf(static_cast<float>(kv->head_dim));
   return r;
 }

@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(128) attn_row_kernel(PagedCache c, PagedRows r
   if (!v.ok) return;
   const int j = t - v.row0;
   if (j < 0 || j >= v.m) return;   // rows behind the last request
-  const int g = head / (r.Hq / c.Hkv), prefix = v.n - v.m;
+  const int g = head / (r.group), prefix = v.n - v.m;
   uint32_t bits[kMaxTreeNodes / 32] = {};
   if (r.parents) ancestors_of(r.parents + v.row0, j, bits, warp == 0 && lane == 0 ? c.status : nullptr);
   bool none = r.parents != nullptr;
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(128) attn_row_kernel(PagedCache c, PagedRows r
 template <typename T, int H>
 __global__ void __launch_bounds__(128) key_weight_kernel(PagedCache c, PagedRows r, float* key_weights) {
   constexpr int D = H / 32;
-  const int i = blockIdx.z, g = blockIdx.y, group = r.Hq / c.Hkv;
+  const int i = blockIdx.z, g = blockIdx.y, group = r.group;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const ReqView v = req_view(c, r, i);
   const int x0 = blockIdx.x * c.ps;
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
   const AttentionLine line{c, r, kWholeRows};
   const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (share.from >= share.to) return;
-  const int quad = threadIdx.x & 63, part = threadIdx.x >> 6, group = r.Hq / c.Hkv;
+  const int quad = threadIdx.x & 63, part = threadIdx.x >> 6, group = r.group;
   for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
     const int rows = w.v.m * group, end = min(sg.t1 * kTile, w.v.n);
     for (int x0 = sg.t0 * kTile; x0 < end; x0 += 256) {
@@ -197,7 +197,7 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
   int n = 1;
   if constexpr (sizeof(T) == 2 && H >= 64) {
     // many rows per request: the tcgen05 kernels
-    if (!list && paged_tc_serves(c, r) && static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kTcRows) * c.n_reqs) {
+    if (!list && paged_tc_serves(c, r) && static_cast<int64_t>(r.T) * (r.group) > static_cast<int64_t>(kTcRows) * c.n_reqs) {
       n = launch_paged_tc(c, r, ws, s);
       if (n < 0 || !key_weights) return n;
       const int w = launch_paged_weigh(c, r, key_weights, s);

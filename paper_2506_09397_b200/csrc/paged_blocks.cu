@@ -123,7 +123,7 @@ struct ScoreLine {
   int n_blocks, n_local;
   __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
   __device__ __forceinline__ int min_share() const { return 1; }
-  __device__ __forceinline__ int tokens() const { return max(1, kScoreRows / (r.Hq / c.Hkv)); }   // of a unit
+  __device__ __forceinline__ int tokens() const { return max(1, kScoreRows / (r.group)); }   // of a unit
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
     w.v = req_view(c, r, i);
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(128, 3) block_score_kernel(PagedCache c, Paged
   const ScoreLine line{c, r, n_blocks, n_local};
   const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (share.from >= share.to) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3, group = r.Hq / c.Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3, group = r.group;
   const bool wide_q = (reinterpret_cast<uintptr_t>(r.q) & 15) == 0 && r.q_stride % 8 == 0;
   for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
     const int j0 = sg.rb * line.tokens(), nj = min(line.tokens(), w.v.m - j0), rows = nj * group;
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(256) block_score_row_kernel(PagedCache c, Page
   constexpr int D = H / 32;
   pdl_launch_dependents();
   pdl_wait();
-  const int t = blockIdx.x, g = blockIdx.y, group = r.Hq / c.Hkv;
+  const int t = blockIdx.x, g = blockIdx.y, group = r.group;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int i = req_of_row(r.cu_q, c.n_reqs, t);
   const ReqView v = req_view(c, r, i);
@@ -342,7 +342,7 @@ int choice_typed(const PagedCache& c, const PagedRows& r, const void* bounds, in
   // few choices among many blocks: a large block each; many choices share an SM
   const int threads = c.table_cols > 512 && static_cast<int64_t>(r.T) * c.Hkv <= 2 * sms ? 1024 : 256;
   if constexpr (sizeof(T) == 2 && H >= 64) {
-    if (r.Hq / c.Hkv <= kScoreRows) {
+    if (r.group <= kScoreRows) {
       SLED_LAUNCH_PDL(block_score_kernel<H>, dim3(3 * sms), dim3(128), 0, s, c, r, static_cast<const T*>(bounds), n_blocks, n_local, scores);
       SLED_LAUNCH_PDL(block_choice_kernel, dim3(r.T, c.Hkv), dim3(threads), 0, s, c, r, n_blocks, n_local, static_cast<const float*>(scores), list);
       return cudaGetLastError() == cudaSuccess ? 2 : -1;

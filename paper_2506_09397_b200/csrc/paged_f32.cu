@@ -57,7 +57,7 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
                                         const Segment& sg, const F32Parts& parts, float* mem) {
   using L = F32<H>;
   constexpr int R = kRows, PER = H / 32;         // dimensions of a lane
-  const int lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
+  const int lane = threadIdx.x & 31, group = r.group;
   float* buffers = mem;
   float* q = mem + kBuffers * L::kBuffer;
   float* p = q + L::kQ;
@@ -67,7 +67,7 @@ __device__ __forceinline__ void work_on(const PagedCache& c, const PagedRows& r,
   int rows, prefix, end;
   if (list_len > 0) {
     rows = min(kRows, group - first);
-    const int x = w.v.n - w.v.m + sg.j, own = x / c.ps;
+    const int x = w.v.n - w.v.m + sg.j, own = quotient(x, c.ps);
     end = (min(list_len, own + 1) - 1) * c.ps + x - own * c.ps + 1;
     prefix = end;
   } else {
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(32 * kWarps) paged_f32_kernel(const PagedCache
   for_segments(line, shares[warp], mine, [&](const ReqWork& w, const Segment& sg) {
     work_on<H>(c, r, list, list_len, w, sg, parts, mem);
     if (sg.last_block >= 0 && (threadIdx.x & 31) == 0) {
-      const int first = sg.rb * kRows, group = r.Hq / c.Hkv;
+      const int first = sg.rb * kRows, group = r.group;
       leave_cut(parts.desc, mine, sg, w.v.row0, w.v.m, list_len > 0 ? sg.j : -1, first, min(kRows, (list_len > 0 ? group : w.v.m * group) - first));
     }
   });

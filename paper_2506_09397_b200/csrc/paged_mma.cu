@@ -30,7 +30,8 @@ struct Smem {
   static constexpr int kGroup = 16 * H * 2;
   static constexpr int kHalf = 4 * kGroup;              // K or V of a tile
   static constexpr int kStage = 2 * kHalf;
-  static constexpr int kMerge = 3 * (H / 8 * 4 / 2 + 4) * 32 * 4;   // three shares, half of their output at a time
+  static constexpr int kMergePitch = 40;                // 32 dimensions of a row; eight rows meet eight times four banks
+  static constexpr int kMerge = 64 * (kMergePitch + 2) * 4;
   static constexpr int kOffMerge = kStages * kStage;
   static constexpr int kOffTree = kOffMerge + kMerge;
   static constexpr int kOffBar = kOffTree + kMaxTreeNodes * (kMaxTreeNodes / 32) * 4;
@@ -54,8 +55,8 @@ struct UnitRows {
   int group, g, j;        // j < 0: all tokens of the request, else that token
   int first, count;       // rows of the unit's block: first .. first + count - 1
   int prefix, end;        // positions below `prefix` are seen by everybody; there are `end` of them
-  __device__ __forceinline__ int token(int r) const { return j >= 0 ? j : (first + r) / group; }
-  __device__ __forceinline__ int head(int r) const { return g * group + (first + r) % group; }
+  __device__ __forceinline__ int token(int r) const { return j >= 0 ? j : quotient(first + r, group); }
+  __device__ __forceinline__ int head(int r) const { return g * group + first + r - quotient(first + r, group) * group; }
 };
 
 struct Parts {
@@ -262,71 +263,74 @@ __device__ __forceinline__ void consume(const PagedCache& c, const PagedRows& r,
     }
   }
 
-  if (MT < 4) {
-    // the warps that shared rows: those with a later share of the keys hand theirs over, half of the output at a time
-    constexpr int kVals = DN * 2 + 4, kShares = 4 / MT;
-    float f[kShares];
-    float f_hi[kShares];
+  if constexpr (MT < 4) {
+    // The warps that shared rows lay their outputs side by side, 32 dimensions at a time, and all threads add them up: four
+    // dimensions of a row (or two rows) each.
+    constexpr int kShares = 4 / MT, kRowsHere = 16 * MT, kPitch = S::kMergePitch;
+    float2* ml = reinterpret_cast<float2*>(merge + 64 * kPitch);
+    const int mine = share * kRowsHere + r_lo, row0 = threadIdx.x >> 3, col = (threadIdx.x & 7) * 4;
+    int tok[MT], hd[MT];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      asm volatile("bar.sync 2, 128;" ::: "memory");
-      if (share > 0) {
-        float* dst = merge + ((share - 1) * MT + mt) * kVals * 32 + lane;
-#pragma unroll
-        for (int i = 0; i < DN / 2; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dst[(i * 4 + e) * 32] = o[half * (DN / 2) + i][e];
-        if (half == 0) {
-          dst[(DN * 2 + 0) * 32] = m_lo;
-          dst[(DN * 2 + 1) * 32] = m_hi;
-          dst[(DN * 2 + 2) * 32] = l_lo;
-          dst[(DN * 2 + 3) * 32] = l_hi;
-        }
+    for (int k = 0; k < MT; ++k) {
+      tok[k] = u.token(row0 + 16 * k);
+      hd[k] = u.head(row0 + 16 * k);
+    }
+#pragma unroll 1
+    for (int part = 0; part < H / 32; ++part) {
+      asm volatile("bar.sync 2, 128;" ::: "memory");      // everybody has read what was there
+      if (part == 0 && tq == 0) {
+        ml[mine] = make_float2(m_lo, l_lo);
+        ml[mine + 8] = make_float2(m_hi, l_hi);
       }
-      asm volatile("bar.sync 2, 128;" ::: "memory");
-      if (share == 0) {
-        if (half == 0) {
-          float n_lo = m_lo, n_hi = m_hi;
-          float om_lo[kShares], om_hi[kShares];
 #pragma unroll
-          for (int sh = 1; sh < kShares; ++sh) {
-            const float* src = merge + ((sh - 1) * MT + mt) * kVals * 32 + lane;
-            om_lo[sh] = src[(DN * 2 + 0) * 32];
-            om_hi[sh] = src[(DN * 2 + 1) * 32];
-            n_lo = fmaxf(n_lo, om_lo[sh]);
-            n_hi = fmaxf(n_hi, om_hi[sh]);
-          }
-          const float s_lo = n_lo == -INFINITY ? 0.f : n_lo, s_hi = n_hi == -INFINITY ? 0.f : n_hi;
-          f[0] = exp2_approx(m_lo - s_lo);
-          f_hi[0] = exp2_approx(m_hi - s_hi);
-          l_lo *= f[0];
-          l_hi *= f_hi[0];
+      for (int z = 0; z < H / 32; ++z)
+        if (z == part) {
 #pragma unroll
-          for (int sh = 1; sh < kShares; ++sh) {
-            const float* src = merge + ((sh - 1) * MT + mt) * kVals * 32 + lane;
-            f[sh] = exp2_approx(om_lo[sh] - s_lo);
-            f_hi[sh] = exp2_approx(om_hi[sh] - s_hi);
-            l_lo = fmaf(f[sh], src[(DN * 2 + 2) * 32], l_lo);
-            l_hi = fmaf(f_hi[sh], src[(DN * 2 + 3) * 32], l_hi);
+          for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<float2*>(merge + mine * kPitch + i * 8 + 2 * tq) = make_float2(o[z * 4 + i][0], o[z * 4 + i][1]);
+            *reinterpret_cast<float2*>(merge + (mine + 8) * kPitch + i * 8 + 2 * tq) = make_float2(o[z * 4 + i][2], o[z * 4 + i][3]);
           }
-          m_lo = n_lo;
-          m_hi = n_hi;
         }
+      asm volatile("bar.sync 2, 128;" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < DN / 2; ++i) {
-          float* x = o[half * (DN / 2) + i];
-          x[0] *= f[0]; x[1] *= f[0]; x[2] *= f_hi[0]; x[3] *= f_hi[0];
+      for (int k = 0; k < MT; ++k) {
+        const int row = row0 + 16 * k;
+        float2 x[kShares];
+        float top = -INFINITY, den = 0.f;
 #pragma unroll
-          for (int sh = 1; sh < kShares; ++sh) {
-            const float* src = merge + ((sh - 1) * MT + mt) * kVals * 32 + lane;
-            x[0] = fmaf(f[sh], src[(i * 4 + 0) * 32], x[0]);
-            x[1] = fmaf(f[sh], src[(i * 4 + 1) * 32], x[1]);
-            x[2] = fmaf(f_hi[sh], src[(i * 4 + 2) * 32], x[2]);
-            x[3] = fmaf(f_hi[sh], src[(i * 4 + 3) * 32], x[3]);
-          }
+        for (int sh = 0; sh < kShares; ++sh) {
+          x[sh] = ml[sh * kRowsHere + row];
+          top = fmaxf(top, x[sh].x);
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int sh = 0; sh < kShares; ++sh) {
+          const float f = exp2_approx(x[sh].x - ref);
+          const float4 y = *reinterpret_cast<const float4*>(merge + (sh * kRowsHere + row) * kPitch + col);
+          den = fmaf(f, x[sh].y, den);
+          sum.x = fmaf(f, y.x, sum.x);
+          sum.y = fmaf(f, y.y, sum.y);
+          sum.z = fmaf(f, y.z, sum.z);
+          sum.w = fmaf(f, y.w, sum.w);
+        }
+        if (row >= u.count || failed || *stop) continue;
+        const int d = part * 32 + col;
+        if (sg.whole) {
+          const float inv = den == 0.f ? 0.f : 1.f / den;    // a row that saw nothing has a sum of 0: its output is 0
+          const int64_t t = u.row0 + tok[k];
+          uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t * r.out_stride + static_cast<int64_t>(hd[k]) * H + d);
+          out[0] = pack_bf16(sum.x * inv, sum.y * inv);
+          out[1] = pack_bf16(sum.z * inv, sum.w * inv);
+          if (r.lse && d == 0) r.lse[t * r.Hq + hd[k]] = den == 0.f ? -INFINITY : (top + log2f(den)) * kLn2;
+        } else {
+          const int64_t at_row = static_cast<int64_t>(sg.slot) * kUnitRows + row;
+          *reinterpret_cast<float4*>(parts.acc + at_row * H + d) = sum;
+          if (d == 0) *reinterpret_cast<float2*>(parts.ml + at_row * 2) = make_float2(top, den);
         }
       }
     }
+    return;
   }
 
   if (!active || share != 0 || failed || *stop) return;
@@ -365,13 +369,13 @@ __device__ __forceinline__ UnitRows unit_rows(const PagedCache& c, const PagedRo
   u.req = sg.req;
   u.row0 = w.v.row0;
   u.m = w.v.m;
-  u.group = r.Hq / c.Hkv;
+  u.group = r.group;
   u.g = sg.g;
   u.first = sg.rb * rows;
   if (list_len > 0) {
     u.j = sg.j;
     u.count = min(rows, u.group - u.first);
-    const int x = w.v.n - w.v.m + sg.j, own = x / c.ps;   // the last chosen block is the token's own
+    const int x = w.v.n - w.v.m + sg.j, own = quotient(x, c.ps);   // the last chosen block is the token's own
     u.end = (min(list_len, own + 1) - 1) * c.ps + x - own * c.ps + 1;
     u.prefix = u.end;
   } else {
@@ -502,7 +506,7 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
   if (u.last_block < 0) return;
   constexpr int D = H / 32, kAtOnce = 8;
   using Words = typename std::conditional<D == 4, float4, typename std::conditional<D == 2, float2, float>::type>::type;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.group;
   const int n_parts = u.last_block - static_cast<int>(blockIdx.x) + 1, n_warps = blockDim.x >> 5;
   auto slot = [&](int p) { return static_cast<int64_t>(p == 0 ? u.slot : 2 * (blockIdx.x + p)) * unit; };
   int row = blockIdx.y * n_warps + warp;

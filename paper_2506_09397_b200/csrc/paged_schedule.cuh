@@ -12,6 +12,19 @@
 
 namespace sled {
 
+// Quotients of what is not negative.  The code around them runs once or twice per kernel, so that fetching instructions is
+// most of its time: small numbers take a handful.  (a + 1/2) / b lies at least 1 / (2 b) from a whole number, and
+// __fdividef is off by 2^-21.5 of its result at most, which is less while a < 2^20.
+__device__ __forceinline__ int quotient(int a, int b) {
+  if (__builtin_expect(a < (1 << 20), 1)) return static_cast<int>(__fdividef(static_cast<float>(a) + 0.5f, static_cast<float>(b)));
+  return static_cast<int>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
+}
+__device__ __forceinline__ long long divide(long long a, long long b) {
+  if (__builtin_expect((a | b) < (1 << 20), 1))
+    return static_cast<int>(__fdividef(static_cast<float>(static_cast<int>(a)) + 0.5f, static_cast<float>(static_cast<int>(b))));
+  return a / b;
+}
+
 constexpr int kTile = 64;        // keys per tile
 constexpr int kUnitRows = 64;    // query rows of a unit at most (tensor cores)
 
@@ -31,7 +44,7 @@ struct ReqWork {
 constexpr int kMinShare = 64;      // of a block
 constexpr int kMinMmaShare = 32;
 constexpr int kMinWarpShare = 24;   // of a warp that has a share of its own
-__device__ __forceinline__ int unit_weight(int tile, int unit, int tiles, int most = kMinShare - 1) { return min(tile + unit / tiles, most); }
+__device__ __forceinline__ int unit_weight(int tile, int unit, int tiles, int most = kMinShare - 1) { return min(tile + quotient(unit, tiles), most); }
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
 
 // The work of attention.  list_len > 0: units attend to chosen blocks, at most list_len per token.  kWholeRows: a unit has
@@ -47,13 +60,13 @@ struct AttentionLine {
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
     w.v = req_view(c, r, i);
-    const int group = r.Hq / c.Hkv;
+    const int group = r.group;
     w.tiles = w.units = w.n_rb = 0;
     w.weight = 1;
     if (!w.v.ok || w.v.m == 0) return w;
     const int rows = list_len > 0 ? group : w.v.m * group;
     int keys = w.v.n;
-    if (list_len > 0) keys = min(list_len, (w.v.n - 1) / c.ps + 1) * c.ps;
+    if (list_len > 0) keys = min(list_len, quotient(w.v.n - 1, c.ps) + 1) * c.ps;
     w.tiles = (keys + tile - 1) / tile;
     w.n_rb = list_len == kWholeRows ? 1 : (rows + unit_rows - 1) / unit_rows;
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
@@ -69,15 +82,11 @@ struct Share {
   int req;               // first request
   long long at;          // where it begins on the line
   long long from, to;    // this share's part of the line
-  long long total;
-  int count;             // shares that the line is cut into: every one of them gets a tile
+  long long each;        // its length, but that the first `rest` shares are one longer
+  int rest;
   ReqWork w;             // of the first request
 };
 
-// quotient of numbers that mostly fit 32 bits
-__device__ __forceinline__ long long divide(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
-}
 
 // Shares `first`, .. `first` + kShares - 1 of at most `most`, into out[] (shared memory).  All threads of the block call it
 // (blockDim.x a multiple of 32, at most 32 * kMostWarps).  The block with share 0 reports the requests that are left out.
@@ -130,7 +139,7 @@ __device__ __forceinline__ void block_shares(const Line& line, int first, int mo
   long long many = divide(total + whole - 1, whole);
   if (many * heaviest > total) --many;
   const int count = static_cast<int>(max(1LL, many));
-  const long long each = divide(total, count), rest = total - each * count;   // the first `rest` shares are one longer
+  const long long each = divide(total, count), rest = total - each * count;
   long long at = before + x - own;
   const long long end = at + own;
 #pragma unroll 1
@@ -148,7 +157,7 @@ __device__ __forceinline__ void block_shares(const Line& line, int first, int mo
           begin += w.cost();
         }
       }
-      out[k] = Share{i, begin, from, to, total, count, w};
+      out[k] = Share{i, begin, from, to, each, static_cast<int>(rest), w};
     }
   }
   __syncthreads();
@@ -162,8 +171,9 @@ __device__ __forceinline__ Share block_share(const Line& line, int block, int mo
 
 // the share that owns the tile which begins at `at`
 __device__ __forceinline__ int owner_of(long long at, const Share& s) {
-  const long long each = divide(s.total, s.count), rest = s.total - each * s.count, longer = (each + 1) * rest;
-  return static_cast<int>(at < longer ? divide(at, each + 1) : rest + divide(at - longer, each));
+  const long long longer = (s.each + 1) * s.rest;
+  const bool early = at < longer;
+  return static_cast<int>(divide(early ? at : at - longer, early ? s.each + 1 : s.each)) + (early ? 0 : s.rest);
 }
 
 // A stretch of one unit that a block works on.
@@ -217,9 +227,10 @@ struct Walk {
     g.req = i;
     g.t0 = static_cast<int>(lt - static_cast<long long>(u) * w.tiles);
     g.t1 = static_cast<int>(min(static_cast<long long>(w.tiles), g.t0 + (lt_end - lt)));
-    g.rb = u % w.n_rb;
-    g.g = u / w.n_rb % line.c.Hkv;
-    g.j = u / w.n_rb / line.c.Hkv;
+    const int of_rb = w.n_rb == 1 ? u : quotient(u, w.n_rb);
+    g.rb = u - of_rb * w.n_rb;
+    g.j = quotient(of_rb, line.c.Hkv);
+    g.g = of_rb - g.j * line.c.Hkv;
     g.whole = g.t0 == 0 && g.t1 == w.tiles;
     g.slot = 2 * block + (first ? 0 : 1);
     g.last_block = -1;

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
   float2* tops = reinterpret_cast<float2*>(ptr + L::kOffTop);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ptr + L::kOffBar + 8 * B_COUNT);
   auto bar = [&](int i) { return base + L::kOffBar + 8u * static_cast<uint32_t>(i); };
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.group;
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *stop = odd[0] = odd[1] = 0;
@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       fence_before();        // O has been read: the next unit's products may overwrite it
       if (joint) asm volatile("bar.sync 1, 256;" ::: "memory");     // by both
       if (u.sg.last_block >= 0 && threadIdx.x == 0)
-        leave_cut(parts.desc, blockIdx.x, u.sg, u.row0, u.m, -1, u.sg.rb * kUnit, min(kUnit, u.m * (r.Hq / c.Hkv) - u.sg.rb * kUnit));
+        leave_cut(parts.desc, blockIdx.x, u.sg, u.row0, u.m, -1, u.sg.rb * kUnit, min(kUnit, u.m * (r.group) - u.sg.rb * kUnit));
     }
   }
 
@@ -600,7 +600,7 @@ int launch_h(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) 
     configured[dev] = true;
   }
   CUtensorMap map_q, map_k, map_v;
-  if (tma_map_bf16_heads(&map_q, r.q, r.T, r.Hq, H, r.q_stride, r.Hq / c.Hkv, kGroupRows / (r.Hq / c.Hkv))) return -1;
+  if (tma_map_bf16_heads(&map_q, r.q, r.T, r.Hq, H, r.q_stride, r.group, kGroupRows / (r.group))) return -1;
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps;
   if (tma_map_bf16_row_octets(&map_k, c.k, rows, H) || tma_map_bf16_row_octets(&map_v, c.v, rows, H)) return -1;
   const int blocks = min(sms, kMaxPagedBlocks / 2);
@@ -622,14 +622,14 @@ int64_t paged_tc_workspace(int h) {
 
 // Q comes in by TMA, heads of whole tokens, and results go out a sector at a time
 bool paged_tc_serves(const PagedCache& c, const PagedRows& r) {
-  const int group = r.Hq / c.Hkv;
+  const int group = r.group;
   return c.dtype == BF16 && (c.h == 64 || c.h == 128) && kGroupRows % group == 0 && r.q_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(r.q) & 15) == 0 &&
          r.out_stride % 16 == 0 && (reinterpret_cast<uintptr_t>(r.out) & 31) == 0;
 }
 
 int launch_paged_tc(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) {
   // units of 256 rows where the requests have more than 128 on average
-  const bool wide = static_cast<int64_t>(r.T) * (r.Hq / c.Hkv) > static_cast<int64_t>(kGroupRows) * c.n_reqs;
+  const bool wide = static_cast<int64_t>(r.T) * (r.group) > static_cast<int64_t>(kGroupRows) * c.n_reqs;
   if (c.h == 128) return wide ? launch_h<128, 2>(c, r, ws, s) : launch_h<128, 1>(c, r, ws, s);
   return wide ? launch_h<64, 2>(c, r, ws, s) : launch_h<64, 1>(c, r, ws, s);
 }

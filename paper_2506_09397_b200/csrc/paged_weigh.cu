@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(320, 1) paged_weigh_kernel(const PagedCache c,
   volatile int* stop = &stop_word;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ptr + L::kOffBar + 8 * B_COUNT);
   auto bar = [&](int i) { return base + L::kOffBar + 8u * static_cast<uint32_t>(i); };
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.Hq / c.Hkv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.group;
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *stop = 0;
@@ -304,7 +304,7 @@ int launch_h(const PagedCache& c, const PagedRows& r, float* key_weights, cudaSt
     configured[dev] = true;
   }
   CUtensorMap map_q, map_k;
-  const int group = r.Hq / c.Hkv;
+  const int group = r.group;
   if (tma_map_bf16_heads(&map_q, r.q, r.T, r.Hq, H, r.q_stride, group, 128 / group)) return -1;
   if (tma_map_bf16_row_octets(&map_k, c.k, static_cast<long long>(c.n_pages) * c.Hkv * c.ps, H)) return -1;
   SLED_LAUNCH_PDL(paged_weigh_kernel<H>, dim3(sms), dim3(320), Wg<H>::kTotal, s, c, r, key_weights, map_q, map_k);
