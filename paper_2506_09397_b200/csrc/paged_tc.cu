@@ -345,7 +345,10 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       float m = -INFINITY, l = 0.f;
       bool ok = true;
       const int step = both ? 1 : 2, t_first = both ? 0 : s;
-      if (t_first >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY));
+      if (t_first >= n_tiles) {   // nothing to do for this group; but it must not give back the Q of a unit that has not begun
+        ok = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_QFULL), (units & 1) ^ 1, stop));
+        if (lane == 0) mbar_arrive(bar(B_QEMPTY));
+      }
       for (int t = 0; t < n_tiles; ++t) {
         const int my_vst = vst, my_vphase = vphase;
         if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }

@@ -26,6 +26,16 @@ def test_many_rows_over_other_pages(page, h):
     _check_attention([page * 5 + 3, page, 1111], q_len, 8, 2, h, BF, parents=[_tree(rng, m, True) for m in q_len], page=page, weigh=True)
 
 
+@pytest.mark.parametrize("h", [64, 128])
+@pytest.mark.parametrize("lo,hi", [(26, 128), (100, 300)])
+def test_many_short_contexts_of_many_rows(lo, hi, h):
+    """Blocks that go through many units of one or two tiles each."""
+    rng = random.Random(lo + h)
+    lens = [rng.randint(lo, hi) for _ in range(90)]
+    q_len = [rng.randint(20, min(n, 32)) for n in lens]
+    _check_attention(lens, q_len, 32, 8, h, BF, parents=[_tree(rng, m, True) for m in q_len], weigh=True)
+
+
 def test_long_chains():
     _check_attention([700, 1025, 300], [300, 1, 300], 8, 2, 128, BF, weigh=True)
 
