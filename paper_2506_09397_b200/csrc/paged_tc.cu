@@ -631,8 +631,14 @@ bool paged_tc_serves(const PagedCache& c, const PagedRows& r) {
 }
 
 int launch_paged_tc(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) {
-  // units of 256 rows where the requests have more than 128 on average
-  const bool wide = static_cast<int64_t>(r.T) * (r.group) > static_cast<int64_t>(kGroupRows) * c.n_reqs;
+  // Units of 256 rows where the requests have more than 128 on average and, as far as the page table allows, there are 32
+  // such tiles to an SM: the keys are read once for all rows, but a unit is longer.  64 nodes of 4 heads, 8 KV heads of 128,
+  // wide and narrow: 4 contexts of 32768 keys (55 tiles to an SM) 178 and 212 us, 64 of 2048 (55) 227 and 248, 8 of 8192
+  // (28) 117 and 115, one of 1000 (0.4) 28 and 22.
+  int sms = 0;
+  if (paged_device(&sms) < 0) return -1;
+  const int64_t rows = static_cast<int64_t>(r.T) * r.group / c.n_reqs, keys = static_cast<int64_t>(c.table_cols) * c.ps;
+  const bool wide = rows > kGroupRows && (rows + kGroupRows - 1) / (2 * kGroupRows) * c.n_reqs * c.Hkv * ((keys + kKeys - 1) / kKeys) >= 32LL * sms;
   if (c.h == 128) return wide ? launch_h<128, 2>(c, r, ws, s) : launch_h<128, 1>(c, r, ws, s);
   return wide ? launch_h<64, 2>(c, r, ws, s) : launch_h<64, 1>(c, r, ws, s);
 }
