@@ -3,10 +3,10 @@
 // The work of a call is a line of key tiles.  Request by request, a request's units - (KV head, block of up to kUnitRows
 // query rows), or with chosen blocks (token, KV head, block of rows) - follow each other, and a unit is `tiles` tiles of
 // kTile keys.  A tile weighs what it costs (a number that depends on how many rows meet it); block c of G takes the tiles
-// that begin in [c C / G, (c + 1) C / G) of the total weight C; G is no larger than leaves every block a tile.  All blocks are resident and end together, whatever the
-// lengths are, a long context spreads over as many of them as it takes, and nothing has to be known on the host.  A unit
-// that is cut leaves one partial result per block; only a block's first and last unit can be cut, so two places per
-// block hold them.
+// that begin in [c C / G, (c + 1) C / G) of the total weight C; G is no larger than leaves every block a
+// tile.  All blocks are resident and end together, whatever the lengths are, a long context spreads over as many of them as
+// it takes, and nothing has to be known on the host.  A unit that is cut leaves one partial result per block; only a
+// block's first and last unit can be cut, so two places per block hold them.
 #pragma once
 #include "paged_device.cuh"
 
@@ -14,7 +14,8 @@ namespace sled {
 
 // Quotients of what is not negative.  The code around them runs once or twice per kernel, so that fetching instructions is
 // most of its time: small numbers take a handful.  (a + 1/2) / b lies at least 1 / (2 b) from a whole number, and
-// __fdividef is off by 2^-21.5 of its result at most, which is less while a < 2^20.
+// __fdividef is off by 2 units in the last place, 2^-22 of its result, which is less while a < 2^20 (a divisor that a float
+// does not hold is larger than a).
 __device__ __forceinline__ int quotient(int a, int b) {
   if (__builtin_expect(a < (1 << 20), 1)) return static_cast<int>(__fdividef(static_cast<float>(a) + 0.5f, static_cast<float>(b)));
   return static_cast<int>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
@@ -41,9 +42,12 @@ struct ReqWork {
 
 // Time of a 64-key tile with up to 16, 32, 64 rows: 1.0 / 1.15 / 1.93 (measured per tile with two blocks on an SM), in
 // sixteenths.  Beginning and ending a unit costs a number of tiles as well; it is spread over the unit's tiles.
-constexpr int kMinShare = 64;      // of a block
+// A share is no smaller than this and no smaller than a tile.  Two tiles of few rows for the warp-level tensor cores (one
+// context of 1000 keys: 12 us, with four tiles 15), one of tcgen05 (700 keys: 13 us, with two 16.5), a warp of the fp32
+// kernel a tile of a long unit or two (24 trees: 29.2 us, without a minimum 30.5).
+constexpr int kMinShare = 64;       // where a unit has whole requests
 constexpr int kMinMmaShare = 32;
-constexpr int kMinWarpShare = 24;   // of a warp that has a share of its own
+constexpr int kMinWarpShare = 24;
 __device__ __forceinline__ int unit_weight(int tile, int unit, int tiles, int most = kMinShare - 1) { return min(tile + quotient(unit, tiles), most); }
 __device__ __forceinline__ int tile_weight(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 18 : 31; }
 
@@ -56,7 +60,9 @@ struct AttentionLine {
   int list_len;
   int unit_rows = kUnitRows, tile = kTile;
   __device__ __forceinline__ int32_t fault(const ReqView& v) const { return req_fault(r, v); }
-  __device__ __forceinline__ int min_share() const { return list_len == kWholeRows ? kMinShare : unit_rows == kUnitRows ? kMinMmaShare : unit_rows < kUnitRows ? kMinWarpShare : 1; }
+  __device__ __forceinline__ int min_share() const {
+    return list_len == kWholeRows ? kMinShare : unit_rows == kUnitRows ? kMinMmaShare : unit_rows < kUnitRows ? kMinWarpShare : 1;
+  }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w;
     w.v = req_view(c, r, i);

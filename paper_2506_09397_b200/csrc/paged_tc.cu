@@ -15,8 +15,10 @@
 //   warps 0-3, 4-7 : softmax and output of the two groups
 //   warps 8, 10    : TMA of K and of V (one block per SM)
 //   warp 9         : tensor-memory allocation, products (one thread); warp 11 only completes the warpgroup
-// The work is shared out as paged_schedule.cuh says.  What binds: the bytes of K and V up to 128 rows, the exponentials
-// (16 a clock and SM) above.  Every wait is bounded; when one runs out the block says so in *status, lets what is under
+// The work is shared out as paged_schedule.cuh says.  What binds: a unit's begin and end (about 20,000 cycles) where units
+// have few tiles; in long ones the bytes of K and V up to about 64 rows, then the products, which one thread issues in
+// order (a 128 x 128 x 16 step takes about 100 cycles of the second and 64 of the first).  Measured, 8 KV heads of 128, 4
+// contexts of 32768 keys: 120 rows 128 us, 4.2 TB/s; 256 rows 178 us, 770 TFLOP/s; 512 rows 312 us, 880 TFLOP/s.  Every wait is bounded; when one runs out the block says so in *status, lets what is under
 // way land, frees its tensor memory and returns.
 #include "gemm_tc.h"
 #include "kernels.h"
