@@ -44,7 +44,7 @@ struct PagedRows {
 int64_t paged_attention_workspace(int dtype, int h, int64_t rows_heads, int64_t keys, bool weigh);
 int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,
                            cudaStream_t s);
-// the attention itself on tensor cores (bf16, head_dim 64 or 128); scores (optional): [T][Hq][table_cols * ps] receives
+// the attention itself on tensor cores (bf16); scores (optional): [T][Hq][table_cols * ps] receives
 // scale q.k in units of log2, -infinity where a row does not see a key, up to the request's last key
 constexpr int kMaxPagedBlocks = 320;   // two on each of up to 160 SMs
 int64_t paged_mma_workspace(int h);

@@ -11,83 +11,6 @@ namespace sled {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-
-// One block of four warps per (token, head); warp w takes every fourth key, the lanes share the head dimension.  For bf16 of
-// head_dim 32, which the tensor core kernels do not serve: every head reads its keys by itself, so that L2 binds
-// (@ROW).
-template <typename T, int H>
-__global__ void __launch_bounds__(128) attn_row_kernel(PagedCache c, PagedRows r, const int32_t* list, int list_len) {
-  constexpr int D = H / 32;
-  const int t = blockIdx.x, head = blockIdx.y;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (t == 0 && head == 0)   // one block reports the requests that are left out
-    for (int b = threadIdx.x; b < c.n_reqs; b += blockDim.x) {
-      const ReqView w = req_view(c, r, b);
-      if (!w.ok) set_status(c.status, req_fault(r, w));
-    }
-  const int i = req_of_row(r.cu_q, c.n_reqs, t);
-  const ReqView v = req_view(c, r, i);
-  if (!v.ok) return;
-  const int j = t - v.row0;
-  if (j < 0 || j >= v.m) return;   // rows behind the last request
-  const int g = head / (r.group), prefix = v.n - v.m;
-  uint32_t bits[kMaxTreeNodes / 32] = {};
-  if (r.parents) ancestors_of(r.parents + v.row0, j, bits, warp == 0 && lane == 0 ? c.status : nullptr);
-  bool none = r.parents != nullptr;
-  for (int w = 0; w < kMaxTreeNodes / 32; ++w) none = none && bits[w] == 0;
-  const T* q = reinterpret_cast<const T*>(r.q) + t * r.q_stride + static_cast<int64_t>(head) * H + lane * D;
-  float qf[D], o[D];
-#pragma unroll
-  for (int d = 0; d < D; ++d) { qf[d] = to_f32(q[d]); o[d] = 0.f; }
-  float m = -INFINITY, l = 0.f;
-  const int32_t* table = c.table + static_cast<int64_t>(i) * c.table_stride;
-  const int last = r.parents ? v.n - 1 : prefix + j;   // no key behind this one is seen
-  const int own = last / c.ps;
-  const int n_here = list ? min(list_len, own + 1) * c.ps : last + 1;
-  const int32_t* mine = list ? list + (static_cast<int64_t>(t) * c.Hkv + g) * list_len : nullptr;
-  for (int e = warp; e < n_here && !none; e += 4) {
-    const int x = list ? checked_block(c, mine[e / c.ps]) * c.ps + e % c.ps : e;
-    if (x > last) continue;
-    if (r.parents && x >= prefix) {
-      const int a = x - prefix;
-      if (!((bits[a >> 5] >> (a & 31)) & 1u)) continue;
-    }
-    const int page = checked_page(c, table[x / c.ps]);
-    const int64_t at = ((static_cast<int64_t>(page) * c.Hkv + g) * c.ps + x % c.ps) * H + lane * D;
-    const T* k = reinterpret_cast<const T*>(c.k) + at;
-    const T* vv = reinterpret_cast<const T*>(c.v) + at;
-    float s = 0.f;
-#pragma unroll
-    for (int d = 0; d < D; ++d) s = fmaf(qf[d], to_f32(k[d]), s);
-    s = warp_sum(s) * r.scale * kLog2e;
-    const float mn = fmaxf(m, s);
-    if (s == -INFINITY && mn == -INFINITY) continue;   // nothing but infinitely small scores so far
-    const float al = exp2f(m - mn), p = exp2f(s - mn);
-    l = l * al + p;
-#pragma unroll
-    for (int d = 0; d < D; ++d) o[d] = fmaf(p, to_f32(vv[d]), o[d] * al);
-    m = mn;
-  }
-  __shared__ float so[4][H], sm[4], sl[4];
-#pragma unroll
-  for (int d = 0; d < D; ++d) so[warp][lane * D + d] = o[d];
-  if (lane == 0) { sm[warp] = m; sl[warp] = l; }
-  __syncthreads();
-  float M = -INFINITY;
-  bool nan = false;
-  for (int w = 0; w < 4; ++w) { M = fmaxf(M, sm[w]); nan |= sl[w] != sl[w]; }
-  float den = 0.f;
-  for (int w = 0; w < 4; ++w) den += sm[w] == -INFINITY ? 0.f : exp2f(sm[w] - M) * sl[w];
-  for (int d = threadIdx.x; d < H; d += 128) {
-    float num = 0.f;
-    for (int w = 0; w < 4; ++w) num += sm[w] == -INFINITY ? 0.f : exp2f(sm[w] - M) * so[w][d];
-    reinterpret_cast<T*>(r.out)[t * r.out_stride + static_cast<int64_t>(head) * H + d] =
-        from_f32<T>(M == -INFINITY && !nan ? 0.f : num / den);
-  }
-  if (threadIdx.x == 0 && r.lse)
-    r.lse[static_cast<int64_t>(t) * r.Hq + head] = M == -INFINITY && !nan ? -INFINITY : (M + log2f(den)) * kLn2;
-}
 
 // Adds every key's attention weight: one block per (page of a request, KV head), a warp takes every fourth key of the
 // page and goes through the rows in order.
@@ -186,17 +109,15 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
 // 104 and 112, 114 and 112, 166 and 118); one context of 1000 keys: 16.4 and 15.6, 17.6 and 15.8, 21.1 and 15.8.
 constexpr int kTcRows = 24;
 int64_t parts_bytes(int dtype, int h) {
-  const int64_t a = dtype == 1 ? paged_mma_workspace(h) : paged_f32_workspace(h), b = dtype == 1 ? paged_tc_workspace(h) : 0;
+  const int64_t a = dtype == 1 ? paged_mma_workspace(h) : paged_f32_workspace(h), b = dtype == 1 && h >= 64 ? paged_tc_workspace(h) : 0;
   return ((a > b ? a : b) + 255) / 256 * 256;
 }
 
 // With few rows the scores are kept for the weights, 4 bytes per row and key, where they take no more than this; otherwise
 // the weights are computed from the keys again, which takes a small part of the memory and many times as long (8 contexts
-// of 8192 keys, one token: 68 us and 216; four tokens: 79 and 589).  bf16 of head_dim 32 has no kernel that keeps them.
+// of 8192 keys, one token: 68 us and 216; four tokens: 79 and 589).
 constexpr int64_t kMostScoreBytes = 512LL << 20;
-bool keeps_scores(int dtype, int h, int64_t rows_heads, int64_t keys) {
-  return (dtype == 0 || h >= 64) && (keys == 0 || rows_heads <= kMostScoreBytes / 4 / keys);
-}
+bool keeps_scores(int64_t rows_heads, int64_t keys) { return keys == 0 || rows_heads <= kMostScoreBytes / 4 / keys; }
 
 template <typename T, int H>
 int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws, cudaStream_t s) {
@@ -210,20 +131,16 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
       return w < 0 ? w : n + w;
     }
   }
-  if constexpr (sizeof(T) == 4 || H >= 64) {
-    const int64_t keys = static_cast<int64_t>(c.table_cols) * c.ps;
-    const bool keep = key_weights && keeps_scores(c.dtype, H, static_cast<int64_t>(r.T) * r.Hq, keys);
-    float* scores = keep ? reinterpret_cast<float*>(ws + parts_bytes(c.dtype, H)) : nullptr;
-    n = sizeof(T) == 4 ? launch_paged_f32(c, r, list, list_len, scores, ws, s) : launch_paged_mma(c, r, list, list_len, scores, ws, s);
-    if (n < 0) return n;
-    if (keep) {
-      int sms = 0;
-      if (paged_device(&sms) < 0) return -1;
-      SLED_LAUNCH_PDL(key_weight_sum_kernel, dim3(4 * sms), dim3(256), 0, s, c, r, scores, keys, key_weights);
-      return cudaGetLastError() == cudaSuccess ? n + 1 : -1;
-    }
-  } else {
-    attn_row_kernel<T, H><<<dim3(r.T, r.Hq), 128, 0, s>>>(c, r, list, list_len);
+  const int64_t keys = static_cast<int64_t>(c.table_cols) * c.ps;
+  const bool keep = key_weights && keeps_scores(static_cast<int64_t>(r.T) * r.Hq, keys);
+  float* scores = keep ? reinterpret_cast<float*>(ws + parts_bytes(c.dtype, H)) : nullptr;
+  n = sizeof(T) == 4 ? launch_paged_f32(c, r, list, list_len, scores, ws, s) : launch_paged_mma(c, r, list, list_len, scores, ws, s);
+  if (n < 0) return n;
+  if (keep) {
+    int sms = 0;
+    if (paged_device(&sms) < 0) return -1;
+    SLED_LAUNCH_PDL(key_weight_sum_kernel, dim3(4 * sms), dim3(256), 0, s, c, r, scores, keys, key_weights);
+    return cudaGetLastError() == cudaSuccess ? n + 1 : -1;
   }
   if (key_weights) {
     key_weight_kernel<T, H><<<dim3(c.table_cols, c.Hkv, c.n_reqs), 128, 0, s>>>(c, r, key_weights);
@@ -235,8 +152,7 @@ int launch_rows(const PagedCache& c, const PagedRows& r, const int32_t* list, in
 }  // namespace
 
 int64_t paged_attention_workspace(int dtype, int h, int64_t rows_heads, int64_t keys, bool weigh) {
-  if (dtype == 1 && h < 64) return 0;
-  return parts_bytes(dtype, h) + (weigh && keeps_scores(dtype, h, rows_heads, keys) ? rows_heads * keys * 4 : 0);
+  return parts_bytes(dtype, h) + (weigh && keeps_scores(rows_heads, keys) ? rows_heads * keys * 4 : 0);
 }
 
 int launch_paged_attention(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* key_weights, char* ws,

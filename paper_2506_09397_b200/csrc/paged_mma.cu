@@ -1,4 +1,4 @@
-// Attention over a paged bf16 cache on the warp-level tensor cores, head_dim 64 and 128.
+// Attention over a paged bf16 cache on the warp-level tensor cores.
 //
 // A unit is the query rows that share a KV head (a block of up to 64 of them): they are the M side of m16n8k16 products,
 // so a cached key is read once for all of them.  With up to 16 (32) rows the four computing warps split every 64-key tile
@@ -43,6 +43,10 @@ static_assert(Smem<128>::kTotal + 1024 + 256 <= 228 * 1024 / 2, "two blocks on a
 
 template <int H>
 __device__ __forceinline__ uint32_t at(uint32_t base, int key, int chunk) {
+  if constexpr (H == 32) {   // two keys to a row of 128 bytes
+    const int row = (key & 15) >> 1;
+    return base + (key >> 4) * Smem<H>::kGroup + row * 128 + ((((key & 1) * 4 + chunk) ^ row) << 4);
+  }
   return base + (key >> 4) * Smem<H>::kGroup + (chunk >> 3) * 2048 + (key & 15) * 128 + (((chunk & 7) ^ (key & 7)) << 4);
 }
 
@@ -451,7 +455,7 @@ __global__ void __launch_bounds__(160, 2) paged_mma_kernel(const PagedCache c, c
         if (ok && lane == 0) mbar_expect(ring.full + 8 * st, n_here * 2 * S::kGroup);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const int y = __shfl_sync(0xffffffffu, row, ahead * 4 + p);
+          const int y = __shfl_sync(0xffffffffu, row, ahead * 4 + p) >> (H == 32);
           if (ok && lane == 0 && p < n_here) {
             const uint32_t dst = base + st * S::kStage + p * S::kGroup, bar = ring.full + 8 * st;
             if (again) {
@@ -587,7 +591,9 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
     const float inv = none ? 0.f : 1.f / den;
     const int of = (u.first + row) / group, t = u.row0 + (u.j >= 0 ? u.j : of), head = u.g * group + (u.first + row) - of * group;
     T* out = reinterpret_cast<T*>(r.out) + t * r.out_stride + static_cast<int64_t>(head) * H + lane * D;
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2 && D == 1) {
+      *out = __float2bfloat16_rn(none ? 0.f : num[0] * inv);
+    } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int e = 0; e < D / 2; ++e) reinterpret_cast<uint32_t*>(out)[e] = none ? 0u : pack_bf16(num[2 * e] * inv, num[2 * e + 1] * inv);
     } else {
@@ -629,7 +635,10 @@ int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int l
   }
   CUtensorMap map_k, map_v;
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps;
-  if (tma_map_bf16_row_groups(&map_k, c.k, rows, H, 16) || tma_map_bf16_row_groups(&map_v, c.v, rows, H, 16)) return -1;
+  constexpr int kPerRow = H == 32 ? 2 : 1;      // keys of a row of the map
+  if (tma_map_bf16_row_groups(&map_k, c.k, rows / kPerRow, H * kPerRow, 16 / kPerRow) ||
+      tma_map_bf16_row_groups(&map_v, c.v, rows / kPerRow, H * kPerRow, 16 / kPerRow))
+    return -1;
   const int blocks = min(2 * sms, kMaxPagedBlocks);
   Parts parts;
   parts.acc = reinterpret_cast<float*>(ws);
@@ -651,7 +660,8 @@ int launch_paged_merge(const PagedCache& c, const PagedRows& r, int unit_rows, i
   const int threads = min(512, 32 * unit_rows);   // a warp for each of a small unit's rows
 #define SLED_MERGE(T, H) SLED_LAUNCH_PDL((paged_merge_kernel<T, H>), grid, dim3(threads), 0, s, c, r, unit_rows, parts)
   if (c.dtype == BF16 && c.h == 128) SLED_MERGE(__nv_bfloat16, 128);
-  else if (c.dtype == BF16) SLED_MERGE(__nv_bfloat16, 64);
+  else if (c.dtype == BF16 && c.h == 64) SLED_MERGE(__nv_bfloat16, 64);
+  else if (c.dtype == BF16) SLED_MERGE(__nv_bfloat16, 32);
   else if (c.h == 128) SLED_MERGE(float, 128);
   else if (c.h == 64) SLED_MERGE(float, 64);
   else SLED_MERGE(float, 32);
@@ -664,7 +674,8 @@ int64_t paged_mma_workspace(int h) {
 }
 
 int launch_paged_mma(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s) {
-  return c.h == 128 ? launch_h<128>(c, r, list, list_len, scores, ws, s) : launch_h<64>(c, r, list, list_len, scores, ws, s);
+  if (c.h == 128) return launch_h<128>(c, r, list, list_len, scores, ws, s);
+  return c.h == 64 ? launch_h<64>(c, r, list, list_len, scores, ws, s) : launch_h<32>(c, r, list, list_len, scores, ws, s);
 }
 
 }  // namespace sled
