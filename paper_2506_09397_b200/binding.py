@@ -522,7 +522,9 @@ def plan_attention(n_keys, q_tokens, n_kv_heads: int, group: int, resident_block
 
 
 # ---- operators over a paged cache: torch CUDA tensors in, enqueued on torch's current stream of the cache's device -----
+# (Devices are compared by their index: a short call takes the GPU about as long as its arguments take here.)
 _TORCH_DT = {torch.float32: SLED_F32, torch.bfloat16: SLED_BF16}
+_I32 = torch.int32
 
 
 def _refuse(what: str, why: str):
@@ -533,8 +535,8 @@ def _ints(t, what: str, name: str, dev, shape=None):
     """A CUDA int32 tensor that is contiguous along its last dimension; returns its address (0 for None)."""
     if t is None:
         return 0
-    if t.dtype is not torch.int32 or t.device != dev or (t.stride(-1) != 1 and t.numel() > 1):
-        _refuse(what, f"{name} must be an int32 tensor on {dev}, contiguous along its last dimension")
+    if t.dtype is not _I32 or t.get_device() != dev or (t.stride(-1) != 1 and t.numel() > 1):
+        _refuse(what, f"{name} must be an int32 tensor on cuda:{dev}, contiguous along its last dimension")
     if shape is not None and t.shape != shape:
         _refuse(what, f"{name} must have shape {shape}")
     return t.data_ptr()
@@ -543,26 +545,28 @@ def _ints(t, what: str, name: str, dev, shape=None):
 def _floats(t, what: str, name: str, dev, shape):
     if t is None:
         return 0
-    if t.dtype is not torch.float32 or t.device != dev or t.shape != shape or not t.is_contiguous():
-        _refuse(what, f"{name} must be a contiguous fp32 tensor of shape {tuple(shape)} on {dev}")
+    if t.dtype is not torch.float32 or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        _refuse(what, f"{name} must be a contiguous fp32 tensor of shape {tuple(shape)} on cuda:{dev}")
     return t.data_ptr()
 
 
 def _paged(what: str, k, v, page_table, n_kv, layers: bool = False) -> SledPagedKv:
     """The cache description of a call, from K, V [n_pages, n_kv_heads, page_size, head_dim] (with a leading n_layers
     where the operator works on all layers), page_table [n_reqs, cols] and n_kv [n_reqs]."""
-    dev, shape = k.device, k.shape
-    if dev.type != "cuda":
+    dev, shape, k_dtype = k.get_device(), k.shape, k.dtype
+    if not k.is_cuda:
         raise SledError(SLED_ERR_NO_DEVICE, f"{what} (tensors must be on a CUDA device)")
-    dtype = _TORCH_DT.get(k.dtype)
+    dtype = _TORCH_DT.get(k_dtype)
     if dtype is None or not (len(shape) == 4 or (layers and len(shape) == 5)):
         _refuse(what, "the cache must be fp32 or bf16, [n_pages, n_kv_heads, page_size, head_dim]"
                 + (", with n_layers in front for all layers" if layers else ""))
-    if not k.is_contiguous() or (v is not None and (v.dtype != k.dtype or v.device != dev or v.shape != shape or not v.is_contiguous())):
+    if not k.is_contiguous() or (v is not None and (v.dtype is not k_dtype or v.get_device() != dev or v.shape != shape or not v.is_contiguous())):
         _refuse(what, "k must be contiguous, and v like k")
-    if page_table.dim() != 2 or n_kv.dim() != 1 or n_kv.shape[0] != page_table.shape[0]:
+    if page_table.dim() != 2 or n_kv.dim() != 1:
         _refuse(what, "page_table [n_reqs, cols] and n_kv [n_reqs]")
     n_reqs, cols = page_table.shape
+    if n_kv.numel() != n_reqs:
+        _refuse(what, "page_table [n_reqs, cols] and n_kv [n_reqs]")
     stride = page_table.stride(0) if n_reqs > 1 else cols
     if stride < cols:
         _refuse(what, "rows of page_table must not overlap")
@@ -572,9 +576,8 @@ def _paged(what: str, k, v, page_table, n_kv, layers: bool = False) -> SledPaged
                        _ints(n_kv, what, "n_kv", dev), n_reqs)
 
 
-def _row_stride(t, what: str, name: str):
+def _row_stride(t, what: str, name: str, rows: int, heads: int, h: int):
     """Elements between the rows of q or out [rows, n_q_heads, head_dim]; a row itself is contiguous."""
-    rows, heads, h = t.shape
     if t.is_contiguous():
         return heads * h
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != h):
@@ -582,19 +585,21 @@ def _row_stride(t, what: str, name: str):
     return t.stride(0) if rows > 1 else heads * h
 
 
-def _query_rows(what: str, q, out, k, n_reqs: int, cu_q):
-    """(out, q's and out's row strides); rows may be apart (q a slice of a wider projection)."""
-    if q.dim() != 3 or q.dtype != k.dtype or q.device != k.device or q.shape[2] != k.shape[3]:
+def _query_rows(what: str, q, out, k, kv, dev: int, cu_q):
+    """(out, q's and out's row strides, rows, heads); rows may be apart (q a slice of a wider projection)."""
+    if q.dim() != 3 or q.dtype is not k.dtype or q.get_device() != dev or q.size(2) != kv.head_dim:
         _refuse(what, "q must be [rows, n_q_heads, head_dim] of the cache's type and device")
-    if cu_q.shape != (n_reqs + 1,):
+    if cu_q.dim() != 1 or cu_q.numel() != kv.n_reqs + 1:
         _refuse(what, "cu_q must be [n_reqs + 1]")
+    rows, heads, h = q.shape
+    q_stride = _row_stride(q, what, "q", rows, heads, h)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:
+        return torch.empty_like(q, memory_format=torch.contiguous_format), q_stride, heads * h, rows, heads
+    if out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != dev:
         _refuse(what, "out must be like q")
-    elif out.data_ptr() == q.data_ptr() and q.numel():
+    if out.data_ptr() == q.data_ptr() and q.numel():
         _refuse(what, "out must not be q: queries are read until the call has run")
-    return out, _row_stride(q, what, "q"), _row_stride(out, what, "out")
+    return out, q_stride, _row_stride(out, what, "out", rows, heads, h), rows, heads
 
 
 def _workspace(what: str, dev, kv, *sizes):
@@ -608,8 +613,8 @@ def _workspace(what: str, dev, kv, *sizes):
     return t, t.data_ptr(), n
 
 
-def _stream_of(dev) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev.index)
+def _stream_of(dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: float = 0.0, out=None, lse=None,
@@ -621,9 +626,8 @@ def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: floa
     wrong (see check_status).  Enqueued on torch's current stream; returns out."""
     what = "sled_attention_tree"
     kv = _paged(what, k, v, page_table, n_kv)
-    dev = k.device
-    out, q_stride, out_stride = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
-    rows, heads, _ = q.shape
+    dev = k.get_device()
+    out, q_stride, out_stride, rows, heads = _query_rows(what, q, out, k, kv, dev, cu_q)
     _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, int(key_weights is not None))
     _check(lib().sled_attention_tree(
         kv, q.data_ptr(), q_stride, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
@@ -641,7 +645,7 @@ def evict_keys(k, v, key_weights, page_table, n_kv, budget: int, *, n_sink: int 
     unless key_weights_out is given.  The caller goes on with min(n_kv, budget) keys."""
     what = "sled_evict_keys"
     kv = _paged(what, k, v, page_table, n_kv, layers=True)
-    dev = k.device
+    dev = k.get_device()
     _held, ws, ws_bytes = _workspace(what, dev, kv)
     w = _floats(key_weights, what, "key_weights", dev, k.shape[:-1])
     w_out = _floats(key_weights_out, what, "key_weights_out", dev, k.shape[:-1]) or w
@@ -654,14 +658,14 @@ def block_bounds(k, page_table, n_kv, bounds, *, first=None, status=None) -> Non
     cache's type, for the pages that hold request i's keys first[i] .. n_kv[i]-1 (first None: all)."""
     what = "sled_block_bounds"
     kv = _paged(what, k, None, page_table, n_kv)
-    dev = k.device
+    dev = k.get_device()
     _check_bounds(what, bounds, k)
     _check(lib().sled_block_bounds(kv, _ints(first, what, "first", dev, (kv.n_reqs,)), bounds.data_ptr(),
                                    _ints(status, what, "status", dev), _stream_of(dev)), what)
 
 
 def _check_bounds(what: str, bounds, k) -> None:
-    if bounds.dtype != k.dtype or bounds.device != k.device or not bounds.is_contiguous() or \
+    if bounds.dtype is not k.dtype or bounds.get_device() != k.get_device() or not bounds.is_contiguous() or \
             tuple(bounds.shape) != (k.shape[0], k.shape[1], 2, k.shape[3]):
         _refuse(what, "bounds must be contiguous [n_pages, n_kv_heads, 2, head_dim] of the cache's type and device")
 
@@ -673,10 +677,9 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
     [rows, n_kv_heads, n_blocks] int32 receives what was read.  Enqueued on torch's current stream; returns out."""
     what = "sled_attention_blocks"
     kv = _paged(what, k, v, page_table, n_kv)
-    dev = k.device
+    dev = k.get_device()
     _check_bounds(what, bounds, k)
-    out, q_stride, out_stride = _query_rows(what, q, out, k, kv.n_reqs, cu_q)
-    rows, heads, _ = q.shape
+    out, q_stride, out_stride, rows, heads = _query_rows(what, q, out, k, kv, dev, cu_q)
     _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, n_blocks)
     if blocks is not None and not blocks.is_contiguous():
         _refuse(what, "blocks must be contiguous")

@@ -67,12 +67,13 @@ int check_rows(const sled_paged_kv* kv, const void* q, int64_t q_stride, const i
 class OnDeviceOf {
  public:
   explicit OnDeviceOf(const void* p) {
-    int n_dev = 0;
-    if (cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev == 0) { cudaGetLastError(); rc_ = SLED_ERR_NO_DEVICE; return; }
     cudaPointerAttributes attr{};
-    const bool ok = cudaPointerGetAttributes(&attr, p) == cudaSuccess && attr.type == cudaMemoryTypeDevice;
-    cudaGetLastError();
-    if (!ok || cudaGetDevice(&before_) != cudaSuccess) { rc_ = SLED_ERR_ARG; return; }
+    if (cudaPointerGetAttributes(&attr, p) != cudaSuccess || attr.type != cudaMemoryTypeDevice || cudaGetDevice(&before_) != cudaSuccess) {
+      int n_dev = 0;
+      rc_ = cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev == 0 ? SLED_ERR_NO_DEVICE : SLED_ERR_ARG;
+      cudaGetLastError();
+      return;
+    }
     if (attr.device != before_) {
       if (cudaSetDevice(attr.device) != cudaSuccess) { cudaGetLastError(); rc_ = SLED_ERR_DEVICE; return; }
       moved_ = true;
