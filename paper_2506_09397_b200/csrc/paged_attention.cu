@@ -65,23 +65,36 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
   const int quad = threadIdx.x & 63, part = threadIdx.x >> 6, group = r.group;
   for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
     const int rows = w.v.m * group, end = min(sg.t1 * kTile, w.v.n);
+    const float* mine = scores + (static_cast<int64_t>(w.v.row0) * r.Hq + sg.g * group) * keys;
+    auto row_of = [&](int i) { return i / group * static_cast<int64_t>(r.Hq) + i % group; };
+    auto bring_lse = [&](int first, int here) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < here; i += 256) {
+        const float l = r.lse[static_cast<int64_t>(w.v.row0) * r.Hq + sg.g * group + row_of(first + i)];
+        lse[i] = l == -INFINITY ? INFINITY : l * kLog2e;   // a row that saw nothing adds nothing
+      }
+      __syncthreads();
+    };
+    if (rows <= kRowsAtOnce) bring_lse(0, rows);
     for (int x0 = sg.t0 * kTile; x0 < end; x0 += 256) {
-      const int x = x0 + quad * 4;
+      const int x = x0 + quad * 4, own = x0 + threadIdx.x;
+      float* to = nullptr;   // of this thread's key, under way while the scores are
+      float old = 0.f;
+      if (own < end) {
+        const int page = c.table[static_cast<int64_t>(sg.req) * c.table_stride + quotient(own, c.ps)];
+        if (page_exists(c, page)) {
+          to = key_weights + (static_cast<int64_t>(page) * c.Hkv + sg.g) * c.ps + own % c.ps;
+          old = *to;
+        }
+      }
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int first = 0; first < rows; first += kRowsAtOnce) {
         const int here = min(kRowsAtOnce, rows - first);
-        __syncthreads();
-        for (int i = threadIdx.x; i < here; i += 256) {
-          const int j = (first + i) / group, hh = (first + i) % group;
-          const float l = r.lse[static_cast<int64_t>(w.v.row0 + j) * r.Hq + sg.g * group + hh];
-          lse[i] = l == -INFINITY ? INFINITY : l * kLog2e;   // a row that saw nothing adds nothing
-        }
-        __syncthreads();
+        if (rows > kRowsAtOnce) bring_lse(first, here);
         if (x < end) {
 #pragma unroll 4
           for (int i = part; i < here; i += 4) {
-            const int j = (first + i) / group, hh = (first + i) % group;
-            const float4 s = *reinterpret_cast<const float4*>(scores + (static_cast<int64_t>(w.v.row0 + j) * r.Hq + sg.g * group + hh) * keys + x);
+            const float4 s = *reinterpret_cast<const float4*>(mine + row_of(first + i) * keys + x);
             sum.x += exp2f(s.x - lse[i]);
             sum.y += exp2f(s.y - lse[i]);
             sum.z += exp2f(s.z - lse[i]);
@@ -91,14 +104,8 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
       }
       sums[part][quad] = sum;
       __syncthreads();
-      const int mine = x0 + threadIdx.x;   // and now a key per thread
-      if (mine < end) {
-        const int page = c.table[static_cast<int64_t>(sg.req) * c.table_stride + mine / c.ps];
-        if (page_exists(c, page)) {
-          const float* s = reinterpret_cast<const float*>(sums) + threadIdx.x;
-          key_weights[(static_cast<int64_t>(page) * c.Hkv + sg.g) * c.ps + mine % c.ps] += (s[0] + s[256]) + (s[512] + s[768]);
-        }
-      }
+      const float* s = reinterpret_cast<const float*>(sums) + threadIdx.x;   // and now a key per thread
+      if (to) *to = old + ((s[0] + s[256]) + (s[512] + s[768]));
       __syncthreads();
     }
   });

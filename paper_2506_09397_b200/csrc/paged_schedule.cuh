@@ -78,7 +78,8 @@ struct AttentionLine {
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
     if (list_len == kWholeRows) w.weight = min(16 + rows, kMinShare - 1);
     else if (unit_rows == kUnitRows) w.weight = unit_weight(tile_weight(min(rows, kUnitRows)), 32, w.tiles);
-    else if (unit_rows > kUnitRows) w.weight = rows > kUnitRows * 2 ? unit_weight(38, 240, w.tiles) : unit_weight(16, 160, w.tiles);
+    // tcgen05, cycles by regression over the blocks: 2200 a tile and 15,000 a unit up to 128 rows, 4000 and 18,500 above
+    else if (unit_rows > kUnitRows) w.weight = rows > kUnitRows * 2 ? unit_weight(38, 175, w.tiles, 38 + 175) : unit_weight(16, 160, w.tiles);
     else w.weight = unit_weight(12, 24, w.tiles, kMinWarpShare - 1);
     return w;
   }
