@@ -358,7 +358,8 @@ int sled_attention_tree(const sled_paged_kv* kv, const void* q, int64_t q_stride
  * caller goes on with min(n_kv, budget) keys.
  *   key_weights      [n_layers][n_pages][n_kv_heads][page_size] fp32
  *   key_weights_out  the weights of the kept keys, at their new slots: key_weights itself, or an array that does not
- *                    overlap it (then requests within the budget are copied, and slots behind the kept keys left alone) */
+ *                    overlap it (then requests within the budget are copied).  Entries of slots behind the kept keys are left
+ *                    as they are: a caller that adds weights up clears those of the keys it appends */
 int sled_evict_keys_workspace(const sled_paged_kv* kv, int64_t* bytes);
 int sled_evict_keys(const sled_paged_kv* kv, float* key_weights, float* key_weights_out, int32_t budget, int32_t n_sink,
                     int32_t n_recent, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);

@@ -342,7 +342,8 @@ template <typename T, int H>
 int choice_typed(const PagedCache& c, const PagedRows& r, const void* bounds, int n_blocks, int n_local, float* scores, int32_t* list, cudaStream_t s) {
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
-  // few choices among many blocks: a large block each; many choices share an SM (@CHOICE)
+  // few choices among many blocks: a large block each; many choices share an SM (a whole call, one token of 30000 keys: 26 us,
+  // with 256 threads 37; 109 tokens of 24 contexts: 151 us, with 1024 threads 159)
   const int threads = c.table_cols > 512 && static_cast<int64_t>(r.T) * c.Hkv <= 2 * sms ? 1024 : 256;
   if constexpr (sizeof(T) == 2 && H >= 64) {
     if (r.group <= kScoreRows) {

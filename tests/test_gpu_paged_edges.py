@@ -4,7 +4,7 @@ import random
 import paged_ref as R
 import pytest
 import torch
-from test_gpu_paged import BF, F32, _check_attention, _check_blocks, _cu, _queries, _tree
+from test_gpu_paged import BF, F32, _check_attention, _check_blocks, _check_eviction, _cu, _queries, _tree
 
 from paper_2506_09397_b200 import binding as B
 
@@ -134,6 +134,17 @@ def _bounds(k, table, n_kv):
     bounds = torch.zeros(k.shape[0], k.shape[1], 2, k.shape[3], dtype=k.dtype, device="cuda")
     B.block_bounds(k, table, n_kv, bounds)
     return (bounds,)
+
+
+@pytest.mark.parametrize("page", [48, 112])
+def test_eviction_and_bounds_of_pages_that_are_no_power_of_two(page):
+    _check_eviction([page * 6 + 1, 70, page * 9, 0], 71, 3, 20, page=page, layers=3, separate=True)
+    k, v, table, n_kv = R.make_cache([page * 3 + 5, page], 2, 64, BF, page, garbage=float("inf"))
+    got = _bounds(k.cuda(), table.cuda(), n_kv.cuda())[0].cpu()
+    for i, n in enumerate([page * 3 + 5, page]):
+        for b in range((n + page - 1) // page):
+            keys = k[table[i, b], :, :min(page, n - b * page)]
+            assert torch.equal(got[table[i, b], :, 0], keys.amin(1)) and torch.equal(got[table[i, b], :, 1], keys.amax(1))
 
 
 def test_results_in_the_place_of_the_queries_are_refused():
