@@ -77,9 +77,11 @@ struct AttentionLine {
     w.n_rb = list_len == kWholeRows ? 1 : (rows + unit_rows - 1) / unit_rows;
     w.units = w.n_rb * c.Hkv * (list_len > 0 ? w.v.m : 1);
     if (list_len == kWholeRows) w.weight = min(16 + rows, kMinShare - 1);
-    else if (unit_rows == kUnitRows) w.weight = unit_weight(tile_weight(min(rows, kUnitRows)), 32, w.tiles);
-    // tcgen05, cycles by regression over the blocks: 2200 a tile and 15,000 a unit up to 128 rows, 4000 and 18,500 above
+    // tcgen05, in cycles by regression over the blocks: 2200 a tile and 15,000 a unit up to 128 rows, 4000 and 18,500 above
     else if (unit_rows > kUnitRows) w.weight = rows > kUnitRows * 2 ? unit_weight(38, 175, w.tiles, 38 + 175) : unit_weight(16, 160, w.tiles);
+    // warp-level tensor cores, likewise: 2100 a tile and 8100 a unit with up to 16 rows (32 contexts of 128 .. 16384 keys with
+    // weights 127 us; half as much for a unit, and capped at 63, 139)
+    else if (unit_rows == kUnitRows) w.weight = unit_weight(tile_weight(min(rows, kUnitRows)), 64, w.tiles, tile_weight(kUnitRows) + 64);
     else w.weight = unit_weight(12, 24, w.tiles, kMinWarpShare - 1);
     return w;
   }
