@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
       __syncthreads();
       for (int i = threadIdx.x; i < here; i += 256) {
         const float l = r.lse[static_cast<int64_t>(w.v.row0) * r.Hq + sg.g * group + row_of(first + i)];
-        lse[i] = l == -INFINITY ? INFINITY : l * kLog2e;   // a row that saw nothing adds nothing
+        lse[i] = l * kLog2e;
       }
       __syncthreads();
     };
@@ -95,10 +95,12 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
 #pragma unroll 4
           for (int i = part; i < here; i += 4) {
             const float4 s = *reinterpret_cast<const float4*>(mine + row_of(first + i) * keys + x);
-            sum.x += exp2f(s.x - lse[i]);
-            sum.y += exp2f(s.y - lse[i]);
-            sum.z += exp2f(s.z - lse[i]);
-            sum.w += exp2f(s.w - lse[i]);
+            const float l = lse[i];
+            const bool some = l != -INFINITY;   // a row that saw nothing adds nothing, whatever its query holds
+            sum.x += some ? exp2f(s.x - l) : 0.f;
+            sum.y += some ? exp2f(s.y - l) : 0.f;
+            sum.z += some ? exp2f(s.z - l) : 0.f;
+            sum.w += some ? exp2f(s.w - l) : 0.f;
           }
         }
       }

@@ -30,7 +30,8 @@ struct Wg {
   static constexpr int kOffBar = kOffK + kStages * kTileBytes;
   static constexpr int kOffLse = kOffBar + 256;            // of the rows at hand, in units of log2, for either group
   static constexpr int kOffToken = kOffLse + 2 * kRows * 4; // token of each of them, one byte, for either group
-  static constexpr int kOffDown = kOffToken + 2 * kRows;    // who sees a node: a set of nodes each
+  static constexpr int kOffNone = kOffToken + 2 * kRows;    // which of them saw nothing, 32 to a word, for either group
+  static constexpr int kOffDown = kOffNone + 2 * kRows / 8; // who sees a node: a set of nodes each
   static constexpr int kOffParent = kOffDown + kMaxTreeNodes * 16;
   static constexpr int kTotal = kOffParent + kMaxTreeNodes + 1024;
 };
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(320, 1) paged_weigh_kernel(const PagedCache c,
     const uint32_t tmem_s = tmem + lanes + s * 256;
     float* lse = reinterpret_cast<float*>(ptr + L::kOffLse) + s * kRows;
     uint8_t* token = ptr + L::kOffToken + s * kRows;
+    uint32_t* none = reinterpret_cast<uint32_t*>(ptr + L::kOffNone) + s * (kRows / 32);
     uint32_t* down = reinterpret_cast<uint32_t*>(ptr + L::kOffDown);
     signed char* parents = reinterpret_cast<signed char*>(ptr + L::kOffParent);
     const float scale = r.scale * kLog2e;
@@ -184,12 +186,14 @@ __global__ void __launch_bounds__(320, 1) paged_weigh_kernel(const PagedCache c,
       auto bring_lse = [&](int rb) {
         group_sync();
         const int rows = min(w.v.m - rb * tokens, tokens) * group;
-        for (int i = key; i < (rows + 31) / 32 * 32; i += 128) {
+        for (int i = key; i < (rows + 31) / 32 * 32; i += 128) {    // whole warps
           float x = INFINITY;        // a row that saw nothing, or is none, adds nothing
           if (i < rows) {
             const float y = r.lse[static_cast<int64_t>(w.v.row0 + rb * tokens + i / group) * r.Hq + sg.g * group + i % group];
             if (y != -INFINITY) x = y * kLog2e;
           }
+          const uint32_t empty = __ballot_sync(0xffffffffu, x == INFINITY);
+          if (lane == 0) none[i >> 5] = empty;
           lse[i] = x;
           token[i] = static_cast<uint8_t>(i / group);
         }
@@ -239,10 +243,10 @@ __global__ void __launch_bounds__(320, 1) paged_weigh_kernel(const PagedCache c,
           for (int q = 0; q * 32 < rows; ++q) {
             float v[32];
             tmem_ld32(tmem_s + q * 32, v);
-            const int left = rows - q * 32;
-            if (left < 32) {      // columns beyond the rows hold nothing that means anything
+            const uint32_t empty = none[q];
+            if (empty) {          // scores of rows that saw nothing, and columns beyond the rows, may be no numbers
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = i < left ? v[i] : 0.f;
+              for (int i = 0; i < 32; ++i) v[i] = (empty >> i) & 1u ? 0.f : v[i];
             }
             if (node_tile && x >= prefix) {
 #pragma unroll

@@ -1,0 +1,91 @@
+"""Operators over a paged cache where numbers, lengths or tables are unusual, against the 64-bit statements of tests/paged_ref.py."""
+import math
+import random
+
+import paged_ref as R
+import pytest
+import torch
+from test_gpu_paged import BF, F32, _cu, _queries, _tree
+
+from paper_2506_09397_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+def _close(got, want, tol):
+    """Equal where the wanted values are no finite numbers, within tol elsewhere."""
+    odd = ~torch.isfinite(want)
+    fine = (got - want).abs() <= tol
+    assert bool(torch.where(odd, (got == want) | (got.isnan() & want.isnan()), fine).all()), \
+        (int((odd & ~((got == want) | (got.isnan() & want.isnan()))).sum()), float((got - want)[~odd].abs().sub(tol[~odd]).max()))
+
+
+def _widened(table, columns):
+    """The same table with `columns` columns; those behind the requests' pages lie outside the pool."""
+    wide = torch.full((table.shape[0], columns), 1 << 30, dtype=torch.int32)
+    wide[:, :table.shape[1]] = table
+    return wide
+
+
+def _check_call(cache, q, lens, q_len, parents=None, *, columns=0, weigh=True):
+    """Runs sled_attention_tree on a cache and queries that may hold anything, and compares out, lse and weights."""
+    k, v, table, n_kv = cache
+    hkv, page, h = k.shape[1:]
+    hq = q.shape[1]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lse = torch.full((sum(q_len), hq), 7.0, device="cuda")
+    w0 = torch.rand(k.shape[:3], generator=torch.Generator().manual_seed(5))
+    w = w0.cuda()
+    flat = None if parents is None else torch.tensor(sum(parents, []), dtype=torch.int32, device="cuda")
+    gpu_table = (_widened(table, columns) if columns else table).cuda()
+    out = B.attention_tree(q.cuda(), k.cuda(), v.cuda(), gpu_table, n_kv.cuda(), _cu(q_len), flat, lse=lse, status=status,
+                           key_weights=w if weigh else None)
+    B.check_status(status)
+    out, lse, w = out.cpu().double(), lse.cpu().double(), w.cpu().double()
+    want_w, tol_w = w0.double().clone(), w0.double() * 2.0 ** -23
+    at = 0
+    for i, (n, m) in enumerate(zip(lens, q_len)):
+        kk, vv = (R.keys_of(x, table[i], n, page) for x in (k, v))
+        see = R.tree_mask(None if parents is None else parents[i], m, n)
+        o, l, p, d_o, d_l, rel = R.attend(q[at:at + m], kk, torch.where(torch.isfinite(vv), vv, 0), see, h ** -0.5, q.dtype)
+        # values that are no numbers reach the rows that see them, and no others
+        seen = p.view(m, hkv, hq // hkv, n) > 0
+        for what, value in ((vv == INF, INF), (vv == -INF, -INF), (vv.isnan(), NAN)):
+            hit = torch.einsum("mgrn,gnd->mgrd", seen.double(), what.double()).reshape(m, hq, h) > 0
+            o = o + torch.where(hit, value, 0.0)
+        _close(out[at:at + m], o, d_o)
+        _close(lse[at:at + m], l, d_l)
+        per = p.view(m, hkv, hq // hkv, n).sum((0, 2))
+        off = (p * rel.nan_to_num()[..., None]).view(m, hkv, hq // hkv, n).sum((0, 2))
+        for b in range((n + page - 1) // page):
+            c = min(page, n - b * page)
+            want_w[table[i, b], :, :c] += per[:, b * page:b * page + c]
+            # the sum of the rows and its addition are rounded too
+            tol_w[table[i, b], :, :c] += off[:, b * page:b * page + c] + per[:, b * page:b * page + c] * (m * hq // hkv + 2) * 2.0 ** -24
+        at += m
+    if weigh:
+        _close(w, want_w, tol_w)
+    return out
+
+
+# (query heads, nodes a request, table columns): weights from kept scores, by tcgen05 (bf16), and without kept scores
+PATHS = [(8, 5, 0), (8, 40, 0), (8, 5, 300000)]
+
+
+@pytest.mark.parametrize("what", [NAN, INF, -INF])
+@pytest.mark.parametrize("hq,m,columns", PATHS)
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_queries_of_unused_nodes_may_be_anything(dtype, hq, m, columns, what):
+    """A batch padded with unused nodes: what their queries hold reaches neither results nor weights."""
+    lens, q_len = [400, 70, 129], [m, m, m]
+    rng = random.Random(m)
+    parents = [_tree(rng, m) for _ in q_len]
+    parents[0][m - 2] = parents[1][2] = -2
+    parents[2] = [-2] * m                                   # a request without any used node
+    q = _queries(q_len, hq, 64, dtype, 3)
+    for i in range(3):
+        for j, row in enumerate(R.tree_mask(parents[i], m, lens[i])):
+            if not bool(row.any()):
+                q[i * m + j] = what
+    _check_call(R.make_cache(lens, 2, 64, dtype, seed=2), q, lens, q_len, parents, columns=columns)
