@@ -96,11 +96,13 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
           for (int i = part; i < here; i += 4) {
             const float4 s = *reinterpret_cast<const float4*>(mine + row_of(first + i) * keys + x);
             const float l = lse[i];
-            const bool some = l != -INFINITY;   // a row that saw nothing adds nothing, whatever its query holds
-            sum.x += some ? exp2f(s.x - l) : 0.f;
-            sum.y += some ? exp2f(s.y - l) : 0.f;
-            sum.z += some ? exp2f(s.z - l) : 0.f;
-            sum.w += some ? exp2f(s.w - l) : 0.f;
+            // A row that saw nothing adds nothing, whatever its query holds; nor does a row to a key that it does not see
+            // (a score of -infinity), also where the row is no number.
+            const bool some = l != -INFINITY;
+            sum.x += some && s.x != -INFINITY ? exp2f(s.x - l) : 0.f;
+            sum.y += some && s.y != -INFINITY ? exp2f(s.y - l) : 0.f;
+            sum.z += some && s.z != -INFINITY ? exp2f(s.z - l) : 0.f;
+            sum.w += some && s.w != -INFINITY ? exp2f(s.w - l) : 0.f;
           }
         }
       }

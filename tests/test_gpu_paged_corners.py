@@ -89,3 +89,15 @@ def test_queries_of_unused_nodes_may_be_anything(dtype, hq, m, columns, what):
             if not bool(row.any()):
                 q[i * m + j] = what
     _check_call(R.make_cache(lens, 2, 64, dtype, seed=2), q, lens, q_len, parents, columns=columns)
+
+
+@pytest.mark.parametrize("hq,m,columns", PATHS)
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("chain", [False, True])
+def test_a_row_that_is_no_number_weighs_only_on_the_keys_it_sees(dtype, hq, m, columns, chain):
+    lens, q_len = [400, 70], [m, m]
+    rng = random.Random(m)
+    parents = None if chain else [[-1] * m, _tree(rng, m)]
+    q = _queries(q_len, hq, 64, dtype, 3)
+    q[1, 3, 9] = NAN                                        # second node of the first request, one head
+    _check_call(R.make_cache(lens, 2, 64, dtype, seed=2), q, lens, q_len, parents, columns=columns)
