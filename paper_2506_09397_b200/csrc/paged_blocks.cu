@@ -1,9 +1,10 @@
 // Bounds of the keys of every block (page) of a cache, and the choice of the blocks that a query attends to.
 //
 // bounds[page][kv head][0/1][d] = smallest / largest k_d over the block's keys.  For a query q every key of the block has
-// q.k <= sum_d max(q_d low_d, q_d high_d) = sum_d max(q_d, 0) high_d + min(q_d, 0) low_d: the block's score for that
-// query, the largest over the heads that share the KV head.  A query reads the n_local blocks that end with its own and,
-// of the earlier ones, those of largest score, the lower block first among equals.
+// q.k <= sum_d max(q_d low_d, q_d high_d) (= sum_d max(q_d, 0) high_d + min(q_d, 0) low_d where all of them are finite):
+// the block's score for that query, the largest over the heads that share the KV head.  A query reads the n_local blocks
+// that end with its own and, of the earlier ones, those of largest score, the lower block first among equals.  Scores are
+// fp32 sums.
 #include <algorithm>
 
 #include "paged_schedule.cuh"
@@ -114,6 +115,19 @@ __global__ void __launch_bounds__(256) block_bounds_kernel(PagedCache c, const i
 // the larger of two scores; a NaN is the largest
 __device__ __forceinline__ float larger(float a, float b) { return a != a || b != b ? NAN : fmaxf(a, b); }
 
+// The score by its definition, for one query and block: bounds or queries that are not finite take this way, since on the
+// tensor cores the zeros of min(q, 0) and max(q, 0) meet the bound that does not count, and 0 times infinity is no number.
+template <typename T, int H>
+__device__ __noinline__ float score_of(const T* q, const T* low) {
+  float s = 0.f;
+#pragma unroll 1
+  for (int d = 0; d < H; ++d) {
+    const float x = to_f32(q[d]);
+    s += larger(x * to_f32(low[d]), x * to_f32(low[H + d]));
+  }
+  return s;
+}
+
 constexpr int kScoreRows = 48;
 
 // Earlier blocks of a request's tokens, in tiles of 64, for units of (KV head, up to 48 rows); nothing where all blocks of
@@ -179,6 +193,7 @@ __global__ void __launch_bounds__(128, 3) block_score_kernel(PagedCache c, Paged
     };
     fetch(sg.t0);
     __syncthreads();
+    uint32_t found = 0;        // all ones in an exponent carry into bit 15 or 31
     {
       // the rows as the two halves of the contraction, all loads under way at once
       constexpr int kVecs = kScoreRows * (H / 8) / 128;
@@ -201,6 +216,7 @@ __global__ void __launch_bounds__(128, 3) block_score_kernel(PagedCache c, Paged
         uint32_t low[4], high[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
+          found |= (in[k] & 0x7f807f80u) + 0x00800080u;
           low[k] = Vec<__nv_bfloat16>::smaller(in[k], 0u);
           high[k] = Vec<__nv_bfloat16>::larger(in[k], 0u);
         }
@@ -208,7 +224,7 @@ __global__ void __launch_bounds__(128, 3) block_score_kernel(PagedCache c, Paged
         *reinterpret_cast<uint4*>(qs + row * kRow + H + 8 * d) = make_uint4(high[0], high[1], high[2], high[3]);
       }
     }
-    __syncthreads();
+    const bool odd = __syncthreads_or((found & 0x80008000u) != 0);   // a query that is not finite
     for (int t = sg.t0; t < sg.t1; ++t) {
 #pragma unroll 1
       for (int mt = 0; mt * 16 < rows; ++mt) {
@@ -239,6 +255,12 @@ __global__ void __launch_bounds__(128, 3) block_score_kernel(PagedCache c, Paged
         const int j = e >> 6, col = e & 63, b = t * 64 + col;
         float best = tile[j * group][col];
         for (int hh = 1; hh < group; ++hh) best = larger(best, tile[j * group + hh][col]);
+        if ((odd || best != best) && b < early) {                     // infinite bounds leave a NaN as well
+          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(r.q) + (w.v.row0 + j0 + j) * r.q_stride + static_cast<int64_t>(sg.g * group) * H;
+          const __nv_bfloat16* low = bounds + (static_cast<int64_t>(checked_page(c, table[b])) * c.Hkv + sg.g) * 2 * H;
+          best = -INFINITY;
+          for (int hh = 0; hh < group; ++hh) best = larger(best, score_of<__nv_bfloat16, H>(q + hh * H, low));
+        }
         if (b < early) scores[(static_cast<int64_t>(w.v.row0 + j0 + j) * c.Hkv + sg.g) * c.table_cols + b] = best;
       }
       __syncthreads();
@@ -273,8 +295,7 @@ __global__ void __launch_bounds__(256) block_score_row_kernel(PagedCache c, Page
 #pragma unroll
       for (int d = 0; d < D; ++d) {
         const float x = to_f32(q[d]);
-        s = fmaf(fmaxf(x, 0.f), high[d], s);
-        s = fmaf(fminf(x, 0.f), low[d], s);
+        s += larger(x * low[d], x * high[d]);
       }
       best = larger(best, warp_sum(s));
     }

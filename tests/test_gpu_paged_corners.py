@@ -101,3 +101,62 @@ def test_a_row_that_is_no_number_weighs_only_on_the_keys_it_sees(dtype, hq, m, c
     q = _queries(q_len, hq, 64, dtype, 3)
     q[1, 3, 9] = NAN                                        # second node of the first request, one head
     _check_call(R.make_cache(lens, 2, 64, dtype, seed=2), q, lens, q_len, parents, columns=columns)
+
+
+def _check_choice(q, bounds, hkv, h, dtype, n_blocks=9, n_local=2):
+    """One token over 40 blocks whose bounds are given; the choice by the definition, in 64 bits."""
+    k, v, table, n_kv = (t.cuda() for t in R.make_cache([640], hkv, h, dtype, garbage=0.0))
+    mine = torch.zeros(k.shape[0], hkv, 2, h, dtype=dtype, device="cuda")
+    mine[table[0].long()] = bounds.cuda()
+    blocks = torch.full((1, hkv, n_blocks), -1, dtype=torch.int32, device="cuda")
+    B.attention_blocks(q.cuda(), k, v, mine, table, n_kv, _cu([1]), n_blocks=n_blocks, n_local=n_local, blocks=blocks)
+    blocks = blocks.cpu().long()
+    early, want = 40 - n_local, n_blocks - n_local
+    s = R.block_scores(q[0], bounds[:early], hkv)
+    finite = torch.where(torch.isfinite(bounds), bounds, 0)[:early].double().abs().amax(2).transpose(0, 1)[:, None]
+    size = (q[0].double().abs().nan_to_num(0, 0, 0).view(hkv, -1, 1, h) * finite).sum(-1).amax((1, 2))
+    off = 2 * size * (2 * h + 8) * 2.0 ** -24               # two scores that are nearer than this may change places
+    s = torch.where(s.isnan(), 3e300, torch.where(s == INF, 2e300, torch.where(s == -INF, -2e300, s)))
+    for g in range(hkv):
+        got = blocks[g * 0, g, :want]
+        rest = torch.ones(early, dtype=torch.bool)
+        rest[got] = False
+        assert bool((got[1:] > got[:-1]).all()) and s[g, got].min() >= s[g, rest].max() - off[g], (g, got.tolist(), s[g].topk(want).indices.sort().values.tolist())
+        edge = s[g, got].min()                              # among equals that are no finite numbers, the lowest blocks
+        if float(edge.abs()) > 1e300:
+            equal = (s[g] == edge).nonzero().flatten()
+            taken = got[s[g, got] == edge]
+            assert torch.equal(taken, equal[:len(taken)])
+
+
+@pytest.mark.parametrize("dtype,h", [(BF, 64), (BF, 128), (BF, 32), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("hq", [2, 8])
+@pytest.mark.parametrize("which", ["high", "low", "both", "many"])
+def test_scores_of_infinite_bounds(dtype, h, hq, which):
+    """An infinite bound counts with the queries whose sign meets it, and with no others."""
+    g = torch.Generator().manual_seed(h + hq)
+    x = torch.randn(40, 2, 2, h, generator=g).sort(2).values.to(dtype)
+    q = torch.randn(1, hq, h, generator=g).to(dtype)
+    q[..., 7], q[..., 8] = -q[..., 7].abs() - 0.1, q[..., 8].abs() + 0.1
+    if which == "high":
+        x[11, :, 1, 7] = INF                                # a query component below 0 meets the low bound
+    elif which == "low":
+        x[11, :, 0, 8] = -INF
+    elif which == "both":
+        x[11, 0, 1, 7] = x[12, 1, 1, 8] = INF               # the second one is met
+        x[13, :, 0, 7] = -INF                               # and so is this
+    else:
+        x[:, :, 1, 7] = INF
+        x[::3, :, 0, 8] = -INF
+    _check_choice(q, x, 2, h, dtype)
+
+
+@pytest.mark.parametrize("dtype,h", [(BF, 64), (BF, 128), (BF, 32), (F32, 64)])
+@pytest.mark.parametrize("what", [NAN, INF, -INF])
+def test_choice_of_queries_that_are_no_numbers(dtype, h, what):
+    g = torch.Generator().manual_seed(h)
+    x = torch.randn(40, 2, 2, h, generator=g).sort(2).values.to(dtype)
+    x[20, :, 0, 3] = x[30, :, 1, 3] = 0                     # infinity times 0 is no number
+    q = torch.randn(1, 8, h, generator=g).to(dtype)
+    q[0, 1, 3] = what                                       # one head of the first KV head
+    _check_choice(q, x, 2, h, dtype)
