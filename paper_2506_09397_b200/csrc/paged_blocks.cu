@@ -28,7 +28,7 @@ struct BoundsLine {
     w.v.ok = w.v.n >= 0 && w.v.n <= static_cast<int64_t>(c.table_cols) * c.ps;
     w.n_rb = 1;
     w.tiles = w.v.ok ? max(0, (w.v.n + c.ps - 1) / c.ps - from(i)) : 0;
-    w.units = w.tiles ? c.Hkv : 0;
+    w.units = w.tiles && !(first && first[i] >= w.v.n) ? c.Hkv : 0;     // nothing where there are no new keys, in a page partly filled either
     w.weight = 1;
     return w;
   }

@@ -103,6 +103,20 @@ def test_a_row_that_is_no_number_weighs_only_on_the_keys_it_sees(dtype, hq, m, c
     _check_call(R.make_cache(lens, 2, 64, dtype, seed=2), q, lens, q_len, parents, columns=columns)
 
 
+# ------------------------------------------------------------------------------------------------------- bounds, choice
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_bounds_without_new_keys_are_left_alone(dtype):
+    lens, first = [20, 20, 20, 33, 16, 47], [20, 25, 100, 32, 16, 47]
+    k, _, table, n_kv = R.make_cache(lens, 2, 64, dtype)
+    got = torch.full((k.shape[0], 2, 2, 64), 9.0, dtype=dtype)
+    want = got.clone()
+    got = got.cuda()
+    B.block_bounds(k.cuda(), table.cuda(), n_kv.cuda(), got, first=torch.tensor(first, dtype=torch.int32, device="cuda"))
+    x = k[table[3, 2], :, :1]                               # only the fourth request has a key there: its 33rd
+    want[table[3, 2]] = torch.stack([x.amin(1), x.amax(1)], 1)
+    assert torch.equal(got.cpu(), want)
+
+
 def _check_choice(q, bounds, hkv, h, dtype, n_blocks=9, n_local=2):
     """One token over 40 blocks whose bounds are given; the choice by the definition, in 64 bits."""
     k, v, table, n_kv = (t.cuda() for t in R.make_cache([640], hkv, h, dtype, garbage=0.0))
