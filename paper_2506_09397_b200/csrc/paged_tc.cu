@@ -307,7 +307,8 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       ++units;
       const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first);
       const bool both = kGroups == 2 && rows > kGroupRows;
-      const int n_tiles = u.sg.t1 - u.sg.t0, prefix = u.n - u.m, end = u.n;
+      // positions below `prefix` are seen by all rows of the unit: those of a chain end with its first row's own
+      const int n_tiles = u.sg.t1 - u.sg.t0, prefix = u.n - u.m + (r.parents ? 0 : first / group + 1), end = u.n;
       const int row = (both ? s * kGroupRows : 0) + row_in_group;      // of the unit
       const bool valid = row < rows, active = (row & ~31) < rows;      // whole warps without rows only keep up
       const int j = valid ? (first + row) / group : 0, head = u.sg.g * group + (valid ? (first + row) % group : 0);
@@ -316,7 +317,7 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
       // those out.)  Either group has its own copy of the parents, so that neither waits for the other.
       RowView view;
       view.tree = r.parents != nullptr;
-      view.last = prefix + j;
+      view.last = u.n - u.m + j;
 #pragma unroll
       for (int i = 0; i < kMaxTreeNodes / 32; ++i) view.bits[i] = 0;
       bool dead = false;
@@ -519,9 +520,11 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
           f_other = x.y;
         }
       }
-      // values that were left out of a group's products, for the rows that see them
+      // values that were left out of a group's products, for the rows that see them (of a chain few keys of the masked tiles
+      // are: a prompt's unit goes through its own last keys only)
       auto add_odd = [&](float* v, int d0, int whose) {
-        for (int x = max(prefix & ~(kKeys - 1), u.sg.t0 * kKeys); x < min(end, u.sg.t1 * kKeys); ++x) {
+        const int behind = min(view.tree ? end : min(end, view.last + 1), u.sg.t1 * kKeys);
+        for (int x = max(prefix & ~(kKeys - 1), u.sg.t0 * kKeys); x < behind; ++x) {
           if (!both && ((x / kKeys - u.sg.t0) & 1) != whose) continue;
           if (!(view.seen(x & ~31, prefix, end) >> (x & 31) & 1u)) continue;
           const int page = checked_page(c, c.table[static_cast<int64_t>(u.sg.req) * c.table_stride + x / c.ps]);

@@ -174,3 +174,27 @@ def test_choice_of_queries_that_are_no_numbers(dtype, h, what):
     q = torch.randn(1, 8, h, generator=g).to(dtype)
     q[0, 1, 3] = what                                       # one head of the first KV head
     _check_choice(q, x, 2, h, dtype)
+
+
+@pytest.mark.parametrize("n,group", [(300000, 1), (3000, 4)])
+def test_long_chains_with_values_that_are_no_numbers(n, group):
+    """A whole prompt as one chain: a value that is no number reaches the rows behind it, and takes the others no time to
+    go round (in the long one every wait of the kernel would run out otherwise)."""
+    h, page = 128, 256
+    k, v, table, n_kv = R.make_cache([n], 1, h, BF, page, seed=7)
+    for x, d, what in ((20, 3, NAN), (n // 2, 70, INF), (n - 2, 90, -INF)):
+        v[table[0, x // page], 0, x % page, d] = what
+    q = _queries([n], group, h, BF, 8)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lse = torch.zeros(n, group, device="cuda")
+    out = B.attention_tree(q.cuda(), k.cuda(), v.cuda(), table.cuda(), n_kv.cuda(), _cu([n]), lse=lse, status=status)
+    B.check_status(status)
+    kk, vv = (R.keys_of(x, table[0], n, page) for x in (k, v))
+    for j in (0, 19, 20, 21, 127, 128, 129, 1000, n // 2 - 1, n // 2, n // 2 + 1, n - 200, n - 3, n - 2, n - 1):
+        see = torch.ones(1, j + 1, dtype=torch.bool)
+        o, l, p, d_o, d_l, _ = R.attend(q[j:j + 1], kk[:, :j + 1], torch.where(torch.isfinite(vv[:, :j + 1]), vv[:, :j + 1], 0), see, h ** -0.5, BF)
+        for x, d, what in ((20, 3, NAN), (n // 2, 70, INF), (n - 2, 90, -INF)):
+            if x <= j:
+                o[..., d] = what
+        _close(out[j:j + 1].cpu().double(), o, d_o)
+        _close(lse[j:j + 1].cpu().double(), l, d_l)
