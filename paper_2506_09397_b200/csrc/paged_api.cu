@@ -36,13 +36,15 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 // sizes and pointers of a cache description; layers: whether more than one layer is allowed
 int check_cache(const sled_paged_kv* kv, bool need_v, bool layers) {
-  if (!kv || !kv->k || (need_v && !kv->v) || !kv->page_table || !kv->n_kv) return SLED_ERR_ARG;
+  if (!kv || !kv->k || (need_v && !kv->v)) return SLED_ERR_ARG;
   if (kv->dtype != SLED_F32 && kv->dtype != SLED_BF16) return SLED_ERR_ARG;
   if (kv->head_dim != 32 && kv->head_dim != 64 && kv->head_dim != 128) return SLED_ERR_ARG;
   if (kv->page_size <= 0 || kv->page_size % 16 || kv->page_size > 256) return SLED_ERR_ARG;
   if (kv->n_layers < 1 || (!layers && kv->n_layers != 1)) return SLED_ERR_ARG;
   if (kv->n_pages < 1 || kv->n_kv_heads < 1 || kv->n_kv_heads > 65535) return SLED_ERR_ARG;
   if (kv->n_reqs < 0 || kv->n_reqs > 65535 || kv->table_cols < 0 || kv->table_stride < kv->table_cols) return SLED_ERR_ARG;
+  // arrays without entries need no address
+  if ((kv->n_reqs > 0 && !kv->n_kv) || (kv->n_reqs > 0 && kv->table_cols > 0 && !kv->page_table)) return SLED_ERR_ARG;
   if (kv->n_layers > 65535) return SLED_ERR_ARG;
   if (!aligned(kv->k, 16) || (kv->v && !aligned(kv->v, 16)) || !aligned(kv->page_table, 4) || !aligned(kv->n_kv, 4)) return SLED_ERR_ARG;
   // rows of one layer, and keys of one request (rounded up to tiles), are counted in 32 bits

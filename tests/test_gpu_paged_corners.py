@@ -176,10 +176,30 @@ def test_choice_of_queries_that_are_no_numbers(dtype, h, what):
     _check_choice(q, x, 2, h, dtype)
 
 
+# -------------------------------------------------------------------------------------------------- arguments, batches
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_batches_of_nothing(dtype):
+    k, v = (torch.zeros(4, 2, 16, 64, dtype=dtype, device="cuda") for _ in range(2))
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")
+    status, w, bounds = ints(1), torch.ones(4, 2, 16, device="cuda"), torch.ones(4, 2, 2, 64, dtype=dtype, device="cuda")
+    # no requests; requests without keys and a table without columns
+    for table, n_kv, cu in ((ints(0, 5), ints(0), ints(1)), (ints(0, 0), ints(0), ints(1)), (ints(3, 0), ints(3), ints(4))):
+        for rows in (0, 2):
+            q = torch.zeros(rows, 8, 64, dtype=dtype, device="cuda")
+            out = torch.full_like(q, 5.0)
+            B.attention_tree(q, k, v, table, n_kv, cu, out=out, key_weights=w, status=status)
+            B.attention_blocks(q, k, v, bounds, table, n_kv, cu, n_blocks=4, out=out, status=status)
+            assert bool((out == 5).all())
+        B.evict_keys(k, v, w, table, n_kv, 8, n_recent=2, status=status)
+        B.block_bounds(k, table, n_kv, bounds, status=status)
+    B.check_status(status)
+    assert bool((w == 1).all()) and bool((bounds == 1).all())
+
+
 @pytest.mark.parametrize("n,group", [(300000, 1), (3000, 4)])
 def test_long_chains_with_values_that_are_no_numbers(n, group):
     """A whole prompt as one chain: a value that is no number reaches the rows behind it, and takes the others no time to
-    go round (in the long one every wait of the kernel would run out otherwise)."""
+    go round (in the long one a wait of the kernel would run out otherwise)."""
     h, page = 128, 256
     k, v, table, n_kv = R.make_cache([n], 1, h, BF, page, seed=7)
     for x, d, what in ((20, 3, NAN), (n // 2, 70, INF), (n - 2, 90, -INF)):
