@@ -532,14 +532,21 @@ def _refuse(what: str, why: str):
 
 
 def _ints(t, what: str, name: str, dev, shape=None):
-    """A CUDA int32 tensor that is contiguous along its last dimension; returns its address (0 for None)."""
+    """A CUDA int32 tensor that is contiguous along its last dimension, if it has any; returns its address (0 for None)."""
     if t is None:
         return 0
-    if t.dtype is not _I32 or t.get_device() != dev or (t.stride(-1) != 1 and t.numel() > 1):
+    if t.dtype is not _I32 or t.get_device() != dev or (t.dim() and t.size(-1) > 1 and t.stride(-1) != 1):
         _refuse(what, f"{name} must be an int32 tensor on cuda:{dev}, contiguous along its last dimension")
     if shape is not None and t.shape != shape:
         _refuse(what, f"{name} must have shape {shape}")
     return t.data_ptr()
+
+
+def _status(t, what: str, dev):
+    """The one word that receives what the kernels find wrong; returns its address (0 for None)."""
+    if t is not None and not t.numel():
+        _refuse(what, "status must have an entry")
+    return _ints(t, what, "status", dev)
 
 
 def _floats(t, what: str, name: str, dev, shape):
@@ -632,7 +639,7 @@ def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: floa
     _check(lib().sled_attention_tree(
         kv, q.data_ptr(), q_stride, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
         scale, out.data_ptr(), out_stride, _floats(lse, what, "lse", dev, (rows, heads)),
-        _floats(key_weights, what, "key_weights", dev, k.shape[:3]), _ints(status, what, "status", dev),
+        _floats(key_weights, what, "key_weights", dev, k.shape[:3]), _status(status, what, dev),
         ws, ws_bytes, _stream_of(dev)), what)
     return out
 
@@ -649,7 +656,7 @@ def evict_keys(k, v, key_weights, page_table, n_kv, budget: int, *, n_sink: int 
     _held, ws, ws_bytes = _workspace(what, dev, kv)
     w = _floats(key_weights, what, "key_weights", dev, k.shape[:-1])
     w_out = _floats(key_weights_out, what, "key_weights_out", dev, k.shape[:-1]) or w
-    _check(lib().sled_evict_keys(kv, w, w_out, budget, n_sink, n_recent, _ints(status, what, "status", dev),
+    _check(lib().sled_evict_keys(kv, w, w_out, budget, n_sink, n_recent, _status(status, what, dev),
                                  ws, ws_bytes, _stream_of(dev)), what)
 
 
@@ -661,7 +668,7 @@ def block_bounds(k, page_table, n_kv, bounds, *, first=None, status=None) -> Non
     dev = k.get_device()
     _check_bounds(what, bounds, k)
     _check(lib().sled_block_bounds(kv, _ints(first, what, "first", dev, (kv.n_reqs,)), bounds.data_ptr(),
-                                   _ints(status, what, "status", dev), _stream_of(dev)), what)
+                                   _status(status, what, dev), _stream_of(dev)), what)
 
 
 def _check_bounds(what: str, bounds, k) -> None:
@@ -686,7 +693,7 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
     _check(lib().sled_attention_blocks(
         kv, bounds.data_ptr(), q.data_ptr(), q_stride, _ints(cu_q, what, "cu_q", dev), rows, heads, scale, n_blocks, n_local,
         out.data_ptr(), out_stride, _ints(blocks, what, "blocks", dev, (rows, kv.n_kv_heads, n_blocks)),
-        _ints(status, what, "status", dev), ws, ws_bytes,
+        _status(status, what, dev), ws, ws_bytes,
         _stream_of(dev)), what)
     return out
 

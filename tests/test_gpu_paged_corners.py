@@ -196,6 +196,28 @@ def test_batches_of_nothing(dtype):
     assert bool((w == 1).all()) and bool((bounds == 1).all())
 
 
+def test_integers_of_any_shape_that_can_be_read():
+    k, v, table, n_kv = (t.cuda() for t in R.make_cache([12, 9], 2, 64, BF, seed=1))
+    q = _queries([1, 1], 8, 64, BF, 2).cuda()
+    want = B.attention_tree(q, k, v, table, n_kv, _cu([1, 1]))
+    assert table.shape[1] == 1
+    tall = torch.stack([table[:, 0], table[:, 0] + 1000], 0).t()[:, :1]          # one column, whose stride says nothing
+    assert tall.stride() == (1, 2)
+    status = torch.zeros((), dtype=torch.int32, device="cuda")
+    assert torch.equal(B.attention_tree(q, k, v, tall, n_kv, _cu([1, 1]), status=status), want)
+    B.check_status(status)
+    n_kv[0] = 17
+    B.attention_tree(q, k, v, table, n_kv, _cu([1, 1]), status=status)
+    with pytest.raises(B.SledError):
+        B.check_status(status)
+    for wrong in (torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros((), dtype=torch.int64, device="cuda")):
+        with pytest.raises(B.SledError):
+            B.attention_tree(q, k, v, table, n_kv, _cu([1, 1]), status=wrong)
+    with pytest.raises(B.SledError):
+        B.block_bounds(k, table, n_kv, torch.zeros(k.shape[0], 2, 2, 64, dtype=BF, device="cuda"),
+                       first=torch.zeros((), dtype=torch.int32, device="cuda"))
+
+
 @pytest.mark.parametrize("n,group", [(300000, 1), (3000, 4)])
 def test_long_chains_with_values_that_are_no_numbers(n, group):
     """A whole prompt as one chain: a value that is no number reaches the rows behind it, and takes the others no time to
