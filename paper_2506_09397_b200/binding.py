@@ -542,6 +542,13 @@ def _ints(t, what: str, name: str, dev, shape=None):
     return t.data_ptr()
 
 
+def _in_32_bits(what: str, **numbers):
+    """Numbers that C takes in 32 bits: a larger one would arrive as another."""
+    for name, x in numbers.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            _refuse(what, f"{name} must be below 2^31")
+
+
 def _status(t, what: str, dev):
     """The one word that receives what the kernels find wrong; returns its address (0 for None)."""
     if t is not None and not t.numel():
@@ -651,6 +658,7 @@ def evict_keys(k, v, key_weights, page_table, n_kv, budget: int, *, n_sink: int 
     the first dimension), changed in place; key_weights [n_layers, n_pages, n_kv_heads, page_size] fp32, changed in place
     unless key_weights_out is given.  The caller goes on with min(n_kv, budget) keys."""
     what = "sled_evict_keys"
+    _in_32_bits(what, budget=budget, n_sink=n_sink, n_recent=n_recent)
     kv = _paged(what, k, v, page_table, n_kv, layers=True)
     dev = k.get_device()
     _held, ws, ws_bytes = _workspace(what, dev, kv)
@@ -683,6 +691,7 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
     n_blocks - n_local earlier ones of largest score for the query.  bounds as block_bounds leaves them; blocks (optional)
     [rows, n_kv_heads, n_blocks] int32 receives what was read.  Enqueued on torch's current stream; returns out."""
     what = "sled_attention_blocks"
+    _in_32_bits(what, n_blocks=n_blocks, n_local=n_local)
     kv = _paged(what, k, v, page_table, n_kv)
     dev = k.get_device()
     _check_bounds(what, bounds, k)
