@@ -5,6 +5,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 namespace sled {
@@ -60,8 +61,18 @@ int launch_paged_tc(const PagedCache& c, const PagedRows& r, char* ws, cudaStrea
 int launch_paged_weigh(const PagedCache& c, const PagedRows& r, float* key_weights, cudaStream_t s);
 // joins the partial results of units of unit_rows rows that were cut over `blocks` shares; desc: two words of 16 bytes a share
 int launch_paged_merge(const PagedCache& c, const PagedRows& r, int unit_rows, int blocks, float* acc, float* ml, int4* desc, cudaStream_t s);
-// the number of SMs of the current device, or a negative value
+// the current device and the number of its SMs, or a negative value
+constexpr int kMaxDevices = 64;
 int paged_device(int* sms);
+// Lets a kernel use so much dynamic shared memory, once per device; done[kMaxDevices]: what has been set.  Host threads that
+// meet here set it twice, which does no harm.
+template <typename Kernel>
+bool allow_shared(Kernel kernel, int bytes, int dev, std::atomic<bool>* done) {
+  if (done[dev].load(std::memory_order_relaxed)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  done[dev].store(true, std::memory_order_relaxed);
+  return true;
+}
 // bounds[page][Hkv][2][h] of the pages that hold the keys first[i] .. n_kv[i]-1 (first null: all keys)
 int launch_block_bounds(const PagedCache& c, const int32_t* first, void* bounds, cudaStream_t s);
 // the blocks of every (row, KV head), ascending, into list [T][Hkv][n_blocks]; scores: room for [T][Hkv][table_cols]

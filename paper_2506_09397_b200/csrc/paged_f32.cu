@@ -337,20 +337,16 @@ __global__ void __launch_bounds__(32 * kWarps) paged_f32_kernel(const PagedCache
   });
 }
 
-constexpr int kMaxDevices = 64;
 constexpr int kPerSm = 4;                     // blocks at most
 constexpr int kMaxShares = kMaxPagedBlocks / 2 * kPerSm * kWarps;
 
 template <int H>
 int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s) {
-  static bool configured[kMaxDevices] = {};
+  static std::atomic<bool> configured[kMaxDevices] = {};
   int sms = 0;
   const int dev = paged_device(&sms);
   if (dev < 0) return -1;
-  if (!configured[dev]) {
-    if (cudaFuncSetAttribute(paged_f32_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, F32<H>::kBytes) != cudaSuccess) return -1;
-    configured[dev] = true;
-  }
+  if (!allow_shared(paged_f32_kernel<H>, F32<H>::kBytes, dev, configured)) return -1;
   constexpr int kResident = std::min(kPerSm, 227 * 1024 / (F32<H>::kBytes + 1024));   // as many as shared memory holds
   const int blocks = min(kResident * sms, kMaxShares / kWarps);
   F32Parts parts;

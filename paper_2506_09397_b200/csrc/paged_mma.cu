@@ -604,20 +604,18 @@ __global__ void __launch_bounds__(512) paged_merge_kernel(const PagedCache c, co
   }
 }
 
-constexpr int kMaxDevices = 64;
-
 }  // namespace
 
 int paged_device(int* sms) {   // asked for once per device
-  static int known[kMaxDevices] = {};
+  static std::atomic<int> known[kMaxDevices] = {};   // by any host thread
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return -1;
-  if (!known[dev]) {
-    int n = 0;
+  int n = known[dev].load(std::memory_order_relaxed);
+  if (!n) {
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return -1;
-    known[dev] = n;
+    known[dev].store(n, std::memory_order_relaxed);
   }
-  *sms = known[dev];
+  *sms = n;
   return dev;
 }
 
@@ -625,14 +623,11 @@ namespace {
 
 template <int H>
 int launch_h(const PagedCache& c, const PagedRows& r, const int32_t* list, int list_len, float* scores, char* ws, cudaStream_t s) {
-  static bool configured[kMaxDevices] = {};
+  static std::atomic<bool> configured[kMaxDevices] = {};
   int sms = 0;
   const int dev = paged_device(&sms);
   if (dev < 0) return -1;
-  if (!configured[dev]) {
-    if (cudaFuncSetAttribute(paged_mma_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<H>::kTotal) != cudaSuccess) return -1;
-    configured[dev] = true;
-  }
+  if (!allow_shared(paged_mma_kernel<H>, Smem<H>::kTotal, dev, configured)) return -1;
   CUtensorMap map_k, map_v;
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps;
   constexpr int kPerRow = H == 32 ? 2 : 1;      // keys of a row of the map

@@ -595,18 +595,13 @@ __global__ void __launch_bounds__(384, 1) paged_tc_kernel(const PagedCache c, co
   if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-constexpr int kMaxDevices = 64;
-
 template <int H, int kGroups>
 int launch_h(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) {
-  static bool configured[kMaxDevices] = {};
+  static std::atomic<bool> configured[kMaxDevices] = {};
   int sms = 0;
   const int dev = paged_device(&sms);
   if (dev < 0) return -1;
-  if (!configured[dev]) {
-    if (cudaFuncSetAttribute(paged_tc_kernel<H, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tc<H, kGroups>::kTotal) != cudaSuccess) return -1;
-    configured[dev] = true;
-  }
+  if (!allow_shared(paged_tc_kernel<H, kGroups>, Tc<H, kGroups>::kTotal, dev, configured)) return -1;
   CUtensorMap map_q, map_k, map_v;
   if (tma_map_bf16_heads(&map_q, r.q, r.T, r.Hq, H, r.q_stride, r.group, kGroupRows / (r.group))) return -1;
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps;

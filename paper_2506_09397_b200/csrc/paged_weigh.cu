@@ -296,18 +296,13 @@ __global__ void __launch_bounds__(320, 1) paged_weigh_kernel(const PagedCache c,
   if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-constexpr int kMaxDevices = 64;
-
 template <int H>
 int launch_h(const PagedCache& c, const PagedRows& r, float* key_weights, cudaStream_t s) {
-  static bool configured[kMaxDevices] = {};
+  static std::atomic<bool> configured[kMaxDevices] = {};
   int sms = 0;
   const int dev = paged_device(&sms);
   if (dev < 0) return -1;
-  if (!configured[dev]) {
-    if (cudaFuncSetAttribute(paged_weigh_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, Wg<H>::kTotal) != cudaSuccess) return -1;
-    configured[dev] = true;
-  }
+  if (!allow_shared(paged_weigh_kernel<H>, Wg<H>::kTotal, dev, configured)) return -1;
   CUtensorMap map_q, map_k;
   const int group = r.group;
   if (tma_map_bf16_heads(&map_q, r.q, r.T, r.Hq, H, r.q_stride, group, 128 / group)) return -1;

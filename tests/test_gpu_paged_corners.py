@@ -1,6 +1,7 @@
 """Operators over a paged cache where numbers, lengths or tables are unusual, against the 64-bit statements of tests/paged_ref.py."""
 import math
 import random
+import threading
 
 import paged_ref as R
 import pytest
@@ -240,3 +241,48 @@ def test_long_chains_with_values_that_are_no_numbers(n, group):
                 o[..., d] = what
         _close(out[j:j + 1].cpu().double(), o, d_o)
         _close(lse[j:j + 1].cpu().double(), l, d_l)
+
+
+def test_calls_from_two_host_threads():
+    """Each thread on a stream of its own, from the process's first calls of these shapes on."""
+    sets = []
+    for seed, (hq, h, dtype, m) in enumerate([(8, 128, BF, 3), (8, 64, BF, 40), (4, 32, F32, 5), (8, 128, F32, 2)]):
+        lens, q_len = [500, 90], [m, m]
+        k, v, table, n_kv = (t.cuda() for t in R.make_cache(lens, 2, h, dtype, seed=seed, garbage=0.0))
+        q = _queries(q_len, hq, h, dtype, seed).cuda()
+        bounds = torch.zeros(k.shape[0], 2, 2, h, dtype=dtype, device="cuda")
+        sets.append((q, k, v, table, n_kv, _cu(q_len), bounds))
+    torch.cuda.synchronize()
+
+    def calls(s):
+        q, k, v, table, n_kv, cu, bounds = s
+        w, mine = torch.zeros(k.shape[:3], device="cuda"), torch.zeros_like(bounds)
+        a = B.attention_tree(q, k, v, table, n_kv, cu, key_weights=w)
+        B.block_bounds(k, table, n_kv, mine)
+        b = B.attention_blocks(q, k, v, mine, table, n_kv, cu, n_blocks=5)
+        kk, vv, ww = k.clone(), v.clone(), w.clone()
+        B.evict_keys(kk, vv, ww, table, n_kv, 60, n_recent=8)
+        return a, w, mine, b, kk, vv, ww
+
+    got, wrong, start = {}, [], threading.Barrier(2)
+
+    def run(name):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                start.wait()
+                got[name] = [[calls(s) for s in sets] for _ in range(10)]
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:      # noqa: BLE001 - the main thread reports it
+            wrong.append(e)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+    want = [calls(s) for s in sets]
+    for rounds in got.values():
+        for results in rounds:
+            for x, y in zip(results, want):
+                assert all(torch.equal(a, b) for a, b in zip(x, y))
