@@ -104,6 +104,71 @@ def test_a_row_that_is_no_number_weighs_only_on_the_keys_it_sees(dtype, hq, m, c
     _check_call(R.make_cache(lens, 2, 64, dtype, seed=2), q, lens, q_len, parents, columns=columns)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_weights_of_trees_where_the_scores_are_too_many_to_keep(dtype):
+    lens, q_len = [100, 37, 16], [9, 5, 1]
+    _check_call(R.make_cache(lens, 2, 64, dtype, seed=6), _queries(q_len, 8, 64, dtype, 7), lens, q_len,
+                [[-1, 0, 0, -2, 3, 1, 5, -1, 7], [-1, 0, 1, 0, 3], [-1]], columns=300000)
+
+
+# --------------------------------------------------------------------------------- units of 256 rows (paged_tc_kernel<H, 2>)
+def _wide_columns(q_len, group, hkv, page=16):
+    """Columns of a page table with which a call takes the kernel of 256-row units: 32 of its tiles to an SM."""
+    rows = sum(q_len) * group // len(q_len)
+    assert rows > 128
+    tiles = 32 * torch.cuda.get_device_properties(0).multi_processor_count
+    units = (rows + 127) // 256 * len(q_len) * hkv
+    return ((tiles + units - 1) // units * 128 + page - 1) // page
+
+
+@pytest.mark.parametrize("h", [64, 128])
+@pytest.mark.parametrize("lens,q_len", [([129, 300], [129, 130]), ([255, 1000, 400], [255, 1, 200]), ([256, 700], [256, 12]),
+                                        ([257, 600, 90], [257, 128, 64]), ([512, 2000], [512, 3]), ([5000, 513, 30], [300, 513, 1])])
+def test_units_of_256_rows_chains(lens, q_len, h):
+    _check_call(R.make_cache(lens, 2, h, BF, seed=1), _queries(q_len, 2, h, BF, 2), lens, q_len, columns=_wide_columns(q_len, 1, 2))
+
+
+@pytest.mark.parametrize("h", [64, 128])
+@pytest.mark.parametrize("hq", [8, 16])
+def test_units_of_256_rows_trees(hq, h):
+    """Requests on both sides of 128 and 256 rows, unused nodes, contexts that are cut into many shares."""
+    rng = random.Random(hq + h)
+    lens, q_len = [64, 300, 128, 90, 4000, 517, 33, 1500], [64, 65, 128, 3, 100, 32, 33, 127]
+    parents = [_tree(rng, m, True) for m in q_len]
+    for p in (parents[0], parents[2], parents[4], parents[7]):
+        p[rng.randrange(len(p))] = -2
+    parents[6] = [-2] * 33
+    _check_call(R.make_cache(lens, 2, h, BF, seed=3), _queries(q_len, hq, h, BF, 4), lens, q_len, parents,
+                columns=_wide_columns(q_len, hq // 2, 2))
+
+
+@pytest.mark.parametrize("what", [NAN, INF, -INF])
+@pytest.mark.parametrize("h", [64, 128])
+@pytest.mark.parametrize("wide", [False, True])
+def test_values_of_nodes_that_are_no_numbers(h, what, wide):
+    """They reach the rows that see them and no others, in units of 128 and of 256 rows, whole and cut ones."""
+    rng = random.Random(9)
+    lens, q_len = [64, 300, 2500, 40], [64, 65, 100, 3]
+    parents = [_tree(rng, m, True) for m in q_len]
+    cache = R.make_cache(lens, 2, h, BF, seed=3)
+    for i, j in ((0, 20), (1, 0), (1, 64), (2, 50), (3, 1)):
+        x = lens[i] - q_len[i] + j
+        cache[1][cache[2][i, x // 16], j % 2, x % 16, 5 + j % h // 2] = what
+    x = lens[1] - q_len[1] - 2                              # and one of the keys that everybody sees, in a tile with nodes
+    cache[1][cache[2][1, x // 16], 1, x % 16, h - 1] = what
+    _check_call(cache, _queries(q_len, 8, h, BF, 4), lens, q_len, parents, columns=_wide_columns(q_len, 4, 2) if wide else 0)
+
+
+@pytest.mark.parametrize("h", [64, 128])
+def test_requests_on_both_sides_of_128_rows(h):
+    """Small requests among large ones, 128 rows or less on average: the narrow kernel, with units of full and of few rows."""
+    rng = random.Random(h + 1)
+    q_len = [rng.choice([8] * 6 + [64, 33, 128]) for _ in range(40)]
+    lens = [rng.randint(m, 2500) for m in q_len]
+    assert 24 < sum(q_len) * 4 / 40 <= 128 and max(q_len) == 128
+    _check_call(R.make_cache(lens, 2, h, BF, seed=5), _queries(q_len, 8, h, BF, 6), lens, q_len, [_tree(rng, m, True) for m in q_len])
+
+
 # ------------------------------------------------------------------------------------------------------- bounds, choice
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_bounds_without_new_keys_are_left_alone(dtype):
@@ -177,6 +242,30 @@ def test_choice_of_queries_that_are_no_numbers(dtype, h, what):
     _check_choice(q, x, 2, h, dtype)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_choice_among_more_blocks_than_stay_in_shared_memory(dtype):
+    lens, hkv, h = [70000], 1, 64
+    k, v, table, n_kv = (t.cuda() for t in R.make_cache(lens, hkv, h, dtype, garbage=0.0))
+    q = _queries([1], 2, h, dtype, 1).cuda()
+    bounds = torch.ones(k.shape[0], hkv, 2, h, dtype=dtype, device="cuda")
+    own = (70000 - 1) // 16
+    for n_blocks, better in ((4110, []), (4110, [4300, 4350]), (30, [10, 4095, 4096, 4097, 4371]), (4000, [4100])):
+        b = bounds.clone()
+        for x in better:                                    # every score term of these is at least as large
+            b[table[0, x].long(), :, 0], b[table[0, x].long(), :, 1] = -2.0, 2.0
+        blocks = torch.full((1, hkv, n_blocks), -1, dtype=torch.int32, device="cuda")
+        out = B.attention_blocks(q, k, v, b, table, n_kv, _cu([1]), n_blocks=n_blocks, n_local=2, blocks=blocks)
+        equal = [x for x in range(own - 1) if x not in better][:n_blocks - 2 - len(better)]
+        want = sorted(equal + better) + [own - 1, own]
+        assert blocks[0, 0].tolist() == want
+        kk, vv = (R.keys_of(x.cpu(), table[0].cpu(), 70000, 16) for x in (k, v))
+        see = torch.zeros(1, hkv, 70000, dtype=torch.bool)
+        for x in want:
+            see[..., x * 16:(x + 1) * 16] = True
+        o, _, _, d_o, _, _ = R.attend(q.cpu(), kk, vv, see, h ** -0.5, dtype)
+        _close(out.cpu().double(), o, d_o)
+
+
 # -------------------------------------------------------------------------------------------------- arguments, batches
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_batches_of_nothing(dtype):
@@ -217,6 +306,23 @@ def test_integers_of_any_shape_that_can_be_read():
     with pytest.raises(B.SledError):
         B.block_bounds(k, table, n_kv, torch.zeros(k.shape[0], 2, 2, 64, dtype=BF, device="cuda"),
                        first=torch.zeros((), dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_requests_in_another_order(dtype):
+    rng = random.Random(8)
+    lens, q_len, parents = [500, 3000, 90, 64], [6, 9, 3, 30], None
+    parents = [_tree(rng, m) for m in q_len]
+    k, v, table, n_kv = R.make_cache(lens, 2, 128, dtype, seed=4)
+    q = _queries(q_len, 8, 128, dtype, 5)
+    rows, at = [], 0
+    for m in q_len:
+        rows.append(list(range(at, at + m)))
+        at += m
+    _check_call((k, v, table, n_kv), q, lens, q_len, parents)
+    for order in ([3, 1, 0, 2], [1, 2, 3, 0]):
+        pick = lambda x: [x[i] for i in order]
+        _check_call((k, v, table[order], n_kv[order]), q[sum(pick(rows), [])], pick(lens), pick(q_len), pick(parents))
 
 
 @pytest.mark.parametrize("n,group", [(300000, 1), (3000, 4)])
