@@ -392,3 +392,18 @@ def test_calls_from_two_host_threads():
         for results in rounds:
             for x, y in zip(results, want):
                 assert all(torch.equal(a, b) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("hq,m,columns", PATHS + [(8, 70, 0)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("chain", [False, True])
+def test_keys_that_are_no_numbers_and_weights(dtype, hq, m, columns, chain):
+    """Rows that see such a key are no numbers, nor are the weights of the keys that those rows see; all others are untouched."""
+    rng = random.Random(m)
+    lens, q_len = [400, 90, 300], [m, m, 1]
+    parents = None if chain else [_tree(rng, m, True), _tree(rng, m), [-1]]
+    cache = R.make_cache(lens, 2, 64, dtype, seed=2)
+    for i, j, g in ((0, 2, 0), (0, m - 1, 1), (1, m - 2, 0)):
+        x = lens[i] - m + j
+        cache[0][cache[2][i, x // 16], g, x % 16, 11] = NAN
+    _check_call(cache, _queries(q_len, hq, 64, dtype, 3), lens, q_len, parents, columns=columns)
