@@ -302,7 +302,8 @@ int sled_attention_ragged(sled_engine* e, int32_t layer, const uint64_t* ctx_ids
 /* A cache that the caller owns, in the layout of the engine's pool: K and V are [n_layers][n_pages][n_kv_heads][page_size]
  * [head_dim], contiguous, 16-byte aligned; key x of request i lies in page page_table[i][x / page_size] at slot
  * x % page_size, for every layer and KV head.  The paper leaves the cache to future work (Section 5); these operators are
- * what a server needs of it beyond the chain drafts of sled_verify_batch.
+ * what a server needs of it beyond the chain drafts of sled_verify_batch.  They serve a caller that holds its cache and runs
+ * its model itself: the pool of a sled_engine has no address outside, and its calls know chains only.
  *
  * All arrays, the request descriptions included, are DEVICE memory of one GPU; the calls enqueue their kernels on `stream`
  * (cudaStream_t or NULL for the default stream) and return without waiting, so they can be captured into a CUDA graph.
@@ -314,11 +315,17 @@ int sled_attention_ragged(sled_engine* e, int32_t layer, const uint64_t* ctx_ids
  * device-side wait that runs out, sets *status (DEVICE, one int32, may be NULL) to the sled_status if it was 0; no call
  * clears it.  Entries of a table row behind the request's
  * last page, slots behind its last key and pages of nobody are never looked at, or do not change results whatever they
- * hold.  A page belongs to at most one request, once, of a call that writes to the cache or to key_weights; out, lse and
- * key_weights share no memory with what the call reads.
+ * hold.  A page belongs to at most one request, once, of a call that writes to the cache or to key_weights (others may share
+ * pages; of a page that requests share with different numbers of keys sled_block_bounds leaves the bounds of either); out,
+ * lse and key_weights share no memory with what the call reads.  n_reqs, n_layers, n_kv_heads and n_q_heads are at most
+ * 65535; arrays without entries may be NULL.
+ * Scores, their maxima and sums, results and weights are held in fp32; over a bf16 cache the softmax's numerators are rounded
+ * to bf16 before they meet V (their sum is not), one rounding of at most 2^-8 of each.
  * workspace: at least the bytes that the call's _workspace function names, 256-byte aligned, used from the call until its
  * kernels have run: calls (or captured graphs) that may run at the same time need a workspace each.  It need not be
- * cleared and nothing in it outlives the call. */
+ * cleared and nothing in it outlives the call.  Its size goes by table_cols * page_size, and so does how the weights of keys
+ * are formed: scores of all rows over so many keys are kept up to 512 MiB, beyond that they are formed anew key by key, which
+ * takes many times as long.  A table should be about as wide as its longest request. */
 #define SLED_MAX_TREE_NODES 128
 typedef struct sled_paged_kv {
   void* k;
@@ -366,14 +373,15 @@ int sled_evict_keys(const sled_paged_kv* kv, float* key_weights, float* key_weig
 
 /* Smallest and largest key of every block (page), per KV head and dimension: bounds [n_pages][n_kv_heads][2][head_dim] of
  * the cache's type, 16-byte aligned.  Written for the blocks that hold any of request i's keys first[i] .. n_kv[i]-1 (first
- * NULL: all); a NaN among the keys gives NaN. */
+ * NULL: all; none where first[i] >= n_kv[i]); a NaN among the keys gives NaN. */
 int sled_block_bounds(const sled_paged_kv* kv, const int32_t* first, void* bounds, int32_t* status, void* stream);
 
 /* Attention over the blocks that a cheap score selects for each query.  Chains as in sled_attention_tree without parents:
  * row j of request i is the key x = n_kv[i] - q_len + j and sees no key behind it.  It reads the n_local blocks that end
  * with its own and, of the earlier ones, the n_blocks - n_local of largest score - the largest, over the heads that share
  * the KV head, of sum_d max(q_d low_d, q_d high_d), which no q.k of the block exceeds - the lower block among equals, a
- * NaN being the largest.  Where there are no more than n_blocks blocks the result is that of full attention.
+ * NaN being the largest.  Scores are fp32 sums: blocks whose scores are nearer than their rounding may change places.
+ * Where there are no more than n_blocks blocks the result is that of full attention.
  *   bounds  as sled_block_bounds leaves them, for every block before a query's last n_local
  *   1 <= n_local <= n_blocks
  *   blocks  may be NULL; [n_rows][n_kv_heads][n_blocks]: the blocks that were read, ascending; entries behind a row's own

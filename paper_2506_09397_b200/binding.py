@@ -637,7 +637,8 @@ def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: floa
     cache.  q [rows, n_q_heads, head_dim]; k, v [n_pages, n_kv_heads, page_size, head_dim]; page_table [n_reqs, cols],
     n_kv [n_reqs], cu_q [n_reqs + 1], parents [rows] int32 (None: chains).  Optional outputs: lse [rows, n_q_heads] fp32;
     key_weights [n_pages, n_kv_heads, page_size] fp32, added to.  status: one int32 that receives what the kernels found
-    wrong (see check_status).  Enqueued on torch's current stream; returns out."""
+    wrong (see check_status).  Enqueued on torch's current stream; returns out.  Rows that belong to no request, or to one that is
+    left out, are not written: in an `out` that the call makes itself they hold nothing that means anything."""
     what = "sled_attention_tree"
     kv = _paged(what, k, v, page_table, n_kv)
     dev = k.get_device()
@@ -689,7 +690,8 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
                      blocks=None, status=None):
     """sled_attention_blocks: causal attention of every request's newest keys over the n_local last blocks (pages) and the
     n_blocks - n_local earlier ones of largest score for the query.  bounds as block_bounds leaves them; blocks (optional)
-    [rows, n_kv_heads, n_blocks] int32 receives what was read.  Enqueued on torch's current stream; returns out."""
+    [rows, n_kv_heads, n_blocks] int32 receives what was read.  Enqueued on torch's current stream; returns out (rows of no
+    request: as in attention_tree)."""
     what = "sled_attention_blocks"
     _in_32_bits(what, n_blocks=n_blocks, n_local=n_local)
     kv = _paged(what, k, v, page_table, n_kv)

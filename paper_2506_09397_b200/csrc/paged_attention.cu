@@ -115,9 +115,13 @@ __global__ void __launch_bounds__(256) key_weight_sum_kernel(PagedCache c, Paged
   });
 }
 
-// Rows per request and KV head (on average) above which the tcgen05 kernels are used.  8 contexts of 8192 keys, 8 KV heads
-// of 128: 24 rows 63 us on the warp-level tensor cores and 69 on tcgen05, 32 rows 64 and 69, 36 rows 86 and 71 (with weights
-// 104 and 112, 114 and 112, 166 and 118); one context of 1000 keys: 16.4 and 15.6, 17.6 and 15.8, 21.1 and 15.8.
+// Rows per request and KV head (on average) above which the tcgen05 kernels are used.  Warp-level tensor cores and tcgen05,
+// us, 8 KV heads of 128, in brackets with weights:
+//   rows                       24                     28                     32                     36
+//   8 contexts of 8192 keys    59 67 (104 109)        61 68 (110 109)        60 69 (118 109)        82 70 (168 116)
+//   one of 1000                15.1 15.5 (25 28)      15.5 15.6 (25 28)      15.9 15.7 (26 27)      19.4 15.9 (31 31)
+//   32 of 128 .. 16384         113 117 (214 236)      114 117 (230 236)      116 118 (239 236)      185 122 (2600 298: scores not kept)
+// So up to 32 rows calls without weights over long contexts give away up to 9 us, and those with weights gain as much.
 constexpr int kTcRows = 24;
 int64_t parts_bytes(int dtype, int h) {
   const int64_t a = dtype == 1 ? paged_mma_workspace(h) : paged_f32_workspace(h), b = dtype == 1 && h >= 64 ? paged_tc_workspace(h) : 0;
@@ -126,7 +130,8 @@ int64_t parts_bytes(int dtype, int h) {
 
 // With few rows the scores are kept for the weights, 4 bytes per row and key, where they take no more than this; otherwise
 // the weights are computed from the keys again, which takes a small part of the memory and many times as long (8 contexts
-// of 8192 keys, one token: 68 us and 216; four tokens: 79 and 589).
+// of 8192 keys, one token: 65 us and 215; four tokens: 78 and 585).  The host knows the width of the page table, not the
+// keys: 33 contexts of 2000 keys, one token, take 67 us with a table of 125 columns and 1170 with one of 8192.
 constexpr int64_t kMostScoreBytes = 512LL << 20;
 bool keeps_scores(int64_t rows_heads, int64_t keys) { return keys == 0 || rows_heads <= kMostScoreBytes / 4 / keys; }
 

@@ -59,7 +59,7 @@ template <> struct Vec<__nv_bfloat16> {
 };
 
 // A warp per (block, KV head): the lanes take 16 bytes each, kRows rows at a time, four such loads under way; every key is
-// read once, which is what bounds it: 24 prompts of 2000 .. 16384 keys, 8 KV heads of 128, 65 us, 87 % of the copy rate, with
+// read once, which is what bounds it: 24 prompts of 2000 .. 16384 keys, 8 KV heads of 128, 65 us, 88 % of the copy rate, with
 // four blocks an SM (two 85 us, six 74, eight 68).
 template <typename T, int H>
 __global__ void __launch_bounds__(256) block_bounds_kernel(PagedCache c, const int32_t* first, T* bounds) {
@@ -363,8 +363,8 @@ template <typename T, int H>
 int choice_typed(const PagedCache& c, const PagedRows& r, const void* bounds, int n_blocks, int n_local, float* scores, int32_t* list, cudaStream_t s) {
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
-  // few choices among many blocks: a large block each; many choices share an SM (a whole call, one token of 30000 keys: 26 us,
-  // with 256 threads 37; 109 tokens of 24 contexts: 151 us, with 1024 threads 159)
+  // few choices among many blocks: a large block each; many choices share an SM (a whole call, one token of 30000 keys: 27 us,
+  // with 256 threads 36; 109 tokens of 24 contexts: 154 us, with 1024 threads 162)
   const int threads = c.table_cols > 512 && static_cast<int64_t>(r.T) * c.Hkv <= 2 * sms ? 1024 : 256;
   if constexpr (sizeof(T) == 2 && H >= 64) {
     if (r.group <= kScoreRows) {

@@ -18,7 +18,7 @@ constexpr int kMostCached = 8192;    // keys whose ranks stay in shared memory
 // One block per (KV head, request, layer).  The weights are read once (their order-preserving bits stay in shared memory),
 // the edge of the choice is found digit by digit, every thread then goes through a stretch of slots and writes down the
 // holes and the keys that fill them; the rest is copying, 16 bytes a thread, four rows under way.  Bound by the rows that move: 32 layers of 8
-// contexts of 1500 .. 6000 keys down to 2048, 8 KV heads of 128, 303 us, 4.8 TB/s read and written (256 threads 349 us, 1024
+// contexts of 1500 .. 6000 keys down to 2048, 8 KV heads of 128, 306 us, 4.7 TB/s read and written (256 threads 349 us, 1024
 // 311); one layer's worth of 16 KB in 11 us is launch, selection and latency.
 __global__ void __launch_bounds__(kThreads) evict_kernel(PagedCache c, const float* weights, float* weights_out, int64_t weight_layer, int budget,
                                                          int n_sink, int n_recent, int32_t* pairs, int row_words) {

@@ -18,8 +18,10 @@
 // The work is shared out as paged_schedule.cuh says.  What binds: a unit's begin and end (about 20,000 cycles) where units
 // have few tiles; in long ones the bytes of K and V up to about 64 rows, then the products, which one thread issues in
 // order (a 128 x 128 x 16 step takes about 100 cycles of the second and 64 of the first).  Measured, 8 KV heads of 128, 4
-// contexts of 32768 keys: 120 rows 128 us, 4.2 TB/s; 256 rows 178 us, 770 TFLOP/s; 512 rows 312 us, 880 TFLOP/s.  Every wait is bounded; when one runs out the block says so in *status, lets what is under
-// way land, frees its tensor memory and returns.
+// contexts of 32768 keys: 120 rows 126 us, 4.3 TB/s; 256 rows 178 us, 770 TFLOP/s; 512 rows 315 us, 870 TFLOP/s.  A row's
+// scores and what outlives a tile do not fit the 168 registers that the compiler may use: 364 - 458 bytes a thread are
+// spilled.  Every wait is bounded; when one runs out the block says so in *status, lets what is under way land, frees its
+// tensor memory and returns.
 #include "gemm_tc.h"
 #include "kernels.h"
 #include "paged_schedule.cuh"
@@ -633,8 +635,8 @@ bool paged_tc_serves(const PagedCache& c, const PagedRows& r) {
 int launch_paged_tc(const PagedCache& c, const PagedRows& r, char* ws, cudaStream_t s) {
   // Units of 256 rows where the requests have more than 128 on average and, as far as the page table allows, there are 32
   // such tiles to an SM: the keys are read once for all rows, but a unit is longer.  64 nodes of 4 heads, 8 KV heads of 128,
-  // wide and narrow: 4 contexts of 32768 keys (55 tiles to an SM) 178 and 212 us, 64 of 2048 (55) 227 and 248, 8 of 8192
-  // (28) 117 and 115, one of 1000 (0.4) 28 and 22.
+  // wide and narrow: 4 contexts of 32768 keys (55 tiles to an SM) 179 and 211 us, 64 of 2048 (55) 229 and 253, 8 of 8192
+  // (28) 118 and 118, one of 1000 (0.4) 28 and 23.
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
   const int64_t rows = static_cast<int64_t>(r.T) * r.group / c.n_reqs, keys = static_cast<int64_t>(c.table_cols) * c.ps;

@@ -8,7 +8,7 @@
 //   warp 9         : tensor-memory allocation, products (one thread)
 // A unit is (request, KV head); rows beyond 256 are gone through 256 at a time within a tile.  What binds: the bytes of K
 // (from L2 where the attention before it has left them there) up to about 128 rows, the exponentials above.  Measured, 8 KV
-// heads of 128, 4 contexts of 32768 keys: 98 us on top of the attention's 128 for 120 rows, 77 on top of 121 for 36.
+// heads of 128, 4 contexts of 32768 keys: 96 us on top of the attention's 126 for 120 rows, 78 on top of 118 for 36.
 #include "gemm_tc.h"
 #include "kernels.h"
 #include "paged_schedule.cuh"
