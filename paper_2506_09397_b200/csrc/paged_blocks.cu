@@ -287,17 +287,29 @@ __global__ void __launch_bounds__(256) block_score_row_kernel(PagedCache c, Page
     const int page = checked_page(c, c.table[static_cast<int64_t>(i) * c.table_stride + b]);
     const T* lo = bounds + (static_cast<int64_t>(page) * c.Hkv + g) * 2 * H + lane * D;
     float low[D], high[D], best = -INFINITY;
+    float zero = 0.f;                                    // a NaN where a bound is not finite
 #pragma unroll
-    for (int d = 0; d < D; ++d) { low[d] = to_f32(lo[d]); high[d] = to_f32(lo[H + d]); }
+    for (int d = 0; d < D; ++d) {
+      low[d] = to_f32(lo[d]);
+      high[d] = to_f32(lo[H + d]);
+      zero = fmaf(0.f, low[d], fmaf(0.f, high[d], zero));
+    }
     for (int hh = 0; hh < group; ++hh) {
       const T* q = reinterpret_cast<const T*>(r.q) + t * r.q_stride + static_cast<int64_t>(g * group + hh) * H + lane * D;
-      float s = 0.f;
+      float s = zero;
 #pragma unroll
       for (int d = 0; d < D; ++d) {
         const float x = to_f32(q[d]);
-        s += larger(x * low[d], x * high[d]);
+        s = fmaf(x, x < 0.f ? low[d] : high[d], s);      // the larger of the two products, where everything is finite
       }
-      best = larger(best, warp_sum(s));
+      s = warp_sum(s);
+      if (!(fabsf(s) < INFINITY)) {                      // bounds, or a query, that are not: the definition
+        s = 0.f;
+#pragma unroll
+        for (int d = 0; d < D; ++d) s += larger(to_f32(q[d]) * low[d], to_f32(q[d]) * high[d]);
+        s = warp_sum(s);
+      }
+      best = larger(best, s);
     }
     if (lane == 0) sc[b] = best;
   }
