@@ -49,7 +49,9 @@ enum sled_status {
 /* returned by sled_poll while a request is still queued (not an error) */
 #define SLED_PENDING 1
 
-enum sled_dtype { SLED_F32 = 0, SLED_BF16 = 1 };
+/* SLED_E4M3 (1 sign, 4 exponent bits with bias 7, 3 mantissa bits, subnormals, no infinities, 0x7f and 0xff no numbers) is a
+ * type of caches that sled_append_keys writes and sled_attention_scaled reads, nothing else. */
+enum sled_dtype { SLED_F32 = 0, SLED_BF16 = 1, SLED_E4M3 = 2 };
 
 /* How the server forms batches (Section 3.4).  STATIC is the paper's scheme: requests wait until a fixed number
  * of them is there.  CONTINUOUS runs whatever has arrived, up to the capacity of a step. */
@@ -391,6 +393,99 @@ int sled_attention_blocks(const sled_paged_kv* kv, const void* bounds, const voi
                           int32_t n_rows, int32_t n_q_heads, float scale, int32_t n_blocks, int32_t n_local, void* out,
                           int64_t out_stride, int32_t* blocks, int32_t* status, void* workspace, int64_t workspace_bytes,
                           void* stream);
+
+/* ---- a decoding step over a cache of one's own: places, positions, keys, attention ------------------------------- */
+
+/* What a step does with a caller's cache besides its model: sled_page_slots gives the new tokens their places,
+ * sled_rotary turns their queries and keys, sled_append_keys writes keys and values into the cache, sled_attention_tree (or,
+ * for caches in 8 bits, sled_attention_scaled) reads it.  As above: DEVICE memory of one GPU unless said otherwise, enqueued
+ * on `stream` without waiting, capturable, *status for what only the GPU sees, nothing kept from call to call. */
+
+/* Places of a step's tokens, from lengths that only the GPU knows.  Request i has n_kv[i] keys in the pages of its table row;
+ * n_keep[i] of them stay (those of rejected drafts go; n_keep NULL: all stay), n_new[i] tokens follow.  Pages that a request
+ * no longer needs go onto the stack of free pages, request by request, a request's in ascending order; then pages that
+ * requests need come off its top, request by request.  (A page belongs to one request.)
+ *   page_size    1 or more;  page_table [n_reqs] rows of table_cols entries, table_stride apart, entries written where a
+ *                request gets a page; entries of pages that went back are left as they are
+ *   free_pages   [free_cap], the first *n_free of them free, the top last.  Returned pages are written at *n_free and on;
+ *                nothing else of it is.  free_cap has to hold the free and the returned ones together
+ *   n_kv_out     [n_reqs]  n_keep + n_new
+ *   n_free_out   [1]
+ *   cu_q         [n_reqs + 1]  row offsets of the new tokens
+ *   positions    [n_rows]  n_keep[i] + j of token j of request i; may be NULL
+ *   slots        [n_rows]  page * page_size + offset within the page; may be NULL
+ *   n_rows       room for the tokens of the call; rows behind the last token get position 0 and slot -1
+ * All or nothing: where *n_free or any request's numbers do not hold together (negative, n_keep above n_kv, more keys than
+ * its table row has room for, more tokens than n_rows) - SLED_ERR_ARG - or the free pages do not suffice -
+ * SLED_ERR_NO_PAGES -, *status is set, no page moves, n_kv_out is n_kv, n_free_out is *n_free and nobody has a row.
+ * Outputs share no memory with inputs or each other: the same call can be made, or replayed, again. */
+int sled_page_slots(const int32_t* n_kv, const int32_t* n_keep, const int32_t* n_new, int32_t n_reqs, int32_t page_size,
+                    int32_t* page_table, int32_t table_stride, int32_t table_cols, int32_t* free_pages, int32_t free_cap,
+                    const int32_t* n_free, int32_t* n_kv_out, int32_t* n_free_out, int32_t* cu_q, int32_t* positions,
+                    int64_t* slots, int32_t n_rows, int32_t* status, void* stream);
+
+/* Radians per position of the pairs of rotary embeddings: f[i] = theta^(-2i/rot_dim), i < rot_dim/2, scaled for contexts
+ * longer than those of the training.  Host only, needs no device.
+ *   SLED_ROTARY_PLAIN    f
+ *   SLED_ROTARY_LINEAR   f / factor
+ *   SLED_ROTARY_BASE     theta * factor^(d/(d-2)) in theta's place (rot_dim d above 2): the lowest frequency is f / factor
+ *   SLED_ROTARY_BANDS    f (s + (1 - s) / factor), s = clamp((t - low) / (high - low), 0, 1) of the turns t = length f / 2 pi that
+ *                        the pair makes in the context length of the training; 0 <= low < high
+ *   SLED_ROTARY_RAMP     the same with s falling from 1 to 0 along the pairs' index, between the (rounded down) index of the
+ *                        pair that makes `high` turns and the (rounded up) one of `low` turns; 0 < low < high, theta above 1.
+ *                        amplitude is 0.1 ln(factor) + 1 for factor above 1
+ * factor, length above 0 (factor for all but PLAIN, length for the last two).  frequencies: HOST [rot_dim/2]; amplitude: HOST,
+ * receives what cosine and sine are multiplied by (1 but for RAMP); may be NULL. */
+enum sled_rotary_scaling { SLED_ROTARY_PLAIN = 0, SLED_ROTARY_LINEAR = 1, SLED_ROTARY_BASE = 2, SLED_ROTARY_BANDS = 3, SLED_ROTARY_RAMP = 4 };
+int sled_rotary_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double length, double low, double high,
+                            double* frequencies, double* amplitude);
+
+/* Rows of heads: element d of head g of row t lies at t * row + g * head + d.  `out` may be `in`, with the same strides;
+ * otherwise they, and the elements of out among each other, share no memory. */
+typedef struct sled_heads {
+  const void* in;
+  int64_t in_row, in_head;
+  void* out;
+  int64_t out_row, out_head;
+  int32_t n_heads;
+} sled_heads;
+
+/* Rotary positions of queries and keys.  The first rot_dim dimensions of every head are pairs - (2i, 2i+1) or the two halves
+ * (i, i + rot_dim/2) -, and pair i of row t is turned by the angle positions[t] * frequencies[i]:
+ *   (a, b) -> amplitude (a cos - b sin, a sin + b cos);  dimensions behind rot_dim are copied.
+ * transpose: the angle is taken negative, which is the gradient of the call without it (and, with amplitude 1, undoes it).
+ * Angles are formed in 64 bits, whatever the position; a pair is turned in 32 bits and rounded once.
+ *   dtype        SLED_F32 or SLED_BF16, of all of q and k;  k may be NULL
+ *   positions    [n_rows], any numbers
+ *   frequencies  [rot_dim/2] fp64
+ *   head_dim     even, at most 512; rot_dim even, 2 .. head_dim */
+enum sled_rotary_pairs { SLED_ROTARY_PAIRS = 0, SLED_ROTARY_HALVES = 1 };
+int sled_rotary(const sled_heads* q, const sled_heads* k, int32_t n_rows, int32_t head_dim, int32_t dtype, const int32_t* positions,
+                const double* frequencies, int32_t rot_dim, int32_t pairs, float amplitude, int32_t transpose, void* stream);
+
+/* New keys and values into the cache: row cu_q[i] + j of k and v is request i's key n_kv[i] - q_len + j (n_kv counts the new
+ * ones), as in the attention calls.  Rows of k and v [n_rows][n_kv_heads][head_dim], k_stride / v_stride elements apart.
+ * A cache of the rows' type (rows_dtype SLED_F32 or SLED_BF16) receives them as they are; k_scale and v_scale are then NULL.
+ * A cache in 8 bits (SLED_E4M3) holds codes and a scale for every block of 16 slots of a page and KV head, k_scale and
+ * v_scale [n_pages][n_kv_heads][page_size / 16] fp32: a key is scale * code.  The scale of a block that receives keys becomes
+ * the smallest power of two, at least 2^-126, of which 448 times is no less than any new finite element of the block or, where
+ * the block has older keys of the request, the scale that it had, if that is larger; then the older keys are coded anew.  A code is
+ * the nearest to element / scale, ties to the even one; infinities and NaN become NaN.  What a rejected draft did to a
+ * scale stays until its block is begun anew.
+ * Slots behind the last key and other pages are left as they are.  A request whose numbers do not hold together is left out, a
+ * page outside the pool is not written; *status says so. */
+#define SLED_SCALE_BLOCK 16
+int sled_append_keys(const sled_paged_kv* kv, float* k_scale, float* v_scale, const void* k, int64_t k_stride, const void* v,
+                     int64_t v_stride, int32_t rows_dtype, const int32_t* cu_q, int32_t n_rows, int32_t* status, void* stream);
+
+/* sled_attention_tree over a cache in 8 bits (kv->dtype SLED_E4M3, with its scales as in sled_append_keys: any finite
+ * numbers).  q and out are bf16; parents, lse, status and workspace as there.  Scores, their maxima and sums are held in fp32;
+ * the softmax's numerators, times their block's scale, are rounded to 16 bits before they meet V (their sum is not), one
+ * rounding of at most 2^-8 of each. */
+int sled_attention_scaled_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int64_t* bytes);
+int sled_attention_scaled(const sled_paged_kv* kv, const float* k_scale, const float* v_scale, const void* q, int64_t q_stride,
+                          const int32_t* cu_q, const int32_t* parents, int32_t n_rows, int32_t n_q_heads, float scale, void* out,
+                          int64_t out_stride, float* lse, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* ---- test and benchmark hooks ------------------------------------------------------- */
 

@@ -8,7 +8,7 @@
 
 namespace sled {
 
-enum DType { F32 = 0, BF16 = 1 };
+enum DType { F32 = 0, BF16 = 1, E4M3 = 2 };
 
 // Device addresses that receive a launch's begin / end time (see common.cuh); null members: no stamps.
 struct Stamp {

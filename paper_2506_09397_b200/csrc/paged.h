@@ -83,6 +83,57 @@ int launch_block_choice(const PagedCache& c, const PagedRows& r, const void* bou
 int launch_evict(const PagedCache& c, float* weights, float* weights_out, int64_t weight_layer, int budget, int n_sink, int n_recent,
                  int32_t* pairs, cudaStream_t s);
 
+// ---- a decoding step's other operators
+// places of new tokens (paged_slots.cu)
+struct SlotsCall {
+  const int32_t *n_kv, *n_keep, *n_new;    // n_keep: null, or what stays of n_kv
+  int n_reqs, page_size;
+  int32_t* table;
+  int table_stride, table_cols;
+  int32_t* free_pages;
+  int free_cap;
+  const int32_t* n_free;
+  int32_t *n_kv_out, *n_free_out, *cu_q, *positions;
+  int64_t* slots;
+  int n_rows;
+  int32_t* status;
+};
+int launch_page_slots(const SlotsCall& a, cudaStream_t s);
+// rotary positions (rotary.cu); strides in elements
+struct RotaryRows {
+  const char* in;
+  char* out;
+  int64_t in_row, in_head, out_row, out_head;
+  int heads;
+};
+struct RotaryCall {
+  RotaryRows q, k;       // k.heads 0: no keys
+  int n_rows, head_dim, half, dtype;
+  bool halves;
+  const int32_t* positions;
+  const double* frequencies;
+  float amplitude, sign;  // of the sine
+};
+int launch_rotary(const RotaryCall& a, cudaStream_t s);
+// new keys into the cache (paged_append.cu); scales null: the cache is of the rows' type
+constexpr int kScaleBlock = 16;          // slots that share a scale
+struct NewRows {
+  const char* k;
+  const char* v;
+  int64_t k_stride, v_stride;            // elements
+  int dtype;
+  const int32_t* cu_q;
+  int T;
+  float *k_scale, *v_scale;
+};
+int launch_append(const PagedCache& c, const NewRows& a, cudaStream_t s);
+// attention over codes with scales [n_pages][Hkv][ps / 16] (paged_scaled.cu)
+struct CacheScales {
+  const float *k, *v;
+};
+int64_t paged_scaled_workspace(int h);
+int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s);
+
 constexpr int kMaxTreeNodes = 128;   // nodes of one request's tree (chains have no limit)
 
 }  // namespace sled
