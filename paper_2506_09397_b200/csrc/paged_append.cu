@@ -20,7 +20,7 @@ namespace sled {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMany = 16;            // rows of a block's span for long calls
+constexpr int kMany = 64;            // rows of a block's span for long calls
 
 // eight elements, as they lie in memory
 template <typename T>
@@ -46,6 +46,20 @@ struct Eight {
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = make_uint4(0, 0, 0, 0);
   }
+  // bits of the largest of `top` and all |x|; infinities and NaN count as what their bits say, no less than 0x7f800000
+  __device__ __forceinline__ uint32_t largest(uint32_t top) const {
+    const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, u[i] & 0x7fffffffu);
+      return top;
+    } else {
+      uint32_t two = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) two = __vmaxu2(two, u[i] & 0x7fff7fffu);
+      return max(top, max(two << 16, two & 0xffff0000u));
+    }
+  }
   __device__ __forceinline__ float at(int i) const {
     const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
     if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
@@ -53,9 +67,9 @@ struct Eight {
   }
 };
 
-// the smallest power of two, at least 2^-126, of which 448 = 1.75 2^8 times is no less than m (finite, not negative)
-__device__ __forceinline__ float least_scale(float m) {
-  const uint32_t u = __float_as_uint(m);
+// the smallest power of two, at least 2^-126, of which 448 = 1.75 2^8 times is no less than the number with the bits u
+// (finite, not negative)
+__device__ __forceinline__ float least_scale(uint32_t u) {
   const int e = static_cast<int>(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);      // biased
   return __uint_as_float(static_cast<uint32_t>(max(e, 1)) << 23);
 }
@@ -70,121 +84,160 @@ __device__ __forceinline__ uint32_t code_pair(float x0, float x1) {
 }
 __device__ __forceinline__ float decode(uint32_t c) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(c), __NV_E4M3))); }
 
+// A cache block that receives keys: the row of the call that holds the first of them, the block's page and first slot there, how
+// many older keys it has and how many new ones it gets.
+struct Target {
+  int row, page, slot0, off, count;
+};
+
 // T: the rows' type; kCodes: the cache holds codes, otherwise T.  kSpan rows of the call per block.
 template <typename T, int H, bool kCodes, int kSpan>
 __global__ void __launch_bounds__(kThreads) append_kernel(const PagedCache c, const NewRows a, bool whole) {
   constexpr int kLanes = H / 8, kAtOnce = 32 / kLanes, kPasses = kScaleBlock / kAtOnce;      // lanes of a row, rows at a time
-  __shared__ int2 found[kSpan];                // of every row that begins a block: request and key; -1
-  pdl_enter();
+  __shared__ Target targets[kSpan];
+  __shared__ int n_targets;
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) n_targets = 0;
+  __syncthreads();
+  pdl_wait();
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kSpan;
   PagedRows r{};
   r.cu_q = a.cu_q;
   r.T = a.T;
   if (threadIdx.x < kSpan) {
-    int2 mine = make_int2(-1, 0);
     const int64_t t = t0 + threadIdx.x;
     if (t < a.T) {
       const int i = req_of_row(a.cu_q, c.n_reqs, static_cast<int>(t));
       const ReqView v = req_view(c, r, i);
       if (v.ok && t >= v.row0 && t < v.row0 + v.m) {
-        const int x = v.n - v.m + static_cast<int>(t - v.row0);
-        if (t == v.row0 || x % kScaleBlock == 0) mine = make_int2(i, x);
+        const int x = v.n - v.m + static_cast<int>(t - v.row0), off = x % kScaleBlock;
+        if (t == v.row0 || off == 0) {
+          const int p = x / c.ps, page = c.table[static_cast<int64_t>(i) * c.table_stride + p];
+          if (page_exists(c, page)) targets[atomicAdd(&n_targets, 1)] = Target{static_cast<int>(t), page, x - p * c.ps - off, off, min(kScaleBlock - off, v.n - x)};
+          else set_status(c.status, SLED_ERR_ARG);
+        }
       }
     }
-    found[threadIdx.x] = mine;
   }
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < c.n_reqs; i += kThreads)
       if (!req_view(c, r, i).ok) set_status(c.status, SLED_ERR_ARG);
   __syncthreads();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = 2 * c.Hkv, sub_row = lane / kLanes, col = lane % kLanes * 8;
-#pragma unroll 1
-  for (int s = 0; s < kSpan; ++s) {
-    const int req = found[s].x, x = found[s].y;
-    if (req < 0) continue;
-    const int n = c.n_kv[req], off = x % kScaleBlock, count = min(kScaleBlock - off, n - x);
-    const int page = c.table[static_cast<int64_t>(req) * c.table_stride + x / c.ps];
-    if (!page_exists(c, page)) {
-      if (threadIdx.x == 0) set_status(c.status, SLED_ERR_ARG);
-      continue;
+  const int n_tasks = n_targets * per;
+  // where a task is: K or V of a head of a target
+  struct Task {
+    Target to;
+    int g;
+    bool is_v;
+  };
+  auto task_at = [&](int task) {
+    const int k = task / per, rest = task - k * per;
+    return Task{targets[k], rest >> 1, (rest & 1) != 0};
+  };
+  auto bring = [&](const Task& k, Eight<T>* y) {
+    const int64_t stride = k.is_v ? a.v_stride : a.k_stride;
+    const T* src = reinterpret_cast<const T*>(k.is_v ? a.v : a.k) + k.to.row * stride + static_cast<int64_t>(k.g) * H + col;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      const int e = p * kAtOnce + sub_row - k.to.off;                 // of the new rows
+      if (e >= 0 && e < k.to.count) y[p].load(src + e * stride, whole);
+      else y[p].zero();
     }
-    const int slot0 = x % c.ps - off;           // the block's first slot
-#pragma unroll 1
-    for (int task = warp; task < per; task += kWarps) {
-      const int g = task >> 1;
-      const bool is_v = task & 1;
-      const T* src = reinterpret_cast<const T*>(is_v ? a.v : a.k) + (t0 + s) * (is_v ? a.v_stride : a.k_stride) + static_cast<int64_t>(g) * H + col;
-      const int64_t stride = is_v ? a.v_stride : a.k_stride;
-      const int64_t head = static_cast<int64_t>(page) * c.Hkv + g;
-      const int64_t first = (head * c.ps + slot0) * H + col;       // element of the cache: the block's first slot, this lane's columns
-      Eight<T> y[kPasses];
+  };
+  auto put = [&](const Task& k, const Eight<T>* y) {
+    const int off = k.to.off, count = k.to.count;
+    const int64_t head = static_cast<int64_t>(k.to.page) * c.Hkv + k.g;
+    const int64_t first = (head * c.ps + k.to.slot0) * H + col;       // element of the cache: the block's first slot, this lane's columns
+    char* cache = const_cast<char*>(k.is_v ? c.v : c.k);
+    if constexpr (!kCodes) {
+      T* to = reinterpret_cast<T*>(cache) + first;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
-        const int e = p * kAtOnce + sub_row - off;                 // of the new rows
-        if (e >= 0 && e < count) y[p].load(src + e * stride, whole);
-        else y[p].zero();
+        const int e = p * kAtOnce + sub_row - off;
+        if (e >= 0 && e < count) y[p].store(to + static_cast<int64_t>(p * kAtOnce + sub_row) * H);
       }
-      if constexpr (!kCodes) {
-        T* to = reinterpret_cast<T*>(const_cast<char*>(is_v ? c.v : c.k)) + first;
+    } else {
+      uint8_t* to = reinterpret_cast<uint8_t*>(cache) + first;
+      float* scale = (k.is_v ? a.v_scale : a.k_scale) + head * (c.ps / kScaleBlock) + k.to.slot0 / kScaleBlock;
+      const float before = off > 0 ? *scale : 0.f;
+      uint32_t top = 0;            // bits of the largest |x|
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-          const int e = p * kAtOnce + sub_row - off;
-          if (e >= 0 && e < count) y[p].store(to + static_cast<int64_t>(p * kAtOnce + sub_row) * H);
-        }
-      } else {
-        uint8_t* to = reinterpret_cast<uint8_t*>(const_cast<char*>(is_v ? c.v : c.k)) + first;
-        float* scale = (is_v ? a.v_scale : a.k_scale) + head * (c.ps / kScaleBlock) + slot0 / kScaleBlock;
-        const float before = off > 0 ? *scale : 0.f;
-        float most = 0.f;
-        bool odd = false;
+      for (int p = 0; p < kPasses; ++p) top = y[p].largest(top);
+      top = __reduce_max_sync(0xffffffffu, top);
+      bool plain = top < 0x7f800000u;
+      if (!plain) {                // without infinities and NaN
+        top = 0;
 #pragma unroll
         for (int p = 0; p < kPasses; ++p)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const float z = fabsf(y[p].at(i));
-            const bool fine = z < INFINITY;
-            odd |= !fine;
-            most = fmaxf(most, fine ? z : 0.f);
+            const uint32_t z = __float_as_uint(y[p].at(i)) & 0x7fffffffu;
+            top = max(top, z < 0x7f800000u ? z : 0u);
           }
-        const float now = fmaxf(least_scale(warp_max(most)), before), inv = 1.f / now;
-        odd |= (__float_as_uint(now) & 0x7fffffu) != 0;      // a scale of the caller's own that is no power of two: true quotients
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-          const int e = p * kAtOnce + sub_row - off;
-          if (e < 0 || e >= count) continue;
-          uint2 w = make_uint2(0, 0);
-          if (!odd) {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              const uint32_t two = code_pair(y[p].at(i) * inv, y[p].at(i + 1) * inv) << (i & 2) * 8;
-              if (i < 4) w.x |= two; else w.y |= two;
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t one = code(__fdiv_rn(y[p].at(i), now)) << (i & 3) * 8;
-              if (i < 4) w.x |= one; else w.y |= one;
-            }
-          }
-          *reinterpret_cast<uint2*>(to + static_cast<int64_t>(p * kAtOnce + sub_row) * H) = w;
-        }
-        if (off > 0 && now != before) {         // older keys of the block follow its scale
-#pragma unroll 1
-          for (int e = sub_row; e < off; e += kAtOnce) {
-            uint2* at = reinterpret_cast<uint2*>(to + static_cast<int64_t>(e) * H);
-            const uint2 old = *at;
-            uint2 w = make_uint2(0, 0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t one = code(__fdiv_rn(decode((i < 4 ? old.x : old.y) >> (i & 3) * 8 & 0xffu) * before, now)) << (i & 3) * 8;
-              if (i < 4) w.x |= one; else w.y |= one;
-            }
-            *at = w;
-          }
-        }
-        if (lane == 0) *scale = now;
+        top = __reduce_max_sync(0xffffffffu, top);
       }
+      const float now = fmaxf(least_scale(top), before), inv = 1.f / now;
+      plain = plain && (__float_as_uint(now) & 0x7fffffu) == 0;      // a scale of the caller's own may be no power of two: true quotients
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        const int e = p * kAtOnce + sub_row - off;
+        if (e < 0 || e >= count) continue;
+        uint2 w = make_uint2(0, 0);
+        if (plain) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const uint32_t two = code_pair(y[p].at(i) * inv, y[p].at(i + 1) * inv) << (i & 2) * 8;
+            if (i < 4) w.x |= two; else w.y |= two;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t one = code(__fdiv_rn(y[p].at(i), now)) << (i & 3) * 8;
+            if (i < 4) w.x |= one; else w.y |= one;
+          }
+        }
+        *reinterpret_cast<uint2*>(to + static_cast<int64_t>(p * kAtOnce + sub_row) * H) = w;
+      }
+      if (off > 0 && now != before) {         // older keys of the block follow its scale
+#pragma unroll 1
+        for (int e = sub_row; e < off; e += kAtOnce) {
+          uint2* at = reinterpret_cast<uint2*>(to + static_cast<int64_t>(e) * H);
+          const uint2 old = *at;
+          uint2 w = make_uint2(0, 0);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t one = code(__fdiv_rn(decode((i < 4 ? old.x : old.y) >> (i & 3) * 8 & 0xffu) * before, now)) << (i & 3) * 8;
+            if (i < 4) w.x |= one; else w.y |= one;
+          }
+          *at = w;
+        }
+      }
+      if (lane == 0) *scale = now;
     }
+  };
+  // the next task's rows are under way while this one's are coded
+  Eight<T> y[2][kPasses];
+  Task k[2];
+  int task = warp;
+  if (task < n_tasks) {
+    k[0] = task_at(task);
+    bring(k[0], y[0]);
+  }
+#pragma unroll 1
+  for (; task < n_tasks; task += 2 * kWarps) {
+    const int second = task + kWarps, third = second + kWarps;
+    if (second < n_tasks) {
+      k[1] = task_at(second);
+      bring(k[1], y[1]);
+    }
+    put(k[0], y[0]);
+    if (second >= n_tasks) break;
+    if (third < n_tasks) {
+      k[0] = task_at(third);
+      bring(k[0], y[0]);
+    }
+    put(k[1], y[1]);
   }
 }
 
@@ -195,7 +248,7 @@ int launch(const PagedCache& c, const NewRows& a, cudaStream_t s) {
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
   // A block per row (most of them then find that another row begins their cache block) while that fills the GPU a few times;
-  // a block per 16 rows beyond.
+  // a block per 64 rows beyond.
   if (a.T <= 16 * sms)
     SLED_LAUNCH_PDL((append_kernel<T, H, kCodes, 1>), dim3(a.T), dim3(kThreads), 0, s, c, a, whole);
   else

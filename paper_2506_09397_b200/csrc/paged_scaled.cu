@@ -16,20 +16,14 @@
 // loads, and the queries are laid out to match.  V goes through transposing matrix loads of 16-bit units - two dimensions of
 // a key -, a byte permutation parts them into the even and the odd dimensions of two keys.  A fifth warp brings the tiles in by
 // TMA and their scales with them, looked up a round ahead.  Work is handed out as paged_schedule.cuh says.
-#include <cuda_fp16.h>
-
 #include "gemm_tc.h"
 #include "kernels.h"
-#include "paged_schedule.cuh"
-#include "warp_mma.cuh"
+#include "paged_scaled.cuh"
 
 namespace sled {
 
 namespace {
 
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kGain = 32768.f;
 
 // A stage holds K, then V: four groups of 16 keys, rows of 128 bytes (of one, two or four keys); the 16-byte chunk c of a row
 // lies at c ^ (row & 7).
@@ -73,81 +67,11 @@ struct UnitRows {
   __device__ __forceinline__ int head(int r) const { return g * group + first + r - quotient(first + r, group) * group; }
 };
 
-struct Parts {
-  float* acc;      // [2 * blocks][kUnitRows][H], not normalised
-  float* ml;       // [2 * blocks][kUnitRows][2]
-  int4* desc;      // [blocks][2]: CutUnit
-};
-
-// two codes, exactly
-__device__ __forceinline__ uint32_t half2_of(uint32_t two_codes) {
-  uint32_t h;
-  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\t}" : "=r"(h) : "r"(two_codes));
-  return h;
-}
-__device__ __forceinline__ uint32_t half2_of_upper(uint32_t four_codes) {
-  uint32_t h;
-  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, y;\n\t}" : "=r"(h) : "r"(four_codes));
-  return h;
-}
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ void mma_half(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// This lane's H / 4 elements of a query row as fp16, times a power of two that brings the row's largest finite element to 2^14;
-// returns the factor that undoes it.  All lanes call it.
-template <int H>
-__device__ __forceinline__ float query_row(const __nv_bfloat16* q, bool valid, uint32_t f[H / 8]) {
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
-  uint32_t most = 0;       // |x| as bits of bf16, times 2^16
-#pragma unroll
-  for (int i = 0; i < H / 8; ++i) {
-    f[i] = valid ? w[i] : 0u;
-    const uint32_t lo = f[i] << 16 & 0x7fff0000u, hi = f[i] & 0x7fff0000u;
-    most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
-  }
-  most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-  most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-  const int e = min(max(268 - static_cast<int>(most >> 23), 1), 253);      // biased exponent of the factor
-  const float up = __uint_as_float(static_cast<uint32_t>(e) << 23);
-#pragma unroll
-  for (int i = 0; i < H / 8; ++i) f[i] = pack_half(__uint_as_float(f[i] << 16) * up, __uint_as_float(f[i] & 0xffff0000u) * up);
-  return __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
-}
-
-// running maximum, sum and numerators' reference of one of a lane's two rows
-struct RowState {
-  float m = -INFINITY, l = 0.f, u = -INFINITY;
-  float ref, num;       // of this tile: m, and the reference of the numerators, finite
-  // takes the tile's largest score and the largest log2 |vs|; returns the factor of the output so far
-  __device__ __forceinline__ float take(float mx, float lv) {
-    const float mn = fmaxf(m, mx);
-    ref = mn == -INFINITY ? 0.f : mn;
-    l *= exp2_approx(m - ref);
-    m = mn;
-    const float un = fmaxf(u, mx + lv);
-    num = un == -INFINITY ? 0.f : un;
-    const float f = exp2_approx(u - num);
-    u = un;
-    return f;
-  }
-  // what a block's 2^(s - m) are multiplied by
-  __device__ __forceinline__ float weight(float vs) const { return u == -INFINITY ? 0.f : vs * kGain * exp2_approx(fminf(ref - num, 110.f)); }
-  // what the output is multiplied by at the end
-  __device__ __forceinline__ float rest() const { return u == -INFINITY ? 0.f : exp2_approx(u - (m == -INFINITY ? 0.f : m)) * (1.f / kGain); }
-};
 
 // One stretch of a unit: MT warps cover the rows, 4 / MT the keys of a tile.
 template <int H, int MT>
 __device__ __forceinline__ void consume(const PagedRows& r, const UnitRows& u, const Segment& sg, Ring& ring, volatile int* stop,
-                                        const float* scales, float* merge, const uint32_t* tree, const Parts& parts) {
+                                        const float* scales, float* merge, const uint32_t* tree, const ScaledParts& parts) {
   using S = Smem<H>;
   constexpr int KS = H / 16, DC = H / 16, NT = 2 * MT;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
@@ -242,6 +166,7 @@ __device__ __forceinline__ void consume(const PagedRows& r, const UnitRows& u, c
 #pragma unroll
         for (int i = 0; i < 2 * DC; ++i) { o[i][0] *= al_lo; o[i][1] *= al_lo; o[i][2] *= al_hi; o[i][3] *= al_hi; }
       }
+      const float unit_lo = lo.unit_weight(), unit_hi = hi.unit_weight();
       uint32_t pf[MT][4];   // the numerators as A operand; their sum is taken before the rounding
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -249,7 +174,7 @@ __device__ __forceinline__ void consume(const PagedRows& r, const UnitRows& u, c
         float p2 = exp2_approx(sc[nt][2] - hi.ref), p3 = exp2_approx(sc[nt][3] - hi.ref);
         lo.l += p0 + p1;
         hi.l += p2 + p3;
-        const float w_lo = lo.weight(vs[nt >> 1]), w_hi = hi.weight(vs[nt >> 1]);
+        const float w_lo = lo.scaled(unit_lo, vs[nt >> 1]), w_hi = hi.scaled(unit_hi, vs[nt >> 1]);
         if (masked) {       // a scale that is no number reaches the rows that see its block, not the others
           p0 = sc[nt][0] == -INFINITY ? 0.f : p0 * w_lo;
           p1 = sc[nt][1] == -INFINITY ? 0.f : p1 * w_lo;
@@ -485,7 +410,7 @@ __device__ __forceinline__ UnitRows unit_rows(const PagedRows& r, const ReqWork&
 
 // 160 threads: warps 0-3 compute, warp 4 brings the tiles in.
 template <int H>
-__global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const Parts parts,
+__global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const ScaledParts parts,
                                                               const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using S = Smem<H>;
   extern __shared__ uint8_t smem_raw[];
@@ -618,7 +543,7 @@ int launch_h(const PagedCache& c, const CacheScales& sc, const PagedRows& r, cha
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps / P;
   if (tma_map_bf16_row_groups(&map_k, c.k, rows, 64, 16 / P) || tma_map_bf16_row_groups(&map_v, c.v, rows, 64, 16 / P)) return -1;
   const int blocks = min(2 * sms, kMaxPagedBlocks);
-  Parts parts;
+  ScaledParts parts;
   parts.acc = reinterpret_cast<float*>(ws);
   parts.ml = parts.acc + 2LL * kMaxPagedBlocks * kUnitRows * H;
   parts.desc = reinterpret_cast<int4*>(parts.ml + 2LL * kMaxPagedBlocks * kUnitRows * 2);
@@ -632,9 +557,15 @@ int launch_h(const PagedCache& c, const CacheScales& sc, const PagedRows& r, cha
 
 }  // namespace
 
-int64_t paged_scaled_workspace(int h) { return paged_mma_workspace(h); }
+int64_t paged_scaled_workspace(int h) {
+  return max(max(paged_mma_workspace(h), scaled_few_workspace(h)), h >= 64 ? paged_tc_workspace(h) : 0);
+}
 
 int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s) {
+  // by the rows per request and KV head, on average
+  const int64_t rows = static_cast<int64_t>(r.T) * r.group;
+  if (rows <= 8LL * c.n_reqs) return launch_scaled_few(c, sc, r, 1, ws, s);
+  if (c.h >= 64 && rows > 24LL * c.n_reqs) return launch_scaled_tc(c, sc, r, ws, s);
   if (c.h == 128) return launch_h<128>(c, sc, r, ws, s);
   return c.h == 64 ? launch_h<64>(c, sc, r, ws, s) : launch_h<32>(c, sc, r, ws, s);
 }

@@ -1,0 +1,88 @@
+// What the warp-level kernels of attention over a cache of e4m3 codes share: codes and queries as fp16, a row's running
+// maximum, sum and numerators' reference.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "paged_schedule.cuh"
+#include "warp_mma.cuh"
+
+namespace sled {
+
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kGain = 32768.f;
+
+// partial results of units that were cut
+struct ScaledParts {
+  float* acc;      // [2 * blocks][rows of a unit][H], not normalised
+  float* ml;       // [2 * blocks][rows of a unit][2]
+  int4* desc;      // [blocks][2]: CutUnit
+};
+
+// two codes, exactly
+__device__ __forceinline__ uint32_t half2_of(uint32_t two_codes) {
+  uint32_t h;
+  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\t}" : "=r"(h) : "r"(two_codes));
+  return h;
+}
+__device__ __forceinline__ uint32_t half2_of_upper(uint32_t four_codes) {
+  uint32_t h;
+  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, y;\n\t}" : "=r"(h) : "r"(four_codes));
+  return h;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void mma_half(float c[4], const uint32_t a[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// This lane's H / 4 elements of a query row as fp16, times a power of two that brings the row's largest finite element to 2^14;
+// returns the factor that undoes it.  All lanes call it.
+template <int H>
+__device__ __forceinline__ float query_row(const __nv_bfloat16* q, bool valid, uint32_t f[H / 8]) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
+  uint32_t most = 0;       // |x| as bits of bf16, times 2^16
+#pragma unroll
+  for (int i = 0; i < H / 8; ++i) {
+    f[i] = valid ? w[i] : 0u;
+    const uint32_t lo = f[i] << 16 & 0x7fff0000u, hi = f[i] & 0x7fff0000u;
+    most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+  }
+  most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+  most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+  const int e = min(max(268 - static_cast<int>(most >> 23), 1), 253);      // biased exponent of the factor
+  const float up = __uint_as_float(static_cast<uint32_t>(e) << 23);
+#pragma unroll
+  for (int i = 0; i < H / 8; ++i) f[i] = pack_half(__uint_as_float(f[i] << 16) * up, __uint_as_float(f[i] & 0xffff0000u) * up);
+  return __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+}
+
+// running maximum, sum and numerators' reference of one of a lane's two rows
+struct RowState {
+  float m = -INFINITY, l = 0.f, u = -INFINITY;
+  float ref, num;       // of this tile: m, and the reference of the numerators, finite
+  // takes the tile's largest score and the largest log2 |vs|; returns the factor of the output so far
+  __device__ __forceinline__ float take(float mx, float lv) {
+    const float mn = fmaxf(m, mx);
+    ref = mn == -INFINITY ? 0.f : mn;
+    l *= exp2_approx(m - ref);
+    m = mn;
+    const float un = fmaxf(u, mx + lv);
+    num = un == -INFINITY ? 0.f : un;
+    const float f = exp2_approx(u - num);
+    u = un;
+    return f;
+  }
+  // what a block's 2^(s - m) are multiplied by: scaled(unit_weight(), vs)
+  __device__ __forceinline__ float unit_weight() const { return kGain * exp2_approx(fminf(ref - num, 110.f)); }
+  __device__ __forceinline__ float scaled(float w, float vs) const { return u == -INFINITY ? 0.f : vs * w; }
+  // what the output is multiplied by at the end
+  __device__ __forceinline__ float rest() const { return u == -INFINITY ? 0.f : exp2_approx(u - (m == -INFINITY ? 0.f : m)) * (1.f / kGain); }
+};
+
+}  // namespace sled

@@ -99,7 +99,7 @@ struct Share {
 
 // Shares `first`, .. `first` + kShares - 1 of at most `most`, into out[] (shared memory).  All threads of the block call it
 // (blockDim.x a multiple of 32, at most 32 * kMostWarps).  The block with share 0 reports the requests that are left out.
-constexpr int kMostWarps = 12;
+constexpr int kMostWarps = 16;
 template <int kShares, typename Line>
 __device__ __forceinline__ void block_shares(const Line& line, int first, int most, Share* out) {
   __shared__ long long sums[kMostWarps];   // (little, so that attention blocks still share an SM)
