@@ -7,14 +7,14 @@
 // the end.
 //     S = Q C^T      (M 128 x N 128 keys, contraction over H)      -> tensor memory, fp32
 //     O += P D       (M 128 x N H, contraction over 128 keys)      P from tensor memory (fp16, over S)
-// The products take 16-bit operands, so four warps turn the codes into fp16 on their way into shared memory: loads of 8 codes a
-// lane, a tile in registers ahead of the one that is written, the ones after it asked into L2.  They bring the queries too, as fp16
-// times a power of two per row.  A score meets its block's scale ks where it leaves tensor memory, a numerator its vs before it is
-// rounded.  The references of a row - m of the scores, u of the numerators - are raised only when something exceeds them
+// The products take 16-bit operands, so four warps turn the codes into fp16: from a ring of pieces of 64 keys, K and V of a tile in
+// turn, into operand tiles.  Each warp brings its sixteen keys of a piece itself, with asynchronous 16-byte
+// copies, and needs nobody to tell it that they have arrived.  They bring the queries too, as fp16 times a power of two per row.  A
+// score meets its block's scale ks where it leaves tensor memory, a numerator its vs before it is rounded.  The references of a row - m of the scores, u of the numerators - are raised only when something exceeds them
 // by more than 2^8; raising u means rescaling the row of O in tensor memory, which happens in a unit's first tiles.
 // Scores are read from tensor memory twice, for the maximum and for the exponentials: no thread holds a row of them.
 //   warps 0-3, 4-7 : softmax and output of the two groups
-//   warps 8-9, 10-11 : K and V from codes to fp16; all four: Q
+//   warps 8-11     : K, V and Q to fp16, scales
 //   warp 12        : tensor-memory allocation, products (one thread); 13-15 only complete the warpgroup
 // Every wait is bounded; when one runs out the block says so in *status, lets what is under way land, frees its tensor
 // memory and returns.
@@ -30,7 +30,9 @@ constexpr int kKeys = 128;                 // keys per tile
 constexpr int kGroupRows = 128;            // rows of a softmax group
 constexpr float kRaiseBy = 8.f;
 constexpr float kTcGain = 64.f;            // numerators are at most 2^8 times this
-constexpr int kScaleSlots = 8;             // tiles whose scales are kept: more than K, V and S stages are ahead of a softmax
+constexpr int kScaleSlots = 16;            // tiles whose scales are kept: more than copies, K, V and S are ahead of a softmax
+constexpr int kScaleWords = 20;            // ks [8], vs [8], the largest log2 |vs|
+constexpr int kPieceKeys = 64;
 
 // Operands lie in groups of eight rows, [H / 64][8 rows][64 columns] (K, V), or as [H / 64][128 rows][64 columns] (Q); rows of
 // 128 bytes, 16-byte chunk c at c ^ (row & 7).
@@ -39,15 +41,17 @@ struct ScaledTc {
   static constexpr int kHalves = H / 64;
   static constexpr int kOctet = kHalves * 1024;          // eight rows
   static constexpr int kTileBytes = 16 * kOctet;         // K, V or 128 rows of Q
-  static constexpr int kKStages = H == 64 ? 4 : kGroups == 1 ? 3 : 2, kVStages = H == 64 ? 4 : 2;
+  static constexpr int kKStages = H == 64 ? 3 : 2, kVStages = H == 64 ? 3 : 2;
   static constexpr int kOffQ = 0;
   static constexpr int kOffK = kGroups * kTileBytes;
   static constexpr int kOffV = kOffK + kKStages * kTileBytes;
-  static constexpr int kOffBar = kOffV + kVStages * kTileBytes;
+  static constexpr int kPieces = H == 64 || kGroups == 1 ? 7 : 3, kPieceBytes = kPieceKeys * H;
+  static constexpr int kOffRaw = kOffV + kVStages * kTileBytes;
+  static constexpr int kOffBar = kOffRaw + kPieces * kPieceBytes;
   static constexpr int kOffTree = kOffBar + 384;         // parents of the nodes, one byte each, for either group
   static constexpr int kOffTop = kOffTree + 2 * kMaxTreeNodes;     // what the groups tell each other about a row
-  static constexpr int kOffScale = kOffTop + kGroupRows * 16;      // [slot][K, V][8]
-  static constexpr int kOffFactor = kOffScale + kScaleSlots * 64;  // of the rows of Q
+  static constexpr int kOffScale = kOffTop + kGroupRows * 16;      // [slot][kScaleWords]
+  static constexpr int kOffFactor = kOffScale + kScaleSlots * kScaleWords * 4;  // of the rows of Q
   static constexpr int kTotal = kOffFactor + kGroups * kGroupRows * 4 + 1024;     // alignment slack
 };
 static_assert(kMaxTreeNodes == 128);
@@ -94,9 +98,10 @@ __device__ __forceinline__ void mul2(float& a, float& b, float f) {
       "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
       : "+f"(a), "+f"(b) : "f"(f));
 }
-__device__ __forceinline__ void prefetch_l2(const void* p, int bytes) {
-  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+__device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // a unit, or the stretch of it that the block works on
 struct TcUnit {
@@ -126,8 +131,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *stop = odd[0] = odd[1] = 0;
-    for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 2); mbar_init(bar(B_KEMPTY + s), 1); }
-    for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 2); mbar_init(bar(B_VEMPTY + s), 1); }
+    for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 4); mbar_init(bar(B_KEMPTY + s), 1); }
+    for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 4); mbar_init(bar(B_VEMPTY + s), 1); }
     mbar_init(bar(B_QFULL), 4);
     mbar_init(bar(B_QEMPTY), 8);
     for (int s = 0; s < 2; ++s) {
@@ -232,19 +237,80 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
     __syncwarp();
   } else if (warp >= 8) {
     // ------------------------------------------------------------------------------------------- codes to fp16: Q, K, V
-    constexpr int kPasses = kKeys / 8, kHalves = L::kHalves;
-    const bool is_k = warp < 10;
-    const uint8_t* codes = reinterpret_cast<const uint8_t*>(is_k ? c.k : c.v);
-    const float* of_blocks = is_k ? sc.k : sc.v;
-    const uint32_t ring = base + (is_k ? L::kOffK : L::kOffV);
-    const int stages = is_k ? L::kKStages : L::kVStages, b_full = is_k ? B_KFULL : B_VFULL, b_empty = is_k ? B_KEMPTY : B_VEMPTY;
-    const int cpp = c.ps / 16, tid = threadIdx.x & 63;
-    const int row = tid >> 3, chunk = tid & 7;      // of a pass: one of eight keys, 8 codes of each half of its dimensions
-    const uint32_t place = row * 128 + ((chunk ^ row) << 4);
-    int st = 0, phase = 1, units = 0, tiles = 0;
+    constexpr int kLanes = H / 8, kAtOnce = 32 / kLanes;      // lanes of a key, keys at a time: a warp has 16 of a piece
+    const int part = warp & 3, chunk = lane % kLanes, sub = lane / kLanes, cpp = c.ps / 16;
+    const uint8_t *k_codes = reinterpret_cast<const uint8_t*>(c.k), *v_codes = reinterpret_cast<const uint8_t*>(c.v);
+    int tiles_issued = 0;
+    int kst = 0, kphase = 1, vst = 0, vphase = 1, units = 0, tiles = 0;
     for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
       const int first = sg.rb * kUnit, total = w.v.m * group, rows = min(kUnit, total - first);
       ++units;
+      const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
+      const int groups = min((w.v.n + 15) / 16, sg.t1 * 8);     // 16-key groups up to the end of the segment
+      // lane l looks after group l of four tiles: the block's place among all and (one warp) its scales; those of the next round
+      // and the table's entries of the one after are under way
+      auto page_of = [&](int e) { return e < groups ? table[quotient(e, cpp)] : 0; };
+      auto block_of = [&](int e, int page) { return e < groups ? (checked_page(c, page) * c.Hkv + sg.g) * cpp + (e - quotient(e, cpp) * cpp) : 0; };
+      int block, page_next = page_of(sg.t0 * 8 + lane), block_next = block_of(sg.t0 * 8 + lane, page_next);
+      float ks, vs, ks_next = 1.f, vs_next = 1.f;
+      auto scales_of = [&](int e) {
+        if (warp == 8 && e < groups) {
+          ks_next = sc.k[block_next];
+          vs_next = sc.v[block_next];
+        }
+      };
+      scales_of(sg.t0 * 8 + lane);
+      page_next = page_of(sg.t0 * 8 + 32 + lane);
+      // piece i of the segment: keys 64 (i % 2) .. of K (i % 4 < 2) or V of tile t0 + i / 4; this warp: 16 of them
+      const int n_pieces = (sg.t1 - sg.t0) * 4;
+      int issued = 0, into = 0;
+      auto issue = [&]() {
+        if (issued < n_pieces) {
+          const int t = sg.t0 + (issued >> 2), ahead = (issued >> 2) & 3;
+          if ((issued & 3) == 0) {
+            if (ahead == 0) {
+              block = block_next;
+              ks = ks_next;
+              vs = vs_next;
+              block_next = block_of((t + 4) * 8 + lane, page_next);
+              ks_next = vs_next = 1.f;
+              scales_of((t + 4) * 8 + lane);
+              page_next = page_of((t + 8) * 8 + lane);
+            }
+            if (warp == 8) {
+              float* to = scales + ((tiles_issued) % kScaleSlots) * kScaleWords;
+              const bool mine = lane >> 3 == ahead;
+              const float lv = warp_max(mine ? __log2f(fabsf(vs)) : -INFINITY);
+              if (mine) {
+                to[lane & 7] = ks;
+                to[8 + (lane & 7)] = vs;
+                if ((lane & 7) == 0) to[16] = lv;
+              }
+            }
+            ++tiles_issued;
+            // what comes four tiles later is asked into L2: two groups a warp, a line a lane
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int which = part * 2 + i;
+              const int64_t at = static_cast<int64_t>(__shfl_sync(0xffffffffu, block_next, ahead * 8 + which)) * 16 * H + (lane & 15) * H;
+              if ((t + 4) * 8 + which < groups && (H == 128 || !(lane & 1))) prefetch_line((lane < 16 ? k_codes : v_codes) + at);
+            }
+          }
+          const int which = (issued & 1) * 4 + part;
+          const int64_t b = __shfl_sync(0xffffffffu, block, ahead * 8 + which);
+          if (t * 8 + which < groups) {
+            const uint8_t* from = (issued & 2 ? v_codes : k_codes) + b * 16 * H + lane * 16;
+            const uint32_t to = base + L::kOffRaw + into * L::kPieceBytes + part * 16 * H + lane * 16;
+#pragma unroll
+            for (int i = 0; i < H / 32; ++i) copy_16(to + i * 512, from + i * 512);
+          }
+          ++issued;
+          if (++into == L::kPieces) into = 0;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+#pragma unroll 1
+      for (int i = 0; i < L::kPieces - 1; ++i) issue();
       // the unit's Q: a row per thread
       if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_QEMPTY), (units & 1), stop))) { *stop = 1; return; }
       for (int s = 0; s < (rows > kGroupRows ? kGroups : 1); ++s) {
@@ -289,87 +355,70 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(B_QFULL));
 
-      const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
-      const int end = w.v.n, groups = min((end + 15) / 16, sg.t1 * 8);     // 16-key groups up to the end of the segment
-      const int prefix = end - w.v.m + (r.parents ? 0 : first / group + 1);
-      // lane l looks after group l of four tiles: its place among all blocks; what comes after them is asked into L2
-      auto block_of = [&](int e) {
-        if (e >= groups) return 0;
-        const int b = quotient(e, cpp);
-        return (checked_page(c, table[b]) * c.Hkv + sg.g) * cpp + (e - b * cpp);
-      };
-      uint2 x[kPasses][kHalves];
-      auto bring = [&](int t, int block) {       // block: this lane's group of the round of t
+      const int end = w.v.n, prefix = end - w.v.m + (r.parents ? 0 : first / group + 1);
+      // a tile of K or V: clean(key, codes) changes what may not become part of a product
+      int piece = 0;
+      auto convert = [&](uint32_t tile, auto clean) {
+#pragma unroll 1
+        for (int p = 0; p < kKeys / kPieceKeys; ++p) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(L::kPieces - 2) : "memory");
+          __syncwarp();
+          const uint32_t from = base + L::kOffRaw + piece * L::kPieceBytes + part * 16 * H + lane * 8, to = tile + (p * 8 + part * 2) * L::kOctet + (chunk >> 3) * 1024;
+          uint2 x[16 / kAtOnce];
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-          const int e = t * 8 + (p >> 1), b = __shfl_sync(0xffffffffu, block, ((t - sg.t0) & 3) * 8 + (p >> 1));
-          const uint8_t* from = codes + (static_cast<int64_t>(b) * 16 + (p & 1) * 8 + row) * H + chunk * 8;
+          for (int i = 0; i < 16 / kAtOnce; ++i)
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x[i].x), "=r"(x[i].y) : "r"(from + i * 256));
 #pragma unroll
-          for (int h = 0; h < kHalves; ++h) x[p][h] = e < groups ? *reinterpret_cast<const uint2*>(from + h * 64) : make_uint2(0, 0);
-        }
-      };
-      int block = block_of(sg.t0 * 8 + lane), later = block_of((sg.t0 + 4) * 8 + lane);
-      if ((warp & 1) == 0) {
-        if (sg.t0 * 8 + lane < groups) prefetch_l2(codes + static_cast<int64_t>(block) * 16 * H, 16 * H);
-        if ((sg.t0 + 4) * 8 + lane < groups) prefetch_l2(codes + static_cast<int64_t>(later) * 16 * H, 16 * H);
-      }
-      float scale = (sg.t0 * 8 + lane) < groups ? of_blocks[block] : 1.f;
-      bring(sg.t0, block);
-      for (int t = sg.t0; t < sg.t1; ++t, ++tiles) {
-        const int ahead = (t - sg.t0) & 3;
-        const bool all = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(b_empty + st), phase, stop));
-        if (!all) { *stop = 1; return; }
-        if ((warp & 1) == 0 && lane >> 3 == ahead) scales[(tiles % kScaleSlots) * 16 + (is_k ? 0 : 8) + (lane & 7)] = scale;
-        const int x0 = t * kKeys;
-        const uint32_t to = ring + st * L::kTileBytes + place;
-        const bool edge = x0 + kKeys > prefix;
-        uint32_t found = 0;
-        if (!edge || is_k) {
-#pragma unroll
-          for (int p = 0; p < kPasses; ++p)
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-              const uint2 v = x[p][h];
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + p * L::kOctet + h * 1024), "r"(half2_of(v.x)), "r"(half2_of_upper(v.x)),
-                           "r"(half2_of(v.y)), "r"(half2_of_upper(v.y)) : "memory");
-            }
-        } else {
-          // A numerator of 0 does not silence a value that is no number: values of positions that hold no key become 0, and so
-          // do those that are no numbers, which the rows that see them get back at the end.
-#pragma unroll
-          for (int p = 0; p < kPasses; ++p)
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-              uint32_t v[2] = {x[p][h].x, x[p][h].y};
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                if (x0 + p * 8 + row >= end) v[i] = 0;
-                const uint32_t none = (v[i] & 0x7f7f7f7fu) + 0x01010101u & 0x80808080u;      // in the bytes 0x7f and 0xff
-                found |= none;
-                v[i] &= ~((none >> 7) * 0xffu);
-              }
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + p * L::kOctet + h * 1024), "r"(half2_of(v[0])), "r"(half2_of_upper(v[0])),
-                           "r"(half2_of(v[1])), "r"(half2_of_upper(v[1])) : "memory");
-            }
-          if (found) odd[units & 1] = units;
+          for (int i = 0; i < 16 / kAtOnce; ++i) {
+            const int key = i * kAtOnce + sub, row = key & 7;
+            clean(p * kPieceKeys + part * 16 + key, x[i]);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (key >> 3) * L::kOctet + row * 128 + (((chunk & 7) ^ row) << 4)), "r"(half2_of(x[i].x)),
+                         "r"(half2_of_upper(x[i].x)), "r"(half2_of(x[i].y)), "r"(half2_of_upper(x[i].y)) : "memory");
+          }
+          issue();       // into the place of the piece before this one, which all lanes have read
+          if (++piece == L::kPieces) piece = 0;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
+      };
+      for (int t = sg.t0; t < sg.t1; ++t, ++tiles) {
+        bool ok = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_KEMPTY + kst), kphase, stop));
+        if (!ok) { *stop = 1; break; }
+        convert(base + L::kOffK + kst * L::kTileBytes, [](int, uint2&) {});
+        if (lane == 0) mbar_arrive(bar(B_KFULL + kst));
+        if (++kst == L::kKStages) { kst = 0; kphase ^= 1; }
+
+        ok = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_VEMPTY + vst), vphase, stop));
+        if (!ok) { *stop = 1; break; }
+        const uint32_t to = base + L::kOffV + vst * L::kTileBytes;
+        const int x0 = t * kKeys;
+        if (x0 + kKeys <= prefix) {
+          convert(to, [](int, uint2&) {});
+        } else {
+          // A numerator of 0 does not silence a value that is no number: values of positions that hold no key become 0, and so
+          // do those that are no numbers, which the rows that see them get back at the end.
+          uint32_t found = 0;
+          convert(to, [&](int key, uint2& x) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              uint32_t y = x0 + key < end ? (i ? x.y : x.x) : 0u;
+              const uint32_t none = ((y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;      // in the bytes 0x7f and 0xff
+              found |= none;
+              y &= ~((none >> 7) * 0xffu);
+              if (i) x.y = y; else x.x = y;
+            }
+          });
+          if (found) odd[units & 1] = units;
+          __syncwarp();
+        }
         if (lane == 0) {
           mbar_arrive(bar(B_SCALE + tiles % kScaleSlots));
-          mbar_arrive(bar(b_full + st));
+          mbar_arrive(bar(B_VFULL + vst));
         }
-        if (t + 1 < sg.t1) {
-          if (ahead == 3) {
-            block = later;
-            scale = (t + 1) * 8 + lane < groups ? of_blocks[block] : 1.f;
-            later = block_of((t + 5) * 8 + lane);
-            if ((warp & 1) == 0 && (t + 5) * 8 + lane < groups) prefetch_l2(codes + static_cast<int64_t>(later) * 16 * H, 16 * H);
-          }
-          bring(t + 1, block);
-        }
-        if (++st == stages) { st = 0; phase ^= 1; }
+        if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");      // (copies are still under way only where the segment was given up)
+      __syncwarp();
     });
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
@@ -449,7 +498,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
         const int x0 = (u.sg.t0 + t) * kKeys;
         const bool masked = x0 + kKeys > prefix;
         if (active) {
-          const float* ks = scales + slot * 16;
+          const float* ks = scales + slot * kScaleWords;
           const float* vs = ks + 8;
           // Scores of tiles that some row does not see all of are scaled and masked in tensor memory, in a pass of its own: the code
           // that every tile runs through stays short.
@@ -469,7 +518,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
             tmem_st_wait();
           }
           const float by = masked ? 1.f : factor;
-          float mx = -INFINITY, lv = -INFINITY;
+          float mx = -INFINITY;
+          const float lv = ks[16];
           float v[2][32];
           tmem_ld32_nowait(tmem_s, v[0]);
 #pragma unroll
@@ -480,11 +530,15 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
               const float f = by * (masked ? 1.f : ks[2 * q + b]);
-              float hi = x[b * 16], lo = x[b * 16];
+              float top = x[b * 16];
+              if (f >= 0.f) {      // (the same for all rows: a row's own factor is positive)
 #pragma unroll
-              for (int i = 1; i < 16; ++i) { hi = fmaxf(hi, x[b * 16 + i]); lo = fminf(lo, x[b * 16 + i]); }
-              mx = fmaxf(mx, (f < 0.f ? lo : hi) * f);
-              lv = fmaxf(lv, __log2f(fabsf(vs[2 * q + b])));
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, x[b * 16 + i]);
+              } else {
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fminf(top, x[b * 16 + i]);
+              }
+              mx = fmaxf(mx, top * f);
             }
           }
           const bool raise = mx > m + kRaiseBy || (m == -INFINITY && mx > -INFINITY);
