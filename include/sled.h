@@ -434,7 +434,7 @@ int sled_page_slots(const int32_t* n_kv, const int32_t* n_keep, const int32_t* n
  *   SLED_ROTARY_RAMP     the same with s falling from 1 to 0 along the pairs' index, between the (rounded down) index of the
  *                        pair that makes `high` turns and the (rounded up) one of `low` turns; 0 < low < high, theta above 1.
  *                        amplitude is 0.1 ln(factor) + 1 for factor above 1
- * factor, length above 0 (factor for all but PLAIN, length for the last two).  frequencies: HOST [rot_dim/2]; amplitude: HOST,
+ * rot_dim: even, 2 .. 512; factor, length above 0 (factor for all but PLAIN, length for the last two).  frequencies: HOST [rot_dim/2]; amplitude: HOST,
  * receives what cosine and sine are multiplied by (1 but for RAMP); may be NULL. */
 enum sled_rotary_scaling { SLED_ROTARY_PLAIN = 0, SLED_ROTARY_LINEAR = 1, SLED_ROTARY_BASE = 2, SLED_ROTARY_BANDS = 3, SLED_ROTARY_RAMP = 4 };
 int sled_rotary_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double length, double low, double high,

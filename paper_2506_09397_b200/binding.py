@@ -176,6 +176,23 @@ def lib():
     return _lib
 
 
+_marshal = None
+
+
+def marshal():
+    """Loads _marshal.so: what this module does for the other calls - checks and marshalling -, compiled, for calls that take the
+    GPU a few microseconds (raises if it has not been built)."""
+    global _marshal
+    if _marshal is None:
+        lib()
+        if not os.path.exists(os.path.join(_HERE, "_marshal.so")):
+            raise RuntimeError("paper_2506_09397_b200/_marshal.so is missing: build it with paper_2506_09397_b200.build.build()")
+        from . import _marshal as m
+        m.set_error(SledError)
+        _marshal = m
+    return _marshal
+
+
 def strerror(code: int) -> str:
     return lib().sled_strerror(code).decode()
 
@@ -538,7 +555,6 @@ def plan_attention(n_keys, q_tokens, n_kv_heads: int, group: int, resident_block
 # ---- operators over a paged cache: torch CUDA tensors in, enqueued on torch's current stream of the cache's device -----
 # (Devices are compared by their index: a short call takes the GPU about as long as its arguments take here.)
 _TORCH_DT = {torch.float32: SLED_F32, torch.bfloat16: SLED_BF16}
-_CACHE_DT = {**_TORCH_DT, torch.float8_e4m3fn: SLED_E4M3}
 _I32 = torch.int32
 
 
@@ -579,15 +595,15 @@ def _floats(t, what: str, name: str, dev, shape):
     return t.data_ptr()
 
 
-def _paged(what: str, k, v, page_table, n_kv, layers: bool = False, types=_TORCH_DT) -> SledPagedKv:
+def _paged(what: str, k, v, page_table, n_kv, layers: bool = False) -> SledPagedKv:
     """The cache description of a call, from K, V [n_pages, n_kv_heads, page_size, head_dim] (with a leading n_layers
-    where the operator works on all layers), page_table [n_reqs, cols] and n_kv [n_reqs]; types: those the operator takes."""
+    where the operator works on all layers), page_table [n_reqs, cols] and n_kv [n_reqs]."""
     dev, shape, k_dtype = k.get_device(), k.shape, k.dtype
     if not k.is_cuda:
         raise SledError(SLED_ERR_NO_DEVICE, f"{what} (tensors must be on a CUDA device)")
-    dtype = types.get(k_dtype)
+    dtype = _TORCH_DT.get(k_dtype)
     if dtype is None or not (len(shape) == 4 or (layers and len(shape) == 5)):
-        _refuse(what, "the cache must be fp32 or bf16" + (" or e4m3" if types is _CACHE_DT else "") + ", [n_pages, n_kv_heads, page_size, head_dim]"
+        _refuse(what, "the cache must be fp32 or bf16, [n_pages, n_kv_heads, page_size, head_dim]"
                 + (", with n_layers in front for all layers" if layers else ""))
     if not k.is_contiguous() or (v is not None and (v.dtype is not k_dtype or v.get_device() != dev or v.shape != shape or not v.is_contiguous())):
         _refuse(what, "k must be contiguous, and v like k")
@@ -614,10 +630,10 @@ def _row_stride(t, what: str, name: str, rows: int, heads: int, h: int):
     return t.stride(0) if rows > 1 else heads * h
 
 
-def _query_rows(what: str, q, out, dtype, kv, dev: int, cu_q):
+def _query_rows(what: str, q, out, k, kv, dev: int, cu_q):
     """(out, q's and out's row strides, rows, heads); rows may be apart (q a slice of a wider projection)."""
-    if q.dim() != 3 or q.dtype is not dtype or q.get_device() != dev or q.size(2) != kv.head_dim:
-        _refuse(what, f"q must be [rows, n_q_heads, head_dim] {dtype} on the cache's device")
+    if q.dim() != 3 or q.dtype is not k.dtype or q.get_device() != dev or q.size(2) != kv.head_dim:
+        _refuse(what, "q must be [rows, n_q_heads, head_dim] of the cache's type and device")
     if cu_q.dim() != 1 or cu_q.numel() != kv.n_reqs + 1:
         _refuse(what, "cu_q must be [n_reqs + 1]")
     rows, heads, h = q.shape
@@ -657,42 +673,18 @@ def attention_tree(q, k, v, page_table, n_kv, cu_q, parents=None, *, scale: floa
     A cache in 8 bits (sled_attention_scaled): k, v torch.float8_e4m3fn with k_scale, v_scale [n_pages, n_kv_heads,
     page_size / 16] fp32, as append_keys leaves them; q and out are bf16, and there are no key_weights."""
     if k_scale is not None or v_scale is not None or k.dtype is torch.float8_e4m3fn:
-        return _attention_scaled(q, k, v, page_table, n_kv, cu_q, parents, scale, out, lse, key_weights, status, k_scale, v_scale)
+        return (_marshal or marshal()).attention_scaled(q, k, v, page_table, n_kv, cu_q, parents, scale, out, lse, key_weights, status,
+                                                        k_scale, v_scale)
     what = "sled_attention_tree"
     kv = _paged(what, k, v, page_table, n_kv)
     dev = k.get_device()
-    out, q_stride, out_stride, rows, heads = _query_rows(what, q, out, k.dtype, kv, dev, cu_q)
+    out, q_stride, out_stride, rows, heads = _query_rows(what, q, out, k, kv, dev, cu_q)
     _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, int(key_weights is not None))
     _check(lib().sled_attention_tree(
         kv, q.data_ptr(), q_stride, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
         scale, out.data_ptr(), out_stride, _floats(lse, what, "lse", dev, (rows, heads)),
         _floats(key_weights, what, "key_weights", dev, k.shape[:3]), _status(status, what, dev),
         ws, ws_bytes, _stream_of(dev)), what)
-    return out
-
-
-def _check_scales(what: str, k, k_scale, v_scale, dev):
-    """Addresses of the scales of a cache in 8 bits, one for 16 slots of a page and KV head."""
-    n_pages, n_heads, page_size, _ = k.shape
-    if k.dtype is not torch.float8_e4m3fn or k_scale is None or v_scale is None:
-        _refuse(what, "an e4m3 cache comes with k_scale and v_scale, another without")
-    shape = (n_pages, n_heads, page_size // SCALE_BLOCK)
-    return _floats(k_scale, what, "k_scale", dev, shape), _floats(v_scale, what, "v_scale", dev, shape)
-
-
-def _attention_scaled(q, k, v, page_table, n_kv, cu_q, parents, scale, out, lse, key_weights, status, k_scale, v_scale):
-    what = "sled_attention_scaled"
-    kv = _paged(what, k, v, page_table, n_kv, types=_CACHE_DT)
-    dev = k.get_device()
-    if key_weights is not None:
-        _refuse(what, "weights of keys are formed over caches of 16 and 32 bits")
-    ks, vs = _check_scales(what, k, k_scale, v_scale, dev)
-    out, q_stride, out_stride, rows, heads = _query_rows(what, q, out, torch.bfloat16, kv, dev, cu_q)
-    _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads)
-    _check(lib().sled_attention_scaled(
-        kv, ks, vs, q.data_ptr(), q_stride, _ints(cu_q, what, "cu_q", dev), _ints(parents, what, "parents", dev, (rows,)), rows, heads,
-        scale, out.data_ptr(), out_stride, _floats(lse, what, "lse", dev, (rows, heads)), _status(status, what, dev), ws, ws_bytes,
-        _stream_of(dev)), what)
     return out
 
 
@@ -741,7 +733,7 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
     kv = _paged(what, k, v, page_table, n_kv)
     dev = k.get_device()
     _check_bounds(what, bounds, k)
-    out, q_stride, out_stride, rows, heads = _query_rows(what, q, out, k.dtype, kv, dev, cu_q)
+    out, q_stride, out_stride, rows, heads = _query_rows(what, q, out, k, kv, dev, cu_q)
     _held, ws, ws_bytes = _workspace(what, dev, kv, rows, heads, n_blocks)
     if blocks is not None and not blocks.is_contiguous():
         _refuse(what, "blocks must be contiguous")
@@ -754,7 +746,7 @@ def attention_blocks(q, k, v, bounds, page_table, n_kv, cu_q, *, n_blocks: int, 
 
 
 # ---- a decoding step over such a cache: places, positions, keys
-SCALE_BLOCK = 16       # slots of a page that share a scale
+SCALE_BLOCK = 16       # slots of a page that share a scale (SLED_SCALE_BLOCK)
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = range(5)
 _PAIRS = {"pairs": 0, "halves": 1}
 
@@ -768,39 +760,13 @@ class PageSlots(NamedTuple):
     n_free: torch.Tensor        # [1] int32
 
 
-def _vector(t, what: str, name: str, dev, n: int, dtype=torch.int32):
-    """Address of a contiguous vector of n entries."""
-    if t.dtype is not dtype or t.get_device() != dev or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
-        _refuse(what, f"{name} must be a contiguous {dtype} vector of {n} on cuda:{dev}")
-    return t.data_ptr()
-
-
 def page_slots(n_kv, n_new, page_table, free_pages, n_free, *, page_size: int, n_rows: int, n_keep=None, out=None, status=None) -> PageSlots:
     """sled_page_slots: places of a step's new tokens.  Request i keeps n_keep[i] (None: all) of its n_kv[i] keys and gets
     n_new[i] tokens; pages that it no longer needs go back to free_pages[:n_free], pages that it needs come off its end; its row of
     page_table [n_reqs, cols] is written.  n_rows: room for the step's tokens.  Returns n_kv and n_free for the next call, the
     tokens' row offsets cu_q, their positions and their slots (page * page_size + offset), in `out` (five such tensors, not
     those of the input) if it is given."""
-    what = "sled_page_slots"
-    _in_32_bits(what, page_size=page_size, n_rows=n_rows)
-    if not n_kv.is_cuda:
-        raise SledError(SLED_ERR_NO_DEVICE, f"{what} (tensors must be on a CUDA device)")
-    dev, n_reqs = n_kv.get_device(), n_kv.numel()
-    if n_rows < 0 or page_table.dim() != 2 or page_table.size(0) != n_reqs or free_pages.dim() != 1:
-        _refuse(what, "page_table [n_reqs, cols], free_pages [cap], n_rows not negative")
-    cols = page_table.size(1)
-    if out is None:
-        i32 = torch.empty(2 * n_reqs + n_rows + 2, dtype=_I32, device=n_kv.device).split((n_reqs, n_reqs + 1, n_rows, 1))
-        out = PageSlots(i32[0], i32[1], i32[2], torch.empty(n_rows, dtype=torch.int64, device=n_kv.device), i32[3])
-    _check(lib().sled_page_slots(
-        _vector(n_kv, what, "n_kv", dev, n_reqs), 0 if n_keep is None else _vector(n_keep, what, "n_keep", dev, n_reqs),
-        _vector(n_new, what, "n_new", dev, n_reqs), n_reqs, page_size, _ints(page_table, what, "page_table", dev),
-        page_table.stride(0) if n_reqs > 1 else cols, cols, _vector(free_pages, what, "free_pages", dev, free_pages.numel()),
-        free_pages.numel(), _vector(n_free, what, "n_free", dev, 1), _vector(out[0], what, "out.n_kv", dev, n_reqs),
-        _vector(out[4], what, "out.n_free", dev, 1), _vector(out[1], what, "out.cu_q", dev, n_reqs + 1),
-        _vector(out[2], what, "out.positions", dev, n_rows), _vector(out[3], what, "out.slots", dev, n_rows, torch.int64), n_rows,
-        _status(status, what, dev), _stream_of(dev)), what)
-    return out if type(out) is PageSlots else PageSlots(*out)
+    return PageSlots._make((_marshal or marshal()).page_slots(n_kv, n_new, page_table, free_pages, n_free, page_size, n_rows, n_keep, out, status))
 
 
 def rotary_frequencies(rot_dim: int, theta: float = 10000.0, *, scaling: int = ROTARY_PLAIN, factor: float = 1.0, length: float = 0.0,
@@ -813,60 +779,19 @@ def rotary_frequencies(rot_dim: int, theta: float = 10000.0, *, scaling: int = R
     return torch.from_numpy(f), amplitude.value
 
 
-def _heads(t, out, what: str, name: str, dev, dtype, rows: int, h: int):
-    if t.dim() != 3 or t.dtype is not dtype or t.get_device() != dev or t.size(0) != rows or t.size(2) != h or (t.stride(2) != 1 and t.numel()):
-        _refuse(what, f"{name} must be [rows, heads, head_dim] {dtype} on cuda:{dev}, heads contiguous")
-    if out is None:
-        out = torch.empty(t.shape, dtype=dtype, device=t.device)
-    elif out.shape != t.shape or out.dtype is not dtype or out.get_device() != dev or (out.stride(2) != 1 and out.numel()):
-        _refuse(what, f"{name}_out must be like {name}")
-    return out, SledHeads(t.data_ptr(), t.stride(0), t.stride(1), out.data_ptr(), out.stride(0), out.stride(1), t.size(1))
-
-
 def rotary(q, k, positions, frequencies, *, style: str = "pairs", amplitude: float = 1.0, inverse: bool = False, q_out=None, k_out=None):
     """sled_rotary: queries and keys [rows, heads, head_dim] (k may be None; rows and heads may be apart, as in slices of a
     projection) turned by positions [rows] int32 times frequencies (fp64, one per pair; the pairs are those of the first
     2 * len(frequencies) dimensions).  style "pairs": (2i, 2i+1); "halves": (i, i + len(frequencies)).  inverse: turned back, which is the
     gradient.  q_out, k_out may be q and k.  Returns (q_out, k_out)."""
-    what = "sled_rotary"
-    if not q.is_cuda:
-        raise SledError(SLED_ERR_NO_DEVICE, f"{what} (tensors must be on a CUDA device)")
-    dev, dtype = q.get_device(), q.dtype
-    if dtype not in _TORCH_DT or q.dim() != 3 or style not in _PAIRS:
-        _refuse(what, "q must be [rows, heads, head_dim], fp32 or bf16; style pairs or halves")
-    rows, _, h = q.shape
-    q_out, qh = _heads(q, q_out, what, "q", dev, dtype, rows, h)
-    kh = None
-    if k is not None:
-        k_out, kh = _heads(k, k_out, what, "k", dev, dtype, rows, h)
-    half = frequencies.numel()
-    _check(lib().sled_rotary(qh, kh, rows, h, _TORCH_DT[dtype], _vector(positions, what, "positions", dev, rows),
-                             _vector(frequencies, what, "frequencies", dev, half, torch.float64), 2 * half, _PAIRS[style], amplitude,
-                             int(inverse), _stream_of(dev)), what)
-    return q_out, k_out
+    return (_marshal or marshal()).rotary(q, k, positions, frequencies, _PAIRS.get(style, -1), amplitude, inverse, q_out, k_out)
 
 
 def append_keys(k, v, k_cache, v_cache, page_table, n_kv, cu_q, *, k_scale=None, v_scale=None, status=None) -> None:
     """sled_append_keys: rows cu_q[i] .. of k and v [rows, n_kv_heads, head_dim] become request i's newest keys (n_kv counts them) in
     the cache [n_pages, n_kv_heads, page_size, head_dim]: as they are in one of their type, as codes in one of
     torch.float8_e4m3fn, with k_scale and v_scale [n_pages, n_kv_heads, page_size / 16] fp32."""
-    what = "sled_append_keys"
-    kv = _paged(what, k_cache, v_cache, page_table, n_kv, types=_CACHE_DT)
-    dev, rows = k_cache.get_device(), k.size(0) if k.dim() else 0
-    if k.dim() != 3 or k.dtype not in _TORCH_DT or k.get_device() != dev or k.shape != (rows, kv.n_kv_heads, kv.head_dim):
-        _refuse(what, f"k must be [rows, n_kv_heads, head_dim], fp32 or bf16, on cuda:{dev}")
-    if v.shape != k.shape or v.dtype is not k.dtype or v.get_device() != dev:
-        _refuse(what, "v must be like k")
-    if kv.dtype != SLED_E4M3 and k.dtype is not k_cache.dtype:
-        _refuse(what, "rows of another type go into a cache of 8 bits only")
-    ks = vs = 0
-    if kv.dtype == SLED_E4M3 or k_scale is not None or v_scale is not None:
-        ks, vs = _check_scales(what, k_cache, k_scale, v_scale, dev)
-    if cu_q.dim() != 1 or cu_q.numel() != kv.n_reqs + 1:
-        _refuse(what, "cu_q must be [n_reqs + 1]")
-    _check(lib().sled_append_keys(kv, ks, vs, k.data_ptr(), _row_stride(k, what, "k", rows, kv.n_kv_heads, kv.head_dim), v.data_ptr(),
-                                  _row_stride(v, what, "v", rows, kv.n_kv_heads, kv.head_dim), _TORCH_DT[k.dtype],
-                                  _ints(cu_q, what, "cu_q", dev), rows, _status(status, what, dev), _stream_of(dev)), what)
+    (_marshal or marshal()).append_keys(k, v, k_cache, v_cache, page_table, n_kv, cu_q, k_scale, v_scale, status)
 
 
 def check_status(status) -> None:

@@ -1,15 +1,17 @@
-"""Builds the CUDA library (libsled.so) in-tree with nvcc for sm_100a."""
+"""Builds the CUDA library (libsled.so) in-tree with nvcc for sm_100a, and the compiled part of the binding (_marshal.so)."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsled.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["engine.cu", "kernels_small.cu", "attention.cu", "attention_mma.cu", "attention_tc.cu", "accept.cu", "gemm_tc.cu", "kv_manager.cpp", "planner.cpp", "no_alloc.cu",
            "paged_attention.cu", "paged_mma.cu", "paged_tc.cu", "paged_f32.cu", "paged_weigh.cu", "paged_blocks.cu", "paged_evict.cu", "paged_slots.cu", "rotary.cu", "paged_append.cu", "paged_scaled.cu", "paged_scaled_few.cu", "paged_scaled_tc.cu", "paged_api.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -57,7 +59,24 @@ def build(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".{os.getpid()}.tmp"
         run([nvcc, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"])
         os.replace(tmp, LIB)
+    build_marshal(force, run)
     return LIB
+
+
+def build_marshal(force: bool, run) -> None:
+    """The binding's argument marshalling, against torch's headers; it finds libsled.so beside itself."""
+    source = os.path.join(CSRC, "marshal.cpp")
+    if not force and not _stale(MARSHAL, [source, os.path.join(HERE, "..", "include", "sled.h")]):
+        return
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include") if os.path.isabs(_nvcc()) else "/usr/local/cuda/include"
+    tmp = MARSHAL + f".{os.getpid()}.tmp"
+    run(["g++", "-std=c++17", "-O2", "-shared", "-fPIC", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+         "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+         "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda, source, "-o", tmp, "-L" + os.path.join(root, "lib"), "-ltorch_python",
+         "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L" + HERE, "-l:libsled.so", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, MARSHAL)
 
 
 if __name__ == "__main__":

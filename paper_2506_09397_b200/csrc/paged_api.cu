@@ -320,7 +320,7 @@ int sled_page_slots(const int32_t* n_kv, const int32_t* n_keep, const int32_t* n
 
 int sled_rotary_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double length, double low, double high,
                             double* frequencies, double* amplitude) {
-  if (rot_dim < 2 || rot_dim % 2 || !frequencies || !(theta > 0) || !std::isfinite(theta)) return SLED_ERR_ARG;
+  if (rot_dim < 2 || rot_dim > 512 || rot_dim % 2 || !frequencies || !(theta > 0) || !std::isfinite(theta)) return SLED_ERR_ARG;
   if (scaling < SLED_ROTARY_PLAIN || scaling > SLED_ROTARY_RAMP) return SLED_ERR_ARG;
   if (scaling != SLED_ROTARY_PLAIN && (!(factor > 0) || !std::isfinite(factor))) return SLED_ERR_ARG;
   if (scaling == SLED_ROTARY_BASE && rot_dim == 2) return SLED_ERR_ARG;
