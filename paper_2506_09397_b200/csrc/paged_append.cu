@@ -20,7 +20,7 @@ namespace sled {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMany = 64;            // rows of a block's span for long calls
+constexpr int kMany = 32;            // rows of a block's span for long calls
 
 // eight elements, as they lie in memory
 template <typename T>
@@ -46,7 +46,9 @@ struct Eight {
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = make_uint4(0, 0, 0, 0);
   }
-  // bits of the largest of `top` and all |x|; infinities and NaN count as what their bits say, no less than 0x7f800000
+  // the largest of `top` and the bits of all |x|, of bf16 in pairs; largest_of(top): the bits as those of a float.  Infinities and
+  // NaN count as what their bits say, no less than 0x7f800000
+  static __device__ __forceinline__ uint32_t largest_of(uint32_t top) { return sizeof(T) == 4 ? top : max(top << 16, top & 0xffff0000u); }
   __device__ __forceinline__ uint32_t largest(uint32_t top) const {
     const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
     if constexpr (sizeof(T) == 4) {
@@ -54,10 +56,8 @@ struct Eight {
       for (int i = 0; i < 8; ++i) top = max(top, u[i] & 0x7fffffffu);
       return top;
     } else {
-      uint32_t two = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) two = __vmaxu2(two, u[i] & 0x7fff7fffu);
-      return max(top, max(two << 16, two & 0xffff0000u));
+      uint32_t two = __vimax3_u16x2(u[0] & 0x7fff7fffu, u[1] & 0x7fff7fffu, top);      // (of 16 bits `top` is a pair)
+      return __vimax3_u16x2(u[2] & 0x7fff7fffu, u[3] & 0x7fff7fffu, two);
     }
   }
   __device__ __forceinline__ float at(int i) const {
@@ -84,6 +84,19 @@ __device__ __forceinline__ uint32_t code_pair(float x0, float x1) {
 }
 __device__ __forceinline__ float decode(uint32_t c) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(c), __NV_E4M3))); }
 
+// req_of_row by a warp, in rounds of 32 samples: a dependent load for a factor of 32 instead of one for a factor of 2
+__device__ __forceinline__ int req_of_row_by_warp(const int32_t* cu_q, int n_reqs, int t) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = n_reqs;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const bool before = lane == 0 || (at < hi && cu_q[at] <= t);
+    lo += (__popc(__ballot_sync(0xffffffffu, before)) - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+
 // A cache block that receives keys: the row of the call that holds the first of them, the block's page and first slot there, how
 // many older keys it has and how many new ones it gets.
 struct Target {
@@ -104,10 +117,12 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const PagedCache c, co
   PagedRows r{};
   r.cu_q = a.cu_q;
   r.T = a.T;
+  int alone = 0;
+  if (kSpan == 1 && threadIdx.x < 32) alone = req_of_row_by_warp(a.cu_q, c.n_reqs, static_cast<int>(t0));
   if (threadIdx.x < kSpan) {
     const int64_t t = t0 + threadIdx.x;
     if (t < a.T) {
-      const int i = req_of_row(a.cu_q, c.n_reqs, static_cast<int>(t));
+      const int i = kSpan == 1 ? alone : req_of_row(a.cu_q, c.n_reqs, static_cast<int>(t));
       const ReqView v = req_view(c, r, i);
       if (v.ok && t >= v.row0 && t < v.row0 + v.m) {
         const int x = v.n - v.m + static_cast<int>(t - v.row0), off = x % kScaleBlock;
@@ -136,13 +151,19 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const PagedCache c, co
     return Task{targets[k], rest >> 1, (rest & 1) != 0};
   };
   auto bring = [&](const Task& k, Eight<T>* y) {
-    const int64_t stride = k.is_v ? a.v_stride : a.k_stride;
-    const T* src = reinterpret_cast<const T*>(k.is_v ? a.v : a.k) + k.to.row * stride + static_cast<int64_t>(k.g) * H + col;
+    const int64_t stride = k.is_v ? a.v_stride : a.k_stride, step = kAtOnce * stride;
+    const int e0 = sub_row - k.to.off;                 // of the new rows
+    const T* src = reinterpret_cast<const T*>(k.is_v ? a.v : a.k) + k.to.row * stride + static_cast<int64_t>(k.g) * H + col + e0 * stride;
+    if (whole && k.to.count == kScaleBlock) {          // a whole block, of aligned rows
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      const int e = p * kAtOnce + sub_row - k.to.off;                 // of the new rows
-      if (e >= 0 && e < k.to.count) y[p].load(src + e * stride, whole);
-      else y[p].zero();
+      for (int p = 0; p < kPasses; ++p) y[p].load(src + p * step, true);
+    } else {
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        const int e = p * kAtOnce + e0;
+        if (e >= 0 && e < k.to.count) y[p].load(src + p * step, whole);
+        else y[p].zero();
+      }
     }
   };
   auto put = [&](const Task& k, const Eight<T>* y) {
@@ -164,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const PagedCache c, co
       uint32_t top = 0;            // bits of the largest |x|
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) top = y[p].largest(top);
-      top = __reduce_max_sync(0xffffffffu, top);
+      top = __reduce_max_sync(0xffffffffu, Eight<T>::largest_of(top));
       bool plain = top < 0x7f800000u;
       if (!plain) {                // without infinities and NaN
         top = 0;
@@ -179,25 +200,33 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const PagedCache c, co
       }
       const float now = fmaxf(least_scale(top), before), inv = 1.f / now;
       plain = plain && (__float_as_uint(now) & 0x7fffffu) == 0;      // a scale of the caller's own may be no power of two: true quotients
+      uint8_t* mine = to + sub_row * H;
+      auto codes = [&](int p) {
+        uint32_t two[4];
 #pragma unroll
-      for (int p = 0; p < kPasses; ++p) {
-        const int e = p * kAtOnce + sub_row - off;
-        if (e < 0 || e >= count) continue;
-        uint2 w = make_uint2(0, 0);
-        if (plain) {
+        for (int i = 0; i < 4; ++i) two[i] = code_pair(y[p].at(2 * i) * inv, y[p].at(2 * i + 1) * inv);
+        return make_uint2(__byte_perm(two[0], two[1], 0x5410), __byte_perm(two[2], two[3], 0x5410));
+      };
+      if (plain && count == kScaleBlock) {
 #pragma unroll
-          for (int i = 0; i < 8; i += 2) {
-            const uint32_t two = code_pair(y[p].at(i) * inv, y[p].at(i + 1) * inv) << (i & 2) * 8;
-            if (i < 4) w.x |= two; else w.y |= two;
+        for (int p = 0; p < kPasses; ++p) *reinterpret_cast<uint2*>(mine + p * kAtOnce * H) = codes(p);
+      } else {
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+          const int e = p * kAtOnce + sub_row - off;
+          if (e < 0 || e >= count) continue;
+          uint2 w = make_uint2(0, 0);
+          if (plain) {
+            w = codes(p);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t one = code(__fdiv_rn(y[p].at(i), now)) << (i & 3) * 8;
+              if (i < 4) w.x |= one; else w.y |= one;
+            }
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t one = code(__fdiv_rn(y[p].at(i), now)) << (i & 3) * 8;
-            if (i < 4) w.x |= one; else w.y |= one;
-          }
+          *reinterpret_cast<uint2*>(mine + p * kAtOnce * H) = w;
         }
-        *reinterpret_cast<uint2*>(to + static_cast<int64_t>(p * kAtOnce + sub_row) * H) = w;
       }
       if (off > 0 && now != before) {         // older keys of the block follow its scale
 #pragma unroll 1
@@ -248,7 +277,8 @@ int launch(const PagedCache& c, const NewRows& a, cudaStream_t s) {
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
   // A block per row (most of them then find that another row begins their cache block) while that fills the GPU a few times;
-  // a block per 64 rows beyond.
+  // a block per 32 rows beyond
+  // (16, 32, 64 rows: 12 prompts of 2000 .. 16384 tokens in 8 bits 151, 141.5, 141 us, 20 chunks of 200 .. 2000 as they are 13.9, 14.3, 18.5).
   if (a.T <= 16 * sms)
     SLED_LAUNCH_PDL((append_kernel<T, H, kCodes, 1>), dim3(a.T), dim3(kThreads), 0, s, c, a, whole);
   else

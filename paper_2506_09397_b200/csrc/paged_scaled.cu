@@ -565,7 +565,7 @@ int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedR
   // by the rows per request and KV head, on average
   const int64_t rows = static_cast<int64_t>(r.T) * r.group;
   if (rows <= 8LL * c.n_reqs) return launch_scaled_few(c, sc, r, 1, ws, s);
-  if (c.h >= 64 && rows > 24LL * c.n_reqs) return launch_scaled_tc(c, sc, r, ws, s);
+  if (c.h >= 64 && rows > 32LL * c.n_reqs) return launch_scaled_tc(c, sc, r, ws, s);
   if (c.h == 128) return launch_h<128>(c, sc, r, ws, s);
   return c.h == 64 ? launch_h<64>(c, sc, r, ws, s) : launch_h<32>(c, sc, r, ws, s);
 }
