@@ -13,7 +13,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsled.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["engine.cu", "kernels_small.cu", "attention.cu", "attention_mma.cu", "attention_tc.cu", "accept.cu", "gemm_tc.cu", "kv_manager.cpp", "planner.cpp", "no_alloc.cu",
-           "paged_attention.cu", "paged_mma.cu", "paged_tc.cu", "paged_f32.cu", "paged_weigh.cu", "paged_blocks.cu", "paged_evict.cu", "paged_slots.cu", "rotary.cu", "paged_append.cu", "paged_scaled.cu", "paged_scaled_few.cu", "paged_scaled_tc.cu", "paged_api.cu"]
+           "paged_attention.cu", "paged_mma.cu", "paged_tc.cu", "paged_f32.cu", "paged_weigh.cu", "paged_blocks.cu", "paged_evict.cu", "paged_slots.cu", "rotary.cu", "paged_append.cu", "paged_scaled.cu", "paged_scaled_tc.cu", "paged_api.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
 

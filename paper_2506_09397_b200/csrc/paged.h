@@ -133,13 +133,10 @@ struct CacheScales {
 };
 int64_t paged_scaled_workspace(int h);
 int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s);
-// the same for units of up to 8 * groups rows (groups 1 or 2; paged_scaled_few.cu)
-constexpr int kFewBlocks = 480;        // three on each of up to 160 SMs
-int64_t scaled_few_workspace(int h);
+constexpr int kScaledBlocks = 480;     // three on each of up to 160 SMs
 // the same on the 5th-generation tensor cores, head_dim 64 or 128, for requests with many query rows (paged_scaled_tc.cu); workspace:
 // paged_tc_workspace
 int launch_scaled_tc(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s);
-int launch_scaled_few(const PagedCache& c, const CacheScales& sc, const PagedRows& r, int groups, char* ws, cudaStream_t s);
 
 constexpr int kMaxTreeNodes = 128;   // nodes of one request's tree (chains have no limit)
 

@@ -1,4 +1,5 @@
-// Attention over a paged cache of e4m3 codes with a scale for every block of 16 slots and KV head, on the warp-level tensor cores.
+// Attention over a paged cache of e4m3 codes with a scale for every block of 16 slots and KV head, on the warp-level tensor cores:
+// decoding and drafts, and every batch of head_dim 32.
 //
 // For a query row r (token, head) and the keys x it sees, of block b: s_x = scale ks_b (q . c_x), o = sum p_x vs_b d_x over the
 // codes c of K and d of V, p the softmax of s.  One pass over the keys with the running maximum m of s and sum l of 2^(s - m);
@@ -9,13 +10,18 @@
 // reference of their own, u = max (s_x + log2 vs_b) so far: they are as large as fp16 allows whatever the blocks' scales are,
 // 11 bits of each down to 2^-29 of the largest.  u is joined with m at the end of a unit.
 //
-// A unit is the query rows that share a KV head (up to 64 of them): the M side of m16n8k16 products, so a cached key is read
-// once for all.  With up to 16 (32) rows the four computing warps split every 64-key tile four (two) ways - 16 keys, one block of
-// scales, each - and merge at the end of the unit; with more, every warp has 16 rows of its own.  The order of the dimensions in
-// the first product is free as long as both operands agree: a lane takes H / 4 consecutive bytes of a key, whole 16-byte
-// loads, and the queries are laid out to match.  V goes through transposing matrix loads of 16-bit units - two dimensions of
-// a key -, a byte permutation parts them into the even and the odd dimensions of two keys.  A fifth warp brings the tiles in by
-// TMA and their scales with them, looked up a round ahead.  Work is handed out as paged_schedule.cuh says.
+// The keys are the M side of m16n8k16 products and the rows the N side, so that eight rows cost half of what sixteen do -
+// products, exponentials, registers:
+//     S^T (16 keys x 8 rows) = C Q^T,    O^T (16 dimensions x 8 rows) += D^T P^T
+// The order of the dimensions in the first product is free as long as both operands agree: a lane takes H / 4 consecutive bytes of
+// a key, whole 16-byte loads, and the queries are laid out to match.  D^T comes from transposing matrix loads of 16-bit units (two
+// dimensions of a key; a byte permutation parts them, the even and the odd dimensions become the two halves of the M side), P^T
+// by a transposition in registers.
+//
+// A unit is the rows that share a KV head, up to 8 (kGroups 1) or 32 of them.  Its keys come in stages of 32, each read by one
+// warp, or by two that have 16 rows each where the unit has more than 16; the four computing warps take stages in turn, know
+// nothing of each other until the end of the unit, and merge there.  A fifth warp brings the stages in by TMA, their scales with
+// them, looked up a round ahead.  Work is handed out as paged_schedule.cuh says.
 #include "gemm_tc.h"
 #include "kernels.h"
 #include "paged_scaled.cuh"
@@ -24,395 +30,265 @@ namespace sled {
 
 namespace {
 
+constexpr int kWarps = 4;
+constexpr int kStageKeys = 32;
 
-// A stage holds K, then V: four groups of 16 keys, rows of 128 bytes (of one, two or four keys); the 16-byte chunk c of a row
-// lies at c ^ (row & 7).
-template <int H>
-struct Smem {
+// A stage holds K, then V: two groups of 16 keys, rows of 128 bytes (of one, two or four keys); the 16-byte chunk c of a row lies
+// at c ^ (row & 7).
+template <int H, int kGroups>
+struct Few {
+  static constexpr int kHalves = kGroups;                           // sixteen rows of a unit, or its eight
+  static constexpr int kWarpRows = 8 * kGroups, kRows = kHalves * kWarpRows;
+  static constexpr int kReaders = kHalves;                          // warps that may read a stage
   static constexpr int kKeysPerRow = 128 / H;
   static constexpr int kCopy = 16 * H;                              // bytes of 16 keys
   static constexpr int kGroup = kCopy < 1024 ? 1024 : kCopy;        // whole rounds of the swizzle
-  static constexpr int kHalf = 4 * kGroup;
+  static constexpr int kHalf = 2 * kGroup;
   static constexpr int kStage = 2 * kHalf;
-  static constexpr int kStages = H == 128 ? 6 : 8;
-  static constexpr int kMergePitch = 48;                            // 32 dimensions of a row; four words of two rows meet 32 banks
-  static constexpr int kMerge = 64 * (kMergePitch + 2) * 4;
-  static constexpr int kOffMerge = kStages * kStage;
-  static constexpr int kOffTree = kOffMerge + kMerge;
-  static constexpr int kOffScale = kOffTree + kMaxTreeNodes * (kMaxTreeNodes / 32) * 4;     // [stage][K, V][4]
-  static constexpr int kOffBar = kOffScale + kStages * 32;
+  static constexpr int kStages = H == 128 ? 8 : 12;
+  static constexpr int kBlocks = kGroups == 1 ? 3 : 2;              // on an SM
+  static constexpr int kDims = 32;                                  // of a round of the merge
+  static constexpr int kPitch = kDims + 4;                          // four rows two apart meet 32 banks
+  static constexpr int kOffQ = kStages * kStage;                    // [8 rows][two products][lane] 16 bytes
+  static constexpr int kOffMerge = kOffQ + kRows / 8 * (H / 32) * 512;
+  static constexpr int kOffMl = kOffMerge + kWarps * kWarpRows * kPitch * 4;
+  static constexpr int kOffRow = kOffMl + kWarps * kWarpRows * 8;   // of a row: what turns products into scores, its node
+  static constexpr int kOffTree = kOffRow + kRows * 8;
+  static constexpr int kOffScale = kOffTree + kMaxTreeNodes * (kMaxTreeNodes / 32) * 4;     // [stage][K, V][2]
+  static constexpr int kOffBar = kOffScale + kStages * 16;
   static constexpr int kTotal = kOffBar + 16 * kStages + 1024;      // alignment slack
 };
-static_assert(Smem<128>::kTotal + 1024 + 256 <= 228 * 1024 / 2, "two blocks on an SM");
+// A place of the ring is always the same warp's within a stretch of a unit, which has then seen all its phases: the parity that it
+// waits for cannot be that of the phase before the last.  (Copies need not arrive in the order in which they were issued.)
+static_assert(Few<128, 1>::kStages % kWarps == 0 && Few<64, 1>::kStages % kWarps == 0, "whole rounds of the warps");
+static_assert(3 * (Few<128, 1>::kTotal + 1024 + 512) <= 228 * 1024 && 2 * (Few<128, 2>::kTotal + 1024 + 512) <= 228 * 1024, "blocks of an SM");
 
-// shared memory address of 16-byte chunk c of a key of the tile
-template <int H>
+template <int H, int G>
 __device__ __forceinline__ uint32_t at(uint32_t base, int key, int c) {
-  constexpr int P = Smem<H>::kKeysPerRow;
+  constexpr int P = Few<H, G>::kKeysPerRow;
   const int row = (key & 15) / P;
-  return base + (key >> 4) * Smem<H>::kGroup + row * 128 + (((key % P * (H / 16) + c) ^ (row & 7)) << 4);
+  return base + (key >> 4) * Few<H, G>::kGroup + row * 128 + (((key % P * (H / 16) + c) ^ (row & 7)) << 4);
 }
 
-struct Ring {
-  uint32_t base, full, empty;
-  int it;                 // tiles so far
+// The line of tiles with units of up to `rows` rows.
+struct FewLine : AttentionLine {
+  __device__ __forceinline__ FewLine(const PagedCache& c, const PagedRows& r, int rows) : AttentionLine{c, r, 0, rows, kTile} {}
+  __device__ __forceinline__ int min_share() const { return kMinMmaShare; }
+  __device__ __forceinline__ ReqWork operator()(int i) const {
+    ReqWork w = AttentionLine::operator()(i);
+    if (w.units > 0) w.weight = unit_weight(16, 64, w.tiles, 80);
+    return w;
+  }
 };
 
-struct UnitRows {
-  int req, row0, m;       // the request's rows
-  int group, g;
-  int first, count;       // rows of the unit's block: first .. first + count - 1
-  int prefix, end;        // positions below `prefix` are seen by everybody; there are `end` of them
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {     // of an 8 x 8 matrix of 16-bit elements
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+struct FewRows {
+  int req, row0, group, g, first, count, prefix, end;
   __device__ __forceinline__ int token(int r) const { return quotient(first + r, group); }
-  __device__ __forceinline__ int head(int r) const { return g * group + first + r - quotient(first + r, group) * group; }
+  __device__ __forceinline__ int head(int r, int token) const { return g * group + first + r - token * group; }
 };
 
+struct FewRing {
+  uint32_t base, full, empty;
+  int it;                 // stages so far
+};
 
-// One stretch of a unit: MT warps cover the rows, 4 / MT the keys of a tile.
-template <int H, int MT>
-__device__ __forceinline__ void consume(const PagedRows& r, const UnitRows& u, const Segment& sg, Ring& ring, volatile int* stop,
-                                        const float* scales, float* merge, const uint32_t* tree, const ScaledParts& parts) {
-  using S = Smem<H>;
-  constexpr int KS = H / 16, DC = H / 16, NT = 2 * MT;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
-  const int mt = warp % MT, share = warp / MT, key_off = share * 16 * MT;
-  const int r_lo = mt * 16 + gq, r_hi = r_lo + 8;
-  const bool active = mt * 16 < u.count, v_lo = r_lo < u.count, v_hi = r_hi < u.count;
-  const int j_lo = v_lo ? u.token(r_lo) : 0, j_hi = v_hi ? u.token(r_hi) : 0;
-  const int h_lo = v_lo ? u.head(r_lo) : 0, h_hi = v_hi ? u.head(r_hi) : 0;
+// What a warp holds of its rows: outputs - dimensions 16 c + 2 gq (0, 1) and + 1 (2, 3) of rows 8 n + 2 tq (0, 2) and + 1 (1, 3) -
+// and of rows 8 n + 2 tq, + 1 (place 2 n, 2 n + 1) maxima and sums, factors, nodes.
+template <int H, int G>
+struct FewState {
+  float o[G][H / 16][4];
+  RowState st[2 * G];
+  float f[2 * G];
+  int node[2 * G];
+};
 
-  uint32_t q_lo[H / 8], q_hi[H / 8];      // of product ks: words 2 ks and 2 ks + 1
-  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(r.q) + tq * (H / 4);
-  const float f_lo = query_row<H>(q + (u.row0 + j_lo) * r.q_stride + static_cast<int64_t>(h_lo) * H, v_lo, q_lo) * (r.scale * kLog2e);
-  const float f_hi = query_row<H>(q + (u.row0 + j_hi) * r.q_stride + static_cast<int64_t>(h_hi) * H, v_hi, q_hi) * (r.scale * kLog2e);
-  float o[2 * DC][4];       // [2 c]: dimensions 16 c + 4 tq + {0, 2} of both rows, [2 c + 1]: + {1, 3}
+// A stage of 32 keys, k0 the position of the first.  kMasked: some row may not see some of them.
+template <int H, int G, bool kMasked>
+__device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool has_tree, const uint32_t* tree, uint32_t kb, float4 blocks, const uint4* q, int k0) {
+  using S = Few<H, G>;
+  const uint32_t vb = kb + S::kHalf;
+  const int lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
+  const float ks[2] = {blocks.x, blocks.y}, vs[2] = {blocks.z, blocks.w};
+  const float lv = fmaxf(__log2f(fabsf(vs[0])), __log2f(fabsf(vs[1])));
+  float sc[2][G][4];       // keys 16 m + gq (0, 1), + 8 (2, 3)
+  {
+    uint32_t w[2][2][H / 16];      // all of the stage's K: the loads run side by side
 #pragma unroll
-  for (int i = 0; i < 2 * DC; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  RowState lo, hi;
-  bool failed = false;
-
-  for (int tile = sg.t0; tile < sg.t1; ++tile, ++ring.it) {
-    const int st = ring.it % S::kStages;
-    if (*stop || !mbar_wait(ring.full + 8 * st, (ring.it / S::kStages) & 1, stop)) { *stop = 1; failed = true; break; }
-    const int k0 = tile * kTile + key_off;    // position of this warp's first key
-    if (active && k0 < u.end) {
-      const uint32_t kb = ring.base + st * S::kStage, vb = kb + S::kHalf;
-      float ks[MT], vs[MT], lv = -INFINITY;
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int kt = 0; kt < MT; ++kt) {
-        ks[kt] = scales[st * 8 + key_off / 16 + kt];
-        vs[kt] = scales[st * 8 + 4 + key_off / 16 + kt];
-        lv = fmaxf(lv, __log2f(fabsf(vs[kt])));
-      }
-      float sc[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
-        uint32_t w[H / 16];
-        const int key = key_off + nt * 8 + gq;
+      for (int e = 0; e < 2; ++e) {
+        const int key = m * 16 + e * 8 + gq;
+        uint32_t* to = w[m][e];
         if constexpr (H == 32) {
-          asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at<H>(kb, key, tq >> 1) + (tq & 1) * 8));
+          asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(to[0]), "=r"(to[1]) : "r"(at<H, G>(kb, key, tq >> 1) + (tq & 1) * 8));
         } else {
 #pragma unroll
           for (int i = 0; i < H / 64; ++i)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
-                         : "r"(at<H>(kb, key, tq * (H / 64) + i)));
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(to[4 * i]), "=r"(to[4 * i + 1]), "=r"(to[4 * i + 2]), "=r"(to[4 * i + 3])
+                         : "r"(at<H, G>(kb, key, tq * (H / 64) + i)));
         }
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          const uint32_t a[4] = {q_lo[2 * s], q_hi[2 * s], q_lo[2 * s + 1], q_hi[2 * s + 1]};
-          mma_half(sc[nt], a, half2_of(w[s]), half2_of_upper(w[s]));
+        for (int n = 0; n < G; ++n) sc[m][n][e] = sc[m][n][2 + e] = 0.f;
+      }
+#pragma unroll
+    for (int s = 0; s < H / 16; s += 2) {
+      uint4 y[G];
+#pragma unroll
+      for (int n = 0; n < G; ++n) y[n] = q[(n * (H / 32) + s / 2) * 32];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          const uint32_t x[4] = {half2_of(w[m][0][s + k]), half2_of(w[m][1][s + k]), half2_of_upper(w[m][0][s + k]), half2_of_upper(w[m][1][s + k])};
+#pragma unroll
+          for (int n = 0; n < G; ++n) mma_half(sc[m][n], x, k ? y[n].z : y[n].x, k ? y[n].w : y[n].y);
         }
-      }
+    }
+  }
+  // V: 16 keys x 32 dimensions a load, two loads under way
+  constexpr int kLoads = 2 * (H / 32);
+  uint32_t vw[2][4];
+  auto load_v = [&](int i) {
+    const int m = i / (H / 32), d = i % (H / 32);
+    uint32_t* b = vw[i & 1];
+    ldmatrix_x4_trans(at<H, G>(vb, m * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), d * 2 + (lane >> 4)), b[0], b[1], b[2], b[3]);
+  };
+  load_v(0);
+  load_v(1);
+  bool change = false;
+  float al[2 * G];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float x = f_lo * ks[nt >> 1], y = f_hi * ks[nt >> 1];
-        sc[nt][0] *= x;
-        sc[nt][1] *= x;
-        sc[nt][2] *= y;
-        sc[nt][3] *= y;
-      }
-      // Everybody sees a tile inside the prefix.  In the others a key that a row does not see, or that does not exist,
-      // becomes -infinity whatever it is (a comparison, not a sum, so that NaN does not survive).
-      const bool masked = k0 + 16 * MT > u.prefix;
-      if (masked) {
+  for (int n = 0; n < G; ++n)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+    for (int e = 0; e < 2; ++e) {
+      float top = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int x = k0 + nt * 8 + 2 * tq + (e & 1), j = e < 2 ? j_lo : j_hi;
-            bool seen = x < u.end;
-            if (x >= u.prefix && seen) {
-              const int a = x - u.prefix;
-              if (r.parents) seen = (tree[j * (kMaxTreeNodes / 32) + (a >> 5)] >> (a & 31)) & 1u;
-              else seen = a <= j;
-            }
-            if (!seen) sc[nt][e] = -INFINITY;
+      for (int m = 0; m < 2; ++m) {
+        const float x = a.f[2 * n + e] * ks[m];
+        sc[m][n][e] *= x;
+        sc[m][n][2 + e] *= x;
+        if constexpr (kMasked) {      // a key that the row does not see, or that does not exist, becomes -infinity whatever it is
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const int key = k0 + m * 16 + z * 8 + gq, of = key - u.prefix, j = a.node[2 * n + e];
+            bool seen = key < u.end;
+            if (of >= 0 && seen) seen = has_tree ? (tree[j * (kMaxTreeNodes / 32) + (of >> 5)] >> (of & 31)) & 1u : of <= j;
+            if (!seen) sc[m][n][2 * z + e] = -INFINITY;
           }
-      }
-      float mx_lo = -INFINITY, mx_hi = -INFINITY;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        mx_lo = fmaxf(mx_lo, fmaxf(sc[nt][0], sc[nt][1]));
-        mx_hi = fmaxf(mx_hi, fmaxf(sc[nt][2], sc[nt][3]));
-      }
-      mx_lo = fmaxf(mx_lo, __shfl_xor_sync(0xffffffffu, mx_lo, 1));
-      mx_lo = fmaxf(mx_lo, __shfl_xor_sync(0xffffffffu, mx_lo, 2));
-      mx_hi = fmaxf(mx_hi, __shfl_xor_sync(0xffffffffu, mx_hi, 1));
-      mx_hi = fmaxf(mx_hi, __shfl_xor_sync(0xffffffffu, mx_hi, 2));
-      const float al_lo = lo.take(mx_lo, lv), al_hi = hi.take(mx_hi, lv);
-      if (__any_sync(0xffffffffu, al_lo != 1.f || al_hi != 1.f)) {
-#pragma unroll
-        for (int i = 0; i < 2 * DC; ++i) { o[i][0] *= al_lo; o[i][1] *= al_lo; o[i][2] *= al_hi; o[i][3] *= al_hi; }
-      }
-      const float unit_lo = lo.unit_weight(), unit_hi = hi.unit_weight();
-      uint32_t pf[MT][4];   // the numerators as A operand; their sum is taken before the rounding
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p0 = exp2_approx(sc[nt][0] - lo.ref), p1 = exp2_approx(sc[nt][1] - lo.ref);
-        float p2 = exp2_approx(sc[nt][2] - hi.ref), p3 = exp2_approx(sc[nt][3] - hi.ref);
-        lo.l += p0 + p1;
-        hi.l += p2 + p3;
-        const float w_lo = lo.scaled(unit_lo, vs[nt >> 1]), w_hi = hi.scaled(unit_hi, vs[nt >> 1]);
-        if (masked) {       // a scale that is no number reaches the rows that see its block, not the others
-          p0 = sc[nt][0] == -INFINITY ? 0.f : p0 * w_lo;
-          p1 = sc[nt][1] == -INFINITY ? 0.f : p1 * w_lo;
-          p2 = sc[nt][2] == -INFINITY ? 0.f : p2 * w_hi;
-          p3 = sc[nt][3] == -INFINITY ? 0.f : p3 * w_hi;
-        } else {
-          p0 *= w_lo;
-          p1 *= w_lo;
-          p2 *= w_hi;
-          p3 *= w_hi;
         }
-        pf[nt >> 1][(nt & 1) * 2] = pack_half(p0, p1);
-        pf[nt >> 1][(nt & 1) * 2 + 1] = pack_half(p2, p3);
+        top = fmaxf(top, fmaxf(sc[m][n][e], sc[m][n][2 + e]));
       }
-      // V: 16 keys x 32 dimensions at a time; word: two dimensions of two keys -> the first of both, the second of both
-      auto load_v = [&](int kt, int d, uint32_t b[4]) {
-        ldmatrix_x4_trans(at<H>(vb, key_off + kt * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), d * 2 + (lane >> 4)), b[0], b[1], b[2], b[3]);
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+      al[2 * n + e] = a.st[2 * n + e].take(top, lv);
+      change |= al[2 * n + e] != 1.f;
+    }
+  if (__any_sync(0xffffffffu, change)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = __byte_perm(b[i], 0, 0x3120);
-      };
-      if (!masked) {
+    for (int n = 0; n < G; ++n)
 #pragma unroll
-        for (int kt = 0; kt < MT; ++kt)
+      for (int c = 0; c < H / 16; ++c) {
+        a.o[n][c][0] *= al[2 * n];
+        a.o[n][c][1] *= al[2 * n + 1];
+        a.o[n][c][2] *= al[2 * n];
+        a.o[n][c][3] *= al[2 * n + 1];
+      }
+  }
+  uint32_t pb[2][G][2];     // the numerators as B operand; their sum is taken before the rounding
 #pragma unroll
-          for (int d = 0; d < H / 32; ++d) {
-            uint32_t b[4];
-            load_v(kt, d, b);
+  for (int n = 0; n < G; ++n) {
+    RowState &r0 = a.st[2 * n], &r1 = a.st[2 * n + 1];
+    const float w0 = r0.unit_weight(), w1 = r1.unit_weight();
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              mma_half(o[4 * d + 2 * c], pf[kt], half2_of(b[2 * c]), half2_of(b[2 * c + 1]));
-              mma_half(o[4 * d + 2 * c + 1], pf[kt], half2_of_upper(b[2 * c]), half2_of_upper(b[2 * c + 1]));
-            }
-          }
-      } else {
+    for (int m = 0; m < 2; ++m) {
+      const float x0 = r0.scaled(w0, vs[m]), x1 = r1.scaled(w1, vs[m]);
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const float s0 = sc[m][n][2 * z], s1 = sc[m][n][2 * z + 1];
+        float p0 = exp2_approx(s0 - r0.ref), p1 = exp2_approx(s1 - r1.ref);
+        r0.l += p0;
+        r1.l += p1;
+        p0 *= x0;
+        p1 *= x1;
+        if constexpr (kMasked) {       // a scale that is no number reaches the rows that see its block, not the others
+          if (s0 == -INFINITY) p0 = 0.f;
+          if (s1 == -INFINITY) p1 = 0.f;
+        }
+        pb[m][n][z] = transposed(pack_half(p0, p1));
+      }
+    }
+  }
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int m = i / (H / 32), d = i % (H / 32), x = k0 + m * 16 + 2 * tq;
+    uint32_t b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = __byte_perm(vw[i & 1][k], 0, 0x3120);      // the even dimension of two keys, the odd one
+    if (i + 2 < kLoads) load_v(i + 2);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint32_t v[4] = {half2_of(b[2 * c]), half2_of_upper(b[2 * c]), half2_of(b[2 * c + 1]), half2_of_upper(b[2 * c + 1])};
+      if constexpr (kMasked) {
         // A numerator of 0 does not silence a code that is no number.  Values of keys that do not exist are taken as 0; of the
-        // others those that are no numbers are left out of the product and given afterwards to the rows that see them.
-        bool odd = false;
+        // others those that are no numbers are left out and given afterwards to the rows that see them.
+        const uint32_t there[2] = {(x < u.end ? 0xffffu : 0u) | (x + 1 < u.end ? 0xffff0000u : 0u),
+                                   (x + 8 < u.end ? 0xffffu : 0u) | (x + 9 < u.end ? 0xffff0000u : 0u)};
 #pragma unroll
-        for (int kt = 0; kt < MT; ++kt) {
-          const int x = k0 + kt * 16 + 2 * tq;
-          const uint32_t there[2] = {(x < u.end ? 0xffffu : 0u) | (x + 1 < u.end ? 0xffff0000u : 0u),
-                                     (x + 8 < u.end ? 0xffffu : 0u) | (x + 9 < u.end ? 0xffff0000u : 0u)};
+        for (int e = 0; e < 4; ++e) {
+          v[e] &= there[e >> 1];
+          const uint32_t off = ((v[e] & 0x7c00u) == 0x7c00u ? 0xffffu : 0u) | ((v[e] & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u);
+          odd |= off != 0;
+          v[e] &= ~off;
+        }
+      }
 #pragma unroll
-          for (int d = 0; d < H / 32; ++d) {
-            uint32_t b[4];
-            load_v(kt, d, b);
+      for (int n = 0; n < G; ++n) mma_half(a.o[n][2 * d + c], v, pb[m][n][0], pb[m][n][1]);
+    }
+  }
+  if constexpr (kMasked) {
+    if (__any_sync(0xffffffffu, odd)) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                uint32_t y[2];
+        for (int z = 0; z < 2; ++z)
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e) {
+            const int src = e * 4 + tq, key = m * 16 + z * 8 + e;
+            bool see[2 * G];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  y[e] = (z ? half2_of_upper(b[2 * c + e]) : half2_of(b[2 * c + e])) & there[e];
-                  const uint32_t off = ((y[e] & 0x7c00u) == 0x7c00u ? 0xffffu : 0u) | ((y[e] & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u);
-                  odd |= off != 0;
-                  y[e] &= ~off;
+            for (int i = 0; i < 2 * G; ++i) see[i] = __shfl_sync(0xffffffffu, sc[m][i >> 1][2 * z + (i & 1)], src) != -INFINITY;
+            if (k0 + key >= u.end) continue;
+#pragma unroll
+            for (int c = 0; c < H / 16; ++c) {
+              uint16_t w;
+              asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(at<H, G>(vb, key, c) + gq * 2));
+#pragma unroll
+              for (int y = 0; y < 2; ++y)
+                if ((w >> 8 * y & 0x7f) == 0x7f) {
+#pragma unroll
+                  for (int i = 0; i < 2 * G; ++i)
+                    if (see[i]) a.o[i >> 1][c][2 * y + (i & 1)] = NAN;
                 }
-                mma_half(o[4 * d + 2 * c + z], pf[kt], y[0], y[1]);
-              }
-          }
-        }
-        if (__any_sync(0xffffffffu, odd)) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-              const int src = (lane & ~3) | (e >> 1);
-              const bool see_lo = __shfl_sync(0xffffffffu, e & 1 ? sc[nt][1] : sc[nt][0], src) != -INFINITY;
-              const bool see_hi = __shfl_sync(0xffffffffu, e & 1 ? sc[nt][3] : sc[nt][2], src) != -INFINITY;
-              const int key = key_off + nt * 8 + e;
-              if (tile * kTile + key >= u.end) continue;
-#pragma unroll
-              for (int c = 0; c < DC; ++c) {
-                uint32_t w;
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(at<H>(vb, key, c) + tq * 4));
-#pragma unroll
-                for (int z = 0; z < 4; ++z)
-                  if ((w >> 8 * z & 0x7fu) == 0x7fu) {
-                    if (see_lo) o[2 * c + (z & 1)][z >> 1] = NAN;
-                    if (see_hi) o[2 * c + (z & 1)][2 + (z >> 1)] = NAN;
-                  }
-              }
             }
-        }
-      }
-    }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(ring.empty + 8 * st);
-  }
-
-  float l_lo = lo.l, l_hi = hi.l, m_lo = lo.m, m_hi = hi.m;
-  l_lo += __shfl_xor_sync(0xffffffffu, l_lo, 1);
-  l_lo += __shfl_xor_sync(0xffffffffu, l_lo, 2);
-  l_hi += __shfl_xor_sync(0xffffffffu, l_hi, 1);
-  l_hi += __shfl_xor_sync(0xffffffffu, l_hi, 2);
-  const float e_lo = lo.rest(), e_hi = hi.rest();
-#pragma unroll
-  for (int i = 0; i < 2 * DC; ++i) { o[i][0] *= e_lo; o[i][1] *= e_lo; o[i][2] *= e_hi; o[i][3] *= e_hi; }
-  if (r.parents) {   // an unused node - it does not even see itself - sees nothing
-    const uint4 b_lo = *reinterpret_cast<const uint4*>(tree + j_lo * (kMaxTreeNodes / 32));
-    const uint4 b_hi = *reinterpret_cast<const uint4*>(tree + j_hi * (kMaxTreeNodes / 32));
-    if (!(b_lo.x | b_lo.y | b_lo.z | b_lo.w)) {
-      m_lo = -INFINITY;
-      l_lo = 0.f;
-#pragma unroll
-      for (int i = 0; i < 2 * DC; ++i) o[i][0] = o[i][1] = 0.f;
-    }
-    if (!(b_hi.x | b_hi.y | b_hi.z | b_hi.w)) {
-      m_hi = -INFINITY;
-      l_hi = 0.f;
-#pragma unroll
-      for (int i = 0; i < 2 * DC; ++i) o[i][2] = o[i][3] = 0.f;
-    }
-  }
-  auto four_lo = [&](int c, float f) { return make_float4(o[2 * c][0] * f, o[2 * c + 1][0] * f, o[2 * c][1] * f, o[2 * c + 1][1] * f); };
-  auto four_hi = [&](int c, float f) { return make_float4(o[2 * c][2] * f, o[2 * c + 1][2] * f, o[2 * c][3] * f, o[2 * c + 1][3] * f); };
-
-  if constexpr (MT < 4) {
-    // The warps that shared rows lay their outputs side by side, 32 dimensions at a time, and all threads add them up: four
-    // dimensions of a row (or two rows) each.
-    constexpr int kShares = 4 / MT, kRowsHere = 16 * MT, kPitch = S::kMergePitch;
-    float2* ml = reinterpret_cast<float2*>(merge + 64 * kPitch);
-    const int mine = share * kRowsHere + r_lo, row0 = threadIdx.x >> 3, col = (threadIdx.x & 7) * 4;
-    int tok[MT], hd[MT];
-#pragma unroll
-    for (int k = 0; k < MT; ++k) {
-      tok[k] = u.token(row0 + 16 * k);
-      hd[k] = u.head(row0 + 16 * k);
-    }
-#pragma unroll 1
-    for (int part = 0; part < H / 32; ++part) {
-      asm volatile("bar.sync 2, 128;" ::: "memory");      // everybody has read what was there
-      if (part == 0 && tq == 0) {
-        ml[mine] = make_float2(m_lo, l_lo);
-        ml[mine + 8] = make_float2(m_hi, l_hi);
-      }
-#pragma unroll
-      for (int z = 0; z < H / 32; ++z)
-        if (z == part) {
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            *reinterpret_cast<float4*>(merge + mine * kPitch + c * 16 + 4 * tq) = four_lo(2 * z + c, 1.f);
-            *reinterpret_cast<float4*>(merge + (mine + 8) * kPitch + c * 16 + 4 * tq) = four_hi(2 * z + c, 1.f);
           }
-        }
-      asm volatile("bar.sync 2, 128;" ::: "memory");
-#pragma unroll
-      for (int k = 0; k < MT; ++k) {
-        const int row = row0 + 16 * k;
-        float2 x[kShares];
-        float top = -INFINITY, den = 0.f;
-#pragma unroll
-        for (int sh = 0; sh < kShares; ++sh) {
-          x[sh] = ml[sh * kRowsHere + row];
-          top = fmaxf(top, x[sh].x);
-        }
-        const float ref = top == -INFINITY ? 0.f : top;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int sh = 0; sh < kShares; ++sh) {
-          const float f = exp2_approx(x[sh].x - ref);
-          const float4 y = *reinterpret_cast<const float4*>(merge + (sh * kRowsHere + row) * kPitch + col);
-          den = fmaf(f, x[sh].y, den);
-          sum.x = fmaf(f, y.x, sum.x);
-          sum.y = fmaf(f, y.y, sum.y);
-          sum.z = fmaf(f, y.z, sum.z);
-          sum.w = fmaf(f, y.w, sum.w);
-        }
-        if (row >= u.count || failed || *stop) continue;
-        const int d = part * 32 + col;
-        if (sg.whole) {
-          const float inv = den == 0.f ? 0.f : 1.f / den;    // a row that saw nothing has a sum of 0: its output is 0
-          const int64_t t = u.row0 + tok[k];
-          uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t * r.out_stride + static_cast<int64_t>(hd[k]) * H + d);
-          out[0] = pack_bf16(sum.x * inv, sum.y * inv);
-          out[1] = pack_bf16(sum.z * inv, sum.w * inv);
-          if (r.lse && d == 0) r.lse[t * r.Hq + hd[k]] = den == 0.f ? -INFINITY : (top + log2f(den)) * kLn2;
-        } else {
-          const int64_t at_row = static_cast<int64_t>(sg.slot) * kUnitRows + row;
-          *reinterpret_cast<float4*>(parts.acc + at_row * H + d) = sum;
-          if (d == 0) *reinterpret_cast<float2*>(parts.ml + at_row * 2) = make_float2(top, den);
-        }
-      }
-    }
-    return;
-  }
-
-  if (!active || share != 0 || failed || *stop) return;
-  if (sg.whole) {
-    // a row that saw nothing has a sum of 0: its output is 0
-    const float i_lo = l_lo == 0.f ? 0.f : 1.f / l_lo, i_hi = l_hi == 0.f ? 0.f : 1.f / l_hi;
-    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(r.out);
-    uint32_t* to_lo = reinterpret_cast<uint32_t*>(out + (u.row0 + j_lo) * r.out_stride + static_cast<int64_t>(h_lo) * H) + 2 * tq;
-    uint32_t* to_hi = reinterpret_cast<uint32_t*>(out + (u.row0 + j_hi) * r.out_stride + static_cast<int64_t>(h_hi) * H) + 2 * tq;
-#pragma unroll
-    for (int c = 0; c < DC; ++c) {
-      const float4 x = four_lo(c, i_lo), y = four_hi(c, i_hi);
-      if (v_lo) { to_lo[8 * c] = pack_bf16(x.x, x.y); to_lo[8 * c + 1] = pack_bf16(x.z, x.w); }
-      if (v_hi) { to_hi[8 * c] = pack_bf16(y.x, y.y); to_hi[8 * c + 1] = pack_bf16(y.z, y.w); }
-    }
-    if (r.lse && tq == 0) {
-      if (v_lo) r.lse[static_cast<int64_t>(u.row0 + j_lo) * r.Hq + h_lo] = l_lo == 0.f ? -INFINITY : (m_lo + log2f(l_lo)) * kLn2;
-      if (v_hi) r.lse[static_cast<int64_t>(u.row0 + j_hi) * r.Hq + h_hi] = l_hi == 0.f ? -INFINITY : (m_hi + log2f(l_hi)) * kLn2;
-    }
-  } else {
-    const int64_t row = static_cast<int64_t>(sg.slot) * kUnitRows;
-#pragma unroll
-    for (int c = 0; c < DC; ++c) {
-      if (v_lo) *reinterpret_cast<float4*>(parts.acc + (row + r_lo) * H + c * 16 + 4 * tq) = four_lo(c, 1.f);
-      if (v_hi) *reinterpret_cast<float4*>(parts.acc + (row + r_hi) * H + c * 16 + 4 * tq) = four_hi(c, 1.f);
-    }
-    if (tq == 0) {
-      if (v_lo) *reinterpret_cast<float2*>(parts.ml + (row + r_lo) * 2) = make_float2(m_lo, l_lo);
-      if (v_hi) *reinterpret_cast<float2*>(parts.ml + (row + r_hi) * 2) = make_float2(m_hi, l_hi);
     }
   }
 }
 
-__device__ __forceinline__ UnitRows unit_rows(const PagedRows& r, const ReqWork& w, const Segment& sg) {
-  UnitRows u;
-  u.req = sg.req;
-  u.row0 = w.v.row0;
-  u.m = w.v.m;
-  u.group = r.group;
-  u.g = sg.g;
-  u.first = sg.rb * kUnitRows;
-  u.count = min(kUnitRows, w.v.m * u.group - u.first);
-  u.end = w.v.n;
-  u.prefix = w.v.n - w.v.m;
-  return u;
-}
-
-// 160 threads: warps 0-3 compute, warp 4 brings the tiles in.
-template <int H>
-__global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const ScaledParts parts,
-                                                              const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  using S = Smem<H>;
+// 160 threads: warps 0-3 compute, warp 4 brings the stages in.
+template <int H, int G>
+__global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const ScaledParts parts,
+                                                                            const __grid_constant__ CUtensorMap map_k,
+                                                                            const __grid_constant__ CUtensorMap map_v) {
+  using S = Few<H, G>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int stop_word;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -420,13 +296,13 @@ __global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c
   volatile int* stop = &stop_word;
   float* scales = reinterpret_cast<float*>(ptr + S::kOffScale);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  Ring ring{base, base + S::kOffBar, base + S::kOffBar + 8 * S::kStages, 0};
+  FewRing ring{base, base + S::kOffBar, base + S::kOffBar + 8 * S::kStages, 0};
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *stop = 0;
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(ring.full + 8 * s, 1);
-      mbar_init(ring.empty + 8 * s, 4);
+      mbar_init(ring.empty + 8 * s, S::kReaders);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_map(&map_k);
@@ -434,7 +310,7 @@ __global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c
   }
   __syncthreads();
   pdl_wait();
-  const AttentionLine line{c, r, 0};
+  const FewLine line(c, r, S::kRows);
   const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (threadIdx.x == 0) leave_none(parts.desc, blockIdx.x);
   if (share.from >= share.to) return;
@@ -443,57 +319,53 @@ __global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c
     const uint64_t first = policy_evict_first(), last = policy_evict_last();
     const int cpp = c.ps / 16;                  // 16-key groups of a page
     for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
-      const UnitRows u = unit_rows(r, w, sg);
       const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
-      const int groups = min((u.end + 15) / 16, sg.t1 * 4);     // that hold any key, up to the end of the segment
+      const int g0 = sg.t0 * (kTile / 16), g1 = min((w.v.n + 15) / 16, sg.t1 * (kTile / 16));     // groups that hold any key
       const uint64_t policy = w.n_rb > 1 ? last : first;        // others read these keys as well: leave them in L2
-      // a lane looks after one of 32 groups (eight tiles): its place and its scales; those of the next round are under way
-      // while this one's tiles are copied
-      auto page_of = [&](int e) { return e < groups ? table[quotient(e, cpp)] : -1; };
-      int block = 0, page_next = page_of(sg.t0 * 4 + lane);
-      float ks = 1.f, vs = 1.f;
-      auto look_up = [&](int e, int& b, float& k, float& v) {   // of the group whose page has arrived
-        b = 0;
-        k = v = 1.f;
-        if (e < groups) {
-          const int of = quotient(e, cpp);
-          b = (checked_page(c, page_next) * c.Hkv + sg.g) * cpp + (e - of * cpp);
-          k = sc.k[b];
-          v = sc.v[b];
+      // a lane looks after one of 32 groups (sixteen stages): its place and its scales; those of the next round are under way
+      // while this one's stages are copied
+      auto page_of = [&](int e) { return e < g1 ? table[quotient(e, cpp)] : -1; };
+      int block = 0, block_next, page_next = page_of(g0 + lane);
+      float ks = 1.f, vs = 1.f, ks_next, vs_next;
+      auto look_up = [&](int e) {               // of the group whose page has arrived
+        block_next = 0;
+        ks_next = vs_next = 1.f;
+        if (e < g1) {
+          block_next = (checked_page(c, page_next) * c.Hkv + sg.g) * cpp + (e - quotient(e, cpp) * cpp);
+          ks_next = sc.k[block_next];
+          vs_next = sc.v[block_next];
         }
       };
-      int block_next;
-      float ks_next, vs_next;
-      look_up(sg.t0 * 4 + lane, block_next, ks_next, vs_next);
-      page_next = page_of(sg.t0 * 4 + 32 + lane);
-      for (int t = sg.t0; t < sg.t1; ++t, ++ring.it) {
-        const int ahead = (t - sg.t0) & 7;
+      look_up(g0 + lane);
+      page_next = page_of(g0 + 32 + lane);
+      for (int e = g0; e < g1; e += 2, ++ring.it) {
+        const int ahead = (e - g0) & 31;
         if (ahead == 0) {
           block = block_next;
           ks = ks_next;
           vs = vs_next;
-          look_up(t * 4 + 32 + lane, block_next, ks_next, vs_next);
-          page_next = page_of(t * 4 + 64 + lane);
+          look_up(e + 32 + lane);
+          page_next = page_of(e + 64 + lane);
         }
-        const int st = ring.it % S::kStages;
+        const int place = ring.it % S::kStages;
         bool ok = true;
         if (lane == 0) {
-          ok = !*stop && mbar_wait(ring.empty + 8 * st, ((ring.it / S::kStages) & 1) ^ 1, stop);
+          ok = !*stop && mbar_wait(ring.empty + 8 * place, ((ring.it / S::kStages) & 1) ^ 1, stop);
           if (!ok) *stop = 1;
         }
         ok = __shfl_sync(0xffffffffu, ok, 0);
         __syncwarp();
-        const int n_here = max(0, min(4, groups - t * 4));
-        const bool mine = lane >> 2 == ahead;
+        const int which = lane - ahead, n_here = min(2, g1 - e);
+        const bool mine = which >= 0 && which < 2;
         if (ok && mine) {
-          scales[st * 8 + (lane & 3)] = ks;
-          scales[st * 8 + 4 + (lane & 3)] = vs;
+          scales[place * 4 + which] = ks;
+          scales[place * 4 + 2 + which] = vs;
         }
         __syncwarp();
-        if (ok && lane == 0) mbar_expect(ring.full + 8 * st, n_here * 2 * S::kCopy);
+        if (ok && lane == 0) mbar_expect(ring.full + 8 * place, n_here * 2 * S::kCopy);
         __syncwarp();
-        if (ok && mine && (lane & 3) < n_here) {
-          const uint32_t dst = base + st * S::kStage + (lane & 3) * S::kGroup, bar = ring.full + 8 * st;
+        if (ok && mine && which < n_here) {
+          const uint32_t dst = base + place * S::kStage + which * S::kGroup, bar = ring.full + 8 * place;
           const int y = block * (16 / S::kKeysPerRow);
           tma_load_3d(dst, &map_k, 0, y, 0, bar, policy);
           tma_load_3d(dst + S::kHalf, &map_v, 0, y, 0, bar, policy);
@@ -502,26 +374,160 @@ __global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c
     });
   } else {
     float* merge = reinterpret_cast<float*>(ptr + S::kOffMerge);
+    float2* ml = reinterpret_cast<float2*>(ptr + S::kOffMl);
+    float2* of_rows = reinterpret_cast<float2*>(ptr + S::kOffRow);
+    uint4* queries = reinterpret_cast<uint4*>(ptr + S::kOffQ);
     uint32_t* tree = reinterpret_cast<uint32_t*>(ptr + S::kOffTree);
+    const int gq = lane >> 2, tq = lane & 3;
     int tree_of = -1;
-    for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
-      const UnitRows u = unit_rows(r, w, sg);
+    Walk<FewLine> walk(line, share, blockIdx.x);
+    Segment next;
+    for (bool have = walk.next(next); have;) {
+      const Segment sg = next;
+      const int first = sg.rb * S::kRows, m = walk.w.v.m;
+      const FewRows u{sg.req, walk.w.v.row0, r.group, sg.g, first, min(S::kRows, m * r.group - first), walk.w.v.n - m, walk.w.v.n};
+      // eight rows a warp: queries as fp16 in the order of the products' operands, factors, nodes
+      if (warp * 8 < u.count) {
+        const int row = warp * 8 + gq, j = row < u.count ? u.token(row) : 0;
+        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(r.q) + (u.row0 + j) * r.q_stride +
+                                   static_cast<int64_t>(row < u.count ? u.head(row, j) : 0) * H + tq * (H / 4);
+        uint32_t q[H / 8];
+        const float f = query_row<H>(src, row < u.count, q) * (r.scale * kLog2e);
+#pragma unroll
+        for (int i = 0; i < H / 32; ++i) queries[(warp * (H / 32) + i) * 32 + lane] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+        if (tq == 0) of_rows[row] = make_float2(f, __int_as_float(j));
+      }
       if (r.parents && tree_of != sg.req) {     // what every node sees among the nodes
         tree_of = sg.req;
-        asm volatile("bar.sync 2, 128;" ::: "memory");
-        if (static_cast<int>(threadIdx.x) < u.m) {
+        if (static_cast<int>(threadIdx.x) < m) {
           uint32_t bits[kMaxTreeNodes / 32];
           ancestors_of(r.parents + u.row0, threadIdx.x, bits, c.status);
 #pragma unroll
           for (int x = 0; x < kMaxTreeNodes / 32; ++x) tree[threadIdx.x * (kMaxTreeNodes / 32) + x] = bits[x];
         }
-        asm volatile("bar.sync 2, 128;" ::: "memory");
       }
-      if (u.count <= 16) consume<H, 1>(r, u, sg, ring, stop, scales, merge, tree, parts);
-      else if (u.count <= 32) consume<H, 2>(r, u, sg, ring, stop, scales, merge, tree, parts);
-      else consume<H, 4>(r, u, sg, ring, stop, scales, merge, tree, parts);
-      if (sg.last_block >= 0 && threadIdx.x == 0) leave_cut(parts.desc, blockIdx.x, sg, u.row0, u.m, -1, u.first, u.count);
-    });
+      asm volatile("bar.sync 2, 128;" ::: "memory");
+      const bool split = u.count > S::kWarpRows;          // two warps to a stage, with sixteen rows each
+      const int half = split ? warp >> 1 : 0, turn = split ? warp & 1 : warp, turns = split ? 2 : kWarps;
+      FewState<H, G> a;
+#pragma unroll
+      for (int n = 0; n < G; ++n) {
+#pragma unroll
+        for (int k = 0; k < H / 16; ++k) a.o[n][k][0] = a.o[n][k][1] = a.o[n][k][2] = a.o[n][k][3] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float2 x = of_rows[half * S::kWarpRows + 8 * n + 2 * tq + e];
+          a.f[2 * n + e] = x.x;
+          a.node[2 * n + e] = half * S::kWarpRows + 8 * n + 2 * tq + e < u.count ? __float_as_int(x.y) : 0;
+        }
+      }
+      const uint4* mine = queries + half * G * (H / 32) * 32 + lane;
+      const int stage0 = sg.t0 * (kTile / kStageKeys), stages = min(sg.t1 * (kTile / kStageKeys), (u.end + kStageKeys - 1) / kStageKeys) - stage0;
+      bool failed = false;
+#pragma unroll 1
+      for (int k = turn; k < stages; k += turns) {
+        const int it = ring.it + k, place = it % S::kStages, k0 = (stage0 + k) * kStageKeys;
+        if (*stop || !mbar_wait(ring.full + 8 * place, (it / S::kStages) & 1, stop)) { *stop = 1; failed = true; break; }
+        const uint32_t kb = ring.base + place * S::kStage;
+        const float4 blocks = *reinterpret_cast<const float4*>(scales + place * 4);
+        if (k0 + kStageKeys <= u.prefix) stage<H, G, false>(a, u, false, tree, kb, blocks, mine, k0);
+        else stage<H, G, true>(a, u, r.parents != nullptr, tree, kb, blocks, mine, k0);
+        __syncwarp();
+        if (lane < (split ? 1 : S::kReaders)) mbar_arrive(ring.empty + 8 * place);
+      }
+      ring.it += stages;
+      have = walk.next(next);        // (while others are still at their stages)
+
+#pragma unroll
+      for (int i = 0; i < 2 * G; ++i) {
+        float l = a.st[i].l;
+        l += __shfl_xor_sync(0xffffffffu, l, 4);
+        l += __shfl_xor_sync(0xffffffffu, l, 8);
+        l += __shfl_xor_sync(0xffffffffu, l, 16);
+        float rest = a.st[i].rest();
+        bool dead = false;
+        if (r.parents) {         // an unused node - it does not even see itself - sees nothing
+          const uint4 b = *reinterpret_cast<const uint4*>(tree + a.node[i] * (kMaxTreeNodes / 32));
+          dead = !(b.x | b.y | b.z | b.w);
+        }
+        if (dead) {
+          a.st[i].m = -INFINITY;
+          l = rest = 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < H / 16; ++k) {
+          float* v = a.o[i >> 1][k] + (i & 1);
+          v[0] = dead ? 0.f : v[0] * rest;
+          v[2] = dead ? 0.f : v[2] * rest;
+        }
+        a.st[i].l = l;
+      }
+      // The warps lay their outputs side by side, kDims dimensions at a time, and all threads add them up, four dimensions of a row
+      // (or of one of either half) each.
+      constexpr int kQuads = S::kDims / 4;
+      const int shares = split ? 2 : kWarps, row_of = threadIdx.x / kQuads, col = threadIdx.x % kQuads * 4;
+#pragma unroll 1
+      for (int part = 0; part < H / S::kDims; ++part) {
+        asm volatile("bar.sync 2, 128;" ::: "memory");      // everybody has read what was there
+        if (part == 0 && gq == 0) {
+#pragma unroll
+          for (int i = 0; i < 2 * G; ++i) ml[warp * S::kWarpRows + (i >> 1) * 8 + 2 * tq + (i & 1)] = make_float2(a.st[i].m, a.st[i].l);
+        }
+#pragma unroll
+        for (int z = 0; z < H / S::kDims; ++z)
+          if (z == part) {
+#pragma unroll
+            for (int n = 0; n < G; ++n)
+#pragma unroll
+              for (int k = 0; k < S::kDims / 16; ++k) {
+                const float* v = a.o[n][z * (S::kDims / 16) + k];
+                float* to = merge + (warp * S::kWarpRows + n * 8 + 2 * tq) * S::kPitch + k * 16 + 2 * gq;
+                *reinterpret_cast<float2*>(to) = make_float2(v[0], v[2]);
+                *reinterpret_cast<float2*>(to + S::kPitch) = make_float2(v[1], v[3]);
+              }
+          }
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+        if (failed || *stop || row_of >= S::kWarpRows) continue;
+#pragma unroll
+        for (int hf = 0; hf < S::kHalves; ++hf) {
+          const int row = hf * S::kWarpRows + row_of;
+          if (row >= u.count) continue;
+          const int from = split ? 2 * hf : 0;             // the first warp that had the row
+          float top = -INFINITY, den = 0.f;
+          for (int w = 0; w < shares; ++w) top = fmaxf(top, ml[(from + w) * S::kWarpRows + row_of].x);
+          const float ref = top == -INFINITY ? 0.f : top;
+          float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) {
+            if (w >= shares) continue;
+            const float2 x = ml[(from + w) * S::kWarpRows + row_of];
+            const float e = exp2_approx(x.x - ref);
+            const float4 y = *reinterpret_cast<const float4*>(merge + ((from + w) * S::kWarpRows + row_of) * S::kPitch + col);
+            den = fmaf(e, x.y, den);
+            sum.x = fmaf(e, y.x, sum.x);
+            sum.y = fmaf(e, y.y, sum.y);
+            sum.z = fmaf(e, y.z, sum.z);
+            sum.w = fmaf(e, y.w, sum.w);
+          }
+          const int d = part * S::kDims + col;
+          if (sg.whole) {
+            const float inv = den == 0.f ? 0.f : 1.f / den;    // a row that saw nothing has a sum of 0: its output is 0
+            const int j = __float_as_int(of_rows[row].y), head = u.head(row, j);
+            const int64_t t = u.row0 + j;
+            uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t * r.out_stride + static_cast<int64_t>(head) * H + d);
+            out[0] = pack_bf16(sum.x * inv, sum.y * inv);
+            out[1] = pack_bf16(sum.z * inv, sum.w * inv);
+            if (r.lse && d == 0) r.lse[t * r.Hq + head] = den == 0.f ? -INFINITY : (top + log2f(den)) * kLn2;
+          } else {
+            const int64_t at_row = static_cast<int64_t>(sg.slot) * S::kRows + row;
+            *reinterpret_cast<float4*>(parts.acc + at_row * H + d) = sum;
+            if (d == 0) *reinterpret_cast<float2*>(parts.ml + at_row * 2) = make_float2(top, den);
+          }
+        }
+      }
+      asm volatile("bar.sync 2, 128;" ::: "memory");       // the next unit's queries and tree may come
+      if (sg.last_block >= 0 && threadIdx.x == 0) leave_cut(parts.desc, blockIdx.x, sg, u.row0, m, -1, u.first, u.count);
+    }
   }
   __syncthreads();
   if (*stop) {
@@ -531,43 +537,46 @@ __global__ void __launch_bounds__(160, 2) paged_scaled_kernel(const PagedCache c
   }
 }
 
-template <int H>
+template <int H, int G>
 int launch_h(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s) {
+  using S = Few<H, G>;
   static std::atomic<bool> configured[kMaxDevices] = {};
   int sms = 0;
   const int dev = paged_device(&sms);
   if (dev < 0) return -1;
-  if (!allow_shared(paged_scaled_kernel<H>, Smem<H>::kTotal, dev, configured)) return -1;
+  if (!allow_shared(scaled_kernel<H, G>, S::kTotal, dev, configured)) return -1;
   CUtensorMap map_k, map_v;     // rows of 128 bytes, as 64 units of 16 bits
-  constexpr int P = Smem<H>::kKeysPerRow;
+  constexpr int P = S::kKeysPerRow;
   const long long rows = static_cast<long long>(c.n_pages) * c.Hkv * c.ps / P;
   if (tma_map_bf16_row_groups(&map_k, c.k, rows, 64, 16 / P) || tma_map_bf16_row_groups(&map_v, c.v, rows, 64, 16 / P)) return -1;
-  const int blocks = min(2 * sms, kMaxPagedBlocks);
+  const int blocks = min(S::kBlocks * sms, kScaledBlocks);
   ScaledParts parts;
   parts.acc = reinterpret_cast<float*>(ws);
-  parts.ml = parts.acc + 2LL * kMaxPagedBlocks * kUnitRows * H;
-  parts.desc = reinterpret_cast<int4*>(parts.ml + 2LL * kMaxPagedBlocks * kUnitRows * 2);
-  SLED_LAUNCH_PDL(paged_scaled_kernel<H>, dim3(blocks), dim3(160), Smem<H>::kTotal, s, c, sc, r, parts, map_k, map_v);
+  parts.ml = parts.acc + 2LL * kScaledBlocks * S::kRows * H;
+  parts.desc = reinterpret_cast<int4*>(parts.ml + 2LL * kScaledBlocks * S::kRows * 2);
+  SLED_LAUNCH_PDL((scaled_kernel<H, G>), dim3(blocks), dim3(160), S::kTotal, s, c, sc, r, parts, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return -1;
   PagedCache of = c;            // the merge goes by the results' type
   of.dtype = BF16;
-  const int n = launch_paged_merge(of, r, kUnitRows, blocks, parts.acc, parts.ml, parts.desc, s);
+  const int n = launch_paged_merge(of, r, S::kRows, blocks, parts.acc, parts.ml, parts.desc, s);
   return n < 0 ? n : n + 1;
 }
 
 }  // namespace
 
 int64_t paged_scaled_workspace(int h) {
-  return max(max(paged_mma_workspace(h), scaled_few_workspace(h)), h >= 64 ? paged_tc_workspace(h) : 0);
+  const int64_t here = 2LL * kScaledBlocks * Few<128, 2>::kRows * (h + 2) * 4 + kScaledBlocks * 32LL;
+  return h >= 64 ? max(here, paged_tc_workspace(h)) : here;
 }
 
 int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s) {
   // by the rows per request and KV head, on average
   const int64_t rows = static_cast<int64_t>(r.T) * r.group;
-  if (rows <= 8LL * c.n_reqs) return launch_scaled_few(c, sc, r, 1, ws, s);
   if (c.h >= 64 && rows > 32LL * c.n_reqs) return launch_scaled_tc(c, sc, r, ws, s);
-  if (c.h == 128) return launch_h<128>(c, sc, r, ws, s);
-  return c.h == 64 ? launch_h<64>(c, sc, r, ws, s) : launch_h<32>(c, sc, r, ws, s);
+  const bool few = rows <= 8LL * c.n_reqs;
+  if (c.h == 128) return few ? launch_h<128, 1>(c, sc, r, ws, s) : launch_h<128, 2>(c, sc, r, ws, s);
+  if (c.h == 64) return few ? launch_h<64, 1>(c, sc, r, ws, s) : launch_h<64, 2>(c, sc, r, ws, s);
+  return few ? launch_h<32, 1>(c, sc, r, ws, s) : launch_h<32, 2>(c, sc, r, ws, s);
 }
 
 }  // namespace sled
