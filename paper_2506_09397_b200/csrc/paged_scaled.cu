@@ -118,37 +118,44 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool 
   const float lv = fmaxf(__log2f(fabsf(vs[0])), __log2f(fabsf(vs[1])));
   float sc[2][G][4];       // keys 16 m + gq (0, 1), + 8 (2, 3)
   {
-    uint32_t w[2][2][H / 16];      // all of the stage's K: the loads run side by side
+    // K, all of the stage's loads side by side where there are registers for it, 16 bytes a lane and key otherwise
+    constexpr int kWords = G == 1 || H == 32 ? H / 16 : 4;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int part = 0; part < H / 16 / kWords; ++part) {
+      uint32_t w[2][2][kWords];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int key = m * 16 + e * 8 + gq;
-        uint32_t* to = w[m][e];
-        if constexpr (H == 32) {
-          asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(to[0]), "=r"(to[1]) : "r"(at<H, G>(kb, key, tq >> 1) + (tq & 1) * 8));
-        } else {
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int i = 0; i < H / 64; ++i)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(to[4 * i]), "=r"(to[4 * i + 1]), "=r"(to[4 * i + 2]), "=r"(to[4 * i + 3])
-                         : "r"(at<H, G>(kb, key, tq * (H / 64) + i)));
+        for (int e = 0; e < 2; ++e) {
+          const int key = m * 16 + e * 8 + gq;
+          uint32_t* to = w[m][e];
+          if constexpr (H == 32) {
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(to[0]), "=r"(to[1]) : "r"(at<H, G>(kb, key, tq >> 1) + (tq & 1) * 8));
+          } else {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i)
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(to[4 * i]), "=r"(to[4 * i + 1]), "=r"(to[4 * i + 2]), "=r"(to[4 * i + 3])
+                           : "r"(at<H, G>(kb, key, tq * (H / 64) + part * (kWords / 4) + i)));
+          }
+          if (part == 0) {
+#pragma unroll
+            for (int n = 0; n < G; ++n) sc[m][n][e] = sc[m][n][2 + e] = 0.f;
+          }
         }
 #pragma unroll
-        for (int n = 0; n < G; ++n) sc[m][n][e] = sc[m][n][2 + e] = 0.f;
+      for (int s = 0; s < kWords; s += 2) {
+        uint4 y[G];
+#pragma unroll
+        for (int n = 0; n < G; ++n) y[n] = q[(n * (H / 32) + part * (kWords / 2) + s / 2) * 32];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            const uint32_t x[4] = {half2_of(w[m][0][s + k]), half2_of(w[m][1][s + k]), half2_of_upper(w[m][0][s + k]), half2_of_upper(w[m][1][s + k])};
+#pragma unroll
+            for (int n = 0; n < G; ++n) mma_half(sc[m][n], x, k ? y[n].z : y[n].x, k ? y[n].w : y[n].y);
+          }
       }
-#pragma unroll
-    for (int s = 0; s < H / 16; s += 2) {
-      uint4 y[G];
-#pragma unroll
-      for (int n = 0; n < G; ++n) y[n] = q[(n * (H / 32) + s / 2) * 32];
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          const uint32_t x[4] = {half2_of(w[m][0][s + k]), half2_of(w[m][1][s + k]), half2_of_upper(w[m][0][s + k]), half2_of_upper(w[m][1][s + k])};
-#pragma unroll
-          for (int n = 0; n < G; ++n) mma_half(sc[m][n], x, k ? y[n].z : y[n].x, k ? y[n].w : y[n].y);
-        }
     }
   }
   // V: 16 keys x 32 dimensions a load, two loads under way
@@ -161,36 +168,59 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool 
   };
   load_v(0);
   load_v(1);
-  bool change = false;
-  float al[2 * G];
+  // The scores less their rows' references.  Where all rows see all keys and nothing exceeds a reference by much - nearly always -
+  // that is all: no maximum over the warp, nothing to rescale.
+  bool calm = !kMasked;
 #pragma unroll
   for (int n = 0; n < G; ++n)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      const RowState& r = a.st[2 * n + e];
       float top = -INFINITY;
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         const float x = a.f[2 * n + e] * ks[m];
-        sc[m][n][e] *= x;
-        sc[m][n][2 + e] *= x;
-        if constexpr (kMasked) {      // a key that the row does not see, or that does not exist, becomes -infinity whatever it is
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          float& s = sc[m][n][2 * z + e];
+          s = kMasked ? s * x : fmaf(s, x, -r.ref);
+          top = fmaxf(top, s);
+        }
+      }
+      if (!kMasked) calm = calm && !(top > r.room(lv));
+    }
+  if (kMasked || !__all_sync(0xffffffffu, calm)) {
+    float al[2 * G];
+#pragma unroll
+    for (int n = 0; n < G; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        RowState& r = a.st[2 * n + e];
+        float top = -INFINITY;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
-            const int key = k0 + m * 16 + z * 8 + gq, of = key - u.prefix, j = a.node[2 * n + e];
-            bool seen = key < u.end;
-            if (of >= 0 && seen) seen = has_tree ? (tree[j * (kMaxTreeNodes / 32) + (of >> 5)] >> (of & 31)) & 1u : of <= j;
-            if (!seen) sc[m][n][2 * z + e] = -INFINITY;
+            float& s = sc[m][n][2 * z + e];
+            if constexpr (kMasked) {      // a key that the row does not see, or that does not exist, becomes -infinity whatever it is
+              const int key = k0 + m * 16 + z * 8 + gq, of = key - u.prefix, j = a.node[2 * n + e];
+              bool seen = key < u.end;
+              if (of >= 0 && seen) seen = has_tree ? (tree[j * (kMaxTreeNodes / 32) + (of >> 5)] >> (of & 31)) & 1u : of <= j;
+              if (!seen) s = -INFINITY;
+            } else {
+              s += r.ref;
+            }
+            top = fmaxf(top, s);
           }
-        }
-        top = fmaxf(top, fmaxf(sc[m][n][e], sc[m][n][2 + e]));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+        al[2 * n + e] = r.take(top, lv);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) sc[m][n][2 * z + e] -= r.ref;
       }
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-      al[2 * n + e] = a.st[2 * n + e].take(top, lv);
-      change |= al[2 * n + e] != 1.f;
-    }
-  if (__any_sync(0xffffffffu, change)) {
 #pragma unroll
     for (int n = 0; n < G; ++n)
 #pragma unroll
@@ -205,14 +235,13 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool 
 #pragma unroll
   for (int n = 0; n < G; ++n) {
     RowState &r0 = a.st[2 * n], &r1 = a.st[2 * n + 1];
-    const float w0 = r0.unit_weight(), w1 = r1.unit_weight();
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const float x0 = r0.scaled(w0, vs[m]), x1 = r1.scaled(w1, vs[m]);
+      const float x0 = r0.w * vs[m], x1 = r1.w * vs[m];
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         const float s0 = sc[m][n][2 * z], s1 = sc[m][n][2 * z + 1];
-        float p0 = exp2_approx(s0 - r0.ref), p1 = exp2_approx(s1 - r1.ref);
+        float p0 = exp2_approx(s0), p1 = exp2_approx(s1);
         r0.l += p0;
         r1.l += p1;
         p0 *= x0;

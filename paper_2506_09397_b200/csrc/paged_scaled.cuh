@@ -10,7 +10,7 @@ namespace sled {
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kGain = 32768.f;
+constexpr float kGain = 128.f;      // numerators are at most 2^8 times this
 
 // partial results of units that were cut
 struct ScaledParts {
@@ -63,25 +63,32 @@ __device__ __forceinline__ float query_row(const __nv_bfloat16* q, bool valid, u
   return __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
 }
 
-// running maximum, sum and numerators' reference of one of a lane's two rows
+// A row's references: m of the scores, with the sum l of 2^(s - m), and u of the numerators 2^(s - u) vs.  They are raised only when
+// something exceeds them by more than 2^kRaiseBy, which cancels in the end; all else goes by ref, m where that is finite.
+constexpr float kRaiseBy = 8.f;
 struct RowState {
   float m = -INFINITY, l = 0.f, u = -INFINITY;
-  float ref, num;       // of this tile: m, and the reference of the numerators, finite
-  // takes the tile's largest score and the largest log2 |vs|; returns the factor of the output so far
+  float ref = 0.f;
+  float w = 0.f;              // a block's 2^(s - ref) are multiplied by this and vs
+  // takes a stage's largest score and the largest log2 |vs|; returns the factor of the output so far
   __device__ __forceinline__ float take(float mx, float lv) {
-    const float mn = fmaxf(m, mx);
-    ref = mn == -INFINITY ? 0.f : mn;
-    l *= exp2_approx(m - ref);
-    m = mn;
-    const float un = fmaxf(u, mx + lv);
-    num = un == -INFINITY ? 0.f : un;
-    const float f = exp2_approx(u - num);
-    u = un;
+    if (mx > m + kRaiseBy || m == -INFINITY) {
+      const float mn = fmaxf(m, mx);
+      ref = mn == -INFINITY ? 0.f : mn;
+      l *= exp2_approx(m - ref);
+      m = mn;
+    }
+    float f = 1.f;
+    if (mx + lv > u + kRaiseBy || u == -INFINITY) {
+      const float un = fmaxf(u, mx + lv);
+      f = exp2_approx(u - (un == -INFINITY ? 0.f : un));
+      u = un;
+    }
+    w = u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - u, 110.f));
     return f;
   }
-  // what a block's 2^(s - m) are multiplied by: scaled(unit_weight(), vs)
-  __device__ __forceinline__ float unit_weight() const { return kGain * exp2_approx(fminf(ref - num, 110.f)); }
-  __device__ __forceinline__ float scaled(float w, float vs) const { return u == -INFINITY ? 0.f : vs * w; }
+  // the largest s - ref that needs no raise
+  __device__ __forceinline__ float room(float lv) const { return m == -INFINITY ? -INFINITY : kRaiseBy + fminf(0.f, (u - lv) - ref); }
   // what the output is multiplied by at the end
   __device__ __forceinline__ float rest() const { return u == -INFINITY ? 0.f : exp2_approx(u - (m == -INFINITY ? 0.f : m)) * (1.f / kGain); }
 };

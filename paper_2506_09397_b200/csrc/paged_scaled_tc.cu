@@ -28,8 +28,6 @@ namespace {
 
 constexpr int kKeys = 128;                 // keys per tile
 constexpr int kGroupRows = 128;            // rows of a softmax group
-constexpr float kRaiseBy = 8.f;
-constexpr float kTcGain = 64.f;            // numerators are at most 2^8 times this
 constexpr int kScaleSlots = 16;            // tiles whose scales are kept: more than copies, K, V and S are ahead of a softmax
 constexpr int kScaleWords = 20;            // ks [8], vs [8], the largest log2 |vs|
 constexpr int kPieceKeys = 64;
@@ -565,7 +563,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
-          const float weight = top_u == -INFINITY ? 0.f : kTcGain * exp2_approx(fminf(ref - top_u, 110.f));
+          const float weight = top_u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - top_u, 110.f));
           float sum0 = 0.f, sum1 = 0.f;
           tmem_ld32_nowait(tmem_s, v[0]);
 #pragma unroll
@@ -611,7 +609,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       // half of the columns each: both results of a row are in the same lane of tensor memory, only maximum, sum and the
       // numerators' reference have to be exchanged.
       const bool joint = !both && n_tiles > 1;
-      const float rest = top_u == -INFINITY ? 0.f : exp2_approx(top_u - (m == -INFINITY ? 0.f : m)) * (1.f / kTcGain);     // of the output
+      const float rest = top_u == -INFINITY ? 0.f : exp2_approx(top_u - (m == -INFINITY ? 0.f : m)) * (1.f / kGain);     // of the output
       if (joint) {
         if (s == 1) tops[row_in_group] = make_float4(m, l, rest, 0.f);
         asm volatile("bar.sync 1, 256;" ::: "memory");
