@@ -20,8 +20,8 @@
 //
 // A unit is the rows that share a KV head, up to 8 (kGroups 1) or 32 of them.  Its keys come in stages of 32, each read by one
 // warp, or by two that have 16 rows each where the unit has more than 16; the four computing warps take stages in turn, know
-// nothing of each other until the end of the unit, and merge there.  A fifth warp brings the stages in by TMA, their scales with
-// them, looked up a round ahead.  Work is handed out as paged_schedule.cuh says.
+// nothing of each other until the end of the unit, and merge there.  A fifth warp (and a sixth) brings the stages in by TMA, their
+// scales with them, looked up a round ahead.  Work is handed out as paged_schedule.cuh says.
 #include "gemm_tc.h"
 #include "kernels.h"
 #include "paged_scaled.cuh"
@@ -47,6 +47,8 @@ struct Few {
   static constexpr int kStage = 2 * kHalf;
   static constexpr int kStages = H == 128 ? 8 : 12;
   static constexpr int kBlocks = kGroups == 1 ? 3 : 2;              // on an SM
+  static constexpr int kProducers = kGroups;                        // warps that bring stages in (a third block leaves no registers for two)
+  static constexpr int kThreads = 32 * (kWarps + kProducers);
   static constexpr int kDims = 32;                                  // of a round of the merge
   static constexpr int kPitch = kDims + 4;                          // four rows two apart meet 32 banks
   static constexpr int kOffQ = kStages * kStage;                    // [8 rows][two products][lane] 16 bytes
@@ -55,12 +57,13 @@ struct Few {
   static constexpr int kOffRow = kOffMl + kWarps * kWarpRows * 8;   // of a row: what turns products into scores, its node
   static constexpr int kOffTree = kOffRow + kRows * 8;
   static constexpr int kOffScale = kOffTree + kMaxTreeNodes * (kMaxTreeNodes / 32) * 4;     // [stage][K, V][2]
-  static constexpr int kOffBar = kOffScale + kStages * 16;
-  static constexpr int kTotal = kOffBar + 16 * kStages + 1024;      // alignment slack
+  static constexpr int kOffUnit = kOffScale + kStages * 16;         // two stretches
+  static constexpr int kOffBar = kOffUnit + 2 * 96;
+  static constexpr int kTotal = kOffBar + 16 * kStages + 32 + 1024; // alignment slack
 };
 // A place of the ring is always the same warp's within a stretch of a unit, which has then seen all its phases: the parity that it
 // waits for cannot be that of the phase before the last.  (Copies need not arrive in the order in which they were issued.)
-static_assert(Few<128, 1>::kStages % kWarps == 0 && Few<64, 1>::kStages % kWarps == 0, "whole rounds of the warps");
+static_assert(Few<128, 1>::kStages % kWarps == 0 && Few<64, 1>::kStages % kWarps == 0, "whole rounds of the warps, and of two producers");
 static_assert(3 * (Few<128, 1>::kTotal + 1024 + 512) <= 228 * 1024 && 2 * (Few<128, 2>::kTotal + 1024 + 512) <= 228 * 1024, "blocks of an SM");
 
 template <int H, int G>
@@ -87,11 +90,25 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {     // of an 8 x 8 
   return y;
 }
 
+// A stretch of a unit, as the fifth warp finds it and the others read it from shared memory: little of it is kept in registers.
+struct FewUnit {
+  Segment sg;
+  int row0, m, n;         // the request's rows and keys
+  int first, count;       // rows of the unit
+  int more;               // 0: there are no more
+};
 struct FewRows {
-  int req, row0, group, g, first, count, prefix, end;
+  int group, g, first;
   __device__ __forceinline__ int token(int r) const { return quotient(first + r, group); }
   __device__ __forceinline__ int head(int r, int token) const { return g * group + first + r - token * group; }
 };
+
+// whether all of the computing threads say so
+__device__ __forceinline__ bool all_of_128(bool x) {
+  int y;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 2, 128, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(y) : "r"(static_cast<int>(x)) : "memory");
+  return y != 0;
+}
 
 struct FewRing {
   uint32_t base, full, empty;
@@ -105,12 +122,12 @@ struct FewState {
   float o[G][H / 16][4];
   RowState st[2 * G];
   float f[2 * G];
-  int node[2 * G];
 };
 
 // A stage of 32 keys, k0 the position of the first.  kMasked: some row may not see some of them.
 template <int H, int G, bool kMasked>
-__device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool has_tree, const uint32_t* tree, uint32_t kb, float4 blocks, const uint4* q, int k0) {
+__device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bool has_tree, const uint32_t* tree, const float2* of_rows, uint32_t kb, float4 blocks,
+                                      const uint4* q, int k0) {
   using S = Few<H, G>;
   const uint32_t vb = kb + S::kHalf;
   const int lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
@@ -197,14 +214,16 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool 
       for (int e = 0; e < 2; ++e) {
         RowState& r = a.st[2 * n + e];
         float top = -INFINITY;
+        int j = 0;
+        if (kMasked) j = __float_as_int(of_rows[8 * n + 2 * tq + e].y);
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
             float& s = sc[m][n][2 * z + e];
             if constexpr (kMasked) {      // a key that the row does not see, or that does not exist, becomes -infinity whatever it is
-              const int key = k0 + m * 16 + z * 8 + gq, of = key - u.prefix, j = a.node[2 * n + e];
-              bool seen = key < u.end;
+              const int key = k0 + m * 16 + z * 8 + gq, of = key - prefix;
+              bool seen = key < end;
               if (of >= 0 && seen) seen = has_tree ? (tree[j * (kMaxTreeNodes / 32) + (of >> 5)] >> (of & 31)) & 1u : of <= j;
               if (!seen) s = -INFINITY;
             } else {
@@ -268,8 +287,8 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool 
       if constexpr (kMasked) {
         // A numerator of 0 does not silence a code that is no number.  Values of keys that do not exist are taken as 0; of the
         // others those that are no numbers are left out and given afterwards to the rows that see them.
-        const uint32_t there[2] = {(x < u.end ? 0xffffu : 0u) | (x + 1 < u.end ? 0xffff0000u : 0u),
-                                   (x + 8 < u.end ? 0xffffu : 0u) | (x + 9 < u.end ? 0xffff0000u : 0u)};
+        const uint32_t there[2] = {(x < end ? 0xffffu : 0u) | (x + 1 < end ? 0xffff0000u : 0u),
+                                   (x + 8 < end ? 0xffffu : 0u) | (x + 9 < end ? 0xffff0000u : 0u)};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           v[e] &= there[e >> 1];
@@ -294,7 +313,7 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool 
             bool see[2 * G];
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i) see[i] = __shfl_sync(0xffffffffu, sc[m][i >> 1][2 * z + (i & 1)], src) != -INFINITY;
-            if (k0 + key >= u.end) continue;
+            if (k0 + key >= end) continue;
 #pragma unroll
             for (int c = 0; c < H / 16; ++c) {
               uint16_t w;
@@ -312,9 +331,9 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, const FewRows& u, bool 
   }
 }
 
-// 160 threads: warps 0-3 compute, warp 4 brings the stages in.
+// Warps 0-3 compute, the others bring the stages in.
 template <int H, int G>
-__global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const ScaledParts parts,
+__global__ void __launch_bounds__(Few<H, G>::kThreads, Few<H, G>::kBlocks) scaled_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const ScaledParts parts,
                                                                             const __grid_constant__ CUtensorMap map_k,
                                                                             const __grid_constant__ CUtensorMap map_v) {
   using S = Few<H, G>;
@@ -326,12 +345,18 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
   float* scales = reinterpret_cast<float*>(ptr + S::kOffScale);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   FewRing ring{base, base + S::kOffBar, base + S::kOffBar + 8 * S::kStages, 0};
+  const uint32_t unit_full = base + S::kOffBar + 16 * S::kStages, unit_empty = unit_full + 16;
+  FewUnit* shared_units = reinterpret_cast<FewUnit*>(ptr + S::kOffUnit);
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *stop = 0;
     for (int s = 0; s < S::kStages; ++s) {
       mbar_init(ring.full + 8 * s, 1);
       mbar_init(ring.empty + 8 * s, S::kReaders);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(unit_full + 8 * s, 1);
+      mbar_init(unit_empty + 8 * s, kWarps);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_map(&map_k);
@@ -344,10 +369,29 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
   if (threadIdx.x == 0) leave_none(parts.desc, blockIdx.x);
   if (share.from >= share.to) return;
 
-  if (warp == 4) {
+  if (warp >= kWarps) {
+    const int producer = warp - kWarps;
     const uint64_t first = policy_evict_first(), last = policy_evict_last();
     const int cpp = c.ps / 16;                  // 16-key groups of a page
+    int units = 0;
+    // (all lanes call it) makes a stretch known to the others once the one before the last has been dealt with
+    auto publish = [&](const FewUnit& u) {
+      bool ok = true;
+      if (lane == 0) {
+        ok = !*stop && mbar_wait(unit_empty + 8 * (units & 1), ((units >> 1) & 1) ^ 1, stop);
+        if (ok) {
+          shared_units[units & 1] = u;
+          mbar_arrive(unit_full + 8 * (units & 1));
+        } else {
+          *stop = 1;
+        }
+      }
+      ++units;
+      return __shfl_sync(0xffffffffu, ok, 0) != 0;
+    };
     for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
+      const int row = sg.rb * S::kRows;
+      if (producer == 0 && !publish(FewUnit{sg, w.v.row0, w.v.m, w.v.n, row, min(S::kRows, w.v.m * r.group - row), 1})) return;
       const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
       const int g0 = sg.t0 * (kTile / 16), g1 = min((w.v.n + 15) / 16, sg.t1 * (kTile / 16));     // groups that hold any key
       const uint64_t policy = w.n_rb > 1 ? last : first;        // others read these keys as well: leave them in L2
@@ -367,40 +411,44 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
       };
       look_up(g0 + lane);
       page_next = page_of(g0 + 32 + lane);
-      for (int e = g0; e < g1; e += 2, ++ring.it) {
-        const int ahead = (e - g0) & 31;
-        if (ahead == 0) {
+      const int stages = (g1 - g0 + 1) / 2;
+      int round = -1;
+      // A place of the ring is always the same producer's, across stretches too: it has itself filled the place the last time, so
+      // that the parity that it waits for cannot be that of the phase before the last, however far the other is behind.
+      for (int k = S::kProducers == 1 ? 0 : (ring.it ^ producer) & 1; k < stages; k += S::kProducers) {
+        const int e = g0 + 2 * k, ahead = (2 * k) & 31;
+        if (k >> 4 != round) {
+          round = k >> 4;
           block = block_next;
           ks = ks_next;
           vs = vs_next;
-          look_up(e + 32 + lane);
-          page_next = page_of(e + 64 + lane);
+          look_up(g0 + ((2 * k) & ~31) + 32 + lane);
+          page_next = page_of(g0 + ((2 * k) & ~31) + 64 + lane);
         }
-        const int place = ring.it % S::kStages;
-        bool ok = true;
-        if (lane == 0) {
-          ok = !*stop && mbar_wait(ring.empty + 8 * place, ((ring.it / S::kStages) & 1) ^ 1, stop);
-          if (!ok) *stop = 1;
+        const int it = ring.it + k, place = it % S::kStages;
+        if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(ring.empty + 8 * place, ((it / S::kStages) & 1) ^ 1, stop))) {
+          *stop = 1;
+          return;
         }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        __syncwarp();
         const int which = lane - ahead, n_here = min(2, g1 - e);
-        const bool mine = which >= 0 && which < 2;
-        if (ok && mine) {
+        if (which >= 0 && which < 2) {
           scales[place * 4 + which] = ks;
           scales[place * 4 + 2 + which] = vs;
         }
         __syncwarp();
-        if (ok && lane == 0) mbar_expect(ring.full + 8 * place, n_here * 2 * S::kCopy);
+        const uint32_t bar = ring.full + 8 * place;
+        if (lane == ahead) mbar_expect(bar, n_here * 2 * S::kCopy);
         __syncwarp();
-        if (ok && mine && which < n_here) {
-          const uint32_t dst = base + place * S::kStage + which * S::kGroup, bar = ring.full + 8 * place;
+        if (which >= 0 && which < n_here) {
+          const uint32_t dst = base + place * S::kStage + which * S::kGroup;
           const int y = block * (16 / S::kKeysPerRow);
           tma_load_3d(dst, &map_k, 0, y, 0, bar, policy);
           tma_load_3d(dst + S::kHalf, &map_v, 0, y, 0, bar, policy);
         }
       }
+      ring.it += stages;
     });
+    if (producer == 0) publish(FewUnit{});
   } else {
     float* merge = reinterpret_cast<float*>(ptr + S::kOffMerge);
     float2* ml = reinterpret_cast<float2*>(ptr + S::kOffMl);
@@ -409,34 +457,35 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
     uint32_t* tree = reinterpret_cast<uint32_t*>(ptr + S::kOffTree);
     const int gq = lane >> 2, tq = lane & 3;
     int tree_of = -1;
-    Walk<FewLine> walk(line, share, blockIdx.x);
-    Segment next;
-    for (bool have = walk.next(next); have;) {
-      const Segment sg = next;
-      const int first = sg.rb * S::kRows, m = walk.w.v.m;
-      const FewRows u{sg.req, walk.w.v.row0, r.group, sg.g, first, min(S::kRows, m * r.group - first), walk.w.v.n - m, walk.w.v.n};
-      // eight rows a warp: queries as fp16 in the order of the products' operands, factors, nodes
-      if (warp * 8 < u.count) {
-        const int row = warp * 8 + gq, j = row < u.count ? u.token(row) : 0;
-        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(r.q) + (u.row0 + j) * r.q_stride +
-                                   static_cast<int64_t>(row < u.count ? u.head(row, j) : 0) * H + tq * (H / 4);
+    for (int units = 0;; ++units) {
+      const FewUnit& at_unit = shared_units[units & 1];
+      const bool known = *stop == 0 && mbar_wait(unit_full + 8 * (units & 1), (units >> 1) & 1, stop);
+      if (!known) *stop = 1;
+      if (!all_of_128(known && at_unit.more)) break;      // (all or none: there are barriers ahead)
+      const FewRows u{r.group, at_unit.sg.g, at_unit.first};
+      const int m = at_unit.m, row0 = at_unit.row0, count = at_unit.count;
+      // eight rows a warp: queries as fp16 in the order of the products' operands, factors, nodes (rows that there are not: 0)
+      if (warp * 8 < S::kRows) {
+        const int row = warp * 8 + gq, j = row < count ? u.token(row) : 0;
+        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(r.q) + (row0 + j) * r.q_stride +
+                                   static_cast<int64_t>(row < count ? u.head(row, j) : 0) * H + tq * (H / 4);
         uint32_t q[H / 8];
-        const float f = query_row<H>(src, row < u.count, q) * (r.scale * kLog2e);
+        const float f = query_row<H>(src, row < count, q) * (r.scale * kLog2e);
 #pragma unroll
         for (int i = 0; i < H / 32; ++i) queries[(warp * (H / 32) + i) * 32 + lane] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
         if (tq == 0) of_rows[row] = make_float2(f, __int_as_float(j));
       }
-      if (r.parents && tree_of != sg.req) {     // what every node sees among the nodes
-        tree_of = sg.req;
+      if (r.parents && tree_of != at_unit.sg.req) {     // what every node sees among the nodes
+        tree_of = at_unit.sg.req;
         if (static_cast<int>(threadIdx.x) < m) {
           uint32_t bits[kMaxTreeNodes / 32];
-          ancestors_of(r.parents + u.row0, threadIdx.x, bits, c.status);
+          ancestors_of(r.parents + row0, threadIdx.x, bits, c.status);
 #pragma unroll
           for (int x = 0; x < kMaxTreeNodes / 32; ++x) tree[threadIdx.x * (kMaxTreeNodes / 32) + x] = bits[x];
         }
       }
       asm volatile("bar.sync 2, 128;" ::: "memory");
-      const bool split = u.count > S::kWarpRows;          // two warps to a stage, with sixteen rows each
+      const bool split = count > S::kWarpRows;            // two warps to a stage, with sixteen rows each
       const int half = split ? warp >> 1 : 0, turn = split ? warp & 1 : warp, turns = split ? 2 : kWarps;
       FewState<H, G> a;
 #pragma unroll
@@ -445,13 +494,12 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
         for (int k = 0; k < H / 16; ++k) a.o[n][k][0] = a.o[n][k][1] = a.o[n][k][2] = a.o[n][k][3] = 0.f;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float2 x = of_rows[half * S::kWarpRows + 8 * n + 2 * tq + e];
-          a.f[2 * n + e] = x.x;
-          a.node[2 * n + e] = half * S::kWarpRows + 8 * n + 2 * tq + e < u.count ? __float_as_int(x.y) : 0;
+          a.f[2 * n + e] = of_rows[half * S::kWarpRows + 8 * n + 2 * tq + e].x;
         }
       }
       const uint4* mine = queries + half * G * (H / 32) * 32 + lane;
-      const int stage0 = sg.t0 * (kTile / kStageKeys), stages = min(sg.t1 * (kTile / kStageKeys), (u.end + kStageKeys - 1) / kStageKeys) - stage0;
+      const int end = at_unit.n, prefix = end - m, stage0 = at_unit.sg.t0 * (kTile / kStageKeys);
+      const int stages = min(at_unit.sg.t1 * (kTile / kStageKeys), (end + kStageKeys - 1) / kStageKeys) - stage0;
       bool failed = false;
 #pragma unroll 1
       for (int k = turn; k < stages; k += turns) {
@@ -459,14 +507,12 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
         if (*stop || !mbar_wait(ring.full + 8 * place, (it / S::kStages) & 1, stop)) { *stop = 1; failed = true; break; }
         const uint32_t kb = ring.base + place * S::kStage;
         const float4 blocks = *reinterpret_cast<const float4*>(scales + place * 4);
-        if (k0 + kStageKeys <= u.prefix) stage<H, G, false>(a, u, false, tree, kb, blocks, mine, k0);
-        else stage<H, G, true>(a, u, r.parents != nullptr, tree, kb, blocks, mine, k0);
+        if (k0 + kStageKeys <= prefix) stage<H, G, false>(a, prefix, end, false, tree, of_rows, kb, blocks, mine, k0);
+        else stage<H, G, true>(a, prefix, end, r.parents != nullptr, tree, of_rows + half * S::kWarpRows, kb, blocks, mine, k0);
         __syncwarp();
         if (lane < (split ? 1 : S::kReaders)) mbar_arrive(ring.empty + 8 * place);
       }
       ring.it += stages;
-      have = walk.next(next);        // (while others are still at their stages)
-
 #pragma unroll
       for (int i = 0; i < 2 * G; ++i) {
         float l = a.st[i].l;
@@ -476,7 +522,8 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
         float rest = a.st[i].rest();
         bool dead = false;
         if (r.parents) {         // an unused node - it does not even see itself - sees nothing
-          const uint4 b = *reinterpret_cast<const uint4*>(tree + a.node[i] * (kMaxTreeNodes / 32));
+          const int j = __float_as_int(of_rows[half * S::kWarpRows + (i >> 1) * 8 + 2 * tq + (i & 1)].y);
+          const uint4 b = *reinterpret_cast<const uint4*>(tree + j * (kMaxTreeNodes / 32));
           dead = !(b.x | b.y | b.z | b.w);
         }
         if (dead) {
@@ -520,7 +567,7 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
 #pragma unroll
         for (int hf = 0; hf < S::kHalves; ++hf) {
           const int row = hf * S::kWarpRows + row_of;
-          if (row >= u.count) continue;
+          if (row >= count) continue;
           const int from = split ? 2 * hf : 0;             // the first warp that had the row
           float top = -INFINITY, den = 0.f;
           for (int w = 0; w < shares; ++w) top = fmaxf(top, ml[(from + w) * S::kWarpRows + row_of].x);
@@ -539,23 +586,24 @@ __global__ void __launch_bounds__(160, Few<H, G>::kBlocks) scaled_kernel(const P
             sum.w = fmaf(e, y.w, sum.w);
           }
           const int d = part * S::kDims + col;
-          if (sg.whole) {
+          if (at_unit.sg.whole) {
             const float inv = den == 0.f ? 0.f : 1.f / den;    // a row that saw nothing has a sum of 0: its output is 0
             const int j = __float_as_int(of_rows[row].y), head = u.head(row, j);
-            const int64_t t = u.row0 + j;
+            const int64_t t = row0 + j;
             uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t * r.out_stride + static_cast<int64_t>(head) * H + d);
             out[0] = pack_bf16(sum.x * inv, sum.y * inv);
             out[1] = pack_bf16(sum.z * inv, sum.w * inv);
             if (r.lse && d == 0) r.lse[t * r.Hq + head] = den == 0.f ? -INFINITY : (top + log2f(den)) * kLn2;
           } else {
-            const int64_t at_row = static_cast<int64_t>(sg.slot) * S::kRows + row;
+            const int64_t at_row = static_cast<int64_t>(at_unit.sg.slot) * S::kRows + row;
             *reinterpret_cast<float4*>(parts.acc + at_row * H + d) = sum;
             if (d == 0) *reinterpret_cast<float2*>(parts.ml + at_row * 2) = make_float2(top, den);
           }
         }
       }
+      if (at_unit.sg.last_block >= 0 && threadIdx.x == 0) leave_cut(parts.desc, blockIdx.x, at_unit.sg, row0, m, -1, u.first, count);
       asm volatile("bar.sync 2, 128;" ::: "memory");       // the next unit's queries and tree may come
-      if (sg.last_block >= 0 && threadIdx.x == 0) leave_cut(parts.desc, blockIdx.x, sg, u.row0, m, -1, u.first, u.count);
+      if (lane == 0) mbar_arrive(unit_empty + 8 * (units & 1));
     }
   }
   __syncthreads();
@@ -583,7 +631,7 @@ int launch_h(const PagedCache& c, const CacheScales& sc, const PagedRows& r, cha
   parts.acc = reinterpret_cast<float*>(ws);
   parts.ml = parts.acc + 2LL * kScaledBlocks * S::kRows * H;
   parts.desc = reinterpret_cast<int4*>(parts.ml + 2LL * kScaledBlocks * S::kRows * 2);
-  SLED_LAUNCH_PDL((scaled_kernel<H, G>), dim3(blocks), dim3(160), S::kTotal, s, c, sc, r, parts, map_k, map_v);
+  SLED_LAUNCH_PDL((scaled_kernel<H, G>), dim3(blocks), dim3(S::kThreads), S::kTotal, s, c, sc, r, parts, map_k, map_v);
   if (cudaGetLastError() != cudaSuccess) return -1;
   PagedCache of = c;            // the merge goes by the results' type
   of.dtype = BF16;
