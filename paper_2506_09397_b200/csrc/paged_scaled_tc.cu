@@ -1,21 +1,22 @@
 // Attention over a paged cache of e4m3 codes on the 5th-generation tensor cores (tcgen05), head_dim 64 and 128: for batches whose
 // requests bring many query rows (drafted trees under grouped-query attention, prompts).
 //
-// Formulas, scales and roundings are those of paged_scaled.cu; units, their sharing out and the two softmax groups are those
-// of paged_tc.cu: a unit is up to 256 query rows that share a KV head, the M side of the products, a row per tensor-memory lane; with
-// more than 128 rows both groups of four warps take every 128-key tile, with fewer they take the tiles in turn and join at
-// the end.
-//     S = Q C^T      (M 128 x N 128 keys, contraction over H)      -> tensor memory, fp32
-//     O += P D       (M 128 x N H, contraction over 128 keys)      P from tensor memory (fp16, over S)
-// The products take 16-bit operands, so four warps turn the codes into fp16: from a ring of pieces of 64 keys, K and V of a tile in
-// turn, into operand tiles.  Each warp brings its sixteen keys of a piece itself, with asynchronous 16-byte
-// copies, and needs nobody to tell it that they have arrived.  They bring the queries too, as fp16 times a power of two per row.  A
-// score meets its block's scale ks where it leaves tensor memory, a numerator its vs before it is rounded.  The references of a row - m of the scores, u of the numerators - are raised only when something exceeds them
-// by more than 2^8; raising u means rescaling the row of O in tensor memory, which happens in a unit's first tiles.
-// Scores are read from tensor memory twice, for the maximum and for the exponentials: no thread holds a row of them.
+// Formulas, scales and roundings are those of paged_scaled.cu.  A unit is up to 256 query rows that share a KV head, the M side of
+// the products, a row per tensor-memory lane; two groups of four warps have the softmax of 128 rows each.  With more than 128
+// rows both groups take every 64-key tile; with fewer they take the tiles in turn, for the same rows, and join at the end.
+//     S = Q C^T      (M 128 x N 64 keys, contraction over H)       -> tensor memory, fp32, two buffers a group
+//     O += P D       (M 128 x N H, contraction over 64 keys)       P from tensor memory (fp16, over S)
+// A group's next scores are formed while it is at the softmax of the present ones.  The products take 16-bit operands, so four warps
+// turn the codes into fp16, from a ring of 64 keys a piece, K and V of a tile in turn, into operand tiles.  Each warp brings its
+// sixteen keys of a piece itself, with asynchronous 16-byte copies, and needs nobody to tell it that they have arrived.  They
+// bring the queries too, as fp16 times a power of two per row.  A score meets its block's scale ks where it leaves tensor memory, a
+// numerator its vs before it is rounded.  The references of a row - m of the scores, u of the numerators - are raised only when
+// something exceeds them by more than 2^8; raising u means rescaling the row of O in tensor memory, which happens in a unit's
+// first tiles.
 //   warps 0-3, 4-7 : softmax and output of the two groups
 //   warps 8-11     : K, V and Q to fp16, scales
-//   warp 12        : tensor-memory allocation, products (one thread); 13-15 only complete the warpgroup
+//   warp 12        : tensor-memory allocation, products (one thread)
+//   warp 13        : the block's stretches of units, for all others; 14 and 15 only complete the warpgroup
 // Every wait is bounded; when one runs out the block says so in *status, lets what is under way land, frees its tensor
 // memory and returns.
 #include "kernels.h"
@@ -26,11 +27,11 @@ namespace sled {
 
 namespace {
 
-constexpr int kKeys = 128;                 // keys per tile
+constexpr int kKeys = 64;                  // keys per tile
 constexpr int kGroupRows = 128;            // rows of a softmax group
 constexpr int kScaleSlots = 16;            // tiles whose scales are kept: more than copies, K, V and S are ahead of a softmax
-constexpr int kScaleWords = 20;            // ks [8], vs [8], the largest log2 |vs|
-constexpr int kPieceKeys = 64;
+constexpr int kScaleWords = 12;            // ks [4], vs [4], the largest log2 |vs|
+constexpr int kUnitSlots = 4;              // stretches of units that are known ahead
 
 // Operands lie in groups of eight rows, [H / 64][8 rows][64 columns] (K, V), or as [H / 64][128 rows][64 columns] (Q); rows of
 // 128 bytes, 16-byte chunk c at c ^ (row & 7).
@@ -38,18 +39,20 @@ template <int H, int kGroups>
 struct ScaledTc {
   static constexpr int kHalves = H / 64;
   static constexpr int kOctet = kHalves * 1024;          // eight rows
-  static constexpr int kTileBytes = 16 * kOctet;         // K, V or 128 rows of Q
-  static constexpr int kKStages = H == 64 ? 3 : 2, kVStages = H == 64 ? 3 : 2;
+  static constexpr int kTileBytes = kKeys / 8 * kOctet;  // K or V
+  static constexpr int kQBytes = kGroupRows / 8 * kOctet;
+  static constexpr int kKStages = 4, kVStages = 4;
   static constexpr int kOffQ = 0;
-  static constexpr int kOffK = kGroups * kTileBytes;
+  static constexpr int kOffK = kGroups * kQBytes;
   static constexpr int kOffV = kOffK + kKStages * kTileBytes;
-  static constexpr int kPieces = H == 64 || kGroups == 1 ? 7 : 3, kPieceBytes = kPieceKeys * H;
+  static constexpr int kPieces = H == 64 || kGroups == 1 ? 7 : 3, kPieceBytes = kKeys * H;
   static constexpr int kOffRaw = kOffV + kVStages * kTileBytes;
   static constexpr int kOffBar = kOffRaw + kPieces * kPieceBytes;
-  static constexpr int kOffTree = kOffBar + 384;         // parents of the nodes, one byte each, for either group
+  static constexpr int kOffTree = kOffBar + 512;         // parents of the nodes, one byte each, for either group
   static constexpr int kOffTop = kOffTree + 2 * kMaxTreeNodes;     // what the groups tell each other about a row
   static constexpr int kOffScale = kOffTop + kGroupRows * 16;      // [slot][kScaleWords]
-  static constexpr int kOffFactor = kOffScale + kScaleSlots * kScaleWords * 4;  // of the rows of Q
+  static constexpr int kOffUnit = kOffScale + kScaleSlots * kScaleWords * 4;
+  static constexpr int kOffFactor = kOffUnit + kUnitSlots * 64;    // of the rows of Q
   static constexpr int kTotal = kOffFactor + kGroups * kGroupRows * 4 + 1024;     // alignment slack
 };
 static_assert(kMaxTreeNodes == 128);
@@ -57,9 +60,9 @@ static_assert(ScaledTc<128, 1>::kTotal + 512 <= 227 * 1024 && ScaledTc<128, 2>::
               "shared memory of one block");
 
 // barriers, 8 bytes each
-enum { B_KFULL = 0, B_KEMPTY = 4, B_VFULL = 8, B_VEMPTY = 12, B_QFULL = 16, B_QEMPTY = 17, B_SFULL = 18, B_PFULL = 20, B_ODONE = 24, B_SCALE = 26,
-       B_COUNT = B_SCALE + kScaleSlots };
-static_assert(B_COUNT * 8 + 4 <= 384);
+enum { B_KFULL = 0, B_KEMPTY = 4, B_VFULL = 8, B_VEMPTY = 12, B_QFULL = 16, B_QEMPTY = 17, B_SFULL = 18, B_PFULL = 22, B_PVDONE = 26, B_ODONE = 28, B_UFULL = 30,
+       B_UEMPTY = B_UFULL + kUnitSlots, B_SCALE = B_UEMPTY + kUnitSlots, B_COUNT = B_SCALE + kScaleSlots };
+static_assert(B_COUNT * 8 + 4 <= 512);
 
 // what a row sees of the request's own nodes
 struct SeenNodes {
@@ -101,11 +104,32 @@ __device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
 }
 __device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-// a unit, or the stretch of it that the block works on
+// A unit, or the stretch of it that the block works on, as warp 13 leaves it in shared memory.
 struct TcUnit {
   Segment sg;
   int row0, m, n;
+  int more;        // 0: there are no more
 };
+static_assert(sizeof(TcUnit) <= 64);
+constexpr int kUnitReaders = 13;       // warps 0 - 12
+
+// The line of 64-key tiles with units of up to unit_rows rows.
+struct TcLine : AttentionLine {
+  __device__ __forceinline__ TcLine(const PagedCache& c, const PagedRows& r, int unit_rows) : AttentionLine{c, r, 0, unit_rows, kKeys} {}
+  __device__ __forceinline__ int min_share() const { return 1; }
+  __device__ __forceinline__ ReqWork operator()(int i) const {
+    ReqWork w = AttentionLine::operator()(i);
+    if (w.units > 0) w.weight = w.v.m * r.group > kGroupRows && unit_rows > kGroupRows ? unit_weight(28, 190, w.tiles, 28 + 190) : unit_weight(16, 190, w.tiles, 16 + 190);
+    return w;
+  }
+};
+
+// whether all threads of the two softmax groups say so
+__device__ __forceinline__ bool all_of_256(bool x) {
+  int y;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 256, p;\n\tselp.b32 %0, 1, 0, q;\n\t}" : "=r"(y) : "r"(static_cast<int>(x)) : "memory");
+  return y != 0;
+}
 
 template <int H, int kGroups>
 __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const ScaledParts parts,
@@ -123,6 +147,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
   float4* tops = reinterpret_cast<float4*>(ptr + L::kOffTop);
   float* scales = reinterpret_cast<float*>(ptr + L::kOffScale);
   float* factors = reinterpret_cast<float*>(ptr + L::kOffFactor);
+  const TcUnit* unit_slots = reinterpret_cast<const TcUnit*>(ptr + L::kOffUnit);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ptr + L::kOffBar + 8 * B_COUNT);
   auto bar = [&](int i) { return base + L::kOffBar + 8u * static_cast<uint32_t>(i); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = r.group;
@@ -134,15 +159,18 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
     mbar_init(bar(B_QFULL), 4);
     mbar_init(bar(B_QEMPTY), 8);
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bar(B_SFULL + s), 1);
+      mbar_init(bar(B_SFULL + 2 * s), 1);
+      mbar_init(bar(B_SFULL + 2 * s + 1), 1);
       mbar_init(bar(B_PFULL + 2 * s), 4);
       mbar_init(bar(B_PFULL + 2 * s + 1), 4);
+      mbar_init(bar(B_PVDONE + s), 1);
       mbar_init(bar(B_ODONE + s), 1);
     }
+    for (int s = 0; s < kUnitSlots; ++s) { mbar_init(bar(B_UFULL + s), 1); mbar_init(bar(B_UEMPTY + s), kUnitReaders); }
     for (int s = 0; s < kScaleSlots; ++s) mbar_init(bar(B_SCALE + s), 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {   // S of the two groups at columns 0 and 128, O at 256 and 384
+  if (warp == 12) {   // S of the two groups at columns 0, 64 and 128, 192, O at 256 and 384
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(const_cast<uint32_t*>(tmem_slot))), "r"(512u)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -152,7 +180,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
   fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_wait();
-  const AttentionLine line{c, r, 0, kUnit, kKeys};
+  const TcLine line(c, r, kUnit);
   const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (threadIdx.x == 0) leave_none(parts.desc, blockIdx.x);
 
@@ -164,73 +192,101 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       constexpr uint32_t kFormat = (1u << 4) | (static_cast<uint32_t>(128 >> 4) << 24);   // fp32 += fp16 x fp16, M 128
       constexpr uint32_t idesc_s = kFormat | (static_cast<uint32_t>(kKeys >> 3) << 17);
       constexpr uint32_t idesc_o = kFormat | (static_cast<uint32_t>(H >> 3) << 17) | (1u << 16);   // V is MN-major
-      int kst = 0, kphase = 0, vst = 0, vphase = 0, units = 0, ip[2] = {0, 0};
-      for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
-        if (*stop) return;
-        const bool both = kGroups == 2 && w.v.m * group - sg.rb * kUnit > kGroupRows;   // both groups have rows of their own
-        const int n_tiles = sg.t1 - sg.t0;
-        const uint32_t q0 = base + L::kOffQ;
+      int kst = 0, kphase = 0, vst = 0, vphase = 0, n_s[2] = {0, 0}, n_p[2] = {0, 0};       // scores and outputs of either group so far
+      for (int units = 0;; ++units) {
+        if (*stop || !mbar_wait(bar(B_UFULL + units % kUnitSlots), (units / kUnitSlots) & 1, stop)) { *stop = 1; break; }
+        const TcUnit& u = unit_slots[units % kUnitSlots];
+        if (!u.more) break;
+        const bool both = kGroups == 2 && u.m * group - u.sg.rb * kUnit > kGroupRows;   // both groups have rows of their own
+        const int n_tiles = u.sg.t1 - u.sg.t0;
         bool ok = mbar_wait(bar(B_QFULL), units & 1, stop);
-        ++units;
-        // K tiles and V tiles are used in order; a tile that both groups take is given back by the second
-        auto scores = [&](int s, bool last_reader) {
-          if (!mbar_wait(bar(B_KFULL + kst), kphase, stop)) return false;
-          fence_after();
-          const uint64_t q = operand_desc(q0 + (both ? s : 0) * L::kTileBytes, 1, 1024);
+        // the scores of group s over the K tile at hand, into the buffer that its outputs two before have left
+        auto scores = [&](int s) {
+          const uint64_t q = operand_desc(base + L::kOffQ + (both ? s : 0) * L::kQBytes, 1, 1024);
           const uint64_t k = operand_desc(base + L::kOffK + kst * L::kTileBytes, 1, L::kOctet);
+          const int b = n_s[s] & 1;
 #pragma unroll
           for (int ks = 0; ks < H / 16; ++ks) {
             const uint32_t within = (ks & 3) * 32;
-            umma_ss(tmem + s * 128, q + (((ks >> 2) * kGroupRows * 128 + within) >> 4), k + (((ks >> 2) * 1024 + within) >> 4), idesc_s, ks != 0);
+            umma_ss(tmem + s * 128 + b * 64, q + (((ks >> 2) * kGroupRows * 128 + within) >> 4), k + (((ks >> 2) * 1024 + within) >> 4), idesc_s, ks != 0);
           }
-          umma_commit(bar(B_SFULL + s));
-          if (last_reader) {
-            umma_commit(bar(B_KEMPTY + kst));
-            if (++kst == L::kKStages) { kst = 0; kphase ^= 1; }
-          }
+          umma_commit(bar(B_SFULL + 2 * s + b));
+          ++n_s[s];
+        };
+        auto k_tile = [&]() {
+          const bool there = mbar_wait(bar(B_KFULL + kst), kphase, stop);
+          fence_after();
+          return there;
+        };
+        auto k_done = [&]() {
+          umma_commit(bar(B_KEMPTY + kst));
+          if (++kst == L::kKStages) { kst = 0; kphase ^= 1; }
+        };
+        auto output = [&](int s, bool first, bool last) {
+          const int b = n_p[s] & 1;
+          if (!mbar_wait(bar(B_PFULL + 2 * s + b), (n_p[s] >> 1) & 1, stop)) return false;
+          fence_after();
+          const uint64_t v = operand_desc(base + L::kOffV + vst * L::kTileBytes, 1024 >> 4, L::kOctet);
+          const uint32_t p = tmem + s * 128 + b * 64;
+#pragma unroll
+          for (int kt = 0; kt < kKeys / 16; ++kt) umma_ts(tmem + 256 + s * 128, p + kt * 8, v + ((kt * 2 * L::kOctet) >> 4), idesc_o, !first || kt != 0);
+          umma_commit(bar(last ? B_ODONE + s : B_PVDONE + s));
+          ++n_p[s];
           return true;
         };
-        auto output = [&](int s, bool first, bool last_reader) {
-          if (!mbar_wait(bar(B_VFULL + vst), vphase, stop)) return false;
-          const uint64_t v = operand_desc(base + L::kOffV + vst * L::kTileBytes, 1024 >> 4, L::kOctet);
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {     // the second half of P is still being made under the first half's products
-            if (!mbar_wait(bar(B_PFULL + 2 * s + half), ip[s] & 1, stop)) return false;
-            fence_after();
-#pragma unroll
-            for (int kt = half * (kKeys / 32); kt < (half + 1) * (kKeys / 32); ++kt)
-              umma_ts(tmem + 256 + s * 128, tmem + s * 128 + kt * 8, v + ((kt * 2 * L::kOctet) >> 4), idesc_o, !first || kt != 0);
-          }
-          ++ip[s];
-          if (last_reader) {
-            umma_commit(bar(B_VEMPTY + vst));
-            if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
-          }
-          return true;
+        auto v_done = [&]() {
+          umma_commit(bar(B_VEMPTY + vst));
+          if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
         };
         if (both) {
-          ok = ok && scores(0, false) && scores(1, true);
-          for (int t = 0; ok && t < n_tiles; ++t)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              ok = ok && output(s, t == 0, s == 1);
+          for (int t = 0; ok && t <= n_tiles; ++t) {       // scores a tile ahead of the outputs
+            if (t < n_tiles) {
+              ok = k_tile();
               if (!ok) break;
-              if (t + 1 < n_tiles) ok = scores(s, s == 1);
-              else umma_commit(bar(B_ODONE + s));
+              scores(0);
+              scores(1);
+              k_done();
             }
+            if (t == 0) continue;
+            ok = mbar_wait(bar(B_VFULL + vst), vphase, stop);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) ok = ok && output(s, t == 1, t == n_tiles);
+            v_done();
+          }
         } else {
-          ok = ok && scores(0, true);
-          if (n_tiles > 1) ok = ok && scores(1, true);
-          for (int t = 0; ok && t < n_tiles; ++t) {
-            const int s = t & 1;
-            ok = output(s, t < 2, true);
-            if (!ok) break;
-            if (t + 2 < n_tiles) ok = scores(s, true);
-            else umma_commit(bar(B_ODONE + s));
+          for (int t = 0; ok && t < n_tiles + 4; ++t) {    // four tiles ahead, two of either group
+            if (t >= 4) {
+              ok = mbar_wait(bar(B_VFULL + vst), vphase, stop) && output(t & 1, t < 6, t + 2 >= n_tiles + 4);
+              if (!ok) break;
+              v_done();
+            }
+            if (t < n_tiles) {
+              ok = k_tile();
+              if (!ok) break;
+              scores(t & 1);
+              k_done();
+            }
           }
         }
         if (!ok) *stop = 1;
-      });
+        mbar_arrive(bar(B_UEMPTY + units % kUnitSlots));
+      }
+    } else if (warp == 13) {
+      // -------------------------------------------------------------------------------------------- stretches of units
+      int units = 0;
+      auto publish = [&](const TcUnit& u) {
+        if (lane == 0) {
+          if (*stop == 0 && mbar_wait(bar(B_UEMPTY + units % kUnitSlots), ((units / kUnitSlots) & 1) ^ 1, stop)) {
+            const_cast<TcUnit*>(unit_slots)[units % kUnitSlots] = u;
+            mbar_arrive(bar(B_UFULL + units % kUnitSlots));
+          } else {
+            *stop = 1;
+          }
+        }
+        ++units;
+      };
+      for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) { publish(TcUnit{sg, w.v.row0, w.v.m, w.v.n, 1}); });
+      publish(TcUnit{});
     }
     __syncwarp();
   } else if (warp >= 8) {
@@ -240,16 +296,21 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
     const uint8_t *k_codes = reinterpret_cast<const uint8_t*>(c.k), *v_codes = reinterpret_cast<const uint8_t*>(c.v);
     int tiles_issued = 0;
     int kst = 0, kphase = 1, vst = 0, vphase = 1, units = 0, tiles = 0;
-    for_segments(line, share, blockIdx.x, [&](const ReqWork& w, const Segment& sg) {
-      const int first = sg.rb * kUnit, total = w.v.m * group, rows = min(kUnit, total - first);
-      ++units;
+    for (;; ++units) {
+      if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_UFULL + units % kUnitSlots), (units / kUnitSlots) & 1, stop))) { *stop = 1; break; }
+      const TcUnit u = unit_slots[units % kUnitSlots];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_UEMPTY + units % kUnitSlots));
+      if (!u.more) break;
+      const Segment& sg = u.sg;
+      const int first = sg.rb * kUnit, total = u.m * group, rows = min(kUnit, total - first);
       const int32_t* table = c.table + static_cast<int64_t>(sg.req) * c.table_stride;
-      const int groups = min((w.v.n + 15) / 16, sg.t1 * 8);     // 16-key groups up to the end of the segment
-      // lane l looks after group l of four tiles: the block's place among all and (one warp) its scales; those of the next round
+      const int groups = min((u.n + 15) / 16, sg.t1 * 4);       // 16-key groups up to the end of the segment
+      // lane l looks after group l of eight tiles: the block's place among all and (one warp) its scales; those of the next round
       // and the table's entries of the one after are under way
       auto page_of = [&](int e) { return e < groups ? table[quotient(e, cpp)] : 0; };
       auto block_of = [&](int e, int page) { return e < groups ? (checked_page(c, page) * c.Hkv + sg.g) * cpp + (e - quotient(e, cpp) * cpp) : 0; };
-      int block, page_next = page_of(sg.t0 * 8 + lane), block_next = block_of(sg.t0 * 8 + lane, page_next);
+      int block, page_next = page_of(sg.t0 * 4 + lane), block_next = block_of(sg.t0 * 4 + lane, page_next);
       float ks, vs, ks_next = 1.f, vs_next = 1.f;
       auto scales_of = [&](int e) {
         if (warp == 8 && e < groups) {
@@ -257,47 +318,44 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           vs_next = sc.v[block_next];
         }
       };
-      scales_of(sg.t0 * 8 + lane);
-      page_next = page_of(sg.t0 * 8 + 32 + lane);
-      // piece i of the segment: keys 64 (i % 2) .. of K (i % 4 < 2) or V of tile t0 + i / 4; this warp: 16 of them
-      const int n_pieces = (sg.t1 - sg.t0) * 4;
+      scales_of(sg.t0 * 4 + lane);
+      page_next = page_of(sg.t0 * 4 + 32 + lane);
+      // piece i of the segment: K (i even) or V of tile t0 + i / 2; this warp: 16 keys
+      const int n_pieces = (sg.t1 - sg.t0) * 2;
       int issued = 0, into = 0;
       auto issue = [&]() {
         if (issued < n_pieces) {
-          const int t = sg.t0 + (issued >> 2), ahead = (issued >> 2) & 3;
-          if ((issued & 3) == 0) {
+          const int t = sg.t0 + (issued >> 1), ahead = (issued >> 1) & 7;
+          if ((issued & 1) == 0) {
             if (ahead == 0) {
               block = block_next;
               ks = ks_next;
               vs = vs_next;
-              block_next = block_of((t + 4) * 8 + lane, page_next);
+              block_next = block_of((t + 8) * 4 + lane, page_next);
               ks_next = vs_next = 1.f;
-              scales_of((t + 4) * 8 + lane);
-              page_next = page_of((t + 8) * 8 + lane);
+              scales_of((t + 8) * 4 + lane);
+              page_next = page_of((t + 16) * 4 + lane);
             }
             if (warp == 8) {
               float* to = scales + ((tiles_issued) % kScaleSlots) * kScaleWords;
-              const bool mine = lane >> 3 == ahead;
-              const float lv = warp_max(mine ? __log2f(fabsf(vs)) : -INFINITY);
+              const bool mine = lane >> 2 == ahead;
+              float lv = __log2f(fabsf(vs));
+              lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1));
+              lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 2));
               if (mine) {
-                to[lane & 7] = ks;
-                to[8 + (lane & 7)] = vs;
-                if ((lane & 7) == 0) to[16] = lv;
+                to[lane & 3] = ks;
+                to[4 + (lane & 3)] = vs;
+                if ((lane & 3) == 0) to[8] = lv;
               }
             }
             ++tiles_issued;
-            // what comes four tiles later is asked into L2: two groups a warp, a line a lane
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int which = part * 2 + i;
-              const int64_t at = static_cast<int64_t>(__shfl_sync(0xffffffffu, block_next, ahead * 8 + which)) * 16 * H + (lane & 15) * H;
-              if ((t + 4) * 8 + which < groups && (H == 128 || !(lane & 1))) prefetch_line((lane < 16 ? k_codes : v_codes) + at);
-            }
+            // what comes eight tiles later is asked into L2: a group a warp, a line a lane
+            const int64_t at = static_cast<int64_t>(__shfl_sync(0xffffffffu, block_next, ahead * 4 + part)) * 16 * H + (lane & 15) * H;
+            if ((t + 8) * 4 + part < groups && (H == 128 || !(lane & 1))) prefetch_line((lane < 16 ? k_codes : v_codes) + at);
           }
-          const int which = (issued & 1) * 4 + part;
-          const int64_t b = __shfl_sync(0xffffffffu, block, ahead * 8 + which);
-          if (t * 8 + which < groups) {
-            const uint8_t* from = (issued & 2 ? v_codes : k_codes) + b * 16 * H + lane * 16;
+          const int64_t b = __shfl_sync(0xffffffffu, block, ahead * 4 + part);
+          if (t * 4 + part < groups) {
+            const uint8_t* from = (issued & 1 ? v_codes : k_codes) + b * 16 * H + lane * 16;
             const uint32_t to = base + L::kOffRaw + into * L::kPieceBytes + part * 16 * H + lane * 16;
 #pragma unroll
             for (int i = 0; i < H / 32; ++i) copy_16(to + i * 512, from + i * 512);
@@ -310,13 +368,13 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
 #pragma unroll 1
       for (int i = 0; i < L::kPieces - 1; ++i) issue();
       // the unit's Q: a row per thread
-      if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_QEMPTY), (units & 1), stop))) { *stop = 1; return; }
+      if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_QEMPTY), (units & 1) ^ 1, stop))) { *stop = 1; break; }
       for (int s = 0; s < (rows > kGroupRows ? kGroups : 1); ++s) {
         const int mine = threadIdx.x & 127, at = first + s * kGroupRows + mine;
         uint4 x[H / 8];
         if (at < total) {
           const int j = quotient(at, group);
-          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(r.q) + (w.v.row0 + j) * r.q_stride + (static_cast<int64_t>(sg.g) * group + (at - j * group)) * H;
+          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(r.q) + (u.row0 + j) * r.q_stride + (static_cast<int64_t>(sg.g) * group + (at - j * group)) * H;
           if (whole_q) {
 #pragma unroll
             for (int i = 0; i < H / 8; ++i) x[i] = reinterpret_cast<const uint4*>(q)[i];
@@ -338,7 +396,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
         const int e = min(max(268 - static_cast<int>(most >> 23), 1), 253);
         const float up = __uint_as_float(static_cast<uint32_t>(e) << 23);
         factors[s * kGroupRows + mine] = __uint_as_float(static_cast<uint32_t>(254 - e) << 23) * (r.scale * kLog2e);
-        const uint32_t to = base + L::kOffQ + s * L::kTileBytes + mine * 128;
+        const uint32_t to = base + L::kOffQ + s * L::kQBytes + mine * 128;
 #pragma unroll
         for (int i = 0; i < H / 8; ++i) {
           uint32_t y[4];
@@ -353,29 +411,26 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(B_QFULL));
 
-      const int end = w.v.n, prefix = end - w.v.m + (r.parents ? 0 : first / group + 1);
+      const int end = u.n, prefix = end - u.m + (r.parents ? 0 : first / group + 1);
       // a tile of K or V: clean(key, codes) changes what may not become part of a product
       int piece = 0;
       auto convert = [&](uint32_t tile, auto clean) {
-#pragma unroll 1
-        for (int p = 0; p < kKeys / kPieceKeys; ++p) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(L::kPieces - 2) : "memory");
-          __syncwarp();
-          const uint32_t from = base + L::kOffRaw + piece * L::kPieceBytes + part * 16 * H + lane * 8, to = tile + (p * 8 + part * 2) * L::kOctet + (chunk >> 3) * 1024;
-          uint2 x[16 / kAtOnce];
+        asm volatile("cp.async.wait_group %0;" ::"n"(L::kPieces - 2) : "memory");
+        __syncwarp();
+        const uint32_t from = base + L::kOffRaw + piece * L::kPieceBytes + part * 16 * H + lane * 8, to = tile + part * 2 * L::kOctet + (chunk >> 3) * 1024;
+        uint2 x[16 / kAtOnce];
 #pragma unroll
-          for (int i = 0; i < 16 / kAtOnce; ++i)
-            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x[i].x), "=r"(x[i].y) : "r"(from + i * 256));
+        for (int i = 0; i < 16 / kAtOnce; ++i)
+          asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x[i].x), "=r"(x[i].y) : "r"(from + i * 256));
 #pragma unroll
-          for (int i = 0; i < 16 / kAtOnce; ++i) {
-            const int key = i * kAtOnce + sub, row = key & 7;
-            clean(p * kPieceKeys + part * 16 + key, x[i]);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (key >> 3) * L::kOctet + row * 128 + (((chunk & 7) ^ row) << 4)), "r"(half2_of(x[i].x)),
-                         "r"(half2_of_upper(x[i].x)), "r"(half2_of(x[i].y)), "r"(half2_of_upper(x[i].y)) : "memory");
-          }
-          issue();       // into the place of the piece before this one, which all lanes have read
-          if (++piece == L::kPieces) piece = 0;
+        for (int i = 0; i < 16 / kAtOnce; ++i) {
+          const int key = i * kAtOnce + sub, row = key & 7;
+          clean(part * 16 + key, x[i]);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (key >> 3) * L::kOctet + row * 128 + (((chunk & 7) ^ row) << 4)), "r"(half2_of(x[i].x)),
+                       "r"(half2_of_upper(x[i].x)), "r"(half2_of(x[i].y)), "r"(half2_of_upper(x[i].y)) : "memory");
         }
+        issue();       // into the place of the piece before this one, which all lanes have read
+        if (++piece == L::kPieces) piece = 0;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       };
@@ -406,7 +461,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
               if (i) x.y = y; else x.x = y;
             }
           });
-          if (found) odd[units & 1] = units;
+          if (found) odd[(units + 1) & 1] = units + 1;
           __syncwarp();
         }
         if (lane == 0) {
@@ -417,7 +472,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       }
       asm volatile("cp.async.wait_all;" ::: "memory");      // (copies are still under way only where the segment was given up)
       __syncwarp();
-    });
+    }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     // ------------------------------------------------------------------------------------------------ softmax, output
@@ -425,18 +480,14 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tmem_s = tmem + lanes + s * 128, tmem_o = tmem + lanes + 256 + s * 128;
     int is = 0, units = 0, tiles = 0;
-    Walk<AttentionLine> walk(line, share, blockIdx.x);
-    TcUnit next;
-    auto advance = [&]() {
-      if (!walk.next(next.sg)) return false;
-      next.row0 = walk.w.v.row0;
-      next.m = walk.w.v.m;
-      next.n = walk.w.v.n;
-      return true;
-    };
     int done[2] = {0, 0};       // units that either group has finished
-    for (bool have = advance(); have;) {
-      const TcUnit u = next;
+    int n_pv = 0;               // outputs of the group, but for the last of every unit
+    for (;;) {
+      const bool known = *stop == 0 && mbar_wait(bar(B_UFULL + units % kUnitSlots), (units / kUnitSlots) & 1, stop);
+      if (!known) *stop = 1;
+      const TcUnit u = unit_slots[units % kUnitSlots];
+      if (!all_of_256(known && u.more)) break;       // (all or none: there are barriers ahead)
+      if (lane == 0) mbar_arrive(bar(B_UEMPTY + units % kUnitSlots));
       ++units;
       const int first = u.sg.rb * kUnit, rows = min(kUnit, u.m * group - first);
       const bool both = kGroups == 2 && rows > kGroupRows;
@@ -487,57 +538,50 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       for (int t = 0; t < n_tiles; ++t, ++tiles) {
         if (!ok || t < t_first || (step == 2 && ((t ^ s) & 1))) continue;
         // (every decision to give up is the whole warp's: the instructions that follow need all lanes)
-        const int slot = tiles % kScaleSlots;
+        const int slot = tiles % kScaleSlots, b = is & 1;
         if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_SCALE + slot), (tiles / kScaleSlots) & 1, stop) &&
-                                         mbar_wait(bar(B_SFULL + s), is & 1, stop))) { ok = false; continue; }
+                                         mbar_wait(bar(B_SFULL + 2 * s + b), (is >> 1) & 1, stop))) { ok = false; continue; }
         ++is;
         fence_after();
         if (t + step >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY));    // the group is done with Q
         const int x0 = (u.sg.t0 + t) * kKeys;
         const bool masked = x0 + kKeys > prefix;
+        const uint32_t tmem_b = tmem_s + b * 64;
         if (active) {
-          const float* ks = scales + slot * kScaleWords;
-          const float* vs = ks + 8;
-          // Scores of tiles that some row does not see all of are scaled and masked in tensor memory, in a pass of its own: the code
-          // that every tile runs through stays short.
+          float4 ks = *reinterpret_cast<const float4*>(scales + slot * kScaleWords);
+          const float4 vs = *reinterpret_cast<const float4*>(scales + slot * kScaleWords + 4);
+          const float lv = scales[slot * kScaleWords + 8];
+          float v[kKeys];
+          tmem_ld32_nowait(tmem_b, v);
+          tmem_ld32_nowait(tmem_b + 32, v + 32);
+          tmem_ld_wait<kKeys>(v);
+          ks.x *= factor;
+          ks.y *= factor;
+          ks.z *= factor;
+          ks.w *= factor;
+          // Scores of tiles that some row does not see all of are scaled and masked first.
           if (masked) {
-#pragma unroll 1
-            for (int q = 0; q < kKeys / 32; ++q) {
-              const uint32_t see = view.seen(x0 + q * 32, prefix, end);
-              float x[32];
-              tmem_ld32(tmem_s + q * 32, x);
-              const float f0 = factor * ks[2 * q], f1 = factor * ks[2 * q + 1];
-              uint32_t y[32];
+            const uint32_t see0 = view.seen(x0, prefix, end), see1 = view.seen(x0 + 32, prefix, end);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) y[i] = (see >> i) & 1u ? __float_as_uint(x[i] * (i < 16 ? f0 : f1)) : 0xff800000u;
-              tmem_st16(tmem_s + q * 32, y);
-              tmem_st16(tmem_s + q * 32 + 16, y + 16);
+            for (int i = 0; i < kKeys; ++i) {
+              const float f = i < 16 ? ks.x : i < 32 ? ks.y : i < 48 ? ks.z : ks.w;
+              v[i] = ((i < 32 ? see0 : see1) >> (i & 31)) & 1u ? v[i] * f : -INFINITY;
             }
-            tmem_st_wait();
+            ks = make_float4(1.f, 1.f, 1.f, 1.f);
           }
-          const float by = masked ? 1.f : factor;
           float mx = -INFINITY;
-          const float lv = ks[16];
-          float v[2][32];
-          tmem_ld32_nowait(tmem_s, v[0]);
 #pragma unroll
-          for (int q = 0; q < kKeys / 32; ++q) {
-            float* x = v[q & 1];
-            tmem_ld_wait<32>(x);
-            if (q + 1 < kKeys / 32) tmem_ld32_nowait(tmem_s + (q + 1) * 32, v[(q + 1) & 1]);
+          for (int q = 0; q < 4; ++q) {
+            const float f = q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w;
+            float top = v[q * 16];
+            if (f >= 0.f) {      // (the same for all rows: a row's own factor is positive)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              const float f = by * (masked ? 1.f : ks[2 * q + b]);
-              float top = x[b * 16];
-              if (f >= 0.f) {      // (the same for all rows: a row's own factor is positive)
+              for (int i = 1; i < 16; ++i) top = fmaxf(top, v[q * 16 + i]);
+            } else {
 #pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, x[b * 16 + i]);
-              } else {
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top = fminf(top, x[b * 16 + i]);
-              }
-              mx = fmaxf(mx, top * f);
+              for (int i = 1; i < 16; ++i) top = fminf(top, v[q * 16 + i]);
             }
+            mx = fmaxf(mx, top * f);
           }
           const bool raise = mx > m + kRaiseBy || (m == -INFINITY && mx > -INFINITY);
           const bool raise_u = mx + lv > top_u + kRaiseBy || (top_u == -INFINITY && mx + lv > -INFINITY);
@@ -548,7 +592,11 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
             }
             const float f = raise_u ? exp2_approx(top_u - (mx + lv)) : 1.f;
             if (raise_u) top_u = mx + lv;
-            if (t != t_first) {   // the products so far are complete: they came before these scores
+            // The output of the group's tile before may be under way; of the one before that it is complete, since these scores came
+            // after it.
+            if (t != t_first && ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(B_PVDONE + s), (n_pv - 1) & 1, stop));
+            if (t != t_first && ok) {
+              fence_after();
 #pragma unroll 1
               for (int q = 0; q < H / 32; ++q) {
                 float o[32];
@@ -565,46 +613,35 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           const float ref = m == -INFINITY ? 0.f : m;
           const float weight = top_u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - top_u, 110.f));
           float sum0 = 0.f, sum1 = 0.f;
-          tmem_ld32_nowait(tmem_s, v[0]);
 #pragma unroll
-          for (int q = 0; q < kKeys / 32; ++q) {
-            float* x = v[q & 1];
-            tmem_ld_wait<32>(x);
-            if (q + 1 < kKeys / 32) tmem_ld32_nowait(tmem_s + (q + 1) * 32, v[(q + 1) & 1]);
+          for (int h = 0; h < 2; ++h) {
             uint32_t p[16];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float f = by * (masked ? 1.f : ks[2 * q + e]), wb = top_u == -INFINITY ? 0.f : weight * vs[2 * q + e];
+              const int q = 2 * h + e;
+              const float f = q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w;
+              const float wb = top_u == -INFINITY ? 0.f : weight * (q == 0 ? vs.x : q == 1 ? vs.y : q == 2 ? vs.z : vs.w);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                float a = x[e * 16 + 2 * i], b = x[e * 16 + 2 * i + 1];
-                fma2(a, b, f, -ref);
+                float a = v[q * 16 + 2 * i], y = v[q * 16 + 2 * i + 1];
+                fma2(a, y, f, -ref);
                 a = exp2_approx(a);
-                b = exp2_approx(b);
-                add2(sum0, sum1, a, b);
-                mul2(a, b, wb);
-                p[e * 8 + i] = pack_half(a, b);
+                y = exp2_approx(y);
+                add2(sum0, sum1, a, y);
+                mul2(a, y, wb);
+                p[e * 8 + i] = pack_half(a, y);
               }
             }
-            tmem_st16(tmem_s + q * 16, p);     // P lies over the scores
-            if (q == kKeys / 64 - 1) {
-              tmem_st_wait();
-              fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * s));
-            }
+            tmem_st16(tmem_b + h * 16, p);     // P lies over the scores
           }
           l += sum0 + sum1;
           tmem_st_wait();
         }
+        if (t + step < n_tiles) ++n_pv;
         fence_before();
         __syncwarp();
-        if (lane == 0) {
-          if (!active) mbar_arrive(bar(B_PFULL + 2 * s));
-          mbar_arrive(bar(B_PFULL + 2 * s + 1));
-        }
+        if (lane == 0) mbar_arrive(bar(B_PFULL + 2 * s + b));
       }
-      have = advance();
       // The groups' results.  With rows of their own each writes its own; groups that shared rows also share the writing,
       // half of the columns each: both results of a row are in the same lane of tensor memory, only maximum, sum and the
       // numerators' reference have to be exchanged.
