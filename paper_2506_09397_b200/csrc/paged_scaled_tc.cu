@@ -15,8 +15,8 @@
 // first tiles.
 //   warps 0-3, 4-7 : softmax and output of the two groups
 //   warps 8-11     : K, V and Q to fp16, scales
-//   warp 12        : tensor-memory allocation, products (one thread)
-//   warp 13        : the block's stretches of units, for all others; 14 and 15 only complete the warpgroup
+//   warps 12, 13   : products of either group (one thread each: a product takes about 70 cycles to issue), tensor-memory allocation
+//   warp 14        : the block's stretches of units, for all others; 15 only completes the warpgroup
 // Every wait is bounded; when one runs out the block says so in *status, lets what is under way land, frees its tensor
 // memory and returns.
 #include "kernels.h"
@@ -104,14 +104,14 @@ __device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
 }
 __device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-// A unit, or the stretch of it that the block works on, as warp 13 leaves it in shared memory.
+// A unit, or the stretch of it that the block works on, as warp 14 leaves it in shared memory.
 struct TcUnit {
   Segment sg;
   int row0, m, n;
   int more;        // 0: there are no more
 };
 static_assert(sizeof(TcUnit) <= 64);
-constexpr int kUnitReaders = 13;       // warps 0 - 12
+constexpr int kUnitReaders = 14;       // warps 0 - 13
 
 // The line of 64-key tiles with units of up to unit_rows rows.
 struct TcLine : AttentionLine {
@@ -154,8 +154,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *stop = odd[0] = odd[1] = 0;
-    for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 4); mbar_init(bar(B_KEMPTY + s), 1); }
-    for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 4); mbar_init(bar(B_VEMPTY + s), 1); }
+    for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 4); mbar_init(bar(B_KEMPTY + s), 2); }
+    for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 4); mbar_init(bar(B_VEMPTY + s), 2); }
     mbar_init(bar(B_QFULL), 4);
     mbar_init(bar(B_QEMPTY), 8);
     for (int s = 0; s < 2; ++s) {
@@ -187,91 +187,61 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
   // The registers of the block, 512 x 128, go where they are needed: 8 warps x 152, 4 x 128, 4 x 80 (all 65,536).
   if (warp >= 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 12 && lane == 0) {
+    if (warp < 14 && lane == 0) {
       // ------------------------------------------------------------------------------------------------ products
       constexpr uint32_t kFormat = (1u << 4) | (static_cast<uint32_t>(128 >> 4) << 24);   // fp32 += fp16 x fp16, M 128
       constexpr uint32_t idesc_s = kFormat | (static_cast<uint32_t>(kKeys >> 3) << 17);
       constexpr uint32_t idesc_o = kFormat | (static_cast<uint32_t>(H >> 3) << 17) | (1u << 16);   // V is MN-major
-      int kst = 0, kphase = 0, vst = 0, vphase = 0, n_s[2] = {0, 0}, n_p[2] = {0, 0};       // scores and outputs of either group so far
+      const int s = warp - 12;
+      int before = 0, n_s = 0, n_p = 0;       // tiles of earlier units, scores and outputs of the group so far
       for (int units = 0;; ++units) {
         if (*stop || !mbar_wait(bar(B_UFULL + units % kUnitSlots), (units / kUnitSlots) & 1, stop)) { *stop = 1; break; }
         const TcUnit& u = unit_slots[units % kUnitSlots];
         if (!u.more) break;
         const bool both = kGroups == 2 && u.m * group - u.sg.rb * kUnit > kGroupRows;   // both groups have rows of their own
-        const int n_tiles = u.sg.t1 - u.sg.t0;
+        const int n_tiles = u.sg.t1 - u.sg.t0, step = both ? 1 : 2, t_first = both ? 0 : s, mine = (n_tiles - t_first + step - 1) / step;
+        // (in every unit, also where the group has no tile: then all K and V of earlier units have been there, and the parity of a
+        // stage that the other group has used last cannot be taken for that of the phase before)
         bool ok = mbar_wait(bar(B_QFULL), units & 1, stop);
-        // the scores of group s over the K tile at hand, into the buffer that its outputs two before have left
-        auto scores = [&](int s) {
-          const uint64_t q = operand_desc(base + L::kOffQ + (both ? s : 0) * L::kQBytes, 1, 1024);
-          const uint64_t k = operand_desc(base + L::kOffK + kst * L::kTileBytes, 1, L::kOctet);
-          const int b = n_s[s] & 1;
+        const uint64_t q = operand_desc(base + L::kOffQ + (both ? s : 0) * L::kQBytes, 1, 1024);
+        // scores go two tiles ahead of the outputs, into the buffer that those have left (products of a thread run in order)
+        for (int i = 0; ok && i < mine + 2; ++i) {
+          if (i >= 2) {
+            const int at = before + t_first + (i - 2) * step, st = at % L::kVStages, b = n_p & 1;
+            ok = mbar_wait(bar(B_VFULL + st), (at / L::kVStages) & 1, stop) && mbar_wait(bar(B_PFULL + 2 * s + b), (n_p >> 1) & 1, stop);
+            if (!ok) break;
+            fence_after();
+            const uint64_t v = operand_desc(base + L::kOffV + st * L::kTileBytes, 1024 >> 4, L::kOctet);
+            const uint32_t p = tmem + s * 128 + b * 64;
 #pragma unroll
-          for (int ks = 0; ks < H / 16; ++ks) {
-            const uint32_t within = (ks & 3) * 32;
-            umma_ss(tmem + s * 128 + b * 64, q + (((ks >> 2) * kGroupRows * 128 + within) >> 4), k + (((ks >> 2) * 1024 + within) >> 4), idesc_s, ks != 0);
+            for (int kt = 0; kt < kKeys / 16; ++kt) umma_ts(tmem + 256 + s * 128, p + kt * 8, v + ((kt * 2 * L::kOctet) >> 4), idesc_o, i != 2 || kt != 0);
+            umma_commit(bar(i == mine + 1 ? B_ODONE + s : B_PVDONE + s));
+            umma_commit(bar(B_VEMPTY + st));
+            if (!both) mbar_arrive(bar(B_VEMPTY + st));      // for the other group
+            ++n_p;
           }
-          umma_commit(bar(B_SFULL + 2 * s + b));
-          ++n_s[s];
-        };
-        auto k_tile = [&]() {
-          const bool there = mbar_wait(bar(B_KFULL + kst), kphase, stop);
-          fence_after();
-          return there;
-        };
-        auto k_done = [&]() {
-          umma_commit(bar(B_KEMPTY + kst));
-          if (++kst == L::kKStages) { kst = 0; kphase ^= 1; }
-        };
-        auto output = [&](int s, bool first, bool last) {
-          const int b = n_p[s] & 1;
-          if (!mbar_wait(bar(B_PFULL + 2 * s + b), (n_p[s] >> 1) & 1, stop)) return false;
-          fence_after();
-          const uint64_t v = operand_desc(base + L::kOffV + vst * L::kTileBytes, 1024 >> 4, L::kOctet);
-          const uint32_t p = tmem + s * 128 + b * 64;
+          if (i < mine) {
+            const int at = before + t_first + i * step, st = at % L::kKStages, b = n_s & 1;
+            ok = mbar_wait(bar(B_KFULL + st), (at / L::kKStages) & 1, stop);
+            if (!ok) break;
+            fence_after();
+            const uint64_t k = operand_desc(base + L::kOffK + st * L::kTileBytes, 1, L::kOctet);
 #pragma unroll
-          for (int kt = 0; kt < kKeys / 16; ++kt) umma_ts(tmem + 256 + s * 128, p + kt * 8, v + ((kt * 2 * L::kOctet) >> 4), idesc_o, !first || kt != 0);
-          umma_commit(bar(last ? B_ODONE + s : B_PVDONE + s));
-          ++n_p[s];
-          return true;
-        };
-        auto v_done = [&]() {
-          umma_commit(bar(B_VEMPTY + vst));
-          if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
-        };
-        if (both) {
-          for (int t = 0; ok && t <= n_tiles; ++t) {       // scores a tile ahead of the outputs
-            if (t < n_tiles) {
-              ok = k_tile();
-              if (!ok) break;
-              scores(0);
-              scores(1);
-              k_done();
+            for (int ks = 0; ks < H / 16; ++ks) {
+              const uint32_t within = (ks & 3) * 32;
+              umma_ss(tmem + s * 128 + b * 64, q + (((ks >> 2) * kGroupRows * 128 + within) >> 4), k + (((ks >> 2) * 1024 + within) >> 4), idesc_s, ks != 0);
             }
-            if (t == 0) continue;
-            ok = mbar_wait(bar(B_VFULL + vst), vphase, stop);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) ok = ok && output(s, t == 1, t == n_tiles);
-            v_done();
-          }
-        } else {
-          for (int t = 0; ok && t < n_tiles + 4; ++t) {    // four tiles ahead, two of either group
-            if (t >= 4) {
-              ok = mbar_wait(bar(B_VFULL + vst), vphase, stop) && output(t & 1, t < 6, t + 2 >= n_tiles + 4);
-              if (!ok) break;
-              v_done();
-            }
-            if (t < n_tiles) {
-              ok = k_tile();
-              if (!ok) break;
-              scores(t & 1);
-              k_done();
-            }
+            umma_commit(bar(B_SFULL + 2 * s + b));
+            umma_commit(bar(B_KEMPTY + st));
+            if (!both) mbar_arrive(bar(B_KEMPTY + st));
+            ++n_s;
           }
         }
+        before += n_tiles;
         if (!ok) *stop = 1;
         mbar_arrive(bar(B_UEMPTY + units % kUnitSlots));
       }
-    } else if (warp == 13) {
+    } else if (warp == 14) {
       // -------------------------------------------------------------------------------------------- stretches of units
       int units = 0;
       auto publish = [&](const TcUnit& u) {
