@@ -29,7 +29,7 @@ namespace {
 
 constexpr int kKeys = 64;                  // keys per tile
 constexpr int kGroupRows = 128;            // rows of a softmax group
-constexpr int kScaleSlots = 16;            // tiles whose scales are kept: more than copies, K, V and S are ahead of a softmax
+constexpr int kScaleSlots = 16;            // tiles whose scales are kept (written before a tile's K): more than copies, K and S are ahead of a softmax
 constexpr int kScaleWords = 12;            // ks [4], vs [4], the largest log2 |vs|
 constexpr int kUnitSlots = 4;              // stretches of units that are known ahead
 
@@ -61,7 +61,7 @@ static_assert(ScaledTc<128, 1>::kTotal + 512 <= 227 * 1024 && ScaledTc<128, 2>::
 
 // barriers, 8 bytes each
 enum { B_KFULL = 0, B_KEMPTY = 4, B_VFULL = 8, B_VEMPTY = 12, B_QFULL = 16, B_QEMPTY = 17, B_SFULL = 18, B_PFULL = 22, B_PVDONE = 26, B_ODONE = 28, B_UFULL = 30,
-       B_UEMPTY = B_UFULL + kUnitSlots, B_SCALE = B_UEMPTY + kUnitSlots, B_COUNT = B_SCALE + kScaleSlots };
+       B_UEMPTY = B_UFULL + kUnitSlots, B_COUNT = B_UEMPTY + kUnitSlots };
 static_assert(B_COUNT * 8 + 4 <= 512);
 
 // what a row sees of the request's own nodes
@@ -167,7 +167,6 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       mbar_init(bar(B_ODONE + s), 1);
     }
     for (int s = 0; s < kUnitSlots; ++s) { mbar_init(bar(B_UFULL + s), 1); mbar_init(bar(B_UEMPTY + s), kUnitReaders); }
-    for (int s = 0; s < kScaleSlots; ++s) mbar_init(bar(B_SCALE + s), 4);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 12) {   // S of the two groups at columns 0, 64 and 128, 192, O at 256 and 384
@@ -265,7 +264,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
     const int part = warp & 3, chunk = lane % kLanes, sub = lane / kLanes, cpp = c.ps / 16;
     const uint8_t *k_codes = reinterpret_cast<const uint8_t*>(c.k), *v_codes = reinterpret_cast<const uint8_t*>(c.v);
     int tiles_issued = 0;
-    int kst = 0, kphase = 1, vst = 0, vphase = 1, units = 0, tiles = 0;
+    int kst = 0, kphase = 1, vst = 0, vphase = 1, units = 0;
     for (;; ++units) {
       if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_UFULL + units % kUnitSlots), (units / kUnitSlots) & 1, stop))) { *stop = 1; break; }
       const TcUnit u = unit_slots[units % kUnitSlots];
@@ -404,7 +403,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       };
-      for (int t = sg.t0; t < sg.t1; ++t, ++tiles) {
+      for (int t = sg.t0; t < sg.t1; ++t) {
         bool ok = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_KEMPTY + kst), kphase, stop));
         if (!ok) { *stop = 1; break; }
         convert(base + L::kOffK + kst * L::kTileBytes, [](int, uint2&) {});
@@ -434,10 +433,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           if (found) odd[(units + 1) & 1] = units + 1;
           __syncwarp();
         }
-        if (lane == 0) {
-          mbar_arrive(bar(B_SCALE + tiles % kScaleSlots));
-          mbar_arrive(bar(B_VFULL + vst));
-        }
+        if (lane == 0) mbar_arrive(bar(B_VFULL + vst));
         if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");      // (copies are still under way only where the segment was given up)
@@ -509,8 +505,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
         if (!ok || t < t_first || (step == 2 && ((t ^ s) & 1))) continue;
         // (every decision to give up is the whole warp's: the instructions that follow need all lanes)
         const int slot = tiles % kScaleSlots, b = is & 1;
-        if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_SCALE + slot), (tiles / kScaleSlots) & 1, stop) &&
-                                         mbar_wait(bar(B_SFULL + 2 * s + b), (is >> 1) & 1, stop))) { ok = false; continue; }
+        if (!__all_sync(0xffffffffu, mbar_wait(bar(B_SFULL + 2 * s + b), (is >> 1) & 1, stop))) { ok = false; continue; }
         ++is;
         fence_after();
         if (t + step >= n_tiles && lane == 0) mbar_arrive(bar(B_QEMPTY));    // the group is done with Q
