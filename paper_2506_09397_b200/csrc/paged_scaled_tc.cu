@@ -7,8 +7,8 @@
 //     S = Q C^T      (M 128 x N 64 keys, contraction over H)       -> tensor memory, fp32, two buffers a group
 //     O += P D       (M 128 x N H, contraction over 64 keys)       P from tensor memory (fp16, over S)
 // A group's next scores are formed while it is at the softmax of the present ones.  The products take 16-bit operands, so four warps
-// turn the codes into fp16, from a ring of 64 keys a piece, K and V of a tile in turn, into operand tiles.  Each warp brings its
-// sixteen keys of a piece itself, with asynchronous 16-byte copies, and needs nobody to tell it that they have arrived.  They
+// turn the codes into fp16, from a ring of three tiles, into operand tiles.  Each warp brings its
+// sixteen keys of a tile itself, with asynchronous 16-byte copies, and needs nobody to tell it that they have arrived.  They
 // bring the queries too, as fp16 times a power of two per row.  A score meets its block's scale ks where it leaves tensor memory, a
 // numerator its vs before it is rounded.  The references of a row - m of the scores, u of the numerators - are raised only when
 // something exceeds them by more than 2^8; raising u means rescaling the row of O in tensor memory, which happens in a unit's
@@ -41,12 +41,12 @@ struct ScaledTc {
   static constexpr int kOctet = kHalves * 1024;          // eight rows
   static constexpr int kTileBytes = kKeys / 8 * kOctet;  // K or V
   static constexpr int kQBytes = kGroupRows / 8 * kOctet;
-  static constexpr int kKStages = 4, kVStages = 4;
+  static constexpr int kStages = kGroups == 1 ? 4 : 3;    // of K and V each
   static constexpr int kOffQ = 0;
   static constexpr int kOffK = kGroups * kQBytes;
-  static constexpr int kOffV = kOffK + kKStages * kTileBytes;
-  static constexpr int kPieces = H == 64 || kGroups == 1 ? 7 : 3, kPieceBytes = kKeys * H;
-  static constexpr int kOffRaw = kOffV + kVStages * kTileBytes;
+  static constexpr int kOffV = kOffK + kStages * kTileBytes;
+  static constexpr int kPieces = 3, kPieceBytes = 2 * kKeys * H;      // codes of K and V of a tile
+  static constexpr int kOffRaw = kOffV + kStages * kTileBytes;
   static constexpr int kOffBar = kOffRaw + kPieces * kPieceBytes;
   static constexpr int kOffTree = kOffBar + 512;         // parents of the nodes, one byte each, for either group
   static constexpr int kOffTop = kOffTree + 2 * kMaxTreeNodes;     // what the groups tell each other about a row
@@ -102,7 +102,6 @@ __device__ __forceinline__ void mul2(float& a, float& b, float f) {
 __device__ __forceinline__ void copy_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void prefetch_line(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // A unit, or the stretch of it that the block works on, as warp 14 leaves it in shared memory.
 struct TcUnit {
@@ -154,8 +153,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     *stop = odd[0] = odd[1] = 0;
-    for (int s = 0; s < L::kKStages; ++s) { mbar_init(bar(B_KFULL + s), 4); mbar_init(bar(B_KEMPTY + s), 2); }
-    for (int s = 0; s < L::kVStages; ++s) { mbar_init(bar(B_VFULL + s), 4); mbar_init(bar(B_VEMPTY + s), 2); }
+    for (int s = 0; s < L::kStages; ++s) { mbar_init(bar(B_KFULL + s), 4); mbar_init(bar(B_KEMPTY + s), 2); }
+    for (int s = 0; s < L::kStages; ++s) { mbar_init(bar(B_VFULL + s), 4); mbar_init(bar(B_VEMPTY + s), 2); }
     mbar_init(bar(B_QFULL), 4);
     mbar_init(bar(B_QEMPTY), 8);
     for (int s = 0; s < 2; ++s) {
@@ -206,8 +205,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
         // scores go two tiles ahead of the outputs, into the buffer that those have left (products of a thread run in order)
         for (int i = 0; ok && i < mine + 2; ++i) {
           if (i >= 2) {
-            const int at = before + t_first + (i - 2) * step, st = at % L::kVStages, b = n_p & 1;
-            ok = mbar_wait(bar(B_VFULL + st), (at / L::kVStages) & 1, stop) && mbar_wait(bar(B_PFULL + 2 * s + b), (n_p >> 1) & 1, stop);
+            const int at = before + t_first + (i - 2) * step, st = at % L::kStages, b = n_p & 1;
+            ok = mbar_wait(bar(B_VFULL + st), (at / L::kStages) & 1, stop) && mbar_wait(bar(B_PFULL + 2 * s + b), (n_p >> 1) & 1, stop);
             if (!ok) break;
             fence_after();
             const uint64_t v = operand_desc(base + L::kOffV + st * L::kTileBytes, 1024 >> 4, L::kOctet);
@@ -220,8 +219,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
             ++n_p;
           }
           if (i < mine) {
-            const int at = before + t_first + i * step, st = at % L::kKStages, b = n_s & 1;
-            ok = mbar_wait(bar(B_KFULL + st), (at / L::kKStages) & 1, stop);
+            const int at = before + t_first + i * step, st = at % L::kStages, b = n_s & 1;
+            ok = mbar_wait(bar(B_KFULL + st), (at / L::kStages) & 1, stop);
             if (!ok) break;
             fence_after();
             const uint64_t k = operand_desc(base + L::kOffK + st * L::kTileBytes, 1, L::kOctet);
@@ -264,7 +263,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
     const int part = warp & 3, chunk = lane % kLanes, sub = lane / kLanes, cpp = c.ps / 16;
     const uint8_t *k_codes = reinterpret_cast<const uint8_t*>(c.k), *v_codes = reinterpret_cast<const uint8_t*>(c.v);
     int tiles_issued = 0;
-    int kst = 0, kphase = 1, vst = 0, vphase = 1, units = 0;
+    int st = 0, phase = 1, units = 0;
     for (;; ++units) {
       if (!__all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_UFULL + units % kUnitSlots), (units / kUnitSlots) & 1, stop))) { *stop = 1; break; }
       const TcUnit u = unit_slots[units % kUnitSlots];
@@ -289,45 +288,40 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       };
       scales_of(sg.t0 * 4 + lane);
       page_next = page_of(sg.t0 * 4 + 32 + lane);
-      // piece i of the segment: K (i even) or V of tile t0 + i / 2; this warp: 16 keys
-      const int n_pieces = (sg.t1 - sg.t0) * 2;
-      int issued = 0, into = 0;
+      // the codes of the next tile, this warp's 16 keys of K and V
+      int issued = sg.t0, into = 0;
       auto issue = [&]() {
-        if (issued < n_pieces) {
-          const int t = sg.t0 + (issued >> 1), ahead = (issued >> 1) & 7;
-          if ((issued & 1) == 0) {
-            if (ahead == 0) {
-              block = block_next;
-              ks = ks_next;
-              vs = vs_next;
-              block_next = block_of((t + 8) * 4 + lane, page_next);
-              ks_next = vs_next = 1.f;
-              scales_of((t + 8) * 4 + lane);
-              page_next = page_of((t + 16) * 4 + lane);
-            }
-            if (warp == 8) {
-              float* to = scales + ((tiles_issued) % kScaleSlots) * kScaleWords;
-              const bool mine = lane >> 2 == ahead;
-              float lv = __log2f(fabsf(vs));
-              lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1));
-              lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 2));
-              if (mine) {
-                to[lane & 3] = ks;
-                to[4 + (lane & 3)] = vs;
-                if ((lane & 3) == 0) to[8] = lv;
-              }
-            }
-            ++tiles_issued;
-            // what comes eight tiles later is asked into L2: a group a warp, a line a lane
-            const int64_t at = static_cast<int64_t>(__shfl_sync(0xffffffffu, block_next, ahead * 4 + part)) * 16 * H + (lane & 15) * H;
-            if ((t + 8) * 4 + part < groups && (H == 128 || !(lane & 1))) prefetch_line((lane < 16 ? k_codes : v_codes) + at);
+        if (issued < sg.t1) {
+          const int t = issued, ahead = (t - sg.t0) & 7;
+          if (ahead == 0) {
+            block = block_next;
+            ks = ks_next;
+            vs = vs_next;
+            block_next = block_of((t + 8) * 4 + lane, page_next);
+            ks_next = vs_next = 1.f;
+            scales_of((t + 8) * 4 + lane);
+            page_next = page_of((t + 16) * 4 + lane);
           }
-          const int64_t b = __shfl_sync(0xffffffffu, block, ahead * 4 + part);
+          if (warp == 8) {
+            float* to = scales + (tiles_issued % kScaleSlots) * kScaleWords;
+            float lv = __log2f(fabsf(vs));
+            lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1));
+            lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 2));
+            if (lane >> 2 == ahead) {
+              to[lane & 3] = ks;
+              to[4 + (lane & 3)] = vs;
+              if ((lane & 3) == 0) to[8] = lv;
+            }
+          }
+          ++tiles_issued;
+          const int64_t at = static_cast<int64_t>(__shfl_sync(0xffffffffu, block, ahead * 4 + part)) * 16 * H + lane * 16;
           if (t * 4 + part < groups) {
-            const uint8_t* from = (issued & 1 ? v_codes : k_codes) + b * 16 * H + lane * 16;
-            const uint32_t to = base + L::kOffRaw + into * L::kPieceBytes + part * 16 * H + lane * 16;
+            const uint32_t to = base + L::kOffRaw + into * L::kPieceBytes + part * 32 * H + lane * 16;
 #pragma unroll
-            for (int i = 0; i < H / 32; ++i) copy_16(to + i * 512, from + i * 512);
+            for (int i = 0; i < H / 32; ++i) {
+              copy_16(to + i * 512, k_codes + at + i * 512);
+              copy_16(to + 16 * H + i * 512, v_codes + at + i * 512);
+            }
           }
           ++issued;
           if (++into == L::kPieces) into = 0;
@@ -381,60 +375,53 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       if (lane == 0) mbar_arrive(bar(B_QFULL));
 
       const int end = u.n, prefix = end - u.m + (r.parents ? 0 : first / group + 1);
-      // a tile of K or V: clean(key, codes) changes what may not become part of a product
       int piece = 0;
-      auto convert = [&](uint32_t tile, auto clean) {
+      for (int t = sg.t0; t < sg.t1; ++t) {
+        const bool ok = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_KEMPTY + st), phase, stop) && mbar_wait(bar(B_VEMPTY + st), phase, stop));
+        if (!ok) { *stop = 1; break; }
         asm volatile("cp.async.wait_group %0;" ::"n"(L::kPieces - 2) : "memory");
         __syncwarp();
-        const uint32_t from = base + L::kOffRaw + piece * L::kPieceBytes + part * 16 * H + lane * 8, to = tile + part * 2 * L::kOctet + (chunk >> 3) * 1024;
-        uint2 x[16 / kAtOnce];
+        const uint32_t from = base + L::kOffRaw + piece * L::kPieceBytes + part * 32 * H + lane * 8, within = st * L::kTileBytes + part * 2 * L::kOctet + (chunk >> 3) * 1024;
+        constexpr int kLoads = 16 / kAtOnce;
+        uint2 x[2 * kLoads];       // K, then V
 #pragma unroll
-        for (int i = 0; i < 16 / kAtOnce; ++i)
+        for (int i = 0; i < 2 * kLoads; ++i)
           asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x[i].x), "=r"(x[i].y) : "r"(from + i * 256));
-#pragma unroll
-        for (int i = 0; i < 16 / kAtOnce; ++i) {
-          const int key = i * kAtOnce + sub, row = key & 7;
-          clean(part * 16 + key, x[i]);
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (key >> 3) * L::kOctet + row * 128 + (((chunk & 7) ^ row) << 4)), "r"(half2_of(x[i].x)),
-                       "r"(half2_of_upper(x[i].x)), "r"(half2_of(x[i].y)), "r"(half2_of_upper(x[i].y)) : "memory");
-        }
-        issue();       // into the place of the piece before this one, which all lanes have read
+        issue();       // into the place of the tile before this one, which all lanes have read
         if (++piece == L::kPieces) piece = 0;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-      };
-      for (int t = sg.t0; t < sg.t1; ++t) {
-        bool ok = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_KEMPTY + kst), kphase, stop));
-        if (!ok) { *stop = 1; break; }
-        convert(base + L::kOffK + kst * L::kTileBytes, [](int, uint2&) {});
-        if (lane == 0) mbar_arrive(bar(B_KFULL + kst));
-        if (++kst == L::kKStages) { kst = 0; kphase ^= 1; }
-
-        ok = __all_sync(0xffffffffu, *stop == 0 && mbar_wait(bar(B_VEMPTY + vst), vphase, stop));
-        if (!ok) { *stop = 1; break; }
-        const uint32_t to = base + L::kOffV + vst * L::kTileBytes;
+        // A numerator of 0 does not silence a value that is no number: values of positions that hold no key become 0, and so do
+        // those that are no numbers, which the rows that see them get back at the end.
         const int x0 = t * kKeys;
-        if (x0 + kKeys <= prefix) {
-          convert(to, [](int, uint2&) {});
-        } else {
-          // A numerator of 0 does not silence a value that is no number: values of positions that hold no key become 0, and so
-          // do those that are no numbers, which the rows that see them get back at the end.
+        if (x0 + kKeys > prefix) {
           uint32_t found = 0;
-          convert(to, [&](int key, uint2& x) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              uint32_t y = x0 + key < end ? (i ? x.y : x.x) : 0u;
+          for (int i = kLoads; i < 2 * kLoads; ++i) {
+            const bool there = x0 + part * 16 + (i - kLoads) * kAtOnce + sub < end;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              uint32_t y = there ? (k ? x[i].y : x[i].x) : 0u;
               const uint32_t none = ((y & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;      // in the bytes 0x7f and 0xff
               found |= none;
               y &= ~((none >> 7) * 0xffu);
-              if (i) x.y = y; else x.x = y;
+              if (k) x[i].y = y; else x[i].x = y;
             }
-          });
+          }
           if (found) odd[(units + 1) & 1] = units + 1;
-          __syncwarp();
         }
-        if (lane == 0) mbar_arrive(bar(B_VFULL + vst));
-        if (++vst == L::kVStages) { vst = 0; vphase ^= 1; }
+#pragma unroll
+        for (int i = 0; i < 2 * kLoads; ++i) {
+          const int key = i % kLoads * kAtOnce + sub, row = key & 7;
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                       ::"r"(base + (i < kLoads ? L::kOffK : L::kOffV) + within + (key >> 3) * L::kOctet + row * 128 + (((chunk & 7) ^ row) << 4)), "r"(half2_of(x[i].x)),
+                       "r"(half2_of_upper(x[i].x)), "r"(half2_of(x[i].y)), "r"(half2_of_upper(x[i].y)) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar(B_KFULL + st));
+          mbar_arrive(bar(B_VFULL + st));
+        }
+        if (++st == L::kStages) { st = 0; phase ^= 1; }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");      // (copies are still under way only where the segment was given up)
       __syncwarp();
