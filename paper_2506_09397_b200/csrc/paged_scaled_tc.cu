@@ -350,11 +350,24 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
 #pragma unroll
           for (int i = 0; i < H / 8; ++i) x[i] = make_uint4(0, 0, 0, 0);
         }
-        uint32_t most = 0;       // |x| as bits of bf16, times 2^16: the largest finite one
+        uint32_t two = 0;        // the largest |x|, in pairs
 #pragma unroll
-        for (int i = 0; i < H / 2; ++i) {
-          const uint32_t v = reinterpret_cast<const uint32_t*>(x)[i], lo = v << 16 & 0x7fff0000u, hi = v & 0x7fff0000u;
-          most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+        for (int i = 0; i < H / 8; ++i) {
+          two = __vimax3_u16x2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu, two);
+          two = __vimax3_u16x2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu, two);
+        }
+        uint32_t most = max(two << 16, two & 0xffff0000u);
+        if (most >= 0x7f800000u) {        // of the finite ones
+          most = 0;
+#pragma unroll
+          for (int i = 0; i < H / 8; ++i) {
+            const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t lo = v[k] << 16 & 0x7fff0000u, hi = v[k] & 0x7fff0000u;
+              most = max(most, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+            }
+          }
         }
         const int e = min(max(268 - static_cast<int>(most >> 23), 1), 253);
         const float up = __uint_as_float(static_cast<uint32_t>(e) << 23);
