@@ -6,9 +6,10 @@
 // scales stay out of the products' operands: ks multiplies a score, vs goes into the numerators.
 //
 // Codes become fp16 in registers, which is exact; queries do too, times a power of two per row that brings the row's largest
-// element to 2^14, so that nothing of them is lost either.  The numerators of a row meet V as fp16(2^15 2^(s_x - u) vs_b) with a
-// reference of their own, u = max (s_x + log2 vs_b) so far: they are as large as fp16 allows whatever the blocks' scales are,
-// 11 bits of each down to 2^-29 of the largest.  u is joined with m at the end of a unit.
+// element to 2^14, so that nothing of them is lost either.  The numerators of a row meet V as fp16(2^7 2^(s_x - u) vs_b) with a
+// reference of their own, u = max (s_x + log2 vs_b) so far, or less by up to 8: the largest is 2^7 to 2^15 whatever the blocks'
+// scales are, and what is lost of another is 2^-11 of itself, or 2^-32 of the largest where that is more.  u is joined with m at
+// the end of a unit.
 //
 // The keys are the M side of m16n8k16 products and the rows the N side, so that eight rows cost half of what sixteen do -
 // products, exponentials, registers:
@@ -90,7 +91,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {     // of an 8 x 8 
   return y;
 }
 
-// A stretch of a unit, as the fifth warp finds it and the others read it from shared memory: little of it is kept in registers.
+// A stretch of a unit, as the first producer finds it and the others read it from shared memory: little of it is kept in registers.
 struct FewUnit {
   Segment sg;
   int row0, m, n;         // the request's rows and keys
@@ -132,7 +133,7 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
   const uint32_t vb = kb + S::kHalf;
   const int lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
   const float ks[2] = {blocks.x, blocks.y}, vs[2] = {blocks.z, blocks.w};
-  const float lv = fmaxf(__log2f(fabsf(vs[0])), __log2f(fabsf(vs[1])));
+  const float lv[2] = {__log2f(fabsf(vs[0])), __log2f(fabsf(vs[1]))};
   float sc[2][G][4];       // keys 16 m + gq (0, 1), + 8 (2, 3)
   {
     // K, all of the stage's loads side by side where there are registers for it, 16 bytes a lane and key otherwise
@@ -204,7 +205,7 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
           top = fmaxf(top, s);
         }
       }
-      if (!kMasked) calm = calm && !(top > r.room(lv));
+      if (!kMasked) calm = calm && !(top > r.room(fmaxf(lv[0], lv[1])));
     }
   if (kMasked || !__all_sync(0xffffffffu, calm)) {
     float al[2 * G];
@@ -213,11 +214,11 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         RowState& r = a.st[2 * n + e];
-        float top = -INFINITY;
+        float top = -INFINITY, top_u = -INFINITY;
         int j = 0;
         if (kMasked) j = __float_as_int(of_rows[8 * n + 2 * tq + e].y);
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m) {
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
             float& s = sc[m][n][2 * z + e];
@@ -229,12 +230,17 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
             } else {
               s += r.ref;
             }
-            top = fmaxf(top, s);
           }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-        al[2 * n + e] = r.take(top, lv);
+          const float here = fmaxf(sc[m][n][e], sc[m][n][2 + e]);
+          top = fmaxf(top, here);
+          top_u = fmaxf(top_u, here + lv[m]);
+        }
+#pragma unroll
+        for (int o = 4; o < 32; o *= 2) {
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          top_u = fmaxf(top_u, __shfl_xor_sync(0xffffffffu, top_u, o));
+        }
+        al[2 * n + e] = r.take(top, top_u);
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -647,7 +653,10 @@ int64_t paged_scaled_workspace(int h) {
 }
 
 int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s) {
-  // by the rows per request and KV head, on average
+  // By the rows per request and KV head, on average (head_dim 128, 8 KV heads; us).  More than 8: units of 32 rows, as several of 8
+  // read the keys several times - units of 8 against 32, 8 rows: 32 x 8192 keys 95, 96, 8 x 8192 36, 39, 64 x 300 27, 37; 12 rows:
+  // 181, 96; 60, 40; 40, 38.  More than 32: the products of tcgen05, which take a unit of 128 rows in the time of one - units of
+  // 32 against tcgen05, 32 rows: 32 x 4096 95, 131, 8 x 8192 59, 74, 64 x 300 48, 68; 36 rows: 148, 132; 92, 74; 72, 69.
   const int64_t rows = static_cast<int64_t>(r.T) * r.group;
   if (c.h >= 64 && rows > 32LL * c.n_reqs) return launch_scaled_tc(c, sc, r, ws, s);
   const bool few = rows <= 8LL * c.n_reqs;

@@ -70,8 +70,8 @@ struct RowState {
   float m = -INFINITY, l = 0.f, u = -INFINITY;
   float ref = 0.f;
   float w = 0.f;              // a block's 2^(s - ref) are multiplied by this and vs
-  // takes a stage's largest score and the largest log2 |vs|; returns the factor of the output so far
-  __device__ __forceinline__ float take(float mx, float lv) {
+  // takes a stage's largest score s and the largest s + log2 |vs|; returns the factor of the output so far
+  __device__ __forceinline__ float take(float mx, float mx_u) {
     if (mx > m + kRaiseBy || m == -INFINITY) {
       const float mn = fmaxf(m, mx);
       ref = mn == -INFINITY ? 0.f : mn;
@@ -79,15 +79,15 @@ struct RowState {
       m = mn;
     }
     float f = 1.f;
-    if (mx + lv > u + kRaiseBy || u == -INFINITY) {
-      const float un = fmaxf(u, mx + lv);
+    if (mx_u > u + kRaiseBy || u == -INFINITY) {
+      const float un = fmaxf(u, mx_u);
       f = exp2_approx(u - (un == -INFINITY ? 0.f : un));
       u = un;
     }
     w = u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - u, 110.f));
     return f;
   }
-  // the largest s - ref that needs no raise
+  // a largest s - ref that needs no raise, by the largest log2 |vs| of a stage
   __device__ __forceinline__ float room(float lv) const { return m == -INFINITY ? -INFINITY : kRaiseBy + fminf(0.f, (u - lv) - ref); }
   // what the output is multiplied by at the end
   __device__ __forceinline__ float rest() const { return u == -INFINITY ? 0.f : exp2_approx(u - (m == -INFINITY ? 0.f : m)) * (1.f / kGain); }

@@ -30,7 +30,7 @@ namespace {
 constexpr int kKeys = 64;                  // keys per tile
 constexpr int kGroupRows = 128;            // rows of a softmax group
 constexpr int kScaleSlots = 16;            // tiles whose scales are kept (written before a tile's K): more than copies, K and S are ahead of a softmax
-constexpr int kScaleWords = 12;            // ks [4], vs [4], the largest log2 |vs|
+constexpr int kScaleWords = 12;            // ks, vs, log2 |vs| of four blocks
 constexpr int kUnitSlots = 4;              // stretches of units that are known ahead
 
 // Operands lie in groups of eight rows, [H / 64][8 rows][64 columns] (K, V), or as [H / 64][128 rows][64 columns] (Q); rows of
@@ -304,13 +304,10 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           }
           if (warp == 8) {
             float* to = scales + (tiles_issued % kScaleSlots) * kScaleWords;
-            float lv = __log2f(fabsf(vs));
-            lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 1));
-            lv = fmaxf(lv, __shfl_xor_sync(0xffffffffu, lv, 2));
             if (lane >> 2 == ahead) {
               to[lane & 3] = ks;
               to[4 + (lane & 3)] = vs;
-              if ((lane & 3) == 0) to[8] = lv;
+              to[8 + (lane & 3)] = __log2f(fabsf(vs));
             }
           }
           ++tiles_issued;
@@ -514,8 +511,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
         const uint32_t tmem_b = tmem_s + b * 64;
         if (active) {
           float4 ks = *reinterpret_cast<const float4*>(scales + slot * kScaleWords);
-          const float4 vs = *reinterpret_cast<const float4*>(scales + slot * kScaleWords + 4);
-          const float lv = scales[slot * kScaleWords + 8];
+          float4 vs = *reinterpret_cast<const float4*>(scales + slot * kScaleWords + 4);
+          const float4 lv = *reinterpret_cast<const float4*>(scales + slot * kScaleWords + 8);
           float v[kKeys];
           tmem_ld32_nowait(tmem_b, v);
           tmem_ld32_nowait(tmem_b + 32, v + 32);
@@ -533,8 +530,13 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
               v[i] = ((i < 32 ? see0 : see1) >> (i & 31)) & 1u ? v[i] * f : -INFINITY;
             }
             ks = make_float4(1.f, 1.f, 1.f, 1.f);
+            // a scale that is no number reaches the rows that see something of its block, not the others
+            if (!(see0 & 0xffffu)) vs.x = 0.f;
+            if (!(see0 >> 16)) vs.y = 0.f;
+            if (!(see1 & 0xffffu)) vs.z = 0.f;
+            if (!(see1 >> 16)) vs.w = 0.f;
           }
-          float mx = -INFINITY;
+          float mx = -INFINITY, mx_u = -INFINITY;      // of the scores, of those plus log2 |vs|
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const float f = q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w;
@@ -546,17 +548,19 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
 #pragma unroll
               for (int i = 1; i < 16; ++i) top = fminf(top, v[q * 16 + i]);
             }
-            mx = fmaxf(mx, top * f);
+            top *= f;
+            mx = fmaxf(mx, top);
+            mx_u = fmaxf(mx_u, top + (q == 0 ? lv.x : q == 1 ? lv.y : q == 2 ? lv.z : lv.w));
           }
           const bool raise = mx > m + kRaiseBy || (m == -INFINITY && mx > -INFINITY);
-          const bool raise_u = mx + lv > top_u + kRaiseBy || (top_u == -INFINITY && mx + lv > -INFINITY);
+          const bool raise_u = mx_u > top_u + kRaiseBy || (top_u == -INFINITY && mx_u > -INFINITY);
           if (__any_sync(0xffffffffu, raise || raise_u)) {
             if (raise) {
               l *= exp2_approx(m - mx);     // 0 where nothing had been seen before
               m = mx;
             }
-            const float f = raise_u ? exp2_approx(top_u - (mx + lv)) : 1.f;
-            if (raise_u) top_u = mx + lv;
+            const float f = raise_u ? exp2_approx(top_u - mx_u) : 1.f;
+            if (raise_u) top_u = mx_u;
             // The output of the group's tile before may be under way; of the one before that it is complete, since these scores came
             // after it.
             if (t != t_first && ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(B_PVDONE + s), (n_pv - 1) & 1, stop));
@@ -755,8 +759,13 @@ int launch_h(const PagedCache& c, const CacheScales& sc, const PagedRows& r, cha
 int launch_scaled_tc(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s) {
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
+  // 256 rows a unit turn every tile into fp16 once for both halves, and pay where there are enough units and tiles to keep all SMs
+  // at it (head_dim 128, 8 KV heads; units of 128 against 256 rows, us): 132 rows, 64 x 300 keys 119, 91, 16 x 1000 63, 56,
+  // 8 x 8192 130, 110; 256 rows, 64 x 300 111, 112, 16 x 1000 69, 71, 64 x 1000 176, 169, 8 x 8192 137, 121.  With few tiles, or
+  // 128 rows, they lose: 132 rows, 8 x 1000 40, 40, 1 x 1000 22, 27; 256 rows, 8 x 1000 45, 50, 1 x 4096 34, 39; 64 rows,
+  // 8 x 8192 76, 108.
   const int64_t rows = static_cast<int64_t>(r.T) * r.group / c.n_reqs, keys = static_cast<int64_t>(c.table_cols) * c.ps;
-  const bool wide = rows > kGroupRows && (rows + kGroupRows - 1) / (2 * kGroupRows) * c.n_reqs * c.Hkv * ((keys + kKeys - 1) / kKeys) >= 32LL * sms;
+  const bool wide = rows > kGroupRows && (rows + kGroupRows - 1) / (2 * kGroupRows) * c.n_reqs * c.Hkv * ((keys + kKeys - 1) / kKeys) >= 12LL * sms;
   if (c.h == 128) return wide ? launch_h<128, 2>(c, sc, r, ws, s) : launch_h<128, 1>(c, sc, r, ws, s);
   return wide ? launch_h<64, 2>(c, sc, r, ws, s) : launch_h<64, 1>(c, sc, r, ws, s);
 }

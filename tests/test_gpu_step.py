@@ -230,8 +230,6 @@ def test_the_gradient_of_rotary(style):
         lhs, rhs = (y.double() * (call(x + d).double() - call(x).double())).sum((1, 2)), (grad * d.double()).sum((1, 2))
         size = a * 2 * (y.double().abs().amax() * (x.double().abs() + d.double().abs()).sum((1, 2)) * 2)
         assert bool(((lhs - rhs).abs() <= size * 2.0 ** -20).all())
-    if a == 1.0:
-        assert False
     back = call(call(x), True).double() / a ** 2        # turned back, but for the amplitude; dimensions behind 48 are copied
     assert float((back - x.double())[..., :48].abs().max()) <= 4 * float(x.abs().max()) * 2.0 ** -20
 
@@ -566,6 +564,18 @@ def test_scaled_scales_of_zero_and_below(wide):
     assert bool((out == 0).all())
 
 
+@pytest.mark.parametrize("h", [32, 64, 128])
+@pytest.mark.parametrize("hq", [2, 12, 40, 200])
+def test_scaled_values_of_nothing_under_the_largest_scores(hq, h):
+    """What is left of a result when its largest probabilities meet values of 0, in a block beside the others."""
+    lens, q_len = [200, 90, 40], [4, 1, 7]
+    cache = list(_coded_cache(lens, 2, h, 16, 12, whole=True, spread=2.0))
+    cache[3] = torch.where(cache[1] > cache[1].nan_to_num(0).quantile(0.7), 0.0, cache[3])
+    _scaled_check(lens, q_len, hq, 2, h, cache=cache)
+    cache[3] = cache[3] * 2.0 ** -100
+    _scaled_check(lens, q_len, hq, 2, h, cache=cache)
+
+
 @pytest.mark.parametrize("wide", [1, 12])
 @pytest.mark.parametrize("size", [2.0 ** -60, 2.0 ** -14, 1e-3, 300.0, 2.0 ** 60])
 def test_scaled_queries_of_any_size(size, wide):
@@ -630,6 +640,116 @@ def test_scaled_rows_of_nobody_are_left_alone_and_wrong_requests_left_out():
     assert st.item() == B.SLED_ERR_ARG      # a parent that is no earlier node
 
 
+# Units of up to 256 rows are for batches of many tiles; how many there may be is what the table has columns for.
+def _many_columns(cache):
+    kc, ks, vc, vs, table, n_kv = cache
+    wide = torch.full((table.shape[0], 4096), -9, dtype=table.dtype)
+    wide[:, :table.shape[1]] = table
+    return kc, ks, vc, vs, wide, n_kv
+
+
+@pytest.mark.parametrize("h", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(64, 2), (40, 1), (48, 3)])
+def test_scaled_units_of_256_rows(hq, hkv, h):
+    rng = random.Random(h + hq)
+    lens = [64, 1, 17, 300, 0, 1025, 129, 700]
+    q_len = [13, 1, 17, 30, 0, 8, 9, 7]
+    cache = _many_columns(_coded_cache(lens, hkv, h, 16, h))
+    _scaled_check(lens, q_len, hq, hkv, h, cache=cache, parents=[_tree(rng, m, roots=True) if m else [] for m in q_len])
+    _scaled_check(lens, q_len, hq, hkv, h, cache=cache)
+    parents = [[-2] + [-1] * (m - 1) if m else [] for m in q_len]            # the first row of every request sees nothing
+    out, lse = _scaled_check(lens, q_len, hq, hkv, h, cache=cache, parents=parents)
+    at = [sum(q_len[:i]) for i, m in enumerate(q_len) if m]
+    assert bool((out[at] == 0).all()) and bool((lse[at] == -math.inf).all())
+
+
+@pytest.mark.parametrize("h", [64, 128])
+def test_scaled_prompts_in_units_of_256_rows(h):
+    lens, q_len = [500, 333, 70, 128], [300, 333, 1, 128]
+    _scaled_check(lens, q_len, 8, 2, h, cache=_many_columns(_coded_cache(lens, 2, h, 16, h)))
+
+
+@pytest.mark.parametrize("columns", [lambda c: c, _many_columns])
+@pytest.mark.parametrize("h", [64, 128])
+def test_scaled_codes_that_are_no_numbers_in_large_units(h, columns):
+    """Keys and values of a node that others do not see, under units of 128 and of 256 rows; scales of zero, below and far apart."""
+    lens, q_len, parents, hq = [150, 70], [20, 9], [[-1] + [0] * 19, [-1] + [0] * 8], 64
+    cache = list(columns(_coded_cache(lens, 2, h, 16, 3, whole=True, spread=3.0)))
+    cache[3][1::3] *= -1
+    cache[3][::5] *= 0
+    for i, (n, m) in enumerate(zip(lens, q_len)):
+        for c in (cache[0], cache[2]):
+            c.view(torch.uint8)[cache[4][i, (n - 2) // 16], :, (n - 2) % 16] = 0xff          # node m - 2
+    kc, ks, vc, vs, table, n_kv = cache
+    q = torch.randn(29, hq, h, generator=torch.Generator().manual_seed(1)).to(BF)
+    lse = torch.empty(29, hq, device="cuda")
+    out = B.attention_tree(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), n_kv.cuda(), _cu(q_len), _i32(sum(parents, [])), lse=lse, k_scale=ks.cuda(),
+                           v_scale=vs.cuda()).cpu().double()
+    clean = [c.double().nan_to_num(0).float().to(E4M3) for c in (kc, vc)]
+    at = 0
+    for i, m in enumerate(q_len):
+        kk, vv = (R.keys_of(S.values(c, s), table[i], lens[i], 16) for c, s in zip(clean, (ks, vs)))
+        o, l, _, d_o, d_l, _ = R.attend(q[at:at + m], kk, vv, R.tree_mask(parents[i], m, lens[i]), h ** -0.5, BF)
+        for j in range(m):
+            if j == m - 2:
+                assert bool(out[at + j].isnan().all()) and bool(lse[at + j].isnan().all())
+                continue
+            assert bool(((out[at + j] - o[j]).abs() <= d_o[j]).all()) and bool(((lse[at + j].cpu().double() - l[j]).abs() <= d_l[j]).all())
+        at += m
+
+
+@pytest.mark.parametrize("columns", [lambda c: c, _many_columns])
+def test_scaled_rows_of_nobody_in_large_units(columns):
+    lens, q_len, hq = [100, 50, 60], [12, 9, 10], 64
+    kc, ks, vc, vs, table, n_kv = (x.cuda() for x in columns(_coded_cache(lens, 2, 128, 16, 0)))
+    q = torch.randn(40, hq, 128, generator=torch.Generator().manual_seed(1)).to(BF).cuda()
+    cu = _i32([2, 14, 23, 33])
+    def call(table, n_kv):
+        out, lse, st = torch.full((40, hq, 128), 5.0, dtype=BF, device="cuda"), torch.full((40, hq), 5.0, device="cuda"), _status()
+        B.attention_tree(q, kc, vc, table, n_kv, cu, k_scale=ks, v_scale=vs, out=out, lse=lse, status=st)
+        return out, lse, st.item()
+    out, lse, st = call(table, n_kv)
+    assert st == 0
+    nobody = [0, 1] + list(range(33, 40))
+    assert bool((out[nobody] == 5).all()) and bool((lse[nobody] == 5).all()) and not bool((lse[2:33] == 5).any())
+    o, l, st = call(table, _i32([100, 8, 60]))            # fewer keys than rows
+    assert st == B.SLED_ERR_ARG and bool((l[14:23] == 5).all())
+    assert torch.equal(o[2:14], out[2:14]) and torch.equal(o[23:33], out[23:33])
+    wrong = table.clone()
+    wrong[1, 0] = kc.shape[0]
+    o, l, st = call(wrong, n_kv)
+    assert st == B.SLED_ERR_ARG and torch.equal(o[2:14], out[2:14]) and torch.equal(o[23:33], out[23:33])
+
+
+@pytest.mark.parametrize("hq,hkv,h,rows,columns", [(32, 8, 128, 1, 0), (6, 2, 32, 2, 0), (8, 2, 64, 4, 0), (32, 8, 128, 7, 0), (16, 2, 32, 30, 0), (32, 8, 128, 30, 0),
+                                                   (64, 2, 64, 12, 4096)])
+def test_scaled_results_do_not_depend_on_where_pages_lie(hq, hkv, h, rows, columns):
+    """Bit for bit, several times: pages in order and scattered arrive at different times."""
+    rng = random.Random(h + rows)
+    lens = [rng.randint(30000, 60000), 5, rng.randint(1, 9000), rng.randint(1, 9000), 64, rng.randint(30000, 60000)]
+    q_len = [min(n, rng.randint(max(1, rows // 2), rows)) for n in lens]
+    pages = [S.up(n, 16) for n in lens]
+    n_pages = sum(pages)
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    codes = [torch.randint(0, 126, (n_pages, hkv, 16, h), dtype=torch.uint8, device="cuda", generator=g) for _ in range(2)]
+    scales = [torch.rand(n_pages, hkv, 1, device="cuda", generator=g) * x for x in (2e-4, 1.0)]
+    q = torch.randn(sum(q_len), hq, h, device="cuda", generator=g).to(BF)
+    want = None
+    for order in [torch.arange(n_pages, device="cuda")] + [torch.randperm(n_pages, device="cuda", generator=g) for _ in range(3)]:
+        table, at = torch.zeros(len(lens), columns or max(pages), dtype=torch.int32, device="cuda"), 0
+        for i, p in enumerate(pages):
+            table[i, :p] = order[at:at + p]
+            at += p
+        to = torch.empty_like(order)
+        to[order] = torch.arange(n_pages, device="cuda")
+        c, s, status = [x[to].view(E4M3) for x in codes], [x[to] for x in scales], _status()
+        for _ in range(3):
+            out = B.attention_tree(q, *c, table, _i32(lens), _cu(q_len), k_scale=s[0], v_scale=s[1], status=status)
+            want = out if want is None else want
+            assert torch.equal(out, want)
+        B.check_status(status)
+
+
 def test_scaled_empty_batches():
     q = torch.zeros(0, 8, 64, dtype=BF, device="cuda")
     c, s = torch.zeros(3, 2, 16, 64, device="cuda").to(E4M3), torch.ones(3, 2, 1, device="cuda")
@@ -681,6 +801,31 @@ def test_scaled_captured_and_side_by_side():
     for st, c, w in zip(streams, calls, want):
         with torch.cuda.stream(st):
             assert torch.equal(c(), w)
+
+
+@pytest.mark.parametrize("dtype", [E4M3, BF])
+def test_caches_of_more_than_four_gigabytes(dtype):
+    """Keys written to, and read from, the last pages of a cache whose offsets pass 32 bits, against the same ones in a small cache."""
+    hkv, h, page, lens = 8, 128, 16, [50, 3]
+    n_pages = (2 ** 32 + 2 ** 26) // (hkv * page * h)                    # elements
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn(sum(lens), hkv, h, generator=g).to(BF).cuda() for _ in range(2))
+    q = torch.randn(40 + 3, 32, h, generator=g).to(BF).cuda()
+    outs = []
+    for n, first in ((8, 0), (n_pages, n_pages - 8)):
+        kc, vc = (torch.empty(n, hkv, page, h, dtype=dtype, device="cuda") for _ in range(2))
+        scales = dict(k_scale=torch.ones(n, hkv, 1, device="cuda"), v_scale=torch.ones(n, hkv, 1, device="cuda")) if dtype == E4M3 else {}
+        table = first + _i32([[7, 0, 3, 1], [5, -1, -1, -1]])
+        B.append_keys(k, v, kc, vc, table, _i32(lens), _cu(lens), **scales)
+        one = [] if dtype is BF else [B.attention_tree(q[:2], kc, vc, table, _i32(lens), _cu([1, 1]), **scales), B.attention_tree(q, kc, vc, table, _i32(lens), _cu([40, 3]), **scales)]
+        outs.append(one + [x[table[0].long()].view(torch.uint8) for x in (kc, vc)] + [s[table[0].long()] for s in scales.values()])
+        del kc, vc
+    filled = [slice(0, 3), (slice(3, 4), slice(None), slice(0, 2))]      # slots without keys hold anything
+    for a, b in zip(*outs):
+        if a.dtype == torch.uint8:
+            assert all(torch.equal(a[f], b[f]) for f in filled)
+        else:
+            assert torch.equal(a, b)
 
 
 # ------------------------------------------------------------------------------------------------- the whole step
