@@ -472,7 +472,8 @@ int sled_rotary(const sled_heads* q, const sled_heads* k, int32_t n_rows, int32_
  * the block has older keys of the request, the scale that it had, if that is larger; then the older keys are coded anew.  A code is
  * the nearest to element / scale, ties to the even one; infinities and NaN become NaN.  What a rejected draft did to a
  * scale stays until its block is begun anew.
- * Slots behind the last key and other pages are left as they are.  A request whose numbers do not hold together is left out, a
+ * Slots behind the last key and other pages are left as they are; the rows lie outside of the cache, and no two requests of a
+ * call write into one page.  A request whose numbers do not hold together is left out, a
  * page outside the pool is not written; *status says so. */
 #define SLED_SCALE_BLOCK 16
 int sled_append_keys(const sled_paged_kv* kv, float* k_scale, float* v_scale, const void* k, int64_t k_stride, const void* v,
@@ -480,8 +481,8 @@ int sled_append_keys(const sled_paged_kv* kv, float* k_scale, float* v_scale, co
 
 /* sled_attention_tree over a cache in 8 bits (kv->dtype SLED_E4M3, with its scales as in sled_append_keys: any finite
  * numbers).  q and out are bf16; parents, lse, status and workspace as there.  Scores, their maxima and sums are held in fp32;
- * the softmax's numerators, times their block's scale, are rounded to 16 bits before they meet V (their sum is not), one
- * rounding of at most 2^-8 of each. */
+ * the softmax's numerators, times their block's scale, are rounded to fp16 before they meet V (their sum is not): by 2^-11 of
+ * each at most, or by 2^-32 of the row's largest where that is more. */
 int sled_attention_scaled_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int64_t* bytes);
 int sled_attention_scaled(const sled_paged_kv* kv, const float* k_scale, const float* v_scale, const void* q, int64_t q_stride,
                           const int32_t* cu_q, const int32_t* parents, int32_t n_rows, int32_t n_q_heads, float scale, void* out,

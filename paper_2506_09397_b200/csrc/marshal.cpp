@@ -6,6 +6,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
@@ -218,11 +219,13 @@ PyObject* rotary(PyObject* const* a) {
   }
   const double amplitude = PyFloat_AsDouble(a[5]);
   if (amplitude == -1.0 && PyErr_Occurred()) throw Refused{1, ""};
+  const int transpose = PyObject_IsTrue(a[6]);
+  if (transpose < 0) throw Refused{1, ""};
   const int64_t rows = q.size(0), half = tensor(a[3], "frequencies").numel();
   if (half > 256) refuse(what, "head_dim is at most 512");
   check(sled_rotary(&qh, given(a[1]) ? &kh : nullptr, static_cast<int32_t>(rows), static_cast<int32_t>(q.size(2)), type,
                     vector_of<int32_t>(a[2], what, "positions", dev, rows, at::kInt), vector_of<double>(a[3], what, "frequencies", dev, half, at::kDouble),
-                    static_cast<int32_t>(2 * half), pairs, static_cast<float>(amplitude), PyObject_IsTrue(a[6]), stream_of(dev)), what);
+                    static_cast<int32_t>(2 * half), pairs, static_cast<float>(amplitude), transpose, stream_of(dev)), what);
   PyObject* q_out = given(a[7]) ? Py_NewRef(a[7]) : THPVariable_Wrap(q_made);
   PyObject* k_out = !given(a[1]) ? Py_NewRef(Py_None) : given(a[8]) ? Py_NewRef(a[8]) : THPVariable_Wrap(k_made);
   PyObject* both = PyTuple_Pack(2, q_out, k_out);
@@ -291,8 +294,8 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }                        // otherwise Python has an error of its own
   } catch (const NotATensor& t) {
     PyErr_Format(PyExc_TypeError, "%s must be a tensor", t.name.c_str());
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {            // torch's own: no memory left, among others
+    torch::translate_exception_to_python(std::current_exception());
   }
   return nullptr;
 }
