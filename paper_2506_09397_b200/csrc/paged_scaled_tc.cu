@@ -130,6 +130,13 @@ __device__ __forceinline__ bool all_of_256(bool x) {
   return y != 0;
 }
 
+// of sixteen, three at a time
+__device__ __forceinline__ float largest16(const float* v) {
+  const auto of3 = [](float x, float y, float z) { return fmaxf(fmaxf(x, y), z); };
+  const float a = of3(of3(v[0], v[1], v[2]), of3(v[3], v[4], v[5]), of3(v[6], v[7], v[8]));
+  return fmaxf(a, of3(of3(v[9], v[10], v[11]), of3(v[12], v[13], v[14]), v[15]));
+}
+
 template <int H, int kGroups>
 __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, const CacheScales sc, const PagedRows r, const ScaledParts parts,
                                                            bool whole_q, bool whole_out) {
@@ -537,20 +544,28 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
             if (!(see1 >> 16)) vs.w = 0.f;
           }
           float mx = -INFINITY, mx_u = -INFINITY;      // of the scores, of those plus log2 |vs|
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float f = q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w;
-            float top = v[q * 16];
-            if (f >= 0.f) {      // (the same for all rows: a row's own factor is positive)
-#pragma unroll
-              for (int i = 1; i < 16; ++i) top = fmaxf(top, v[q * 16 + i]);
-            } else {
-#pragma unroll
-              for (int i = 1; i < 16; ++i) top = fminf(top, v[q * 16 + i]);
-            }
-            top *= f;
+          const auto of_block = [&](int q, float top) {
+            top *= q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w;
             mx = fmaxf(mx, top);
             mx_u = fmaxf(mx_u, top + (q == 0 ? lv.x : q == 1 ? lv.y : q == 2 ? lv.z : lv.w));
+          };
+          if (fminf(fminf(ks.x, ks.y), fminf(ks.z, ks.w)) >= 0.f) {      // (the same for all rows: a row's own factor is positive)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) of_block(q, largest16(v + q * 16));
+          } else {
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              float most = -INFINITY, least = INFINITY;
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                if (k == q)
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) {
+                    most = fmaxf(most, v[k * 16 + i]);
+                    least = fminf(least, v[k * 16 + i]);
+                  }
+              of_block(q, (q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w) >= 0.f ? most : least);
+            }
           }
           const bool raise = mx > m + kRaiseBy || (m == -INFINITY && mx > -INFINITY);
           const bool raise_u = mx_u > top_u + kRaiseBy || (top_u == -INFINITY && mx_u > -INFINITY);

@@ -147,9 +147,12 @@ __global__ void __launch_bounds__(kThreads) page_slots_kernel(const SlotsCall a,
   };
   for (int64_t k = first_row; k < n_back; k += step) a.free_pages[n_free + k] = returned(static_cast<int>(k));
 
+  // a block's rows are neighbours: a thread's next row is mostly of the same request
   int begin = 0, end = 0, req = 0, taken = 0;      // the request of the last row, and its rows
   SlotsReq r{};
-  for (int64_t row = first_row; row < a.n_rows; row += step) {
+  const int64_t each = (a.n_rows + static_cast<int64_t>(gridDim.x) * kThreads - 1) / (static_cast<int64_t>(gridDim.x) * kThreads) * kThreads;
+  const int64_t last = min((blockIdx.x + 1) * each, static_cast<int64_t>(a.n_rows));
+  for (int64_t row = blockIdx.x * each + threadIdx.x; row < last; row += kThreads) {
     const int t = static_cast<int>(row);
     if (t >= n_rows) {
       if (a.positions) a.positions[t] = 0;
