@@ -520,56 +520,62 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           float4 ks = *reinterpret_cast<const float4*>(scales + slot * kScaleWords);
           float4 vs = *reinterpret_cast<const float4*>(scales + slot * kScaleWords + 4);
           const float4 lv = *reinterpret_cast<const float4*>(scales + slot * kScaleWords + 8);
-          float v[kKeys];
-          tmem_ld32_nowait(tmem_b, v);
-          tmem_ld32_nowait(tmem_b + 32, v + 32);
-          tmem_ld_wait<kKeys>(v);
           ks.x *= factor;
           ks.y *= factor;
           ks.z *= factor;
           ks.w *= factor;
-          // Scores of tiles that some row does not see all of are scaled and masked first.
-          if (masked) {
-            const uint32_t see0 = view.seen(x0, prefix, end), see1 = view.seen(x0 + 32, prefix, end);
-#pragma unroll
-            for (int i = 0; i < kKeys; ++i) {
-              const float f = i < 16 ? ks.x : i < 32 ? ks.y : i < 48 ? ks.z : ks.w;
-              v[i] = ((i < 32 ? see0 : see1) >> (i & 31)) & 1u ? v[i] * f : -INFINITY;
-            }
-            ks = make_float4(1.f, 1.f, 1.f, 1.f);
-            // a scale that is no number reaches the rows that see something of its block, not the others
-            if (!(see0 & 0xffffu)) vs.x = 0.f;
-            if (!(see0 >> 16)) vs.y = 0.f;
-            if (!(see1 & 0xffffu)) vs.z = 0.f;
-            if (!(see1 >> 16)) vs.w = 0.f;
-          }
-          float mx = -INFINITY, mx_u = -INFINITY;      // of the scores, of those plus log2 |vs|
-          const auto of_block = [&](int q, float top) {
-            top *= q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w;
-            mx = fmaxf(mx, top);
-            mx_u = fmaxf(mx_u, top + (q == 0 ? lv.x : q == 1 ? lv.y : q == 2 ? lv.z : lv.w));
-          };
-          if (fminf(fminf(ks.x, ks.y), fminf(ks.z, ks.w)) >= 0.f) {      // (the same for all rows: a row's own factor is positive)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) of_block(q, largest16(v + q * 16));
-          } else {
+          const bool below = fminf(fminf(ks.x, ks.y), fminf(ks.z, ks.w)) < 0.f;      // (the same for all rows: a row's own factor is positive)
+          // Exponentials by the references that there are, and the largest scores beside them; where those call for other references -
+          // in a unit's first tiles - once more.
+          uint32_t p[kKeys / 2];
+          float sum0, sum1;
 #pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-              float most = -INFINITY, least = INFINITY;
+          for (int pass = 0;; ++pass) {
+            float v[kKeys];
+            tmem_ld32_nowait(tmem_b, v);
+            tmem_ld32_nowait(tmem_b + 32, v + 32);
+            tmem_ld_wait<kKeys>(v);
+            float4 by = ks;
+            // Scores of tiles that some row does not see all of are scaled and masked first; so are those of scales below 0.
+            if (masked || below) {
+              const uint32_t see0 = view.seen(x0, prefix, end), see1 = view.seen(x0 + 32, prefix, end);
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (k == q)
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) {
-                    most = fmaxf(most, v[k * 16 + i]);
-                    least = fminf(least, v[k * 16 + i]);
-                  }
-              of_block(q, (q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w) >= 0.f ? most : least);
+              for (int i = 0; i < kKeys; ++i) {
+                const float f = i < 16 ? ks.x : i < 32 ? ks.y : i < 48 ? ks.z : ks.w;
+                v[i] = ((i < 32 ? see0 : see1) >> (i & 31)) & 1u ? v[i] * f : -INFINITY;
+              }
+              by = make_float4(1.f, 1.f, 1.f, 1.f);
+              // a scale that is no number reaches the rows that see something of its block, not the others
+              if (!(see0 & 0xffffu)) vs.x = 0.f;
+              if (!(see0 >> 16)) vs.y = 0.f;
+              if (!(see1 & 0xffffu)) vs.z = 0.f;
+              if (!(see1 >> 16)) vs.w = 0.f;
             }
-          }
-          const bool raise = mx > m + kRaiseBy || (m == -INFINITY && mx > -INFINITY);
-          const bool raise_u = mx_u > top_u + kRaiseBy || (top_u == -INFINITY && mx_u > -INFINITY);
-          if (__any_sync(0xffffffffu, raise || raise_u)) {
+            const float ref = m == -INFINITY ? 0.f : m;
+            const float weight = top_u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - top_u, 110.f));
+            float mx = -INFINITY, mx_u = -INFINITY;      // of the scores, of those plus log2 |vs|
+            sum0 = sum1 = 0.f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float f = q == 0 ? by.x : q == 1 ? by.y : q == 2 ? by.z : by.w;
+              const float wb = top_u == -INFINITY ? 0.f : weight * (q == 0 ? vs.x : q == 1 ? vs.y : q == 2 ? vs.z : vs.w);
+              const float top = largest16(v + q * 16) * f;
+              mx = fmaxf(mx, top);
+              mx_u = fmaxf(mx_u, top + (q == 0 ? lv.x : q == 1 ? lv.y : q == 2 ? lv.z : lv.w));
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float a = v[q * 16 + 2 * i], y = v[q * 16 + 2 * i + 1];
+                fma2(a, y, f, -ref);
+                a = exp2_approx(a);
+                y = exp2_approx(y);
+                add2(sum0, sum1, a, y);
+                mul2(a, y, wb);
+                p[q * 8 + i] = pack_half(a, y);
+              }
+            }
+            const bool raise = mx > m + kRaiseBy || (m == -INFINITY && mx > -INFINITY);
+            const bool raise_u = mx_u > top_u + kRaiseBy || (top_u == -INFINITY && mx_u > -INFINITY);
+            if (pass == 1 || !__any_sync(0xffffffffu, raise || raise_u)) break;
             if (raise) {
               l *= exp2_approx(m - mx);     // 0 where nothing had been seen before
               m = mx;
@@ -594,30 +600,8 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
               tmem_st_wait();
             }
           }
-          const float ref = m == -INFINITY ? 0.f : m;
-          const float weight = top_u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - top_u, 110.f));
-          float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t p[16];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int q = 2 * h + e;
-              const float f = q == 0 ? ks.x : q == 1 ? ks.y : q == 2 ? ks.z : ks.w;
-              const float wb = top_u == -INFINITY ? 0.f : weight * (q == 0 ? vs.x : q == 1 ? vs.y : q == 2 ? vs.z : vs.w);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                float a = v[q * 16 + 2 * i], y = v[q * 16 + 2 * i + 1];
-                fma2(a, y, f, -ref);
-                a = exp2_approx(a);
-                y = exp2_approx(y);
-                add2(sum0, sum1, a, y);
-                mul2(a, y, wb);
-                p[e * 8 + i] = pack_half(a, y);
-              }
-            }
-            tmem_st16(tmem_b + h * 16, p);     // P lies over the scores
-          }
+          tmem_st16(tmem_b, p);     // P lies over the scores
+          tmem_st16(tmem_b + 16, p + 16);
           l += sum0 + sum1;
           tmem_st_wait();
         }
