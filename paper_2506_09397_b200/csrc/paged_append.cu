@@ -7,7 +7,8 @@
 //
 // A warp does one (block, KV head) of K or of V: it holds all of the block's new rows in registers, so that they are read
 // once, and a lane writes the 8 codes of the 8 elements that it read.  Bound by its bytes for prompts, by latency (row offsets,
-// lengths, table, then rows and scale together) for decoding steps.
+// lengths, table, then rows and scale together) for decoding steps: 12 prompts of 2000 .. 16384 tokens, 8 KV heads of 128, in 8 bits 110 us (87 %
+// of the copy rate), 48 requests with 1 .. 9 tokens 5.9 us, 20 chunks of 200 .. 2000 tokens as they are, heads of 64, 12 us.
 #include <cuda_fp8.h>
 
 #include <cuda_fp16.h>
@@ -20,7 +21,7 @@ namespace sled {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMany = 32;            // rows of a block's span for long calls
+constexpr int kSome = 8, kMany = 32;            // rows of a block's span for longer calls
 
 // eight elements, as they lie in memory
 template <typename T>
@@ -276,13 +277,21 @@ int launch(const PagedCache& c, const NewRows& a, cudaStream_t s) {
   const bool whole = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & 15) == 0 && a.k_stride % kRow == 0 && a.v_stride % kRow == 0;
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
-  // A block per row (most of them then find that another row begins their cache block) while that fills the GPU a few times;
-  // a block per 32 rows beyond
-  // (16, 32, 64 rows: 12 prompts of 2000 .. 16384 tokens in 8 bits 151, 141.5, 141 us, 20 chunks of 200 .. 2000 as they are 13.9, 14.3, 18.5).
-  if (a.T <= 16 * sms)
-    SLED_LAUNCH_PDL((append_kernel<T, H, kCodes, 1>), dim3(a.T), dim3(kThreads), 0, s, c, a, whole);
-  else
-    SLED_LAUNCH_PDL((append_kernel<T, H, kCodes, kMany>), dim3((a.T + kMany - 1LL) / kMany), dim3(kThreads), 0, s, c, a, whole);
+  const auto by = [&](auto kernel, int span) {
+    SLED_LAUNCH_PDL(kernel, dim3(static_cast<unsigned>((static_cast<int64_t>(a.T) + span - 1) / span)), dim3(kThreads), 0, s, c, a, whole);
+  };
+  // A block per row where there are few rows, or few to a request (a cache block or more then begins with nearly every row); else
+  // one per 8 rows, or 32 where those still fill the GPU.  8 bits, 8 heads of 128, requests x rows, us for 1, 8, 32 rows a block:
+  // 1 x 7 4.7, 7.4, 7.4, 48 x 5 5.7, 8.8, 24, 300 x 2 9.1, 13.5, 43; 64 x 8 6.8, 6.2, 16, 300 x 4 11.3, 9.0, 26, 40 x 100 18.4, 10.4,
+  // 11.6, 3000 x 4 94, 60, 65; 16 x 500 28, 16.2, 15.5, 4 x 2000 28, 13.2, 12.7 (16 and 64 rows for 12 prompts of 2000 .. 16384: 112
+  // and 109.5 against 109.6; for 20 chunks of 200 .. 2000 as they are 12.1 and 14.3 against 12.0).
+  if (a.T <= 3LL * sms || a.T < 4LL * c.n_reqs) {
+    by(append_kernel<T, H, kCodes, 1>, 1);
+  } else if (a.T < 40LL * sms || a.T < 16LL * c.n_reqs) {
+    by(append_kernel<T, H, kCodes, kSome>, kSome);
+  } else {
+    by(append_kernel<T, H, kCodes, kMany>, kMany);
+  }
   return cudaGetLastError() == cudaSuccess ? 1 : -1;
 }
 

@@ -12,7 +12,14 @@
 // bring the queries too, as fp16 times a power of two per row.  A score meets its block's scale ks where it leaves tensor memory, a
 // numerator its vs before it is rounded.  The references of a row - m of the scores, u of the numerators - are raised only when
 // something exceeds them by more than 2^8; raising u means rescaling the row of O in tensor memory, which happens in a unit's
-// first tiles.
+// first tiles.  So a tile's exponentials are formed by the references that there are, beside the search for its largest scores, and
+// once more where those call for others.
+//
+// 64 trees of 48 - 64 nodes over 512 - 4096 keys, 8 KV heads of 128 for 32: 229 us; 512 rows over four contexts of 32768 keys 320 us
+// (860 TFLOP/s), 128 rows 122 us.  A 64-key tile of 256 rows takes about 2400 cycles: 1900 of them are a softmax warp's own (load of
+// the scores 180, exponentials and maxima, vote, store and arrival 270, in one chain, two such warps on a scheduler), products
+// and their waits 1500 beside them, conversion 1150.  A unit costs about 17,000 cycles more (Q, first scores, last output, results
+// to memory), which is what short contexts pay.
 //   warps 0-3, 4-7 : softmax and output of the two groups
 //   warps 8-11     : K, V and Q to fp16, scales
 //   warps 12, 13   : products of either group (one thread each: a product takes about 70 cycles to issue), tensor-memory allocation
@@ -759,10 +766,10 @@ int launch_scaled_tc(const PagedCache& c, const CacheScales& sc, const PagedRows
   int sms = 0;
   if (paged_device(&sms) < 0) return -1;
   // 256 rows a unit turn every tile into fp16 once for both halves, and pay where there are enough units and tiles to keep all SMs
-  // at it (head_dim 128, 8 KV heads; units of 128 against 256 rows, us): 132 rows, 64 x 300 keys 119, 91, 16 x 1000 63, 56,
-  // 8 x 8192 130, 110; 256 rows, 64 x 300 111, 112, 16 x 1000 69, 71, 64 x 1000 176, 169, 8 x 8192 137, 121.  With few tiles, or
-  // 128 rows, they lose: 132 rows, 8 x 1000 40, 40, 1 x 1000 22, 27; 256 rows, 8 x 1000 45, 50, 1 x 4096 34, 39; 64 rows,
-  // 8 x 8192 76, 108.
+  // at it (head_dim 128, 8 KV heads; units of 128 against 256 rows, us): 132 rows, 64 x 300 keys 111, 88, 16 x 1000 60, 55,
+  // 8 x 8192 129, 105; 256 rows, 64 x 300 105, 110, 16 x 1000 67, 69, 64 x 1000 169, 165, 8 x 8192 134, 115.  With few tiles, or
+  // up to 128 rows, they lose: 132 rows, 8 x 1000 40, 40, 1 x 1000 22, 28; 256 rows, 8 x 1000 45, 50, 1 x 4096 34, 39; 64 rows,
+  // 8 x 8192 74, 107.
   const int64_t rows = static_cast<int64_t>(r.T) * r.group / c.n_reqs, keys = static_cast<int64_t>(c.table_cols) * c.ps;
   const bool wide = rows > kGroupRows && (rows + kGroupRows - 1) / (2 * kGroupRows) * c.n_reqs * c.Hkv * ((keys + kKeys - 1) / kKeys) >= 12LL * sms;
   if (c.h == 128) return wide ? launch_h<128, 2>(c, sc, r, ws, s) : launch_h<128, 1>(c, sc, r, ws, s);

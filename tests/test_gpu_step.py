@@ -309,6 +309,31 @@ def test_append_prompts_in_8_bits(dtype):
     _append_check([3] * 40, [70] * 40, 1, 64, 16, dtype)
 
 
+@pytest.mark.parametrize("h", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_append_long_prompts_in_8_bits(dtype, h):
+    _append_check([0, 333, 0, 7, 50], [3100, 500, 1, 2900, 700], 1, h, 16, dtype, seed=h)
+
+
+@pytest.mark.parametrize("new", [[4100, 2000, 1, 900], [3, 5, 4, 6] * 60, [1] * 700])
+def test_append_as_they_are_for_few_and_many_rows(new):
+    g = torch.Generator().manual_seed(3)
+    first = [17, 0, 5, 40] * (len(new) // 4)
+    lens = [a + b for a, b in zip(first, new)]
+    _, _, table = _paged(lens, 2, 64, 16, 4)
+    cache = torch.randn(sum(S.up(n, 16) for n in lens) + 3, 2, 16, 64, generator=g).to(BF)
+    rows = [torch.randn(sum(new), 2, 64, generator=g).to(BF) for _ in range(2)]
+    dev = [cache.cuda(), cache.cuda()]
+    B.append_keys(rows[0].cuda(), rows[1].cuda(), dev[0], dev[1], table.cuda(), _i32(lens), _cu(new))
+    for x, d in zip(rows, dev):
+        c, at = cache.clone(), 0
+        for i, (a, m) in enumerate(zip(first, new)):
+            slot = torch.arange(a, a + m)
+            c[table[i, slot // 16].long(), :, slot % 16] = x[at:at + m]
+            at += m
+        assert torch.equal(d.cpu(), c)
+
+
 def test_append_to_many_requests():
     rng = random.Random(3)
     first = [rng.randint(0, 40) for _ in range(1200)]
