@@ -1,8 +1,8 @@
 """Thin ctypes binding of libsled.so: same names as include/sled.h, argument marshalling only.
 
 Every step of the verification path runs inside the CUDA library; this module only turns
-Python objects into the plain pointers and sizes the C boundary takes.  There is no CPU
-fallback: loading fails loudly when the library has not been built.
+Python objects into the plain pointers and sizes the C boundary takes (compiled, in _marshal.so, for the operators of
+a decoding step).  There is no CPU fallback: loading fails loudly when the library has not been built.
 """
 from __future__ import annotations
 
