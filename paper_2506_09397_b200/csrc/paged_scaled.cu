@@ -79,13 +79,21 @@ __device__ __forceinline__ uint32_t at(uint32_t base, int key, int c) {
   return base + (key >> 4) * Few<H, G>::kGroup + row * 128 + (((key % P * (H / 16) + c) ^ (row & 7)) << 4);
 }
 
+// What a tile costs whose rows go to two warps (of others: 16), and a unit of 8 or 32 rows beside its tiles.  8 KV heads of 128, us:
+// 32 contexts of 128 .. 16384 keys, 16 rows, with 16, 32, 64, 128, 192 for a unit 105, 93, 71, 58, 54, 4 rows (8 to a unit) with 16, 32,
+// 64, 96, 128 57, 49.4, 42.0, 41.6, 41.8; 8 x 30000 keys of 12 to 20 rows with 16, 22, 26, 30, 34, 40 for a tile of two warps 147, 124,
+// 114, 109, 115, 125.
+constexpr int kSplitTile = 30, kUnit8 = 96, kUnit32 = 192;
 // The line of tiles with units of up to `rows` rows.
 struct FewLine : AttentionLine {
   __device__ __forceinline__ FewLine(const PagedCache& c, const PagedRows& r, int rows) : AttentionLine{c, r, 0, rows, kTile} {}
   __device__ __forceinline__ int min_share() const { return kMinMmaShare; }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w = AttentionLine::operator()(i);
-    if (w.units > 0) w.weight = unit_weight(16, 64, w.tiles, 80);
+    if (w.units > 0) {
+      const int tile = min(w.v.m * r.group, unit_rows) > 16 ? kSplitTile : 16, unit = unit_rows == 8 ? kUnit8 : kUnit32;
+      w.weight = unit_weight(tile, unit, w.tiles, tile + unit);
+    }
     return w;
   }
 };
