@@ -119,13 +119,16 @@ struct TcUnit {
 static_assert(sizeof(TcUnit) <= 64);
 constexpr int kUnitReaders = 14;       // warps 0 - 13
 
-// The line of 64-key tiles with units of up to unit_rows rows.
+// The line of 64-key tiles with units of up to unit_rows rows.  A tile costs about as much with few rows as with many, a unit 7.5
+// times that (8 KV heads of 128, us, with 16 : 130, 20 : 160, 28 : 200, 28 : 220, 28 : 260 for them: 64 trees of 48 - 64 nodes - , - , - ,
+// 224.6, 225.6; 32 contexts of 128 .. 16384 keys, 64 rows 103, 103, 103, - , - ; 8 to 60 tokens each, where units of up to 128 rows
+// weigh 16 : 190, 20 : 160, 25 : 200, 28 : 200 beside 28 : 220 for the others, 231, 198, 170, 161).
 struct TcLine : AttentionLine {
   __device__ __forceinline__ TcLine(const PagedCache& c, const PagedRows& r, int unit_rows) : AttentionLine{c, r, 0, unit_rows, kKeys} {}
   __device__ __forceinline__ int min_share() const { return 1; }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w = AttentionLine::operator()(i);
-    if (w.units > 0) w.weight = w.v.m * r.group > kGroupRows && unit_rows > kGroupRows ? unit_weight(28, 190, w.tiles, 28 + 190) : unit_weight(16, 190, w.tiles, 16 + 190);
+    if (w.units > 0) w.weight = unit_weight(28, 210, w.tiles, 28 + 210);
     return w;
   }
 };
