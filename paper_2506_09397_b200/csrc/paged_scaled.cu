@@ -85,14 +85,16 @@ __device__ __forceinline__ uint32_t at(uint32_t base, int key, int c) {
 // 114, 109, 115, 125.
 constexpr int kSplitTile = 30, kUnit8 = 96, kUnit32 = 192;
 // The line of tiles with units of up to `rows` rows.
+template <int kRows>
 struct FewLine : AttentionLine {
-  __device__ __forceinline__ FewLine(const PagedCache& c, const PagedRows& r, int rows) : AttentionLine{c, r, 0, rows, kTile} {}
+  static constexpr int kUnit = kRows == 8 ? kUnit8 : kUnit32, kSlack = kUnit;
+  __device__ __forceinline__ FewLine(const PagedCache& c, const PagedRows& r) : AttentionLine{c, r, 0, kRows, kTile} {}
   __device__ __forceinline__ int min_share() const { return kMinMmaShare; }
   __device__ __forceinline__ ReqWork operator()(int i) const {
     ReqWork w = AttentionLine::operator()(i);
     if (w.units > 0) {
-      const int tile = min(w.v.m * r.group, unit_rows) > 16 ? kSplitTile : 16, unit = unit_rows == 8 ? kUnit8 : kUnit32;
-      w.weight = unit_weight(tile, unit, w.tiles, tile + unit);
+      const int tile = min(w.v.m * r.group, kRows) > 16 ? kSplitTile : 16;
+      w.weight = unit_weight(tile, kUnit, w.tiles, tile + kUnit);
     }
     return w;
   }
@@ -383,7 +385,7 @@ __global__ void __launch_bounds__(Few<H, G>::kThreads, Few<H, G>::kBlocks) scale
   }
   __syncthreads();
   pdl_wait();
-  const FewLine line(c, r, S::kRows);
+  const FewLine<S::kRows> line(c, r);
   const Share share = block_share(line, blockIdx.x, gridDim.x);
   if (threadIdx.x == 0) leave_none(parts.desc, blockIdx.x);
   if (share.from >= share.to) return;

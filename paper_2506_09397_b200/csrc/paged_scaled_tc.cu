@@ -124,6 +124,7 @@ constexpr int kUnitReaders = 14;       // warps 0 - 13
 // 224.6, 225.6; 32 contexts of 128 .. 16384 keys, 64 rows 103, 103, 103, - , - ; 8 to 60 tokens each, where units of up to 128 rows
 // weigh 16 : 190, 20 : 160, 25 : 200, 28 : 200 beside 28 : 220 for the others, 231, 198, 170, 161).
 struct TcLine : AttentionLine {
+  static constexpr int kSlack = 210;
   __device__ __forceinline__ TcLine(const PagedCache& c, const PagedRows& r, int unit_rows) : AttentionLine{c, r, 0, unit_rows, kKeys} {}
   __device__ __forceinline__ int min_share() const { return 1; }
   __device__ __forceinline__ ReqWork operator()(int i) const {
