@@ -26,7 +26,7 @@
 //
 // Bound by the bytes of long caches - one token, 8 KV heads of 128: 4 x 131072 keys 170 us (6.3 TB/s), 32 x 8192 92 us (5.9),
 // 32 of 128 .. 16384 45 us; 16 rows: 4 x 131072 179 us (6.0) -, between 17 and 32 rows by conversions, products and exponentials
-// of two warps a stage (20 rows, 4 x 131072: 295 us), and by latency where there is little to read (one context of 64 keys 10.2 us,
+// of two warps a stage (20 rows, 4 x 131072: 295 us), and by latency where there is little to read (one context of 64 keys 10.8 us,
 // of which the merge's launch is 3).
 #include "gemm_tc.h"
 #include "kernels.h"
@@ -669,9 +669,9 @@ int64_t paged_scaled_workspace(int h) {
 
 int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedRows& r, char* ws, cudaStream_t s) {
   // By the rows per request and KV head, on average (head_dim 128, 8 KV heads; us).  More than 8: units of 32 rows, as several of 8
-  // read the keys several times - units of 8 against 32, 8 rows: 32 x 8192 keys 95, 96, 8 x 8192 36, 39, 64 x 300 27, 37; 12 rows:
-  // 181, 96; 60, 40; 40, 38.  More than 32: the products of tcgen05, which take a unit of 128 rows in the time of one - units of
-  // 32 against tcgen05, 32 rows: 32 x 4096 96, 128, 8 x 8192 60, 72, 64 x 300 49, 60; 36 rows: 151, 128; 93, 72; 74, 62.  (head_dim
+  // read the keys several times - units of 8 against 32, 8 rows: 32 x 8192 keys 94, 98, 8 x 8192 34, 37, 64 x 300 26, 28; 12 rows:
+  // 179, 98; 56, 37; 40, 29.  More than 32: the products of tcgen05, which take a unit of 128 rows in the time of one - units of
+  // 32 against tcgen05, 32 rows: 32 x 4096 97, 128, 8 x 8192 58, 72, 64 x 300 38, 48; 36 rows: 151, 129; 93, 73; 61, 48.  (head_dim
   // 32 has no kernel of that kind: its products would be half empty.)
   const int64_t rows = static_cast<int64_t>(r.T) * r.group;
   if (c.h >= 64 && rows > 32LL * c.n_reqs) return launch_scaled_tc(c, sc, r, ws, s);

@@ -775,6 +775,18 @@ def test_scaled_results_do_not_depend_on_where_pages_lie(hq, hkv, h, rows, colum
         B.check_status(status)
 
 
+@pytest.mark.parametrize("hq,hkv,h", [(8, 2, 128), (6, 2, 32), (32, 8, 64), (64, 2, 128)])
+@pytest.mark.parametrize("batch,length,rows", [(1, 4100, 3), (1, 9000, 1), (12, 512, 4), (40, 300, 1), (100, 64, 2), (90, 65, 9), (3, 1000, 7), (20, 700, 1)])
+def test_scaled_units_that_are_alike(batch, length, rows, hq, hkv, h):
+    _scaled_check([length] * batch, [rows] * batch, hq, hkv, h, seed=batch + rows)
+
+
+@pytest.mark.parametrize("columns", [lambda c: c, _many_columns])
+def test_scaled_wide_units_that_are_alike(columns):
+    for batch, length, rows in ((1, 2500, 40), (9, 300, 9), (30, 130, 20)):
+        _scaled_check([length] * batch, [rows] * batch, 32, 2, 128, cache=columns(_coded_cache([length] * batch, 2, 128, 16, rows)))
+
+
 def test_scaled_empty_batches():
     q = torch.zeros(0, 8, 64, dtype=BF, device="cuda")
     c, s = torch.zeros(3, 2, 16, 64, device="cuda").to(E4M3), torch.ones(3, 2, 1, device="cuda")
