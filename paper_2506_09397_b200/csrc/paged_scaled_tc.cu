@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
     for (int s = 0; s < L::kStages; ++s) { mbar_init(bar(B_KFULL + s), 4); mbar_init(bar(B_KEMPTY + s), 2); }
     for (int s = 0; s < L::kStages; ++s) { mbar_init(bar(B_VFULL + s), 4); mbar_init(bar(B_VEMPTY + s), 2); }
     mbar_init(bar(B_QFULL), 4);
-    mbar_init(bar(B_QEMPTY), 8);
+    mbar_init(bar(B_QEMPTY), 10);       // the softmax warps and the two product threads
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar(B_SFULL + 2 * s), 1);
       mbar_init(bar(B_SFULL + 2 * s + 1), 1);
@@ -217,8 +217,11 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
         const bool both = kGroups == 2 && u.m * group - u.sg.rb * kUnit > kGroupRows;   // both groups have rows of their own
         const int n_tiles = u.sg.t1 - u.sg.t0, step = both ? 1 : 2, t_first = both ? 0 : s, mine = (n_tiles - t_first + step - 1) / step;
         // (in every unit, also where the group has no tile: then all K and V of earlier units have been there, and the parity of a
-        // stage that the other group has used last cannot be taken for that of the phase before)
+        // stage that the other group has used last cannot be taken for that of the phase before.  Q is given back by this thread
+        // too, by now: without it the others could be through with units of one tile, two phases of this barrier, before a group
+        // without tiles has looked at the first)
         bool ok = mbar_wait(bar(B_QFULL), units & 1, stop);
+        mbar_arrive(bar(B_QEMPTY));
         const uint64_t q = operand_desc(base + L::kOffQ + (both ? s : 0) * L::kQBytes, 1, 1024);
         // scores go two tiles ahead of the outputs, into the buffer that those have left (products of a thread run in order)
         for (int i = 0; ok && i < mine + 2; ++i) {
