@@ -482,7 +482,9 @@ int sled_append_keys(const sled_paged_kv* kv, float* k_scale, float* v_scale, co
 /* sled_attention_tree over a cache in 8 bits (kv->dtype SLED_E4M3, with its scales as in sled_append_keys: any finite
  * numbers).  q and out are bf16; parents, lse, status and workspace as there.  Scores, their maxima and sums are held in fp32;
  * the softmax's numerators, times their block's scale, are rounded to fp16 before they meet V (their sum is not): by 2^-11 of
- * each at most, or by 2^-32 of the row's largest where that is more. */
+ * each at most, or by 2^-32 of the row's largest where that is more.  Keys of less than 2^-111 of the row's largest probability may
+ * count as less than that.  Outputs are sums of exponentials, of 2^8 at most, times values until they are divided by the sum of the
+ * exponentials: these sums must be below 2^128. */
 int sled_attention_scaled_workspace(const sled_paged_kv* kv, int32_t n_rows, int32_t n_q_heads, int64_t* bytes);
 int sled_attention_scaled(const sled_paged_kv* kv, const float* k_scale, const float* v_scale, const void* q, int64_t q_stride,
                           const int32_t* cu_q, const int32_t* parents, int32_t n_rows, int32_t n_q_heads, float scale, void* out,

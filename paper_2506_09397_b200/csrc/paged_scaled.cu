@@ -277,7 +277,7 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
     RowState &r0 = a.st[2 * n], &r1 = a.st[2 * n + 1];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const float x0 = r0.w * vs[m], x1 = r1.w * vs[m];
+      const float x0 = block_weight(r0.w, vs[m]), x1 = block_weight(r1.w, vs[m]);
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         const float s0 = sc[m][n][2 * z], s1 = sc[m][n][2 * z + 1];
@@ -554,8 +554,8 @@ __global__ void __launch_bounds__(Few<H, G>::kThreads, Few<H, G>::kBlocks) scale
 #pragma unroll
         for (int k = 0; k < H / 16; ++k) {
           float* v = a.o[i >> 1][k] + (i & 1);
-          v[0] = dead ? 0.f : v[0] * rest;
-          v[2] = dead ? 0.f : v[2] * rest;
+          v[0] = dead ? 0.f : v[0] * rest * rest;
+          v[2] = dead ? 0.f : v[2] * rest * rest;
         }
         a.st[i].l = l;
       }

@@ -10,7 +10,7 @@ namespace sled {
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kGain = 128.f;      // numerators are at most 2^8 times this
+constexpr float kHalfGain = 3.5f;   // numerators are at most 2^8 times 2^7
 
 // partial results of units that were cut
 struct ScaledParts {
@@ -63,13 +63,26 @@ __device__ __forceinline__ float query_row(const __nv_bfloat16* q, bool valid, u
   return __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
 }
 
+// A block's 2^(s - ref) become numerators by 2^(7 + ref - u) vs.  Scales may be any finite numbers, so that neither the power of two, 2^-129 to
+// 2^164 where a row weighs anything, nor its inverse need be a float: both are kept as their square roots, and multiplied twice.
+// (A row whose u lies further below its ref than 193 has results below 2^-149.)
+__device__ __forceinline__ float weight_root(float ref, float u) { return exp2_approx(fminf(fmaf(ref - u, 0.5f, kHalfGain), 100.f)); }
+__device__ __forceinline__ float rest_root(float m, float u) { return u == -INFINITY ? 0.f : exp2_approx(fmaf(u - (m == -INFINITY ? 0.f : m), 0.5f, -kHalfGain)); }
+// What 2^(s - ref) is multiplied by, at most 2^126 in size: nothing is larger but what multiplies exponentials below 2^-111, in a
+// block whose scale is above 2^(119 + u - ref); NaN stays.
+__device__ __forceinline__ float block_weight(float root, float vs) {
+  float y;
+  asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(root * vs * root), "f"(0x1p126f));
+  return y;
+}
+
 // A row's references: m of the scores, with the sum l of 2^(s - m), and u of the numerators 2^(s - u) vs.  They are raised only when
 // something exceeds them by more than 2^kRaiseBy, which cancels in the end; all else goes by ref, m where that is finite.
 constexpr float kRaiseBy = 8.f;
 struct RowState {
   float m = -INFINITY, l = 0.f, u = -INFINITY;
   float ref = 0.f;
-  float w = 0.f;              // a block's 2^(s - ref) are multiplied by this and vs
+  float w = 0.f;              // the root of what a block's 2^(s - ref) are multiplied by beside vs
   // takes a stage's largest score s and the largest s + log2 |vs|; returns the factor of the output so far
   __device__ __forceinline__ float take(float mx, float mx_u) {
     if (mx > m + kRaiseBy || m == -INFINITY) {
@@ -84,13 +97,13 @@ struct RowState {
       f = exp2_approx(u - (un == -INFINITY ? 0.f : un));
       u = un;
     }
-    w = u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - u, 110.f));
+    w = u == -INFINITY ? 0.f : weight_root(ref, u);
     return f;
   }
   // a largest s - ref that needs no raise, by the largest log2 |vs| of a stage
   __device__ __forceinline__ float room(float lv) const { return m == -INFINITY ? -INFINITY : kRaiseBy + fminf(0.f, (u - lv) - ref); }
-  // what the output is multiplied by at the end
-  __device__ __forceinline__ float rest() const { return u == -INFINITY ? 0.f : exp2_approx(u - (m == -INFINITY ? 0.f : m)) * (1.f / kGain); }
+  // the root of what the output is multiplied by at the end
+  __device__ __forceinline__ float rest() const { return rest_root(m, u); }
 };
 
 }  // namespace sled

@@ -566,13 +566,13 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
               if (!(see1 >> 16)) vs.w = 0.f;
             }
             const float ref = m == -INFINITY ? 0.f : m;
-            const float weight = top_u == -INFINITY ? 0.f : kGain * exp2_approx(fminf(ref - top_u, 110.f));
+            const float weight = weight_root(ref, top_u);
             float mx = -INFINITY, mx_u = -INFINITY;      // of the scores, of those plus log2 |vs|
             sum0 = sum1 = 0.f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const float f = q == 0 ? by.x : q == 1 ? by.y : q == 2 ? by.z : by.w;
-              const float wb = top_u == -INFINITY ? 0.f : weight * (q == 0 ? vs.x : q == 1 ? vs.y : q == 2 ? vs.z : vs.w);
+              const float wb = top_u == -INFINITY ? 0.f : block_weight(weight, q == 0 ? vs.x : q == 1 ? vs.y : q == 2 ? vs.z : vs.w);
               const float top = largest16(v + q * 16) * f;
               mx = fmaxf(mx, top);
               mx_u = fmaxf(mx_u, top + (q == 0 ? lv.x : q == 1 ? lv.y : q == 2 ? lv.z : lv.w));
@@ -628,7 +628,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       // half of the columns each: both results of a row are in the same lane of tensor memory, only maximum, sum and the
       // numerators' reference have to be exchanged.
       const bool joint = !both && n_tiles > 1;
-      const float rest = top_u == -INFINITY ? 0.f : exp2_approx(top_u - (m == -INFINITY ? 0.f : m)) * (1.f / kGain);     // of the output
+      const float rest = rest_root(m, top_u);     // its square is the output's
       if (joint) {
         if (s == 1) tops[row_in_group] = make_float4(m, l, rest, 0.f);
         asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -640,7 +640,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       if (both || joint) ++done[1];
       if (!ok) *stop = 1;
       fence_after();
-      float f_mine = rest, f_other = 0.f;      // factors of the group's own result and of the other's
+      float f_mine = rest, f_other = 0.f, rest_other = 0.f;      // factors of the group's own result and of the other's, beside `rest`
       if (!joint || s == 0) {
         if (joint) {
           const float4 x = tops[row_in_group];
@@ -648,6 +648,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           const float a = exp2_approx(m - ref), b = exp2_approx(x.x - ref);
           f_mine = a * rest;
           f_other = b * x.z;
+          rest_other = x.z;
           l = l * a + x.y * b;
           m = top;
         }
@@ -657,7 +658,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           f_mine *= inv;
           f_other *= inv;
         }
-        if (joint) tops[row_in_group] = make_float4(f_other, f_mine, 0.f, 0.f);
+        if (joint) tops[row_in_group] = make_float4(f_other, f_mine, rest, 0.f);
       }
       if (joint) {
         asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -665,6 +666,7 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
           const float4 x = tops[row_in_group];
           f_mine = x.x;
           f_other = x.y;
+          rest_other = x.z;
         }
       }
       // codes that were left out of a group's products, for the rows that see them (of a chain few keys of the masked tiles
@@ -694,10 +696,10 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
             tmem_ld32(tmem + lanes + 256 + (s ^ 1) * 128 + q * 32, o);
             if (odd[units & 1] == units) add_odd(o, q * 32, s ^ 1);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = v[i] * f_mine + o[i] * f_other;
+            for (int i = 0; i < 32; ++i) v[i] = v[i] * f_mine * rest + o[i] * f_other * rest_other;
           } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= f_mine;
+            for (int i = 0; i < 32; ++i) v[i] = v[i] * f_mine * rest;
           }
           if (valid && u.sg.whole) {
             uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + t_row * r.out_stride + static_cast<int64_t>(head) * H + q * 32);

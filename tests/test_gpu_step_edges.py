@@ -1,8 +1,11 @@
-"""Edges of a decoding step's operators over a caller's paged cache: units of one tile in a row."""
+"""Edges of a decoding step's operators over a caller's paged cache: units of one tile in a row, value scales of any size, what is lost to
+the rounding of numerators."""
 import math
 import random
 
+import paged_ref as R
 import pytest
+import step_ref as S
 import test_gpu_step as T
 import torch
 
@@ -31,3 +34,84 @@ def test_many_units_of_one_tile(longest, columns):
         again = B.attention_tree(q, kc, vc, table, n_kv, T._cu(q_len), k_scale=ks, v_scale=vs, status=status)
         assert torch.equal(first, again)
     B.check_status(status)
+
+
+def _run(cache, q_len, q, parents=None, scale=0.0):
+    kc, ks, vc, vs, table, n_kv = (x.cuda() for x in cache)
+    status = T._status()
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    out = B.attention_tree(q.cuda(), kc, vc, table, n_kv, T._cu(q_len), parents, scale=scale, lse=lse, k_scale=ks, v_scale=vs, status=status)
+    B.check_status(status)
+    return out.cpu().double(), lse.cpu().double()
+
+
+@pytest.mark.parametrize("h", [32, 64, 128])
+@pytest.mark.parametrize("hq", [2, 12, 40, 200])
+@pytest.mark.parametrize("power", [-126, -120, -112, -100, -60, 60, 110])
+def test_value_scales_of_any_size(power, hq, h):
+    """All value scales the same power of two; results are compared times its inverse, so that the bound's absolute part says nothing."""
+    lens, q_len = [200, 90, 40], [4, 1, 7]
+    kc, ks, vc, vs, table, n_kv = T._coded_cache(lens, 2, h, 16, 12, whole=True)
+    if power > 100:                  # sums of exponentials times values stay in fp32
+        vc = (vc.double().nan_to_num(0) / 448).to(E4M3)
+    one = torch.where(vs.isnan(), vs, 1.0)
+    q = torch.randn(sum(q_len), hq, h, generator=torch.Generator().manual_seed(5)).to(BF)
+    out, lse = _run((kc, ks, vc, one * 2.0 ** power, table, n_kv), q_len, q)
+    out = out * 2.0 ** -power
+    at = 0
+    for i, (n, m) in enumerate(zip(lens, q_len)):
+        kk, vv = (R.keys_of(S.values(c, s), table[i], n, 16) for c, s in ((kc, ks), (vc, one)))
+        o, l, _, d_o, d_l, _ = R.attend(q[at:at + m], kk, vv, R.tree_mask(None, m, n), h ** -0.5, BF)
+        d_o += 2.0 ** (-134 - power)             # half a step of the smallest results, 2^-133
+        assert bool(((out[at:at + m] - o).abs() <= d_o).all()), (i, float(((out[at:at + m] - o).abs() / d_o).max()))
+        assert bool(((lse[at:at + m] - l).abs() <= d_l).all())
+        at += m
+
+
+@pytest.mark.parametrize("hq", [2, 12, 40, 200])
+@pytest.mark.parametrize("gap", [60, 100, 118, 124, 131, 160, 400])
+def test_values_of_nothing_under_scores_far_above_the_others(gap, hq):
+    """The first block's keys have the largest scores by 2^gap, values of 0 and the smallest scale, the others' values are large: what
+    the others weigh, down to 2^-111 of the largest, is exact; below, they count as no more than they are."""
+    lens, q_len, h = [90, 40], [4, 1], 64
+    kc, ks, vc, vs, table, n_kv = T._coded_cache(lens, 2, h, 16, 3, whole=True)
+    kc, vc, vs = torch.full(kc.shape, -1.0).to(E4M3), vc.clone(), torch.full(vs.shape, 2.0 ** 30)
+    ks = torch.ones(ks.shape)
+    for i in range(len(lens)):
+        kc[table[i, 0]] = torch.ones(()).to(E4M3)
+        vc.view(torch.uint8)[table[i, 0]] = 0
+        vs[table[i, 0]] = 2.0 ** -126
+    scale = gap * math.log(2) / (2 * h)          # scores +- gap ln(2) / 2
+    q = torch.ones(sum(q_len), hq, h).to(BF)
+    out, lse = _run((kc, ks, vc, vs, table, n_kv), q_len, q, scale=scale)
+    at = 0
+    for i, (n, m) in enumerate(zip(lens, q_len)):
+        kk, vv = (R.keys_of(S.values(c, s), table[i], n, 16) for c, s in ((kc, ks), (vc, vs)))
+        see = R.tree_mask(None, m, n)
+        o, l, p, d_o, d_l, _ = R.attend(q[at:at + m], kk, vv, see, scale, BF)
+        weight = torch.where(p < 2.0 ** -111 * p.amax(-1, keepdim=True), p, 0)
+        d_o += torch.einsum("mrn,rnd->mrd", weight, vv.abs().repeat_interleave(hq // 2, 0))
+        assert bool(((out[at:at + m] - o).abs() <= d_o).all()), (i, float(((out[at:at + m] - o).abs() / d_o).max()))
+        assert bool(((lse[at:at + m] - l).abs() <= d_l).all())
+        at += m
+
+
+@pytest.mark.parametrize("h", [32, 64, 128])
+@pytest.mark.parametrize("hq", [4, 24, 80])
+def test_numerators_are_rounded_by_no_more_than_said(hq, h):
+    """Keys in pairs of nearly the same score and opposite values: what is left is small beside what was added up, so that it shows the
+    numerators' rounding, 2^-11 of each, and not the results' own.  (Rounded to bf16 they would be off by up to 2^-8.)"""
+    lens, q_len = [16, 8, 32, 24], [1] * 4
+    kc, ks, vc, vs, table, n_kv = T._coded_cache(lens, 2, h, 16, 31, whole=True)
+    k8, v8 = kc.view(torch.uint8).clone(), vc.view(torch.uint8).clone()
+    k8[:, :, 1::2], v8[:, :, 1::2] = k8[:, :, ::2], v8[:, :, ::2] ^ 0x80
+    k8[:, :, 1::2, 0] = torch.where(k8[:, :, ::2, 0] & 0x7f == 0, k8[:, :, ::2, 0], k8[:, :, ::2, 0] - 1)       # a code nearer to 0
+    kc, vc = k8.view(E4M3), v8.view(E4M3)
+    q = torch.randn(sum(q_len), hq, h, generator=torch.Generator().manual_seed(5)).to(BF)
+    out, _ = _run((kc, ks, vc, vs, table, n_kv), q_len, q)
+    for i, n in enumerate(lens):
+        kk, vv = (R.keys_of(S.values(c, s), table[i], n, 16) for c, s in ((kc, ks), (vc, vs)))
+        o, _, p, d_o, _, _ = R.attend(q[i:i + 1], kk, vv, R.tree_mask(None, 1, n), h ** -0.5, BF)
+        spread = torch.einsum("mrn,rnd->mrd", p, vv.abs().repeat_interleave(hq // 2, 0))
+        d_o += (2.0 ** -11 - 2.0 ** -8) * spread          # numerators in fp16, or 2^-32 of the largest, which is less here
+        assert bool(((out[i] - o[0]).abs() <= d_o[0]).all()), (i, float(((out[i] - o[0]).abs() / d_o[0]).max()))
