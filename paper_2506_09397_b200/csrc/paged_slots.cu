@@ -31,13 +31,15 @@ struct SlotsReq {
   __device__ __forceinline__ int take() const { return max(0, want - have); }
   __device__ __forceinline__ int back() const { return max(0, have - want); }
 };
+// pages of n keys; n + page_size need not fit in 32 bits
+__device__ __forceinline__ int pages_of(int n, int page_size) { return n > 0 ? (n - 1) / page_size + 1 : 0; }
 __device__ __forceinline__ bool slots_req(const SlotsCall& a, int i, SlotsReq& r) {
   const int n = a.n_kv[i], keep = a.n_keep ? a.n_keep[i] : n, fresh = a.n_new[i];
   const long long most = static_cast<long long>(a.table_cols) * a.page_size;       // below 2^31
   if (n < 0 || keep < 0 || keep > n || fresh < 0 || n > most || keep + static_cast<long long>(fresh) > most) return false;
   r.keep = keep;
-  r.have = (n + a.page_size - 1) / a.page_size;
-  r.want = (keep + fresh + a.page_size - 1) / a.page_size;
+  r.have = pages_of(n, a.page_size);
+  r.want = pages_of(keep + fresh, a.page_size);
   r.rows = fresh;
   return true;
 }

@@ -1,5 +1,5 @@
-"""Edges of a decoding step's operators over a caller's paged cache: units of one tile in a row, value scales of any size, what is lost to
-the rounding of numerators."""
+"""Edges of a decoding step's operators over a caller's paged cache: places in pages of any size, units of one tile in a row, value
+scales of any size, what is lost to the rounding of numerators."""
 import math
 import random
 
@@ -13,6 +13,18 @@ from paper_2506_09397_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
 BF, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+
+
+# ------------------------------------------------------------------------------------------------------- places
+@pytest.mark.parametrize("page,cols", [(1 << 30, 1), (1_500_000_000, 1), (2 ** 31 - 1025, 1), (715_827_000, 3), (3000, 715_827), (1, 2_000_000)])
+def test_places_in_pages_of_any_size(page, cols):
+    """A request's keys and a page's slots together need more than 32 bits."""
+    full = page * cols
+    rng = random.Random(page)
+    T._slots_case(rng, [full - 7, 0, 5], [full - 9, 0, 5], [9, 4, 0], page, cols=cols)
+    T._slots_case(rng, [full, 0, full - page // 2], [0, 0, full - page // 2], [3, 12, page // 2 if page < 10 else 7], page, cols=cols, extra_rows=2)
+    T._slots_case(rng, [0, full - 1], [0, full - 1], [2, 1], page, cols=cols, spare=0)
+    T._slots_case(rng, [0, full - 1], [0, full - 1], [2, 1], page, cols=cols, spare=0, short=1)
 
 
 # ------------------------------------------------------------------------------- attention over a cache in 8 bits
