@@ -1,7 +1,7 @@
 // New keys and values into a paged cache: as they are, or as e4m3 codes with a scale for every block of 16 slots and KV head.
 //
 // A block that receives keys: let m be the largest finite |x| of its new rows and 2^e, e >= -126, the smallest power of two with
-// m <= 448 2^e.  Its scale becomes s' = max(2^e, s) where it has older keys (s their scale), else 2^e; code = e4m3(x / s').
+// m <= 448 2^e.  Its scale becomes s' = max(2^e, |s|) where it has older keys (s their scale), else 2^e; code = e4m3(x / s').
 // With powers of two nothing is lost by the quotient, and older codes that move from s to s' only lose what falls below the
 // smallest code.
 //
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const PagedCache c, co
           }
         top = __reduce_max_sync(0xffffffffu, top);
       }
-      const float now = fmaxf(least_scale(top), before), inv = 1.f / now;
+      const float now = fmaxf(least_scale(top), fabsf(before)), inv = 1.f / now;      // (a caller's own scale may be below 0)
       plain = plain && (__float_as_uint(now) & 0x7fffffu) == 0;      // a scale of the caller's own may be no power of two: true quotients
       uint8_t* mine = to + sub_row * H;
       auto codes = [&](int p) {

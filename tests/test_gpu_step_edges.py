@@ -1,5 +1,5 @@
-"""Edges of a decoding step's operators over a caller's paged cache: places in pages of any size, units of one tile in a row, value
-scales of any size, what is lost to the rounding of numerators."""
+"""Edges of a decoding step's operators over a caller's paged cache: places in pages of any size, keys beside
+scales below 0, units of one tile in a row, value scales of any size, what is lost to the rounding of numerators."""
 import math
 import random
 
@@ -25,6 +25,38 @@ def test_places_in_pages_of_any_size(page, cols):
     T._slots_case(rng, [full, 0, full - page // 2], [0, 0, full - page // 2], [3, 12, page // 2 if page < 10 else 7], page, cols=cols, extra_rows=2)
     T._slots_case(rng, [0, full - 1], [0, full - 1], [2, 1], page, cols=cols, spare=0)
     T._slots_case(rng, [0, full - 1], [0, full - 1], [2, 1], page, cols=cols, spare=0, short=1)
+
+
+# ---------------------------------------------------------------------------------------------------------- keys
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scale", [-4.0, -0.3, -2.0 ** -9, -1e20])
+def test_append_beside_scales_below_0(scale, dtype):
+    """Attention reads scales below 0; older keys of such a block stay what they were."""
+    page, h, first, new = 32, 64, [5, 20, 0], [3, 30, 9]
+    lens = [a + b for a, b in zip(first, new)]
+    kept = [T._paged(lens, 2, h, page, 7 + i) for i in range(2)]
+    table = kept[0][2]
+    g = torch.Generator().manual_seed(3)
+    rows = [torch.randn(sum(new), 2, h, generator=g).to(dtype) for _ in range(2)]
+    before = [(c.clone(), torch.full_like(s, scale)) for c, s, _ in kept]
+    after = [(c.cuda(), s.cuda()) for c, s in before]
+    status = T._status()
+    B.append_keys(*(x.cuda() for x in rows), after[0][0], after[1][0], table.cuda(), T._i32(lens), T._cu(new), k_scale=after[0][1], v_scale=after[1][1],
+                  status=status)
+    B.check_status(status)
+    for x, was, now in zip(rows, before, after):
+        at = 0
+        for i, (a, m) in enumerate(zip(first, new)):
+            old, got, size = (R.keys_of(y, table[i], a + m, page) for y in (S.values(*was), S.values(now[0].cpu(), now[1].cpu()),
+                                                                         now[1].cpu().double().abs().repeat_interleave(16, -1)))
+            want = torch.cat([old[:, :a], x[at:at + m].double().transpose(0, 1)], 1)
+            assert torch.equal(got[:, :a].isnan(), want[:, :a].isnan())
+            # half a step of a code, or of the smallest code; quotients are of 32 bits
+            off = (got - want).abs() - want.abs() * (2.0 ** -4 + 2.0 ** -20) - 2.0 ** -10 * size[..., None]
+            assert bool((off.nan_to_num(0) <= 0).all())
+            untouched = a // 16 * 16
+            assert torch.equal(got[:, :untouched].nan_to_num(7), old[:, :untouched].nan_to_num(7))
+            at += m
 
 
 # ------------------------------------------------------------------------------- attention over a cache in 8 bits
