@@ -26,6 +26,16 @@ struct Refused {
 void check(int code, const char* what) {
   if (code != SLED_OK) throw Refused{code, what};
 }
+// The call itself, without the interpreter's lock: a launch may wait for room in its stream's queue, and the stream for a host
+// function that needs the lock.  Nothing of Python is touched meanwhile: tensors are the caller's, addresses are known.
+template <typename Call>
+int unlocked(Call call) {
+  struct Unlocked {
+    PyThreadState* state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+  } now;
+  return call();
+}
 struct NotATensor {
   std::string name;
 };
@@ -162,8 +172,13 @@ PyObject* attention_scaled(PyObject* const* a) {
   int64_t bytes = 0;
   check(sled_attention_scaled_workspace(&kv, rows, heads, &bytes), what);
   const at::Tensor ws = at::empty({bytes}, q.options().dtype(at::kByte));
-  check(sled_attention_scaled(&kv, ks, vs, q.data_ptr(), q_stride, ints(cu_q, what, "cu_q", dev), parents, rows, heads, static_cast<float>(scale),
-                              out.data_ptr(), out_stride, lse, status_of(a[11], what, dev), ws.data_ptr(), bytes, stream_of(dev)), what);
+  const void* const queries = q.data_ptr();
+  void *const results = out.data_ptr(), *const space = ws.data_ptr(), *const stream = stream_of(dev);
+  int32_t *const offsets = ints(cu_q, what, "cu_q", dev), *const status = status_of(a[11], what, dev);
+  check(unlocked([&] {
+    return sled_attention_scaled(&kv, ks, vs, queries, q_stride, offsets, parents, rows, heads, static_cast<float>(scale), results, out_stride, lse, status, space,
+                                 bytes, stream);
+  }), what);
   if (!given(a[8])) return THPVariable_Wrap(made);
   Py_INCREF(a[8]);
   return a[8];
@@ -183,8 +198,12 @@ PyObject* append_keys(PyObject* const* a) {
   float *ks = nullptr, *vs = nullptr;
   if (kv.dtype == SLED_E4M3 || given(a[7]) || given(a[8])) scales_of(what, k_cache, a[7], a[8], &ks, &vs);
   if (cu_q.dim() != 1 || cu_q.numel() != static_cast<int64_t>(kv.n_reqs) + 1) refuse(what, "cu_q must be [n_reqs + 1]");
-  check(sled_append_keys(&kv, ks, vs, k.data_ptr(), row_stride(k, what, "k"), v.data_ptr(), row_stride(v, what, "v"), type,
-                         ints(cu_q, what, "cu_q", dev), rows_of(k, what), status_of(a[9], what, dev), stream_of(dev)), what);
+  const void *const keys = k.data_ptr(), *const values = v.data_ptr();
+  const int64_t k_stride = row_stride(k, what, "k"), v_stride = row_stride(v, what, "v");
+  const int32_t rows = rows_of(k, what);
+  int32_t *const offsets = ints(cu_q, what, "cu_q", dev), *const status = status_of(a[9], what, dev);
+  void* const stream = stream_of(dev);
+  check(unlocked([&] { return sled_append_keys(&kv, ks, vs, keys, k_stride, values, v_stride, type, offsets, rows, status, stream); }), what);
   Py_RETURN_NONE;
 }
 
@@ -223,9 +242,15 @@ PyObject* rotary(PyObject* const* a) {
   if (transpose < 0) throw Refused{1, ""};
   const int64_t rows = q.size(0), half = tensor(a[3], "frequencies").numel();
   if (half > 256) refuse(what, "head_dim is at most 512");
-  check(sled_rotary(&qh, given(a[1]) ? &kh : nullptr, static_cast<int32_t>(rows), static_cast<int32_t>(q.size(2)), type,
-                    vector_of<int32_t>(a[2], what, "positions", dev, rows, at::kInt), vector_of<double>(a[3], what, "frequencies", dev, half, at::kDouble),
-                    static_cast<int32_t>(2 * half), pairs, static_cast<float>(amplitude), transpose, stream_of(dev)), what);
+  const int32_t head_dim = static_cast<int32_t>(q.size(2));
+  const int32_t* const positions = vector_of<int32_t>(a[2], what, "positions", dev, rows, at::kInt);
+  const double* const frequencies = vector_of<double>(a[3], what, "frequencies", dev, half, at::kDouble);
+  const sled_heads* const keys = given(a[1]) ? &kh : nullptr;
+  void* const stream = stream_of(dev);
+  check(unlocked([&] {
+    return sled_rotary(&qh, keys, static_cast<int32_t>(rows), head_dim, type, positions, frequencies, static_cast<int32_t>(2 * half), pairs,
+                       static_cast<float>(amplitude), transpose, stream);
+  }), what);
   PyObject* q_out = given(a[7]) ? Py_NewRef(a[7]) : THPVariable_Wrap(q_made);
   PyObject* k_out = !given(a[1]) ? Py_NewRef(Py_None) : given(a[8]) ? Py_NewRef(a[8]) : THPVariable_Wrap(k_made);
   PyObject* both = PyTuple_Pack(2, q_out, k_out);
@@ -264,15 +289,21 @@ PyObject* page_slots(PyObject* const* a) {
     ~Hold() { for (int i = 0; i < 5; ++i) Py_DECREF(p[i]); }
   } hold{out};
   const int32_t n_reqs = static_cast<int32_t>(n);
-  check(sled_page_slots(vector_of<int32_t>(a[0], what, "n_kv", dev, n, at::kInt),
-                        given(a[7]) ? vector_of<int32_t>(a[7], what, "n_keep", dev, n, at::kInt) : nullptr,
-                        vector_of<int32_t>(a[1], what, "n_new", dev, n, at::kInt), n_reqs, page_size, ints(table, what, "page_table", dev),
-                        static_cast<int32_t>(stride), static_cast<int32_t>(cols), vector_of<int32_t>(a[3], what, "free_pages", dev, cap, at::kInt),
-                        static_cast<int32_t>(cap), vector_of<int32_t>(a[4], what, "n_free", dev, 1, at::kInt),
-                        vector_of<int32_t>(out[0], what, "out.n_kv", dev, n, at::kInt), vector_of<int32_t>(out[4], what, "out.n_free", dev, 1, at::kInt),
-                        vector_of<int32_t>(out[1], what, "out.cu_q", dev, n + 1, at::kInt),
-                        vector_of<int32_t>(out[2], what, "out.positions", dev, n_rows, at::kInt),
-                        vector_of<int64_t>(out[3], what, "out.slots", dev, n_rows, at::kLong), n_rows, status_of(a[9], what, dev), stream_of(dev)), what);
+  const int32_t* const have = vector_of<int32_t>(a[0], what, "n_kv", dev, n, at::kInt);
+  const int32_t* const keep = given(a[7]) ? vector_of<int32_t>(a[7], what, "n_keep", dev, n, at::kInt) : nullptr;
+  const int32_t* const fresh = vector_of<int32_t>(a[1], what, "n_new", dev, n, at::kInt);
+  int32_t *const pages = ints(table, what, "page_table", dev), *const stack = vector_of<int32_t>(a[3], what, "free_pages", dev, cap, at::kInt);
+  const int32_t* const n_free = vector_of<int32_t>(a[4], what, "n_free", dev, 1, at::kInt);
+  int32_t *const n_kv_out = vector_of<int32_t>(out[0], what, "out.n_kv", dev, n, at::kInt), *const n_free_out = vector_of<int32_t>(out[4], what, "out.n_free", dev, 1, at::kInt);
+  int32_t* const cu_q = vector_of<int32_t>(out[1], what, "out.cu_q", dev, n + 1, at::kInt);
+  int32_t* const positions = vector_of<int32_t>(out[2], what, "out.positions", dev, n_rows, at::kInt);
+  int64_t* const slots = vector_of<int64_t>(out[3], what, "out.slots", dev, n_rows, at::kLong);
+  int32_t* const status = status_of(a[9], what, dev);
+  void* const stream = stream_of(dev);
+  check(unlocked([&] {
+    return sled_page_slots(have, keep, fresh, n_reqs, page_size, pages, static_cast<int32_t>(stride), static_cast<int32_t>(cols), stack, static_cast<int32_t>(cap),
+                           n_free, n_kv_out, n_free_out, cu_q, positions, slots, n_rows, status, stream);
+  }), what);
   return PyTuple_Pack(5, out[0], out[1], out[2], out[3], out[4]);
 }
 

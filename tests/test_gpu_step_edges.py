@@ -2,6 +2,8 @@
 scales below 0, units of one tile in a row, value scales of any size, what is lost to the rounding of numerators."""
 import math
 import random
+import threading
+import time
 
 import paged_ref as R
 import pytest
@@ -159,3 +161,42 @@ def test_numerators_are_rounded_by_no_more_than_said(hq, h):
         spread = torch.einsum("mrn,rnd->mrd", p, vv.abs().repeat_interleave(hq // 2, 0))
         d_o += (2.0 ** -11 - 2.0 ** -8) * spread          # numerators in fp16, or 2^-32 of the largest, which is less here
         assert bool(((out[i] - o[0]).abs() <= d_o[0]).all()), (i, float(((out[i] - o[0]).abs() / d_o[0]).max()))
+
+
+# ---------------------------------------------------------------------------------------------------------- calls
+@pytest.mark.parametrize("name", ["page_slots", "rotary", "append_keys", "attention"])
+def test_other_threads_run_while_a_launch_waits(name):
+    """A stream's queue that is full makes a launch wait; the interpreter's other threads go on meanwhile."""
+    i, table = T._i32([1]), T._i32([[0, 1]])
+    cache, scale = torch.zeros(3, 2, 16, 64, device="cuda").to(E4M3), torch.ones(3, 2, 1, device="cuda")
+    rows, free = torch.zeros(1, 2, 64, dtype=BF, device="cuda"), T._i32([2])
+    values, value_scale, out = cache.clone(), scale.clone(), torch.empty_like(rows)
+    slots = B.page_slots(i, i, table, free, T._i32([1]), page_size=16, n_rows=1)
+    frequencies, n_free = B.rotary_frequencies(64)[0].cuda(), T._i32([1])
+    cu = T._cu([1])
+    call = {"page_slots": lambda: B.page_slots(i, i, table, free, n_free, page_size=16, n_rows=1, out=slots),
+            "rotary": lambda: B.rotary(rows, None, i, frequencies, q_out=out),
+            "append_keys": lambda: B.append_keys(rows, rows, cache, values, table, i, cu, k_scale=scale, v_scale=value_scale),
+            "attention": lambda: B.attention_tree(rows, cache, values, table, i, cu, k_scale=scale, v_scale=value_scale, out=out)}[name]
+    call()
+    torch.cuda.synchronize()
+    ticks, done = [], threading.Event()
+
+    def tick():
+        while not done.is_set():
+            ticks.append(time.perf_counter())
+            time.sleep(0.001)
+
+    other = threading.Thread(target=tick)
+    other.start()
+    begin = time.perf_counter()
+    torch.cuda._sleep(int(1.2e9))            # cycles: 0.6 s and more
+    for _ in range(4000):
+        call()
+    end = time.perf_counter()
+    done.set()
+    other.join()
+    torch.cuda.synchronize()
+    assert end - begin > 0.4                 # the queue was full
+    seen = [begin] + [t for t in ticks if begin <= t <= end] + [end]
+    assert max(b - a for a, b in zip(seen, seen[1:])) < 0.2
