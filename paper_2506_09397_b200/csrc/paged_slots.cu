@@ -31,8 +31,8 @@ struct SlotsReq {
   __device__ __forceinline__ int take() const { return max(0, want - have); }
   __device__ __forceinline__ int back() const { return max(0, have - want); }
 };
-// pages of n keys; n + page_size need not fit in 32 bits
-__device__ __forceinline__ int pages_of(int n, int page_size) { return n > 0 ? (n - 1) / page_size + 1 : 0; }
+// pages of n keys; the sum is below 2^32 for every length and page size that the call accepts
+__device__ __forceinline__ int pages_of(int n, int page_size) { return static_cast<int>((static_cast<unsigned>(n) + page_size - 1) / page_size); }
 __device__ __forceinline__ bool slots_req(const SlotsCall& a, int i, SlotsReq& r) {
   const int n = a.n_kv[i], keep = a.n_keep ? a.n_keep[i] : n, fresh = a.n_new[i];
   const long long most = static_cast<long long>(a.table_cols) * a.page_size;       // below 2^31
