@@ -188,6 +188,10 @@ def marshal():
         if not os.path.exists(os.path.join(_HERE, "_marshal.so")):
             raise RuntimeError("paper_2506_09397_b200/_marshal.so is missing: build it with paper_2506_09397_b200.build.build()")
         from . import _marshal as m
+        from .build import marshal_for
+        if m.built_for != marshal_for():
+            raise RuntimeError(f"paper_2506_09397_b200/_marshal.so was built for {m.built_for}, this is {marshal_for()}: build it again with "
+                               "paper_2506_09397_b200.build.build()")
         m.set_error(SledError)
         _marshal = m
     return _marshal

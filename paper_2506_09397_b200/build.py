@@ -6,6 +6,7 @@ import subprocess
 import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
+from importlib.metadata import version
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -63,10 +64,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def marshal_for() -> str:
+    """What _marshal.so is tied to: the versions of torch and of Python whose classes it was compiled against."""
+    return f"torch {version('torch')}, {sysconfig.get_config_var('SOABI')}"
+
+
 def build_marshal(force: bool, run) -> None:
-    """The binding's argument marshalling, against torch's headers; it finds libsled.so beside itself."""
-    source = os.path.join(CSRC, "marshal.cpp")
-    if not force and not _stale(MARSHAL, [source, os.path.join(HERE, "..", "include", "sled.h")]):
+    """The binding's argument marshalling, against torch's headers; it finds libsled.so beside itself.  Built again for another torch or
+    Python, too."""
+    source, note, tied_to = os.path.join(CSRC, "marshal.cpp"), os.path.join(OBJ, "marshal.txt"), marshal_for()
+    built_for = ""
+    if os.path.exists(note):
+        with open(note) as f:
+            built_for = f.read()
+    if not force and built_for == tied_to and not _stale(MARSHAL, [source, os.path.join(HERE, "..", "include", "sled.h")]):
         return
     import torch
     root = os.path.dirname(torch.__file__)
@@ -74,9 +85,11 @@ def build_marshal(force: bool, run) -> None:
     tmp = MARSHAL + f".{os.getpid()}.tmp"
     run(["g++", "-std=c++17", "-O2", "-shared", "-fPIC", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
          "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
-         "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda, source, "-o", tmp, "-L" + os.path.join(root, "lib"), "-ltorch_python",
+         f'-DSLED_BUILT_FOR="{tied_to}"', "-isystem", sysconfig.get_paths()["include"], "-isystem", cuda, source, "-o", tmp, "-L" + os.path.join(root, "lib"), "-ltorch_python",
          "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L" + HERE, "-l:libsled.so", "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, MARSHAL)
+    with open(note, "w") as f:
+        f.write(tied_to)
 
 
 if __name__ == "__main__":

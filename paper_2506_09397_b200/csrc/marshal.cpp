@@ -351,4 +351,11 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_method
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__marshal() {
+  PyObject* m = PyModule_Create(&g_module);
+  if (m && PyModule_AddStringConstant(m, "built_for", SLED_BUILT_FOR)) {      // the torch and Python that it is tied to
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
