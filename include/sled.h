@@ -480,7 +480,8 @@ int sled_append_keys(const sled_paged_kv* kv, float* k_scale, float* v_scale, co
                      int64_t v_stride, int32_t rows_dtype, const int32_t* cu_q, int32_t n_rows, int32_t* status, void* stream);
 
 /* sled_attention_tree over a cache in 8 bits (kv->dtype SLED_E4M3, with its scales as in sled_append_keys: any finite
- * numbers).  q and out are bf16; parents, lse, status and workspace as there.  Scores, their maxima and sums are held in fp32;
+ * numbers).  q and out are bf16; parents, lse, status and workspace as there.  Scores, their maxima and sums are held in fp32, of
+ * queries whose elements below 2^-31 of their row's largest in size are off by up to 2^-39 of that (the others are exact);
  * the softmax's numerators, times their block's scale, are rounded to fp16 before they meet V (their sum is not): by 2^-11 of
  * each at most, or by 2^-32 of the row's largest where that is more.  Keys of less than 2^-111 of the row's largest probability may
  * count as less than that.  Outputs are sums of exponentials, of 2^8 at most, times values until they are divided by the sum of the

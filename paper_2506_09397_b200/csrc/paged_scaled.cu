@@ -6,7 +6,7 @@
 // scales stay out of the products' operands: ks multiplies a score, vs goes into the numerators.
 //
 // Codes become fp16 in registers, which is exact; queries do too, times a power of two per row that brings the row's largest
-// element to 2^14, so that nothing of them is lost either.  The numerators of a row meet V as fp16(2^7 2^(s_x - u) vs_b) with a
+// element to 2^14 .. 2^15: of them is lost what lies below 2^-39 of the largest, all of it of elements below 2^-31 of it.  The numerators of a row meet V as fp16(2^7 2^(s_x - u) vs_b) with a
 // reference of their own, u = max (s_x + log2 vs_b) so far, or less by up to 8: the largest is 2^7 to 2^15 whatever the blocks'
 // scales are, and what is lost of another is 2^-11 of itself, or 2^-32 of the largest where that is more.  u is joined with m at
 // the end of a unit.

@@ -42,7 +42,7 @@ __device__ __forceinline__ void mma_half(float c[4], const uint32_t a[4], uint32
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// This lane's H / 4 elements of a query row as fp16, times a power of two that brings the row's largest finite element to 2^14;
+// This lane's H / 4 elements of a query row as fp16, times a power of two that brings the row's largest finite element to 2^14 .. 2^15;
 // returns the factor that undoes it.  All lanes call it.
 template <int H>
 __device__ __forceinline__ float query_row(const __nv_bfloat16* q, bool valid, uint32_t f[H / 8]) {

@@ -1,5 +1,6 @@
 """Edges of a decoding step's operators over a caller's paged cache: places in pages of any size, keys beside
-scales below 0, units of one tile in a row, value scales of any size, what is lost to the rounding of numerators."""
+scales below 0, units of one tile in a row, value scales of any size, what is lost to the rounding of queries
+and numerators, calls that wait."""
 import math
 import random
 import threading
@@ -161,6 +162,33 @@ def test_numerators_are_rounded_by_no_more_than_said(hq, h):
         spread = torch.einsum("mrn,rnd->mrd", p, vv.abs().repeat_interleave(hq // 2, 0))
         d_o += (2.0 ** -11 - 2.0 ** -8) * spread          # numerators in fp16, or 2^-32 of the largest, which is less here
         assert bool(((out[i] - o[0]).abs() <= d_o[0]).all()), (i, float(((out[i] - o[0]).abs() / d_o[0]).max()))
+
+
+@pytest.mark.parametrize("h", [32, 64, 128])
+@pytest.mark.parametrize("hq", [4, 24, 80])
+@pytest.mark.parametrize("ratio", [20, 30, 34, 37, 45])
+def test_queries_with_one_element_far_above_the_others(ratio, hq, h):
+    """The largest element meets codes of 0, so that scores are what the others make of them: those are off by 2^-39 of the largest at most
+    where they are below 2^-31 of it, and exact elsewhere."""
+    lens, q_len = [100, 40, 200], [1, 3, 2]
+    kc, ks, vc, vs, table, n_kv = T._coded_cache(lens, 2, h, 16, 41, whole=True)
+    kc = kc.view(torch.uint8).clone()
+    kc[..., 3] = 0
+    kc = kc.view(E4M3)
+    q = torch.randn(sum(q_len), hq, h, generator=torch.Generator().manual_seed(6)).to(BF)
+    q[..., 3] = 2.0 ** ratio
+    out, lse = _run((kc, ks, vc, vs, table, n_kv), q_len, q)
+    at = 0
+    for i, (n, m) in enumerate(zip(lens, q_len)):
+        kk, vv = (R.keys_of(S.values(c, s), table[i], n, 16) for c, s in ((kc, ks), (vc, vs)))
+        o, l, p, d_o, d_l, _ = R.attend(q[at:at + m], kk, vv, R.tree_mask(None, m, n), h ** -0.5, BF)
+        mine = q[at:at + m].double()
+        off = torch.where(mine.abs() < 2.0 ** (ratio - 31), 2.0 ** (ratio - 39), 0).clamp_max(mine.abs())      # of an element; no more than itself
+        d_s = torch.einsum("mgrd,gnd->mgrn", off.view(m, 2, hq // 2, h), kk.abs()).amax(-1).reshape(m, hq) * h ** -0.5
+        spread = torch.einsum("mrn,rnd->mrd", p, vv.abs().repeat_interleave(hq // 2, 0))
+        assert bool(((lse[at:at + m] - l).abs() <= d_l + d_s).all())
+        assert bool(((out[at:at + m] - o).abs() <= d_o + torch.expm1(2 * d_s)[..., None] * spread).all())
+        at += m
 
 
 # ---------------------------------------------------------------------------------------------------------- calls
