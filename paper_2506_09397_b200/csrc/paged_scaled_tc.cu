@@ -265,7 +265,11 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
       int units = 0;
       auto publish = [&](const TcUnit& u) {
         if (lane == 0) {
-          if (*stop == 0 && mbar_wait(bar(B_UEMPTY + units % kUnitSlots), ((units / kUnitSlots) & 1) ^ 1, stop)) {
+          // (a slot becomes free when its stretch is done with, which may take many times what other waits do: as long as nobody
+          // else gives up, up to a minute; 2^31 keys take half of that)
+          bool free = false;
+          for (int tries = 0; !free && tries < 600 && *stop == 0; ++tries) free = mbar_wait(bar(B_UEMPTY + units % kUnitSlots), ((units / kUnitSlots) & 1) ^ 1, stop);
+          if (free) {
             const_cast<TcUnit*>(unit_slots)[units % kUnitSlots] = u;
             mbar_arrive(bar(B_UFULL + units % kUnitSlots));
           } else {

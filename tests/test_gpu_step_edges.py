@@ -83,6 +83,26 @@ def test_many_units_of_one_tile(longest, columns):
     B.check_status(status)
 
 
+def test_stretches_that_take_longer_than_a_wait():
+    """Four contexts of twelve million keys, the same 256 each time, to every SM: a quarter of a second each."""
+    hq, h, n, batch = 40, 64, 48 * 1024 * 256, 4 * torch.cuda.get_device_properties(0).multi_processor_count
+    kc, ks, vc, vs, where, _ = T._coded_cache([256], 1, h, 256, 2)
+    q = torch.randn(1, hq, h, generator=torch.Generator().manual_seed(7)).to(BF)
+    page_of = int(where[0, 0])
+    kk, vv = (R.keys_of(S.values(c, s), where[0], 256, 256) for c, s in ((kc, ks), (vc, vs)))
+    o, l, p, d_o, d_l, _ = R.attend(q, kk, vv, R.tree_mask(None, 1, 256), h ** -0.5, BF)
+    # sums and outputs of a row: 16 keys at a time are added to what there is, an addition off by 2^-24
+    rel = n // 16 * 2.0 ** -24
+    spread = torch.einsum("mrn,rnd->mrd", p, vv.abs().repeat_interleave(hq, 0))
+    table = torch.full((batch, n // 256), page_of, dtype=torch.int32, device="cuda")
+    status, lse = T._status(), torch.zeros(batch, hq, device="cuda")
+    out = B.attention_tree(q.cuda().expand(batch, -1, -1).contiguous(), kc.cuda(), vc.cuda(), table, T._i32([n] * batch), T._cu([1] * batch), lse=lse,
+                           k_scale=ks.cuda(), v_scale=vs.cuda(), status=status)
+    B.check_status(status)
+    assert bool(((out.cpu().double() - o).abs() <= d_o + 2 * rel * spread).all())
+    assert bool(((lse.cpu().double() - (l + math.log(n // 256))).abs() <= d_l + rel).all())
+
+
 def _run(cache, q_len, q, parents=None, scale=0.0):
     kc, ks, vc, vs, table, n_kv = (x.cuda() for x in cache)
     status = T._status()
