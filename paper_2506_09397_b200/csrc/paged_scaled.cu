@@ -220,9 +220,19 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
           top = fmaxf(top, s);
         }
       }
-      if (!kMasked) calm = calm && !(top > r.room(fmaxf(lv[0], lv[1])));
+      if (!kMasked) calm = calm && top < r.room(fmaxf(lv[0], lv[1]));
     }
-  if (kMasked || !__all_sync(0xffffffffu, calm)) {
+  // what the exponentials of a row and block are multiplied by (of more rows there are not the registers to keep it)
+  constexpr bool kKept = G == 1;
+  float by[kKept ? 2 * G : 1][2];
+  if (!kMasked && __all_sync(0xffffffffu, calm)) {
+    if constexpr (kKept) {
+#pragma unroll
+      for (int i = 0; i < 2 * G; ++i)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) by[i][m] = plain_weight(a.st[i].w, vs[m]);
+    }
+  } else {
     float al[2 * G];
 #pragma unroll
     for (int n = 0; n < G; ++n)
@@ -260,6 +270,10 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
         for (int m = 0; m < 2; ++m)
 #pragma unroll
           for (int z = 0; z < 2; ++z) sc[m][n][2 * z + e] -= r.ref;
+        if constexpr (kKept) {
+#pragma unroll
+          for (int m = 0; m < 2; ++m) by[2 * n + e][m] = block_weight(r.w, vs[m]);
+        }
       }
 #pragma unroll
     for (int n = 0; n < G; ++n)
@@ -277,7 +291,7 @@ __device__ __forceinline__ void stage(FewState<H, G>& a, int prefix, int end, bo
     RowState &r0 = a.st[2 * n], &r1 = a.st[2 * n + 1];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const float x0 = block_weight(r0.w, vs[m]), x1 = block_weight(r1.w, vs[m]);
+      const float x0 = kKept ? by[kKept ? 2 * n : 0][m] : block_weight(r0.w, vs[m]), x1 = kKept ? by[kKept ? 2 * n + 1 : 0][m] : block_weight(r1.w, vs[m]);
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         const float s0 = sc[m][n][2 * z], s1 = sc[m][n][2 * z + 1];

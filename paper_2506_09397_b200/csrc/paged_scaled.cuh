@@ -69,12 +69,15 @@ __device__ __forceinline__ float query_row(const __nv_bfloat16* q, bool valid, u
 __device__ __forceinline__ float weight_root(float ref, float u) { return exp2_approx(fminf(fmaf(ref - u, 0.5f, kHalfGain), 100.f)); }
 __device__ __forceinline__ float rest_root(float m, float u) { return u == -INFINITY ? 0.f : exp2_approx(fmaf(u - (m == -INFINITY ? 0.f : m), 0.5f, -kHalfGain)); }
 // What 2^(s - ref) is multiplied by, at most 2^126 in size: nothing is larger but what multiplies exponentials below 2^-111, in a
-// block whose scale is above 2^(119 + u - ref); NaN stays.
-__device__ __forceinline__ float block_weight(float root, float vs) {
+// block whose scale is above 2^(119 + u - ref); NaN stays.  plain_weight: where there is no such block.
+__device__ __forceinline__ float plain_weight(float root, float vs) { return root * vs * root; }
+__device__ __forceinline__ float at_most_2_126(float x) {
   float y;
-  asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(root * vs * root), "f"(0x1p126f));
+  asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(0x1p126f));
   return y;
 }
+__device__ __forceinline__ float block_weight(float root, float vs) { return at_most_2_126(plain_weight(root, vs)); }
+constexpr float kPlainRoom = -118.f;      // u - ref less a scale's log2: where plain_weight is finite
 
 // A row's references: m of the scores, with the sum l of 2^(s - m), and u of the numerators 2^(s - u) vs.  They are raised only when
 // something exceeds them by more than 2^kRaiseBy, which cancels in the end; all else goes by ref, m where that is finite.
@@ -100,8 +103,11 @@ struct RowState {
     w = u == -INFINITY ? 0.f : weight_root(ref, u);
     return f;
   }
-  // a largest s - ref that needs no raise, by the largest log2 |vs| of a stage
-  __device__ __forceinline__ float room(float lv) const { return m == -INFINITY ? -INFINITY : kRaiseBy + fminf(0.f, (u - lv) - ref); }
+  // what s - ref has to be below to need no raise, by the largest log2 |vs| of a stage; -infinity where plain_weight may not be finite
+  __device__ __forceinline__ float room(float lv) const {
+    const float x = (u - lv) - ref;
+    return m == -INFINITY || x < kPlainRoom ? -INFINITY : kRaiseBy + fminf(0.f, x);
+  }
   // the root of what the output is multiplied by at the end
   __device__ __forceinline__ float rest() const { return rest_root(m, u); }
 };

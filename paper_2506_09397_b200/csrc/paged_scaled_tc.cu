@@ -570,13 +570,18 @@ __global__ void __launch_bounds__(512, 1) scaled_tc_kernel(const PagedCache c, c
               if (!(see1 >> 16)) vs.w = 0.f;
             }
             const float ref = m == -INFINITY ? 0.f : m;
-            const float weight = weight_root(ref, top_u);
+            const float weight = top_u == -INFINITY ? 0.f : weight_root(ref, top_u);
+            float wx = vs.x, wy = vs.y, wz = vs.z, ww = vs.w;
+            mul2(wx, wy, weight);
+            mul2(wz, ww, weight);
+            mul2(wx, wy, weight);
+            mul2(wz, ww, weight);
             float mx = -INFINITY, mx_u = -INFINITY;      // of the scores, of those plus log2 |vs|
             sum0 = sum1 = 0.f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const float f = q == 0 ? by.x : q == 1 ? by.y : q == 2 ? by.z : by.w;
-              const float wb = top_u == -INFINITY ? 0.f : block_weight(weight, q == 0 ? vs.x : q == 1 ? vs.y : q == 2 ? vs.z : vs.w);
+              const float wb = at_most_2_126(q == 0 ? wx : q == 1 ? wy : q == 2 ? wz : ww);
               const float top = largest16(v + q * 16) * f;
               mx = fmaxf(mx, top);
               mx_u = fmaxf(mx_u, top + (q == 0 ? lv.x : q == 1 ? lv.y : q == 2 ? lv.z : lv.w));
