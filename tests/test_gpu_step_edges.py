@@ -135,6 +135,34 @@ def test_value_scales_of_any_size(power, hq, h):
         at += m
 
 
+@pytest.mark.parametrize("h", [32, 64, 128])
+@pytest.mark.parametrize("hq", [2, 12, 40, 200])
+@pytest.mark.parametrize("sharp", [0.0, 1.0, 8.0, 30.0])
+def test_value_scales_far_apart(sharp, hq, h):
+    """Value scales 2^-126 .. 2^100 and zeros, block by block, under scores from flat to far apart."""
+    lens, q_len = [200, 90, 700], [4, 1, 3]
+    kc, ks, vc, vs, table, n_kv = T._coded_cache(lens, 2, h, 16, 51, whole=True)
+    g = torch.Generator().manual_seed(52)
+    vs = torch.where(vs.isnan(), vs, torch.exp2(torch.randint(-126, 101, vs.shape, generator=g).float()))
+    vs = torch.where(torch.rand(vs.shape, generator=g) < 0.2, vs * 0, vs)
+    q = (torch.randn(sum(q_len), hq, h, generator=g) * sharp).to(BF)
+    out, lse = _run((kc, ks, vc, vs, table, n_kv), q_len, q)
+    at = 0
+    for i, (n, m) in enumerate(zip(lens, q_len)):
+        kk, vv = (R.keys_of(S.values(c, s), table[i], n, 16) for c, s in ((kc, ks), (vc, vs)))
+        o, l, p, d_o, d_l, _ = R.attend(q[at:at + m], kk, vv, R.tree_mask(None, m, n), h ** -0.5, BF)
+        wide = lambda x: x.abs().repeat_interleave(hq // 2, 0)
+        numerators = p * wide(R.keys_of(vs.double().repeat_interleave(16, -1), table[i], n, 16))
+        codes = wide(R.keys_of(vc.double(), table[i], n, 16))
+        # numerators are off by 2^-11 of each (in the bound with 2^-8), or by 2^-32 of the row's largest; a weight below 2^-111 of the
+        # largest may count as less
+        d_o += torch.einsum("mrn,rnd->mrd", (2.0 ** -32 * numerators.amax(-1, keepdim=True)).expand_as(p), codes)
+        d_o += torch.einsum("mrn,rnd->mrd", torch.where(p < 2.0 ** -111 * p.amax(-1, keepdim=True), p, 0), wide(vv))
+        assert bool(((out[at:at + m] - o).abs() <= d_o).all()), (i, float(((out[at:at + m] - o).abs() / d_o).max()))
+        assert bool(((lse[at:at + m] - l).abs() <= d_l).all())
+        at += m
+
+
 @pytest.mark.parametrize("hq", [2, 12, 40, 200])
 @pytest.mark.parametrize("gap", [60, 100, 118, 124, 131, 160, 400])
 def test_values_of_nothing_under_scores_far_above_the_others(gap, hq):
