@@ -454,7 +454,8 @@ typedef struct sled_heads {
  * (i, i + rot_dim/2) -, and pair i of row t is turned by the angle positions[t] * frequencies[i]:
  *   (a, b) -> amplitude (a cos - b sin, a sin + b cos);  dimensions behind rot_dim are copied.
  * transpose: the angle is taken negative, which is the gradient of the call without it (and, with amplitude 1, undoes it).
- * Angles are formed in 64 bits, whatever the position; a pair is turned in 32 bits and rounded once.
+ * Angles are formed in 64 bits, whatever the position: off by 3 2^-53 of their size, 2^-20.4 at 2^31.  A pair is turned in 32 bits
+ * and rounded once.
  *   dtype        SLED_F32 or SLED_BF16, of all of q and k;  k may be NULL
  *   positions    [n_rows], any numbers
  *   frequencies  [rot_dim/2] fp64
@@ -470,7 +471,8 @@ int sled_rotary(const sled_heads* q, const sled_heads* k, int32_t n_rows, int32_
  * v_scale [n_pages][n_kv_heads][page_size / 16] fp32: a key is scale * code.  The scale of a block that receives keys becomes
  * the smallest power of two, at least 2^-126, of which 448 times is no less than any new finite element of the block or, where
  * the block has older keys of the request, the size of the scale that it had, if that is larger; older keys are coded anew where it changes.  A code is
- * the nearest to element / scale, ties to the even one; infinities and NaN become NaN.  What a rejected draft did to a
+ * the nearest to element / scale, ties to the even one (a quotient by a caller's own scale that is no power of two is rounded to 32 bits
+ * first); infinities and NaN become NaN.  What a rejected draft did to a
  * scale stays until its block is begun anew.
  * Slots behind the last key and other pages are left as they are; the rows lie outside of the cache, and no two requests of a
  * call write into one page.  A request whose numbers do not hold together is left out, a

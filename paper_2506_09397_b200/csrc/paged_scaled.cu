@@ -24,9 +24,9 @@
 // nothing of each other until the end of the unit, and merge there.  A fifth warp (and a sixth) brings the stages in by TMA, their
 // scales with them, looked up a round ahead.  Work is handed out as paged_schedule.cuh says.
 //
-// Bound by the bytes of long caches - one token, 8 KV heads of 128: 4 x 131072 keys 170 us (6.3 TB/s), 32 x 8192 92 us (5.9),
-// 32 of 128 .. 16384 45 us; 16 rows: 4 x 131072 179 us (6.0) -, between 17 and 32 rows by conversions, products and exponentials
-// of two warps a stage (20 rows, 4 x 131072: 295 us), and by latency where there is little to read (one context of 64 keys 10.8 us,
+// Bound by the bytes of long caches - one token, 8 KV heads of 128: 4 x 131072 keys 172 us (6.2 TB/s), 32 x 8192 93 us (5.8),
+// 32 of 128 .. 16384 45 us; 16 rows: 4 x 131072 173 us (6.2) -, between 17 and 32 rows by conversions, products and exponentials
+// of two warps a stage (20 rows, 4 x 131072: 298 us), and by latency where there is little to read (one context of 64 keys 10.9 us,
 // of which the merge's launch is 3).
 #include "gemm_tc.h"
 #include "kernels.h"
@@ -686,7 +686,8 @@ int launch_paged_scaled(const PagedCache& c, const CacheScales& sc, const PagedR
   // read the keys several times - units of 8 against 32, 8 rows: 32 x 8192 keys 94, 98, 8 x 8192 34, 37, 64 x 300 26, 28; 12 rows:
   // 179, 98; 56, 37; 40, 29.  More than 32: the products of tcgen05, which take a unit of 128 rows in the time of one - units of
   // 32 against tcgen05, 32 rows: 32 x 4096 97, 128, 8 x 8192 58, 72, 64 x 300 38, 48; 36 rows: 151, 129; 93, 73; 61, 48.  (head_dim
-  // 32 has no kernel of that kind: its products would be half empty.)
+  // 32 has no kernel of that kind: its products would be half empty.)  What a batch has on average need not suit all of it: 31 single
+  // tokens over 512 .. 8192 keys 39 us, a chunk of 100 tokens over 2000 keys 27, both in one call 70; a chunk of 500 54, with them 126.
   const int64_t rows = static_cast<int64_t>(r.T) * r.group;
   if (c.h >= 64 && rows > 32LL * c.n_reqs) return launch_scaled_tc(c, sc, r, ws, s);
   const bool few = rows <= 8LL * c.n_reqs;

@@ -15,8 +15,8 @@
 // first tiles.  So a tile's exponentials are formed by the references that there are, beside the search for its largest scores, and
 // once more where those call for others.
 //
-// 64 trees of 48 - 64 nodes over 512 - 4096 keys, 8 KV heads of 128 for 32: 226 us; 512 rows over four contexts of 32768 keys 320 us
-// (860 TFLOP/s), 128 rows 122 us.  A 64-key tile of 256 rows takes about 2400 cycles: 1900 of them are a softmax warp's own (load of
+// 64 trees of 48 - 64 nodes over 512 - 4096 keys, 8 KV heads of 128 for 32: 226 us; 512 rows over four contexts of 32768 keys 321 us
+// (857 TFLOP/s), 128 rows 128 us.  A 64-key tile of 256 rows takes about 2400 cycles: 1900 of them are a softmax warp's own (load of
 // the scores 180, exponentials and maxima, vote, store and arrival 270, in one chain, two such warps on a scheduler), products
 // and their waits 1500 beside them, conversion 1150.  A unit costs about 17,000 cycles more (Q, first scores, last output, results
 // to memory), which is what short contexts pay.
@@ -787,7 +787,8 @@ int launch_scaled_tc(const PagedCache& c, const CacheScales& sc, const PagedRows
   // at it (head_dim 128, 8 KV heads; units of 128 against 256 rows, us): 132 rows, 64 x 300 keys 87, 69, 16 x 1000 49, 39, 20 x 2000
   // 103, 90, 8 x 8192 129, 105; 256 rows, 64 x 300 87, 77, 16 x 1000 50, 42, 20 x 2000 111, 107, 8 x 8192 135, 115 (64 x 1000, where
   // units of 256 do not share out as well: 153, 165).  With few tiles, or up to 128 rows, they lose: 132 rows, 8 x 1000 30, 34,
-  // 1 x 1000 23, 24, 1 x 4096 27, 32; 256 rows, 30, 42; 23, 31; 27, 40; 64 rows, 8 x 8192 75, 107, 64 x 300 50, 56.
+  // 1 x 1000 23, 24, 1 x 4096 27, 32; 256 rows, 30, 42; 23, 31; 27, 40; 64 rows, 8 x 8192 75, 107, 64 x 300 50, 56.  How many tiles there
+  // are the host knows only from the table's width: with columns for 131072 keys the calls with few tiles take the longer of their two.
   const int64_t rows = static_cast<int64_t>(r.T) * r.group / c.n_reqs, keys = static_cast<int64_t>(c.table_cols) * c.ps;
   const bool wide = rows > kGroupRows && (rows + kGroupRows - 1) / (2 * kGroupRows) * c.n_reqs * c.Hkv * ((keys + kKeys - 1) / kKeys) >= 12LL * sms;
   if (c.h == 128) return wide ? launch_h<128, 2>(c, sc, r, ws, s) : launch_h<128, 1>(c, sc, r, ws, s);

@@ -10,7 +10,7 @@
 // blocks.  A taken page that has just been returned is looked up where the returning request had it, not on the stack.
 //
 // Latency only: 64 requests with a few tokens each 4.2 us (lengths, sums, table, one behind the other), 300 prompts with 440,000
-// tokens 9.0 us (their 5 MB of results would take 0.8; two blocks an SM - with four, six 11.4, 9.9 -, five rows a thread).
+// tokens 8.8 us (their 5 MB of results would take 0.8; two blocks an SM - with four, six 11.4, 9.9 -, five rows a thread).
 #include "kernels.h"
 #include "paged_device.cuh"
 

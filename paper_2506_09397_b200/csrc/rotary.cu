@@ -2,7 +2,8 @@
 //
 //   (a, b) -> (a c - b s, a s + b c),   c, s = amplitude cos, sin of p f_i
 //
-// The angle is formed in fp64 and brought into (-1/2, 1/2] turns there, so that a far position costs nothing in accuracy; its
+// The angle is formed in fp64 and brought into (-1/2, 1/2] turns there.  It is off by 3 roundings, 3 2^-53 of its size: less than a pair's
+// rounding to 32 bits for angles up to 2^26, 2^-20.4 at 2^31.  Its
 // cosine and sine are taken in fp32 of the leading 24 bits and corrected by the rest (c - s d, s + c d, an angle d of less than 2^-23).
 // They are computed once per row and pair, into shared memory, and serve all heads of the row.
 //
