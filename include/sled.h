@@ -470,9 +470,9 @@ int sled_rotary(const sled_heads* q, const sled_heads* k, int32_t n_rows, int32_
  * A cache in 8 bits (SLED_E4M3) holds codes and a scale for every block of 16 slots of a page and KV head, k_scale and
  * v_scale [n_pages][n_kv_heads][page_size / 16] fp32: a key is scale * code.  The scale of a block that receives keys becomes
  * the smallest power of two, at least 2^-126, of which 448 times is no less than any new finite element of the block or, where
- * the block has older keys of the request, the size of the scale that it had, if that is larger; older keys are coded anew where it changes.  A code is
- * the nearest to element / scale, ties to the even one (a quotient by a caller's own scale that is no power of two is rounded to 32 bits
- * first); infinities and NaN become NaN.  What a rejected draft did to a
+ * the block has older keys of the request, the size of the scale that it had, if that is larger; older keys are coded anew where
+ * the scale changes.  A code is the nearest to element / scale, ties to the even one (a quotient by a caller's own scale that is no
+ * power of two is rounded to 32 bits first); infinities and NaN become NaN.  What a rejected draft did to a
  * scale stays until its block is begun anew.
  * Slots behind the last key and other pages are left as they are; the rows lie outside of the cache, and no two requests of a
  * call write into one page.  A request whose numbers do not hold together is left out, a
